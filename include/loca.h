@@ -472,6 +472,55 @@ int loca_calib_fit_rsvd(const float* E_probe, const float* G_probe, int64_t Np, 
                         float* P, float* Q, float* sigma, void* workspace, size_t workspace_bytes,
                         void* stream);
 
+/* ---------------------------------------------------------------------------------------------
+ * Operators around the pass: the head loss from hidden states, the adapted projection of many
+ * requests with its gradients, and gradient clipping.
+ * ------------------------------------------------------------------------------------------- */
+
+/*
+ * loca_head_loss — softmax cross entropy of hidden states against a large vocabulary head, with
+ * the label-column error of loca_error, without the logits in memory (Eq. 4; Lemma S3).
+ *
+ *   z = H W^T,   lse_n = log sum_v exp z[n, v],   loss_n = w_n (lse_n - z[n, y_n])
+ *   E[n, c] = w_n (exp(z[n, label_cols[c]] - lse_n) - [y_n == label_cols[c]])
+ *
+ * H           N x d bf16 hidden states, row pitch ldh elements (ldh >= d)
+ * W           V x d bf16 head, contiguous
+ * y           N int32 vocabulary indices; a label outside [0, V) (-1, -100) masks its position:
+ *             loss, lse and the row of E are 0, whatever H holds there
+ * w           N float weights, or NULL for all ones
+ * label_cols  C int32 vocabulary indices in [0, V), 1 <= C <= 1024; with E only (else NULL, C 0)
+ * loss        N float output;  lse  N float output, or NULL;  E  N x C float output, or NULL
+ * d a multiple of 8, ldh a multiple of 8, H and W 16-byte aligned (TMA); N, V <= 2^24, d <= 65536.
+ * Arithmetic: bf16 products on the tensor cores, fp32 sums restarted every 1024 terms, fp32
+ * exponentials and normalisers.  Deterministic.  Masked positions cost no product.
+ */
+int loca_head_loss_workspace_size(int64_t N, int64_t V, int64_t d, int32_t C, size_t* bytes);
+int loca_head_loss(const void* H, int64_t ldh, int64_t N, int64_t d, const void* W, int64_t V, const int32_t* y,
+                   const float* w, const int32_t* label_cols, int32_t C, float* loss, float* lse, float* E,
+                   void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * loca_head_loss_backward — gradients of  grad_scale * sum_n dloss_n loss_n  for the hidden states
+ * and the head, in pieces of the vocabulary.
+ *
+ *   dZ[n, v] = dloss_n w_n (exp(z[n, v] - lse_n) - [v == y_n])
+ *   dH = grad_scale dZ W  (N x d),   dW = grad_scale dZ^T H  (V x d)
+ *
+ * lse    N float, from loca_head_loss on the same H, W, y
+ * dloss  N float gradient of each position's loss, or NULL for ones
+ * dH     N x d bf16 output, row pitch lddh (a multiple of 8), or NULL; rows of masked positions are
+ *        0.  With unit weights it is the d-wide top error that loca_calib_fit_rsvd takes (in fp32)
+ * dW     V x d bf16 output, or NULL; at least one of dH and dW
+ * The logits are computed again; dZ is rounded to bf16 as an operand, sums are fp32, each gradient
+ * is rounded once.  Deterministic.  The workspace holds dZ of one piece of the vocabulary (up to
+ * 1 GiB, more for a dW over more than 2^19 positions) and the fp32 sums of dH.
+ */
+int loca_head_loss_backward_workspace_size(int64_t N, int64_t V, int64_t d, int want_dH, int want_dW, size_t* bytes);
+int loca_head_loss_backward(const void* H, int64_t ldh, int64_t N, int64_t d, const void* W, int64_t V,
+                            const int32_t* y, const float* w, const float* lse, const float* dloss, float grad_scale,
+                            void* dH, int64_t lddh, void* dW, void* workspace, size_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -1,0 +1,482 @@
+// Persistent CTA-pair matrix product on the sm_103a tensor cores, with the work on a finished
+// 256 x 256 tile left to the caller:  D[m, n] = sum_k A[m, k] B[n, k]   (bf16 in, fp32 sums).
+//
+// Used by the head loss (logit tiles that never leave the chip, and the two gradient products) and
+// by the adapter projection.  Each operand is K-major (k contiguous) or MN-major (m or n
+// contiguous); the tensor maps and the MMA descriptors carry the difference.
+//
+// Why this shape.  A pair of CTAs holds a 256 x 256 fp32 tile (128 rows per CTA: half of TMEM) and
+// loads 16 KB of A and 16 KB of B per CTA and 64-wide k-block, 64 bytes per tensor-core cycle and
+// SM, below the ~85 bytes per cycle the TMA ring takes from L2.  The other half of TMEM holds the
+// next tile, so the MMAs of a tile run while eight warps read the tile before it.
+//   warp 0       TMA producer (both CTAs): its CTA's 128 rows of A and 128 rows of B per k-block
+//   warp 1       one thread of the even CTA issues the MMAs (M = 256, N = 256, K = 16)
+//   warps 2..9   take the sums out of TMEM: warp w holds rows 32 (w & 3) .. + 31 of its CTA, one row
+//                per lane, and 128 of the 256 columns, in registers
+// Segments: the tensor cores' fp32 accumulation loses a fraction of an ulp of the running sum at
+// every step, always toward zero.  The sums restart every `seg_kb` k-blocks and the epilogue warps
+// add the segments in registers with round-to-nearest additions, which bounds that bias whatever K
+// is (a logit at K = 5120 comes out ~10x nearer to its 64-bit value than with one accumulator).
+// A segment is also the unit of the TMEM double buffer.
+// Every wait is bounded; the failure path is that of the Gram kernel: the first waiter that gives up
+// records LOCA_ERR_TIMEOUT and raises the launch's abort flag, every role stops at its own point,
+// the even CTA settles the copies that only one CTA issued, MMAs and copies in flight land, TMEM is
+// freed and both CTAs leave together.
+#pragma once
+
+#include <cuda.h>
+#include <cuda_bf16.h>
+
+#include "loca_internal.h"
+#include "tc_ptx.cuh"
+
+namespace loca {
+namespace gp {
+
+using namespace tc;
+
+constexpr int TM = 256;               // tile rows per CTA pair
+constexpr int TN = 256;               // tile columns
+constexpr int HALF = 128;             // rows of A, and of B, loaded per CTA
+constexpr int BK = 64;                // k per pipeline stage
+constexpr int STAGES = 6;
+constexpr int OPB = HALF * BK * 2;    // bytes of one operand of a stage (16 KB)
+constexpr int STAGE_BYTES = 2 * OPB;
+constexpr int SUB = 64 * BK * 2;      // one 64 x 64 swizzled box (8 KB)
+constexpr int EPI_WARPS = 8;
+constexpr int BOX = 4096;             // one epilogue warp's staging box: 32 rows x 128 bytes
+constexpr int THREADS = 64 + 32 * EPI_WARPS;
+constexpr int BARS = 2 * STAGES + 5;  // full[S], empty[S], acc_full[2], acc_empty[2], drain
+constexpr int SMEM = STAGES * STAGE_BYTES + EPI_WARPS * BOX + 256 + 1024;
+static_assert(SMEM <= 232448, "shared memory per CTA");
+static_assert(BARS * 8 + 8 <= 256, "barrier area");
+
+// One launch's work.  Tiles are taken in groups of `group` row tiles that sweep all column tiles,
+// row tile fastest: the CTA pairs at work share a few column tiles and one group of row tiles,
+// which stay in L2.
+struct Geo {
+  int m_tiles, n_tiles;  // upper bounds (rows_live may lower m_tiles, k_live the k-blocks)
+  int nkb;               // k-blocks of the product
+  int splits;            // the k-blocks are cut into this many ranges, each a tile of its own
+  int seg_kb;            // k-blocks per accumulation segment
+  int group;
+  int m_first;           // row tiles of rows_live that come before this launch's rows
+  const int32_t* rows_live;  // device count of rows of A that matter, or null
+  const int32_t* k_live;     // device count of k that matter, or null
+  int32_t* status;
+  int32_t* abort_flag;
+  unsigned long long limit_ns;
+};
+
+struct Tile {
+  int m, n, split;
+  int kb0, kb1;
+};
+
+struct Live {
+  int m_tiles, nkb, total;
+};
+
+__device__ __forceinline__ Live live_of(const Geo& g) {
+  Live v;
+  v.m_tiles = g.m_tiles;
+  v.nkb = g.nkb;
+  if (g.rows_live) {  // at least one row tile in all, so that a call with no live row still writes zeros
+    int t = (*g.rows_live + TM - 1) / TM;
+    if (t < 1) t = 1;
+    t -= g.m_first;
+    if (t < 0) t = 0;
+    if (t < v.m_tiles) v.m_tiles = t;
+  }
+  if (g.k_live) {
+    int t = (*g.k_live + BK - 1) / BK;
+    if (t < 1) t = 1;
+    if (t < v.nkb) v.nkb = t;
+  }
+  v.total = v.m_tiles * g.n_tiles * g.splits;
+  return v;
+}
+
+__device__ __forceinline__ Tile tile_of(const Geo& g, const Live& v, int it) {
+  Tile t;
+  const int per_split = v.m_tiles * g.n_tiles;
+  t.split = it / per_split;
+  int r = it - t.split * per_split;
+  const int per_group = g.group * g.n_tiles;
+  const int gi = r / per_group;
+  r -= gi * per_group;
+  const int m0 = gi * g.group;
+  const int gm = v.m_tiles - m0 < g.group ? v.m_tiles - m0 : g.group;
+  t.n = r / gm;
+  t.m = m0 + r - t.n * gm;
+  const int per = (v.nkb + g.splits - 1) / g.splits;
+  t.kb0 = t.split * per < v.nkb ? t.split * per : v.nkb;
+  t.kb1 = t.kb0 + per < v.nkb ? t.kb0 + per : v.nkb;
+  return t;
+}
+
+// Byte offset of 16-byte chunk `u` of row `row` in a 128-byte swizzled box.
+__device__ __forceinline__ uint32_t box_off(int row, int u) {
+  return uint32_t(row) * 128u + (uint32_t(u ^ (row & 7)) << 4);
+}
+
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
+  const __nv_bfloat162 p = __floats2bfloat162_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&p);
+}
+
+// Hands a warp's 32 rows x 64 bf16 columns (thread `lane` holds its row's values f(i), i < 64) to the
+// TMA unit as one box of a 2-D map at (c0, r0).  The box buffer's previous contents have been read
+// before it is written again.
+template <class F>
+__device__ __forceinline__ void store_box_bf16(uint8_t* box, const CUtensorMap* map, int lane, int c0, int r0, F&& f) {
+  if (lane == 0) bulk_wait_group_read0();
+  __syncwarp();
+#pragma unroll
+  for (int u = 0; u < 8; ++u) {
+    uint4 q;
+    q.x = pack_bf16(f(8 * u), f(8 * u + 1));
+    q.y = pack_bf16(f(8 * u + 2), f(8 * u + 3));
+    q.z = pack_bf16(f(8 * u + 4), f(8 * u + 5));
+    q.w = pack_bf16(f(8 * u + 6), f(8 * u + 7));
+    *reinterpret_cast<uint4*>(box + box_off(lane, u)) = q;
+  }
+  fence_proxy_async_smem();
+  __syncwarp();
+  if (lane == 0) {
+    if (LOCA_REQUIRE(c0 >= 0 && r0 >= 0 && c0 % 8 == 0)) tma_store_2d(map, smem_u32(box), c0, r0);
+    bulk_commit_group();
+  }
+}
+
+// Extension of the k axis: for row tile m, entries(m) further stages whose A rows come from the map
+// tmAx (row coordinate a_row of the CTA's 128 rows) and whose B rows from tmBx (b_row0 + the tile's
+// column, block b_block).  None here; the adapter projection has one.
+struct NoExt {
+  static constexpr bool kOn = false;
+  __device__ int entries(int) const { return 0; }
+  __device__ void entry(int, int, uint32_t, int&, int&) const {}
+};
+
+// Epi: struct with  void operator()(const Tile&, float (&v)[128], int row, int col0, int lane,
+//                                   uint8_t* box, const CUtensorMap* out) const
+// called once per finished tile by every epilogue thread, with the sums of row `row` (of the whole
+// operand A), columns col0 .. col0 + 127.
+template <bool kAmn, bool kBmn, class Epi, class Ext>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
+    k_gemm_pair(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB,
+                const __grid_constant__ CUtensorMap tmAx, const __grid_constant__ CUtensorMap tmBx,
+                const __grid_constant__ CUtensorMap tmO, const __grid_constant__ Geo g,
+                const __grid_constant__ Epi epi, const __grid_constant__ Ext ext) {
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  uint8_t* boxes = smem + STAGES * STAGE_BYTES;
+  uint64_t* bars = reinterpret_cast<uint64_t*>(boxes + EPI_WARPS * BOX);
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + BARS);
+  uint32_t* odd_issued = tmem_slot + 1;
+  const uint32_t smem_base = smem_u32(smem);
+  const uint32_t bar_base = smem_u32(bars);
+  auto full_bar = [&](int s) { return bar_base + 8u * s; };
+  auto empty_bar = [&](int s) { return bar_base + 8u * (STAGES + s); };
+  auto acc_full = [&](uint32_t b) { return bar_base + 8u * (2 * STAGES + b); };
+  auto acc_empty = [&](uint32_t b) { return bar_base + 8u * (2 * STAGES + 2 + b); };
+  const uint32_t drain_bar = bar_base + 8u * (2 * STAGES + 4);
+
+  const int warp = threadIdx.x >> 5;
+  const int lane = threadIdx.x & 31;
+  const uint32_t rank = cluster_ctarank();
+  const bool leader = rank == 0;
+  const int cid = int(cluster_id_x());
+  const int ncl = int(ncluster_x());
+  const WaitCtl wc{g.status, g.abort_flag, g.limit_ns};
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < STAGES; ++s) {
+      mbar_init(full_bar(s), 1);
+      mbar_init(empty_bar(s), 1);
+    }
+    for (uint32_t b = 0; b < 2; ++b) {
+      mbar_init(acc_full(b), 1);
+      mbar_init(acc_empty(b), 2 * EPI_WARPS);  // lane 0 of the epilogue warps of both CTAs
+    }
+    mbar_init(drain_bar, 1);
+    *odd_issued = 0;
+    mbar_init_fence();
+    prefetch_tensormap(&tmA);
+    prefetch_tensormap(&tmB);
+    prefetch_tensormap(&tmO);
+    if (Ext::kOn) {
+      prefetch_tensormap(&tmAx);
+      prefetch_tensormap(&tmBx);
+    }
+  }
+  if (warp == 1) tmem_alloc_pair(smem_u32(tmem_slot), 512);
+  fence_before();
+  cluster_sync();
+  fence_after();
+  const uint32_t tmem_base = *tmem_slot;
+  const Live lv = live_of(g);
+  uint32_t iters_done = 0;
+
+  if (warp == 0) {
+    if (lane == 0) {
+      // ---------------- TMA producer (both CTAs)
+      int stage = 0;
+      uint32_t phase = 0;
+      uint32_t iter = 0;
+      bool ok = true;
+      for (int it = cid; it < lv.total && ok; it += ncl) {
+        const Tile t = tile_of(g, lv, it);
+        const int m0 = t.m * TM + int(rank) * HALF;
+        const int n0 = t.n * TN + int(rank) * HALF;
+        const int nx = Ext::kOn ? ext.entries(t.m) : 0;
+        const int nb = t.kb1 - t.kb0;
+        for (int j = 0; j < nb + nx; ++j) {
+          if (!mbar_try_wait_cluster(empty_bar(stage), phase ^ 1u) &&
+              !mbar_wait_cluster(empty_bar(stage), phase ^ 1u, wc)) {
+            ok = false;
+            break;
+          }
+          if (leader) mbar_arrive_expect_tx(full_bar(stage), 2u * STAGE_BYTES);
+          const uint32_t fb = mapa_shared(full_bar(stage), 0);
+          const uint32_t a = smem_base + uint32_t(stage) * STAGE_BYTES;
+          const uint32_t b = a + OPB;
+          if (!Ext::kOn || j < nb) {
+            const int k0 = (t.kb0 + j) * BK;
+            if (kAmn) {
+              tma_load_2d_pair(a, &tmA, fb, m0, k0);
+              tma_load_2d_pair(a + SUB, &tmA, fb, m0 + 64, k0);
+            } else {
+              tma_load_2d_pair(a, &tmA, fb, k0, m0);
+            }
+            if (kBmn) {
+              tma_load_2d_pair(b, &tmB, fb, n0, k0);
+              tma_load_2d_pair(b + SUB, &tmB, fb, n0 + 64, k0);
+            } else {
+              tma_load_2d_pair(b, &tmB, fb, k0, n0);
+            }
+          } else {
+            int a_row, block;
+            ext.entry(t.m, j - nb, rank, a_row, block);
+            tma_load_2d_pair(a, &tmAx, fb, 0, a_row);
+            tma_load_3d_pair(b, &tmBx, fb, 0, n0, block);
+          }
+          ++iter;
+          if (++stage == STAGES) { stage = 0; phase ^= 1u; }
+        }
+      }
+      if (!leader) st_shared_cluster_u32(mapa_shared(smem_u32(odd_issued), 0), iter);
+      iters_done = iter;
+    }
+    __syncwarp();
+  } else if (warp == 1) {
+    if (lane == 0 && leader) {
+      // ---------------- MMA issuer (even CTA)
+      int stage = 0;
+      uint32_t phase = 0, seg = 0;
+      bool ok = true, issued = false;
+      constexpr uint32_t kKLbo = 16u;  // K-major with the 128-byte swizzle: leading offset unused
+      const uint64_t a_kmaj = sdesc(smem_base, kKLbo, 1024u, kSwizzle128B);
+      const uint64_t a0 = kAmn ? sdesc(smem_base, SUB, 1024u, kSwizzle128B) : a_kmaj;
+      const uint64_t b_kmaj = sdesc(smem_base + OPB, kKLbo, 1024u, kSwizzle128B);
+      const uint64_t b0 = kBmn ? sdesc(smem_base + OPB, SUB, 1024u, kSwizzle128B) : b_kmaj;
+      constexpr uint64_t kAStep = kAmn ? 2048 >> 4 : 32 >> 4, kBStep = kBmn ? 2048 >> 4 : 32 >> 4;
+      constexpr uint32_t kId = tc::idesc(1, 1, kAmn ? 1 : 0, kBmn ? 1 : 0, TM, TN);
+      constexpr uint32_t kIdX = tc::idesc(1, 1, 0, 0, TM, TN);
+      for (int it = cid; it < lv.total && ok; it += ncl) {
+        const Tile t = tile_of(g, lv, it);
+        const int nb = t.kb1 - t.kb0;
+        const int all = nb + (Ext::kOn ? ext.entries(t.m) : 0);
+        uint32_t d = 0;
+        for (int j = 0, in_seg = 0; j < all; ++j) {
+          if (in_seg == 0) {
+            const uint32_t b = seg & 1u;
+            if (!mbar_try_wait_cluster(acc_empty(b), ((seg >> 1) & 1u) ^ 1u) &&
+                !mbar_wait_cluster(acc_empty(b), ((seg >> 1) & 1u) ^ 1u, wc)) {
+              ok = false;
+              break;
+            }
+            d = tmem_base + b * uint32_t(TN);
+          }
+          if (!mbar_try_wait_cluster(full_bar(stage), phase) && !mbar_wait_cluster(full_bar(stage), phase, wc)) {
+            ok = false;
+            break;
+          }
+          fence_after();
+          const uint64_t so = uint64_t(stage) * uint64_t(STAGE_BYTES >> 4);
+          if (!Ext::kOn || j < nb) {
+#pragma unroll
+            for (int kk = 0; kk < BK / 16; ++kk)
+              mma_f16_pair(d, a0 + so + kk * kAStep, b0 + so + kk * kBStep, kId, (in_seg | kk) != 0 ? 1u : 0u);
+          } else {
+#pragma unroll
+            for (int kk = 0; kk < BK / 16; ++kk)
+              mma_f16_pair(d, a_kmaj + so + kk * 2, b_kmaj + so + kk * 2, kIdX, (in_seg | kk) != 0 ? 1u : 0u);
+          }
+          issued = true;
+          mma_commit_pair_mc(empty_bar(stage), 0x3);
+          if (++stage == STAGES) { stage = 0; phase ^= 1u; }
+          if (++in_seg == g.seg_kb || j == all - 1) {
+            mma_commit_pair_mc(acc_full(seg & 1u), 0x3);
+            ++seg;
+            in_seg = 0;
+          }
+        }
+      }
+      if (issued) {
+        mma_commit_pair(drain_bar);
+        mbar_drain(drain_bar, 0, kDrainLimitNs);
+      }
+    }
+    __syncwarp();
+  } else {
+    // ---------------- epilogue: warps 2..9; TMEM lane quarter = warp % 4, column half = (warp - 2) / 4
+    const int q = warp & 3;
+    const int h = (warp - 2) >> 2;
+    uint8_t* box = boxes + (warp - 2) * BOX;
+    uint32_t seg = 0;
+    bool go = true;
+    for (int it = cid; it < lv.total && go; it += ncl) {
+      const Tile t = tile_of(g, lv, it);
+      const int all = t.kb1 - t.kb0 + (Ext::kOn ? ext.entries(t.m) : 0);
+      const int nseg = (all + g.seg_kb - 1) / g.seg_kb;
+      float v[128];
+      if (nseg == 0) {
+#pragma unroll
+        for (int i = 0; i < 128; ++i) v[i] = 0.f;
+      }
+      for (int s = 0; s < nseg; ++s, ++seg) {
+        const uint32_t b = seg & 1u;
+        const bool ok = mbar_wait_cluster(acc_full(b), (seg >> 1) & 1u, wc);
+        if (!__all_sync(0xffffffffu, ok)) {
+          go = false;
+          break;
+        }
+        fence_after();
+        const uint32_t ta = tmem_base + (uint32_t(q * 32) << 16) + b * uint32_t(TN) + uint32_t(h * 128);
+        if (s == 0) {
+#pragma unroll
+          for (int c = 0; c < 4; ++c) tmem_ld32(ta + c * 32, v + c * 32);
+        } else {
+#pragma unroll
+          for (int c = 0; c < 4; ++c) {
+            float u[32];
+            tmem_ld32(ta + c * 32, u);
+#pragma unroll
+            for (int i = 0; i < 32; ++i) v[c * 32 + i] += u[i];
+          }
+        }
+        fence_before();
+        __syncwarp();
+        if (lane == 0) {
+          if (leader) mbar_arrive(acc_empty(b));
+          else mbar_arrive_remote(mapa_shared(acc_empty(b), 0));
+        }
+      }
+      if (!go) break;
+      epi(t, v, t.m * TM + int(rank) * HALF + q * 32 + lane, t.n * TN + h * 128, lane, box, &tmO);
+    }
+    if (lane == 0) bulk_wait_group0();  // every box written before the CTA can leave
+    __syncwarp();
+  }
+
+  fence_before();
+  cluster_sync();  // every role has stopped; the odd CTA's issue count is visible
+  fence_after();
+  if (warp == 0 && lane == 0 && leader) {
+    // Copies in flight when a role gave up: every stage carries the same bytes.  An iteration the
+    // odd CTA never issued gets its bytes settled, one only the odd CTA issued gets armed, and each
+    // of the last STAGES iterations is waited for (the earlier ones have landed).
+    const uint32_t n_even = iters_done;
+    const uint32_t n_odd = *reinterpret_cast<volatile uint32_t*>(odd_issued);
+    const uint32_t hi = n_even > n_odd ? n_even : n_odd;
+    const uint32_t lo = hi > uint32_t(STAGES) ? hi - uint32_t(STAGES) : 0u;
+    for (uint32_t i = lo; i < hi; ++i) {
+      const int s = int(i % STAGES);
+      if (i >= n_odd && i < n_even) mbar_complete_tx(full_bar(s), STAGE_BYTES);
+      else if (i >= n_even && i < n_odd) mbar_arrive_expect_tx(full_bar(s), STAGE_BYTES);
+      mbar_drain(full_bar(s), (i / STAGES) & 1u, kDrainLimitNs);
+    }
+  }
+  fence_before();
+  cluster_sync();
+  fence_after();
+  if (warp == 1) tmem_dealloc_pair(tmem_base, 512);
+}
+
+// ------------------------------------------------------------------ host side
+// 2-D map of a row-major matrix: `cols` contiguous elements, `rows` rows, pitch in elements.
+inline bool map_2d(CUtensorMap* m, CUtensorMapDataType type, int esize, const void* base, int64_t cols, int64_t rows,
+                   int64_t pitch, int box_cols, int box_rows) {
+  auto fn = tensor_map_encoder();
+  if (!fn) return false;
+  cuuint64_t dims[2] = {cuuint64_t(cols), cuuint64_t(rows)};
+  cuuint64_t strides[1] = {cuuint64_t(pitch) * esize};
+  cuuint32_t box[2] = {cuuint32_t(box_cols), cuuint32_t(box_rows)};
+  cuuint32_t estr[2] = {1, 1};
+  return fn(m, type, 2, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+            CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+inline bool map_3d(CUtensorMap* m, CUtensorMapDataType type, int esize, const void* base, int64_t cols, int64_t rows,
+                   int64_t blocks, int64_t pitch, int64_t block_pitch, int box_cols, int box_rows) {
+  auto fn = tensor_map_encoder();
+  if (!fn) return false;
+  cuuint64_t dims[3] = {cuuint64_t(cols), cuuint64_t(rows), cuuint64_t(blocks)};
+  cuuint64_t strides[2] = {cuuint64_t(pitch) * esize, cuuint64_t(block_pitch) * esize};
+  cuuint32_t box[3] = {cuuint32_t(box_cols), cuuint32_t(box_rows), 1};
+  cuuint32_t estr[3] = {1, 1, 1};
+  return fn(m, type, 3, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+            CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+// An operand whose k is contiguous: boxes of 64 k x 128 rows.
+inline bool map_kmajor(CUtensorMap* m, const void* base, int64_t k, int64_t rows, int64_t pitch) {
+  return map_2d(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, base, k, rows, pitch, BK, HALF);
+}
+// An operand whose rows (m or n) are contiguous: boxes of 64 rows x 64 k.
+inline bool map_mnmajor(CUtensorMap* m, const void* base, int64_t rows, int64_t k, int64_t pitch) {
+  return map_2d(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, base, rows, k, pitch, 64, BK);
+}
+// A bf16 output written in boxes of 64 columns x 32 rows.
+inline bool map_out_bf16(CUtensorMap* m, void* base, int64_t cols, int64_t rows, int64_t pitch) {
+  return map_2d(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, base, cols, rows, pitch, 64, 32);
+}
+
+// Pairs of CTAs that can be resident at once (76 on 152 SMs).
+template <class K>
+inline int resident_pairs(K kernel) {
+  int clusters = sm_count() / 2;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(unsigned(2 * clusters));
+  cfg.blockDim = dim3(THREADS);
+  cfg.dynamicSmemBytes = SMEM;
+  cudaLaunchAttribute at[1];
+  at[0].id = cudaLaunchAttributeClusterDimension;
+  at[0].val.clusterDim.x = 2;
+  at[0].val.clusterDim.y = 1;
+  at[0].val.clusterDim.z = 1;
+  cfg.attrs = at;
+  cfg.numAttrs = 1;
+  int n = 0;
+  if (cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) == cudaSuccess && n > 0 && n < clusters) clusters = n;
+  cudaGetLastError();
+  return clusters;
+}
+
+template <bool kAmn, bool kBmn, class Epi, class Ext>
+inline cudaError_t launch(const CUtensorMap& a, const CUtensorMap& b, const CUtensorMap& ax, const CUtensorMap& bx,
+                          const CUtensorMap& o, const Geo& g, const Epi& epi, const Ext& ext, cudaStream_t s) {
+  auto kernel = k_gemm_pair<kAmn, kBmn, Epi, Ext>;
+  cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM);
+  if (e != cudaSuccess) return e;
+  static const int pairs = resident_pairs(kernel);
+  const int64_t total = int64_t(g.m_tiles) * g.n_tiles * g.splits;
+  if (total < 1) return cudaSuccess;
+  const int n = total < pairs ? int(total) : pairs;
+  kernel<<<2 * n, THREADS, SMEM, s>>>(a, b, ax, bx, o, g, epi, ext);
+  return cudaGetLastError();
+}
+
+}  // namespace gp
+}  // namespace loca

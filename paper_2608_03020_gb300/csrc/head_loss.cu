@@ -1,0 +1,578 @@
+// Head loss over a large vocabulary without the logits in memory, and its gradients.
+//   z = H W^T,  lse_n = log sum_v exp z_nv,  loss_n = w_n (lse_n - z_{n, y_n})      (masked: 0)
+//   E[n, c] = w_n (exp(z_{n, l_c} - lse_n) - [y_n = l_c])      the label-column error of Eq. 4
+//   dZ = g_n w_n (exp(z - lse) - [v = y_n]),  dH = scale dZ W,  dW = scale dZ^T H
+// dH is the d-wide top error W_u^T eps of the one-shot calibration (Eq. 5).
+//
+// k_head_rows    the rows whose label is in range, one after the other (their hidden states copied,
+//                zero rows up to the next tile): masked rows cost no product, and whatever stands
+//                in them (infinities, NaN) reaches neither another row nor dW
+// k_gemm_pair    logit tiles (256 x 256) on the tensor cores.  Forward: each epilogue thread has 128
+//                logits of one row in registers and writes their maximum and sum of exponentials,
+//                plus the target's and the label words' logits where its columns hold them.
+//                Backward: the same tiles again, turned into dZ = g w (p - onehot), rounded to bf16
+//                as the operand of the two gradient products, for one piece of the vocabulary at a
+//                time (a bf16 operand moves a sum of many such products by less than the gradients'
+//                own rounding to bf16; the factor `scale` is applied to the fp32 sums, so it
+//                rounds nothing)
+// k_head_join    combines a row's maxima and sums in a fixed order: lse, loss, E
+// k_head_dh      sums the k ranges of dH, scales, rounds once and puts each row back in its place
+// Computing the logits a second time costs 2 N d V operations; keeping them would cost 4 N V bytes
+// (2.5 GB per 4096 tokens at V = 151936).
+#include <cuda_bf16.h>
+#include <cuda_runtime.h>
+
+#include <cstring>
+
+#include "gemm_pair.cuh"
+
+namespace loca {
+namespace {
+
+using namespace tc;
+
+constexpr float kLog2e = 1.4426950408889634f;
+
+constexpr int kRowsPerBlock = 32;
+constexpr int kPadBlocks = 16;         // blocks of k_head_rows that write the zero rows
+constexpr int64_t kFwdRows = 16384;    // rows per forward piece (bounds the partial maxima and sums)
+constexpr int64_t kBwdRows = 8192;     // rows per backward piece when dW is not wanted
+constexpr int64_t kDzBytes = int64_t(1) << 30;  // dZ of one piece of the vocabulary
+constexpr int kSegKb = 16;             // logits: 1024 k per accumulation segment
+constexpr int kSegKbGrad = 64;         // gradients (rounded to bf16): 4096 k per segment
+
+// e^(a - b).  The difference is taken first, so that a probability of one comes out as one and large
+// logits lose nothing to the scaling.
+__device__ __forceinline__ float exp_diff(float a, float b) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"((a - b) * kLog2e));
+  return y;
+}
+
+struct Rows {
+  int32_t* abort_flag;
+  int32_t* count;   // rows with a label in [0, V)
+  int32_t* idx;     // their places in the call's order
+  int32_t* y;       // their labels (-1 in the padding)
+  float* w;         // their weights (0 in the padding)
+  float* lse;       // backward: their normalisers
+  __nv_bfloat16* H; // their hidden states, then zero rows up to a multiple of 256
+};
+
+__device__ __forceinline__ bool live_label(int32_t y, int64_t V) { return y >= 0 && y < V; }
+
+// Live labels among y[0 .. n), counted by the whole block.
+__device__ int count_live(const int32_t* __restrict__ y, int64_t n, int64_t V, int* scratch) {
+  int c = 0;
+  for (int64_t i = threadIdx.x; i < n; i += blockDim.x) c += live_label(y[i], V) ? 1 : 0;
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) c += __shfl_xor_sync(0xffffffffu, c, o);
+  __syncthreads();
+  if ((threadIdx.x & 31) == 0) scratch[threadIdx.x >> 5] = c;
+  __syncthreads();
+  int sum = 0;
+  for (int i = 0; i < int(blockDim.x >> 5); ++i) sum += scratch[i];
+  return sum;
+}
+
+// Blocks 0 .. nb - 1 take kRowsPerBlock source rows each: the live ones move to their place among the
+// live rows, the others' outputs are zeroed.  The last kPadBlocks blocks write the zero rows behind.
+// Bound: reads and writes 2 N d bytes each way; every block counts the labels before its own rows
+// (4 N bytes from L2), which keeps the pass one launch without a scan.
+__global__ void __launch_bounds__(256)
+    k_head_rows(const __nv_bfloat16* __restrict__ H, int64_t ldh, int64_t N, int64_t d, int64_t V,
+                const int32_t* __restrict__ y, const float* __restrict__ w, const float* __restrict__ dloss,
+                const float* __restrict__ lse, Rows out, int64_t npad, int nb, float* loss0, float* lse0, float* E0,
+                int C, __nv_bfloat16* dH0, int64_t lddh) {
+  __shared__ int scratch[8];
+  __shared__ int place[kRowsPerBlock];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int64_t dv = d / 8;  // 16-byte vectors of a row
+  if (blockIdx.x == 0 && threadIdx.x == 0) *out.abort_flag = 0;
+  if (int(blockIdx.x) >= nb) {
+    const int64_t total = count_live(y, N, V, scratch);
+    if (int(blockIdx.x) == nb && threadIdx.x == 0) *out.count = int32_t(total);
+    int64_t end = (total + gp::TM - 1) / gp::TM * gp::TM;
+    if (end < gp::TM) end = gp::TM;
+    for (int64_t r = total + (blockIdx.x - nb) * 8 + warp; r < end; r += kPadBlocks * 8) {
+      if (!LOCA_CHECK(r, npad)) break;
+      uint4* dst = reinterpret_cast<uint4*>(out.H + r * d);
+      for (int64_t i = lane; i < dv; i += 32) dst[i] = make_uint4(0, 0, 0, 0);
+      if (lane == 0) {
+        out.idx[r] = -1;
+        out.y[r] = -1;
+        out.w[r] = 0.f;
+        if (lse) out.lse[r] = 0.f;
+      }
+    }
+    return;
+  }
+  const int64_t r0 = int64_t(blockIdx.x) * kRowsPerBlock;
+  const int base = count_live(y, r0, V, scratch);
+  if (warp == 0) {
+    const int64_t n = r0 + lane;
+    const int32_t yn = n < N ? y[n] : -1;
+    const bool live = live_label(yn, V);
+    const unsigned all = __ballot_sync(0xffffffffu, live);
+    const int p = live ? base + __popc(all & ((1u << lane) - 1u)) : -1;
+    place[lane] = p;
+    if (live && LOCA_CHECK(p, npad)) {
+      out.idx[p] = int32_t(n);
+      out.y[p] = yn;
+      out.w[p] = (w ? w[n] : 1.f) * (dloss ? dloss[n] : 1.f);
+      if (lse) out.lse[p] = lse[n];
+    }
+  }
+  __syncthreads();
+  for (int i = warp; i < kRowsPerBlock; i += 8) {
+    const int64_t n = r0 + i;
+    if (n >= N) break;
+    const int p = place[i];
+    if (p >= 0) {
+      const uint4* src = reinterpret_cast<const uint4*>(H + n * ldh);
+      uint4* dst = reinterpret_cast<uint4*>(out.H + int64_t(p) * d);
+      for (int64_t j = lane; j < dv; j += 32) dst[j] = src[j];
+    } else {
+      if (lane == 0 && loss0) loss0[n] = 0.f;
+      if (lane == 0 && lse0) lse0[n] = 0.f;
+      if (E0)
+        for (int c = lane; c < C; c += 32) E0[n * C + c] = 0.f;
+      if (dH0) {
+        uint4* z = reinterpret_cast<uint4*>(dH0 + n * lddh);
+        for (int64_t j = lane; j < dv; j += 32) z[j] = make_uint4(0, 0, 0, 0);
+      }
+    }
+  }
+}
+
+// ------------------------------------------------------------------ epilogues of the logit tiles
+// Forward: maximum and sum of exponentials of 128 logits of a row.
+struct EpiStats {
+  float2* part;        // (2 column tiles) x pitch
+  int64_t pitch;       // rows of a piece
+  const int32_t* y;    // this piece's rows
+  float* zy;           // the target's logit
+  const int32_t* cols; // label words
+  int C;
+  float* zc;           // C x pitch: the label words' logits
+  int64_t V;
+
+  __device__ __forceinline__ void operator()(const gp::Tile& t, float (&v)[128], int row, int col0, int lane, uint8_t*,
+                                             const CUtensorMap*) const {
+    if (!LOCA_CHECK(row, pitch)) return;
+    const int left = int(V - col0 < 128 ? V - col0 : 128);  // columns of the vocabulary among these
+    if (left < 128) {
+#pragma unroll
+      for (int i = 0; i < 128; ++i)
+        if (i >= left) v[i] = -INFINITY;
+    }
+    float m0 = v[0], m1 = v[1], m2 = v[2], m3 = v[3];
+#pragma unroll
+    for (int i = 4; i < 128; i += 4) {
+      m0 = fmaxf(m0, v[i]);
+      m1 = fmaxf(m1, v[i + 1]);
+      m2 = fmaxf(m2, v[i + 2]);
+      m3 = fmaxf(m3, v[i + 3]);
+    }
+    const float m = fmaxf(fmaxf(m0, m1), fmaxf(m2, m3));
+    float s0 = 0.f, s1 = 0.f, s2 = 0.f, s3 = 0.f;
+    if (left > 0 && m != -INFINITY) {
+#pragma unroll
+      for (int i = 0; i < 128; i += 4) {
+        s0 += exp_diff(v[i], m);
+        s1 += exp_diff(v[i + 1], m);
+        s2 += exp_diff(v[i + 2], m);
+        s3 += exp_diff(v[i + 3], m);
+      }
+    }
+    part[int64_t(col0 / 128) * pitch + row] = make_float2(m, (s0 + s1) + (s2 + s3));
+    const int at = y[row] - col0;
+    if (__any_sync(0xffffffffu, at >= 0 && at < left)) {
+#pragma unroll
+      for (int i = 0; i < 128; ++i)
+        if (i == at) zy[row] = v[i];
+    }
+    for (int c0 = 0; c0 < C; c0 += 32) {
+      const int col = c0 + lane < C ? cols[c0 + lane] - col0 : -1;
+      unsigned here = __ballot_sync(0xffffffffu, col >= 0 && col < left);
+      while (here) {
+        const int b = __ffs(here) - 1;
+        here &= here - 1;
+        const int j = __shfl_sync(0xffffffffu, col, b);
+        float z = 0.f;
+#pragma unroll
+        for (int i = 0; i < 128; ++i)
+          if (i == j) z = v[i];
+        zc[int64_t(c0 + b) * pitch + row] = z;
+      }
+    }
+  }
+};
+
+// Backward: dZ = g w (p - onehot) of the same tile, bf16, for the gradient products.  Columns past
+// the vocabulary and rows past the live ones are zero.
+struct EpiDz {
+  const float* lse;
+  const float* w;      // w_n dloss_n
+  const int32_t* y;
+  const int32_t* count;
+  int64_t row_first;   // this piece's first row among the live rows
+  int64_t v_first;     // this piece's first vocabulary column
+  int64_t v_end;       // end of the vocabulary
+
+  __device__ __forceinline__ void operator()(const gp::Tile&, float (&v)[128], int row, int col0, int lane, uint8_t* box,
+                                             const CUtensorMap* out) const {
+    const bool live = row_first + row < *count;
+    const float l = lse[row];
+    const float g = live ? w[row] : 0.f;
+    const int64_t vc = v_first + col0;
+    const int left = int(v_end - vc < 128 ? v_end - vc : 128);
+    const int64_t at64 = int64_t(y[row]) - vc;
+    const int at = at64 >= 0 && at64 < 128 ? int(at64) : -1;
+#pragma unroll
+    for (int i = 0; i < 128; ++i) {
+      const float p = exp_diff(v[i], l) - (i == at ? 1.f : 0.f);
+      v[i] = live && i < left ? g * p : 0.f;
+    }
+    const int r0 = row - lane;
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
+      gp::store_box_bf16(box, out, lane, col0 + 64 * b, r0, [&](int i) { return v[64 * b + i]; });
+  }
+};
+
+// dH: fp32 sums of one k range, stored or added to the sums of the earlier pieces of the vocabulary
+// (one writer per element and launch: a fixed order of additions).
+struct EpiAcc {
+  int64_t rows;  // rows of one split's sums
+  int add;
+
+  __device__ __forceinline__ void operator()(const gp::Tile& t, float (&v)[128], int row, int col0, int lane, uint8_t* box,
+                                             const CUtensorMap* out) const {
+    const int r0 = row - lane;
+    if (r0 >= rows) return;
+#pragma unroll
+    for (int b = 0; b < 4; ++b) {
+      if (lane == 0) bulk_wait_group_read0();
+      __syncwarp();
+#pragma unroll
+      for (int u = 0; u < 8; ++u)
+        *reinterpret_cast<float4*>(box + gp::box_off(lane, u)) =
+            make_float4(v[32 * b + 4 * u], v[32 * b + 4 * u + 1], v[32 * b + 4 * u + 2], v[32 * b + 4 * u + 3]);
+      fence_proxy_async_smem();
+      __syncwarp();
+      if (lane == 0) {
+        if (LOCA_REQUIRE(col0 >= 0 && r0 >= 0)) {
+          if (add) tma_reduce_add_3d(out, smem_u32(box), col0 + 32 * b, r0, t.split);
+          else tma_store_3d(out, smem_u32(box), col0 + 32 * b, r0, t.split);
+        }
+        bulk_commit_group();
+      }
+    }
+  }
+};
+
+// dW: scaled and rounded once.
+struct EpiScaled {
+  float scale;
+
+  __device__ __forceinline__ void operator()(const gp::Tile&, float (&v)[128], int row, int col0, int lane, uint8_t* box,
+                                             const CUtensorMap* out) const {
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
+      gp::store_box_bf16(box, out, lane, col0 + 64 * b, row - lane, [&](int i) { return scale * v[64 * b + i]; });
+  }
+};
+
+// ------------------------------------------------------------------ joins
+// 32 rows per block, `blockDim.y` groups of partial maxima and sums.
+__global__ void __launch_bounds__(1024)
+    k_head_join(const float2* __restrict__ part, int64_t pitch, int nparts, Rows in, int64_t row_first,
+                const float* __restrict__ zy, const float* __restrict__ zc, const int32_t* __restrict__ cols, int C,
+                float* __restrict__ loss, float* __restrict__ lse, float* __restrict__ E) {
+  __shared__ float2 sh[32][33];
+  const int64_t row = int64_t(blockIdx.x) * 32 + threadIdx.x;
+  const bool live = row_first + row < *in.count;
+  float m = -INFINITY, s = 0.f;
+  if (live) {
+    for (int p = threadIdx.y; p < nparts; p += blockDim.y) {
+      const float2 q = part[int64_t(p) * pitch + row];
+      const float mm = fmaxf(m, q.x);
+      if (mm != -INFINITY) s = s * exp_diff(m, mm) + q.y * exp_diff(q.x, mm);
+      else s += q.y;  // keeps a NaN
+      m = mm;
+    }
+  }
+  sh[threadIdx.y][threadIdx.x] = make_float2(m, s);
+  __syncthreads();
+  if (threadIdx.y != 0 || !live) return;
+  for (int j = 1; j < int(blockDim.y); ++j) {
+    const float2 q = sh[j][threadIdx.x];
+    const float mm = fmaxf(m, q.x);
+    if (mm != -INFINITY) s = s * exp_diff(m, mm) + q.y * exp_diff(q.x, mm);
+    else s += q.y;
+    m = mm;
+  }
+  const float l = m + logf(s);
+  const int64_t k = row_first + row;
+  const int32_t n = in.idx[k];
+  const float w = in.w[k];
+  loss[n] = w * (l - zy[row]);
+  if (lse) lse[n] = l;
+  if (E) {
+    const int32_t y = in.y[k];
+    for (int c = 0; c < C; ++c)
+      E[int64_t(n) * C + c] = w * (exp_diff(zc[int64_t(c) * pitch + row], l) - (cols[c] == y ? 1.f : 0.f));
+  }
+}
+
+__global__ void __launch_bounds__(256)
+    k_head_dh(const float* __restrict__ part, int64_t rows, int splits, int64_t d, Rows in, int64_t row_first,
+              float scale, __nv_bfloat16* __restrict__ dH, int64_t lddh) {
+  const int64_t dv = d / 8;
+  const int64_t row = int64_t(blockIdx.x);
+  if (row_first + row >= *in.count) return;
+  const int64_t n = in.idx[row_first + row];
+  for (int64_t j = threadIdx.x; j < dv; j += blockDim.x) {
+    float a[8] = {};
+    for (int s = 0; s < splits; ++s) {
+      const float4* p = reinterpret_cast<const float4*>(part + (int64_t(s) * rows + row) * d + 8 * j);
+      const float4 x = p[0], z = p[1];
+      a[0] += x.x; a[1] += x.y; a[2] += x.z; a[3] += x.w;
+      a[4] += z.x; a[5] += z.y; a[6] += z.z; a[7] += z.w;
+    }
+    uint4 q;
+    q.x = gp::pack_bf16(scale * a[0], scale * a[1]);
+    q.y = gp::pack_bf16(scale * a[2], scale * a[3]);
+    q.z = gp::pack_bf16(scale * a[4], scale * a[5]);
+    q.w = gp::pack_bf16(scale * a[6], scale * a[7]);
+    *reinterpret_cast<uint4*>(dH + n * lddh + 8 * j) = q;
+  }
+}
+
+// ------------------------------------------------------------------ host side
+int64_t round_up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
+
+struct RowsWs {
+  size_t flags, idx, y, w, lse, H, total;
+};
+RowsWs rows_ws(int64_t N, int64_t d) {
+  const size_t np = size_t(round_up(N < 1 ? 1 : N, gp::TM));
+  RowsWs o{};
+  size_t at = 0;
+  o.flags = at; at += 256;
+  o.idx = at; at += align256(4 * np);
+  o.y = at; at += align256(4 * np);
+  o.w = at; at += align256(4 * np);
+  o.lse = at; at += align256(4 * np);
+  o.H = at; at += align256(2 * np * size_t(d));
+  o.total = at;
+  return o;
+}
+Rows rows_at(void* ws, const RowsWs& o) {
+  uint8_t* b = static_cast<uint8_t*>(ws);
+  Rows r;
+  r.abort_flag = reinterpret_cast<int32_t*>(b + o.flags);
+  r.count = r.abort_flag + 1;
+  r.idx = reinterpret_cast<int32_t*>(b + o.idx);
+  r.y = reinterpret_cast<int32_t*>(b + o.y);
+  r.w = reinterpret_cast<float*>(b + o.w);
+  r.lse = reinterpret_cast<float*>(b + o.lse);
+  r.H = reinterpret_cast<__nv_bfloat16*>(b + o.H);
+  return r;
+}
+
+struct FwdWs {
+  RowsWs rows;
+  int64_t piece;
+  size_t part, zy, zc, total;
+};
+FwdWs fwd_ws(int64_t N, int64_t V, int64_t d, int C) {
+  FwdWs o{};
+  o.rows = rows_ws(N, d);
+  const int64_t np = round_up(N < 1 ? 1 : N, gp::TM);
+  o.piece = np < kFwdRows ? np : kFwdRows;
+  const size_t nparts = 2 * size_t((V + gp::TN - 1) / gp::TN);
+  size_t at = o.rows.total;
+  o.part = at; at += align256(nparts * size_t(o.piece) * sizeof(float2));
+  o.zy = at; at += align256(4 * size_t(o.piece));
+  o.zc = at; at += align256(4 * size_t(o.piece) * size_t(C));
+  o.total = at;
+  return o;
+}
+
+struct BwdWs {
+  RowsWs rows;
+  int64_t piece;  // rows of dZ
+  int64_t vc;     // vocabulary columns of dZ (a multiple of 256)
+  int splits;     // k ranges of dH
+  size_t dz, part, total;
+};
+// k ranges of the dH product: its tiles (rows / 256 x d / 256) are few, so one range per tile would
+// leave the last wave of CTA pairs mostly idle.  More ranges fill it and cost 8 bytes per element
+// and range (written, then read by k_head_dh).  Both sides of the choice in tensor-core cycles.
+int dh_splits(int64_t rows, int64_t d, int64_t vc) {
+  const int64_t pairs = sm_count() / 2;
+  const int64_t tiles = (rows / gp::TM) * ((d + gp::TN - 1) / gp::TN);
+  const double nkb = double(vc) / gp::BK;
+  int best = 1;
+  double best_c = 0;
+  for (int s = 1; s <= 8; ++s) {
+    if (s > 1 && nkb / s < 16) break;
+    const double waves = double((tiles * s + pairs - 1) / pairs);
+    const double c = waves * (nkb / s * 512.0 + 2000.0) + double(s) * double(rows) * double(d) * 8.0 / 3000.0;
+    if (s == 1 || c < best_c) {
+      best = s;
+      best_c = c;
+    }
+  }
+  return best;
+}
+BwdWs bwd_ws(int64_t N, int64_t V, int64_t d, bool dh, bool dw) {
+  BwdWs o{};
+  o.rows = rows_ws(N, d);
+  const int64_t np = round_up(N < 1 ? 1 : N, gp::TM);
+  o.piece = dw || np < kBwdRows ? np : kBwdRows;
+  const int64_t vp = round_up(V, gp::TN);
+  int64_t vc = kDzBytes / (2 * o.piece) / gp::TN * gp::TN;
+  if (vc < 4 * gp::TN) vc = 4 * gp::TN;
+  if (vc > vp) vc = vp;
+  const int64_t chunks = (vp + vc - 1) / vc;
+  o.vc = round_up((vp + chunks - 1) / chunks, gp::TN);
+  o.splits = dh ? dh_splits(o.piece, d, o.vc) : 0;
+  size_t at = o.rows.total;
+  o.dz = at; at += align256(2 * size_t(o.piece) * size_t(o.vc));
+  o.part = at; at += align256(4 * size_t(o.splits) * size_t(o.piece) * size_t(d));
+  o.total = at;
+  return o;
+}
+
+gp::Geo geo(int64_t m_tiles, int64_t n_tiles, int64_t nkb, int seg_kb, const Rows& r, int32_t* status) {
+  gp::Geo g{};
+  g.m_tiles = int(m_tiles);
+  g.n_tiles = int(n_tiles);
+  g.nkb = int(nkb);
+  g.splits = 1;
+  g.seg_kb = seg_kb;
+  g.group = 16;
+  g.status = status;
+  g.abort_flag = r.abort_flag;
+  g.limit_ns = wait_limit_ns();
+  return g;
+}
+
+cudaError_t launch_rows(const void* H, int64_t ldh, int64_t N, int64_t d, int64_t V, const int32_t* y, const float* w,
+                        const float* dloss, const float* lse, const Rows& r, float* loss0, float* lse0, float* E0, int C,
+                        void* dH0, int64_t lddh, cudaStream_t s) {
+  const int64_t nb = (N + kRowsPerBlock - 1) / kRowsPerBlock;
+  k_head_rows<<<unsigned(nb + kPadBlocks), 256, 0, s>>>(
+      static_cast<const __nv_bfloat16*>(H), ldh, N, d, V, y, w, dloss, lse, r, round_up(N < 1 ? 1 : N, gp::TM), int(nb),
+      loss0, lse0, E0, C, static_cast<__nv_bfloat16*>(dH0), lddh);
+  return cudaGetLastError();
+}
+
+}  // namespace
+
+size_t head_loss_workspace_bytes(int64_t N, int64_t V, int64_t d, int C) { return fwd_ws(N, V, d, C).total; }
+size_t head_loss_backward_workspace_bytes(int64_t N, int64_t V, int64_t d, bool dh, bool dw) {
+  return bwd_ws(N, V, d, dh, dw).total;
+}
+
+cudaError_t launch_head_loss(const void* H, int64_t ldh, int64_t N, int64_t d, const void* W, int64_t V,
+                             const int32_t* y, const float* w, const int32_t* cols, int C, float* loss, float* lse,
+                             float* E, void* workspace, int32_t* status, cudaStream_t s) {
+  const FwdWs lay = fwd_ws(N, V, d, C);
+  uint8_t* ws = static_cast<uint8_t*>(workspace);
+  const Rows r = rows_at(workspace, lay.rows);
+  cudaError_t e = launch_rows(H, ldh, N, d, V, y, w, nullptr, nullptr, r, loss, lse, E, C, nullptr, 0, s);
+  if (e != cudaSuccess) return e;
+  const int64_t np = round_up(N, gp::TM);
+  const int64_t vt = (V + gp::TN - 1) / gp::TN;
+  CUtensorMap mb;
+  if (!gp::map_kmajor(&mb, W, d, V, d)) return cudaErrorInvalidValue;
+  float2* part = reinterpret_cast<float2*>(ws + lay.part);
+  float* zy = reinterpret_cast<float*>(ws + lay.zy);
+  float* zc = reinterpret_cast<float*>(ws + lay.zc);
+  for (int64_t p0 = 0; p0 < np; p0 += lay.piece) {
+    const int64_t rows = np - p0 < lay.piece ? np - p0 : lay.piece;
+    CUtensorMap ma;
+    if (!gp::map_kmajor(&ma, r.H + p0 * d, d, rows, d)) return cudaErrorInvalidValue;
+    gp::Geo g = geo(rows / gp::TM, vt, (d + gp::BK - 1) / gp::BK, kSegKb, r, status);
+    g.rows_live = r.count;
+    g.m_first = int(p0 / gp::TM);
+    EpiStats epi{part, lay.piece, r.y + p0, zy, cols, E ? C : 0, zc, V};
+    e = gp::launch<false, false>(ma, mb, ma, mb, ma, g, epi, gp::NoExt{}, s);
+    if (e != cudaSuccess) return e;
+    k_head_join<<<unsigned(rows / 32), dim3(32, 2 * vt >= 128 ? 32 : 8), 0, s>>>(part, lay.piece, int(2 * vt), r, p0, zy,
+                                                                               zc, cols, C, loss, lse, E);
+    e = cudaGetLastError();
+    if (e != cudaSuccess) return e;
+  }
+  return cudaSuccess;
+}
+
+cudaError_t launch_head_loss_backward(const void* H, int64_t ldh, int64_t N, int64_t d, const void* W, int64_t V,
+                                      const int32_t* y, const float* w, const float* lse, const float* dloss,
+                                      float scale, void* dH, int64_t lddh, void* dW, void* workspace, int32_t* status,
+                                      cudaStream_t s) {
+  const BwdWs lay = bwd_ws(N, V, d, dH != nullptr, dW != nullptr);
+  uint8_t* ws = static_cast<uint8_t*>(workspace);
+  const Rows r = rows_at(workspace, lay.rows);
+  cudaError_t e = launch_rows(H, ldh, N, d, V, y, w, dloss, lse, r, nullptr, nullptr, nullptr, 0, dH, lddh, s);
+  if (e != cudaSuccess) return e;
+  const int64_t np = round_up(N < 1 ? 1 : N, gp::TM);
+  const int64_t dt = (d + gp::TN - 1) / gp::TN;
+  const __nv_bfloat16* Wb = static_cast<const __nv_bfloat16*>(W);
+  void* dz = ws + lay.dz;
+  float* part = reinterpret_cast<float*>(ws + lay.part);
+  for (int64_t p0 = 0; p0 < np; p0 += lay.piece) {
+    const int64_t rows = np - p0 < lay.piece ? np - p0 : lay.piece;
+    for (int64_t v0 = 0; v0 < V; v0 += lay.vc) {
+      const int64_t vn = V - v0 < lay.vc ? V - v0 : lay.vc;   // columns of the vocabulary
+      const int64_t vtiles = (vn + gp::TN - 1) / gp::TN;
+      CUtensorMap mh, mw, mz_out, mz_k, mw_mn;
+      if (!gp::map_kmajor(&mh, r.H + p0 * d, d, rows, d) || !gp::map_kmajor(&mw, Wb + v0 * d, d, vn, d) ||
+          !gp::map_out_bf16(&mz_out, dz, lay.vc, lay.piece, lay.vc))
+        return cudaErrorInvalidValue;
+      gp::Geo g = geo(rows / gp::TM, vtiles, (d + gp::BK - 1) / gp::BK, kSegKb, r, status);
+      g.rows_live = r.count;
+      g.m_first = int(p0 / gp::TM);
+      e = gp::launch<false, false>(mh, mw, mh, mw, mz_out, g,
+                                   EpiDz{r.lse + p0, r.w + p0, r.y + p0, r.count, p0, v0, V}, gp::NoExt{}, s);
+      if (e != cudaSuccess) return e;
+      if (dH) {
+        CUtensorMap mo;
+        if (!gp::map_kmajor(&mz_k, dz, lay.vc, lay.piece, lay.vc) || !gp::map_mnmajor(&mw_mn, Wb + v0 * d, d, vn, d) ||
+            !gp::map_3d(&mo, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 4, part, d, lay.piece, lay.splits, d, lay.piece * d, 32,
+                        32))
+          return cudaErrorInvalidValue;
+        gp::Geo gh = geo(rows / gp::TM, dt, (vn + gp::BK - 1) / gp::BK, kSegKbGrad, r, status);
+        gh.rows_live = r.count;
+        gh.m_first = g.m_first;
+        gh.splits = lay.splits;
+        e = gp::launch<false, true>(mz_k, mw_mn, mz_k, mw_mn, mo, gh, EpiAcc{lay.piece, v0 > 0 ? 1 : 0}, gp::NoExt{}, s);
+        if (e != cudaSuccess) return e;
+      }
+      if (dW) {
+        CUtensorMap mz_mn, mh_mn, mo;
+        __nv_bfloat16* o = static_cast<__nv_bfloat16*>(dW) + v0 * d;
+        if (!gp::map_mnmajor(&mz_mn, dz, lay.vc, lay.piece, lay.vc) || !gp::map_mnmajor(&mh_mn, r.H, d, np, d) ||
+            !gp::map_out_bf16(&mo, o, d, vn, d))
+          return cudaErrorInvalidValue;
+        gp::Geo gw = geo(vtiles, dt, np / gp::BK, kSegKbGrad, r, status);
+        gw.k_live = r.count;
+        e = gp::launch<true, true>(mz_mn, mh_mn, mz_mn, mh_mn, mo, gw, EpiScaled{scale}, gp::NoExt{}, s);
+        if (e != cudaSuccess) return e;
+      }
+    }
+    if (dH) {
+      k_head_dh<<<unsigned(rows), 256, 0, s>>>(part, lay.piece, lay.splits, d, r, p0, scale,
+                                              static_cast<__nv_bfloat16*>(dH), lddh);
+      e = cudaGetLastError();
+      if (e != cudaSuccess) return e;
+    }
+  }
+  return cudaSuccess;
+}
+
+}  // namespace loca

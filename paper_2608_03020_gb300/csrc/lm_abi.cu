@@ -1,0 +1,113 @@
+// C ABI entry points of the operators around the pass (head loss, adapted projection, gradient
+// clipping): host-side validation and dispatch.  See include/loca.h for the contract of each.
+#include <cuda_runtime.h>
+
+#include <cmath>
+
+#include "loca_internal.h"
+
+using namespace loca;
+
+namespace {
+
+template <class... A>
+int fail(int code, const char* fmt, A... a) {
+  return set_error_message(code, fmt, a...);
+}
+int clear() { return set_error_message(LOCA_OK, "%s", ""); }
+int cuda_fail(cudaError_t e, const char* where) { return fail(LOCA_ERR_CUDA, "%s: %s", where, cudaGetErrorString(e)); }
+bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
+
+int check_ws(const void* workspace, size_t have, size_t need) {
+  if (have < need || (need > 0 && !workspace))
+    return fail(LOCA_ERR_WORKSPACE, "workspace too small: need %zu bytes, got %zu", need, workspace ? have : size_t(0));
+  if (!aligned(workspace, 256)) return fail(LOCA_ERR_ALIGNMENT, "workspace must be 256-byte aligned");
+  return LOCA_OK;
+}
+
+int check_head(int64_t N, int64_t V, int64_t d) {
+  if (N < 0 || N > (int64_t(1) << 24)) return fail(LOCA_ERR_SHAPE, "need 0 <= N <= 2^24, got %lld", (long long)N);
+  if (V < 1 || V > (int64_t(1) << 24)) return fail(LOCA_ERR_SHAPE, "need 1 <= V <= 2^24, got %lld", (long long)V);
+  if (d < 8 || d > 65536 || d % 8 != 0)
+    return fail(LOCA_ERR_SHAPE, "need 8 <= d <= 65536, a multiple of 8, got %lld", (long long)d);
+  return LOCA_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int loca_head_loss_workspace_size(int64_t N, int64_t V, int64_t d, int32_t C, size_t* bytes) {
+  clear();
+  if (!bytes) return fail(LOCA_ERR_INVALID_ARG, "bytes is NULL");
+  const int rc = check_head(N, V, d);
+  if (rc != LOCA_OK) return rc;
+  if (C < 0 || C > 1024) return fail(LOCA_ERR_SHAPE, "need 0 <= C <= 1024, got %d", C);
+  *bytes = head_loss_workspace_bytes(N, V, d, C);
+  return LOCA_OK;
+}
+
+int loca_head_loss(const void* H, int64_t ldh, int64_t N, int64_t d, const void* W, int64_t V, const int32_t* y,
+                   const float* w, const int32_t* label_cols, int32_t C, float* loss, float* lse, float* E,
+                   void* workspace, size_t workspace_bytes, void* stream) {
+  clear();
+  int rc = check_head(N, V, d);
+  if (rc != LOCA_OK) return rc;
+  if (C < 0 || C > 1024 || (E && C < 1)) return fail(LOCA_ERR_SHAPE, "E needs 1 <= C <= 1024 label columns, got %d", C);
+  if (N == 0) return LOCA_OK;
+  if (!H || !W || !y || !loss) return fail(LOCA_ERR_INVALID_ARG, "H, W, y and loss are required");
+  if (E && !label_cols) return fail(LOCA_ERR_INVALID_ARG, "E needs label_cols");
+  if (ldh < d) return fail(LOCA_ERR_SHAPE, "row pitch of H %lld is below d = %lld", (long long)ldh, (long long)d);
+  if (ldh % 8 != 0 || !aligned(H, 16) || !aligned(W, 16))
+    return fail(LOCA_ERR_ALIGNMENT, "H and W need 16-byte alignment and a row pitch that is a multiple of 8");
+  if (!aligned(y, 4) || !aligned(w, 4) || !aligned(label_cols, 4) || !aligned(loss, 4) || !aligned(lse, 4) ||
+      !aligned(E, 4))
+    return fail(LOCA_ERR_ALIGNMENT, "y, w, label_cols, loss, lse and E need 4-byte alignment");
+  rc = check_ws(workspace, workspace_bytes, head_loss_workspace_bytes(N, V, d, C));
+  if (rc != LOCA_OK) return rc;
+  int32_t* status = device_status_word();
+  if (!status) return fail(LOCA_ERR_CUDA, "cannot resolve the device status word");
+  const cudaError_t e = launch_head_loss(H, ldh, N, d, W, V, y, w, label_cols, C, loss, lse, E, workspace, status,
+                                         static_cast<cudaStream_t>(stream));
+  if (e != cudaSuccess) return cuda_fail(e, "loca_head_loss launch");
+  return LOCA_OK;
+}
+
+int loca_head_loss_backward_workspace_size(int64_t N, int64_t V, int64_t d, int want_dH, int want_dW, size_t* bytes) {
+  clear();
+  if (!bytes) return fail(LOCA_ERR_INVALID_ARG, "bytes is NULL");
+  const int rc = check_head(N, V, d);
+  if (rc != LOCA_OK) return rc;
+  *bytes = head_loss_backward_workspace_bytes(N, V, d, want_dH != 0, want_dW != 0);
+  return LOCA_OK;
+}
+
+int loca_head_loss_backward(const void* H, int64_t ldh, int64_t N, int64_t d, const void* W, int64_t V,
+                            const int32_t* y, const float* w, const float* lse, const float* dloss, float grad_scale,
+                            void* dH, int64_t lddh, void* dW, void* workspace, size_t workspace_bytes, void* stream) {
+  clear();
+  int rc = check_head(N, V, d);
+  if (rc != LOCA_OK) return rc;
+  if (!dH && !dW) return fail(LOCA_ERR_INVALID_ARG, "dH or dW is required");
+  if (N == 0 && !dW) return LOCA_OK;
+  if (!W || (N > 0 && (!H || !y || !lse))) return fail(LOCA_ERR_INVALID_ARG, "H, W, y and lse are required");
+  if (N > 0 && (ldh < d || (dH && lddh < d)))
+    return fail(LOCA_ERR_SHAPE, "row pitch of H %lld or dH %lld is below d = %lld", (long long)ldh, (long long)lddh,
+                (long long)d);
+  if ((N > 0 && (ldh % 8 != 0 || (dH && lddh % 8 != 0))) || !aligned(H, 16) || !aligned(W, 16) || !aligned(dH, 16) ||
+      !aligned(dW, 16))
+    return fail(LOCA_ERR_ALIGNMENT, "H, W, dH and dW need 16-byte alignment and row pitches that are multiples of 8");
+  if (!aligned(y, 4) || !aligned(w, 4) || !aligned(lse, 4) || !aligned(dloss, 4))
+    return fail(LOCA_ERR_ALIGNMENT, "y, w, lse and dloss need 4-byte alignment");
+  if (!std::isfinite(grad_scale)) return fail(LOCA_ERR_INVALID_ARG, "grad_scale must be finite");
+  rc = check_ws(workspace, workspace_bytes, head_loss_backward_workspace_bytes(N, V, d, dH != nullptr, dW != nullptr));
+  if (rc != LOCA_OK) return rc;
+  int32_t* status = device_status_word();
+  if (!status) return fail(LOCA_ERR_CUDA, "cannot resolve the device status word");
+  const cudaError_t e = launch_head_loss_backward(H, ldh, N, d, W, V, y, w, lse, dloss, grad_scale, N > 0 ? dH : nullptr,
+                                                  lddh, dW, workspace, status, static_cast<cudaStream_t>(stream));
+  if (e != cudaSuccess) return cuda_fail(e, "loca_head_loss_backward launch");
+  return LOCA_OK;
+}
+
+}  // extern "C"

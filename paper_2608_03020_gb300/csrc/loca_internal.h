@@ -158,4 +158,15 @@ cudaError_t launch_calib_rsvd(const float* E_probe, const float* G_probe, int64_
                               float beta, int r, int ell, int q, const float* Omega, float* P, float* Q,
                               float* sigma, void* workspace, int32_t* status, cudaStream_t s);
 
+// ---- head loss from hidden states (head_loss.cu)
+size_t head_loss_workspace_bytes(int64_t N, int64_t V, int64_t d, int C);
+size_t head_loss_backward_workspace_bytes(int64_t N, int64_t V, int64_t d, bool dh, bool dw);
+cudaError_t launch_head_loss(const void* H, int64_t ldh, int64_t N, int64_t d, const void* W, int64_t V,
+                             const int32_t* y, const float* w, const int32_t* cols, int C, float* loss, float* lse,
+                             float* E, void* workspace, int32_t* status, cudaStream_t s);
+cudaError_t launch_head_loss_backward(const void* H, int64_t ldh, int64_t N, int64_t d, const void* W, int64_t V,
+                                      const int32_t* y, const float* w, const float* lse, const float* dloss,
+                                      float scale, void* dH, int64_t lddh, void* dW, void* workspace, int32_t* status,
+                                      cudaStream_t s);
+
 }  // namespace loca

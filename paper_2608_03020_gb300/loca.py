@@ -79,6 +79,13 @@ SIGNATURES = [
     ("loca_calib_fit_rsvd_workspace_size", ctypes.c_int, [_I64, _I32, _I64, _I32, _I32, _I32, ctypes.POINTER(_SZ)]),
     ("loca_calib_fit_rsvd", ctypes.c_int,
      [_P, _P, _I64, _I32, _I64, _I32, _F, _I32, _I32, _I32, _P, _P, _P, _P, _P, _SZ, _P]),
+    ("loca_head_loss_workspace_size", ctypes.c_int, [_I64, _I64, _I64, _I32, ctypes.POINTER(_SZ)]),
+    ("loca_head_loss", ctypes.c_int,
+     [_P, _I64, _I64, _I64, _P, _I64, _P, _P, _P, _I32, _P, _P, _P, _P, _SZ, _P]),
+    ("loca_head_loss_backward_workspace_size", ctypes.c_int,
+     [_I64, _I64, _I64, ctypes.c_int, ctypes.c_int, ctypes.POINTER(_SZ)]),
+    ("loca_head_loss_backward", ctypes.c_int,
+     [_P, _I64, _I64, _I64, _P, _I64, _P, _P, _P, _P, _F, _P, _I64, _P, _P, _SZ, _P]),
 ]
 
 
@@ -628,6 +635,88 @@ def loca_calib_fit_rsvd(E_probe, G_probe, beta, r, Omega, q, P, Q, sigma=None, w
     rc = lib().loca_calib_fit_rsvd(_ptr(E_probe), _ptr(G_probe), Np, m, d, L, float(beta), r, ell, int(q),
                                    _ptr(Omega), _ptr(P), _ptr(Q), _ptr(sigma), _ptr(ws), nbytes, _stream(stream))
     _check(rc, "loca_calib_fit_rsvd")
+
+
+def _rows2d(t, name, dtype, shape=None):
+    """A 2-D CUDA tensor with unit column stride (rows may be spaced); returns its row pitch."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise TypeError(f"{name} must be a CUDA tensor")
+    if t.dtype != dtype:
+        raise TypeError(f"{name} has dtype {t.dtype}, expected {dtype}")
+    if t.dim() != 2 or (shape is not None and tuple(t.shape) != tuple(shape)):
+        raise ValueError(f"{name} must have shape {tuple(shape) if shape else '2-D'}, got {tuple(t.shape)}")
+    if t.shape[1] > 1 and t.stride(1) != 1:
+        raise ValueError(f"{name} must have unit column stride")
+    pitch = t.stride(0) if t.shape[0] > 1 else t.shape[1]
+    if pitch < t.shape[1]:
+        raise ValueError(f"{name} must have a row pitch of at least its columns")
+    return pitch
+
+
+def head_loss_workspace_size(N, V, d, C=0) -> int:
+    out = ctypes.c_size_t(0)
+    _check(lib().loca_head_loss_workspace_size(N, V, d, C, ctypes.byref(out)), "loca_head_loss_workspace_size")
+    return out.value
+
+
+def loca_head_loss(H, W, y, loss, lse=None, w=None, label_cols=None, E=None, workspace=None, stream=None):
+    """Cross entropy of hidden states ``H`` (N x d bf16, rows may be spaced) against the head ``W``
+    (V x d bf16) at labels ``y`` (N int32; outside [0, V) = masked) without the logits in memory:
+    fills ``loss`` and ``lse`` (N float) and, for ``label_cols`` (C int32), the label-column error
+    ``E`` (N x C float) that :func:`loca_targets` takes."""
+    ldh = _rows2d(H, "H", torch.bfloat16)
+    N, d = H.shape
+    _dev(W, "W", torch.bfloat16, 2)
+    _dev(y, "y", torch.int32, 1)
+    _dev(loss, "loss", torch.float32, 1)
+    _dev(lse, "lse", torch.float32, 1)
+    _dev(w, "w", torch.float32, 1)
+    _dev(label_cols, "label_cols", torch.int32, 1)
+    _dev(E, "E", torch.float32, 2)
+    V = W.shape[0]
+    if (W.shape[1] != d or y.numel() != N or loss.numel() != N or (lse is not None and lse.numel() != N)
+            or (w is not None and w.numel() != N)):
+        raise ValueError("W must be V x d; y, loss, lse and w must have N entries")
+    C = 0 if label_cols is None else label_cols.numel()
+    if E is not None and tuple(E.shape) != (N, C):
+        raise ValueError("E must be N x C for the C entries of label_cols")
+    nbytes = head_loss_workspace_size(N, V, d, C)
+    ws = _workspace(nbytes, H.device, workspace)
+    rc = lib().loca_head_loss(_ptr(H), ldh, N, d, _ptr(W), V, _ptr(y), _ptr(w), _ptr(label_cols), C, _ptr(loss),
+                              _ptr(lse), _ptr(E), _ptr(ws), nbytes, _stream(stream))
+    _check(rc, "loca_head_loss")
+
+
+def head_loss_backward_workspace_size(N, V, d, want_dH=True, want_dW=True) -> int:
+    out = ctypes.c_size_t(0)
+    _check(lib().loca_head_loss_backward_workspace_size(N, V, d, int(bool(want_dH)), int(bool(want_dW)),
+                                                        ctypes.byref(out)), "loca_head_loss_backward_workspace_size")
+    return out.value
+
+
+def loca_head_loss_backward(H, W, y, lse, dH=None, dW=None, w=None, dloss=None, grad_scale=1.0, workspace=None,
+                            stream=None):
+    """Gradients of ``grad_scale * sum_n dloss[n] * loss[n]`` of :func:`loca_head_loss` for the hidden
+    states (``dH``, N x d bf16, rows may be spaced) and the head (``dW``, V x d bf16), in pieces of
+    the vocabulary; ``lse`` is the forward call's."""
+    ldh = _rows2d(H, "H", torch.bfloat16)
+    N, d = H.shape
+    _dev(W, "W", torch.bfloat16, 2)
+    _dev(y, "y", torch.int32, 1)
+    _dev(lse, "lse", torch.float32, 1)
+    _dev(w, "w", torch.float32, 1)
+    _dev(dloss, "dloss", torch.float32, 1)
+    lddh = 0 if dH is None else _rows2d(dH, "dH", torch.bfloat16, (N, d))
+    _dev(dW, "dW", torch.bfloat16, 2)
+    V = W.shape[0]
+    if (W.shape[1] != d or y.numel() != N or lse.numel() != N or (w is not None and w.numel() != N)
+            or (dloss is not None and dloss.numel() != N) or (dW is not None and tuple(dW.shape) != (V, d))):
+        raise ValueError("W and dW must be V x d; y, lse, w and dloss must have N entries")
+    nbytes = head_loss_backward_workspace_size(N, V, d, dH is not None, dW is not None)
+    ws = _workspace(nbytes, H.device, workspace)
+    rc = lib().loca_head_loss_backward(_ptr(H), ldh, N, d, _ptr(W), V, _ptr(y), _ptr(w), _ptr(lse), _ptr(dloss),
+                                       float(grad_scale), _ptr(dH), lddh, _ptr(dW), _ptr(ws), nbytes, _stream(stream))
+    _check(rc, "loca_head_loss_backward")
 
 
 class Pass:
