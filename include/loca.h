@@ -521,6 +521,48 @@ int loca_head_loss_backward(const void* H, int64_t ldh, int64_t N, int64_t d, co
                             const int32_t* y, const float* w, const float* lse, const float* dloss, float grad_scale,
                             void* dH, int64_t lddh, void* dW, void* workspace, size_t workspace_bytes, void* stream);
 
+/*
+ * Adapters of many requests beside a shared frozen projection (Eq. 1), forward and backward:
+ *
+ *   U = X A_a,   Y = X W^T + s_a U B_a^T                       a = ids[n]; outside [0, n): Y = X W^T
+ *   T = s_a dY B_a,   dX = dY W + T A_a^T,   dA_a = X_a^T T_a,   dB_a = s_a dY_a^T U_a
+ *
+ * X, dX are N x d_in and Y, dY N x d_out, bf16 with row pitches; W is d_out x d_in bf16, contiguous;
+ * A is n x d_in x k and B n x d_out x k (the layouts of loca_ridge_solve's A and B), LOCA_F32 or
+ * LOCA_BF16; 1 <= k <= 64, 1 <= n <= 65535, N <= 2^22, d_in and d_out multiples of 8 (8 .. 65536).
+ *
+ * loca_adapter_pack  lays A and s B out for the kernels (three bf16 parts of each value, which keep
+ *                    fp32 adapters to 2^-26) in `packed` (256-byte aligned, loca_adapter_packed_size
+ *                    bytes): once for serving, after every update in training.  scale: n float, or
+ *                    NULL for ones.  An adapter with a value that is not finite (in A, or in s B)
+ *                    gives NaN in every output of its own tokens and touches no other's
+ * loca_adapter_plan  groups the tokens of one step by adapter in `plan` (256-byte aligned,
+ *                    loca_adapter_plan_size bytes), on the device; it serves every projection of the
+ *                    step with the same ids and n.  ids: N int32 in any order
+ * loca_adapter_apply     Y.  The low-rank term is multiplied in bf16 (U rounded once) and added in
+ *                    fp32; Y is rounded once
+ * loca_adapter_backward  dX (like Y; with row pitch), dA (n x d_in x k) and dB (n x d_out x k) of
+ *                    type grad_dtype; each may be NULL, not all.  U and T are kept to 2^-26 for dA
+ *                    and dB.  An adapter without a token gets zeros.  A token outside an adapter
+ *                    reaches its gradients in no way, whatever its row holds
+ * loca_adapter_workspace_size  scratch of one apply (backward 0) or of apply and backward (1)
+ * All are deterministic.  X, dY, Y, dX, W 16-byte aligned, row pitches multiples of 8.
+ */
+int loca_adapter_packed_size(int32_t n, int64_t d_in, int64_t d_out, int32_t k, size_t* bytes);
+int loca_adapter_pack(const void* A, const void* B, int dtype, int32_t n, int64_t d_in, int64_t d_out, int32_t k,
+                      const float* scale, void* packed, void* stream);
+int loca_adapter_plan_size(int64_t N, int32_t n, size_t* bytes);
+int loca_adapter_plan(const int32_t* ids, int64_t N, int32_t n, void* plan, void* stream);
+int loca_adapter_workspace_size(int64_t N, int64_t d_in, int64_t d_out, int32_t k, int32_t n, int backward,
+                                size_t* bytes);
+int loca_adapter_apply(const void* X, int64_t ldx, int64_t N, int64_t d_in, const void* W, int64_t d_out,
+                       const void* packed, int32_t n, int32_t k, const void* plan, void* Y, int64_t ldy,
+                       void* workspace, size_t workspace_bytes, void* stream);
+int loca_adapter_backward(const void* X, int64_t ldx, const void* dY, int64_t lddy, int64_t N, int64_t d_in,
+                          const void* W, int64_t d_out, const void* packed, int32_t n, int32_t k, const void* plan,
+                          void* dX, int64_t lddx, void* dA, void* dB, int grad_dtype, void* workspace,
+                          size_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

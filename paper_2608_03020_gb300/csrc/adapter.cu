@@ -1,0 +1,1399 @@
+// Low-rank adapters of many requests beside a shared projection, forward and backward.
+//   U = X A_a,  Y = X W^T + s_a U B_a^T                       (Eq. 1 with a frozen W; a = ids[n])
+//   T = s_a dY B_a,  dX = dY W + T A_a^T,  dA_a = X_a^T T_a,  dB_a = s_a dY_a^T U_a
+// X is N x d_in, W d_out x d_in, A_a d_in x k, B_a d_out x k; a token without an adapter (id outside
+// [0, n)) gets X W^T alone.
+//
+// Adapters as extra k.  For a tile of tokens, X W^T and the low-rank term are one product over a
+// longer k axis: behind the d_in columns of [X | U] and [W | s B] come, for each adapter that the
+// tile's tokens use, the k columns of U (rows of tokens with another adapter zero) against that
+// adapter's k columns of s B.  Eight requests in a tile of 256 cost eight more k-blocks; a decode
+// batch of 64 adapters costs 64 steps of k = 16.  The plan finds each tile's adapters on the device;
+// a (tile of 128 tokens, adapter) pair is a slot.
+//
+//   k_plan_*          slots of the token tiles, slots of each adapter (one plan serves every
+//                     projection of a step)
+//   k_adapter_pack    A and s B as three bf16 parts (hi + mid + lo = the fp32 value to 2^-26)
+//   k_adapter_shrink  U (or T) of every slot: tokens x k sums over d.  Bound: the read of X
+//   k_gemm_pair       the extended product in 256 x 256 tiles (many tokens)
+//   k_adapter_few     the extended product with the roles of the operands exchanged, W's rows as M,
+//                     the tokens as N, k split over a cluster (few tokens).  Bound: the read of W
+//   k_adapter_grad    dA and dB: channels x k sums over an adapter's tokens.  Bound: the read of X, dY
+//   k_adapter_join    sums the token ranges of dA, dB in a fixed order, scales, rounds once
+// Rounding.  The low-rank term of a bf16 output uses the first part of U and of s B: its relative
+// error 2^-8 is of a term that is itself rounded to bf16 with the sum.  dA and dB may be fp32, so U and
+// T are then summed from all three parts of the adapters and passed on in three parts.
+#include <cuda_bf16.h>
+#include <cuda_runtime.h>
+
+#include <cstring>
+
+#include "gemm_pair.cuh"
+
+namespace loca {
+namespace {
+
+using namespace tc;
+
+constexpr int kTile = 128;       // tokens of a plan tile (one slot: 128 x 64 values of U)
+constexpr int kMaxK = 64;
+constexpr int kParts = 3;
+constexpr int kSlotRows = 128;
+constexpr size_t kSlotElems = size_t(kSlotRows) * kMaxK;
+
+__host__ __device__ inline int k_padded(int k) { return (k + 7) / 8 * 8; }
+
+// ------------------------------------------------------------------ plan
+// Offsets in int32 from the start of the plan.
+struct PlanLay {
+  int64_t tiles, pairs, smax;
+  int64_t tok_slot, tile_base, adapter, tile, count, pair_count, pair_ad, pair_s0, pair_s1, ad_off, ad_slots, total;
+};
+PlanLay plan_lay(int64_t N, int n) {
+  PlanLay p{};
+  p.tiles = (N + kTile - 1) / kTile;
+  p.pairs = (p.tiles + 1) / 2;
+  const int64_t per = n < kTile ? n : kTile;
+  p.smax = p.tiles * per < N ? p.tiles * per : N;
+  int64_t at = 0;
+  auto take = [&](int64_t c) {
+    const int64_t o = at;
+    at += (c + 63) / 64 * 64;
+    return o;
+  };
+  p.tok_slot = take(N);
+  p.tile_base = take(p.tiles + 2);
+  p.adapter = take(p.smax);
+  p.tile = take(p.smax);
+  p.count = take(p.smax);
+  p.pair_count = take(p.pairs);
+  p.pair_ad = take(p.smax);
+  p.pair_s0 = take(p.smax);
+  p.pair_s1 = take(p.smax);
+  p.ad_off = take(n + 1);
+  p.ad_slots = take(p.smax);
+  p.total = at;
+  return p;
+}
+
+// A tile's distinct adapters in the order of their first tokens.  fill 0: counts them into
+// tile_base[tile + 1]; fill 1: writes the tile's slots at tile_base[tile].
+__global__ void __launch_bounds__(kTile) k_plan_tiles(const int32_t* __restrict__ ids, int64_t N, int n, int32_t* plan,
+                                                      PlanLay p, int fill) {
+  __shared__ int32_t id[kTile];
+  __shared__ int32_t warp_sum[4];
+  __shared__ int32_t rank[kTile];
+  const int j = threadIdx.x, lane = j & 31, warp = j >> 5;
+  const int64_t tile = blockIdx.x, tok = tile * kTile + j;
+  int a = tok < N ? ids[tok] : -1;
+  if (a >= n) a = -1;
+  id[j] = a;
+  __syncthreads();
+  int first = a >= 0 ? j : -1, members = 0;
+  if (a >= 0)
+    for (int i = 0; i < kTile; ++i)
+      if (id[i] == a) {
+        if (i < first) first = i;
+        ++members;
+      }
+  const bool mine = first == j;
+  const unsigned all = __ballot_sync(0xffffffffu, mine);
+  if (lane == 0) warp_sum[warp] = __popc(all);
+  __syncthreads();
+  int before = __popc(all & ((1u << lane) - 1u)), total = 0;
+  for (int w = 0; w < 4; ++w) {
+    if (w < warp) before += warp_sum[w];
+    total += warp_sum[w];
+  }
+  if (!fill) {
+    if (j == 0) plan[p.tile_base + tile + 1] = total;
+    return;
+  }
+  const int base = plan[p.tile_base + tile];
+  if (mine) {
+    rank[j] = before;
+    const int s = base + before;
+    if (LOCA_CHECK(s, p.smax)) {
+      plan[p.adapter + s] = a;
+      plan[p.tile + s] = int32_t(tile);
+      plan[p.count + s] = members;
+    }
+  }
+  __syncthreads();
+  if (tok < N) plan[p.tok_slot + tok] = a >= 0 ? base + rank[first] : -1;
+}
+
+// tile_base: counts to offsets (one block; `tiles` entries in runs of 1024).
+__global__ void __launch_bounds__(1024) k_plan_scan(int32_t* plan, PlanLay p) {
+  __shared__ int32_t sums[32];
+  int32_t* base = plan + p.tile_base;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  int32_t carry = 0;
+  for (int64_t t0 = 0; t0 < p.tiles; t0 += 1024) {
+    const int64_t t = t0 + threadIdx.x;
+    int32_t x = t < p.tiles ? base[t + 1] : 0;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int32_t y = __shfl_up_sync(0xffffffffu, x, o);
+      if (lane >= o) x += y;
+    }
+    if (lane == 31) sums[warp] = x;
+    __syncthreads();
+    int32_t off = carry, all = 0;
+    for (int w = 0; w < 32; ++w) {
+      if (w < warp) off += sums[w];
+      all += sums[w];
+    }
+    if (t < p.tiles) base[t + 1] = off + x;
+    carry += all;
+    __syncthreads();
+  }
+  if (threadIdx.x == 0) base[0] = 0;
+  // an odd last tile has an empty partner
+  if (threadIdx.x == 0) base[p.tiles + 1] = carry;
+}
+
+// Adapters of a pair of tiles (256 rows of the CTA-pair product), with each half's slot or -1.
+__global__ void __launch_bounds__(kTile) k_plan_pairs(int32_t* plan, PlanLay p) {
+  __shared__ int32_t warp_sum[4];
+  const int j = threadIdx.x, lane = j & 31, warp = j >> 5;
+  const int64_t t0 = 2 * int64_t(blockIdx.x);
+  const int b0 = plan[p.tile_base + t0], b1 = plan[p.tile_base + t0 + 1];
+  const int b2 = t0 + 1 < p.tiles ? plan[p.tile_base + t0 + 2] : b1;
+  const int n0 = b1 - b0, n1 = b2 - b1;
+  if (j < n0) {
+    const int a = plan[p.adapter + b0 + j];
+    int other = -1;
+    for (int i = 0; i < n1; ++i)
+      if (plan[p.adapter + b1 + i] == a) other = b1 + i;
+    plan[p.pair_ad + b0 + j] = a;
+    plan[p.pair_s0 + b0 + j] = b0 + j;
+    plan[p.pair_s1 + b0 + j] = other;
+  }
+  bool alone = j < n1;
+  int a1 = -1;
+  if (j < n1) {
+    a1 = plan[p.adapter + b1 + j];
+    for (int i = 0; i < n0; ++i)
+      if (plan[p.adapter + b0 + i] == a1) alone = false;
+  }
+  const unsigned all = __ballot_sync(0xffffffffu, alone);
+  if (lane == 0) warp_sum[warp] = __popc(all);
+  __syncthreads();
+  int at = n0 + __popc(all & ((1u << lane) - 1u)), total = n0;
+  for (int w = 0; w < 4; ++w) {
+    if (w < warp) at += warp_sum[w];
+    total += warp_sum[w];
+  }
+  if (alone) {
+    plan[p.pair_ad + b0 + at] = a1;
+    plan[p.pair_s0 + b0 + at] = -1;
+    plan[p.pair_s1 + b0 + at] = b1 + j;
+  }
+  if (j == 0) plan[p.pair_count + blockIdx.x] = total;
+}
+
+// Slots of each adapter, in the order of the tiles: block a takes adapter a.
+__global__ void __launch_bounds__(256) k_plan_adapters(int32_t* plan, PlanLay p, int n) {
+  __shared__ int32_t below, sums[8];
+  const int a = blockIdx.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int total = plan[p.tile_base + p.tiles];
+  if (threadIdx.x == 0) below = 0;
+  __syncthreads();
+  int c = 0;
+  for (int s = threadIdx.x; s < total; s += 256) c += plan[p.adapter + s] < a ? 1 : 0;
+  atomicAdd(&below, c);  // an integer count: the order of the additions does not matter
+  __syncthreads();
+  int at = below;
+  if (threadIdx.x == 0) {
+    plan[p.ad_off + a] = at;
+    if (a == n - 1) plan[p.ad_off + n] = total;
+  }
+  for (int s0 = 0; s0 < total; s0 += 256) {
+    const int s = s0 + threadIdx.x;
+    const bool mine = s < total && plan[p.adapter + s] == a;
+    const unsigned all = __ballot_sync(0xffffffffu, mine);
+    if (lane == 0) sums[warp] = __popc(all);
+    __syncthreads();
+    int off = at + __popc(all & ((1u << lane) - 1u)), here = 0;
+    for (int w = 0; w < 8; ++w) {
+      if (w < warp) off += sums[w];
+      here += sums[w];
+    }
+    if (mine && LOCA_CHECK(off, p.smax)) plan[p.ad_slots + off] = s;
+    at += here;
+    __syncthreads();
+  }
+}
+
+// ------------------------------------------------------------------ packed adapters
+// A: kParts x n x d_in x kp bf16, then s B: kParts x n x d_out x kp, then the n scales (fp32) and n
+// marks.  In a shared tile an adapter's columns meet the other tokens' zeros, and zero times infinity
+// is not zero: values that are not finite are stored as zero and their adapter is marked, and U and
+// T of a marked adapter's tokens are NaN.  One request's broken adapter so spoils its own outputs
+// (all of them) and nobody else's.
+struct PackLay {
+  size_t a, b, scale, marks, total;
+};
+PackLay pack_lay(int n, int64_t d_in, int64_t d_out, int k) {
+  const size_t kp = size_t(k_padded(k));
+  PackLay p{};
+  p.a = 0;
+  p.b = align256(2 * kParts * size_t(n) * size_t(d_in) * kp);
+  p.scale = p.b + align256(2 * kParts * size_t(n) * size_t(d_out) * kp);
+  p.marks = p.scale + align256(4 * size_t(n));
+  p.total = p.marks + align256(4 * size_t(n));
+  return p;
+}
+
+__device__ __forceinline__ void split3(float x, __nv_bfloat16 (&o)[3]) {
+  o[0] = __float2bfloat16_rn(x);
+  x -= __bfloat162float(o[0]);
+  o[1] = __float2bfloat16_rn(x);
+  x -= __bfloat162float(o[1]);
+  o[2] = __float2bfloat16_rn(x);
+}
+
+template <class T>
+__device__ __forceinline__ float as_float(T x);
+template <>
+__device__ __forceinline__ float as_float<float>(float x) { return x; }
+template <>
+__device__ __forceinline__ float as_float<__nv_bfloat16>(__nv_bfloat16 x) { return __bfloat162float(x); }
+
+template <class T>
+__global__ void __launch_bounds__(256)
+    k_adapter_pack(const T* __restrict__ A, const T* __restrict__ B, int n, int64_t d_in, int64_t d_out, int k, int kp,
+                   const float* __restrict__ scale, __nv_bfloat16* __restrict__ pa, __nv_bfloat16* __restrict__ pb,
+                   float* __restrict__ ps, int32_t* __restrict__ marks) {
+  const int64_t na = int64_t(n) * d_in * kp, nb = int64_t(n) * d_out * kp;
+  const int64_t stride = int64_t(gridDim.x) * blockDim.x;
+  for (int64_t i = int64_t(blockIdx.x) * blockDim.x + threadIdx.x; i < na + nb; i += stride) {
+    const bool isb = i >= na;
+    const int64_t e = isb ? i - na : i;
+    const int64_t row = e / kp;
+    const int c = int(e - row * kp);
+    float x = 0.f;
+    if (c < k) x = as_float<T>(isb ? B[row * k + c] : A[row * k + c]);
+    if (isb && scale) x *= scale[row / d_out];
+    if (!isfinite(__bfloat162float(__float2bfloat16_rn(x)))) {
+      x = 0.f;
+      marks[row / (isb ? d_out : d_in)] = 1;
+    }
+    __nv_bfloat16 o[3];
+    split3(x, o);
+    __nv_bfloat16* to = isb ? pb : pa;
+    const int64_t pitch = isb ? nb : na;
+#pragma unroll
+    for (int q = 0; q < 3; ++q) to[q * pitch + e] = o[q];
+  }
+  for (int64_t i = int64_t(blockIdx.x) * blockDim.x + threadIdx.x; i < n; i += stride) ps[i] = scale ? scale[i] : 1.f;
+}
+
+// ------------------------------------------------------------------ U and T: tokens x k sums over d
+// One item per slot, its d axis split over the CTAs of a cluster.  A slot with more than kFewTokens
+// tokens goes through the tensor cores: M = the tile's 128 tokens, N = 64 columns per part of the
+// adapter.  A slot with fewer (decode) multiplies its tokens one by one, reading the adapter once:
+// the tile's other rows would cost 64 times the loads.  The CTAs add their sums through distributed
+// shared memory in rank order, zero the rows of other slots and write the parts.
+constexpr int kFewTokens = 16;
+constexpr int kTokGroup = 4;
+constexpr int kShrinkThreads = 192;
+constexpr int kShrinkSeg = 8;                    // k-blocks per accumulation segment (three parts)
+constexpr int kMaxStages = 8;
+constexpr int kRedBytes = kSlotRows * kMaxK * 4; // 32 KB of fp32 sums, in the place of the ring
+constexpr int kXBytes = 128 * 64 * 2, kPBytes = 64 * 64 * 2;
+
+struct ShrinkGeo {
+  const __nv_bfloat16* X;
+  int64_t ldx, N, d;
+  const __nv_bfloat16* P;  // packed adapter operand: part x adapter x d x kp
+  const int32_t* marks;
+  int n, kp, parts, stages;
+  const int32_t* plan;
+  PlanLay p;
+  __nv_bfloat16* out;  // parts x smax x 128 x 64
+  int32_t* status;
+  int32_t* abort_flag;
+  unsigned long long limit_ns;
+};
+int shrink_ring(int parts, int stages) {
+  const int b = stages * (kXBytes + parts * kPBytes);
+  return b > kRedBytes ? b : kRedBytes;
+}
+int shrink_smem(int parts, int stages) { return shrink_ring(parts, stages) + 512 + 1024; }
+
+// Position of (row, col) in the fp32 sums: 16-byte chunks swizzled over the rows (no bank conflicts).
+__device__ __forceinline__ int red_at(int row, int col) {
+  return row * kMaxK + (((col >> 2) ^ (row & 15)) << 2) + (col & 3);
+}
+
+// The few tokens of a slot, rows list[0 .. members): sums over k0 .. k1 into red.  Thread t takes the
+// 16-byte chunk t % nc of the adapter rows t / nc, t / nc + stride, ...
+__device__ __forceinline__ void shrink_few(const ShrinkGeo& g, int a, int64_t row0, const int* list, int members,
+                                           int64_t k0, int64_t k1, float* red, float* part) {
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int chunks = g.kp / 8;
+  const int nc = chunks <= 1 ? 1 : chunks <= 2 ? 2 : chunks <= 4 ? 4 : 8;
+  const int c = threadIdx.x % nc, r0 = threadIdx.x / nc, stride = kShrinkThreads / nc;
+  const int64_t pitch = int64_t(g.n) * g.d * g.kp;
+  const __nv_bfloat16* P = g.P + int64_t(a) * g.d * g.kp + c * 8;
+  for (int t0 = 0; t0 < members; t0 += kTokGroup) {
+    float acc[kTokGroup][8];
+    const __nv_bfloat16* x[kTokGroup];
+#pragma unroll
+    for (int t = 0; t < kTokGroup; ++t) {
+      const int m = t0 + t < members ? t0 + t : members - 1;
+      x[t] = g.X + (row0 + list[m]) * g.ldx;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) acc[t][i] = 0.f;
+    }
+    if (c < chunks) {
+#pragma unroll 4
+      for (int64_t k = k0 + r0; k < k1; k += stride) {
+        float w[8] = {};
+        for (int q = g.parts - 1; q >= 0; --q) {
+          const uint4 v = *reinterpret_cast<const uint4*>(P + q * pitch + k * g.kp);
+          const __nv_bfloat162* h = reinterpret_cast<const __nv_bfloat162*>(&v);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const float2 f = __bfloat1622float2(h[i]);
+            w[2 * i] += f.x;
+            w[2 * i + 1] += f.y;
+          }
+        }
+#pragma unroll
+        for (int t = 0; t < kTokGroup; ++t) {
+          const float xv = __bfloat162float(x[t][k]);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) acc[t][i] = fmaf(xv, w[i], acc[t][i]);
+        }
+      }
+    }
+#pragma unroll
+    for (int t = 0; t < kTokGroup; ++t)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        float v = acc[t][i];
+        for (int o = nc; o < 32; o <<= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+        if (lane < nc) part[(warp * kTokGroup + t) * kMaxK + lane * 8 + i] = v;
+      }
+    __syncthreads();
+    for (int e = threadIdx.x; e < kTokGroup * kMaxK; e += kShrinkThreads) {
+      const int t = e / kMaxK, col = e % kMaxK;
+      if (t0 + t < members) {
+        float v = 0.f;
+        if (col < g.kp)
+          for (int w = 0; w < kShrinkThreads / 32; ++w) v += part[(w * kTokGroup + t) * kMaxK + col];
+        red[red_at(list[t0 + t], col)] = v;
+      }
+    }
+    __syncthreads();
+  }
+}
+
+__global__ void __launch_bounds__(kShrinkThreads, 1)
+    k_adapter_shrink(const __grid_constant__ CUtensorMap tmX, const __grid_constant__ CUtensorMap tmP,
+                     const __grid_constant__ ShrinkGeo g) {
+  extern __shared__ uint8_t smem_raw[];
+  __shared__ float few_part[kShrinkThreads / 32 * kTokGroup * kMaxK];
+  __shared__ int few_list[kFewTokens];
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  const int stage_bytes = kXBytes + g.parts * kPBytes;
+  const int ring = g.stages * stage_bytes > kRedBytes ? g.stages * stage_bytes : kRedBytes;
+  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + ring);
+  const uint32_t bar_base = smem_u32(bars);
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 * kMaxStages + 5);
+  auto full_bar = [&](int s) { return bar_base + 8u * s; };
+  auto empty_bar = [&](int s) { return bar_base + 8u * (kMaxStages + s); };
+  auto acc_full = [&](uint32_t b) { return bar_base + 8u * (2 * kMaxStages + b); };
+  auto acc_empty = [&](uint32_t b) { return bar_base + 8u * (2 * kMaxStages + 2 + b); };
+  const uint32_t drain_bar = bar_base + 8u * (2 * kMaxStages + 4);
+  float* red = reinterpret_cast<float*>(smem);  // [128][64] sums of this CTA
+
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t smem_base = smem_u32(smem);
+  const WaitCtl wc{g.status, g.abort_flag, g.limit_ns};
+  const int ks = int(cluster_nctarank()), rank = int(cluster_ctarank());
+  const int cid = int(cluster_id_x()), ncl = int(ncluster_x());
+  const uint32_t acc_cols = uint32_t(64 * g.parts);
+  const uint32_t cols = g.parts == 1 ? 128u : 512u;
+
+  launch_dependents();
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < kMaxStages; ++s) {
+      mbar_init(full_bar(s), 1);
+      mbar_init(empty_bar(s), 1);
+    }
+    for (uint32_t b = 0; b < 2; ++b) {
+      mbar_init(acc_full(b), 1);
+      mbar_init(acc_empty(b), 4);
+    }
+    mbar_init(drain_bar, 1);
+    mbar_init_fence();
+    prefetch_tensormap(&tmX);
+    prefetch_tensormap(&tmP);
+  }
+  if (warp == 1) tmem_alloc(smem_u32(tmem_slot), cols);
+  fence_before();
+  __syncthreads();
+  fence_after();
+  const uint32_t tmem_base = *tmem_slot;
+  const int nkb = int((g.d + 63) / 64);
+  const int per = (nkb + ks - 1) / ks;
+  const int kb0 = rank * per < nkb ? rank * per : nkb;
+  const int kb1 = kb0 + per < nkb ? kb0 + per : nkb;
+  const int nb = kb1 - kb0;
+  const int seg_kb = g.parts == 1 ? 64 : kShrinkSeg;
+  const int total = g.plan[g.p.tile_base + g.p.tiles];
+
+  int stage = 0;
+  uint32_t phase = 0, iter = 0, seg = 0;
+  bool ok = true, issued = false;
+  for (int s = cid; s < total; s += ncl) {
+    const int a = g.plan[g.p.adapter + s];
+    const int64_t row0 = int64_t(g.plan[g.p.tile + s]) * kTile;
+    const int members = g.plan[g.p.count + s];
+    if (members <= kFewTokens) {
+      if (warp == 0) {
+        int at = 0;
+        for (int b = 0; b < kTile; b += 32) {
+          const int64_t tok = row0 + b + lane;
+          const bool mine = tok < g.N && g.plan[g.p.tok_slot + tok] == s;
+          const unsigned all = __ballot_sync(0xffffffffu, mine);
+          const int pos = at + __popc(all & ((1u << lane) - 1u));
+          if (mine && pos < kFewTokens) few_list[pos] = b + lane;
+          at += __popc(all);
+        }
+      }
+      __syncthreads();
+      const int64_t k1 = int64_t(kb1) * 64 < g.d ? int64_t(kb1) * 64 : g.d;
+      shrink_few(g, a, row0, few_list, members, int64_t(kb0) * 64, k1, red, few_part);
+    } else if (warp == 0) {
+      // ---------------- TMA producer
+      if (lane == 0 && ok) {
+        for (int kb = kb0; kb < kb1; ++kb) {
+          if (!mbar_try_wait(empty_bar(stage), phase ^ 1u) && !mbar_wait(empty_bar(stage), phase ^ 1u, wc)) {
+            ok = false;
+            break;
+          }
+          mbar_arrive_expect_tx(full_bar(stage), uint32_t(stage_bytes));
+          const uint32_t dst = smem_base + uint32_t(stage * stage_bytes);
+          tma_load_2d(dst, &tmX, full_bar(stage), kb * 64, int(row0));
+          for (int q = 0; q < g.parts; ++q)
+            tma_load_3d(dst + kXBytes + q * kPBytes, &tmP, full_bar(stage), 0, kb * 64, q * g.n + a);
+          ++iter;
+          if (++stage == g.stages) { stage = 0; phase ^= 1u; }
+        }
+      }
+      __syncwarp();
+    } else if (warp == 1) {
+      // ---------------- MMA issuer: X tile (K-major) x the adapter's rows (MN-major, a part per 64 columns)
+      if (lane == 0 && ok) {
+        const uint32_t id = tc::idesc(1, 1, 0, 1, 128, acc_cols);
+        for (int j = 0, in_seg = 0; j < nb; ++j) {
+          const uint32_t b = seg & 1u;
+          if (in_seg == 0 && !mbar_try_wait(acc_empty(b), ((seg >> 1) & 1u) ^ 1u) &&
+              !mbar_wait(acc_empty(b), ((seg >> 1) & 1u) ^ 1u, wc)) {
+            ok = false;
+            break;
+          }
+          if (!mbar_try_wait(full_bar(stage), phase) && !mbar_wait(full_bar(stage), phase, wc)) {
+            ok = false;
+            break;
+          }
+          fence_after();
+          const uint32_t st = smem_base + uint32_t(stage * stage_bytes);
+          const uint64_t ad = sdesc(st, 16u, 1024u, kSwizzle128B);
+          const uint64_t bd = sdesc(st + kXBytes, kPBytes, 1024u, kSwizzle128B);
+          const uint32_t d = tmem_base + b * acc_cols;
+#pragma unroll
+          for (int kk = 0; kk < 4; ++kk)
+            mma_f16(d, ad + kk * 2, bd + kk * (2048 >> 4), id, (in_seg | kk) != 0 ? 1u : 0u);
+          issued = true;
+          mma_commit(empty_bar(stage));
+          if (++stage == g.stages) { stage = 0; phase ^= 1u; }
+          if (++in_seg == seg_kb || j == nb - 1) {
+            mma_commit(acc_full(b));
+            ++seg;
+            in_seg = 0;
+          }
+        }
+      }
+      __syncwarp();
+    } else {
+      // ---------------- sums of the segments and of the parts; after the last segment's MMAs every
+      // load of the item has been read, so the sums may take the ring's place
+      const int q = warp & 3;
+      float u[64];
+#pragma unroll
+      for (int i = 0; i < 64; ++i) u[i] = 0.f;
+      const int nseg = (nb + seg_kb - 1) / seg_kb;
+      for (int j = 0; j < nseg && ok; ++j) {
+        const uint32_t b = seg & 1u;
+        const bool got = mbar_wait(acc_full(b), (seg >> 1) & 1u, wc);
+        if (!__all_sync(0xffffffffu, got)) {
+          ok = false;
+          break;
+        }
+        fence_after();
+        const uint32_t ta = tmem_base + (uint32_t(q * 32) << 16) + b * acc_cols;
+        for (int p = 0; p < g.parts; ++p) {
+#pragma unroll
+          for (int c = 0; c < 2; ++c) {
+            float v[32];
+            tmem_ld32(ta + uint32_t(p * 64 + c * 32), v);
+#pragma unroll
+            for (int i = 0; i < 32; ++i) u[c * 32 + i] += v[i];
+          }
+        }
+        fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(acc_empty(b));
+        ++seg;
+      }
+      if (ok) {
+        const int row = q * 32 + lane;
+#pragma unroll
+        for (int c = 0; c < 16; ++c)
+          *reinterpret_cast<float4*>(red + red_at(row, 4 * c)) =
+              make_float4(u[4 * c], u[4 * c + 1], u[4 * c + 2], u[4 * c + 3]);
+      }
+    }
+    __syncwarp();
+    cluster_sync();  // every CTA's sums are in its shared memory
+    const int rows_per = kSlotRows / ks;
+    const uint32_t red_s = smem_u32(red);
+    for (int e = threadIdx.x; e < rows_per * 8; e += kShrinkThreads) {
+      const int row = rank * rows_per + e / 8, ch = e % 8;
+      const int64_t tok = row0 + row;
+      float v[8] = {};
+      if (tok < g.N && g.plan[g.p.tok_slot + tok] == s) {
+        const uint32_t o0 = red_s + 4u * uint32_t(red_at(row, ch * 8));
+        const uint32_t o1 = red_s + 4u * uint32_t(red_at(row, ch * 8 + 4));
+        for (int j = 0; j < ks; ++j) {
+          const float4 x = ld_shared_cluster_f32x4(mapa_shared(o0, uint32_t(j)));
+          const float4 y = ld_shared_cluster_f32x4(mapa_shared(o1, uint32_t(j)));
+          v[0] += x.x; v[1] += x.y; v[2] += x.z; v[3] += x.w;
+          v[4] += y.x; v[5] += y.y; v[6] += y.z; v[7] += y.w;
+        }
+        if (g.marks[a]) {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) v[i] = __int_as_float(0x7fffffff);
+        }
+      }
+      __nv_bfloat16 o[8][3];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) split3(v[i], o[i]);
+#pragma unroll
+      for (int q = 0; q < kParts; ++q) {
+        if (q < g.parts) {
+          __align__(16) __nv_bfloat16 w[8];
+#pragma unroll
+          for (int i = 0; i < 8; ++i) w[i] = o[i][q];
+          if (LOCA_CHECK(s, g.p.smax))
+            *reinterpret_cast<uint4*>(g.out + ((int64_t(q) * g.p.smax + s) * kSlotRows + row) * kMaxK + ch * 8) =
+                *reinterpret_cast<const uint4*>(w);
+        }
+      }
+    }
+    fence_proxy_async_smem();  // the ring's next loads come after these accesses
+    __syncwarp();
+    cluster_sync();
+  }
+  if (warp == 1 && lane == 0 && issued) {
+    mma_commit(drain_bar);
+    mbar_drain(drain_bar, 0, kDrainLimitNs);
+  }
+  if (warp == 0 && lane == 0) {  // copies in flight when a role gave up
+    const uint32_t n = uint32_t(g.stages);
+    for (uint32_t i = iter > n ? iter - n : 0u; i < iter; ++i)
+      mbar_drain(full_bar(int(i % n)), (i / n) & 1u, kDrainLimitNs);
+  }
+  __syncwarp();
+  fence_before();
+  __syncthreads();
+  fence_after();
+  if (warp == 1) tmem_dealloc(tmem_base, cols);
+}
+
+// ------------------------------------------------------------------ few tokens
+// D[o, n] = sum_k W[o, k] X[n, k] + (slots)  with the output channels as M = 128 and up to 128 tokens
+// as N, so that a step of 1 to 64 tokens reads W once at full tiles.  The k axis (and the slots
+// behind it) is split over a cluster of up to 8 CTAs, which add their sums through distributed
+// shared memory in rank order: d_out / 128 tiles alone would keep 28 of 152 SMs busy at
+// d_out = 3584.  The loads of W and X do not wait for k_adapter_shrink; those of U do.
+constexpr int kFewThreads = 192;
+constexpr int kWBytes = 128 * 64 * 2;
+
+struct FewGeo {
+  int64_t N, d, o;       // tokens, k, output channels
+  int nt;                // tokens per tile (a multiple of 16, at most 128)
+  int stages;
+  int ksteps;            // MMA steps of 16 per slot
+  const int32_t* plan;
+  int64_t tile_base, adapter;
+  __nv_bfloat16* Y;
+  int64_t ldy;
+  int32_t* status;
+  int32_t* abort_flag;
+  unsigned long long limit_ns;
+};
+int few_ring(int nt, int stages) {
+  const int b = stages * (kWBytes + nt * 128);
+  return b > nt * 512 ? b : nt * 512;
+}
+int few_smem(int nt, int stages) { return few_ring(nt, stages) + 512 + 1024; }
+
+template <bool kWmn>
+__global__ void __launch_bounds__(kFewThreads, 1)
+    k_adapter_few(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUtensorMap tmX,
+                  const __grid_constant__ CUtensorMap tmB, const __grid_constant__ CUtensorMap tmU,
+                  const __grid_constant__ FewGeo g) {
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  const int stage_bytes = kWBytes + g.nt * 128;
+  const int ring = g.stages * stage_bytes > g.nt * 512 ? g.stages * stage_bytes : g.nt * 512;
+  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + ring);
+  const uint32_t bar_base = smem_u32(bars);
+  constexpr int kBarStages = 12;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 * kBarStages + 1);
+  auto full_bar = [&](int s) { return bar_base + 8u * s; };
+  auto empty_bar = [&](int s) { return bar_base + 8u * (kBarStages + s); };
+  const uint32_t acc_full = bar_base + 8u * (2 * kBarStages);
+  float* red = reinterpret_cast<float*>(smem);  // [token][128 channels]
+
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t smem_base = smem_u32(smem);
+  const WaitCtl wc{g.status, g.abort_flag, g.limit_ns};
+  const int ks = int(cluster_nctarank()), rank = int(cluster_ctarank());
+  const int o0 = int(cluster_id_x()) * 128;
+  const int64_t tile = blockIdx.y;
+  const int64_t n0 = tile * g.nt;
+  const uint32_t cols = g.nt <= 32 ? 32u : g.nt <= 64 ? 64u : 128u;
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < kBarStages; ++s) {
+      mbar_init(full_bar(s), 1);
+      mbar_init(empty_bar(s), 1);
+    }
+    mbar_init(acc_full, 1);
+    mbar_init_fence();
+    prefetch_tensormap(&tmW);
+    prefetch_tensormap(&tmX);
+    prefetch_tensormap(&tmB);
+    prefetch_tensormap(&tmU);
+  }
+  if (warp == 1) tmem_alloc(smem_u32(tmem_slot), cols);
+  fence_before();
+  __syncthreads();
+  fence_after();
+  const uint32_t tmem_base = *tmem_slot;
+  const int nkb = int((g.d + 63) / 64);
+  const int slot0 = g.plan[g.tile_base + tile];
+  const int steps = nkb + g.plan[g.tile_base + tile + 1] - slot0;
+  const int per = (steps + ks - 1) / ks;
+  const int j0 = rank * per < steps ? rank * per : steps;
+  const int j1 = j0 + per < steps ? j0 + per : steps;
+  uint32_t iter = 0;
+
+  if (warp == 0) {
+    if (lane == 0) {
+      int stage = 0;
+      uint32_t phase = 0;
+      bool waited = false;
+      for (int j = j0; j < j1; ++j) {
+        if (!mbar_try_wait(empty_bar(stage), phase ^ 1u) && !mbar_wait(empty_bar(stage), phase ^ 1u, wc)) break;
+        mbar_arrive_expect_tx(full_bar(stage), uint32_t(stage_bytes));
+        const uint32_t a = smem_base + uint32_t(stage * stage_bytes), b = a + kWBytes;
+        if (j < nkb) {
+          if (kWmn) {
+            tma_load_2d(a, &tmW, full_bar(stage), o0, j * 64);
+            tma_load_2d(a + kWBytes / 2, &tmW, full_bar(stage), o0 + 64, j * 64);
+          } else {
+            tma_load_2d(a, &tmW, full_bar(stage), j * 64, o0);
+          }
+          tma_load_2d(b, &tmX, full_bar(stage), j * 64, int(n0));
+        } else {
+          if (!waited) {
+            wait_for_previous();  // U
+            waited = true;
+          }
+          const int s = slot0 + j - nkb;
+          tma_load_3d(a, &tmB, full_bar(stage), 0, o0, g.plan[g.adapter + s]);
+          tma_load_2d(b, &tmU, full_bar(stage), 0, s * kSlotRows);
+        }
+        ++iter;
+        if (++stage == g.stages) { stage = 0; phase ^= 1u; }
+      }
+      if (!waited) wait_for_previous();
+    }
+    __syncwarp();
+  } else if (warp == 1) {
+    if (lane == 0) {
+      int stage = 0;
+      uint32_t phase = 0;
+      const uint32_t id = tc::idesc(1, 1, kWmn ? 1 : 0, 0, 128, uint32_t(g.nt));
+      const uint32_t idx = tc::idesc(1, 1, 0, 0, 128, uint32_t(g.nt));
+      for (int j = j0; j < j1; ++j) {
+        if (!mbar_try_wait(full_bar(stage), phase) && !mbar_wait(full_bar(stage), phase, wc)) break;
+        fence_after();
+        const uint32_t st = smem_base + uint32_t(stage * stage_bytes);
+        const uint64_t ak = sdesc(st, 16u, 1024u, kSwizzle128B);
+        const uint64_t bk = sdesc(st + kWBytes, 16u, 1024u, kSwizzle128B);
+        if (j < nkb) {
+          const uint64_t ad = kWmn ? sdesc(st, kWBytes / 2, 1024u, kSwizzle128B) : ak;
+#pragma unroll
+          for (int kk = 0; kk < 4; ++kk)
+            mma_f16(tmem_base, ad + kk * (kWmn ? 2048 >> 4 : 2), bk + kk * 2, id, j > j0 || kk > 0 ? 1u : 0u);
+        } else {
+          for (int kk = 0; kk < g.ksteps; ++kk)
+            mma_f16(tmem_base, ak + kk * 2, bk + kk * 2, idx, j > j0 || kk > 0 ? 1u : 0u);
+        }
+        mma_commit(empty_bar(stage));
+        if (++stage == g.stages) { stage = 0; phase ^= 1u; }
+      }
+      // completes once every MMA issued above has; the epilogue and the end of the kernel wait for it
+      mma_commit(acc_full);
+    }
+    __syncwarp();
+  } else {
+    const int q = warp & 3;
+    const bool got = j1 > j0 && mbar_wait(acc_full, 0, wc);
+    const bool all = __all_sync(0xffffffffu, got);
+    fence_after();
+    for (int c = 0; c < g.nt / 16; ++c) {
+      float v[16];
+      if (all) {
+        tmem_ld16(tmem_base + (uint32_t(q * 32) << 16) + uint32_t(c * 16), v);
+      } else {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) v[i] = 0.f;
+      }
+#pragma unroll
+      for (int i = 0; i < 16; ++i) red[(c * 16 + i) * 128 + q * 32 + lane] = v[i];
+    }
+    fence_before();
+    __syncwarp();
+  }
+  cluster_sync();
+  fence_after();
+  if (warp >= 2) {
+    const int i = (warp - 2) * 32 + lane;
+    const int64_t o = o0 + i;
+    const uint32_t red_s = smem_u32(red);
+    const int nt = int(g.N - n0 < g.nt ? g.N - n0 : g.nt);
+    for (int t = rank; t < nt; t += ks) {
+      float y = 0.f;
+      for (int j = 0; j < ks; ++j) y += ld_shared_cluster_f32(mapa_shared(red_s + 4u * uint32_t(t * 128 + i), uint32_t(j)));
+      if (o < g.o && LOCA_CHECK(n0 + t, g.N)) g.Y[(n0 + t) * g.ldy + o] = __float2bfloat16_rn(y);
+    }
+  }
+  if (warp == 0 && lane == 0) {
+    const uint32_t n = uint32_t(g.stages);
+    for (uint32_t i = iter > n ? iter - n : 0u; i < iter; ++i)
+      mbar_drain(full_bar(int(i % n)), (i / n) & 1u, kDrainLimitNs);
+  }
+  if (warp == 1 && lane == 0) mbar_drain(acc_full, 0, kDrainLimitNs);
+  __syncwarp();
+  fence_before();
+  cluster_sync();  // no CTA leaves while its peers read its sums
+  fence_after();
+  if (warp == 1) tmem_dealloc(tmem_base, cols);
+}
+
+// ------------------------------------------------------------------ many tokens
+struct AdapterExt {
+  static constexpr bool kOn = true;
+  const int32_t* plan;
+  int64_t tile_base, pair_count, pair_ad, pair_s0, pair_s1;
+  int none_row;  // past the last slot: the loads fill zeros
+  int nsteps;
+
+  __device__ int ksteps() const { return nsteps; }
+  __device__ int entries(int m) const { return plan[pair_count + m]; }
+  __device__ void entry(int m, int j, uint32_t rank, int& a_row, int& block) const {
+    const int at = plan[tile_base + 2 * int64_t(m)] + j;
+    const int s = plan[(rank ? pair_s1 : pair_s0) + at];
+    a_row = s < 0 ? none_row : s * kSlotRows;
+    block = plan[pair_ad + at];
+  }
+};
+
+struct EpiRows {
+  __device__ __forceinline__ void operator()(const gp::Tile&, float (&v)[128], int row, int col0, int lane, uint8_t* box,
+                                             const CUtensorMap* out) const {
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
+      gp::store_box_bf16(box, out, lane, col0 + 64 * b, row - lane, [&](int i) { return v[64 * b + i]; });
+  }
+};
+
+// ------------------------------------------------------------------ dA and dB: channels x k sums over tokens
+// One item per (adapter, 128 channels, range of its slots): M = channels, N = 64 columns per part of U
+// or T, K = the slot's 128 tokens in two stages, both operands MN-major as they lie in memory.  The
+// segments (512 tokens) are added in registers.  A slot whose tile also holds other tokens has those
+// rows of X (or dY) zeroed in shared memory first: their U is zero, but a product with whatever else
+// stands there (infinities, NaN) need not be.
+constexpr int kGradThreads = 224;
+constexpr int kGradStages = 5;
+constexpr int kGradStageBytes = kXBytes + kParts * kPBytes;  // 40 KB
+constexpr int kGradSeg = 8;
+constexpr int kGradSmem = kGradStages * kGradStageBytes + 512 + 1024;
+
+struct GradGeo {
+  int64_t N, d;     // tokens, channels
+  int n, kp, ctiles, ranges;
+  const int32_t* plan;
+  PlanLay p;
+  float* part;      // ranges x n x d x kp
+  int32_t* status;
+  int32_t* abort_flag;
+  unsigned long long limit_ns;
+};
+
+__global__ void __launch_bounds__(kGradThreads, 1)
+    k_adapter_grad(const __grid_constant__ CUtensorMap tmS, const __grid_constant__ CUtensorMap tmU,
+                   const __grid_constant__ GradGeo g) {
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + kGradStages * kGradStageBytes);
+  const uint32_t bar_base = smem_u32(bars);
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 3 * kGradStages + 5);
+  auto full_bar = [&](int s) { return bar_base + 8u * s; };
+  auto empty_bar = [&](int s) { return bar_base + 8u * (kGradStages + s); };
+  auto ready_bar = [&](int s) { return bar_base + 8u * (2 * kGradStages + s); };
+  auto acc_full = [&](uint32_t b) { return bar_base + 8u * (3 * kGradStages + b); };
+  auto acc_empty = [&](uint32_t b) { return bar_base + 8u * (3 * kGradStages + 2 + b); };
+  const uint32_t drain_bar = bar_base + 8u * (3 * kGradStages + 4);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t smem_base = smem_u32(smem);
+  const WaitCtl wc{g.status, g.abort_flag, g.limit_ns};
+  constexpr uint32_t kCols = 64 * kParts;
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < kGradStages; ++s) {
+      mbar_init(full_bar(s), 1);
+      mbar_init(empty_bar(s), 1);
+      mbar_init(ready_bar(s), 1);
+    }
+    for (uint32_t b = 0; b < 2; ++b) {
+      mbar_init(acc_full(b), 1);
+      mbar_init(acc_empty(b), 4);
+    }
+    mbar_init(drain_bar, 1);
+    mbar_init_fence();
+    prefetch_tensormap(&tmS);
+    prefetch_tensormap(&tmU);
+  }
+  if (warp == 1) tmem_alloc(smem_u32(tmem_slot), 512);
+  fence_before();
+  __syncthreads();
+  fence_after();
+  const uint32_t tmem_base = *tmem_slot;
+  const int per_a = g.ctiles * g.ranges;
+  const int items = g.n * per_a;
+  uint32_t iter = 0;
+  struct Item {
+    int a, ct, range, s0, s1;  // s0 .. s1: places in the adapter's list of slots
+  };
+  auto item_of = [&](int it) {
+    Item w;
+    w.a = it / per_a;
+    const int r = it - w.a * per_a;
+    w.range = r / g.ctiles;  // channel tiles fastest: CTAs at work share a range's U or T
+    w.ct = r - w.range * g.ctiles;
+    const int b0 = g.plan[g.p.ad_off + w.a], b1 = g.plan[g.p.ad_off + w.a + 1];
+    const int per = (b1 - b0 + g.ranges - 1) / g.ranges;
+    w.s0 = b0 + w.range * per < b1 ? b0 + w.range * per : b1;
+    w.s1 = w.s0 + per < b1 ? w.s0 + per : b1;
+    return w;
+  };
+
+  if (warp == 0) {
+    if (lane == 0) {
+      int stage = 0;
+      uint32_t phase = 0;
+      bool ok = true;
+      for (int it = blockIdx.x; it < items && ok; it += gridDim.x) {
+        const Item w = item_of(it);
+        for (int l = w.s0; l < w.s1 && ok; ++l) {
+          const int s = g.plan[g.p.ad_slots + l];
+          const int row = g.plan[g.p.tile + s] * kTile;
+          for (int h = 0; h < 2; ++h) {
+            if (!mbar_try_wait(empty_bar(stage), phase ^ 1u) && !mbar_wait(empty_bar(stage), phase ^ 1u, wc)) {
+              ok = false;
+              break;
+            }
+            mbar_arrive_expect_tx(full_bar(stage), uint32_t(kGradStageBytes));
+            const uint32_t dst = smem_base + uint32_t(stage * kGradStageBytes);
+            tma_load_2d(dst, &tmS, full_bar(stage), w.ct * 128, row + 64 * h);
+            tma_load_2d(dst + kXBytes / 2, &tmS, full_bar(stage), w.ct * 128 + 64, row + 64 * h);
+            for (int q = 0; q < kParts; ++q)
+              tma_load_3d(dst + kXBytes + q * kPBytes, &tmU, full_bar(stage), 0, s * kSlotRows + 64 * h, q);
+            ++iter;
+            if (++stage == kGradStages) { stage = 0; phase ^= 1u; }
+          }
+        }
+      }
+    }
+    __syncwarp();
+  } else if (warp == 6) {
+    // ---------------- rows of other tokens: zero
+    int stage = 0;
+    uint32_t phase = 0;
+    bool ok = true;
+    for (int it = blockIdx.x; it < items && ok; it += gridDim.x) {
+      const Item w = item_of(it);
+      for (int l = w.s0; l < w.s1 && ok; ++l) {
+        const int s = g.plan[g.p.ad_slots + l];
+        const int64_t row = int64_t(g.plan[g.p.tile + s]) * kTile;
+        const int64_t in_tile = g.N - row < kTile ? g.N - row : kTile;
+        const bool mixed = g.plan[g.p.count + s] < in_tile;
+        for (int h = 0; h < 2; ++h) {
+          const bool got = mbar_wait(full_bar(stage), phase, wc);
+          if (!__all_sync(0xffffffffu, got)) {
+            ok = false;
+            break;
+          }
+          if (mixed) {
+            uint8_t* box = smem + stage * kGradStageBytes;
+            for (int r = lane; r < 64; r += 32) {
+              const int64_t tok = row + 64 * h + r;
+              if (tok < g.N && g.plan[g.p.tok_slot + tok] != s) {
+#pragma unroll
+                for (int u = 0; u < 8; ++u) {
+                  *reinterpret_cast<uint4*>(box + r * 128 + u * 16) = make_uint4(0, 0, 0, 0);
+                  *reinterpret_cast<uint4*>(box + kXBytes / 2 + r * 128 + u * 16) = make_uint4(0, 0, 0, 0);
+                }
+              }
+            }
+            fence_proxy_async_smem();
+          }
+          __syncwarp();
+          if (lane == 0) mbar_arrive(ready_bar(stage));
+          if (++stage == kGradStages) { stage = 0; phase ^= 1u; }
+        }
+      }
+    }
+  } else if (warp == 1) {
+    if (lane == 0) {
+      int stage = 0;
+      uint32_t phase = 0, seg = 0;
+      bool ok = true, issued = false;
+      constexpr uint32_t kId = tc::idesc(1, 1, 1, 1, 128, kCols);
+      for (int it = blockIdx.x; it < items && ok; it += gridDim.x) {
+        const Item w = item_of(it);
+        const int nb = 2 * (w.s1 - w.s0);
+        for (int j = 0, in_seg = 0; j < nb; ++j) {
+          const uint32_t b = seg & 1u;
+          if (in_seg == 0 && !mbar_try_wait(acc_empty(b), ((seg >> 1) & 1u) ^ 1u) &&
+              !mbar_wait(acc_empty(b), ((seg >> 1) & 1u) ^ 1u, wc)) {
+            ok = false;
+            break;
+          }
+          if ((!mbar_try_wait(full_bar(stage), phase) && !mbar_wait(full_bar(stage), phase, wc)) ||
+              (!mbar_try_wait(ready_bar(stage), phase) && !mbar_wait(ready_bar(stage), phase, wc))) {
+            ok = false;
+            break;
+          }
+          fence_after();
+          const uint32_t st = smem_base + uint32_t(stage * kGradStageBytes);
+          const uint64_t ad = sdesc(st, kXBytes / 2, 1024u, kSwizzle128B);
+          const uint64_t bd = sdesc(st + kXBytes, kPBytes, 1024u, kSwizzle128B);
+          const uint32_t d = tmem_base + b * 256u;
+#pragma unroll
+          for (int kk = 0; kk < 4; ++kk)
+            mma_f16(d, ad + kk * (2048 >> 4), bd + kk * (2048 >> 4), kId, (in_seg | kk) != 0 ? 1u : 0u);
+          issued = true;
+          mma_commit(empty_bar(stage));
+          if (++stage == kGradStages) { stage = 0; phase ^= 1u; }
+          if (++in_seg == kGradSeg || j == nb - 1) {
+            mma_commit(acc_full(b));
+            ++seg;
+            in_seg = 0;
+          }
+        }
+      }
+      if (issued) {
+        mma_commit(drain_bar);
+        mbar_drain(drain_bar, 0, kDrainLimitNs);
+      }
+    }
+    __syncwarp();
+  } else {
+    const int q = warp & 3;
+    uint32_t seg = 0;
+    bool ok = true;
+    for (int it = blockIdx.x; it < items && ok; it += gridDim.x) {
+      const Item w = item_of(it);
+      const int nseg = (2 * (w.s1 - w.s0) + kGradSeg - 1) / kGradSeg;
+      float u[64];
+#pragma unroll
+      for (int i = 0; i < 64; ++i) u[i] = 0.f;
+      for (int j = 0; j < nseg; ++j) {
+        const uint32_t b = seg & 1u;
+        const bool got = mbar_wait(acc_full(b), (seg >> 1) & 1u, wc);
+        if (!__all_sync(0xffffffffu, got)) {
+          ok = false;
+          break;
+        }
+        fence_after();
+        const uint32_t ta = tmem_base + (uint32_t(q * 32) << 16) + b * 256u;
+        for (int p = 0; p < kParts; ++p) {
+#pragma unroll
+          for (int c = 0; c < 2; ++c) {
+            float v[32];
+            tmem_ld32(ta + uint32_t(p * 64 + c * 32), v);
+#pragma unroll
+            for (int i = 0; i < 32; ++i) u[c * 32 + i] += v[i];
+          }
+        }
+        fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(acc_empty(b));
+        ++seg;
+      }
+      if (!ok) break;
+      const int64_t ch = int64_t(w.ct) * 128 + q * 32 + lane;
+      if (ch < g.d) {
+        float* to = g.part + ((int64_t(w.range) * g.n + w.a) * g.d + ch) * g.kp;
+#pragma unroll
+        for (int c = 0; c < 16; ++c)
+          if (4 * c < g.kp)
+            *reinterpret_cast<float4*>(to + 4 * c) = make_float4(u[4 * c], u[4 * c + 1], u[4 * c + 2], u[4 * c + 3]);
+      }
+    }
+  }
+  if (warp == 0 && lane == 0)
+    for (uint32_t i = iter > kGradStages ? iter - kGradStages : 0u; i < iter; ++i)
+      mbar_drain(full_bar(int(i % kGradStages)), (i / kGradStages) & 1u, kDrainLimitNs);
+  __syncwarp();
+  fence_before();
+  __syncthreads();
+  fence_after();
+  if (warp == 1) tmem_dealloc(tmem_base, 512);
+}
+
+template <class T>
+__global__ void __launch_bounds__(256)
+    k_adapter_join(const float* __restrict__ part, int ranges, int n, int64_t d, int k, int kp,
+                   const float* __restrict__ scale, T* __restrict__ out) {
+  const int64_t rows = int64_t(n) * d;
+  for (int64_t i = int64_t(blockIdx.x) * blockDim.x + threadIdx.x; i < rows * k; i += int64_t(gridDim.x) * blockDim.x) {
+    const int64_t row = i / k;
+    const int c = int(i - row * k);
+    float v = 0.f;
+    for (int r = 0; r < ranges; ++r) v += part[(int64_t(r) * rows + row) * kp + c];
+    if (scale) v *= scale[row / d];
+    if constexpr (sizeof(T) == 4) out[i] = v;
+    else out[i] = __float2bfloat16_rn(v);
+  }
+}
+
+// ------------------------------------------------------------------ host side
+struct AdapterWs {
+  size_t flags, u, t, part, total;
+  int parts;
+  int ranges_in, ranges_out;
+};
+// Token ranges of dA / dB: enough items for two rounds of the SMs, at most one per token tile.
+int grad_ranges(int n, int64_t d, int64_t tiles) {
+  const int64_t items = int64_t(n) * ((d + 127) / 128);
+  int64_t r = (2 * int64_t(sm_count()) + items - 1) / items;
+  if (r > tiles) r = tiles;
+  return int(r < 1 ? 1 : r);
+}
+AdapterWs adapter_ws(int64_t N, int64_t d_in, int64_t d_out, int k, int n, bool backward) {
+  AdapterWs w{};
+  const PlanLay p = plan_lay(N, n);
+  w.parts = backward ? kParts : 1;
+  const size_t one = align256(2 * kSlotElems * size_t(p.smax < 1 ? 1 : p.smax) * size_t(w.parts));
+  size_t at = 256;
+  w.u = at; at += one;
+  if (backward) {
+    w.t = at; at += one;
+    w.ranges_in = grad_ranges(n, d_in, p.tiles);
+    w.ranges_out = grad_ranges(n, d_out, p.tiles);
+    const size_t kp = size_t(k_padded(k));
+    const size_t pi = size_t(w.ranges_in) * n * size_t(d_in) * kp, po = size_t(w.ranges_out) * n * size_t(d_out) * kp;
+    w.part = at; at += align256(4 * (pi > po ? pi : po));
+  }
+  w.total = at;
+  return w;
+}
+
+struct Call {
+  int64_t N;
+  int n, k, kp;
+  PlanLay p;
+  const int32_t* plan;
+  int32_t* status;
+  int32_t* abort_flag;
+  cudaStream_t s;
+};
+
+template <class... P, class... A>
+cudaError_t launch_cluster(void (*kernel)(P...), dim3 grid, int threads, int smem, int cluster, bool after,
+                           cudaStream_t s, A... args) {
+  cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  if (e != cudaSuccess) return e;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3(unsigned(threads));
+  cfg.dynamicSmemBytes = size_t(smem);
+  cfg.stream = s;
+  cudaLaunchAttribute at[2];
+  at[0].id = cudaLaunchAttributeClusterDimension;
+  at[0].val.clusterDim.x = unsigned(cluster);
+  at[0].val.clusterDim.y = 1;
+  at[0].val.clusterDim.z = 1;
+  at[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[1].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = at;
+  cfg.numAttrs = after ? 2 : 1;
+  return cudaLaunchKernelEx(&cfg, kernel, args...);
+}
+
+// Largest power of two up to 8 that keeps items * ks within the SMs and leaves each CTA two k-blocks.
+int cluster_split(int64_t items, int64_t blocks) {
+  int ks = 1;
+  while (ks < 8 && items * ks * 2 <= sm_count() && blocks >= 4 * ks) ks *= 2;
+  return ks;
+}
+
+// U (or T) of every slot: rows X (N x d) against the packed operand P.
+cudaError_t shrink(const Call& c, const void* X, int64_t ldx, int64_t d, const __nv_bfloat16* P,
+                   const int32_t* marks, int parts, void* out) {
+  CUtensorMap mx, mp;
+  if (!gp::map_kmajor(&mx, X, d, c.N, ldx) ||
+      !gp::map_3d(&mp, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, P, c.kp, d, int64_t(kParts) * c.n, c.kp, d * c.kp, 64, 64))
+    return cudaErrorInvalidValue;
+  ShrinkGeo g{};
+  g.X = static_cast<const __nv_bfloat16*>(X);
+  g.ldx = ldx;
+  g.N = c.N;
+  g.d = d;
+  g.P = P;
+  g.marks = marks;
+  g.n = c.n;
+  g.kp = c.kp;
+  g.parts = parts;
+  // few tokens: a small ring, so that k_adapter_few's CTAs fit beside these
+  g.stages = parts > 1 ? 5 : c.N <= kTile ? 3 : kMaxStages;
+  g.plan = c.plan;
+  g.p = c.p;
+  g.out = static_cast<__nv_bfloat16*>(out);
+  g.status = c.status;
+  g.abort_flag = c.abort_flag;
+  g.limit_ns = wait_limit_ns();
+  // slots are known to the device only: between one per tile and smax
+  int64_t guess = c.p.tiles > c.n ? c.p.tiles : c.n;
+  if (guess > c.p.smax) guess = c.p.smax;
+  const int ks = cluster_split(guess, (d + 63) / 64);
+  int64_t clusters = sm_count() / ks;
+  if (clusters > c.p.smax) clusters = c.p.smax;
+  return launch_cluster(k_adapter_shrink, dim3(unsigned(clusters * ks)), kShrinkThreads, shrink_smem(parts, g.stages), ks,
+                        false, c.s, mx, mp, g);
+}
+
+// Y = X W^T + U (packed B)^T (kWmn false: W is o x d) or dX = dY W + T (packed A)^T (true: W is d x o).
+template <bool kWmn>
+cudaError_t project(const Call& c, const void* X, int64_t ldx, int64_t d, const void* W, int64_t o,
+                    const __nv_bfloat16* P, const void* U, void* Y, int64_t ldy) {
+  const int64_t slots = c.p.smax;
+  const int64_t tiles = ((c.N + gp::TM - 1) / gp::TM) * ((o + gp::TN - 1) / gp::TN);
+  const bool few = c.N <= kTile || 2 * tiles < sm_count() / 2;
+  CUtensorMap mw, mx, mb, mu;
+  if (kWmn ? !gp::map_mnmajor(&mw, W, o, d, o) : !gp::map_kmajor(&mw, W, d, o, d)) return cudaErrorInvalidValue;
+  if (!gp::map_3d(&mb, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, P, c.kp, o, c.n, c.kp, o * c.kp, 64, 128))
+    return cudaErrorInvalidValue;
+  if (few) {
+    FewGeo g{};
+    g.N = c.N;
+    g.d = d;
+    g.o = o;
+    g.nt = c.N >= kTile ? kTile : int((c.N + 15) / 16 * 16);
+    g.stages = 110 * 1024 / (kWBytes + g.nt * 128);
+    g.ksteps = (c.k + 15) / 16;
+    g.plan = c.plan;
+    g.tile_base = c.p.tile_base;
+    g.adapter = c.p.adapter;
+    g.Y = static_cast<__nv_bfloat16*>(Y);
+    g.ldy = ldy;
+    g.status = c.status;
+    g.abort_flag = c.abort_flag;
+    g.limit_ns = wait_limit_ns();
+    if (!gp::map_2d(&mx, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, X, d, c.N, ldx, 64, g.nt) ||
+        !gp::map_2d(&mu, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, U, kMaxK, slots * kSlotRows, kMaxK, 64, g.nt))
+      return cudaErrorInvalidValue;
+    const int64_t ot = (o + 127) / 128, nt = (c.N + g.nt - 1) / g.nt;
+    const int ks = cluster_split(ot * nt, (d + 63) / 64);
+    return launch_cluster(k_adapter_few<kWmn>, dim3(unsigned(ot * ks), unsigned(nt)), kFewThreads,
+                          few_smem(g.nt, g.stages), ks, true, c.s, mw, mx, mb, mu, g);
+  }
+  CUtensorMap mo;
+  if (!gp::map_kmajor(&mx, X, d, c.N, ldx) || !gp::map_out_bf16(&mo, Y, o, c.N, ldy) ||
+      !gp::map_2d(&mu, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, U, kMaxK, slots * kSlotRows, kMaxK, 64, 128))
+    return cudaErrorInvalidValue;
+  gp::Geo g{};
+  g.m_tiles = int((c.N + gp::TM - 1) / gp::TM);
+  g.n_tiles = int((o + gp::TN - 1) / gp::TN);
+  g.nkb = int((d + gp::BK - 1) / gp::BK);
+  g.splits = 1;
+  g.seg_kb = 64;
+  g.group = 16;
+  g.status = c.status;
+  g.abort_flag = c.abort_flag;
+  g.limit_ns = wait_limit_ns();
+  const AdapterExt ext{c.plan, c.p.tile_base, c.p.pair_count, c.p.pair_ad, c.p.pair_s0, c.p.pair_s1,
+                       int(slots * kSlotRows), (c.k + 15) / 16};
+  return gp::launch<false, kWmn>(mx, mw, mu, mb, mo, g, EpiRows{}, ext, c.s);
+}
+
+cudaError_t grad(const Call& c, const void* S, int64_t lds, int64_t d, const void* U, int ranges, float* part,
+                 const float* scale, void* out, int dtype) {
+  CUtensorMap ms, mu;
+  if (!gp::map_mnmajor(&ms, S, d, c.N, lds) ||
+      !gp::map_3d(&mu, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, U, kMaxK, c.p.smax * kSlotRows, kParts, kMaxK,
+                  c.p.smax * int64_t(kSlotElems), 64, 64))
+    return cudaErrorInvalidValue;
+  GradGeo g{};
+  g.N = c.N;
+  g.d = d;
+  g.n = c.n;
+  g.kp = c.kp;
+  g.ctiles = int((d + 127) / 128);
+  g.ranges = ranges;
+  g.plan = c.plan;
+  g.p = c.p;
+  g.part = part;
+  g.status = c.status;
+  g.abort_flag = c.abort_flag;
+  g.limit_ns = wait_limit_ns();
+  cudaError_t e = cudaFuncSetAttribute(k_adapter_grad, cudaFuncAttributeMaxDynamicSharedMemorySize, kGradSmem);
+  if (e != cudaSuccess) return e;
+  const int64_t items = int64_t(c.n) * g.ctiles * ranges;
+  const int blocks = int(items < sm_count() ? items : sm_count());
+  k_adapter_grad<<<blocks, kGradThreads, kGradSmem, c.s>>>(ms, mu, g);
+  e = cudaGetLastError();
+  if (e != cudaSuccess) return e;
+  const int64_t values = int64_t(c.n) * d * c.k;
+  const unsigned jb = unsigned(values / 256 + 1 < 4 * sm_count() ? values / 256 + 1 : 4 * sm_count());
+  if (dtype == LOCA_F32)
+    k_adapter_join<float><<<jb, 256, 0, c.s>>>(part, ranges, c.n, d, c.k, c.kp, scale, static_cast<float*>(out));
+  else
+    k_adapter_join<__nv_bfloat16><<<jb, 256, 0, c.s>>>(part, ranges, c.n, d, c.k, c.kp, scale,
+                                                       static_cast<__nv_bfloat16*>(out));
+  return cudaGetLastError();
+}
+
+Call call_of(int64_t N, int n, int k, const void* plan, void* workspace, int32_t* status, cudaStream_t s) {
+  Call c{};
+  c.N = N;
+  c.n = n;
+  c.k = k;
+  c.kp = k_padded(k);
+  c.p = plan_lay(N, n);
+  c.plan = static_cast<const int32_t*>(plan);
+  c.status = status;
+  c.abort_flag = static_cast<int32_t*>(workspace);
+  c.s = s;
+  return c;
+}
+
+}  // namespace
+
+int adapter_max_k() { return kMaxK; }
+size_t adapter_packed_bytes(int n, int64_t d_in, int64_t d_out, int k) { return pack_lay(n, d_in, d_out, k).total; }
+size_t adapter_plan_bytes(int64_t N, int n) { return 4 * size_t(plan_lay(N, n).total); }
+size_t adapter_workspace_bytes(int64_t N, int64_t d_in, int64_t d_out, int k, int n, bool backward) {
+  return adapter_ws(N, d_in, d_out, k, n, backward).total;
+}
+
+cudaError_t launch_adapter_pack(const void* A, const void* B, int dtype, int n, int64_t d_in, int64_t d_out, int k,
+                                const float* scale, void* packed, cudaStream_t s) {
+  const PackLay p = pack_lay(n, d_in, d_out, k);
+  uint8_t* b = static_cast<uint8_t*>(packed);
+  __nv_bfloat16* pa = reinterpret_cast<__nv_bfloat16*>(b + p.a);
+  __nv_bfloat16* pb = reinterpret_cast<__nv_bfloat16*>(b + p.b);
+  float* ps = reinterpret_cast<float*>(b + p.scale);
+  int32_t* marks = reinterpret_cast<int32_t*>(b + p.marks);
+  const cudaError_t e = cudaMemsetAsync(marks, 0, 4 * size_t(n), s);
+  if (e != cudaSuccess) return e;
+  const int kp = k_padded(k);
+  const int64_t values = int64_t(n) * (d_in + d_out) * kp;
+  const unsigned blocks = unsigned(values / 256 + 1 < 8 * sm_count() ? values / 256 + 1 : 8 * sm_count());
+  if (dtype == LOCA_F32)
+    k_adapter_pack<float><<<blocks, 256, 0, s>>>(static_cast<const float*>(A), static_cast<const float*>(B), n, d_in,
+                                                 d_out, k, kp, scale, pa, pb, ps, marks);
+  else
+    k_adapter_pack<__nv_bfloat16><<<blocks, 256, 0, s>>>(static_cast<const __nv_bfloat16*>(A),
+                                                         static_cast<const __nv_bfloat16*>(B), n, d_in, d_out, k, kp,
+                                                         scale, pa, pb, ps, marks);
+  return cudaGetLastError();
+}
+
+cudaError_t launch_adapter_plan(const int32_t* ids, int64_t N, int n, void* plan, cudaStream_t s) {
+  const PlanLay p = plan_lay(N, n);
+  int32_t* pl = static_cast<int32_t*>(plan);
+  const unsigned tiles = unsigned(p.tiles);
+  k_plan_tiles<<<tiles, kTile, 0, s>>>(ids, N, n, pl, p, 0);
+  k_plan_scan<<<1, 1024, 0, s>>>(pl, p);
+  k_plan_tiles<<<tiles, kTile, 0, s>>>(ids, N, n, pl, p, 1);
+  k_plan_pairs<<<unsigned(p.pairs), kTile, 0, s>>>(pl, p);
+  k_plan_adapters<<<unsigned(n), 256, 0, s>>>(pl, p, n);
+  return cudaGetLastError();
+}
+
+cudaError_t launch_adapter_apply(const void* X, int64_t ldx, int64_t N, int64_t d_in, const void* W, int64_t d_out,
+                                 const void* packed, int n, int k, const void* plan, void* Y, int64_t ldy,
+                                 void* workspace, int32_t* status, cudaStream_t s) {
+  const Call c = call_of(N, n, k, plan, workspace, status, s);
+  const AdapterWs w = adapter_ws(N, d_in, d_out, k, n, false);
+  const PackLay pk = pack_lay(n, d_in, d_out, k);
+  const uint8_t* pb = static_cast<const uint8_t*>(packed);
+  uint8_t* ws = static_cast<uint8_t*>(workspace);
+  cudaError_t e = cudaMemsetAsync(workspace, 0, 4, s);
+  if (e != cudaSuccess) return e;
+  e = shrink(c, X, ldx, d_in, reinterpret_cast<const __nv_bfloat16*>(pb + pk.a),
+             reinterpret_cast<const int32_t*>(pb + pk.marks), 1, ws + w.u);
+  if (e != cudaSuccess) return e;
+  return project<false>(c, X, ldx, d_in, W, d_out, reinterpret_cast<const __nv_bfloat16*>(pb + pk.b), ws + w.u, Y, ldy);
+}
+
+cudaError_t launch_adapter_backward(const void* X, int64_t ldx, const void* dY, int64_t lddy, int64_t N, int64_t d_in,
+                                    const void* W, int64_t d_out, const void* packed, int n, int k, const void* plan,
+                                    void* dX, int64_t lddx, void* dA, void* dB, int grad_dtype, void* workspace,
+                                    int32_t* status, cudaStream_t s) {
+  const Call c = call_of(N, n, k, plan, workspace, status, s);
+  const AdapterWs w = adapter_ws(N, d_in, d_out, k, n, true);
+  const PackLay pk = pack_lay(n, d_in, d_out, k);
+  const uint8_t* pb = static_cast<const uint8_t*>(packed);
+  const __nv_bfloat16* pa = reinterpret_cast<const __nv_bfloat16*>(pb + pk.a);
+  const int32_t* marks = reinterpret_cast<const int32_t*>(pb + pk.marks);
+  const __nv_bfloat16* pB = reinterpret_cast<const __nv_bfloat16*>(pb + pk.b);
+  uint8_t* ws = static_cast<uint8_t*>(workspace);
+  float* part = reinterpret_cast<float*>(ws + w.part);
+  cudaError_t e = cudaMemsetAsync(workspace, 0, 4, s);
+  if (e != cudaSuccess) return e;
+  if (dB) {
+    e = shrink(c, X, ldx, d_in, pa, marks, kParts, ws + w.u);
+    if (e != cudaSuccess) return e;
+    e = grad(c, dY, lddy, d_out, ws + w.u, w.ranges_out, part, reinterpret_cast<const float*>(pb + pk.scale), dB,
+             grad_dtype);
+    if (e != cudaSuccess) return e;
+  }
+  if (dA || dX) {
+    e = shrink(c, dY, lddy, d_out, pB, marks, dA ? kParts : 1, ws + w.t);
+    if (e != cudaSuccess) return e;
+  }
+  if (dX) {
+    e = project<true>(c, dY, lddy, d_out, W, d_in, pa, ws + w.t, dX, lddx);
+    if (e != cudaSuccess) return e;
+  }
+  if (dA) e = grad(c, X, ldx, d_in, ws + w.t, w.ranges_in, part, nullptr, dA, grad_dtype);
+  return e;
+}
+
+}  // namespace loca

@@ -151,9 +151,10 @@ __device__ __forceinline__ void store_box_bf16(uint8_t* box, const CUtensorMap* 
 
 // Extension of the k axis: for row tile m, entries(m) further stages whose A rows come from the map
 // tmAx (row coordinate a_row of the CTA's 128 rows) and whose B rows from tmBx (b_row0 + the tile's
-// column, block b_block).  None here; the adapter projection has one.
+// column, block b_block), ksteps() MMA steps of 16 each.  None here; the adapter projection has one.
 struct NoExt {
   static constexpr bool kOn = false;
+  __device__ int ksteps() const { return 4; }
   __device__ int entries(int) const { return 0; }
   __device__ void entry(int, int, uint32_t, int&, int&) const {}
 };
@@ -309,8 +310,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
             for (int kk = 0; kk < BK / 16; ++kk)
               mma_f16_pair(d, a0 + so + kk * kAStep, b0 + so + kk * kBStep, kId, (in_seg | kk) != 0 ? 1u : 0u);
           } else {
-#pragma unroll
-            for (int kk = 0; kk < BK / 16; ++kk)
+            for (int kk = 0; kk < ext.ksteps(); ++kk)
               mma_f16_pair(d, a_kmaj + so + kk * 2, b_kmaj + so + kk * 2, kIdX, (in_seg | kk) != 0 ? 1u : 0u);
           }
           issued = true;

@@ -33,6 +33,25 @@ int check_head(int64_t N, int64_t V, int64_t d) {
   return LOCA_OK;
 }
 
+int check_adapter(int64_t N, int64_t d_in, int64_t d_out, int32_t k, int32_t n) {
+  if (N < 0 || N > (int64_t(1) << 22)) return fail(LOCA_ERR_SHAPE, "need 0 <= N <= 2^22, got %lld", (long long)N);
+  if (d_in < 8 || d_in > 65536 || d_in % 8 != 0 || d_out < 8 || d_out > 65536 || d_out % 8 != 0)
+    return fail(LOCA_ERR_SHAPE, "need 8 <= d_in, d_out <= 65536, multiples of 8, got %lld, %lld", (long long)d_in,
+                (long long)d_out);
+  if (k < 1 || k > adapter_max_k()) return fail(LOCA_ERR_SHAPE, "need 1 <= k <= %d, got %d", adapter_max_k(), k);
+  if (n < 1 || n > 65535) return fail(LOCA_ERR_SHAPE, "need 1 <= n <= 65535 adapters, got %d", n);
+  return LOCA_OK;
+}
+
+// A bf16 matrix that TMA reads or writes: pitch at least its columns, 16-byte rows.
+int check_rows(const void* p, int64_t pitch, int64_t cols, const char* name) {
+  if (pitch < cols)
+    return fail(LOCA_ERR_SHAPE, "row pitch of %s %lld is below its %lld columns", name, (long long)pitch, (long long)cols);
+  if (pitch % 8 != 0 || !aligned(p, 16))
+    return fail(LOCA_ERR_ALIGNMENT, "%s needs 16-byte alignment and a row pitch that is a multiple of 8", name);
+  return LOCA_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -107,6 +126,121 @@ int loca_head_loss_backward(const void* H, int64_t ldh, int64_t N, int64_t d, co
   const cudaError_t e = launch_head_loss_backward(H, ldh, N, d, W, V, y, w, lse, dloss, grad_scale, N > 0 ? dH : nullptr,
                                                   lddh, dW, workspace, status, static_cast<cudaStream_t>(stream));
   if (e != cudaSuccess) return cuda_fail(e, "loca_head_loss_backward launch");
+  return LOCA_OK;
+}
+
+int loca_adapter_packed_size(int32_t n, int64_t d_in, int64_t d_out, int32_t k, size_t* bytes) {
+  clear();
+  if (!bytes) return fail(LOCA_ERR_INVALID_ARG, "bytes is NULL");
+  const int rc = check_adapter(0, d_in, d_out, k, n);
+  if (rc != LOCA_OK) return rc;
+  *bytes = adapter_packed_bytes(n, d_in, d_out, k);
+  return LOCA_OK;
+}
+
+int loca_adapter_pack(const void* A, const void* B, int dtype, int32_t n, int64_t d_in, int64_t d_out, int32_t k,
+                      const float* scale, void* packed, void* stream) {
+  clear();
+  if (dtype != LOCA_F32 && dtype != LOCA_BF16) return fail(LOCA_ERR_UNSUPPORTED_DTYPE, "unknown dtype code %d", dtype);
+  const int rc = check_adapter(0, d_in, d_out, k, n);
+  if (rc != LOCA_OK) return rc;
+  if (!A || !B || !packed) return fail(LOCA_ERR_INVALID_ARG, "A, B and packed are required");
+  const size_t es = dtype == LOCA_F32 ? 4 : 2;
+  if (!aligned(A, es) || !aligned(B, es) || !aligned(scale, 4) || !aligned(packed, 256))
+    return fail(LOCA_ERR_ALIGNMENT, "A, B and scale need the alignment of their elements, packed 256 bytes");
+  const cudaError_t e =
+      launch_adapter_pack(A, B, dtype, n, d_in, d_out, k, scale, packed, static_cast<cudaStream_t>(stream));
+  if (e != cudaSuccess) return cuda_fail(e, "loca_adapter_pack launch");
+  return LOCA_OK;
+}
+
+int loca_adapter_plan_size(int64_t N, int32_t n, size_t* bytes) {
+  clear();
+  if (!bytes) return fail(LOCA_ERR_INVALID_ARG, "bytes is NULL");
+  const int rc = check_adapter(N, 8, 8, 1, n);
+  if (rc != LOCA_OK) return rc;
+  *bytes = adapter_plan_bytes(N, n);
+  return LOCA_OK;
+}
+
+int loca_adapter_plan(const int32_t* ids, int64_t N, int32_t n, void* plan, void* stream) {
+  clear();
+  const int rc = check_adapter(N, 8, 8, 1, n);
+  if (rc != LOCA_OK) return rc;
+  if (N == 0) return LOCA_OK;
+  if (!ids || !plan) return fail(LOCA_ERR_INVALID_ARG, "ids and plan are required");
+  if (!aligned(ids, 4) || !aligned(plan, 256))
+    return fail(LOCA_ERR_ALIGNMENT, "ids needs 4-byte, plan 256-byte alignment");
+  const cudaError_t e = launch_adapter_plan(ids, N, n, plan, static_cast<cudaStream_t>(stream));
+  if (e != cudaSuccess) return cuda_fail(e, "loca_adapter_plan launch");
+  return LOCA_OK;
+}
+
+int loca_adapter_workspace_size(int64_t N, int64_t d_in, int64_t d_out, int32_t k, int32_t n, int backward,
+                                size_t* bytes) {
+  clear();
+  if (!bytes) return fail(LOCA_ERR_INVALID_ARG, "bytes is NULL");
+  const int rc = check_adapter(N, d_in, d_out, k, n);
+  if (rc != LOCA_OK) return rc;
+  *bytes = adapter_workspace_bytes(N, d_in, d_out, k, n, backward != 0);
+  return LOCA_OK;
+}
+
+int loca_adapter_apply(const void* X, int64_t ldx, int64_t N, int64_t d_in, const void* W, int64_t d_out,
+                       const void* packed, int32_t n, int32_t k, const void* plan, void* Y, int64_t ldy,
+                       void* workspace, size_t workspace_bytes, void* stream) {
+  clear();
+  int rc = check_adapter(N, d_in, d_out, k, n);
+  if (rc != LOCA_OK) return rc;
+  if (N == 0) return LOCA_OK;
+  if (!X || !W || !packed || !plan || !Y) return fail(LOCA_ERR_INVALID_ARG, "X, W, packed, plan and Y are required");
+  if ((rc = check_rows(X, ldx, d_in, "X")) != LOCA_OK || (rc = check_rows(Y, ldy, d_out, "Y")) != LOCA_OK ||
+      (rc = check_rows(W, d_in, d_in, "W")) != LOCA_OK)
+    return rc;
+  if (!aligned(packed, 256) || !aligned(plan, 256))
+    return fail(LOCA_ERR_ALIGNMENT, "packed and plan need 256-byte alignment");
+  rc = check_ws(workspace, workspace_bytes, adapter_workspace_bytes(N, d_in, d_out, k, n, false));
+  if (rc != LOCA_OK) return rc;
+  int32_t* status = device_status_word();
+  if (!status) return fail(LOCA_ERR_CUDA, "cannot resolve the device status word");
+  const cudaError_t e = launch_adapter_apply(X, ldx, N, d_in, W, d_out, packed, n, k, plan, Y, ldy, workspace, status,
+                                             static_cast<cudaStream_t>(stream));
+  if (e != cudaSuccess) return cuda_fail(e, "loca_adapter_apply launch");
+  return LOCA_OK;
+}
+
+int loca_adapter_backward(const void* X, int64_t ldx, const void* dY, int64_t lddy, int64_t N, int64_t d_in,
+                          const void* W, int64_t d_out, const void* packed, int32_t n, int32_t k, const void* plan,
+                          void* dX, int64_t lddx, void* dA, void* dB, int grad_dtype, void* workspace,
+                          size_t workspace_bytes, void* stream) {
+  clear();
+  int rc = check_adapter(N, d_in, d_out, k, n);
+  if (rc != LOCA_OK) return rc;
+  if (grad_dtype != LOCA_F32 && grad_dtype != LOCA_BF16)
+    return fail(LOCA_ERR_UNSUPPORTED_DTYPE, "unknown dtype code %d", grad_dtype);
+  if (!dX && !dA && !dB) return fail(LOCA_ERR_INVALID_ARG, "one of dX, dA and dB is required");
+  const size_t es = grad_dtype == LOCA_F32 ? 4 : 2;
+  if (!aligned(dA, es) || !aligned(dB, es))
+    return fail(LOCA_ERR_ALIGNMENT, "dA and dB need the alignment of their elements");
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  if (N == 0) {  // sums over no token
+    cudaError_t e = dA ? cudaMemsetAsync(dA, 0, es * size_t(n) * size_t(d_in) * size_t(k), s) : cudaSuccess;
+    if (e == cudaSuccess && dB) e = cudaMemsetAsync(dB, 0, es * size_t(n) * size_t(d_out) * size_t(k), s);
+    return e == cudaSuccess ? int(LOCA_OK) : cuda_fail(e, "loca_adapter_backward memset");
+  }
+  if (!X || !dY || !W || !packed || !plan) return fail(LOCA_ERR_INVALID_ARG, "X, dY, W, packed and plan are required");
+  if ((rc = check_rows(X, ldx, d_in, "X")) != LOCA_OK || (rc = check_rows(dY, lddy, d_out, "dY")) != LOCA_OK ||
+      (rc = check_rows(W, d_in, d_in, "W")) != LOCA_OK || (dX && (rc = check_rows(dX, lddx, d_in, "dX")) != LOCA_OK))
+    return rc;
+  if (!aligned(packed, 256) || !aligned(plan, 256))
+    return fail(LOCA_ERR_ALIGNMENT, "packed and plan need 256-byte alignment");
+  rc = check_ws(workspace, workspace_bytes, adapter_workspace_bytes(N, d_in, d_out, k, n, true));
+  if (rc != LOCA_OK) return rc;
+  int32_t* status = device_status_word();
+  if (!status) return fail(LOCA_ERR_CUDA, "cannot resolve the device status word");
+  const cudaError_t e = launch_adapter_backward(X, ldx, dY, lddy, N, d_in, W, d_out, packed, n, k, plan, dX, lddx, dA, dB,
+                                                grad_dtype, workspace, status, s);
+  if (e != cudaSuccess) return cuda_fail(e, "loca_adapter_backward launch");
   return LOCA_OK;
 }
 

@@ -169,4 +169,20 @@ cudaError_t launch_head_loss_backward(const void* H, int64_t ldh, int64_t N, int
                                       float scale, void* dH, int64_t lddh, void* dW, void* workspace, int32_t* status,
                                       cudaStream_t s);
 
+// ---- adapters beside a shared projection (adapter.cu)
+int adapter_max_k();
+size_t adapter_packed_bytes(int n, int64_t d_in, int64_t d_out, int k);
+size_t adapter_plan_bytes(int64_t N, int n);
+size_t adapter_workspace_bytes(int64_t N, int64_t d_in, int64_t d_out, int k, int n, bool backward);
+cudaError_t launch_adapter_pack(const void* A, const void* B, int dtype, int n, int64_t d_in, int64_t d_out, int k,
+                                const float* scale, void* packed, cudaStream_t s);
+cudaError_t launch_adapter_plan(const int32_t* ids, int64_t N, int n, void* plan, cudaStream_t s);
+cudaError_t launch_adapter_apply(const void* X, int64_t ldx, int64_t N, int64_t d_in, const void* W, int64_t d_out,
+                                 const void* packed, int n, int k, const void* plan, void* Y, int64_t ldy,
+                                 void* workspace, int32_t* status, cudaStream_t s);
+cudaError_t launch_adapter_backward(const void* X, int64_t ldx, const void* dY, int64_t lddy, int64_t N, int64_t d_in,
+                                    const void* W, int64_t d_out, const void* packed, int n, int k, const void* plan,
+                                    void* dX, int64_t lddx, void* dA, void* dB, int grad_dtype, void* workspace,
+                                    int32_t* status, cudaStream_t s);
+
 }  // namespace loca

@@ -86,6 +86,16 @@ SIGNATURES = [
      [_I64, _I64, _I64, ctypes.c_int, ctypes.c_int, ctypes.POINTER(_SZ)]),
     ("loca_head_loss_backward", ctypes.c_int,
      [_P, _I64, _I64, _I64, _P, _I64, _P, _P, _P, _P, _F, _P, _I64, _P, _P, _SZ, _P]),
+    ("loca_adapter_packed_size", ctypes.c_int, [_I32, _I64, _I64, _I32, ctypes.POINTER(_SZ)]),
+    ("loca_adapter_pack", ctypes.c_int, [_P, _P, ctypes.c_int, _I32, _I64, _I64, _I32, _P, _P, _P]),
+    ("loca_adapter_plan_size", ctypes.c_int, [_I64, _I32, ctypes.POINTER(_SZ)]),
+    ("loca_adapter_plan", ctypes.c_int, [_P, _I64, _I32, _P, _P]),
+    ("loca_adapter_workspace_size", ctypes.c_int,
+     [_I64, _I64, _I64, _I32, _I32, ctypes.c_int, ctypes.POINTER(_SZ)]),
+    ("loca_adapter_apply", ctypes.c_int,
+     [_P, _I64, _I64, _I64, _P, _I64, _P, _I32, _I32, _P, _P, _I64, _P, _SZ, _P]),
+    ("loca_adapter_backward", ctypes.c_int,
+     [_P, _I64, _P, _I64, _I64, _I64, _P, _I64, _P, _I32, _I32, _P, _P, _I64, _P, _P, ctypes.c_int, _P, _SZ, _P]),
 ]
 
 
@@ -717,6 +727,106 @@ def loca_head_loss_backward(H, W, y, lse, dH=None, dW=None, w=None, dloss=None, 
     rc = lib().loca_head_loss_backward(_ptr(H), ldh, N, d, _ptr(W), V, _ptr(y), _ptr(w), _ptr(lse), _ptr(dloss),
                                        float(grad_scale), _ptr(dH), lddh, _ptr(dW), _ptr(ws), nbytes, _stream(stream))
     _check(rc, "loca_head_loss_backward")
+
+
+class AdapterSet:
+    """The device layout of ``n`` adapters of one projection: ``A`` (n x d_in x k) and ``B``
+    (n x d_out x k), float32 or bfloat16, each with an optional ``scale`` (n float).  Call
+    :meth:`pack` once for serving and after every update in training."""
+
+    def __init__(self, n, d_in, d_out, k, device="cuda"):
+        out = ctypes.c_size_t(0)
+        _check(lib().loca_adapter_packed_size(n, d_in, d_out, k, ctypes.byref(out)), "loca_adapter_packed_size")
+        self.n, self.d_in, self.d_out, self.k = int(n), int(d_in), int(d_out), int(k)
+        self.packed = torch.zeros(out.value, dtype=torch.uint8, device=device)
+
+    def pack(self, A, B, scale=None, stream=None):
+        _dev(A, "A", (torch.float32, torch.bfloat16), 3)
+        _dev(B, "B", A.dtype, 3)
+        _dev(scale, "scale", torch.float32, 1)
+        if (tuple(A.shape) != (self.n, self.d_in, self.k) or tuple(B.shape) != (self.n, self.d_out, self.k)
+                or (scale is not None and scale.numel() != self.n)):
+            raise ValueError("A must be n x d_in x k, B n x d_out x k and scale have n entries")
+        rc = lib().loca_adapter_pack(_ptr(A), _ptr(B), _code(A.dtype), self.n, self.d_in, self.d_out, self.k, _ptr(scale),
+                                     _ptr(self.packed), _stream(stream))
+        _check(rc, "loca_adapter_pack")
+        return self
+
+
+class AdapterPlan:
+    """The tokens of one step grouped by adapter: ``ids`` (N int32 in any order; outside [0, n) = no
+    adapter).  One plan serves every projection of the step; :meth:`update` takes the next step's
+    ids of the same length."""
+
+    def __init__(self, ids, n, stream=None):
+        _dev(ids, "ids", torch.int32, 1)
+        self.N, self.n = ids.numel(), int(n)
+        out = ctypes.c_size_t(0)
+        _check(lib().loca_adapter_plan_size(self.N, self.n, ctypes.byref(out)), "loca_adapter_plan_size")
+        self.buf = torch.empty(max(out.value, 256), dtype=torch.uint8, device=ids.device)
+        self.update(ids, stream=stream)
+
+    def update(self, ids, stream=None):
+        _dev(ids, "ids", torch.int32, 1)
+        if ids.numel() != self.N:
+            raise ValueError(f"the plan is for {self.N} tokens, got {ids.numel()}")
+        rc = lib().loca_adapter_plan(_ptr(ids), self.N, self.n, _ptr(self.buf), _stream(stream))
+        _check(rc, "loca_adapter_plan")
+        return self
+
+
+def adapter_workspace_size(N, d_in, d_out, k, n, backward=False) -> int:
+    out = ctypes.c_size_t(0)
+    _check(lib().loca_adapter_workspace_size(N, d_in, d_out, k, n, int(bool(backward)), ctypes.byref(out)),
+           "loca_adapter_workspace_size")
+    return out.value
+
+
+def _adapter_args(X, W, adapters, plan):
+    ldx = _rows2d(X, "X", torch.bfloat16)
+    _dev(W, "W", torch.bfloat16, 2)
+    N, d_in = X.shape
+    if d_in != adapters.d_in or tuple(W.shape) != (adapters.d_out, d_in):
+        raise ValueError(f"the adapters are for a {adapters.d_out} x {adapters.d_in} projection, got X {tuple(X.shape)}, "
+                         f"W {tuple(W.shape)}")
+    if plan.N != N or plan.n != adapters.n:
+        raise ValueError(f"the plan is for {plan.N} tokens and {plan.n} adapters, got {N} and {adapters.n}")
+    return ldx, N, d_in
+
+
+def loca_adapter_apply(X, W, adapters, plan, Y, workspace=None, stream=None):
+    """``Y = X W^T + s_a (X A_a) B_a^T`` for tokens with an adapter each (or none): ``X`` N x d_in and
+    ``Y`` N x d_out bf16 (rows may be spaced), ``W`` d_out x d_in bf16, ``adapters`` an
+    :class:`AdapterSet`, ``plan`` an :class:`AdapterPlan` of the tokens' adapters."""
+    ldx, N, d_in = _adapter_args(X, W, adapters, plan)
+    ldy = _rows2d(Y, "Y", torch.bfloat16, (N, adapters.d_out))
+    nbytes = adapter_workspace_size(N, d_in, adapters.d_out, adapters.k, adapters.n)
+    ws = _workspace(nbytes, X.device, workspace)
+    rc = lib().loca_adapter_apply(_ptr(X), ldx, N, d_in, _ptr(W), adapters.d_out, _ptr(adapters.packed), adapters.n,
+                                  adapters.k, _ptr(plan.buf), _ptr(Y), ldy, _ptr(ws), nbytes, _stream(stream))
+    _check(rc, "loca_adapter_apply")
+
+
+def loca_adapter_backward(X, dY, W, adapters, plan, dX=None, dA=None, dB=None, workspace=None, stream=None):
+    """Gradients of :func:`loca_adapter_apply` for the frozen projection's input (``dX``, N x d_in
+    bf16) and the adapters (``dA`` n x d_in x k, ``dB`` n x d_out x k, float32 or bfloat16); the
+    adapters as last packed."""
+    ldx, N, d_in = _adapter_args(X, W, adapters, plan)
+    lddy = _rows2d(dY, "dY", torch.bfloat16, (N, adapters.d_out))
+    lddx = 0 if dX is None else _rows2d(dX, "dX", torch.bfloat16, (N, d_in))
+    both = (torch.float32, torch.bfloat16)
+    _dev(dA, "dA", both, 3)
+    _dev(dB, "dB", both if dA is None else dA.dtype, 3)
+    if ((dA is not None and tuple(dA.shape) != (adapters.n, d_in, adapters.k))
+            or (dB is not None and tuple(dB.shape) != (adapters.n, adapters.d_out, adapters.k))):
+        raise ValueError("dA must be n x d_in x k and dB n x d_out x k")
+    kind = torch.float32 if dA is None and dB is None else (dB if dA is None else dA).dtype
+    nbytes = adapter_workspace_size(N, d_in, adapters.d_out, adapters.k, adapters.n, backward=True)
+    ws = _workspace(nbytes, X.device, workspace)
+    rc = lib().loca_adapter_backward(_ptr(X), ldx, _ptr(dY), lddy, N, d_in, _ptr(W), adapters.d_out,
+                                     _ptr(adapters.packed), adapters.n, adapters.k, _ptr(plan.buf), _ptr(dX), lddx,
+                                     _ptr(dA), _ptr(dB), _code(kind), _ptr(ws), nbytes, _stream(stream))
+    _check(rc, "loca_adapter_backward")
 
 
 class Pass:
