@@ -563,6 +563,26 @@ int loca_adapter_backward(const void* X, int64_t ldx, const void* dY, int64_t ld
                           void* dX, int64_t lddx, void* dA, void* dB, int grad_dtype, void* workspace,
                           size_t workspace_bytes, void* stream);
 
+/*
+ * loca_grad_clip — global norm of a list of gradient tensors, and their clipping:
+ *
+ *   norm = sqrt(sum_t sum_i g_t[i]^2),   out_t = f g_t,   f = max_norm / norm if norm > max_norm, else 1
+ *
+ * grads  host array of n device pointers;  numel  host array of n element counts (0 allowed);
+ * dtype  host array of n codes, LOCA_F32 or LOCA_BF16 (a list may mix them)
+ * out    host array of n device pointers, each the tensor itself or one that overlaps no tensor of
+ *        the list; or NULL for clipping in place (f = 1 then writes nothing)
+ * max_norm  > 0; infinity gives the norm alone
+ * norm   one float, device memory: the norm before clipping.  A norm that is not finite says so here;
+ *        f is then 0 (infinite norm) or 1 (NaN), and the caller should skip the step
+ * Pointers need the alignment of their elements; n <= 100000.  Sums in fp32 over at most 64 squares
+ * and in fp64 above, no overflow below the square root of fp64's range.  Deterministic.  The host
+ * arrays are read before the call returns.
+ */
+int loca_grad_clip_workspace_size(int32_t n, size_t* bytes);
+int loca_grad_clip(const void* const* grads, void* const* out, const int64_t* numel, const int32_t* dtype, int32_t n,
+                   float max_norm, float* norm, void* workspace, size_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

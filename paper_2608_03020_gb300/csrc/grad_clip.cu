@@ -1,0 +1,261 @@
+// Global norm of many gradient tensors and their clipping:
+//   norm = sqrt(sum_t sum_i g_t[i]^2),  out_t = f g_t,  f = max_norm / norm if norm > max_norm, else 1
+//
+// Two launches per up to kMany tensors, whatever their number and sizes: the list of tensors travels
+// in the kernel's parameters, cut into chunks of kChunk elements that the blocks take in turn.
+//   k_clip_sumsq   squares summed in fp32 over the (at most kChunk / 256) elements of a thread and chunk,
+//                  everything above in fp64, in a fixed order; a thread whose fp32 sum leaves the range
+//                  in which it is exact enough (overflow, squares near the smallest normal) sums its
+//                  elements again in fp64
+//   k_clip_scale   every block adds the partial sums in the same order and scales its chunks, the last
+//                  ones first: they are the ones still in L2.  In place with f = 1 nothing is written
+// Bound: HBM, one read for the norm, and the second read (as far as L2 does not hold it) and one write
+// for the clipping.
+#include <cuda_bf16.h>
+#include <cuda_runtime.h>
+
+#include <cstring>
+
+#include "loca_internal.h"
+#include "tc_ptx.cuh"
+
+namespace loca {
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kChunk = 8192;
+constexpr int kFew = 64;     // tensors of one launch: a small list keeps the launch short
+constexpr int kMany = 1000;  // 24 KB of parameters
+
+template <int kCap>
+struct List {
+  const void* in[kCap];
+  void* out[kCap];
+  int64_t numel_type[kCap];   // 2 numel + (1 if bf16)
+  int32_t chunk_end[kCap];    // chunks up to and including this tensor's
+  int32_t n;
+  int32_t chunks;
+};
+
+struct Chunk {
+  int t;
+  int64_t first;
+  int count;
+  bool bf16;
+};
+template <int kCap>
+__device__ __forceinline__ Chunk chunk_of(const List<kCap>& l, int c) {
+  int lo = 0, hi = l.n - 1;
+  while (lo < hi) {
+    const int mid = (lo + hi) / 2;
+    if (l.chunk_end[mid] > c) hi = mid;
+    else lo = mid + 1;
+  }
+  Chunk k;
+  k.t = lo;
+  k.bf16 = (l.numel_type[lo] & 1) != 0;
+  const int64_t numel = l.numel_type[lo] >> 1;
+  k.first = int64_t(c - (lo ? l.chunk_end[lo - 1] : 0)) * kChunk;
+  k.count = int(numel - k.first < kChunk ? numel - k.first : kChunk);
+  return k;
+}
+
+__device__ __forceinline__ float to_f(float x) { return x; }
+__device__ __forceinline__ float to_f(__nv_bfloat16 x) { return __bfloat162float(x); }
+
+// f(value) over this thread's share of a chunk: 16-byte vectors where the address allows, single
+// elements at the two ends.
+template <class T, class F>
+__device__ __forceinline__ void each(const T* p, int count, F&& f) {
+  constexpr int kVec = 16 / sizeof(T);
+  int head = int((16 - (reinterpret_cast<uintptr_t>(p) & 15)) & 15) / int(sizeof(T));
+  if (head > count) head = count;
+  const int vecs = (count - head) / kVec;
+  for (int i = threadIdx.x; i < head; i += kThreads) f(to_f(p[i]));
+#pragma unroll 4
+  for (int i = threadIdx.x; i < vecs; i += kThreads) {
+    const uint4 q = __ldg(reinterpret_cast<const uint4*>(p + head) + i);
+    const T* v = reinterpret_cast<const T*>(&q);
+#pragma unroll
+    for (int j = 0; j < kVec; ++j) f(to_f(v[j]));
+  }
+  for (int i = head + vecs * kVec + threadIdx.x; i < count; i += kThreads) f(to_f(p[i]));
+}
+
+template <class T>
+__device__ __forceinline__ double sum_squares(const T* p, int count) {
+  float s = 0.f;
+  each(p, count, [&](float g) { s = fmaf(g, g, s); });
+  if (s >= 1e-30f && s <= 1e38f) return double(s);
+  double d = 0.0;
+  each(p, count, [&](float g) { d = fma(double(g), double(g), d); });
+  return d;
+}
+
+__device__ __forceinline__ double block_sum(double v, double* sh) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  __syncthreads();
+  if ((threadIdx.x & 31) == 0) sh[threadIdx.x >> 5] = v;
+  __syncthreads();
+  double s = 0.0;
+#pragma unroll
+  for (int w = 0; w < kThreads / 32; ++w) s += sh[w];
+  return s;
+}
+
+template <int kCap>
+__global__ void __launch_bounds__(kThreads) k_clip_sumsq(const __grid_constant__ List<kCap> l, double* part) {
+  __shared__ double sh[kThreads / 32];
+  tc::launch_dependents();
+  double s = 0.0;
+  for (int c = blockIdx.x; c < l.chunks; c += gridDim.x) {
+    const Chunk k = chunk_of(l, c);
+    s += k.bf16 ? sum_squares(static_cast<const __nv_bfloat16*>(l.in[k.t]) + k.first, k.count)
+                : sum_squares(static_cast<const float*>(l.in[k.t]) + k.first, k.count);
+  }
+  s = block_sum(s, sh);
+  if (threadIdx.x == 0) part[blockIdx.x] = s;
+}
+
+template <class T>
+__device__ __forceinline__ T from_f(float x);
+template <>
+__device__ __forceinline__ float from_f<float>(float x) { return x; }
+template <>
+__device__ __forceinline__ __nv_bfloat16 from_f<__nv_bfloat16>(float x) { return __float2bfloat16_rn(x); }
+
+template <class T>
+__device__ __forceinline__ void scale_chunk(const T* p, T* o, int count, float f) {
+  constexpr int kVec = 16 / sizeof(T);
+  const uintptr_t a = reinterpret_cast<uintptr_t>(p) & 15, b = reinterpret_cast<uintptr_t>(o) & 15;
+  if (a != b) {  // the two do not share 16-byte boundaries
+    for (int i = threadIdx.x; i < count; i += kThreads) o[i] = from_f<T>(f * to_f(p[i]));
+    return;
+  }
+  int head = int((16 - a) & 15) / int(sizeof(T));
+  if (head > count) head = count;
+  const int vecs = (count - head) / kVec;
+  for (int i = threadIdx.x; i < head; i += kThreads) o[i] = from_f<T>(f * to_f(p[i]));
+#pragma unroll 4
+  for (int i = threadIdx.x; i < vecs; i += kThreads) {
+    uint4 q = *(reinterpret_cast<const uint4*>(p + head) + i);
+    T* v = reinterpret_cast<T*>(&q);
+#pragma unroll
+    for (int j = 0; j < kVec; ++j) v[j] = from_f<T>(f * to_f(v[j]));
+    __stcs(reinterpret_cast<uint4*>(o + head) + i, q);
+  }
+  for (int i = head + vecs * kVec + threadIdx.x; i < count; i += kThreads) o[i] = from_f<T>(f * to_f(p[i]));
+}
+
+template <int kCap>
+__global__ void __launch_bounds__(kThreads)
+    k_clip_scale(const __grid_constant__ List<kCap> l, const double* part, int parts, float max_norm, float* norm) {
+  __shared__ double sh[kThreads / 32];
+  tc::wait_for_previous();
+  double s = 0.0;
+  for (int i = threadIdx.x; i < parts; i += kThreads) s += part[i];
+  s = block_sum(s, sh);
+  const double n = sqrt(s);
+  if (blockIdx.x == 0 && threadIdx.x == 0) *norm = float(n);
+  const float f = n > double(max_norm) ? float(double(max_norm) / n) : 1.f;
+  for (int c = l.chunks - 1 - int(blockIdx.x); c >= 0; c -= int(gridDim.x)) {
+    const Chunk k = chunk_of(l, c);
+    if (f == 1.f && l.in[k.t] == l.out[k.t]) continue;
+    if (k.bf16)
+      scale_chunk(static_cast<const __nv_bfloat16*>(l.in[k.t]) + k.first, static_cast<__nv_bfloat16*>(l.out[k.t]) + k.first,
+                  k.count, f);
+    else
+      scale_chunk(static_cast<const float*>(l.in[k.t]) + k.first, static_cast<float*>(l.out[k.t]) + k.first, k.count, f);
+  }
+}
+
+int clip_blocks() { return 4 * sm_count(); }
+
+template <int kCap>
+void fill(List<kCap>& l, const void* const* grads, void* const* out, const int64_t* numel, const int32_t* dtype, int n) {
+  int64_t chunks = 0;
+  for (int i = 0; i < n; ++i) {
+    l.in[i] = grads[i];
+    l.out[i] = out ? out[i] : const_cast<void*>(grads[i]);
+    l.numel_type[i] = 2 * numel[i] + (dtype[i] == LOCA_BF16 ? 1 : 0);
+    chunks += (numel[i] + kChunk - 1) / kChunk;
+    l.chunk_end[i] = int32_t(chunks);
+  }
+  l.n = n;
+  l.chunks = int32_t(chunks);
+}
+
+struct Args {
+  const void* const* grads;
+  void* const* out;
+  const int64_t* numel;
+  const int32_t* dtype;
+  int n;
+};
+
+template <int kCap>
+cudaError_t sumsq(const Args& a, double* part, cudaStream_t s) {
+  List<kCap> l;
+  fill(l, a.grads, a.out, a.numel, a.dtype, a.n);
+  k_clip_sumsq<kCap><<<unsigned(clip_blocks()), kThreads, 0, s>>>(l, part);
+  return cudaGetLastError();
+}
+
+template <int kCap>
+cudaError_t scale(const Args& a, const double* part, int parts, float max_norm, float* norm, cudaStream_t s) {
+  List<kCap> l;
+  fill(l, a.grads, a.out, a.numel, a.dtype, a.n);
+  cudaLaunchConfig_t cfg = {};
+  const int blocks = clip_blocks();
+  cfg.gridDim = dim3(unsigned(l.chunks < blocks ? (l.chunks < 1 ? 1 : l.chunks) : blocks));
+  cfg.blockDim = dim3(kThreads);
+  cfg.stream = s;
+  cudaLaunchAttribute at[1];
+  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = at;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, k_clip_scale<kCap>, l, part, parts, max_norm, norm);
+}
+
+Args part_of(const Args& a, int first) {
+  Args b = a;
+  b.n = a.n - first < kMany ? a.n - first : kMany;
+  b.grads += first;
+  if (b.out) b.out += first;
+  b.numel += first;
+  b.dtype += first;
+  return b;
+}
+
+}  // namespace
+
+int64_t grad_clip_max_numel() { return int64_t(kChunk) * 2000000; }
+
+size_t grad_clip_workspace_bytes(int n) {
+  const size_t launches = n < 1 ? 1 : (size_t(n) + kMany - 1) / kMany;
+  return align256(launches * size_t(clip_blocks()) * sizeof(double));
+}
+
+cudaError_t launch_grad_clip(const void* const* grads, void* const* out, const int64_t* numel, const int32_t* dtype,
+                             int n, float max_norm, float* norm, void* workspace, cudaStream_t s) {
+  const Args all{grads, out, numel, dtype, n};
+  double* part = static_cast<double*>(workspace);
+  int parts = 0;
+  for (int i = 0; i < n || i == 0; i += kMany) {
+    const Args a = part_of(all, i);
+    const cudaError_t e = a.n <= kFew ? sumsq<kFew>(a, part + parts, s) : sumsq<kMany>(a, part + parts, s);
+    if (e != cudaSuccess) return e;
+    parts += clip_blocks();
+  }
+  for (int i = 0; i < n || i == 0; i += kMany) {
+    const Args a = part_of(all, i);
+    const cudaError_t e = a.n <= kFew ? scale<kFew>(a, part, parts, max_norm, norm, s)
+                                      : scale<kMany>(a, part, parts, max_norm, norm, s);
+    if (e != cudaSuccess) return e;
+  }
+  return cudaSuccess;
+}
+
+}  // namespace loca

@@ -244,4 +244,40 @@ int loca_adapter_backward(const void* X, int64_t ldx, const void* dY, int64_t ld
   return LOCA_OK;
 }
 
+int loca_grad_clip_workspace_size(int32_t n, size_t* bytes) {
+  clear();
+  if (!bytes) return fail(LOCA_ERR_INVALID_ARG, "bytes is NULL");
+  if (n < 0 || n > 100000) return fail(LOCA_ERR_SHAPE, "need 0 <= n <= 100000 tensors, got %d", n);
+  *bytes = grad_clip_workspace_bytes(n);
+  return LOCA_OK;
+}
+
+int loca_grad_clip(const void* const* grads, void* const* out, const int64_t* numel, const int32_t* dtype, int32_t n,
+                   float max_norm, float* norm, void* workspace, size_t workspace_bytes, void* stream) {
+  clear();
+  if (n < 0 || n > 100000) return fail(LOCA_ERR_SHAPE, "need 0 <= n <= 100000 tensors, got %d", n);
+  if (!(max_norm > 0.f)) return fail(LOCA_ERR_INVALID_ARG, "max_norm must be positive");
+  if (!norm || (n > 0 && (!grads || !numel || !dtype)))
+    return fail(LOCA_ERR_INVALID_ARG, "grads, numel, dtype and norm are required");
+  if (!aligned(norm, 4)) return fail(LOCA_ERR_ALIGNMENT, "norm needs 4-byte alignment");
+  int64_t total = 0;
+  for (int32_t i = 0; i < n; ++i) {
+    if (dtype[i] != LOCA_F32 && dtype[i] != LOCA_BF16)
+      return fail(LOCA_ERR_UNSUPPORTED_DTYPE, "tensor %d has unknown dtype code %d", i, dtype[i]);
+    if (numel[i] < 0 || numel[i] > grad_clip_max_numel() || (total += numel[i]) > grad_clip_max_numel())
+      return fail(LOCA_ERR_SHAPE, "tensor %d: element counts must be >= 0 and sum to at most %lld", i,
+                  (long long)grad_clip_max_numel());
+    const size_t es = dtype[i] == LOCA_F32 ? 4 : 2;
+    if (numel[i] > 0 && (!grads[i] || (out && !out[i]))) return fail(LOCA_ERR_INVALID_ARG, "tensor %d is NULL", i);
+    if (!aligned(grads[i], es) || (out && !aligned(out[i], es)))
+      return fail(LOCA_ERR_ALIGNMENT, "tensor %d needs the alignment of its elements", i);
+  }
+  const int rc = check_ws(workspace, workspace_bytes, grad_clip_workspace_bytes(n));
+  if (rc != LOCA_OK) return rc;
+  const cudaError_t e = launch_grad_clip(grads, out, numel, dtype, n, max_norm, norm, workspace,
+                                         static_cast<cudaStream_t>(stream));
+  if (e != cudaSuccess) return cuda_fail(e, "loca_grad_clip launch");
+  return LOCA_OK;
+}
+
 }  // extern "C"

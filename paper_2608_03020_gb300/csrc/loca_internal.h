@@ -185,4 +185,10 @@ cudaError_t launch_adapter_backward(const void* X, int64_t ldx, const void* dY, 
                                     void* dX, int64_t lddx, void* dA, void* dB, int grad_dtype, void* workspace,
                                     int32_t* status, cudaStream_t s);
 
+// ---- gradient norm and clipping (grad_clip.cu); grads, out, numel, dtype: host arrays
+int64_t grad_clip_max_numel();
+size_t grad_clip_workspace_bytes(int n);
+cudaError_t launch_grad_clip(const void* const* grads, void* const* out, const int64_t* numel, const int32_t* dtype,
+                             int n, float max_norm, float* norm, void* workspace, cudaStream_t s);
+
 }  // namespace loca

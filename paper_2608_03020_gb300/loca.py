@@ -96,6 +96,8 @@ SIGNATURES = [
      [_P, _I64, _I64, _I64, _P, _I64, _P, _I32, _I32, _P, _P, _I64, _P, _SZ, _P]),
     ("loca_adapter_backward", ctypes.c_int,
      [_P, _I64, _P, _I64, _I64, _I64, _P, _I64, _P, _I32, _I32, _P, _P, _I64, _P, _P, ctypes.c_int, _P, _SZ, _P]),
+    ("loca_grad_clip_workspace_size", ctypes.c_int, [_I32, ctypes.POINTER(_SZ)]),
+    ("loca_grad_clip", ctypes.c_int, [_P, _P, _P, _P, _I32, _F, _P, _P, _SZ, _P]),
 ]
 
 
@@ -827,6 +829,47 @@ def loca_adapter_backward(X, dY, W, adapters, plan, dX=None, dA=None, dB=None, w
                                      _ptr(adapters.packed), adapters.n, adapters.k, _ptr(plan.buf), _ptr(dX), lddx,
                                      _ptr(dA), _ptr(dB), _code(kind), _ptr(ws), nbytes, _stream(stream))
     _check(rc, "loca_adapter_backward")
+
+
+class GradClip:
+    """Global norm and clipping of one list of gradient tensors (float32 and bfloat16, any shapes,
+    contiguous): in place, or into ``out`` (tensors of the same shapes and types).  Holds the list
+    from step to step; :meth:`run` enqueues one step."""
+
+    def __init__(self, grads, out=None):
+        self.grads = list(grads)
+        self.out = None if out is None else list(out)
+        if self.out is not None and len(self.out) != len(self.grads):
+            raise ValueError("out must have one tensor for each of grads")
+        for i, t in enumerate(self.grads):
+            _dev(t, f"grads[{i}]", (torch.float32, torch.bfloat16))
+            if t is None:
+                raise TypeError(f"grads[{i}] must be a CUDA tensor")
+            if self.out is not None:
+                if self.out[i] is None:
+                    raise TypeError(f"out[{i}] must be a CUDA tensor")
+                _dev(self.out[i], f"out[{i}]", t.dtype)
+                if self.out[i].numel() != t.numel():
+                    raise ValueError(f"out[{i}] has {self.out[i].numel()} elements, grads[{i}] {t.numel()}")
+        n = len(self.grads)
+        self._in = (ctypes.c_void_p * max(n, 1))(*[t.data_ptr() for t in self.grads])
+        self._out = None if out is None else (ctypes.c_void_p * max(n, 1))(*[t.data_ptr() for t in self.out])
+        self._numel = (ctypes.c_int64 * max(n, 1))(*[t.numel() for t in self.grads])
+        self._dtype = (ctypes.c_int32 * max(n, 1))(*[_code(t.dtype) for t in self.grads])
+        size = ctypes.c_size_t(0)
+        _check(lib().loca_grad_clip_workspace_size(n, ctypes.byref(size)), "loca_grad_clip_workspace_size")
+        self._bytes = size.value
+        self._ws = torch.empty(size.value, dtype=torch.uint8, device=self.grads[0].device if n else "cuda")
+
+    def run(self, max_norm, norm, stream=None):
+        """Writes the global norm before clipping to ``norm`` (one float, device) and the gradients
+        scaled by ``min(1, max_norm / norm)``; ``max_norm = inf`` gives the norm alone."""
+        _dev(norm, "norm", torch.float32)
+        if norm is None or norm.numel() != 1:
+            raise ValueError("norm must be a CUDA tensor of one element")
+        rc = lib().loca_grad_clip(self._in, self._out, self._numel, self._dtype, len(self.grads), float(max_norm),
+                                  _ptr(norm), _ptr(self._ws), self._bytes, _stream(stream))
+        _check(rc, "loca_grad_clip")
 
 
 class Pass:

@@ -1,8 +1,8 @@
 """Adapters beside a shared projection, forward and backward, against the definition in 64 bits.
 
-Tolerances, fixed before the first run.  Outputs in bf16 carry one rounding of the sum (2^-9 relative
-to it) and, for the low-rank term, of U and of s B (2^-9 each, relative to that term): 2^-8 of the sum
-plus 2^-8 of the term, in norm.  Gradients of the adapters in float32: U and T from three-part
+Tolerances, fixed before the first run.  Outputs in bf16 carry one rounding of the sum (uniform within
+2^-8 of a binade's size, so below 2^-9 in norm) and, for the low-rank term, of U and of s B (the same,
+relative to that term): 2^-8 of the sum plus 2^-8 of the term, in norm.  Gradients of the adapters in float32: U and T from three-part
 adapters, in three parts (2^-26 each), summed on the tensor cores in segments of 32 steps, each step
 losing up to 2^-22 of the running sum: 32 * 2^-22 = 8e-6 in each of two sums, so 2e-5 of the products'
 absolute sums; taken as 2e-5 in norm.  In bf16 one rounding more: 2^-9 + 2e-5.

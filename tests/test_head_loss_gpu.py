@@ -5,7 +5,7 @@ up to 2^-22 of the running sum per step, toward zero, and a sum restarts after 6
 within 64 * 2^-22 = 1.5e-5 of the largest partial sum, taken as 2e-5 (1 + max |z|) with the fp32
 exponentials (2 ulp each).  ``loss``, ``lse`` and ``E`` (whose derivative with respect to a logit is at
 most w) are held to that times the weight.  Gradients come out in bf16: one rounding of dZ and one of
-the sum, each at most 2^-9 relative, so 2^-8 in norm.
+the sum, each uniform within 2^-8 of a binade's size, so less than 2^-8 together in norm.
 """
 
 import pytest
