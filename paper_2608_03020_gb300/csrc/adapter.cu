@@ -26,7 +26,7 @@
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
-#include <cstring>
+#include <atomic>
 
 #include "gemm_pair.cuh"
 
@@ -309,17 +309,19 @@ struct ShrinkGeo {
   int64_t ldx, N, d;
   const __nv_bfloat16* P;  // packed adapter operand: part x adapter x d x kp
   const int32_t* marks;
-  int n, kp, parts, stages;
+  int n, kp, stages;
   const int32_t* plan;
   PlanLay p;
   __nv_bfloat16* out;  // parts x smax x 128 x 64
   int32_t* status;
   int32_t* abort_flag;
   unsigned long long limit_ns;
+  int32_t mark;
 };
+constexpr int kFewXBytes = kTokGroup * 4096 * 2;  // X of the few tokens, behind the sums
 int shrink_ring(int parts, int stages) {
   const int b = stages * (kXBytes + parts * kPBytes);
-  return b > kRedBytes ? b : kRedBytes;
+  return b > kRedBytes + kFewXBytes ? b : kRedBytes + kFewXBytes;
 }
 int shrink_smem(int parts, int stages) { return shrink_ring(parts, stages) + 512 + 1024; }
 
@@ -328,79 +330,112 @@ __device__ __forceinline__ int red_at(int row, int col) {
   return row * kMaxK + (((col >> 2) ^ (row & 15)) << 2) + (col & 3);
 }
 
-// The few tokens of a slot, rows list[0 .. members): sums over k0 .. k1 into red.  Thread t takes the
-// 16-byte chunk t % nc of the adapter rows t / nc, t / nc + stride, ...
+// The few tokens of a slot, rows list[0 .. members): sums over k0 .. k1 into red, kTok tokens at a time.
+// Their X is staged in shared memory; thread t takes the 16-byte chunk t % nc of the adapter rows
+// t / nc, t / nc + stride, ... with kBatch loads in flight.
+constexpr int kFewK = 4096;   // k staged at a time
+template <int kP, int kTok>
 __device__ __forceinline__ void shrink_few(const ShrinkGeo& g, int a, int64_t row0, const int* list, int members,
-                                           int64_t k0, int64_t k1, float* red, float* part) {
+                                           int64_t k0, int64_t k1, float* red, __nv_bfloat16* xs, float* part) {
+  constexpr int kBatch = kP == 1 ? 8 : 2;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int chunks = g.kp / 8;
   const int nc = chunks <= 1 ? 1 : chunks <= 2 ? 2 : chunks <= 4 ? 4 : 8;
   const int c = threadIdx.x % nc, r0 = threadIdx.x / nc, stride = kShrinkThreads / nc;
   const int64_t pitch = int64_t(g.n) * g.d * g.kp;
   const __nv_bfloat16* P = g.P + int64_t(a) * g.d * g.kp + c * 8;
-  for (int t0 = 0; t0 < members; t0 += kTokGroup) {
-    float acc[kTokGroup][8];
-    const __nv_bfloat16* x[kTokGroup];
+  for (int t0 = 0; t0 < members; t0 += kTok) {
+    float acc[kTok][8];
 #pragma unroll
-    for (int t = 0; t < kTokGroup; ++t) {
-      const int m = t0 + t < members ? t0 + t : members - 1;
-      x[t] = g.X + (row0 + list[m]) * g.ldx;
+    for (int t = 0; t < kTok; ++t)
 #pragma unroll
       for (int i = 0; i < 8; ++i) acc[t][i] = 0.f;
-    }
-    if (c < chunks) {
-#pragma unroll 4
-      for (int64_t k = k0 + r0; k < k1; k += stride) {
-        float w[8] = {};
-        for (int q = g.parts - 1; q >= 0; --q) {
-          const uint4 v = *reinterpret_cast<const uint4*>(P + q * pitch + k * g.kp);
-          const __nv_bfloat162* h = reinterpret_cast<const __nv_bfloat162*>(&v);
+    for (int64_t kc = k0; kc < k1; kc += kFewK) {
+      const int kn = int(k1 - kc < kFewK ? k1 - kc : kFewK);
+      auto load = [&](uint4 (&v)[kBatch][kP], int r) {
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const float2 f = __bfloat1622float2(h[i]);
-            w[2 * i] += f.x;
-            w[2 * i + 1] += f.y;
+        for (int j = 0; j < kBatch; ++j)
+#pragma unroll
+          for (int q = 0; q < kP; ++q)
+            if (c < chunks && r + j * stride < kn)
+              v[j][q] = __ldg(reinterpret_cast<const uint4*>(P + q * pitch + (kc + r + j * stride) * g.kp));
+      };
+      uint4 v[kBatch][kP];
+      load(v, r0);  // in flight while X is staged
+      __syncthreads();
+#pragma unroll
+      for (int t = 0; t < kTok; ++t) {
+        const int m = t0 + t < members ? t0 + t : members - 1;
+        const uint4* src = reinterpret_cast<const uint4*>(g.X + (row0 + list[m]) * g.ldx + kc);
+        for (int i = threadIdx.x; i < kn / 8; i += kShrinkThreads) reinterpret_cast<uint4*>(xs + t * kFewK)[i] = src[i];
+      }
+      __syncthreads();
+      for (int r = r0; r < kn; r += kBatch * stride) {
+        if (r != r0) load(v, r);
+        if (c < chunks) {
+#pragma unroll
+          for (int j = 0; j < kBatch; ++j) {
+            if (r + j * stride < kn) {
+              float w[8] = {};
+#pragma unroll
+              for (int q = kP - 1; q >= 0; --q) {
+                const __nv_bfloat162* h = reinterpret_cast<const __nv_bfloat162*>(&v[j][q]);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                  const float2 f = __bfloat1622float2(h[i]);
+                  w[2 * i] += f.x;
+                  w[2 * i + 1] += f.y;
+                }
+              }
+#pragma unroll
+              for (int t = 0; t < kTok; ++t) {
+                const float x = __bfloat162float(xs[t * kFewK + r + j * stride]);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) acc[t][i] = fmaf(x, w[i], acc[t][i]);
+              }
+            }
           }
         }
-#pragma unroll
-        for (int t = 0; t < kTokGroup; ++t) {
-          const float xv = __bfloat162float(x[t][k]);
-#pragma unroll
-          for (int i = 0; i < 8; ++i) acc[t][i] = fmaf(xv, w[i], acc[t][i]);
-        }
       }
     }
+    __syncwarp();
 #pragma unroll
-    for (int t = 0; t < kTokGroup; ++t)
+    for (int t = 0; t < kTok; ++t)
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        float v = acc[t][i];
-        for (int o = nc; o < 32; o <<= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-        if (lane < nc) part[(warp * kTokGroup + t) * kMaxK + lane * 8 + i] = v;
+        float s = acc[t][i];
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1)
+          if (o >= nc) s += __shfl_xor_sync(0xffffffffu, s, o);
+        if (lane < nc) part[(warp * kTok + t) * kMaxK + lane * 8 + i] = s;
       }
     __syncthreads();
-    for (int e = threadIdx.x; e < kTokGroup * kMaxK; e += kShrinkThreads) {
+    for (int e = threadIdx.x; e < kTok * kMaxK; e += kShrinkThreads) {
       const int t = e / kMaxK, col = e % kMaxK;
       if (t0 + t < members) {
-        float v = 0.f;
-        if (col < g.kp)
-          for (int w = 0; w < kShrinkThreads / 32; ++w) v += part[(w * kTokGroup + t) * kMaxK + col];
-        red[red_at(list[t0 + t], col)] = v;
+        float s = 0.f;
+        if (col < g.kp) {
+#pragma unroll
+          for (int w = 0; w < kShrinkThreads / 32; ++w) s += part[(w * kTok + t) * kMaxK + col];
+        }
+        red[red_at(list[t0 + t], col)] = s;
       }
     }
     __syncthreads();
   }
 }
 
+template <int kP>
 __global__ void __launch_bounds__(kShrinkThreads, 1)
     k_adapter_shrink(const __grid_constant__ CUtensorMap tmX, const __grid_constant__ CUtensorMap tmP,
                      const __grid_constant__ ShrinkGeo g) {
   extern __shared__ uint8_t smem_raw[];
   __shared__ float few_part[kShrinkThreads / 32 * kTokGroup * kMaxK];
   __shared__ int few_list[kFewTokens];
+  __shared__ uint32_t members_of[kTile / 32];  // the tile's rows that belong to the slot
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
-  const int stage_bytes = kXBytes + g.parts * kPBytes;
-  const int ring = g.stages * stage_bytes > kRedBytes ? g.stages * stage_bytes : kRedBytes;
+  constexpr int stage_bytes = kXBytes + kP * kPBytes;
+  const int ring = g.stages * stage_bytes > kRedBytes + kFewXBytes ? g.stages * stage_bytes : kRedBytes + kFewXBytes;
   uint64_t* bars = reinterpret_cast<uint64_t*>(smem + ring);
   const uint32_t bar_base = smem_u32(bars);
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 * kMaxStages + 5);
@@ -410,17 +445,20 @@ __global__ void __launch_bounds__(kShrinkThreads, 1)
   auto acc_empty = [&](uint32_t b) { return bar_base + 8u * (2 * kMaxStages + 2 + b); };
   const uint32_t drain_bar = bar_base + 8u * (2 * kMaxStages + 4);
   float* red = reinterpret_cast<float*>(smem);  // [128][64] sums of this CTA
+  __nv_bfloat16* few_x = reinterpret_cast<__nv_bfloat16*>(smem + kRedBytes);
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t smem_base = smem_u32(smem);
-  const WaitCtl wc{g.status, g.abort_flag, g.limit_ns};
+  const WaitCtl wc{g.status, g.abort_flag, g.limit_ns, g.mark};
   const int ks = int(cluster_nctarank()), rank = int(cluster_ctarank());
   const int cid = int(cluster_id_x()), ncl = int(ncluster_x());
-  const uint32_t acc_cols = uint32_t(64 * g.parts);
-  const uint32_t cols = g.parts == 1 ? 128u : 512u;
+  constexpr uint32_t acc_cols = uint32_t(64 * kP);
+  constexpr uint32_t cols = kP == 1 ? 128u : 512u;
 
   launch_dependents();
+  const int total = g.plan[g.p.tile_base + g.p.tiles];
   if (threadIdx.x == 0) {
+    if (blockIdx.x == 0) *g.abort_flag = 0;  // a captured call that gave up may be replayed
     for (int s = 0; s < kMaxStages; ++s) {
       mbar_init(full_bar(s), 1);
       mbar_init(empty_bar(s), 1);
@@ -444,8 +482,7 @@ __global__ void __launch_bounds__(kShrinkThreads, 1)
   const int kb0 = rank * per < nkb ? rank * per : nkb;
   const int kb1 = kb0 + per < nkb ? kb0 + per : nkb;
   const int nb = kb1 - kb0;
-  const int seg_kb = g.parts == 1 ? 64 : kShrinkSeg;
-  const int total = g.plan[g.p.tile_base + g.p.tiles];
+  constexpr int seg_kb = kP == 1 ? 64 : kShrinkSeg;
 
   int stage = 0;
   uint32_t phase = 0, iter = 0, seg = 0;
@@ -454,21 +491,28 @@ __global__ void __launch_bounds__(kShrinkThreads, 1)
     const int a = g.plan[g.p.adapter + s];
     const int64_t row0 = int64_t(g.plan[g.p.tile + s]) * kTile;
     const int members = g.plan[g.p.count + s];
+    const bool spoiled = g.marks[a] != 0;
+    if (warp >= 2) {  // the rows of the tile that are this slot's
+      const int r = (warp - 2) * 32 + lane;
+      const bool mine = row0 + r < g.N && g.plan[g.p.tok_slot + row0 + r] == s;
+      const unsigned all = __ballot_sync(0xffffffffu, mine);
+      if (lane == 0) members_of[warp - 2] = all;
+    }
     if (members <= kFewTokens) {
+      __syncthreads();
       if (warp == 0) {
         int at = 0;
-        for (int b = 0; b < kTile; b += 32) {
-          const int64_t tok = row0 + b + lane;
-          const bool mine = tok < g.N && g.plan[g.p.tok_slot + tok] == s;
-          const unsigned all = __ballot_sync(0xffffffffu, mine);
+        for (int b = 0; b < kTile / 32; ++b) {
+          const unsigned all = members_of[b];
           const int pos = at + __popc(all & ((1u << lane) - 1u));
-          if (mine && pos < kFewTokens) few_list[pos] = b + lane;
+          if ((all >> lane & 1u) && pos < kFewTokens) few_list[pos] = b * 32 + lane;
           at += __popc(all);
         }
       }
       __syncthreads();
-      const int64_t k1 = int64_t(kb1) * 64 < g.d ? int64_t(kb1) * 64 : g.d;
-      shrink_few(g, a, row0, few_list, members, int64_t(kb0) * 64, k1, red, few_part);
+      const int64_t k0 = int64_t(kb0) * 64, k1 = int64_t(kb1) * 64 < g.d ? int64_t(kb1) * 64 : g.d;
+      if (members == 1) shrink_few<kP, 1>(g, a, row0, few_list, members, k0, k1, red, few_x, few_part);
+      else shrink_few<kP, kTokGroup>(g, a, row0, few_list, members, k0, k1, red, few_x, few_part);
     } else if (warp == 0) {
       // ---------------- TMA producer
       if (lane == 0 && ok) {
@@ -480,7 +524,8 @@ __global__ void __launch_bounds__(kShrinkThreads, 1)
           mbar_arrive_expect_tx(full_bar(stage), uint32_t(stage_bytes));
           const uint32_t dst = smem_base + uint32_t(stage * stage_bytes);
           tma_load_2d(dst, &tmX, full_bar(stage), kb * 64, int(row0));
-          for (int q = 0; q < g.parts; ++q)
+#pragma unroll
+          for (int q = 0; q < kP; ++q)
             tma_load_3d(dst + kXBytes + q * kPBytes, &tmP, full_bar(stage), 0, kb * 64, q * g.n + a);
           ++iter;
           if (++stage == g.stages) { stage = 0; phase ^= 1u; }
@@ -490,7 +535,7 @@ __global__ void __launch_bounds__(kShrinkThreads, 1)
     } else if (warp == 1) {
       // ---------------- MMA issuer: X tile (K-major) x the adapter's rows (MN-major, a part per 64 columns)
       if (lane == 0 && ok) {
-        const uint32_t id = tc::idesc(1, 1, 0, 1, 128, acc_cols);
+        constexpr uint32_t id = tc::idesc(1, 1, 0, 1, 128, acc_cols);
         for (int j = 0, in_seg = 0; j < nb; ++j) {
           const uint32_t b = seg & 1u;
           if (in_seg == 0 && !mbar_try_wait(acc_empty(b), ((seg >> 1) & 1u) ^ 1u) &&
@@ -538,7 +583,8 @@ __global__ void __launch_bounds__(kShrinkThreads, 1)
         }
         fence_after();
         const uint32_t ta = tmem_base + (uint32_t(q * 32) << 16) + b * acc_cols;
-        for (int p = 0; p < g.parts; ++p) {
+#pragma unroll
+        for (int p = 0; p < kP; ++p) {
 #pragma unroll
           for (int c = 0; c < 2; ++c) {
             float v[32];
@@ -566,35 +612,39 @@ __global__ void __launch_bounds__(kShrinkThreads, 1)
     const uint32_t red_s = smem_u32(red);
     for (int e = threadIdx.x; e < rows_per * 8; e += kShrinkThreads) {
       const int row = rank * rows_per + e / 8, ch = e % 8;
-      const int64_t tok = row0 + row;
       float v[8] = {};
-      if (tok < g.N && g.plan[g.p.tok_slot + tok] == s) {
+      if (members_of[row >> 5] >> (row & 31) & 1u) {
         const uint32_t o0 = red_s + 4u * uint32_t(red_at(row, ch * 8));
         const uint32_t o1 = red_s + 4u * uint32_t(red_at(row, ch * 8 + 4));
-        for (int j = 0; j < ks; ++j) {
-          const float4 x = ld_shared_cluster_f32x4(mapa_shared(o0, uint32_t(j)));
-          const float4 y = ld_shared_cluster_f32x4(mapa_shared(o1, uint32_t(j)));
-          v[0] += x.x; v[1] += x.y; v[2] += x.z; v[3] += x.w;
-          v[4] += y.x; v[5] += y.y; v[6] += y.z; v[7] += y.w;
-        }
-        if (g.marks[a]) {
+        float4 x[8], y[8];  // all loads first: one round trip
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+          if (j < ks) {
+            x[j] = ld_shared_cluster_f32x4(mapa_shared(o0, uint32_t(j)));
+            y[j] = ld_shared_cluster_f32x4(mapa_shared(o1, uint32_t(j)));
+          }
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+          if (j < ks) {
+            v[0] += x[j].x; v[1] += x[j].y; v[2] += x[j].z; v[3] += x[j].w;
+            v[4] += y[j].x; v[5] += y[j].y; v[6] += y[j].z; v[7] += y[j].w;
+          }
+        if (spoiled) {
 #pragma unroll
           for (int i = 0; i < 8; ++i) v[i] = __int_as_float(0x7fffffff);
         }
       }
-      __nv_bfloat16 o[8][3];
+      __nv_bfloat16* to = g.out + (int64_t(s) * kSlotRows + row) * kMaxK + ch * 8;
+      const int64_t pitch = g.p.smax * int64_t(kSlotElems);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) split3(v[i], o[i]);
+      for (int q = 0; q < kP; ++q) {
+        __align__(16) __nv_bfloat16 w[8];
 #pragma unroll
-      for (int q = 0; q < kParts; ++q) {
-        if (q < g.parts) {
-          __align__(16) __nv_bfloat16 w[8];
-#pragma unroll
-          for (int i = 0; i < 8; ++i) w[i] = o[i][q];
-          if (LOCA_CHECK(s, g.p.smax))
-            *reinterpret_cast<uint4*>(g.out + ((int64_t(q) * g.p.smax + s) * kSlotRows + row) * kMaxK + ch * 8) =
-                *reinterpret_cast<const uint4*>(w);
+        for (int i = 0; i < 8; ++i) {
+          w[i] = __float2bfloat16_rn(v[i]);
+          v[i] -= __bfloat162float(w[i]);
         }
+        if (LOCA_CHECK(s, g.p.smax)) *reinterpret_cast<uint4*>(to + q * pitch) = *reinterpret_cast<const uint4*>(w);
       }
     }
     fence_proxy_async_smem();  // the ring's next loads come after these accesses
@@ -638,6 +688,7 @@ struct FewGeo {
   int32_t* status;
   int32_t* abort_flag;
   unsigned long long limit_ns;
+  int32_t mark;
 };
 int few_ring(int nt, int stages) {
   const int b = stages * (kWBytes + nt * 128);
@@ -665,7 +716,7 @@ __global__ void __launch_bounds__(kFewThreads, 1)
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t smem_base = smem_u32(smem);
-  const WaitCtl wc{g.status, g.abort_flag, g.limit_ns};
+  const WaitCtl wc{g.status, g.abort_flag, g.limit_ns, g.mark};
   const int ks = int(cluster_nctarank()), rank = int(cluster_ctarank());
   const int o0 = int(cluster_id_x()) * 128;
   const int64_t tile = blockIdx.y;
@@ -850,6 +901,7 @@ struct GradGeo {
   int32_t* status;
   int32_t* abort_flag;
   unsigned long long limit_ns;
+  int32_t mark;
 };
 
 __global__ void __launch_bounds__(kGradThreads, 1)
@@ -868,7 +920,7 @@ __global__ void __launch_bounds__(kGradThreads, 1)
   const uint32_t drain_bar = bar_base + 8u * (3 * kGradStages + 4);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t smem_base = smem_u32(smem);
-  const WaitCtl wc{g.status, g.abort_flag, g.limit_ns};
+  const WaitCtl wc{g.status, g.abort_flag, g.limit_ns, g.mark};
   constexpr uint32_t kCols = 64 * kParts;
 
   if (threadIdx.x == 0) {
@@ -1130,6 +1182,7 @@ struct Call {
   const int32_t* plan;
   int32_t* status;
   int32_t* abort_flag;
+  int32_t mark;  // this call's value of the abort flag: the workspace needs no clearing
   cudaStream_t s;
 };
 
@@ -1178,7 +1231,6 @@ cudaError_t shrink(const Call& c, const void* X, int64_t ldx, int64_t d, const _
   g.marks = marks;
   g.n = c.n;
   g.kp = c.kp;
-  g.parts = parts;
   // few tokens: a small ring, so that k_adapter_few's CTAs fit beside these
   g.stages = parts > 1 ? 5 : c.N <= kTile ? 3 : kMaxStages;
   g.plan = c.plan;
@@ -1187,14 +1239,15 @@ cudaError_t shrink(const Call& c, const void* X, int64_t ldx, int64_t d, const _
   g.status = c.status;
   g.abort_flag = c.abort_flag;
   g.limit_ns = wait_limit_ns();
+  g.mark = c.mark;
   // slots are known to the device only: between one per tile and smax
   int64_t guess = c.p.tiles > c.n ? c.p.tiles : c.n;
   if (guess > c.p.smax) guess = c.p.smax;
   const int ks = cluster_split(guess, (d + 63) / 64);
   int64_t clusters = sm_count() / ks;
   if (clusters > c.p.smax) clusters = c.p.smax;
-  return launch_cluster(k_adapter_shrink, dim3(unsigned(clusters * ks)), kShrinkThreads, shrink_smem(parts, g.stages), ks,
-                        false, c.s, mx, mp, g);
+  return launch_cluster(parts == 1 ? k_adapter_shrink<1> : k_adapter_shrink<kParts>, dim3(unsigned(clusters * ks)),
+                        kShrinkThreads, shrink_smem(parts, g.stages), ks, false, c.s, mx, mp, g);
 }
 
 // Y = X W^T + U (packed B)^T (kWmn false: W is o x d) or dX = dY W + T (packed A)^T (true: W is d x o).
@@ -1224,6 +1277,7 @@ cudaError_t project(const Call& c, const void* X, int64_t ldx, int64_t d, const 
     g.status = c.status;
     g.abort_flag = c.abort_flag;
     g.limit_ns = wait_limit_ns();
+    g.mark = c.mark;
     if (!gp::map_2d(&mx, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, X, d, c.N, ldx, 64, g.nt) ||
         !gp::map_2d(&mu, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, U, kMaxK, slots * kSlotRows, kMaxK, 64, g.nt))
       return cudaErrorInvalidValue;
@@ -1246,6 +1300,7 @@ cudaError_t project(const Call& c, const void* X, int64_t ldx, int64_t d, const 
   g.status = c.status;
   g.abort_flag = c.abort_flag;
   g.limit_ns = wait_limit_ns();
+  g.mark = c.mark;
   const AdapterExt ext{c.plan, c.p.tile_base, c.p.pair_count, c.p.pair_ad, c.p.pair_s0, c.p.pair_s1,
                        int(slots * kSlotRows), (c.k + 15) / 16};
   return gp::launch<false, kWmn>(mx, mw, mu, mb, mo, g, EpiRows{}, ext, c.s);
@@ -1271,6 +1326,7 @@ cudaError_t grad(const Call& c, const void* S, int64_t lds, int64_t d, const voi
   g.status = c.status;
   g.abort_flag = c.abort_flag;
   g.limit_ns = wait_limit_ns();
+  g.mark = c.mark;
   cudaError_t e = cudaFuncSetAttribute(k_adapter_grad, cudaFuncAttributeMaxDynamicSharedMemorySize, kGradSmem);
   if (e != cudaSuccess) return e;
   const int64_t items = int64_t(c.n) * g.ctiles * ranges;
@@ -1298,6 +1354,9 @@ Call call_of(int64_t N, int n, int k, const void* plan, void* workspace, int32_t
   c.plan = static_cast<const int32_t*>(plan);
   c.status = status;
   c.abort_flag = static_cast<int32_t*>(workspace);
+  // no earlier call's mark (nor, but for one chance in 2^31, what else lay in the workspace)
+  static std::atomic<uint32_t> calls{0x2545f491u};
+  c.mark = int32_t(calls.fetch_add(0x9e3779b1u, std::memory_order_relaxed) | 1u);
   c.s = s;
   return c;
 }
@@ -1354,9 +1413,7 @@ cudaError_t launch_adapter_apply(const void* X, int64_t ldx, int64_t N, int64_t 
   const PackLay pk = pack_lay(n, d_in, d_out, k);
   const uint8_t* pb = static_cast<const uint8_t*>(packed);
   uint8_t* ws = static_cast<uint8_t*>(workspace);
-  cudaError_t e = cudaMemsetAsync(workspace, 0, 4, s);
-  if (e != cudaSuccess) return e;
-  e = shrink(c, X, ldx, d_in, reinterpret_cast<const __nv_bfloat16*>(pb + pk.a),
+  cudaError_t e = shrink(c, X, ldx, d_in, reinterpret_cast<const __nv_bfloat16*>(pb + pk.a),
              reinterpret_cast<const int32_t*>(pb + pk.marks), 1, ws + w.u);
   if (e != cudaSuccess) return e;
   return project<false>(c, X, ldx, d_in, W, d_out, reinterpret_cast<const __nv_bfloat16*>(pb + pk.b), ws + w.u, Y, ldy);
@@ -1375,8 +1432,7 @@ cudaError_t launch_adapter_backward(const void* X, int64_t ldx, const void* dY, 
   const __nv_bfloat16* pB = reinterpret_cast<const __nv_bfloat16*>(pb + pk.b);
   uint8_t* ws = static_cast<uint8_t*>(workspace);
   float* part = reinterpret_cast<float*>(ws + w.part);
-  cudaError_t e = cudaMemsetAsync(workspace, 0, 4, s);
-  if (e != cudaSuccess) return e;
+  cudaError_t e = cudaSuccess;
   if (dB) {
     e = shrink(c, X, ldx, d_in, pa, marks, kParts, ws + w.u);
     if (e != cudaSuccess) return e;

@@ -66,6 +66,7 @@ struct Geo {
   int32_t* status;
   int32_t* abort_flag;
   unsigned long long limit_ns;
+  int32_t mark = 1;  // value of the abort flag that means this launch's
 };
 
 struct Tile {
@@ -189,7 +190,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
   const bool leader = rank == 0;
   const int cid = int(cluster_id_x());
   const int ncl = int(ncluster_x());
-  const WaitCtl wc{g.status, g.abort_flag, g.limit_ns};
+  const WaitCtl wc{g.status, g.abort_flag, g.limit_ns, g.mark};
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < STAGES; ++s) {

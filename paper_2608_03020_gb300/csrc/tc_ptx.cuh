@@ -47,8 +47,9 @@ __device__ __forceinline__ bool mbar_try_wait(uint32_t bar, uint32_t parity) {
 
 struct WaitCtl {
   int32_t* status;               // library status word (sticky error code)
-  volatile int32_t* abort_flag;  // launch-local: set by the first waiter that gives up
+  volatile int32_t* abort_flag;  // launch-local: set to `mark` by the first waiter that gives up
   uint64_t limit_ns;
+  int32_t mark = 1;              // a launch with a mark of its own needs no cleared flag
 };
 
 // Bounded wait for the phase of parity `parity` of barrier `bar`.  Returns false when the wait
@@ -64,11 +65,11 @@ static __device__ __noinline__ bool mbar_wait(uint32_t bar, uint32_t parity, con
     if ((it & 7u) == 0) {
       if (globaltimer() - t0 > w.limit_ns) {
         atomicExch(w.status, int32_t(LOCA_ERR_TIMEOUT));
-        *w.abort_flag = 1;
+        *w.abort_flag = w.mark;
         __threadfence();
         return false;
       }
-      if ((it & 127u) == 0 && *w.abort_flag != 0) return false;
+      if ((it & 127u) == 0 && *w.abort_flag == w.mark) return false;
     }
   }
 }
@@ -136,11 +137,11 @@ static __device__ __noinline__ bool mbar_wait_cluster(uint32_t bar, uint32_t par
     if ((it & 7u) == 0) {
       if (globaltimer() - t0 > w.limit_ns) {
         atomicExch(w.status, int32_t(LOCA_ERR_TIMEOUT));
-        *w.abort_flag = 1;
+        *w.abort_flag = w.mark;
         __threadfence();
         return false;
       }
-      if ((it & 127u) == 0 && *w.abort_flag != 0) return false;
+      if ((it & 127u) == 0 && *w.abort_flag == w.mark) return false;
     }
   }
 }
