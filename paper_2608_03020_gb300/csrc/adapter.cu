@@ -41,13 +41,15 @@ constexpr int kParts = 3;
 constexpr int kSlotRows = 128;
 constexpr size_t kSlotElems = size_t(kSlotRows) * kMaxK;
 
-__host__ __device__ inline int k_padded(int k) { return (k + 7) / 8 * 8; }
+// Rows of the packed adapters: whole MMA steps of 16 (TMA moves boxes of 16-byte rows at half the pace
+// of 32-byte ones: k = 8 took 51 us in k_adapter_shrink at d = 3584 where k = 16 took 33).
+__host__ __device__ inline int k_padded(int k) { return (k + 15) / 16 * 16; }
 
 // ------------------------------------------------------------------ plan
 // Offsets in int32 from the start of the plan.
 struct PlanLay {
   int64_t tiles, pairs, smax;
-  int64_t tok_slot, tile_base, adapter, tile, count, pair_count, pair_ad, pair_s0, pair_s1, ad_off, ad_slots, total;
+  int64_t tok_slot, tok_adapter, tile_base, adapter, tile, count, pair_count, pair_ad, pair_s0, pair_s1, ad_off, ad_slots, total;
 };
 PlanLay plan_lay(int64_t N, int n) {
   PlanLay p{};
@@ -62,6 +64,7 @@ PlanLay plan_lay(int64_t N, int n) {
     return o;
   };
   p.tok_slot = take(N);
+  p.tok_adapter = take(N);
   p.tile_base = take(p.tiles + 2);
   p.adapter = take(p.smax);
   p.tile = take(p.smax);
@@ -120,7 +123,10 @@ __global__ void __launch_bounds__(kTile) k_plan_tiles(const int32_t* __restrict_
     }
   }
   __syncthreads();
-  if (tok < N) plan[p.tok_slot + tok] = a >= 0 ? base + rank[first] : -1;
+  if (tok < N) {
+    plan[p.tok_slot + tok] = a >= 0 ? base + rank[first] : -1;
+    plan[p.tok_adapter + tok] = a;
+  }
 }
 
 // tile_base: counts to offsets (one block; `tiles` entries in runs of 1024).
@@ -291,37 +297,37 @@ __global__ void __launch_bounds__(256)
 }
 
 // ------------------------------------------------------------------ U and T: tokens x k sums over d
-// One item per slot, its d axis split over the CTAs of a cluster.  A slot with more than kFewTokens
-// tokens goes through the tensor cores: M = the tile's 128 tokens, N = 64 columns per part of the
-// adapter.  A slot with fewer (decode) multiplies its tokens one by one, reading the adapter once:
-// the tile's other rows would cost 64 times the loads.  The CTAs add their sums through distributed
-// shared memory in rank order, zero the rows of other slots and write the parts.
-constexpr int kFewTokens = 16;
-constexpr int kTokGroup = 4;
+// One item per slot: M = the tile's 128 tokens, N = 64 columns per part of the adapter, K = d.  With
+// few slots the d axis is split over the CTAs of a cluster, which add their sums through distributed
+// shared memory in rank order.  Rows of other slots are written as zeros.
 constexpr int kShrinkThreads = 192;
 constexpr int kShrinkSeg = 8;                    // k-blocks per accumulation segment (three parts)
 constexpr int kMaxStages = 8;
 constexpr int kRedBytes = kSlotRows * kMaxK * 4; // 32 KB of fp32 sums, in the place of the ring
 constexpr int kXBytes = 128 * 64 * 2, kPBytes = 64 * 64 * 2;
 
-struct ShrinkGeo {
+struct ShrinkOne {
   const __nv_bfloat16* X;
-  int64_t ldx, N, d;
+  int64_t ldx, d;
   const __nv_bfloat16* P;  // packed adapter operand: part x adapter x d x kp
+  __nv_bfloat16* out;      // parts x smax x 128 x 64
+};
+struct ShrinkGeo {
+  ShrinkOne one[2];  // a backward pass makes U from X and T from dY in one launch
+  int sets;
+  int64_t N;
   const int32_t* marks;
   int n, kp, stages;
   const int32_t* plan;
   PlanLay p;
-  __nv_bfloat16* out;  // parts x smax x 128 x 64
   int32_t* status;
   int32_t* abort_flag;
   unsigned long long limit_ns;
   int32_t mark;
 };
-constexpr int kFewXBytes = kTokGroup * 4096 * 2;  // X of the few tokens, behind the sums
 int shrink_ring(int parts, int stages) {
   const int b = stages * (kXBytes + parts * kPBytes);
-  return b > kRedBytes + kFewXBytes ? b : kRedBytes + kFewXBytes;
+  return b > kRedBytes ? b : kRedBytes;
 }
 int shrink_smem(int parts, int stages) { return shrink_ring(parts, stages) + 512 + 1024; }
 
@@ -330,112 +336,16 @@ __device__ __forceinline__ int red_at(int row, int col) {
   return row * kMaxK + (((col >> 2) ^ (row & 15)) << 2) + (col & 3);
 }
 
-// The few tokens of a slot, rows list[0 .. members): sums over k0 .. k1 into red, kTok tokens at a time.
-// Their X is staged in shared memory; thread t takes the 16-byte chunk t % nc of the adapter rows
-// t / nc, t / nc + stride, ... with kBatch loads in flight.
-constexpr int kFewK = 4096;   // k staged at a time
-template <int kP, int kTok>
-__device__ __forceinline__ void shrink_few(const ShrinkGeo& g, int a, int64_t row0, const int* list, int members,
-                                           int64_t k0, int64_t k1, float* red, __nv_bfloat16* xs, float* part) {
-  constexpr int kBatch = kP == 1 ? 8 : 2;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int chunks = g.kp / 8;
-  const int nc = chunks <= 1 ? 1 : chunks <= 2 ? 2 : chunks <= 4 ? 4 : 8;
-  const int c = threadIdx.x % nc, r0 = threadIdx.x / nc, stride = kShrinkThreads / nc;
-  const int64_t pitch = int64_t(g.n) * g.d * g.kp;
-  const __nv_bfloat16* P = g.P + int64_t(a) * g.d * g.kp + c * 8;
-  for (int t0 = 0; t0 < members; t0 += kTok) {
-    float acc[kTok][8];
-#pragma unroll
-    for (int t = 0; t < kTok; ++t)
-#pragma unroll
-      for (int i = 0; i < 8; ++i) acc[t][i] = 0.f;
-    for (int64_t kc = k0; kc < k1; kc += kFewK) {
-      const int kn = int(k1 - kc < kFewK ? k1 - kc : kFewK);
-      auto load = [&](uint4 (&v)[kBatch][kP], int r) {
-#pragma unroll
-        for (int j = 0; j < kBatch; ++j)
-#pragma unroll
-          for (int q = 0; q < kP; ++q)
-            if (c < chunks && r + j * stride < kn)
-              v[j][q] = __ldg(reinterpret_cast<const uint4*>(P + q * pitch + (kc + r + j * stride) * g.kp));
-      };
-      uint4 v[kBatch][kP];
-      load(v, r0);  // in flight while X is staged
-      __syncthreads();
-#pragma unroll
-      for (int t = 0; t < kTok; ++t) {
-        const int m = t0 + t < members ? t0 + t : members - 1;
-        const uint4* src = reinterpret_cast<const uint4*>(g.X + (row0 + list[m]) * g.ldx + kc);
-        for (int i = threadIdx.x; i < kn / 8; i += kShrinkThreads) reinterpret_cast<uint4*>(xs + t * kFewK)[i] = src[i];
-      }
-      __syncthreads();
-      for (int r = r0; r < kn; r += kBatch * stride) {
-        if (r != r0) load(v, r);
-        if (c < chunks) {
-#pragma unroll
-          for (int j = 0; j < kBatch; ++j) {
-            if (r + j * stride < kn) {
-              float w[8] = {};
-#pragma unroll
-              for (int q = kP - 1; q >= 0; --q) {
-                const __nv_bfloat162* h = reinterpret_cast<const __nv_bfloat162*>(&v[j][q]);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                  const float2 f = __bfloat1622float2(h[i]);
-                  w[2 * i] += f.x;
-                  w[2 * i + 1] += f.y;
-                }
-              }
-#pragma unroll
-              for (int t = 0; t < kTok; ++t) {
-                const float x = __bfloat162float(xs[t * kFewK + r + j * stride]);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) acc[t][i] = fmaf(x, w[i], acc[t][i]);
-              }
-            }
-          }
-        }
-      }
-    }
-    __syncwarp();
-#pragma unroll
-    for (int t = 0; t < kTok; ++t)
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        float s = acc[t][i];
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1)
-          if (o >= nc) s += __shfl_xor_sync(0xffffffffu, s, o);
-        if (lane < nc) part[(warp * kTok + t) * kMaxK + lane * 8 + i] = s;
-      }
-    __syncthreads();
-    for (int e = threadIdx.x; e < kTok * kMaxK; e += kShrinkThreads) {
-      const int t = e / kMaxK, col = e % kMaxK;
-      if (t0 + t < members) {
-        float s = 0.f;
-        if (col < g.kp) {
-#pragma unroll
-          for (int w = 0; w < kShrinkThreads / 32; ++w) s += part[(w * kTok + t) * kMaxK + col];
-        }
-        red[red_at(list[t0 + t], col)] = s;
-      }
-    }
-    __syncthreads();
-  }
-}
-
 template <int kP>
 __global__ void __launch_bounds__(kShrinkThreads, 1)
-    k_adapter_shrink(const __grid_constant__ CUtensorMap tmX, const __grid_constant__ CUtensorMap tmP,
+    k_adapter_shrink(const __grid_constant__ CUtensorMap tmX0, const __grid_constant__ CUtensorMap tmP0,
+                     const __grid_constant__ CUtensorMap tmX1, const __grid_constant__ CUtensorMap tmP1,
                      const __grid_constant__ ShrinkGeo g) {
   extern __shared__ uint8_t smem_raw[];
-  __shared__ float few_part[kShrinkThreads / 32 * kTokGroup * kMaxK];
-  __shared__ int few_list[kFewTokens];
   __shared__ uint32_t members_of[kTile / 32];  // the tile's rows that belong to the slot
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   constexpr int stage_bytes = kXBytes + kP * kPBytes;
-  const int ring = g.stages * stage_bytes > kRedBytes + kFewXBytes ? g.stages * stage_bytes : kRedBytes + kFewXBytes;
+  const int ring = g.stages * stage_bytes > kRedBytes ? g.stages * stage_bytes : kRedBytes;
   uint64_t* bars = reinterpret_cast<uint64_t*>(smem + ring);
   const uint32_t bar_base = smem_u32(bars);
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 * kMaxStages + 5);
@@ -445,7 +355,6 @@ __global__ void __launch_bounds__(kShrinkThreads, 1)
   auto acc_empty = [&](uint32_t b) { return bar_base + 8u * (2 * kMaxStages + 2 + b); };
   const uint32_t drain_bar = bar_base + 8u * (2 * kMaxStages + 4);
   float* red = reinterpret_cast<float*>(smem);  // [128][64] sums of this CTA
-  __nv_bfloat16* few_x = reinterpret_cast<__nv_bfloat16*>(smem + kRedBytes);
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t smem_base = smem_u32(smem);
@@ -455,10 +364,7 @@ __global__ void __launch_bounds__(kShrinkThreads, 1)
   constexpr uint32_t acc_cols = uint32_t(64 * kP);
   constexpr uint32_t cols = kP == 1 ? 128u : 512u;
 
-  launch_dependents();
-  const int total = g.plan[g.p.tile_base + g.p.tiles];
   if (threadIdx.x == 0) {
-    if (blockIdx.x == 0) *g.abort_flag = 0;  // a captured call that gave up may be replayed
     for (int s = 0; s < kMaxStages; ++s) {
       mbar_init(full_bar(s), 1);
       mbar_init(empty_bar(s), 1);
@@ -469,51 +375,52 @@ __global__ void __launch_bounds__(kShrinkThreads, 1)
     }
     mbar_init(drain_bar, 1);
     mbar_init_fence();
-    prefetch_tensormap(&tmX);
-    prefetch_tensormap(&tmP);
+    prefetch_tensormap(&tmX0);
+    prefetch_tensormap(&tmP0);
+    if (g.sets > 1) {
+      prefetch_tensormap(&tmX1);
+      prefetch_tensormap(&tmP1);
+    }
   }
   if (warp == 1) tmem_alloc(smem_u32(tmem_slot), cols);
   fence_before();
   __syncthreads();
   fence_after();
   const uint32_t tmem_base = *tmem_slot;
-  const int nkb = int((g.d + 63) / 64);
-  const int per = (nkb + ks - 1) / ks;
-  const int kb0 = rank * per < nkb ? rank * per : nkb;
-  const int kb1 = kb0 + per < nkb ? kb0 + per : nkb;
-  const int nb = kb1 - kb0;
+  wait_for_previous();
+  launch_dependents();
+  if (blockIdx.x == 0 && threadIdx.x == 0) *g.abort_flag = 0;  // a captured call that gave up may be replayed
+  const int total = g.plan[g.p.tile_base + g.p.tiles];
   constexpr int seg_kb = kP == 1 ? 64 : kShrinkSeg;
+  const int64_t part_pitch = g.p.smax * int64_t(kSlotElems);
 
   int stage = 0;
   uint32_t phase = 0, iter = 0, seg = 0;
   bool ok = true, issued = false;
-  for (int s = cid; s < total; s += ncl) {
+  for (int it = cid; it < total * g.sets; it += ncl) {
+    const int set = it >= total ? 1 : 0;
+    const int s = it - set * total;
+    const ShrinkOne& o = g.one[set];
+    const int nkb = int((o.d + 63) / 64);
+    const int per = (nkb + ks - 1) / ks;
+    const int kb0 = rank * per < nkb ? rank * per : nkb;
+    const int kb1 = kb0 + per < nkb ? kb0 + per : nkb;
+    const int nb = kb1 - kb0;
     const int a = g.plan[g.p.adapter + s];
     const int64_t row0 = int64_t(g.plan[g.p.tile + s]) * kTile;
-    const int members = g.plan[g.p.count + s];
     const bool spoiled = g.marks[a] != 0;
-    if (warp >= 2) {  // the rows of the tile that are this slot's
-      const int r = (warp - 2) * 32 + lane;
-      const bool mine = row0 + r < g.N && g.plan[g.p.tok_slot + row0 + r] == s;
-      const unsigned all = __ballot_sync(0xffffffffu, mine);
-      if (lane == 0) members_of[warp - 2] = all;
-    }
-    if (members <= kFewTokens) {
-      __syncthreads();
-      if (warp == 0) {
-        int at = 0;
-        for (int b = 0; b < kTile / 32; ++b) {
-          const unsigned all = members_of[b];
-          const int pos = at + __popc(all & ((1u << lane) - 1u));
-          if ((all >> lane & 1u) && pos < kFewTokens) few_list[pos] = b * 32 + lane;
-          at += __popc(all);
-        }
+    // one CTA for the whole k: the sums go from registers to memory, and the roles need not meet
+    const bool direct = ks == 1;
+    bool mine = false;  // this thread's row of the tile is the slot's
+    if (warp >= 2) {
+      const int r = (warp & 3) * 32 + lane;
+      mine = row0 + r < g.N && g.plan[g.p.tok_slot + row0 + r] == s;
+      if (!direct) {
+        const unsigned all = __ballot_sync(0xffffffffu, mine);
+        if (lane == 0) members_of[warp & 3] = all;
       }
-      __syncthreads();
-      const int64_t k0 = int64_t(kb0) * 64, k1 = int64_t(kb1) * 64 < g.d ? int64_t(kb1) * 64 : g.d;
-      if (members == 1) shrink_few<kP, 1>(g, a, row0, few_list, members, k0, k1, red, few_x, few_part);
-      else shrink_few<kP, kTokGroup>(g, a, row0, few_list, members, k0, k1, red, few_x, few_part);
-    } else if (warp == 0) {
+    }
+    if (warp == 0) {
       // ---------------- TMA producer
       if (lane == 0 && ok) {
         for (int kb = kb0; kb < kb1; ++kb) {
@@ -523,10 +430,10 @@ __global__ void __launch_bounds__(kShrinkThreads, 1)
           }
           mbar_arrive_expect_tx(full_bar(stage), uint32_t(stage_bytes));
           const uint32_t dst = smem_base + uint32_t(stage * stage_bytes);
-          tma_load_2d(dst, &tmX, full_bar(stage), kb * 64, int(row0));
+          tma_load_2d(dst, set ? &tmX1 : &tmX0, full_bar(stage), kb * 64, int(row0));
 #pragma unroll
           for (int q = 0; q < kP; ++q)
-            tma_load_3d(dst + kXBytes + q * kPBytes, &tmP, full_bar(stage), 0, kb * 64, q * g.n + a);
+            tma_load_3d(dst + kXBytes + q * kPBytes, set ? &tmP1 : &tmP0, full_bar(stage), 0, kb * 64, q * g.n + a);
           ++iter;
           if (++stage == g.stages) { stage = 0; phase ^= 1u; }
         }
@@ -598,7 +505,25 @@ __global__ void __launch_bounds__(kShrinkThreads, 1)
         if (lane == 0) mbar_arrive(acc_empty(b));
         ++seg;
       }
-      if (ok) {
+      if (ok && direct) {
+        __nv_bfloat16* to = o.out + (int64_t(s) * kSlotRows + q * 32 + lane) * kMaxK;
+#pragma unroll
+        for (int i = 0; i < 64; ++i) u[i] = mine ? (spoiled ? __int_as_float(0x7fffffff) : u[i]) : 0.f;
+#pragma unroll
+        for (int p = 0; p < kP; ++p) {
+#pragma unroll
+          for (int c = 0; c < 8; ++c) {
+            __align__(16) __nv_bfloat16 w[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+              w[i] = __float2bfloat16_rn(u[8 * c + i]);
+              u[8 * c + i] -= __bfloat162float(w[i]);
+            }
+            if (LOCA_CHECK(s, g.p.smax))
+              *reinterpret_cast<uint4*>(to + p * part_pitch + 8 * c) = *reinterpret_cast<const uint4*>(w);
+          }
+        }
+      } else if (ok) {
         const int row = q * 32 + lane;
 #pragma unroll
         for (int c = 0; c < 16; ++c)
@@ -606,6 +531,7 @@ __global__ void __launch_bounds__(kShrinkThreads, 1)
               make_float4(u[4 * c], u[4 * c + 1], u[4 * c + 2], u[4 * c + 3]);
       }
     }
+    if (direct) continue;
     __syncwarp();
     cluster_sync();  // every CTA's sums are in its shared memory
     const int rows_per = kSlotRows / ks;
@@ -634,8 +560,7 @@ __global__ void __launch_bounds__(kShrinkThreads, 1)
           for (int i = 0; i < 8; ++i) v[i] = __int_as_float(0x7fffffff);
         }
       }
-      __nv_bfloat16* to = g.out + (int64_t(s) * kSlotRows + row) * kMaxK + ch * 8;
-      const int64_t pitch = g.p.smax * int64_t(kSlotElems);
+      __nv_bfloat16* to = o.out + (int64_t(s) * kSlotRows + row) * kMaxK + ch * 8;
 #pragma unroll
       for (int q = 0; q < kP; ++q) {
         __align__(16) __nv_bfloat16 w[8];
@@ -644,7 +569,7 @@ __global__ void __launch_bounds__(kShrinkThreads, 1)
           w[i] = __float2bfloat16_rn(v[i]);
           v[i] -= __bfloat162float(w[i]);
         }
-        if (LOCA_CHECK(s, g.p.smax)) *reinterpret_cast<uint4*>(to + q * pitch) = *reinterpret_cast<const uint4*>(w);
+        if (LOCA_CHECK(s, g.p.smax)) *reinterpret_cast<uint4*>(to + q * part_pitch) = *reinterpret_cast<const uint4*>(w);
       }
     }
     fence_proxy_async_smem();  // the ring's next loads come after these accesses
@@ -667,12 +592,92 @@ __global__ void __launch_bounds__(kShrinkThreads, 1)
   if (warp == 1) tmem_dealloc(tmem_base, cols);
 }
 
+// ------------------------------------------------------------------ a step's tokens, one by one
+// U of single tokens for a decode batch whose tokens mostly have an adapter each: a tile of 128 rows
+// per slot would load X 64 times.  One block per (token, range of d), fp32 sums of the adapter's first
+// part, left as one partial sum per range; k_adapter_few adds them.  Bound: the read of each token's
+// adapter (2 d k bytes; shared adapters come from L2).
+constexpr int kTokThreads = 256;
+constexpr int kTokAhead = 4;
+
+struct TokGeo {
+  const __nv_bfloat16* X;
+  int64_t ldx, d, N;
+  const __nv_bfloat16* P;  // adapter x d x kp
+  const int32_t* marks;
+  const int32_t* tok_adapter;
+  int kp, ranges;
+  float* out;              // ranges x N x kp
+  int32_t* abort_flag;
+};
+
+__global__ void __launch_bounds__(kTokThreads) k_adapter_tokens(const TokGeo g) {
+  __shared__ float part[kTokThreads / 32][kMaxK];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  wait_for_previous();
+  launch_dependents();
+  if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) *g.abort_flag = 0;
+  const int64_t n = blockIdx.y;
+  const int a = g.tok_adapter[n];
+  if (a < 0) return;  // k_adapter_few does not read this token's sums
+  const bool spoiled = g.marks[a] != 0;
+  const int chunks = g.kp / 8;  // 16-byte chunks of an adapter row: 2, 4, 6 or 8
+  const int nc = chunks <= 2 ? 2 : chunks <= 4 ? 4 : 8;
+  const int c = threadIdx.x % nc, stride = kTokThreads / nc;
+  const int64_t blocks = (g.d + 63) / 64, per = (blocks + g.ranges - 1) / g.ranges * 64;
+  const int64_t k0 = int64_t(blockIdx.x) * per;
+  const int64_t k1 = k0 + per < g.d ? k0 + per : g.d;
+  const __nv_bfloat16* P = g.P + int64_t(a) * g.d * g.kp + c * 8;
+  const __nv_bfloat16* x = g.X + n * g.ldx;
+  float acc[8] = {};
+  if (c < chunks) {
+    for (int64_t k = k0 + threadIdx.x / nc; k < k1; k += kTokAhead * stride) {
+      uint4 v[kTokAhead];
+      float xv[kTokAhead];
+#pragma unroll
+      for (int j = 0; j < kTokAhead; ++j) {
+        const int64_t r = k + j * stride;
+        v[j] = r < k1 ? __ldg(reinterpret_cast<const uint4*>(P + r * g.kp)) : make_uint4(0, 0, 0, 0);
+        xv[j] = r < k1 ? __bfloat162float(x[r]) : 0.f;
+      }
+#pragma unroll
+      for (int j = 0; j < kTokAhead; ++j) {
+        const __nv_bfloat162* h = reinterpret_cast<const __nv_bfloat162*>(&v[j]);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float2 f = __bfloat1622float2(h[i]);
+          acc[2 * i] = fmaf(xv[j], f.x, acc[2 * i]);
+          acc[2 * i + 1] = fmaf(xv[j], f.y, acc[2 * i + 1]);
+        }
+      }
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+#pragma unroll
+    for (int o = 2; o < 32; o <<= 1)
+      if (o >= nc) acc[i] += __shfl_xor_sync(0xffffffffu, acc[i], o);
+    if (lane < nc) part[warp][lane * 8 + i] = acc[i];
+  }
+  __syncthreads();
+  if (threadIdx.x < unsigned(g.kp)) {
+    float s = 0.f;
+#pragma unroll
+    for (int w = 0; w < kTokThreads / 32; ++w) s += part[w][threadIdx.x];
+    g.out[(int64_t(blockIdx.x) * g.N + n) * g.kp + threadIdx.x] = spoiled ? __int_as_float(0x7fffffff) : s;
+  }
+}
+
 // ------------------------------------------------------------------ few tokens
-// D[o, n] = sum_k W[o, k] X[n, k] + (slots)  with the output channels as M = 128 and up to 128 tokens
-// as N, so that a step of 1 to 64 tokens reads W once at full tiles.  The k axis (and the slots
-// behind it) is split over a cluster of up to 8 CTAs, which add their sums through distributed
-// shared memory in rank order: d_out / 128 tiles alone would keep 28 of 152 SMs busy at
-// d_out = 3584.  The loads of W and X do not wait for k_adapter_shrink; those of U do.
+// D[o, n] = sum_k W[o, k] X[n, k] with the output channels as M = 128 and up to 128 tokens as N, so
+// that a step of 1 to 64 tokens reads W once at full tiles.  The k axis is split over a cluster of up
+// to 8 CTAs, which add their sums through distributed shared memory in rank order: d_out / 128 tiles
+// alone would keep 28 of 152 SMs busy at d_out = 3584.  The low-rank term comes in one of two ways:
+//   slots (batches that share few adapters)  as k blocks behind those of W and X, from U's slots
+//   tokens (an adapter for most tokens)      the epilogue warps, idle until the sums are complete,
+//                                            multiply U by each token's rows of s B meanwhile: a
+//                                            k-block per adapter would cost as much as W itself
+// The loads of W and X do not wait for U; only what follows them does.
 constexpr int kFewThreads = 192;
 constexpr int kWBytes = 128 * 64 * 2;
 
@@ -681,8 +686,12 @@ struct FewGeo {
   int nt;                // tokens per tile (a multiple of 16, at most 128)
   int stages;
   int ksteps;            // MMA steps of 16 per slot
+  int tokens;            // 1: the low-rank term token by token
+  int kp, ranges;        // tokens: U's columns and partial sums
+  const float* U;        // tokens: ranges x N x kp
+  const __nv_bfloat16* B;  // tokens: adapter x o x kp
   const int32_t* plan;
-  int64_t tile_base, adapter;
+  int64_t tile_base, adapter, tok_adapter;
   __nv_bfloat16* Y;
   int64_t ldy;
   int32_t* status;
@@ -690,11 +699,16 @@ struct FewGeo {
   unsigned long long limit_ns;
   int32_t mark;
 };
-int few_ring(int nt, int stages) {
+__host__ __device__ inline int few_ring(int nt, int stages) {
   const int b = stages * (kWBytes + nt * 128);
   return b > nt * 512 ? b : nt * 512;
 }
-int few_smem(int nt, int stages) { return few_ring(nt, stages) + 512 + 1024; }
+// tokens of a tile that one of ks CTAs finishes
+__host__ __device__ inline int few_own(int nt, int ks) { return (nt + ks - 1) / ks; }
+__host__ __device__ inline int few_low(int nt, int ks, int kp) { return few_own(nt, ks) * (512 + 4 * kp + 4); }
+int few_smem(int nt, int stages, int low) { return few_ring(nt, stages) + low + 512 + 1024; }
+
+__device__ __forceinline__ void epi_bar() { asm volatile("bar.sync 1, 128;" ::: "memory"); }
 
 template <bool kWmn>
 __global__ void __launch_bounds__(kFewThreads, 1)
@@ -704,23 +718,27 @@ __global__ void __launch_bounds__(kFewThreads, 1)
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   const int stage_bytes = kWBytes + g.nt * 128;
-  const int ring = g.stages * stage_bytes > g.nt * 512 ? g.stages * stage_bytes : g.nt * 512;
-  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + ring);
+  const int ks = int(cluster_nctarank()), rank = int(cluster_ctarank());
+  const int own = few_own(g.nt, ks);
+  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + few_ring(g.nt, g.stages));
   const uint32_t bar_base = smem_u32(bars);
   constexpr int kBarStages = 12;
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 * kBarStages + 1);
+  float* low = reinterpret_cast<float*>(smem + few_ring(g.nt, g.stages) + 512);  // [own][128] low-rank term
+  float* us = low + own * 128;                                                  // [own][kp] U
+  int32_t* ad = reinterpret_cast<int32_t*>(us + own * g.kp);                    // [own] adapters
   auto full_bar = [&](int s) { return bar_base + 8u * s; };
   auto empty_bar = [&](int s) { return bar_base + 8u * (kBarStages + s); };
   const uint32_t acc_full = bar_base + 8u * (2 * kBarStages);
-  float* red = reinterpret_cast<float*>(smem);  // [token][128 channels]
+  float* red = reinterpret_cast<float*>(smem);  // [token][128 channels], in the ring's place
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t smem_base = smem_u32(smem);
   const WaitCtl wc{g.status, g.abort_flag, g.limit_ns, g.mark};
-  const int ks = int(cluster_nctarank()), rank = int(cluster_ctarank());
   const int o0 = int(cluster_id_x()) * 128;
   const int64_t tile = blockIdx.y;
   const int64_t n0 = tile * g.nt;
+  const int ntok = int(g.N - n0 < g.nt ? g.N - n0 : g.nt);
   const uint32_t cols = g.nt <= 32 ? 32u : g.nt <= 64 ? 64u : 128u;
 
   if (threadIdx.x == 0) {
@@ -740,9 +758,11 @@ __global__ void __launch_bounds__(kFewThreads, 1)
   __syncthreads();
   fence_after();
   const uint32_t tmem_base = *tmem_slot;
+  // the launch that makes U lets this one start only once everything before it has completed: X, W,
+  // the packed adapters and the plan may be read now, U only after wait_for_previous()
   const int nkb = int((g.d + 63) / 64);
-  const int slot0 = g.plan[g.tile_base + tile];
-  const int steps = nkb + g.plan[g.tile_base + tile + 1] - slot0;
+  const int slot0 = g.tokens ? 0 : g.plan[g.tile_base + tile];
+  const int steps = nkb + (g.tokens ? 0 : g.plan[g.tile_base + tile + 1] - slot0);
   const int per = (steps + ks - 1) / ks;
   const int j0 = rank * per < steps ? rank * per : steps;
   const int j1 = j0 + per < steps ? j0 + per : steps;
@@ -793,10 +813,10 @@ __global__ void __launch_bounds__(kFewThreads, 1)
         const uint64_t ak = sdesc(st, 16u, 1024u, kSwizzle128B);
         const uint64_t bk = sdesc(st + kWBytes, 16u, 1024u, kSwizzle128B);
         if (j < nkb) {
-          const uint64_t ad = kWmn ? sdesc(st, kWBytes / 2, 1024u, kSwizzle128B) : ak;
+          const uint64_t ad0 = kWmn ? sdesc(st, kWBytes / 2, 1024u, kSwizzle128B) : ak;
 #pragma unroll
           for (int kk = 0; kk < 4; ++kk)
-            mma_f16(tmem_base, ad + kk * (kWmn ? 2048 >> 4 : 2), bk + kk * 2, id, j > j0 || kk > 0 ? 1u : 0u);
+            mma_f16(tmem_base, ad0 + kk * (kWmn ? 2048 >> 4 : 2), bk + kk * 2, id, j > j0 || kk > 0 ? 1u : 0u);
         } else {
           for (int kk = 0; kk < g.ksteps; ++kk)
             mma_f16(tmem_base, ak + kk * 2, bk + kk * 2, idx, j > j0 || kk > 0 ? 1u : 0u);
@@ -809,6 +829,61 @@ __global__ void __launch_bounds__(kFewThreads, 1)
     }
     __syncwarp();
   } else {
+    const int i = (warp - 2) * 32 + lane;
+    if (g.tokens) {
+      // this CTA's tokens n0 + rank + ks t: U's partial sums in order, then a row of s B per thread
+      for (int t = i; t < own; t += 128) ad[t] = rank + ks * t < ntok ? g.plan[g.tok_adapter + n0 + rank + ks * t] : -1;
+      wait_for_previous();
+      epi_bar();
+      for (int e = i; e < own * g.kp; e += 128) {
+        const int t = e / g.kp, c = e - t * g.kp;
+        float u = 0.f;
+        if (ad[t] >= 0) {
+          const float* p = g.U + (n0 + rank + ks * t) * g.kp + c;
+          float x[8];
+#pragma unroll
+          for (int r = 0; r < 8; ++r) x[r] = r < g.ranges ? p[r * g.N * g.kp] : 0.f;
+#pragma unroll
+          for (int r = 0; r < 8; ++r) u += x[r];
+        }
+        us[e] = u;
+      }
+      epi_bar();
+      const int64_t o = o0 + i;
+      for (int t0 = 0; t0 < own; t0 += 4) {  // four tokens' rows in flight
+        float y[4] = {};
+        for (int c = 0; c < g.kp; c += 16) {
+          uint4 v[4][2];
+#pragma unroll
+          for (int t = 0; t < 4; ++t) {
+            const int a = t0 + t < own ? ad[t0 + t] : -1;
+            if (a >= 0 && o < g.o) {
+              const uint4* p = reinterpret_cast<const uint4*>(g.B + (int64_t(a) * g.o + o) * g.kp + c);
+              v[t][0] = __ldg(p);
+              v[t][1] = __ldg(p + 1);
+            } else {
+              v[t][0] = v[t][1] = make_uint4(0, 0, 0, 0);
+            }
+          }
+#pragma unroll
+          for (int t = 0; t < 4; ++t) {
+            if (t0 + t < own) {
+              const float* u = us + (t0 + t) * g.kp + c;
+              const __nv_bfloat162* h = reinterpret_cast<const __nv_bfloat162*>(&v[t][0]);
+#pragma unroll
+              for (int q = 0; q < 8; ++q) {
+                const float2 f = __bfloat1622float2(h[q]);
+                y[t] = fmaf(u[2 * q], f.x, y[t]);
+                y[t] = fmaf(u[2 * q + 1], f.y, y[t]);
+              }
+            }
+          }
+        }
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+          if (t0 + t < own) low[(t0 + t) * 128 + i] = y[t];
+      }
+    }
     const int q = warp & 3;
     const bool got = j1 > j0 && mbar_wait(acc_full, 0, wc);
     const bool all = __all_sync(0xffffffffu, got);
@@ -819,10 +894,10 @@ __global__ void __launch_bounds__(kFewThreads, 1)
         tmem_ld16(tmem_base + (uint32_t(q * 32) << 16) + uint32_t(c * 16), v);
       } else {
 #pragma unroll
-        for (int i = 0; i < 16; ++i) v[i] = 0.f;
+        for (int x = 0; x < 16; ++x) v[x] = 0.f;
       }
 #pragma unroll
-      for (int i = 0; i < 16; ++i) red[(c * 16 + i) * 128 + q * 32 + lane] = v[i];
+      for (int x = 0; x < 16; ++x) red[(c * 16 + x) * 128 + q * 32 + lane] = v[x];
     }
     fence_before();
     __syncwarp();
@@ -833,11 +908,17 @@ __global__ void __launch_bounds__(kFewThreads, 1)
     const int i = (warp - 2) * 32 + lane;
     const int64_t o = o0 + i;
     const uint32_t red_s = smem_u32(red);
-    const int nt = int(g.N - n0 < g.nt ? g.N - n0 : g.nt);
-    for (int t = rank; t < nt; t += ks) {
-      float y = 0.f;
-      for (int j = 0; j < ks; ++j) y += ld_shared_cluster_f32(mapa_shared(red_s + 4u * uint32_t(t * 128 + i), uint32_t(j)));
-      if (o < g.o && LOCA_CHECK(n0 + t, g.N)) g.Y[(n0 + t) * g.ldy + o] = __float2bfloat16_rn(y);
+    for (int t = 0; t < own; ++t) {
+      const int n = rank + ks * t;
+      if (n >= ntok) break;
+      float x[8];  // all loads first: one round trip
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        x[j] = j < ks ? ld_shared_cluster_f32(mapa_shared(red_s + 4u * uint32_t(n * 128 + i), uint32_t(j))) : 0.f;
+      float y = g.tokens ? low[t * 128 + i] : 0.f;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) y += x[j];
+      if (o < g.o && LOCA_CHECK(n0 + n, g.N)) g.Y[(n0 + n) * g.ldy + o] = __float2bfloat16_rn(y);
     }
   }
   if (warp == 0 && lane == 0) {
@@ -892,12 +973,17 @@ constexpr int kGradStageBytes = kXBytes + kParts * kPBytes;  // 40 KB
 constexpr int kGradSeg = 8;
 constexpr int kGradSmem = kGradStages * kGradStageBytes + 512 + 1024;
 
+struct GradOne {
+  int64_t d;        // channels
+  int ctiles, ranges, items;
+  float* part;      // ranges x n x d x kp
+};
 struct GradGeo {
-  int64_t N, d;     // tokens, channels
-  int n, kp, ctiles, ranges;
+  GradOne one[2];
+  int64_t N;
+  int n, kp, items;  // of both
   const int32_t* plan;
   PlanLay p;
-  float* part;      // ranges x n x d x kp
   int32_t* status;
   int32_t* abort_flag;
   unsigned long long limit_ns;
@@ -905,7 +991,8 @@ struct GradGeo {
 };
 
 __global__ void __launch_bounds__(kGradThreads, 1)
-    k_adapter_grad(const __grid_constant__ CUtensorMap tmS, const __grid_constant__ CUtensorMap tmU,
+    k_adapter_grad(const __grid_constant__ CUtensorMap tmS0, const __grid_constant__ CUtensorMap tmU0,
+                   const __grid_constant__ CUtensorMap tmS1, const __grid_constant__ CUtensorMap tmU1,
                    const __grid_constant__ GradGeo g) {
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
@@ -935,28 +1022,37 @@ __global__ void __launch_bounds__(kGradThreads, 1)
     }
     mbar_init(drain_bar, 1);
     mbar_init_fence();
-    prefetch_tensormap(&tmS);
-    prefetch_tensormap(&tmU);
+    prefetch_tensormap(&tmS0);
+    prefetch_tensormap(&tmU0);
+    if (g.one[1].items) {
+      prefetch_tensormap(&tmS1);
+      prefetch_tensormap(&tmU1);
+    }
   }
   if (warp == 1) tmem_alloc(smem_u32(tmem_slot), 512);
   fence_before();
   __syncthreads();
   fence_after();
   const uint32_t tmem_base = *tmem_slot;
-  const int per_a = g.ctiles * g.ranges;
-  const int items = g.n * per_a;
+  wait_for_previous();
+  launch_dependents();
+  const int items = g.items;
   uint32_t iter = 0;
   struct Item {
-    int a, ct, range, s0, s1;  // s0 .. s1: places in the adapter's list of slots
+    int set, a, ct, range, s0, s1;  // s0 .. s1: places in the adapter's list of slots
   };
   auto item_of = [&](int it) {
     Item w;
+    w.set = it >= g.one[0].items ? 1 : 0;
+    const GradOne& o = g.one[w.set];
+    if (w.set) it -= g.one[0].items;
+    const int per_a = o.ctiles * o.ranges;
     w.a = it / per_a;
     const int r = it - w.a * per_a;
-    w.range = r / g.ctiles;  // channel tiles fastest: CTAs at work share a range's U or T
-    w.ct = r - w.range * g.ctiles;
+    w.range = r / o.ctiles;  // channel tiles fastest: CTAs at work share a range's U or T
+    w.ct = r - w.range * o.ctiles;
     const int b0 = g.plan[g.p.ad_off + w.a], b1 = g.plan[g.p.ad_off + w.a + 1];
-    const int per = (b1 - b0 + g.ranges - 1) / g.ranges;
+    const int per = (b1 - b0 + o.ranges - 1) / o.ranges;
     w.s0 = b0 + w.range * per < b1 ? b0 + w.range * per : b1;
     w.s1 = w.s0 + per < b1 ? w.s0 + per : b1;
     return w;
@@ -979,10 +1075,12 @@ __global__ void __launch_bounds__(kGradThreads, 1)
             }
             mbar_arrive_expect_tx(full_bar(stage), uint32_t(kGradStageBytes));
             const uint32_t dst = smem_base + uint32_t(stage * kGradStageBytes);
-            tma_load_2d(dst, &tmS, full_bar(stage), w.ct * 128, row + 64 * h);
-            tma_load_2d(dst + kXBytes / 2, &tmS, full_bar(stage), w.ct * 128 + 64, row + 64 * h);
+            const CUtensorMap* ms = w.set ? &tmS1 : &tmS0;
+            const CUtensorMap* mu = w.set ? &tmU1 : &tmU0;
+            tma_load_2d(dst, ms, full_bar(stage), w.ct * 128, row + 64 * h);
+            tma_load_2d(dst + kXBytes / 2, ms, full_bar(stage), w.ct * 128 + 64, row + 64 * h);
             for (int q = 0; q < kParts; ++q)
-              tma_load_3d(dst + kXBytes + q * kPBytes, &tmU, full_bar(stage), 0, s * kSlotRows + 64 * h, q);
+              tma_load_3d(dst + kXBytes + q * kPBytes, mu, full_bar(stage), 0, s * kSlotRows + 64 * h, q);
             ++iter;
             if (++stage == kGradStages) { stage = 0; phase ^= 1u; }
           }
@@ -1108,8 +1206,9 @@ __global__ void __launch_bounds__(kGradThreads, 1)
       }
       if (!ok) break;
       const int64_t ch = int64_t(w.ct) * 128 + q * 32 + lane;
-      if (ch < g.d) {
-        float* to = g.part + ((int64_t(w.range) * g.n + w.a) * g.d + ch) * g.kp;
+      const GradOne& o = g.one[w.set];
+      if (ch < o.d) {
+        float* to = o.part + ((int64_t(w.range) * g.n + w.a) * o.d + ch) * g.kp;
 #pragma unroll
         for (int c = 0; c < 16; ++c)
           if (4 * c < g.kp)
@@ -1127,26 +1226,51 @@ __global__ void __launch_bounds__(kGradThreads, 1)
   if (warp == 1) tmem_dealloc(tmem_base, 512);
 }
 
+struct JoinOne {
+  const float* part;
+  const float* scale;  // per adapter, or null
+  void* out;
+  int64_t rows, d;     // n d rows of k values (0: nothing to do)
+  int ranges;
+};
 template <class T>
-__global__ void __launch_bounds__(256)
-    k_adapter_join(const float* __restrict__ part, int ranges, int n, int64_t d, int k, int kp,
-                   const float* __restrict__ scale, T* __restrict__ out) {
-  const int64_t rows = int64_t(n) * d;
-  for (int64_t i = int64_t(blockIdx.x) * blockDim.x + threadIdx.x; i < rows * k; i += int64_t(gridDim.x) * blockDim.x) {
+__global__ void __launch_bounds__(256) k_adapter_join(const JoinOne j0, const JoinOne j1, int k, int kp) {
+  wait_for_previous();
+  launch_dependents();
+  const int64_t n0 = j0.rows * k;
+  for (int64_t e = int64_t(blockIdx.x) * blockDim.x + threadIdx.x; e < n0 + j1.rows * k;
+       e += int64_t(gridDim.x) * blockDim.x) {
+    const JoinOne& j = e < n0 ? j0 : j1;
+    const int64_t i = e < n0 ? e : e - n0;
     const int64_t row = i / k;
     const int c = int(i - row * k);
+    const float* p = j.part + row * kp + c;
+    const int64_t pitch = j.rows * kp;
     float v = 0.f;
-    for (int r = 0; r < ranges; ++r) v += part[(int64_t(r) * rows + row) * kp + c];
-    if (scale) v *= scale[row / d];
-    if constexpr (sizeof(T) == 4) out[i] = v;
-    else out[i] = __float2bfloat16_rn(v);
+#pragma unroll 8
+    for (int r = 0; r < j.ranges; ++r) v += p[r * pitch];
+    if (j.scale) v *= j.scale[row / j.d];
+    if constexpr (sizeof(T) == 4) static_cast<float*>(j.out)[i] = v;
+    else static_cast<__nv_bfloat16*>(j.out)[i] = __float2bfloat16_rn(v);
   }
 }
 
 // ------------------------------------------------------------------ host side
+// Token by token, or by slots: a batch in which one adapter serves few tokens (there are more than
+// N / 4 adapters) spends one slot per token or two.  64 tokens with an adapter each at d = 3584,
+// k = 16: 30 us by slots; measured both ways below.
+bool by_token(int64_t N, int n) { return N <= 16 || (N <= 512 && 4 * int64_t(n) > N); }
+// Ranges of d for the token kernel: about four blocks per SM.
+int tok_ranges(int64_t N, int64_t d) {
+  int64_t r = 4 * int64_t(sm_count()) / (N < 1 ? 1 : N);
+  const int64_t most = (d + 255) / 256;
+  if (r > most) r = most;
+  if (r > 8) r = 8;
+  return int(r < 1 ? 1 : r);
+}
+
 struct AdapterWs {
-  size_t flags, u, t, part, total;
-  int parts;
+  size_t u, t, part_in, part_out, total;
   int ranges_in, ranges_out;
 };
 // Token ranges of dA / dB: enough items for two rounds of the SMs, at most one per token tile.
@@ -1159,17 +1283,19 @@ int grad_ranges(int n, int64_t d, int64_t tiles) {
 AdapterWs adapter_ws(int64_t N, int64_t d_in, int64_t d_out, int k, int n, bool backward) {
   AdapterWs w{};
   const PlanLay p = plan_lay(N, n);
-  w.parts = backward ? kParts : 1;
-  const size_t one = align256(2 * kSlotElems * size_t(p.smax < 1 ? 1 : p.smax) * size_t(w.parts));
-  size_t at = 256;
-  w.u = at; at += one;
+  const size_t one = align256(2 * kSlotElems * size_t(p.smax < 1 ? 1 : p.smax) * size_t(backward ? kParts : 1));
+  size_t at = 256;  // the launches' abort flag
+  // U: the slots' tiles, or the tokens' partial sums
+  const size_t tok = align256(4 * 8 * size_t(N) * size_t(k_padded(k)));
+  const size_t need = by_token(N, n) && tok > one ? tok : one;
+  w.u = at; at += need;
   if (backward) {
-    w.t = at; at += one;
+    w.t = at; at += need;
     w.ranges_in = grad_ranges(n, d_in, p.tiles);
     w.ranges_out = grad_ranges(n, d_out, p.tiles);
     const size_t kp = size_t(k_padded(k));
-    const size_t pi = size_t(w.ranges_in) * n * size_t(d_in) * kp, po = size_t(w.ranges_out) * n * size_t(d_out) * kp;
-    w.part = at; at += align256(4 * (pi > po ? pi : po));
+    w.part_in = at; at += align256(4 * size_t(w.ranges_in) * n * size_t(d_in) * kp);
+    w.part_out = at; at += align256(4 * size_t(w.ranges_out) * n * size_t(d_out) * kp);
   }
   w.total = at;
   return w;
@@ -1186,10 +1312,13 @@ struct Call {
   cudaStream_t s;
 };
 
+// Every launch may start while the one before it ends (its prologue runs early; wait_for_previous()
+// holds back what depends on it).
 template <class... P, class... A>
-cudaError_t launch_cluster(void (*kernel)(P...), dim3 grid, int threads, int smem, int cluster, bool after,
-                           cudaStream_t s, A... args) {
-  cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+cudaError_t launch_cluster(void (*kernel)(P...), dim3 grid, int threads, int smem, int cluster, cudaStream_t s,
+                           A... args) {
+  cudaError_t e = cudaSuccess;
+  if (smem > 48 * 1024) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = grid;
@@ -1204,7 +1333,7 @@ cudaError_t launch_cluster(void (*kernel)(P...), dim3 grid, int threads, int sme
   at[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   at[1].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = at;
-  cfg.numAttrs = after ? 2 : 1;
+  cfg.numAttrs = 2;
   return cudaLaunchKernelEx(&cfg, kernel, args...);
 }
 
@@ -1215,19 +1344,32 @@ int cluster_split(int64_t items, int64_t blocks) {
   return ks;
 }
 
-// U (or T) of every slot: rows X (N x d) against the packed operand P.
-cudaError_t shrink(const Call& c, const void* X, int64_t ldx, int64_t d, const __nv_bfloat16* P,
-                   const int32_t* marks, int parts, void* out) {
-  CUtensorMap mx, mp;
-  if (!gp::map_kmajor(&mx, X, d, c.N, ldx) ||
-      !gp::map_3d(&mp, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, P, c.kp, d, int64_t(kParts) * c.n, c.kp, d * c.kp, 64, 64))
-    return cudaErrorInvalidValue;
+// U and / or T of every slot: rows X (N x d) against the packed operand P, `sets` of them in one launch.
+struct Shrink {
+  const void* X;
+  int64_t ldx, d;
+  const __nv_bfloat16* P;
+  void* out;
+};
+cudaError_t shrink(const Call& c, const Shrink* set, int sets, const int32_t* marks, int parts) {
+  CUtensorMap mx[2], mp[2];
   ShrinkGeo g{};
-  g.X = static_cast<const __nv_bfloat16*>(X);
-  g.ldx = ldx;
+  int64_t dmin = 0;
+  for (int i = 0; i < sets; ++i) {
+    const Shrink& v = set[i];
+    if (!gp::map_kmajor(&mx[i], v.X, v.d, c.N, v.ldx) ||
+        !gp::map_3d(&mp[i], CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, v.P, c.kp, v.d, int64_t(kParts) * c.n, c.kp, v.d * c.kp,
+                    64, 64))
+      return cudaErrorInvalidValue;
+    g.one[i].X = static_cast<const __nv_bfloat16*>(v.X);
+    g.one[i].ldx = v.ldx;
+    g.one[i].d = v.d;
+    g.one[i].P = v.P;
+    g.one[i].out = static_cast<__nv_bfloat16*>(v.out);
+    if (i == 0 || v.d < dmin) dmin = v.d;
+  }
+  g.sets = sets;
   g.N = c.N;
-  g.d = d;
-  g.P = P;
   g.marks = marks;
   g.n = c.n;
   g.kp = c.kp;
@@ -1235,7 +1377,6 @@ cudaError_t shrink(const Call& c, const void* X, int64_t ldx, int64_t d, const _
   g.stages = parts > 1 ? 5 : c.N <= kTile ? 3 : kMaxStages;
   g.plan = c.plan;
   g.p = c.p;
-  g.out = static_cast<__nv_bfloat16*>(out);
   g.status = c.status;
   g.abort_flag = c.abort_flag;
   g.limit_ns = wait_limit_ns();
@@ -1243,20 +1384,40 @@ cudaError_t shrink(const Call& c, const void* X, int64_t ldx, int64_t d, const _
   // slots are known to the device only: between one per tile and smax
   int64_t guess = c.p.tiles > c.n ? c.p.tiles : c.n;
   if (guess > c.p.smax) guess = c.p.smax;
-  const int ks = cluster_split(guess, (d + 63) / 64);
+  const int ks = cluster_split(guess * sets, (dmin + 63) / 64);
   int64_t clusters = sm_count() / ks;
-  if (clusters > c.p.smax) clusters = c.p.smax;
+  if (clusters > c.p.smax * sets) clusters = c.p.smax * sets;
+  const int second = sets - 1;
   return launch_cluster(parts == 1 ? k_adapter_shrink<1> : k_adapter_shrink<kParts>, dim3(unsigned(clusters * ks)),
-                        kShrinkThreads, shrink_smem(parts, g.stages), ks, false, c.s, mx, mp, g);
+                        kShrinkThreads, shrink_smem(parts, g.stages), ks, c.s, mx[0], mp[0], mx[second], mp[second], g);
 }
 
-// Y = X W^T + U (packed B)^T (kWmn false: W is o x d) or dX = dY W + T (packed A)^T (true: W is d x o).
+// U of every token, in partial sums (ranges x N x kp fp32 at `out`).
+cudaError_t tokens(const Call& c, const void* X, int64_t ldx, int64_t d, const __nv_bfloat16* P, const int32_t* marks,
+                   void* out) {
+  TokGeo g{};
+  g.X = static_cast<const __nv_bfloat16*>(X);
+  g.ldx = ldx;
+  g.d = d;
+  g.N = c.N;
+  g.P = P;
+  g.marks = marks;
+  g.tok_adapter = c.plan + c.p.tok_adapter;
+  g.kp = c.kp;
+  g.ranges = tok_ranges(c.N, d);
+  g.out = static_cast<float*>(out);
+  g.abort_flag = c.abort_flag;
+  return launch_cluster(k_adapter_tokens, dim3(unsigned(g.ranges), unsigned(c.N)), kTokThreads, 0, 1, c.s, g);
+}
+
+// Y = X W^T + U (packed B)^T (kWmn false: W is o x d) or dX = dY W + T (packed A)^T (true: W is d x o);
+// U as slots, or as the tokens' partial sums.
 template <bool kWmn>
 cudaError_t project(const Call& c, const void* X, int64_t ldx, int64_t d, const void* W, int64_t o,
-                    const __nv_bfloat16* P, const void* U, void* Y, int64_t ldy) {
+                    const __nv_bfloat16* P, const void* U, bool token_sums, void* Y, int64_t ldy) {
   const int64_t slots = c.p.smax;
   const int64_t tiles = ((c.N + gp::TM - 1) / gp::TM) * ((o + gp::TN - 1) / gp::TN);
-  const bool few = c.N <= kTile || 2 * tiles < sm_count() / 2;
+  const bool few = token_sums || c.N <= kTile || 2 * tiles < sm_count() / 2;
   CUtensorMap mw, mx, mb, mu;
   if (kWmn ? !gp::map_mnmajor(&mw, W, o, d, o) : !gp::map_kmajor(&mw, W, d, o, d)) return cudaErrorInvalidValue;
   if (!gp::map_3d(&mb, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, P, c.kp, o, c.n, c.kp, o * c.kp, 64, 128))
@@ -1267,24 +1428,40 @@ cudaError_t project(const Call& c, const void* X, int64_t ldx, int64_t d, const 
     g.d = d;
     g.o = o;
     g.nt = c.N >= kTile ? kTile : int((c.N + 15) / 16 * 16);
-    g.stages = 110 * 1024 / (kWBytes + g.nt * 128);
     g.ksteps = (c.k + 15) / 16;
+    g.tokens = token_sums ? 1 : 0;
+    g.kp = c.kp;
+    g.ranges = tok_ranges(c.N, d);
+    g.U = static_cast<const float*>(U);
+    g.B = P;
     g.plan = c.plan;
     g.tile_base = c.p.tile_base;
     g.adapter = c.p.adapter;
+    g.tok_adapter = c.p.tok_adapter;
     g.Y = static_cast<__nv_bfloat16*>(Y);
     g.ldy = ldy;
     g.status = c.status;
     g.abort_flag = c.abort_flag;
     g.limit_ns = wait_limit_ns();
     g.mark = c.mark;
-    if (!gp::map_2d(&mx, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, X, d, c.N, ldx, 64, g.nt) ||
+    if (!gp::map_2d(&mx, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, X, d, c.N, ldx, 64, g.nt)) return cudaErrorInvalidValue;
+    mu = mx;
+    if (!token_sums &&
         !gp::map_2d(&mu, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, U, kMaxK, slots * kSlotRows, kMaxK, 64, g.nt))
       return cudaErrorInvalidValue;
     const int64_t ot = (o + 127) / 128, nt = (c.N + g.nt - 1) / g.nt;
-    const int ks = cluster_split(ot * nt, (d + 63) / 64);
+    int ks = int(sm_count() / (ot * nt));
+    const int64_t most = (d + 127) / 128;  // two k-blocks for each CTA
+    if (ks > most) ks = int(most);
+    if (ks > 8) ks = 8;
+    if (ks < 1) ks = 1;
+    // slots of one tile: a ring that fits beside a CTA of k_adapter_shrink with its small one
+    const int low = token_sums ? few_low(g.nt, ks, c.kp) : 0;
+    const int room = (token_sums || c.N > kTile ? 200 : 110) * 1024 - low;
+    g.stages = room / (kWBytes + g.nt * 128);  // at least 3: low is at most 98 KB
+    if (g.stages > 12) g.stages = 12;
     return launch_cluster(k_adapter_few<kWmn>, dim3(unsigned(ot * ks), unsigned(nt)), kFewThreads,
-                          few_smem(g.nt, g.stages), ks, true, c.s, mw, mx, mb, mu, g);
+                          few_smem(g.nt, g.stages, low), ks, c.s, mw, mx, mb, mu, g);
   }
   CUtensorMap mo;
   if (!gp::map_kmajor(&mx, X, d, c.N, ldx) || !gp::map_out_bf16(&mo, Y, o, c.N, ldy) ||
@@ -1306,42 +1483,58 @@ cudaError_t project(const Call& c, const void* X, int64_t ldx, int64_t d, const 
   return gp::launch<false, kWmn>(mx, mw, mu, mb, mo, g, EpiRows{}, ext, c.s);
 }
 
-cudaError_t grad(const Call& c, const void* S, int64_t lds, int64_t d, const void* U, int ranges, float* part,
-                 const float* scale, void* out, int dtype) {
-  CUtensorMap ms, mu;
-  if (!gp::map_mnmajor(&ms, S, d, c.N, lds) ||
-      !gp::map_3d(&mu, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, U, kMaxK, c.p.smax * kSlotRows, kParts, kMaxK,
-                  c.p.smax * int64_t(kSlotElems), 64, 64))
-    return cudaErrorInvalidValue;
+// dA from X and T, and / or dB from dY and U.
+struct Grad {
+  const void* S;
+  int64_t lds, d;
+  const void* U;
+  int ranges;
+  float* part;
+  const float* scale;
+  void* out;
+};
+cudaError_t grad(const Call& c, const Grad* set, int sets, int dtype) {
+  CUtensorMap ms[2], mu[2];
   GradGeo g{};
+  JoinOne j[2] = {};
+  int64_t values = 0;
+  for (int i = 0; i < sets; ++i) {
+    const Grad& v = set[i];
+    if (!gp::map_mnmajor(&ms[i], v.S, v.d, c.N, v.lds) ||
+        !gp::map_3d(&mu[i], CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, v.U, kMaxK, c.p.smax * kSlotRows, kParts, kMaxK,
+                    c.p.smax * int64_t(kSlotElems), 64, 64))
+      return cudaErrorInvalidValue;
+    g.one[i].d = v.d;
+    g.one[i].ctiles = int((v.d + 127) / 128);
+    g.one[i].ranges = v.ranges;
+    g.one[i].items = c.n * g.one[i].ctiles * v.ranges;
+    g.one[i].part = v.part;
+    g.items += g.one[i].items;
+    j[i].part = v.part;
+    j[i].scale = v.scale;
+    j[i].out = v.out;
+    j[i].rows = int64_t(c.n) * v.d;
+    j[i].d = v.d;
+    j[i].ranges = v.ranges;
+    values += j[i].rows * c.k;
+  }
   g.N = c.N;
-  g.d = d;
   g.n = c.n;
   g.kp = c.kp;
-  g.ctiles = int((d + 127) / 128);
-  g.ranges = ranges;
   g.plan = c.plan;
   g.p = c.p;
-  g.part = part;
   g.status = c.status;
   g.abort_flag = c.abort_flag;
   g.limit_ns = wait_limit_ns();
   g.mark = c.mark;
-  cudaError_t e = cudaFuncSetAttribute(k_adapter_grad, cudaFuncAttributeMaxDynamicSharedMemorySize, kGradSmem);
+  const int second = sets - 1;
+  const unsigned blocks = unsigned(g.items < sm_count() ? g.items : sm_count());
+  const cudaError_t e = launch_cluster(k_adapter_grad, dim3(blocks), kGradThreads, kGradSmem, 1, c.s, ms[0], mu[0],
+                                       ms[second], mu[second], g);
   if (e != cudaSuccess) return e;
-  const int64_t items = int64_t(c.n) * g.ctiles * ranges;
-  const int blocks = int(items < sm_count() ? items : sm_count());
-  k_adapter_grad<<<blocks, kGradThreads, kGradSmem, c.s>>>(ms, mu, g);
-  e = cudaGetLastError();
-  if (e != cudaSuccess) return e;
-  const int64_t values = int64_t(c.n) * d * c.k;
-  const unsigned jb = unsigned(values / 256 + 1 < 4 * sm_count() ? values / 256 + 1 : 4 * sm_count());
-  if (dtype == LOCA_F32)
-    k_adapter_join<float><<<jb, 256, 0, c.s>>>(part, ranges, c.n, d, c.k, c.kp, scale, static_cast<float*>(out));
-  else
-    k_adapter_join<__nv_bfloat16><<<jb, 256, 0, c.s>>>(part, ranges, c.n, d, c.k, c.kp, scale,
-                                                       static_cast<__nv_bfloat16*>(out));
-  return cudaGetLastError();
+  const unsigned jb = unsigned(values / 256 + 1 < 8 * sm_count() ? values / 256 + 1 : 8 * sm_count());
+  return launch_cluster(dtype == LOCA_F32 ? k_adapter_join<float> : k_adapter_join<__nv_bfloat16>, dim3(jb), 256, 0, 1,
+                        c.s, j[0], j[1], c.k, c.kp);
 }
 
 Call call_of(int64_t N, int n, int k, const void* plan, void* workspace, int32_t* status, cudaStream_t s) {
@@ -1413,10 +1606,14 @@ cudaError_t launch_adapter_apply(const void* X, int64_t ldx, int64_t N, int64_t 
   const PackLay pk = pack_lay(n, d_in, d_out, k);
   const uint8_t* pb = static_cast<const uint8_t*>(packed);
   uint8_t* ws = static_cast<uint8_t*>(workspace);
-  cudaError_t e = shrink(c, X, ldx, d_in, reinterpret_cast<const __nv_bfloat16*>(pb + pk.a),
-             reinterpret_cast<const int32_t*>(pb + pk.marks), 1, ws + w.u);
+  const __nv_bfloat16* pa = reinterpret_cast<const __nv_bfloat16*>(pb + pk.a);
+  const int32_t* marks = reinterpret_cast<const int32_t*>(pb + pk.marks);
+  const bool tok = by_token(N, n);
+  const Shrink u{X, ldx, d_in, pa, ws + w.u};
+  const cudaError_t e = tok ? tokens(c, X, ldx, d_in, pa, marks, ws + w.u) : shrink(c, &u, 1, marks, 1);
   if (e != cudaSuccess) return e;
-  return project<false>(c, X, ldx, d_in, W, d_out, reinterpret_cast<const __nv_bfloat16*>(pb + pk.b), ws + w.u, Y, ldy);
+  return project<false>(c, X, ldx, d_in, W, d_out, reinterpret_cast<const __nv_bfloat16*>(pb + pk.b), ws + w.u, tok, Y,
+                        ldy);
 }
 
 cudaError_t launch_adapter_backward(const void* X, int64_t ldx, const void* dY, int64_t lddy, int64_t N, int64_t d_in,
@@ -1431,25 +1628,25 @@ cudaError_t launch_adapter_backward(const void* X, int64_t ldx, const void* dY, 
   const int32_t* marks = reinterpret_cast<const int32_t*>(pb + pk.marks);
   const __nv_bfloat16* pB = reinterpret_cast<const __nv_bfloat16*>(pb + pk.b);
   uint8_t* ws = static_cast<uint8_t*>(workspace);
-  float* part = reinterpret_cast<float*>(ws + w.part);
-  cudaError_t e = cudaSuccess;
-  if (dB) {
-    e = shrink(c, X, ldx, d_in, pa, marks, kParts, ws + w.u);
-    if (e != cudaSuccess) return e;
-    e = grad(c, dY, lddy, d_out, ws + w.u, w.ranges_out, part, reinterpret_cast<const float*>(pb + pk.scale), dB,
-             grad_dtype);
-    if (e != cudaSuccess) return e;
-  }
-  if (dA || dX) {
-    e = shrink(c, dY, lddy, d_out, pB, marks, dA ? kParts : 1, ws + w.t);
-    if (e != cudaSuccess) return e;
-  }
+  const Shrink u{X, ldx, d_in, pa, ws + w.u}, t{dY, lddy, d_out, pB, ws + w.t};
+  Shrink set[2] = {t, t};
+  int sets = 0;
+  if (dA || dX) set[sets++] = t;
+  if (dB) set[sets++] = u;
+  cudaError_t e = shrink(c, set, sets, marks, dA || dB ? kParts : 1);
+  if (e != cudaSuccess) return e;
   if (dX) {
-    e = project<true>(c, dY, lddy, d_out, W, d_in, pa, ws + w.t, dX, lddx);
+    e = project<true>(c, dY, lddy, d_out, W, d_in, pa, ws + w.t, false, dX, lddx);
     if (e != cudaSuccess) return e;
   }
-  if (dA) e = grad(c, X, ldx, d_in, ws + w.t, w.ranges_in, part, nullptr, dA, grad_dtype);
-  return e;
+  const Grad ga{X, ldx, d_in, ws + w.t, w.ranges_in, reinterpret_cast<float*>(ws + w.part_in), nullptr, dA};
+  const Grad gb{dY, lddy, d_out, ws + w.u, w.ranges_out, reinterpret_cast<float*>(ws + w.part_out),
+                reinterpret_cast<const float*>(pb + pk.scale), dB};
+  Grad grads[2] = {ga, ga};
+  int ng = 0;
+  if (dA) grads[ng++] = ga;
+  if (dB) grads[ng++] = gb;
+  return ng ? grad(c, grads, ng, grad_dtype) : cudaSuccess;
 }
 
 }  // namespace loca

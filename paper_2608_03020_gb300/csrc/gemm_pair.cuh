@@ -217,6 +217,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
   cluster_sync();
   fence_after();
   const uint32_t tmem_base = *tmem_slot;
+  wait_for_previous();  // the launch before has completed (the prologue above ran beside its end)
+  launch_dependents();
   const Live lv = live_of(g);
   uint32_t iters_done = 0;
 
@@ -465,6 +467,23 @@ inline int resident_pairs(K kernel) {
   return clusters;
 }
 
+// A launch whose prologue may run beside the end of the launch before it; the kernel calls
+// wait_for_previous() before it touches what that launch reads or writes.
+template <class... P, class... A>
+inline cudaError_t launch_early(void (*kernel)(P...), dim3 grid, dim3 block, size_t smem, cudaStream_t s, A... args) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = grid;
+  cfg.blockDim = block;
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = s;
+  cudaLaunchAttribute at[1];
+  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = at;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, kernel, args...);
+}
+
 template <bool kAmn, bool kBmn, class Epi, class Ext>
 inline cudaError_t launch(const CUtensorMap& a, const CUtensorMap& b, const CUtensorMap& ax, const CUtensorMap& bx,
                           const CUtensorMap& o, const Geo& g, const Epi& epi, const Ext& ext, cudaStream_t s) {
@@ -475,8 +494,7 @@ inline cudaError_t launch(const CUtensorMap& a, const CUtensorMap& b, const CUte
   const int64_t total = int64_t(g.m_tiles) * g.n_tiles * g.splits;
   if (total < 1) return cudaSuccess;
   const int n = total < pairs ? int(total) : pairs;
-  kernel<<<2 * n, THREADS, SMEM, s>>>(a, b, ax, bx, o, g, epi, ext);
-  return cudaGetLastError();
+  return launch_early(kernel, dim3(unsigned(2 * n)), dim3(THREADS), SMEM, s, a, b, ax, bx, o, g, epi, ext);
 }
 
 }  // namespace gp

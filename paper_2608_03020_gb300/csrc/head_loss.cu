@@ -33,7 +33,7 @@ using namespace tc;
 
 constexpr float kLog2e = 1.4426950408889634f;
 
-constexpr int kRowsPerBlock = 32;
+constexpr int kRowsPerBlock = 8;          // one per warp
 constexpr int kPadBlocks = 16;         // blocks of k_head_rows that write the zero rows
 constexpr int64_t kFwdRows = 16384;    // rows per forward piece (bounds the partial maxima and sums)
 constexpr int64_t kBwdRows = 8192;     // rows per backward piece when dW is not wanted
@@ -85,9 +85,11 @@ __global__ void __launch_bounds__(256)
                 const float* __restrict__ lse, Rows out, int64_t npad, int nb, float* loss0, float* lse0, float* E0,
                 int C, __nv_bfloat16* dH0, int64_t lddh) {
   __shared__ int scratch[8];
-  __shared__ int place[kRowsPerBlock];
+  __shared__ int place[32];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int64_t dv = d / 8;  // 16-byte vectors of a row
+  wait_for_previous();
+  launch_dependents();
   if (blockIdx.x == 0 && threadIdx.x == 0) *out.abort_flag = 0;
   if (int(blockIdx.x) >= nb) {
     const int64_t total = count_live(y, N, V, scratch);
@@ -111,7 +113,7 @@ __global__ void __launch_bounds__(256)
   const int base = count_live(y, r0, V, scratch);
   if (warp == 0) {
     const int64_t n = r0 + lane;
-    const int32_t yn = n < N ? y[n] : -1;
+    const int32_t yn = lane < kRowsPerBlock && n < N ? y[n] : -1;
     const bool live = live_label(yn, V);
     const unsigned all = __ballot_sync(0xffffffffu, live);
     const int p = live ? base + __popc(all & ((1u << lane) - 1u)) : -1;
@@ -131,7 +133,8 @@ __global__ void __launch_bounds__(256)
     if (p >= 0) {
       const uint4* src = reinterpret_cast<const uint4*>(H + n * ldh);
       uint4* dst = reinterpret_cast<uint4*>(out.H + int64_t(p) * d);
-      for (int64_t j = lane; j < dv; j += 32) dst[j] = src[j];
+#pragma unroll 8
+      for (int64_t j = lane; j < dv; j += 32) dst[j] = __ldg(src + j);
     } else {
       if (lane == 0 && loss0) loss0[n] = 0.f;
       if (lane == 0 && lse0) lse0[n] = 0.f;
@@ -291,16 +294,27 @@ __global__ void __launch_bounds__(1024)
                 const float* __restrict__ zy, const float* __restrict__ zc, const int32_t* __restrict__ cols, int C,
                 float* __restrict__ loss, float* __restrict__ lse, float* __restrict__ E) {
   __shared__ float2 sh[32][33];
+  wait_for_previous();
+  launch_dependents();
   const int64_t row = int64_t(blockIdx.x) * 32 + threadIdx.x;
   const bool live = row_first + row < *in.count;
   float m = -INFINITY, s = 0.f;
   if (live) {
-    for (int p = threadIdx.y; p < nparts; p += blockDim.y) {
-      const float2 q = part[int64_t(p) * pitch + row];
-      const float mm = fmaxf(m, q.x);
-      if (mm != -INFINITY) s = s * exp_diff(m, mm) + q.y * exp_diff(q.x, mm);
-      else s += q.y;  // keeps a NaN
-      m = mm;
+    constexpr int kAhead = 8;
+    for (int p0 = threadIdx.y; p0 < nparts; p0 += kAhead * int(blockDim.y)) {
+      float2 q[kAhead];
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i) {
+        const int p = p0 + i * int(blockDim.y);
+        q[i] = p < nparts ? part[int64_t(p) * pitch + row] : make_float2(-INFINITY, 0.f);
+      }
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i) {
+        const float mm = fmaxf(m, q[i].x);
+        if (mm != -INFINITY) s = s * exp_diff(m, mm) + q[i].y * exp_diff(q[i].x, mm);
+        else s += q[i].y;  // keeps a NaN
+        m = mm;
+      }
     }
   }
   sh[threadIdx.y][threadIdx.x] = make_float2(m, s);
@@ -331,6 +345,8 @@ __global__ void __launch_bounds__(256)
               float scale, __nv_bfloat16* __restrict__ dH, int64_t lddh) {
   const int64_t dv = d / 8;
   const int64_t row = int64_t(blockIdx.x);
+  wait_for_previous();
+  launch_dependents();
   if (row_first + row >= *in.count) return;
   const int64_t n = in.idx[row_first + row];
   for (int64_t j = threadIdx.x; j < dv; j += blockDim.x) {
@@ -465,10 +481,10 @@ cudaError_t launch_rows(const void* H, int64_t ldh, int64_t N, int64_t d, int64_
                         const float* dloss, const float* lse, const Rows& r, float* loss0, float* lse0, float* E0, int C,
                         void* dH0, int64_t lddh, cudaStream_t s) {
   const int64_t nb = (N + kRowsPerBlock - 1) / kRowsPerBlock;
-  k_head_rows<<<unsigned(nb + kPadBlocks), 256, 0, s>>>(
-      static_cast<const __nv_bfloat16*>(H), ldh, N, d, V, y, w, dloss, lse, r, round_up(N < 1 ? 1 : N, gp::TM), int(nb),
-      loss0, lse0, E0, C, static_cast<__nv_bfloat16*>(dH0), lddh);
-  return cudaGetLastError();
+  return gp::launch_early(k_head_rows, dim3(unsigned(nb + kPadBlocks)), dim3(256), 0, s,
+                          static_cast<const __nv_bfloat16*>(H), ldh, N, d, V, y, w, dloss, lse, r,
+                          round_up(N < 1 ? 1 : N, gp::TM), int(nb), loss0, lse0, E0, C,
+                          static_cast<__nv_bfloat16*>(dH0), lddh);
 }
 
 }  // namespace
@@ -503,9 +519,8 @@ cudaError_t launch_head_loss(const void* H, int64_t ldh, int64_t N, int64_t d, c
     EpiStats epi{part, lay.piece, r.y + p0, zy, cols, E ? C : 0, zc, V};
     e = gp::launch<false, false>(ma, mb, ma, mb, ma, g, epi, gp::NoExt{}, s);
     if (e != cudaSuccess) return e;
-    k_head_join<<<unsigned(rows / 32), dim3(32, 2 * vt >= 128 ? 32 : 8), 0, s>>>(part, lay.piece, int(2 * vt), r, p0, zy,
-                                                                               zc, cols, C, loss, lse, E);
-    e = cudaGetLastError();
+    e = gp::launch_early(k_head_join, dim3(unsigned(rows / 32)), dim3(32, 2 * vt >= 128 ? 32 : 8), 0, s, part, lay.piece,
+                         int(2 * vt), r, p0, zy, zc, cols, C, loss, lse, E);
     if (e != cudaSuccess) return e;
   }
   return cudaSuccess;
@@ -566,9 +581,8 @@ cudaError_t launch_head_loss_backward(const void* H, int64_t ldh, int64_t N, int
       }
     }
     if (dH) {
-      k_head_dh<<<unsigned(rows), 256, 0, s>>>(part, lay.piece, lay.splits, d, r, p0, scale,
-                                              static_cast<__nv_bfloat16*>(dH), lddh);
-      e = cudaGetLastError();
+      e = gp::launch_early(k_head_dh, dim3(unsigned(rows)), dim3(256), 0, s, part, lay.piece, lay.splits, d, r, p0, scale,
+                           static_cast<__nv_bfloat16*>(dH), lddh);
       if (e != cudaSuccess) return e;
     }
   }
