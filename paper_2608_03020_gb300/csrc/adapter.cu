@@ -833,8 +833,14 @@ __global__ void __launch_bounds__(kFewThreads, 1)
     if (g.tokens) {
       // this CTA's tokens n0 + rank + ks t: U's partial sums in order, then a row of s B per thread
       for (int t = i; t < own; t += 128) ad[t] = rank + ks * t < ntok ? g.plan[g.tok_adapter + n0 + rank + ks * t] : -1;
-      wait_for_previous();
       epi_bar();
+      if (o0 + i < g.o)
+        for (int t = 0; t < own; ++t)
+          if (ad[t] >= 0) {
+            const __nv_bfloat16* p = g.B + (int64_t(ad[t]) * g.o + o0 + i) * g.kp;
+            for (int c = 0; c < g.kp; c += 16) asm volatile("prefetch.global.L2 [%0];" ::"l"(p + c));
+          }
+      wait_for_previous();
       for (int e = i; e < own * g.kp; e += 128) {
         const int t = e / g.kp, c = e - t * g.kp;
         float u = 0.f;
@@ -1319,6 +1325,7 @@ cudaError_t launch_cluster(void (*kernel)(P...), dim3 grid, int threads, int sme
                            A... args) {
   cudaError_t e = cudaSuccess;
   if (smem > 48 * 1024) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  else e = gp::keep_carveout(kernel);
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = grid;

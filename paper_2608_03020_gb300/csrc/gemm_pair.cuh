@@ -467,6 +467,13 @@ inline int resident_pairs(K kernel) {
   return clusters;
 }
 
+// Small kernels between those with 200 KB of shared memory ask for the same split of L1: changing it
+// drains the SM (64 single tokens through an adapted projection: 27.1 us with the change, 23.4 without).
+template <class K>
+inline cudaError_t keep_carveout(K kernel) {
+  return cudaFuncSetAttribute(kernel, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared);
+}
+
 // A launch whose prologue may run beside the end of the launch before it; the kernel calls
 // wait_for_previous() before it touches what that launch reads or writes.
 template <class... P, class... A>
@@ -481,6 +488,10 @@ inline cudaError_t launch_early(void (*kernel)(P...), dim3 grid, dim3 block, siz
   at[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = at;
   cfg.numAttrs = 1;
+  if (smem == 0) {
+    const cudaError_t e = keep_carveout(kernel);
+    if (e != cudaSuccess) return e;
+  }
   return cudaLaunchKernelEx(&cfg, kernel, args...);
 }
 

@@ -10,6 +10,7 @@ streams.  There is no CPU fallback: importing works without a GPU, calling needs
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 
 import torch
@@ -158,8 +159,14 @@ def _ptr(t):
     return None if t is None else ctypes.c_void_p(t.data_ptr())
 
 
+# handle of the current stream without building a Stream object (3 us of a call that takes 6)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
 def _stream(stream):
     if stream is None:
+        if _raw_stream is not None:
+            return ctypes.c_void_p(_raw_stream(torch.cuda.current_device()))
         stream = torch.cuda.current_stream()
     return ctypes.c_void_p(stream.cuda_stream)
 
@@ -655,16 +662,19 @@ def _rows2d(t, name, dtype, shape=None):
         raise TypeError(f"{name} must be a CUDA tensor")
     if t.dtype != dtype:
         raise TypeError(f"{name} has dtype {t.dtype}, expected {dtype}")
-    if t.dim() != 2 or (shape is not None and tuple(t.shape) != tuple(shape)):
-        raise ValueError(f"{name} must have shape {tuple(shape) if shape else '2-D'}, got {tuple(t.shape)}")
-    if t.shape[1] > 1 and t.stride(1) != 1:
+    size, stride = t.shape, t.stride()
+    if len(size) != 2 or (shape is not None and size != shape):
+        raise ValueError(f"{name} must have shape {tuple(shape) if shape else '2-D'}, got {tuple(size)}")
+    rows, cols = size
+    if cols > 1 and stride[1] != 1:
         raise ValueError(f"{name} must have unit column stride")
-    pitch = t.stride(0) if t.shape[0] > 1 else t.shape[1]
-    if pitch < t.shape[1]:
+    pitch = stride[0] if rows > 1 else cols
+    if pitch < cols:
         raise ValueError(f"{name} must have a row pitch of at least its columns")
     return pitch
 
 
+@functools.lru_cache(maxsize=1024)  # a size depends on the arguments alone
 def head_loss_workspace_size(N, V, d, C=0) -> int:
     out = ctypes.c_size_t(0)
     _check(lib().loca_head_loss_workspace_size(N, V, d, C, ctypes.byref(out)), "loca_head_loss_workspace_size")
@@ -699,6 +709,7 @@ def loca_head_loss(H, W, y, loss, lse=None, w=None, label_cols=None, E=None, wor
     _check(rc, "loca_head_loss")
 
 
+@functools.lru_cache(maxsize=1024)  # a size depends on the arguments alone
 def head_loss_backward_workspace_size(N, V, d, want_dH=True, want_dW=True) -> int:
     out = ctypes.c_size_t(0)
     _check(lib().loca_head_loss_backward_workspace_size(N, V, d, int(bool(want_dH)), int(bool(want_dW)),
@@ -777,6 +788,7 @@ class AdapterPlan:
         return self
 
 
+@functools.lru_cache(maxsize=1024)  # a size depends on the arguments alone
 def adapter_workspace_size(N, d_in, d_out, k, n, backward=False) -> int:
     out = ctypes.c_size_t(0)
     _check(lib().loca_adapter_workspace_size(N, d_in, d_out, k, n, int(bool(backward)), ctypes.byref(out)),
