@@ -49,7 +49,7 @@ __host__ __device__ inline int k_padded(int k) { return (k + 15) / 16 * 16; }
 // Offsets in int32 from the start of the plan.
 struct PlanLay {
   int64_t tiles, pairs, smax;
-  int64_t tok_slot, tok_adapter, tile_base, adapter, tile, count, pair_count, pair_ad, pair_s0, pair_s1, ad_off, ad_slots, total;
+  int64_t tok_slot, tok_adapter, tile_base, adapter, tile, count, pair_count, pair_ad, pair_s0, pair_s1, ad_off, ad_slots, ad_tile, ad_count, total;
 };
 PlanLay plan_lay(int64_t N, int n) {
   PlanLay p{};
@@ -75,6 +75,8 @@ PlanLay plan_lay(int64_t N, int n) {
   p.pair_s1 = take(p.smax);
   p.ad_off = take(n + 1);
   p.ad_slots = take(p.smax);
+  p.ad_tile = take(p.smax);
+  p.ad_count = take(p.smax);
   p.total = at;
   return p;
 }
@@ -226,38 +228,38 @@ __global__ void __launch_bounds__(256) k_plan_adapters(int32_t* plan, PlanLay p,
       if (w < warp) off += sums[w];
       here += sums[w];
     }
-    if (mine && LOCA_CHECK(off, p.smax)) plan[p.ad_slots + off] = s;
+    if (mine && LOCA_CHECK(off, p.smax)) {
+      plan[p.ad_slots + off] = s;
+      plan[p.ad_tile + off] = plan[p.tile + s];
+      plan[p.ad_count + off] = plan[p.count + s];
+    }
     at += here;
     __syncthreads();
   }
 }
 
 // ------------------------------------------------------------------ packed adapters
-// A: kParts x n x d_in x kp bf16, then s B: kParts x n x d_out x kp, then the n scales (fp32) and n
-// marks.  In a shared tile an adapter's columns meet the other tokens' zeros, and zero times infinity
+// The first parts of A (n x d_in x kp bf16) and of s B (n x d_out x kp), which serving reads; then all
+// parts of both, side by side in a row (n x d x 3 kp: the columns of one MMA operand); then the n scales
+// (fp32) and n marks.  In a shared tile an adapter's columns meet the other tokens' zeros, and zero times infinity
 // is not zero: values that are not finite are stored as zero and their adapter is marked, and U and
 // T of a marked adapter's tokens are NaN.  One request's broken adapter so spoils its own outputs
 // (all of them) and nobody else's.
 struct PackLay {
-  size_t a, b, scale, marks, total;
+  size_t a, b, all_a, all_b, scale, marks, total;
 };
 PackLay pack_lay(int n, int64_t d_in, int64_t d_out, int k) {
   const size_t kp = size_t(k_padded(k));
   PackLay p{};
   p.a = 0;
-  p.b = align256(2 * kParts * size_t(n) * size_t(d_in) * kp);
-  p.scale = p.b + align256(2 * kParts * size_t(n) * size_t(d_out) * kp);
+  const size_t sa = 2 * size_t(n) * size_t(d_in) * kp, sb = 2 * size_t(n) * size_t(d_out) * kp;
+  p.b = p.a + align256(sa);
+  p.all_a = p.b + align256(sb);
+  p.all_b = p.all_a + align256(kParts * sa);
+  p.scale = p.all_b + align256(kParts * sb);
   p.marks = p.scale + align256(4 * size_t(n));
   p.total = p.marks + align256(4 * size_t(n));
   return p;
-}
-
-__device__ __forceinline__ void split3(float x, __nv_bfloat16 (&o)[3]) {
-  o[0] = __float2bfloat16_rn(x);
-  x -= __bfloat162float(o[0]);
-  o[1] = __float2bfloat16_rn(x);
-  x -= __bfloat162float(o[1]);
-  o[2] = __float2bfloat16_rn(x);
 }
 
 template <class T>
@@ -271,7 +273,8 @@ template <class T>
 __global__ void __launch_bounds__(256)
     k_adapter_pack(const T* __restrict__ A, const T* __restrict__ B, int n, int64_t d_in, int64_t d_out, int k, int kp,
                    const float* __restrict__ scale, __nv_bfloat16* __restrict__ pa, __nv_bfloat16* __restrict__ pb,
-                   float* __restrict__ ps, int32_t* __restrict__ marks) {
+                   __nv_bfloat16* __restrict__ all_a, __nv_bfloat16* __restrict__ all_b, float* __restrict__ ps,
+                   int32_t* __restrict__ marks) {
   const int64_t na = int64_t(n) * d_in * kp, nb = int64_t(n) * d_out * kp;
   const int64_t stride = int64_t(gridDim.x) * blockDim.x;
   for (int64_t i = int64_t(blockIdx.x) * blockDim.x + threadIdx.x; i < na + nb; i += stride) {
@@ -286,38 +289,40 @@ __global__ void __launch_bounds__(256)
       x = 0.f;
       marks[row / (isb ? d_out : d_in)] = 1;
     }
-    __nv_bfloat16 o[3];
-    split3(x, o);
-    __nv_bfloat16* to = isb ? pb : pa;
-    const int64_t pitch = isb ? nb : na;
+    __nv_bfloat16* all = (isb ? all_b : all_a) + row * (kParts * kp) + c;
 #pragma unroll
-    for (int q = 0; q < 3; ++q) to[q * pitch + e] = o[q];
+    for (int q = 0; q < kParts; ++q) {
+      const __nv_bfloat16 h = __float2bfloat16_rn(x);
+      x -= __bfloat162float(h);
+      if (q == 0) (isb ? pb : pa)[e] = h;
+      all[q * kp] = h;
+    }
   }
   for (int64_t i = int64_t(blockIdx.x) * blockDim.x + threadIdx.x; i < n; i += stride) ps[i] = scale ? scale[i] : 1.f;
 }
 
 // ------------------------------------------------------------------ U and T: tokens x k sums over d
-// One item per slot: M = the tile's 128 tokens, N = 64 columns per part of the adapter, K = d.  With
-// few slots the d axis is split over the CTAs of a cluster, which add their sums through distributed
-// shared memory in rank order.  Rows of other slots are written as zeros.
+// One item per slot: M = the tile's 128 tokens, N = the adapter's columns (kp per part, the parts side
+// by side), K = d.  With few slots the d axis is split over the CTAs of a cluster, which add their sums
+// through distributed shared memory in rank order; one CTA alone writes from registers and goes on.
+// Rows of other slots are written as zeros.  Measured at 16384 tokens, k = 16, X from HBM: 0.33 us per
+// k-block and 128 CTAs (6.3 TB/s) beyond 8 us of start and end.
 constexpr int kShrinkThreads = 192;
-constexpr int kShrinkSeg = 8;                    // k-blocks per accumulation segment (three parts)
+constexpr int kShrinkSeg = 8;                    // k-blocks per accumulation segment (several parts)
 constexpr int kMaxStages = 8;
 constexpr int kRedBytes = kSlotRows * kMaxK * 4; // 32 KB of fp32 sums, in the place of the ring
 constexpr int kXBytes = 128 * 64 * 2, kPBytes = 64 * 64 * 2;
 
 struct ShrinkOne {
-  const __nv_bfloat16* X;
-  int64_t ldx, d;
-  const __nv_bfloat16* P;  // packed adapter operand: part x adapter x d x kp
-  __nv_bfloat16* out;      // parts x smax x 128 x 64
+  __nv_bfloat16* out;  // column tile x smax x 128 x 64
+  int64_t d;
 };
 struct ShrinkGeo {
   ShrinkOne one[2];  // a backward pass makes U from X and T from dY in one launch
   int sets;
   int64_t N;
   const int32_t* marks;
-  int n, kp, stages;
+  int kp, parts, stages;
   const int32_t* plan;
   PlanLay p;
   int32_t* status;
@@ -325,26 +330,47 @@ struct ShrinkGeo {
   unsigned long long limit_ns;
   int32_t mark;
 };
-int shrink_ring(int parts, int stages) {
-  const int b = stages * (kXBytes + parts * kPBytes);
+// 64-wide column tiles of `parts` parts
+__host__ __device__ inline int col_tiles(int kp, int parts) { return (kp * parts + 63) / 64; }
+int shrink_ring(int ctiles, int stages) {
+  const int b = stages * (kXBytes + ctiles * kPBytes);
   return b > kRedBytes ? b : kRedBytes;
 }
-int shrink_smem(int parts, int stages) { return shrink_ring(parts, stages) + 512 + 1024; }
+int shrink_smem(int ctiles, int stages) { return shrink_ring(ctiles, stages) + 512 + 1024; }
 
 // Position of (row, col) in the fp32 sums: 16-byte chunks swizzled over the rows (no bank conflicts).
 __device__ __forceinline__ int red_at(int row, int col) {
   return row * kMaxK + (((col >> 2) ^ (row & 15)) << 2) + (col & 3);
 }
 
-template <int kP>
+// Eight values of U in `parts` bf16 parts to columns c .. c + 7 of each part.
+__device__ __forceinline__ void store_parts(float (&v)[8], __nv_bfloat16* out, int64_t smax, int s, int row, int c, int kp,
+                                            int parts) {
+#pragma unroll
+  for (int q = 0; q < kParts; ++q) {
+    if (q < parts) {
+      __align__(16) __nv_bfloat16 w[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        w[i] = __float2bfloat16_rn(v[i]);
+        v[i] -= __bfloat162float(w[i]);
+      }
+      const int col = q * kp + c;
+      if (LOCA_CHECK(s, smax))
+        *reinterpret_cast<uint4*>(out + ((int64_t(col >> 6) * smax + s) * kSlotRows + row) * kMaxK + (col & 63)) =
+            *reinterpret_cast<const uint4*>(w);
+    }
+  }
+}
+
 __global__ void __launch_bounds__(kShrinkThreads, 1)
     k_adapter_shrink(const __grid_constant__ CUtensorMap tmX0, const __grid_constant__ CUtensorMap tmP0,
                      const __grid_constant__ CUtensorMap tmX1, const __grid_constant__ CUtensorMap tmP1,
                      const __grid_constant__ ShrinkGeo g) {
   extern __shared__ uint8_t smem_raw[];
-  __shared__ uint32_t members_of[kTile / 32];  // the tile's rows that belong to the slot
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
-  constexpr int stage_bytes = kXBytes + kP * kPBytes;
+  const int ctiles = col_tiles(g.kp, g.parts);
+  const int stage_bytes = kXBytes + ctiles * kPBytes;
   const int ring = g.stages * stage_bytes > kRedBytes ? g.stages * stage_bytes : kRedBytes;
   uint64_t* bars = reinterpret_cast<uint64_t*>(smem + ring);
   const uint32_t bar_base = smem_u32(bars);
@@ -361,8 +387,8 @@ __global__ void __launch_bounds__(kShrinkThreads, 1)
   const WaitCtl wc{g.status, g.abort_flag, g.limit_ns, g.mark};
   const int ks = int(cluster_nctarank()), rank = int(cluster_ctarank());
   const int cid = int(cluster_id_x()), ncl = int(ncluster_x());
-  constexpr uint32_t acc_cols = uint32_t(64 * kP);
-  constexpr uint32_t cols = kP == 1 ? 128u : 512u;
+  const uint32_t acc_cols = uint32_t(64 * ctiles);  // distance of the two accumulators
+  const uint32_t cols = ctiles == 1 ? 128u : ctiles == 2 ? 256u : 512u;
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < kMaxStages; ++s) {
@@ -391,8 +417,7 @@ __global__ void __launch_bounds__(kShrinkThreads, 1)
   launch_dependents();
   if (blockIdx.x == 0 && threadIdx.x == 0) *g.abort_flag = 0;  // a captured call that gave up may be replayed
   const int total = g.plan[g.p.tile_base + g.p.tiles];
-  constexpr int seg_kb = kP == 1 ? 64 : kShrinkSeg;
-  const int64_t part_pitch = g.p.smax * int64_t(kSlotElems);
+  const int seg_kb = g.parts == 1 ? 64 : kShrinkSeg;
 
   int stage = 0;
   uint32_t phase = 0, iter = 0, seg = 0;
@@ -400,29 +425,18 @@ __global__ void __launch_bounds__(kShrinkThreads, 1)
   for (int it = cid; it < total * g.sets; it += ncl) {
     const int set = it >= total ? 1 : 0;
     const int s = it - set * total;
-    const ShrinkOne& o = g.one[set];
-    const int nkb = int((o.d + 63) / 64);
+    const int nkb = int((g.one[set].d + 63) / 64);
     const int per = (nkb + ks - 1) / ks;
     const int kb0 = rank * per < nkb ? rank * per : nkb;
     const int kb1 = kb0 + per < nkb ? kb0 + per : nkb;
     const int nb = kb1 - kb0;
     const int a = g.plan[g.p.adapter + s];
     const int64_t row0 = int64_t(g.plan[g.p.tile + s]) * kTile;
-    const bool spoiled = g.marks[a] != 0;
-    // one CTA for the whole k: the sums go from registers to memory, and the roles need not meet
-    const bool direct = ks == 1;
-    bool mine = false;  // this thread's row of the tile is the slot's
-    if (warp >= 2) {
-      const int r = (warp & 3) * 32 + lane;
-      mine = row0 + r < g.N && g.plan[g.p.tok_slot + row0 + r] == s;
-      if (!direct) {
-        const unsigned all = __ballot_sync(0xffffffffu, mine);
-        if (lane == 0) members_of[warp & 3] = all;
-      }
-    }
     if (warp == 0) {
       // ---------------- TMA producer
       if (lane == 0 && ok) {
+        const CUtensorMap* mx = set ? &tmX1 : &tmX0;
+        const CUtensorMap* mp = set ? &tmP1 : &tmP0;
         for (int kb = kb0; kb < kb1; ++kb) {
           if (!mbar_try_wait(empty_bar(stage), phase ^ 1u) && !mbar_wait(empty_bar(stage), phase ^ 1u, wc)) {
             ok = false;
@@ -430,19 +444,18 @@ __global__ void __launch_bounds__(kShrinkThreads, 1)
           }
           mbar_arrive_expect_tx(full_bar(stage), uint32_t(stage_bytes));
           const uint32_t dst = smem_base + uint32_t(stage * stage_bytes);
-          tma_load_2d(dst, set ? &tmX1 : &tmX0, full_bar(stage), kb * 64, int(row0));
-#pragma unroll
-          for (int q = 0; q < kP; ++q)
-            tma_load_3d(dst + kXBytes + q * kPBytes, set ? &tmP1 : &tmP0, full_bar(stage), 0, kb * 64, q * g.n + a);
+          tma_load_2d(dst, mx, full_bar(stage), kb * 64, int(row0));
+          for (int q = 0; q < ctiles; ++q)
+            tma_load_3d(dst + kXBytes + q * kPBytes, mp, full_bar(stage), q * 64, kb * 64, a);
           ++iter;
           if (++stage == g.stages) { stage = 0; phase ^= 1u; }
         }
       }
       __syncwarp();
     } else if (warp == 1) {
-      // ---------------- MMA issuer: X tile (K-major) x the adapter's rows (MN-major, a part per 64 columns)
+      // ---------------- MMA issuer: X tile (K-major) x the adapter's rows (MN-major)
       if (lane == 0 && ok) {
-        constexpr uint32_t id = tc::idesc(1, 1, 0, 1, 128, acc_cols);
+        const uint32_t id = tc::idesc(1, 1, 0, 1, 128, uint32_t(g.kp * g.parts));
         for (int j = 0, in_seg = 0; j < nb; ++j) {
           const uint32_t b = seg & 1u;
           if (in_seg == 0 && !mbar_try_wait(acc_empty(b), ((seg >> 1) & 1u) ^ 1u) &&
@@ -474,9 +487,11 @@ __global__ void __launch_bounds__(kShrinkThreads, 1)
       }
       __syncwarp();
     } else {
-      // ---------------- sums of the segments and of the parts; after the last segment's MMAs every
-      // load of the item has been read, so the sums may take the ring's place
+      // ---------------- sums of the segments and of the parts
       const int q = warp & 3;
+      const int row = q * 32 + lane;
+      const bool mine = row0 + row < g.N && g.plan[g.p.tok_slot + row0 + row] == s;
+      const bool spoiled = g.marks[a] != 0;
       float u[64];
 #pragma unroll
       for (int i = 0; i < 64; ++i) u[i] = 0.f;
@@ -490,14 +505,15 @@ __global__ void __launch_bounds__(kShrinkThreads, 1)
         }
         fence_after();
         const uint32_t ta = tmem_base + (uint32_t(q * 32) << 16) + b * acc_cols;
+        for (int p = 0; p < g.parts; ++p) {
 #pragma unroll
-        for (int p = 0; p < kP; ++p) {
+          for (int c = 0; c < 4; ++c) {
+            if (c * 16 < g.kp) {
+              float v[16];
+              tmem_ld16(ta + uint32_t(p * g.kp + c * 16), v);
 #pragma unroll
-          for (int c = 0; c < 2; ++c) {
-            float v[32];
-            tmem_ld32(ta + uint32_t(p * 64 + c * 32), v);
-#pragma unroll
-            for (int i = 0; i < 32; ++i) u[c * 32 + i] += v[i];
+              for (int i = 0; i < 16; ++i) u[c * 16 + i] += v[i];
+            }
           }
         }
         fence_before();
@@ -505,72 +521,51 @@ __global__ void __launch_bounds__(kShrinkThreads, 1)
         if (lane == 0) mbar_arrive(acc_empty(b));
         ++seg;
       }
-      if (ok && direct) {
-        __nv_bfloat16* to = o.out + (int64_t(s) * kSlotRows + q * 32 + lane) * kMaxK;
 #pragma unroll
-        for (int i = 0; i < 64; ++i) u[i] = mine ? (spoiled ? __int_as_float(0x7fffffff) : u[i]) : 0.f;
+      for (int i = 0; i < 64; ++i) u[i] = mine ? (spoiled ? __int_as_float(0x7fffffff) : u[i]) : 0.f;
+      if (ok && ks == 1) {
 #pragma unroll
-        for (int p = 0; p < kP; ++p) {
+        for (int c = 0; c < 8; ++c)
+          if (c * 8 < g.kp) {
+            float v[8];
 #pragma unroll
-          for (int c = 0; c < 8; ++c) {
-            __align__(16) __nv_bfloat16 w[8];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-              w[i] = __float2bfloat16_rn(u[8 * c + i]);
-              u[8 * c + i] -= __bfloat162float(w[i]);
-            }
-            if (LOCA_CHECK(s, g.p.smax))
-              *reinterpret_cast<uint4*>(to + p * part_pitch + 8 * c) = *reinterpret_cast<const uint4*>(w);
+            for (int i = 0; i < 8; ++i) v[i] = u[8 * c + i];
+            store_parts(v, g.one[set].out, g.p.smax, s, row, c * 8, g.kp, g.parts);
           }
-        }
       } else if (ok) {
-        const int row = q * 32 + lane;
+        // after the last segment's MMAs every load of the item has been read: the sums may take the
+        // ring's place
 #pragma unroll
         for (int c = 0; c < 16; ++c)
-          *reinterpret_cast<float4*>(red + red_at(row, 4 * c)) =
-              make_float4(u[4 * c], u[4 * c + 1], u[4 * c + 2], u[4 * c + 3]);
+          if (c * 4 < g.kp)
+            *reinterpret_cast<float4*>(red + red_at(row, 4 * c)) =
+                make_float4(u[4 * c], u[4 * c + 1], u[4 * c + 2], u[4 * c + 3]);
       }
     }
-    if (direct) continue;
+    if (ks == 1) continue;  // the roles need not meet
     __syncwarp();
     cluster_sync();  // every CTA's sums are in its shared memory
-    const int rows_per = kSlotRows / ks;
+    const int rows_per = kSlotRows / ks, chunks = g.kp / 8;
     const uint32_t red_s = smem_u32(red);
-    for (int e = threadIdx.x; e < rows_per * 8; e += kShrinkThreads) {
-      const int row = rank * rows_per + e / 8, ch = e % 8;
+    for (int e = threadIdx.x; e < rows_per * chunks; e += kShrinkThreads) {
+      const int row = rank * rows_per + e / chunks, ch = e % chunks;
+      const uint32_t o0 = red_s + 4u * uint32_t(red_at(row, ch * 8));
+      const uint32_t o1 = red_s + 4u * uint32_t(red_at(row, ch * 8 + 4));
+      float4 x[8], y[8];  // all loads first: one round trip
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        if (j < ks) {
+          x[j] = ld_shared_cluster_f32x4(mapa_shared(o0, uint32_t(j)));
+          y[j] = ld_shared_cluster_f32x4(mapa_shared(o1, uint32_t(j)));
+        }
       float v[8] = {};
-      if (members_of[row >> 5] >> (row & 31) & 1u) {
-        const uint32_t o0 = red_s + 4u * uint32_t(red_at(row, ch * 8));
-        const uint32_t o1 = red_s + 4u * uint32_t(red_at(row, ch * 8 + 4));
-        float4 x[8], y[8];  // all loads first: one round trip
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
-          if (j < ks) {
-            x[j] = ld_shared_cluster_f32x4(mapa_shared(o0, uint32_t(j)));
-            y[j] = ld_shared_cluster_f32x4(mapa_shared(o1, uint32_t(j)));
-          }
-#pragma unroll
-        for (int j = 0; j < 8; ++j)
-          if (j < ks) {
-            v[0] += x[j].x; v[1] += x[j].y; v[2] += x[j].z; v[3] += x[j].w;
-            v[4] += y[j].x; v[5] += y[j].y; v[6] += y[j].z; v[7] += y[j].w;
-          }
-        if (spoiled) {
-#pragma unroll
-          for (int i = 0; i < 8; ++i) v[i] = __int_as_float(0x7fffffff);
+      for (int j = 0; j < 8; ++j)
+        if (j < ks) {
+          v[0] += x[j].x; v[1] += x[j].y; v[2] += x[j].z; v[3] += x[j].w;
+          v[4] += y[j].x; v[5] += y[j].y; v[6] += y[j].z; v[7] += y[j].w;
         }
-      }
-      __nv_bfloat16* to = o.out + (int64_t(s) * kSlotRows + row) * kMaxK + ch * 8;
-#pragma unroll
-      for (int q = 0; q < kP; ++q) {
-        __align__(16) __nv_bfloat16 w[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          w[i] = __float2bfloat16_rn(v[i]);
-          v[i] -= __bfloat162float(w[i]);
-        }
-        if (LOCA_CHECK(s, g.p.smax)) *reinterpret_cast<uint4*>(to + q * part_pitch) = *reinterpret_cast<const uint4*>(w);
-      }
+      store_parts(v, g.one[set].out, g.p.smax, s, row, ch * 8, g.kp, g.parts);
     }
     fence_proxy_async_smem();  // the ring's next loads come after these accesses
     __syncwarp();
@@ -968,16 +963,14 @@ struct EpiRows {
 };
 
 // ------------------------------------------------------------------ dA and dB: channels x k sums over tokens
-// One item per (adapter, 128 channels, range of its slots): M = channels, N = 64 columns per part of U
-// or T, K = the slot's 128 tokens in two stages, both operands MN-major as they lie in memory.  The
-// segments (512 tokens) are added in registers.  A slot whose tile also holds other tokens has those
-// rows of X (or dY) zeroed in shared memory first: their U is zero, but a product with whatever else
-// stands there (infinities, NaN) need not be.
+// One item per (adapter, 128 channels, range of its slots): M = channels, N = the columns of U or T
+// (kp per part, side by side), K = the slot's 128 tokens in two stages, both operands MN-major as they
+// lie in memory.  The segments (512 tokens) are added in registers.  A slot whose tile also holds other
+// tokens has those rows of X (or dY) zeroed in shared memory first: their U is zero, but a product with
+// whatever else stands there (infinities, NaN) need not be.
 constexpr int kGradThreads = 224;
-constexpr int kGradStages = 5;
-constexpr int kGradStageBytes = kXBytes + kParts * kPBytes;  // 40 KB
+constexpr int kGradMaxStages = 8;
 constexpr int kGradSeg = 8;
-constexpr int kGradSmem = kGradStages * kGradStageBytes + 512 + 1024;
 
 struct GradOne {
   int64_t d;        // channels
@@ -987,7 +980,7 @@ struct GradOne {
 struct GradGeo {
   GradOne one[2];
   int64_t N;
-  int n, kp, items;  // of both
+  int n, kp, parts, stages, items;  // items of both
   const int32_t* plan;
   PlanLay p;
   int32_t* status;
@@ -995,6 +988,7 @@ struct GradGeo {
   unsigned long long limit_ns;
   int32_t mark;
 };
+int grad_smem(int utiles, int stages) { return stages * (kXBytes + utiles * kPBytes) + 512 + 1024; }
 
 __global__ void __launch_bounds__(kGradThreads, 1)
     k_adapter_grad(const __grid_constant__ CUtensorMap tmS0, const __grid_constant__ CUtensorMap tmU0,
@@ -1002,22 +996,26 @@ __global__ void __launch_bounds__(kGradThreads, 1)
                    const __grid_constant__ GradGeo g) {
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
-  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + kGradStages * kGradStageBytes);
+  const int utiles = col_tiles(g.kp, g.parts);
+  const int stage_bytes = kXBytes + utiles * kPBytes;
+  const int stages = g.stages;
+  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + stages * stage_bytes);
   const uint32_t bar_base = smem_u32(bars);
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 3 * kGradStages + 5);
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 3 * kGradMaxStages + 5);
   auto full_bar = [&](int s) { return bar_base + 8u * s; };
-  auto empty_bar = [&](int s) { return bar_base + 8u * (kGradStages + s); };
-  auto ready_bar = [&](int s) { return bar_base + 8u * (2 * kGradStages + s); };
-  auto acc_full = [&](uint32_t b) { return bar_base + 8u * (3 * kGradStages + b); };
-  auto acc_empty = [&](uint32_t b) { return bar_base + 8u * (3 * kGradStages + 2 + b); };
-  const uint32_t drain_bar = bar_base + 8u * (3 * kGradStages + 4);
+  auto empty_bar = [&](int s) { return bar_base + 8u * (kGradMaxStages + s); };
+  auto ready_bar = [&](int s) { return bar_base + 8u * (2 * kGradMaxStages + s); };
+  auto acc_full = [&](uint32_t b) { return bar_base + 8u * (3 * kGradMaxStages + b); };
+  auto acc_empty = [&](uint32_t b) { return bar_base + 8u * (3 * kGradMaxStages + 2 + b); };
+  const uint32_t drain_bar = bar_base + 8u * (3 * kGradMaxStages + 4);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t smem_base = smem_u32(smem);
   const WaitCtl wc{g.status, g.abort_flag, g.limit_ns, g.mark};
-  constexpr uint32_t kCols = 64 * kParts;
+  const uint32_t acc_cols = uint32_t(64 * utiles);
+  const uint32_t cols = utiles == 1 ? 128u : utiles == 2 ? 256u : 512u;
 
   if (threadIdx.x == 0) {
-    for (int s = 0; s < kGradStages; ++s) {
+    for (int s = 0; s < kGradMaxStages; ++s) {
       mbar_init(full_bar(s), 1);
       mbar_init(empty_bar(s), 1);
       mbar_init(ready_bar(s), 1);
@@ -1035,7 +1033,7 @@ __global__ void __launch_bounds__(kGradThreads, 1)
       prefetch_tensormap(&tmU1);
     }
   }
-  if (warp == 1) tmem_alloc(smem_u32(tmem_slot), 512);
+  if (warp == 1) tmem_alloc(smem_u32(tmem_slot), cols);
   fence_before();
   __syncthreads();
   fence_after();
@@ -1071,25 +1069,33 @@ __global__ void __launch_bounds__(kGradThreads, 1)
       bool ok = true;
       for (int it = blockIdx.x; it < items && ok; it += gridDim.x) {
         const Item w = item_of(it);
+        const CUtensorMap* ms = w.set ? &tmS1 : &tmS0;
+        const CUtensorMap* mu = w.set ? &tmU1 : &tmU0;
+        int s = 0, tile = 0;
+        if (w.s0 < w.s1) {
+          s = g.plan[g.p.ad_slots + w.s0];
+          tile = g.plan[g.p.ad_tile + w.s0];
+        }
         for (int l = w.s0; l < w.s1 && ok; ++l) {
-          const int s = g.plan[g.p.ad_slots + l];
-          const int row = g.plan[g.p.tile + s] * kTile;
+          const int ln = l + 1 < w.s1 ? l + 1 : l;  // the next slot's entries are under way meanwhile
+          const int s_next = g.plan[g.p.ad_slots + ln], tile_next = g.plan[g.p.ad_tile + ln];
+          const int row = tile * kTile;
           for (int h = 0; h < 2; ++h) {
             if (!mbar_try_wait(empty_bar(stage), phase ^ 1u) && !mbar_wait(empty_bar(stage), phase ^ 1u, wc)) {
               ok = false;
               break;
             }
-            mbar_arrive_expect_tx(full_bar(stage), uint32_t(kGradStageBytes));
-            const uint32_t dst = smem_base + uint32_t(stage * kGradStageBytes);
-            const CUtensorMap* ms = w.set ? &tmS1 : &tmS0;
-            const CUtensorMap* mu = w.set ? &tmU1 : &tmU0;
+            mbar_arrive_expect_tx(full_bar(stage), uint32_t(stage_bytes));
+            const uint32_t dst = smem_base + uint32_t(stage * stage_bytes);
             tma_load_2d(dst, ms, full_bar(stage), w.ct * 128, row + 64 * h);
             tma_load_2d(dst + kXBytes / 2, ms, full_bar(stage), w.ct * 128 + 64, row + 64 * h);
-            for (int q = 0; q < kParts; ++q)
+            for (int q = 0; q < utiles; ++q)
               tma_load_3d(dst + kXBytes + q * kPBytes, mu, full_bar(stage), 0, s * kSlotRows + 64 * h, q);
             ++iter;
-            if (++stage == kGradStages) { stage = 0; phase ^= 1u; }
+            if (++stage == stages) { stage = 0; phase ^= 1u; }
           }
+          s = s_next;
+          tile = tile_next;
         }
       }
     }
@@ -1101,19 +1107,27 @@ __global__ void __launch_bounds__(kGradThreads, 1)
     bool ok = true;
     for (int it = blockIdx.x; it < items && ok; it += gridDim.x) {
       const Item w = item_of(it);
+      int s = 0, tile = 0, count = 0;
+      if (w.s0 < w.s1) {
+        s = g.plan[g.p.ad_slots + w.s0];
+        tile = g.plan[g.p.ad_tile + w.s0];
+        count = g.plan[g.p.ad_count + w.s0];
+      }
       for (int l = w.s0; l < w.s1 && ok; ++l) {
-        const int s = g.plan[g.p.ad_slots + l];
-        const int64_t row = int64_t(g.plan[g.p.tile + s]) * kTile;
+        const int ln = l + 1 < w.s1 ? l + 1 : l;
+        const int s_next = g.plan[g.p.ad_slots + ln], tile_next = g.plan[g.p.ad_tile + ln];
+        const int count_next = g.plan[g.p.ad_count + ln];
+        const int64_t row = int64_t(tile) * kTile;
         const int64_t in_tile = g.N - row < kTile ? g.N - row : kTile;
-        const bool mixed = g.plan[g.p.count + s] < in_tile;
+        const bool mixed = count < in_tile;
         for (int h = 0; h < 2; ++h) {
-          const bool got = mbar_wait(full_bar(stage), phase, wc);
+          const bool got = mbar_try_wait(full_bar(stage), phase) || mbar_wait(full_bar(stage), phase, wc);
           if (!__all_sync(0xffffffffu, got)) {
             ok = false;
             break;
           }
           if (mixed) {
-            uint8_t* box = smem + stage * kGradStageBytes;
+            uint8_t* box = smem + stage * stage_bytes;
             for (int r = lane; r < 64; r += 32) {
               const int64_t tok = row + 64 * h + r;
               if (tok < g.N && g.plan[g.p.tok_slot + tok] != s) {
@@ -1128,8 +1142,11 @@ __global__ void __launch_bounds__(kGradThreads, 1)
           }
           __syncwarp();
           if (lane == 0) mbar_arrive(ready_bar(stage));
-          if (++stage == kGradStages) { stage = 0; phase ^= 1u; }
+          if (++stage == stages) { stage = 0; phase ^= 1u; }
         }
+        s = s_next;
+        tile = tile_next;
+        count = count_next;
       }
     }
   } else if (warp == 1) {
@@ -1137,7 +1154,7 @@ __global__ void __launch_bounds__(kGradThreads, 1)
       int stage = 0;
       uint32_t phase = 0, seg = 0;
       bool ok = true, issued = false;
-      constexpr uint32_t kId = tc::idesc(1, 1, 1, 1, 128, kCols);
+      const uint32_t id = tc::idesc(1, 1, 1, 1, 128, uint32_t(g.kp * g.parts));
       for (int it = blockIdx.x; it < items && ok; it += gridDim.x) {
         const Item w = item_of(it);
         const int nb = 2 * (w.s1 - w.s0);
@@ -1154,16 +1171,16 @@ __global__ void __launch_bounds__(kGradThreads, 1)
             break;
           }
           fence_after();
-          const uint32_t st = smem_base + uint32_t(stage * kGradStageBytes);
+          const uint32_t st = smem_base + uint32_t(stage * stage_bytes);
           const uint64_t ad = sdesc(st, kXBytes / 2, 1024u, kSwizzle128B);
           const uint64_t bd = sdesc(st + kXBytes, kPBytes, 1024u, kSwizzle128B);
-          const uint32_t d = tmem_base + b * 256u;
+          const uint32_t d = tmem_base + b * acc_cols;
 #pragma unroll
           for (int kk = 0; kk < 4; ++kk)
-            mma_f16(d, ad + kk * (2048 >> 4), bd + kk * (2048 >> 4), kId, (in_seg | kk) != 0 ? 1u : 0u);
+            mma_f16(d, ad + kk * (2048 >> 4), bd + kk * (2048 >> 4), id, (in_seg | kk) != 0 ? 1u : 0u);
           issued = true;
           mma_commit(empty_bar(stage));
-          if (++stage == kGradStages) { stage = 0; phase ^= 1u; }
+          if (++stage == stages) { stage = 0; phase ^= 1u; }
           if (++in_seg == kGradSeg || j == nb - 1) {
             mma_commit(acc_full(b));
             ++seg;
@@ -1189,20 +1206,22 @@ __global__ void __launch_bounds__(kGradThreads, 1)
       for (int i = 0; i < 64; ++i) u[i] = 0.f;
       for (int j = 0; j < nseg; ++j) {
         const uint32_t b = seg & 1u;
-        const bool got = mbar_wait(acc_full(b), (seg >> 1) & 1u, wc);
+        const bool got = mbar_try_wait(acc_full(b), (seg >> 1) & 1u) || mbar_wait(acc_full(b), (seg >> 1) & 1u, wc);
         if (!__all_sync(0xffffffffu, got)) {
           ok = false;
           break;
         }
         fence_after();
-        const uint32_t ta = tmem_base + (uint32_t(q * 32) << 16) + b * 256u;
-        for (int p = 0; p < kParts; ++p) {
+        const uint32_t ta = tmem_base + (uint32_t(q * 32) << 16) + b * acc_cols;
+        for (int p = 0; p < g.parts; ++p) {
 #pragma unroll
-          for (int c = 0; c < 2; ++c) {
-            float v[32];
-            tmem_ld32(ta + uint32_t(p * 64 + c * 32), v);
+          for (int c = 0; c < 4; ++c) {
+            if (c * 16 < g.kp) {
+              float v[16];
+              tmem_ld16(ta + uint32_t(p * g.kp + c * 16), v);
 #pragma unroll
-            for (int i = 0; i < 32; ++i) u[c * 32 + i] += v[i];
+              for (int i = 0; i < 16; ++i) u[c * 16 + i] += v[i];
+            }
           }
         }
         fence_before();
@@ -1222,14 +1241,16 @@ __global__ void __launch_bounds__(kGradThreads, 1)
       }
     }
   }
-  if (warp == 0 && lane == 0)
-    for (uint32_t i = iter > kGradStages ? iter - kGradStages : 0u; i < iter; ++i)
-      mbar_drain(full_bar(int(i % kGradStages)), (i / kGradStages) & 1u, kDrainLimitNs);
+  if (warp == 0 && lane == 0) {
+    const uint32_t n = uint32_t(stages);
+    for (uint32_t i = iter > n ? iter - n : 0u; i < iter; ++i)
+      mbar_drain(full_bar(int(i % n)), (i / n) & 1u, kDrainLimitNs);
+  }
   __syncwarp();
   fence_before();
   __syncthreads();
   fence_after();
-  if (warp == 1) tmem_dealloc(tmem_base, 512);
+  if (warp == 1) tmem_dealloc(tmem_base, cols);
 }
 
 struct JoinOne {
@@ -1239,25 +1260,44 @@ struct JoinOne {
   int64_t rows, d;     // n d rows of k values (0: nothing to do)
   int ranges;
 };
+// Four lanes share the ranges of four neighbouring columns of a row; their sums meet in a fixed order.
 template <class T>
 __global__ void __launch_bounds__(256) k_adapter_join(const JoinOne j0, const JoinOne j1, int k, int kp) {
   wait_for_previous();
   launch_dependents();
-  const int64_t n0 = j0.rows * k;
-  for (int64_t e = int64_t(blockIdx.x) * blockDim.x + threadIdx.x; e < n0 + j1.rows * k;
-       e += int64_t(gridDim.x) * blockDim.x) {
-    const JoinOne& j = e < n0 ? j0 : j1;
-    const int64_t i = e < n0 ? e : e - n0;
-    const int64_t row = i / k;
-    const int c = int(i - row * k);
-    const float* p = j.part + row * kp + c;
-    const int64_t pitch = j.rows * kp;
-    float v = 0.f;
-#pragma unroll 8
-    for (int r = 0; r < j.ranges; ++r) v += p[r * pitch];
-    if (j.scale) v *= j.scale[row / j.d];
-    if constexpr (sizeof(T) == 4) static_cast<float*>(j.out)[i] = v;
-    else static_cast<__nv_bfloat16*>(j.out)[i] = __float2bfloat16_rn(v);
+  const int lane4 = threadIdx.x & 3;
+  const int64_t groups = (j0.rows + j1.rows) * (kp / 4);
+  for (int64_t b0 = int64_t(blockIdx.x) * 64; b0 < groups; b0 += int64_t(gridDim.x) * 64) {
+    const int64_t gi = b0 + threadIdx.x / 4;
+    const bool on = gi < groups;
+    const int64_t flat = on ? gi / (kp / 4) : 0;
+    const int c = on ? int(gi - flat * (kp / 4)) * 4 : 0;
+    const JoinOne& j = flat < j0.rows ? j0 : j1;
+    const int64_t row = flat < j0.rows ? flat : flat - j0.rows;
+    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (on) {
+      const float* p = j.part + row * kp + c;
+      const int64_t pitch = j.rows * kp;
+#pragma unroll 4
+      for (int r = lane4; r < j.ranges; r += 4) {
+        const float4 x = *reinterpret_cast<const float4*>(p + r * pitch);
+        v.x += x.x; v.y += x.y; v.z += x.z; v.w += x.w;
+      }
+    }
+#pragma unroll
+    for (int o = 1; o < 4; o <<= 1) {
+      v.x += __shfl_xor_sync(0xffffffffu, v.x, o);
+      v.y += __shfl_xor_sync(0xffffffffu, v.y, o);
+      v.z += __shfl_xor_sync(0xffffffffu, v.z, o);
+      v.w += __shfl_xor_sync(0xffffffffu, v.w, o);
+    }
+    const int col = c + lane4;
+    if (on && col < k) {
+      float x = lane4 == 0 ? v.x : lane4 == 1 ? v.y : lane4 == 2 ? v.z : v.w;
+      if (j.scale) x *= j.scale[row / j.d];
+      if constexpr (sizeof(T) == 4) static_cast<float*>(j.out)[row * k + col] = x;
+      else static_cast<__nv_bfloat16*>(j.out)[row * k + col] = __float2bfloat16_rn(x);
+    }
   }
 }
 
@@ -1289,7 +1329,8 @@ int grad_ranges(int n, int64_t d, int64_t tiles) {
 AdapterWs adapter_ws(int64_t N, int64_t d_in, int64_t d_out, int k, int n, bool backward) {
   AdapterWs w{};
   const PlanLay p = plan_lay(N, n);
-  const size_t one = align256(2 * kSlotElems * size_t(p.smax < 1 ? 1 : p.smax) * size_t(backward ? kParts : 1));
+  const size_t one = align256(2 * kSlotElems * size_t(p.smax < 1 ? 1 : p.smax) *
+                              size_t(col_tiles(k_padded(k), backward ? kParts : 1)));
   size_t at = 256;  // the launches' abort flag
   // U: the slots' tiles, or the tokens' partial sums
   const size_t tok = align256(4 * 8 * size_t(N) * size_t(k_padded(k)));
@@ -1364,24 +1405,23 @@ cudaError_t shrink(const Call& c, const Shrink* set, int sets, const int32_t* ma
   int64_t dmin = 0;
   for (int i = 0; i < sets; ++i) {
     const Shrink& v = set[i];
+    const int64_t pitch = parts == 1 ? c.kp : kParts * c.kp;  // the first parts alone, or all side by side
     if (!gp::map_kmajor(&mx[i], v.X, v.d, c.N, v.ldx) ||
-        !gp::map_3d(&mp[i], CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, v.P, c.kp, v.d, int64_t(kParts) * c.n, c.kp, v.d * c.kp,
-                    64, 64))
+        !gp::map_3d(&mp[i], CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, v.P, parts * c.kp, v.d, c.n, pitch, v.d * pitch, 64, 64))
       return cudaErrorInvalidValue;
-    g.one[i].X = static_cast<const __nv_bfloat16*>(v.X);
-    g.one[i].ldx = v.ldx;
     g.one[i].d = v.d;
-    g.one[i].P = v.P;
     g.one[i].out = static_cast<__nv_bfloat16*>(v.out);
     if (i == 0 || v.d < dmin) dmin = v.d;
   }
   g.sets = sets;
   g.N = c.N;
   g.marks = marks;
-  g.n = c.n;
   g.kp = c.kp;
+  g.parts = parts;
   // few tokens: a small ring, so that k_adapter_few's CTAs fit beside these
-  g.stages = parts > 1 ? 5 : c.N <= kTile ? 3 : kMaxStages;
+  const int ctiles = col_tiles(c.kp, parts);
+  g.stages = parts == 1 && c.N <= kTile ? 3 : 200 * 1024 / (kXBytes + ctiles * kPBytes);
+  if (g.stages > kMaxStages) g.stages = kMaxStages;
   g.plan = c.plan;
   g.p = c.p;
   g.status = c.status;
@@ -1395,8 +1435,8 @@ cudaError_t shrink(const Call& c, const Shrink* set, int sets, const int32_t* ma
   int64_t clusters = sm_count() / ks;
   if (clusters > c.p.smax * sets) clusters = c.p.smax * sets;
   const int second = sets - 1;
-  return launch_cluster(parts == 1 ? k_adapter_shrink<1> : k_adapter_shrink<kParts>, dim3(unsigned(clusters * ks)),
-                        kShrinkThreads, shrink_smem(parts, g.stages), ks, c.s, mx[0], mp[0], mx[second], mp[second], g);
+  return launch_cluster(k_adapter_shrink, dim3(unsigned(clusters * ks)), kShrinkThreads, shrink_smem(ctiles, g.stages),
+                        ks, c.s, mx[0], mp[0], mx[second], mp[second], g);
 }
 
 // U of every token, in partial sums (ranges x N x kp fp32 at `out`).
@@ -1500,15 +1540,16 @@ struct Grad {
   const float* scale;
   void* out;
 };
-cudaError_t grad(const Call& c, const Grad* set, int sets, int dtype) {
+cudaError_t grad(const Call& c, const Grad* set, int sets, int parts, int dtype) {
   CUtensorMap ms[2], mu[2];
   GradGeo g{};
   JoinOne j[2] = {};
-  int64_t values = 0;
+  int64_t groups = 0;
+  const int utiles = col_tiles(c.kp, parts);
   for (int i = 0; i < sets; ++i) {
     const Grad& v = set[i];
     if (!gp::map_mnmajor(&ms[i], v.S, v.d, c.N, v.lds) ||
-        !gp::map_3d(&mu[i], CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, v.U, kMaxK, c.p.smax * kSlotRows, kParts, kMaxK,
+        !gp::map_3d(&mu[i], CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, v.U, kMaxK, c.p.smax * kSlotRows, utiles, kMaxK,
                     c.p.smax * int64_t(kSlotElems), 64, 64))
       return cudaErrorInvalidValue;
     g.one[i].d = v.d;
@@ -1523,11 +1564,14 @@ cudaError_t grad(const Call& c, const Grad* set, int sets, int dtype) {
     j[i].rows = int64_t(c.n) * v.d;
     j[i].d = v.d;
     j[i].ranges = v.ranges;
-    values += j[i].rows * c.k;
+    groups += j[i].rows * (c.kp / 4);
   }
   g.N = c.N;
   g.n = c.n;
   g.kp = c.kp;
+  g.parts = parts;
+  g.stages = 200 * 1024 / (kXBytes + utiles * kPBytes);
+  if (g.stages > kGradMaxStages) g.stages = kGradMaxStages;
   g.plan = c.plan;
   g.p = c.p;
   g.status = c.status;
@@ -1536,10 +1580,10 @@ cudaError_t grad(const Call& c, const Grad* set, int sets, int dtype) {
   g.mark = c.mark;
   const int second = sets - 1;
   const unsigned blocks = unsigned(g.items < sm_count() ? g.items : sm_count());
-  const cudaError_t e = launch_cluster(k_adapter_grad, dim3(blocks), kGradThreads, kGradSmem, 1, c.s, ms[0], mu[0],
+  const cudaError_t e = launch_cluster(k_adapter_grad, dim3(blocks), kGradThreads, grad_smem(utiles, g.stages), 1, c.s, ms[0], mu[0],
                                        ms[second], mu[second], g);
   if (e != cudaSuccess) return e;
-  const unsigned jb = unsigned(values / 256 + 1 < 8 * sm_count() ? values / 256 + 1 : 8 * sm_count());
+  const unsigned jb = unsigned(groups / 64 + 1 < 16 * sm_count() ? groups / 64 + 1 : 16 * sm_count());
   return launch_cluster(dtype == LOCA_F32 ? k_adapter_join<float> : k_adapter_join<__nv_bfloat16>, dim3(jb), 256, 0, 1,
                         c.s, j[0], j[1], c.k, c.kp);
 }
@@ -1576,6 +1620,8 @@ cudaError_t launch_adapter_pack(const void* A, const void* B, int dtype, int n, 
   uint8_t* b = static_cast<uint8_t*>(packed);
   __nv_bfloat16* pa = reinterpret_cast<__nv_bfloat16*>(b + p.a);
   __nv_bfloat16* pb = reinterpret_cast<__nv_bfloat16*>(b + p.b);
+  __nv_bfloat16* all_a = reinterpret_cast<__nv_bfloat16*>(b + p.all_a);
+  __nv_bfloat16* all_b = reinterpret_cast<__nv_bfloat16*>(b + p.all_b);
   float* ps = reinterpret_cast<float*>(b + p.scale);
   int32_t* marks = reinterpret_cast<int32_t*>(b + p.marks);
   const cudaError_t e = cudaMemsetAsync(marks, 0, 4 * size_t(n), s);
@@ -1585,11 +1631,11 @@ cudaError_t launch_adapter_pack(const void* A, const void* B, int dtype, int n, 
   const unsigned blocks = unsigned(values / 256 + 1 < 8 * sm_count() ? values / 256 + 1 : 8 * sm_count());
   if (dtype == LOCA_F32)
     k_adapter_pack<float><<<blocks, 256, 0, s>>>(static_cast<const float*>(A), static_cast<const float*>(B), n, d_in,
-                                                 d_out, k, kp, scale, pa, pb, ps, marks);
+                                                 d_out, k, kp, scale, pa, pb, all_a, all_b, ps, marks);
   else
     k_adapter_pack<__nv_bfloat16><<<blocks, 256, 0, s>>>(static_cast<const __nv_bfloat16*>(A),
                                                          static_cast<const __nv_bfloat16*>(B), n, d_in, d_out, k, kp,
-                                                         scale, pa, pb, ps, marks);
+                                                         scale, pa, pb, all_a, all_b, ps, marks);
   return cudaGetLastError();
 }
 
@@ -1633,14 +1679,17 @@ cudaError_t launch_adapter_backward(const void* X, int64_t ldx, const void* dY, 
   const uint8_t* pb = static_cast<const uint8_t*>(packed);
   const __nv_bfloat16* pa = reinterpret_cast<const __nv_bfloat16*>(pb + pk.a);
   const int32_t* marks = reinterpret_cast<const int32_t*>(pb + pk.marks);
-  const __nv_bfloat16* pB = reinterpret_cast<const __nv_bfloat16*>(pb + pk.b);
   uint8_t* ws = static_cast<uint8_t*>(workspace);
-  const Shrink u{X, ldx, d_in, pa, ws + w.u}, t{dY, lddy, d_out, pB, ws + w.t};
+  // gradients in fp32 take three parts of U, T and the adapters, in bf16 two (2^-17), dX alone one
+  const int parts = !dA && !dB ? 1 : grad_dtype == LOCA_F32 ? kParts : 2;
+  const __nv_bfloat16* sa = reinterpret_cast<const __nv_bfloat16*>(pb + (parts == 1 ? pk.a : pk.all_a));
+  const __nv_bfloat16* sb = reinterpret_cast<const __nv_bfloat16*>(pb + (parts == 1 ? pk.b : pk.all_b));
+  const Shrink u{X, ldx, d_in, sa, ws + w.u}, t{dY, lddy, d_out, sb, ws + w.t};
   Shrink set[2] = {t, t};
   int sets = 0;
   if (dA || dX) set[sets++] = t;
   if (dB) set[sets++] = u;
-  cudaError_t e = shrink(c, set, sets, marks, dA || dB ? kParts : 1);
+  cudaError_t e = shrink(c, set, sets, marks, parts);
   if (e != cudaSuccess) return e;
   if (dX) {
     e = project<true>(c, dY, lddy, d_out, W, d_in, pa, ws + w.t, false, dX, lddx);
@@ -1653,7 +1702,7 @@ cudaError_t launch_adapter_backward(const void* X, int64_t ldx, const void* dY, 
   int ng = 0;
   if (dA) grads[ng++] = ga;
   if (dB) grads[ng++] = gb;
-  return ng ? grad(c, grads, ng, grad_dtype) : cudaSuccess;
+  return ng ? grad(c, grads, ng, parts, grad_dtype) : cudaSuccess;
 }
 
 }  // namespace loca
