@@ -49,7 +49,7 @@ __host__ __device__ inline int k_padded(int k) { return (k + 15) / 16 * 16; }
 // Offsets in int32 from the start of the plan.
 struct PlanLay {
   int64_t tiles, pairs, smax;
-  int64_t tok_slot, tok_adapter, tile_base, adapter, tile, count, pair_count, pair_ad, pair_s0, pair_s1, ad_off, ad_slots, ad_tile, ad_count, total;
+  int64_t tok_slot, tok_adapter, tile_base, adapter, tile, count, pair_count, pair_ad, pair_s0, pair_s1, ad_off, ad_slots, ad_tile, ad_count, ad_adapter, total;
 };
 PlanLay plan_lay(int64_t N, int n) {
   PlanLay p{};
@@ -77,6 +77,7 @@ PlanLay plan_lay(int64_t N, int n) {
   p.ad_slots = take(p.smax);
   p.ad_tile = take(p.smax);
   p.ad_count = take(p.smax);
+  p.ad_adapter = take(p.smax);
   p.total = at;
   return p;
 }
@@ -232,6 +233,7 @@ __global__ void __launch_bounds__(256) k_plan_adapters(int32_t* plan, PlanLay p,
       plan[p.ad_slots + off] = s;
       plan[p.ad_tile + off] = plan[p.tile + s];
       plan[p.ad_count + off] = plan[p.count + s];
+      plan[p.ad_adapter + off] = a;
     }
     at += here;
     __syncthreads();
@@ -963,9 +965,11 @@ struct EpiRows {
 };
 
 // ------------------------------------------------------------------ dA and dB: channels x k sums over tokens
-// One item per (adapter, 128 channels, range of its slots): M = channels, N = the columns of U or T
-// (kp per part, side by side), K = the slot's 128 tokens in two stages, both operands MN-major as they
-// lie in memory.  The segments (512 tokens) are added in registers.  A slot whose tile also holds other
+// The slots, in the order of their adapters, are cut into equal ranges; one item per (128 channels,
+// range).  M = channels, N = the columns of U or T (kp per part, side by side), K = the slots' 128 tokens
+// in two stages, both operands MN-major as they lie in memory.  A range that crosses from one adapter to
+// the next writes a partial sum for each: range r's of adapter a is number r + a (each step of the list
+// raises r or a, so no two share a number).  The segments (512 tokens) are added in registers.  A slot whose tile also holds other
 // tokens has those rows of X (or dY) zeroed in shared memory first: their U is zero, but a product with
 // whatever else stands there (infinities, NaN) need not be.
 constexpr int kGradThreads = 224;
@@ -975,7 +979,7 @@ constexpr int kGradSeg = 8;
 struct GradOne {
   int64_t d;        // channels
   int ctiles, ranges, items;
-  float* part;      // ranges x n x d x kp
+  float* part;      // (ranges + n) x d x kp
 };
 struct GradGeo {
   GradOne one[2];
@@ -1043,23 +1047,26 @@ __global__ void __launch_bounds__(kGradThreads, 1)
   const int items = g.items;
   uint32_t iter = 0;
   struct Item {
-    int set, a, ct, range, s0, s1;  // s0 .. s1: places in the adapter's list of slots
+    int set, ct, range, s0, s1;  // s0 .. s1: places in the list of slots by adapter
   };
+  const int all_slots = g.plan[g.p.tile_base + g.p.tiles];
   auto item_of = [&](int it) {
     Item w;
     w.set = it >= g.one[0].items ? 1 : 0;
     const GradOne& o = g.one[w.set];
     if (w.set) it -= g.one[0].items;
-    const int per_a = o.ctiles * o.ranges;
-    w.a = it / per_a;
-    const int r = it - w.a * per_a;
-    w.range = r / o.ctiles;  // channel tiles fastest: CTAs at work share a range's U or T
-    w.ct = r - w.range * o.ctiles;
-    const int b0 = g.plan[g.p.ad_off + w.a], b1 = g.plan[g.p.ad_off + w.a + 1];
-    const int per = (b1 - b0 + o.ranges - 1) / o.ranges;
-    w.s0 = b0 + w.range * per < b1 ? b0 + w.range * per : b1;
-    w.s1 = w.s0 + per < b1 ? w.s0 + per : b1;
+    w.range = it / o.ctiles;  // channel tiles fastest: CTAs at work share a range's U or T
+    w.ct = it - w.range * o.ctiles;
+    const int per = (all_slots + o.ranges - 1) / o.ranges;
+    w.s0 = w.range * per < all_slots ? w.range * per : all_slots;
+    w.s1 = w.s0 + per < all_slots ? w.s0 + per : all_slots;
     return w;
+  };
+  // end of the run of slots of one adapter that starts at place l
+  auto run_end = [&](int l, const Item& w, int& a) {
+    a = g.plan[g.p.ad_adapter + l];
+    const int e = g.plan[g.p.ad_off + a + 1];
+    return e < w.s1 ? e : w.s1;
   };
 
   if (warp == 0) {
@@ -1157,8 +1164,10 @@ __global__ void __launch_bounds__(kGradThreads, 1)
       const uint32_t id = tc::idesc(1, 1, 1, 1, 128, uint32_t(g.kp * g.parts));
       for (int it = blockIdx.x; it < items && ok; it += gridDim.x) {
         const Item w = item_of(it);
+        int end = w.s0, a = 0;
         const int nb = 2 * (w.s1 - w.s0);
         for (int j = 0, in_seg = 0; j < nb; ++j) {
+          if (w.s0 + j / 2 == end) end = run_end(end, w, a);
           const uint32_t b = seg & 1u;
           if (in_seg == 0 && !mbar_try_wait(acc_empty(b), ((seg >> 1) & 1u) ^ 1u) &&
               !mbar_wait(acc_empty(b), ((seg >> 1) & 1u) ^ 1u, wc)) {
@@ -1181,7 +1190,7 @@ __global__ void __launch_bounds__(kGradThreads, 1)
           issued = true;
           mma_commit(empty_bar(stage));
           if (++stage == stages) { stage = 0; phase ^= 1u; }
-          if (++in_seg == kGradSeg || j == nb - 1) {
+          if (++in_seg == kGradSeg || j == 2 * (end - w.s0) - 1) {  // full, or the adapter's last slot here
             mma_commit(acc_full(b));
             ++seg;
             in_seg = 0;
@@ -1200,44 +1209,49 @@ __global__ void __launch_bounds__(kGradThreads, 1)
     bool ok = true;
     for (int it = blockIdx.x; it < items && ok; it += gridDim.x) {
       const Item w = item_of(it);
-      const int nseg = (2 * (w.s1 - w.s0) + kGradSeg - 1) / kGradSeg;
-      float u[64];
+      const GradOne& o = g.one[w.set];
+      const int64_t ch = int64_t(w.ct) * 128 + q * 32 + lane;
+      for (int l = w.s0; l < w.s1 && ok;) {
+        int a;
+        const int end = run_end(l, w, a);
+        const int nseg = (2 * (end - l) + kGradSeg - 1) / kGradSeg;
+        float u[64];
 #pragma unroll
-      for (int i = 0; i < 64; ++i) u[i] = 0.f;
-      for (int j = 0; j < nseg; ++j) {
-        const uint32_t b = seg & 1u;
-        const bool got = mbar_try_wait(acc_full(b), (seg >> 1) & 1u) || mbar_wait(acc_full(b), (seg >> 1) & 1u, wc);
-        if (!__all_sync(0xffffffffu, got)) {
-          ok = false;
-          break;
-        }
-        fence_after();
-        const uint32_t ta = tmem_base + (uint32_t(q * 32) << 16) + b * acc_cols;
-        for (int p = 0; p < g.parts; ++p) {
+        for (int i = 0; i < 64; ++i) u[i] = 0.f;
+        for (int j = 0; j < nseg; ++j) {
+          const uint32_t b = seg & 1u;
+          const bool got = mbar_try_wait(acc_full(b), (seg >> 1) & 1u) || mbar_wait(acc_full(b), (seg >> 1) & 1u, wc);
+          if (!__all_sync(0xffffffffu, got)) {
+            ok = false;
+            break;
+          }
+          fence_after();
+          const uint32_t ta = tmem_base + (uint32_t(q * 32) << 16) + b * acc_cols;
+          for (int p = 0; p < g.parts; ++p) {
 #pragma unroll
-          for (int c = 0; c < 4; ++c) {
-            if (c * 16 < g.kp) {
-              float v[16];
-              tmem_ld16(ta + uint32_t(p * g.kp + c * 16), v);
+            for (int c = 0; c < 4; ++c) {
+              if (c * 16 < g.kp) {
+                float v[16];
+                tmem_ld16(ta + uint32_t(p * g.kp + c * 16), v);
 #pragma unroll
-              for (int i = 0; i < 16; ++i) u[c * 16 + i] += v[i];
+                for (int i = 0; i < 16; ++i) u[c * 16 + i] += v[i];
+              }
             }
           }
+          fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(acc_empty(b));
+          ++seg;
         }
-        fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(acc_empty(b));
-        ++seg;
-      }
-      if (!ok) break;
-      const int64_t ch = int64_t(w.ct) * 128 + q * 32 + lane;
-      const GradOne& o = g.one[w.set];
-      if (ch < o.d) {
-        float* to = o.part + ((int64_t(w.range) * g.n + w.a) * o.d + ch) * g.kp;
+        if (!ok) break;
+        if (ch < o.d && LOCA_CHECK(w.range + a, o.ranges + g.n)) {
+          float* to = o.part + (int64_t(w.range + a) * o.d + ch) * g.kp;
 #pragma unroll
-        for (int c = 0; c < 16; ++c)
-          if (4 * c < g.kp)
-            *reinterpret_cast<float4*>(to + 4 * c) = make_float4(u[4 * c], u[4 * c + 1], u[4 * c + 2], u[4 * c + 3]);
+          for (int c = 0; c < 16; ++c)
+            if (4 * c < g.kp)
+              *reinterpret_cast<float4*>(to + 4 * c) = make_float4(u[4 * c], u[4 * c + 1], u[4 * c + 2], u[4 * c + 3]);
+        }
+        l = end;
       }
     }
   }
@@ -1262,9 +1276,12 @@ struct JoinOne {
 };
 // Four lanes share the ranges of four neighbouring columns of a row; their sums meet in a fixed order.
 template <class T>
-__global__ void __launch_bounds__(256) k_adapter_join(const JoinOne j0, const JoinOne j1, int k, int kp) {
+__global__ void __launch_bounds__(256)
+    k_adapter_join(const JoinOne j0, const JoinOne j1, int k, int kp, const int32_t* __restrict__ plan,
+                   const __grid_constant__ PlanLay pl) {
   wait_for_previous();
   launch_dependents();
+  const int all_slots = plan[pl.tile_base + pl.tiles];
   const int lane4 = threadIdx.x & 3;
   const int64_t groups = (j0.rows + j1.rows) * (kp / 4);
   for (int64_t b0 = int64_t(blockIdx.x) * 64; b0 < groups; b0 += int64_t(gridDim.x) * 64) {
@@ -1275,13 +1292,19 @@ __global__ void __launch_bounds__(256) k_adapter_join(const JoinOne j0, const Jo
     const JoinOne& j = flat < j0.rows ? j0 : j1;
     const int64_t row = flat < j0.rows ? flat : flat - j0.rows;
     float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+    const int64_t a = row / j.d;
     if (on) {
-      const float* p = j.part + row * kp + c;
-      const int64_t pitch = j.rows * kp;
+      const int s0 = plan[pl.ad_off + a], s1 = plan[pl.ad_off + a + 1];
+      if (s0 < s1) {  // the ranges that hold slots of this adapter
+        const int per = (all_slots + j.ranges - 1) / j.ranges;
+        const int r1 = (s1 - 1) / per;
+        const float* p = j.part + row * kp + c;  // number r + a: row is a d + channel
+        const int64_t pitch = j.d * kp;
 #pragma unroll 4
-      for (int r = lane4; r < j.ranges; r += 4) {
-        const float4 x = *reinterpret_cast<const float4*>(p + r * pitch);
-        v.x += x.x; v.y += x.y; v.z += x.z; v.w += x.w;
+        for (int r = s0 / per + lane4; r <= r1; r += 4) {
+          const float4 x = *reinterpret_cast<const float4*>(p + r * pitch);
+          v.x += x.x; v.y += x.y; v.z += x.z; v.w += x.w;
+        }
       }
     }
 #pragma unroll
@@ -1294,7 +1317,7 @@ __global__ void __launch_bounds__(256) k_adapter_join(const JoinOne j0, const Jo
     const int col = c + lane4;
     if (on && col < k) {
       float x = lane4 == 0 ? v.x : lane4 == 1 ? v.y : lane4 == 2 ? v.z : v.w;
-      if (j.scale) x *= j.scale[row / j.d];
+      if (j.scale) x *= j.scale[a];
       if constexpr (sizeof(T) == 4) static_cast<float*>(j.out)[row * k + col] = x;
       else static_cast<__nv_bfloat16*>(j.out)[row * k + col] = __float2bfloat16_rn(x);
     }
@@ -1317,14 +1340,22 @@ int tok_ranges(int64_t N, int64_t d) {
 
 struct AdapterWs {
   size_t u, t, part_in, part_out, total;
-  int ranges_in, ranges_out;
+  int ranges;
 };
-// Token ranges of dA / dB: enough items for two rounds of the SMs, at most one per token tile.
-int grad_ranges(int n, int64_t d, int64_t tiles) {
-  const int64_t items = int64_t(n) * ((d + 127) / 128);
-  int64_t r = (2 * int64_t(sm_count()) + items - 1) / items;
-  if (r > tiles) r = tiles;
-  return int(r < 1 ? 1 : r);
+// Ranges of the slots: whole rounds of the SMs over the items of both gradients (`ctiles` channel tiles in all),
+// against two slots' time to begin and end an item.
+int grad_ranges(int64_t ctiles, int64_t tiles) {
+  int best = 1;
+  int64_t best_c = 0;
+  for (int64_t r = 1; r <= 64 && r <= tiles; ++r) {
+    const int64_t rounds = (ctiles * r + sm_count() - 1) / sm_count();
+    const int64_t c = rounds * ((tiles + r - 1) / r + 2);
+    if (r == 1 || c < best_c) {
+      best = int(r);
+      best_c = c;
+    }
+  }
+  return best;
 }
 AdapterWs adapter_ws(int64_t N, int64_t d_in, int64_t d_out, int k, int n, bool backward) {
   AdapterWs w{};
@@ -1338,11 +1369,10 @@ AdapterWs adapter_ws(int64_t N, int64_t d_in, int64_t d_out, int k, int n, bool 
   w.u = at; at += need;
   if (backward) {
     w.t = at; at += need;
-    w.ranges_in = grad_ranges(n, d_in, p.tiles);
-    w.ranges_out = grad_ranges(n, d_out, p.tiles);
-    const size_t kp = size_t(k_padded(k));
-    w.part_in = at; at += align256(4 * size_t(w.ranges_in) * n * size_t(d_in) * kp);
-    w.part_out = at; at += align256(4 * size_t(w.ranges_out) * n * size_t(d_out) * kp);
+    w.ranges = grad_ranges((d_in + 127) / 128 + (d_out + 127) / 128, p.tiles);
+    const size_t parts = size_t(w.ranges) + size_t(n), kp = size_t(k_padded(k));
+    w.part_in = at; at += align256(4 * parts * size_t(d_in) * kp);
+    w.part_out = at; at += align256(4 * parts * size_t(d_out) * kp);
   }
   w.total = at;
   return w;
@@ -1555,7 +1585,7 @@ cudaError_t grad(const Call& c, const Grad* set, int sets, int parts, int dtype)
     g.one[i].d = v.d;
     g.one[i].ctiles = int((v.d + 127) / 128);
     g.one[i].ranges = v.ranges;
-    g.one[i].items = c.n * g.one[i].ctiles * v.ranges;
+    g.one[i].items = g.one[i].ctiles * v.ranges;
     g.one[i].part = v.part;
     g.items += g.one[i].items;
     j[i].part = v.part;
@@ -1585,7 +1615,7 @@ cudaError_t grad(const Call& c, const Grad* set, int sets, int parts, int dtype)
   if (e != cudaSuccess) return e;
   const unsigned jb = unsigned(groups / 64 + 1 < 16 * sm_count() ? groups / 64 + 1 : 16 * sm_count());
   return launch_cluster(dtype == LOCA_F32 ? k_adapter_join<float> : k_adapter_join<__nv_bfloat16>, dim3(jb), 256, 0, 1,
-                        c.s, j[0], j[1], c.k, c.kp);
+                        c.s, j[0], j[1], c.k, c.kp, c.plan, c.p);
 }
 
 Call call_of(int64_t N, int n, int k, const void* plan, void* workspace, int32_t* status, cudaStream_t s) {
@@ -1695,8 +1725,8 @@ cudaError_t launch_adapter_backward(const void* X, int64_t ldx, const void* dY, 
     e = project<true>(c, dY, lddy, d_out, W, d_in, pa, ws + w.t, false, dX, lddx);
     if (e != cudaSuccess) return e;
   }
-  const Grad ga{X, ldx, d_in, ws + w.t, w.ranges_in, reinterpret_cast<float*>(ws + w.part_in), nullptr, dA};
-  const Grad gb{dY, lddy, d_out, ws + w.u, w.ranges_out, reinterpret_cast<float*>(ws + w.part_out),
+  const Grad ga{X, ldx, d_in, ws + w.t, w.ranges, reinterpret_cast<float*>(ws + w.part_in), nullptr, dA};
+  const Grad gb{dY, lddy, d_out, ws + w.u, w.ranges, reinterpret_cast<float*>(ws + w.part_out),
                 reinterpret_cast<const float*>(pb + pk.scale), dB};
   Grad grads[2] = {ga, ga};
   int ng = 0;
