@@ -49,7 +49,7 @@ __host__ __device__ inline int k_padded(int k) { return (k + 15) / 16 * 16; }
 // Offsets in int32 from the start of the plan.
 struct PlanLay {
   int64_t tiles, pairs, smax;
-  int64_t tok_slot, tok_adapter, tile_base, adapter, tile, count, pair_count, pair_ad, pair_s0, pair_s1, ad_off, ad_slots, ad_tile, ad_count, ad_adapter, total;
+  int64_t tok_slot, tok_adapter, tile_base, adapter, tile, mask, pair_count, pair_ad, pair_s0, pair_s1, ad_off, ad_slots, ad_tile, ad_adapter, ad_mask, total;
 };
 PlanLay plan_lay(int64_t N, int n) {
   PlanLay p{};
@@ -68,7 +68,6 @@ PlanLay plan_lay(int64_t N, int n) {
   p.tile_base = take(p.tiles + 2);
   p.adapter = take(p.smax);
   p.tile = take(p.smax);
-  p.count = take(p.smax);
   p.pair_count = take(p.pairs);
   p.pair_ad = take(p.smax);
   p.pair_s0 = take(p.smax);
@@ -76,8 +75,9 @@ PlanLay plan_lay(int64_t N, int n) {
   p.ad_off = take(n + 1);
   p.ad_slots = take(p.smax);
   p.ad_tile = take(p.smax);
-  p.ad_count = take(p.smax);
   p.ad_adapter = take(p.smax);
+  p.mask = take(4 * p.smax);
+  p.ad_mask = take(4 * p.smax);
   p.total = at;
   return p;
 }
@@ -95,13 +95,16 @@ __global__ void __launch_bounds__(kTile) k_plan_tiles(const int32_t* __restrict_
   if (a >= n) a = -1;
   id[j] = a;
   __syncthreads();
-  int first = a >= 0 ? j : -1, members = 0;
+  int first = a >= 0 ? j : -1;
+  uint32_t rows[kTile / 32] = {};  // the tile's tokens with this token's adapter
   if (a >= 0)
-    for (int i = 0; i < kTile; ++i)
-      if (id[i] == a) {
-        if (i < first) first = i;
-        ++members;
-      }
+#pragma unroll
+    for (int w = 0; w < kTile / 32; ++w)
+      for (int i = 0; i < 32; ++i)
+        if (id[32 * w + i] == a) {
+          if (32 * w + i < first) first = 32 * w + i;
+          rows[w] |= 1u << i;
+        }
   const bool mine = first == j;
   const unsigned all = __ballot_sync(0xffffffffu, mine);
   if (lane == 0) warp_sum[warp] = __popc(all);
@@ -122,7 +125,7 @@ __global__ void __launch_bounds__(kTile) k_plan_tiles(const int32_t* __restrict_
     if (LOCA_CHECK(s, p.smax)) {
       plan[p.adapter + s] = a;
       plan[p.tile + s] = int32_t(tile);
-      plan[p.count + s] = members;
+      for (int w = 0; w < kTile / 32; ++w) plan[p.mask + 4 * int64_t(s) + w] = int32_t(rows[w]);
     }
   }
   __syncthreads();
@@ -232,7 +235,7 @@ __global__ void __launch_bounds__(256) k_plan_adapters(int32_t* plan, PlanLay p,
     if (mine && LOCA_CHECK(off, p.smax)) {
       plan[p.ad_slots + off] = s;
       plan[p.ad_tile + off] = plan[p.tile + s];
-      plan[p.ad_count + off] = plan[p.count + s];
+      for (int w = 0; w < kTile / 32; ++w) plan[p.ad_mask + 4 * int64_t(off) + w] = plan[p.mask + 4 * int64_t(s) + w];
       plan[p.ad_adapter + off] = a;
     }
     at += here;
@@ -492,7 +495,7 @@ __global__ void __launch_bounds__(kShrinkThreads, 1)
       // ---------------- sums of the segments and of the parts
       const int q = warp & 3;
       const int row = q * 32 + lane;
-      const bool mine = row0 + row < g.N && g.plan[g.p.tok_slot + row0 + row] == s;
+      const bool mine = uint32_t(g.plan[g.p.mask + 4 * int64_t(s) + q]) >> lane & 1u;
       const bool spoiled = g.marks[a] != 0;
       float u[64];
 #pragma unroll
@@ -1021,8 +1024,8 @@ __global__ void __launch_bounds__(kGradThreads, 1)
   if (threadIdx.x == 0) {
     for (int s = 0; s < kGradMaxStages; ++s) {
       mbar_init(full_bar(s), 1);
-      mbar_init(empty_bar(s), 1);
-      mbar_init(ready_bar(s), 1);
+      mbar_init(empty_bar(s), 2);  // the MMAs that read the stage, and the warp that zeroes rows
+      mbar_init(ready_bar(s), 1);  // stages of mixed slots only
     }
     for (uint32_t b = 0; b < 2; ++b) {
       mbar_init(acc_full(b), 1);
@@ -1061,6 +1064,11 @@ __global__ void __launch_bounds__(kGradThreads, 1)
     w.s0 = w.range * per < all_slots ? w.range * per : all_slots;
     w.s1 = w.s0 + per < all_slots ? w.s0 + per : all_slots;
     return w;
+  };
+  // place l's tokens among its tile's, and whether the tile also holds tokens of others
+  auto mask_of = [&](int l) { return *reinterpret_cast<const uint4*>(g.plan + g.p.ad_mask + 4 * int64_t(l)); };
+  auto is_mixed = [&](const uint4& m, int64_t row) {
+    return __popc(m.x) + __popc(m.y) + __popc(m.z) + __popc(m.w) < int(g.N - row < kTile ? g.N - row : kTile);
   };
   // end of the run of slots of one adapter that starts at place l
   auto run_end = [&](int l, const Item& w, int& a) {
@@ -1108,25 +1116,26 @@ __global__ void __launch_bounds__(kGradThreads, 1)
     }
     __syncwarp();
   } else if (warp == 6) {
-    // ---------------- rows of other tokens: zero
+    // ---------------- rows of other tokens: zero.  Every stage is waited for in turn (a phase must not
+    // pass unseen), but the MMAs wait for this warp only where there is something to zero
     int stage = 0;
     uint32_t phase = 0;
     bool ok = true;
     for (int it = blockIdx.x; it < items && ok; it += gridDim.x) {
       const Item w = item_of(it);
-      int s = 0, tile = 0, count = 0;
+      uint4 m = make_uint4(0, 0, 0, 0), m_next = m;
+      int tile = 0, tile_next = 0;
       if (w.s0 < w.s1) {
-        s = g.plan[g.p.ad_slots + w.s0];
-        tile = g.plan[g.p.ad_tile + w.s0];
-        count = g.plan[g.p.ad_count + w.s0];
+        m_next = mask_of(w.s0);
+        tile_next = g.plan[g.p.ad_tile + w.s0];
       }
       for (int l = w.s0; l < w.s1 && ok; ++l) {
+        m = m_next;
+        tile = tile_next;
         const int ln = l + 1 < w.s1 ? l + 1 : l;
-        const int s_next = g.plan[g.p.ad_slots + ln], tile_next = g.plan[g.p.ad_tile + ln];
-        const int count_next = g.plan[g.p.ad_count + ln];
-        const int64_t row = int64_t(tile) * kTile;
-        const int64_t in_tile = g.N - row < kTile ? g.N - row : kTile;
-        const bool mixed = count < in_tile;
+        m_next = mask_of(ln);
+        tile_next = g.plan[g.p.ad_tile + ln];
+        const bool mixed = is_mixed(m, int64_t(tile) * kTile);
         for (int h = 0; h < 2; ++h) {
           const bool got = mbar_try_wait(full_bar(stage), phase) || mbar_wait(full_bar(stage), phase, wc);
           if (!__all_sync(0xffffffffu, got)) {
@@ -1135,49 +1144,72 @@ __global__ void __launch_bounds__(kGradThreads, 1)
           }
           if (mixed) {
             uint8_t* box = smem + stage * stage_bytes;
-            for (int r = lane; r < 64; r += 32) {
-              const int64_t tok = row + 64 * h + r;
-              if (tok < g.N && g.plan[g.p.tok_slot + tok] != s) {
 #pragma unroll
-                for (int u = 0; u < 8; ++u) {
-                  *reinterpret_cast<uint4*>(box + r * 128 + u * 16) = make_uint4(0, 0, 0, 0);
-                  *reinterpret_cast<uint4*>(box + kXBytes / 2 + r * 128 + u * 16) = make_uint4(0, 0, 0, 0);
+            for (int r = 0; r < 2; ++r) {
+              const uint32_t rows = h == 0 ? (r == 0 ? m.x : m.y) : (r == 0 ? m.z : m.w);
+              if (!(rows >> lane & 1u)) {  // (rows past the last token are zero already)
+                uint8_t* to = box + (32 * r + lane) * 128;
+#pragma unroll
+                for (int u = 0; u < 8; ++u) {  // each lane begins at another 16 bytes: no bank conflicts
+                  *reinterpret_cast<uint4*>(to + ((u + lane) & 7) * 16) = make_uint4(0, 0, 0, 0);
+                  *reinterpret_cast<uint4*>(to + kXBytes / 2 + ((u + lane) & 7) * 16) = make_uint4(0, 0, 0, 0);
                 }
               }
             }
             fence_proxy_async_smem();
           }
           __syncwarp();
-          if (lane == 0) mbar_arrive(ready_bar(stage));
+          if (lane == 0) {
+            if (mixed) mbar_arrive(ready_bar(stage));
+            mbar_arrive(empty_bar(stage));
+          }
           if (++stage == stages) { stage = 0; phase ^= 1u; }
         }
-        s = s_next;
-        tile = tile_next;
-        count = count_next;
       }
     }
   } else if (warp == 1) {
     if (lane == 0) {
       int stage = 0;
-      uint32_t phase = 0, seg = 0;
+      uint32_t phase = 0, seg = 0, ready_phase = 0;  // bit s: parity of the next use of ready_bar(s)
       bool ok = true, issued = false;
       const uint32_t id = tc::idesc(1, 1, 1, 1, 128, uint32_t(g.kp * g.parts));
       for (int it = blockIdx.x; it < items && ok; it += gridDim.x) {
         const Item w = item_of(it);
         int end = w.s0, a = 0;
+        uint4 m_next = make_uint4(0, 0, 0, 0);
+        int tile_next = 0;
+        bool mixed = false;
+        if (w.s0 < w.s1) {
+          m_next = mask_of(w.s0);
+          tile_next = g.plan[g.p.ad_tile + w.s0];
+        }
         const int nb = 2 * (w.s1 - w.s0);
         for (int j = 0, in_seg = 0; j < nb; ++j) {
-          if (w.s0 + j / 2 == end) end = run_end(end, w, a);
+          const int l = w.s0 + j / 2;
+          if ((j & 1) == 0) {
+            if (l == end) end = run_end(end, w, a);
+            mixed = is_mixed(m_next, int64_t(tile_next) * kTile);
+            const int ln = l + 1 < w.s1 ? l + 1 : l;  // the next slot's entries are under way meanwhile
+            m_next = mask_of(ln);
+            tile_next = g.plan[g.p.ad_tile + ln];
+          }
           const uint32_t b = seg & 1u;
           if (in_seg == 0 && !mbar_try_wait(acc_empty(b), ((seg >> 1) & 1u) ^ 1u) &&
               !mbar_wait(acc_empty(b), ((seg >> 1) & 1u) ^ 1u, wc)) {
             ok = false;
             break;
           }
-          if ((!mbar_try_wait(full_bar(stage), phase) && !mbar_wait(full_bar(stage), phase, wc)) ||
-              (!mbar_try_wait(ready_bar(stage), phase) && !mbar_wait(ready_bar(stage), phase, wc))) {
+          if (!mbar_try_wait(full_bar(stage), phase) && !mbar_wait(full_bar(stage), phase, wc)) {
             ok = false;
             break;
+          }
+          if (mixed) {
+            const uint32_t par = ready_phase >> stage & 1u;
+            if (!mbar_try_wait(ready_bar(stage), par) && !mbar_wait(ready_bar(stage), par, wc)) {
+              ok = false;
+              break;
+            }
+            ready_phase ^= 1u << stage;
           }
           fence_after();
           const uint32_t st = smem_base + uint32_t(stage * stage_bytes);
