@@ -1578,7 +1578,7 @@ cudaError_t project(const Call& c, const void* X, int64_t ldx, int64_t d, const 
     return cudaErrorInvalidValue;
   gp::Geo g{};
   g.m_tiles = int((c.N + gp::TM - 1) / gp::TM);
-  g.n_tiles = int((o + gp::TN - 1) / gp::TN);
+  g.cols = int(o);
   g.nkb = int((d + gp::BK - 1) / gp::BK);
   g.splits = 1;
   g.seg_kb = 64;
@@ -1589,7 +1589,8 @@ cudaError_t project(const Call& c, const void* X, int64_t ldx, int64_t d, const 
   g.mark = c.mark;
   const AdapterExt ext{c.plan, c.p.tile_base, c.p.pair_count, c.p.pair_ad, c.p.pair_s0, c.p.pair_s1,
                        int(slots * kSlotRows), (c.k + 15) / 16};
-  return gp::launch<false, kWmn>(mx, mw, mu, mb, mo, g, EpiRows{}, ext, c.s);
+  return d <= gp::kWideK ? gp::launch<true, false, kWmn>(mx, mw, mu, mb, mo, g, EpiRows{}, ext, c.s)
+                         : gp::launch<false, false, kWmn>(mx, mw, mu, mb, mo, g, EpiRows{}, ext, c.s);
 }
 
 // dA from X and T, and / or dB from dY and U.

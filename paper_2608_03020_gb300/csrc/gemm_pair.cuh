@@ -5,19 +5,24 @@
 // by the adapter projection.  Each operand is K-major (k contiguous) or MN-major (m or n
 // contiguous); the tensor maps and the MMA descriptors carry the difference.
 //
-// Why this shape.  A pair of CTAs holds a 256 x 256 fp32 tile (128 rows per CTA: half of TMEM) and
-// loads 16 KB of A and 16 KB of B per CTA and 64-wide k-block, 64 bytes per tensor-core cycle and
-// SM, below the ~85 bytes per cycle the TMA ring takes from L2.  The other half of TMEM holds the
-// next tile, so the MMAs of a tile run while eight warps read the tile before it.
-//   warp 0       TMA producer (both CTAs): its CTA's 128 rows of A and 128 rows of B per k-block
+// Two shapes (kWide).  Narrow: a pair of CTAs holds a 256 x 256 fp32 tile (128 rows per CTA: half of
+// TMEM); the other half of TMEM takes the next tile while eight warps read this one.  Wide: 256 x 512,
+// two accumulators that share A, all of TMEM.  What bounds the narrow one is shared memory: per 64-wide
+// k-block and CTA the loads write 32 KB and the MMAs read 32 KB in the 512 cycles that the MMAs take,
+// 128 bytes per cycle, all that shared memory moves, and a k-block took 672 cycles (with a quarter of
+// the MMAs, about 450).  The wide one writes 48 KB for 1024 cycles of MMAs.  Its epilogue is not
+// hidden behind a second buffer, so the MMAs of the next tile's first four k-blocks go to the first
+// accumulator, which is read first, before any goes to the second.
+//   warp 0       TMA producer (both CTAs): its CTA's 128 rows of A and 128 rows of B per accumulator
 //   warp 1       one thread of the even CTA issues the MMAs (M = 256, N = 256, K = 16)
 //   warps 2..9   take the sums out of TMEM: warp w holds rows 32 (w & 3) .. + 31 of its CTA, one row
-//                per lane, and 128 of the 256 columns, in registers
-// Segments: the tensor cores' fp32 accumulation loses a fraction of an ulp of the running sum at
-// every step, always toward zero.  The sums restart every `seg_kb` k-blocks and the epilogue warps
-// add the segments in registers with round-to-nearest additions, which bounds that bias whatever K
-// is (a logit at K = 5120 comes out ~10x nearer to its 64-bit value than with one accumulator).
-// A segment is also the unit of the TMEM double buffer.
+//                per lane, and 128 of an accumulator's 256 columns, in registers
+// Segments (narrow only): the tensor cores' fp32 accumulation loses a fraction of an ulp of the running
+// sum at every step, always toward zero.  The sums restart every `seg_kb` k-blocks and the epilogue
+// warps add the segments in registers with round-to-nearest additions, which bounds that bias whatever
+// K is (a logit at K = 5120 comes out ~10x nearer to its 64-bit value than with one accumulator).  A
+// segment is also the unit of the TMEM double buffer.  The wide shape serves outputs in bf16 with K up
+// to kWideK, where the bias (below 2^-13 of a sum) disappears in the rounding.
 // Every wait is bounded; the failure path is that of the Gram kernel: the first waiter that gives up
 // records LOCA_ERR_TIMEOUT and raises the launch's abort flag, every role stops at its own point,
 // the even CTA settles the copies that only one CTA issued, MMAs and copies in flight land, TMEM is
@@ -36,26 +41,35 @@ namespace gp {
 using namespace tc;
 
 constexpr int TM = 256;               // tile rows per CTA pair
-constexpr int TN = 256;               // tile columns
+constexpr int TN = 256;               // columns of an accumulator
 constexpr int HALF = 128;             // rows of A, and of B, loaded per CTA
 constexpr int BK = 64;                // k per pipeline stage
-constexpr int STAGES = 6;
-constexpr int OPB = HALF * BK * 2;    // bytes of one operand of a stage (16 KB)
-constexpr int STAGE_BYTES = 2 * OPB;
+constexpr int OPB = HALF * BK * 2;    // 16 KB: 128 rows of an operand in one stage
 constexpr int SUB = 64 * BK * 2;      // one 64 x 64 swizzled box (8 KB)
 constexpr int EPI_WARPS = 8;
 constexpr int BOX = 4096;             // one epilogue warp's staging box: 32 rows x 128 bytes
 constexpr int THREADS = 64 + 32 * EPI_WARPS;
-constexpr int BARS = 2 * STAGES + 5;  // full[S], empty[S], acc_full[2], acc_empty[2], drain
-constexpr int SMEM = STAGES * STAGE_BYTES + EPI_WARPS * BOX + 256 + 1024;
+constexpr int64_t kWideK = 16384;
+template <bool kWide>
+struct Shape {
+  static constexpr int kAcc = kWide ? 2 : 1;       // accumulators of a tile
+  static constexpr int kCols = TN * kAcc;
+  static constexpr int kStages = kWide ? 4 : 6;
+  static constexpr int kStageBytes = (1 + kAcc) * OPB;
+  static constexpr int kBars = 2 * kStages + 5;    // full[S], empty[S], acc_full[2], acc_empty[2], drain
+};
+constexpr int SMEM = 12 * OPB + EPI_WARPS * BOX + 256 + 1024;
 static_assert(SMEM <= 232448, "shared memory per CTA");
-static_assert(BARS * 8 + 8 <= 256, "barrier area");
+static_assert(Shape<false>::kStages * Shape<false>::kStageBytes == 12 * OPB, "ring");
+static_assert(Shape<true>::kStages * Shape<true>::kStageBytes == 12 * OPB, "ring");
+static_assert(Shape<false>::kBars * 8 + 8 <= 256, "barrier area");
 
 // One launch's work.  Tiles are taken in groups of `group` row tiles that sweep all column tiles,
 // row tile fastest: the CTA pairs at work share a few column tiles and one group of row tiles,
 // which stay in L2.
 struct Geo {
-  int m_tiles, n_tiles;  // upper bounds (rows_live may lower m_tiles, k_live the k-blocks)
+  int m_tiles, n_tiles;  // upper bounds (rows_live may lower m_tiles, k_live the k-blocks); set by launch()
+  int cols;              // columns of the output
   int nkb;               // k-blocks of the product
   int splits;            // the k-blocks are cut into this many ranges, each a tile of its own
   int seg_kb;            // k-blocks per accumulation segment
@@ -70,7 +84,7 @@ struct Geo {
 };
 
 struct Tile {
-  int m, n, split;
+  int m, col0, split;
   int kb0, kb1;
 };
 
@@ -98,6 +112,7 @@ __device__ __forceinline__ Live live_of(const Geo& g) {
   return v;
 }
 
+template <int kCols>
 __device__ __forceinline__ Tile tile_of(const Geo& g, const Live& v, int it) {
   Tile t;
   const int per_split = v.m_tiles * g.n_tiles;
@@ -108,8 +123,9 @@ __device__ __forceinline__ Tile tile_of(const Geo& g, const Live& v, int it) {
   r -= gi * per_group;
   const int m0 = gi * g.group;
   const int gm = v.m_tiles - m0 < g.group ? v.m_tiles - m0 : g.group;
-  t.n = r / gm;
-  t.m = m0 + r - t.n * gm;
+  const int n = r / gm;
+  t.m = m0 + r - n * gm;
+  t.col0 = n * kCols;
   const int per = (v.nkb + g.splits - 1) / g.splits;
   t.kb0 = t.split * per < v.nkb ? t.split * per : v.nkb;
   t.kb1 = t.kb0 + per < v.nkb ? t.kb0 + per : v.nkb;
@@ -164,12 +180,14 @@ struct NoExt {
 //                                   uint8_t* box, const CUtensorMap* out) const
 // called once per finished tile by every epilogue thread, with the sums of row `row` (of the whole
 // operand A), columns col0 .. col0 + 127.
-template <bool kAmn, bool kBmn, class Epi, class Ext>
+template <bool kWide, bool kAmn, bool kBmn, class Epi, class Ext>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
     k_gemm_pair(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB,
                 const __grid_constant__ CUtensorMap tmAx, const __grid_constant__ CUtensorMap tmBx,
                 const __grid_constant__ CUtensorMap tmO, const __grid_constant__ Geo g,
                 const __grid_constant__ Epi epi, const __grid_constant__ Ext ext) {
+  using S = Shape<kWide>;
+  constexpr int STAGES = S::kStages, STAGE_BYTES = S::kStageBytes, BARS = S::kBars;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   uint8_t* boxes = smem + STAGES * STAGE_BYTES;
@@ -230,9 +248,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
       uint32_t iter = 0;
       bool ok = true;
       for (int it = cid; it < lv.total && ok; it += ncl) {
-        const Tile t = tile_of(g, lv, it);
+        const Tile t = tile_of<S::kCols>(g, lv, it);
         const int m0 = t.m * TM + int(rank) * HALF;
-        const int n0 = t.n * TN + int(rank) * HALF;
+        const int n0 = t.col0 + int(rank) * HALF;
         const int nx = Ext::kOn ? ext.entries(t.m) : 0;
         const int nb = t.kb1 - t.kb0;
         for (int j = 0; j < nb + nx; ++j) {
@@ -253,17 +271,21 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
             } else {
               tma_load_2d_pair(a, &tmA, fb, k0, m0);
             }
-            if (kBmn) {
-              tma_load_2d_pair(b, &tmB, fb, n0, k0);
-              tma_load_2d_pair(b + SUB, &tmB, fb, n0 + 64, k0);
-            } else {
-              tma_load_2d_pair(b, &tmB, fb, k0, n0);
+#pragma unroll
+            for (int c = 0; c < S::kAcc; ++c) {
+              if (kBmn) {
+                tma_load_2d_pair(b + c * OPB, &tmB, fb, n0 + c * TN, k0);
+                tma_load_2d_pair(b + c * OPB + SUB, &tmB, fb, n0 + c * TN + 64, k0);
+              } else {
+                tma_load_2d_pair(b + c * OPB, &tmB, fb, k0, n0 + c * TN);
+              }
             }
           } else {
             int a_row, block;
             ext.entry(t.m, j - nb, rank, a_row, block);
             tma_load_2d_pair(a, &tmAx, fb, 0, a_row);
-            tma_load_3d_pair(b, &tmBx, fb, 0, n0, block);
+#pragma unroll
+            for (int c = 0; c < S::kAcc; ++c) tma_load_3d_pair(b + c * OPB, &tmBx, fb, 0, n0 + c * TN, block);
           }
           ++iter;
           if (++stage == STAGES) { stage = 0; phase ^= 1u; }
@@ -287,42 +309,82 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
       constexpr uint64_t kAStep = kAmn ? 2048 >> 4 : 32 >> 4, kBStep = kBmn ? 2048 >> 4 : 32 >> 4;
       constexpr uint32_t kId = tc::idesc(1, 1, kAmn ? 1 : 0, kBmn ? 1 : 0, TM, TN);
       constexpr uint32_t kIdX = tc::idesc(1, 1, 0, 0, TM, TN);
+      // the MMAs of one k-block into accumulator c
+      auto block = [&](int s, uint32_t d, int c, bool from_ext, bool first) {
+        const uint64_t so = uint64_t(s) * uint64_t(STAGE_BYTES >> 4), bo = so + uint64_t(c) * uint64_t(OPB >> 4);
+        if (!Ext::kOn || !from_ext) {
+#pragma unroll
+          for (int kk = 0; kk < BK / 16; ++kk)
+            mma_f16_pair(d, a0 + so + kk * kAStep, b0 + bo + kk * kBStep, kId, !first || kk != 0 ? 1u : 0u);
+        } else {
+          for (int kk = 0; kk < ext.ksteps(); ++kk)
+            mma_f16_pair(d, a_kmaj + so + kk * 2, b_kmaj + bo + kk * 2, kIdX, !first || kk != 0 ? 1u : 0u);
+        }
+      };
+      auto wait_full = [&](int s, uint32_t ph) {
+        if (!mbar_try_wait_cluster(full_bar(s), ph) && !mbar_wait_cluster(full_bar(s), ph, wc)) return false;
+        fence_after();
+        return true;
+      };
+      auto wait_acc = [&](uint32_t b, uint32_t ph) {
+        if (!mbar_try_wait_cluster(acc_empty(b), ph) && !mbar_wait_cluster(acc_empty(b), ph, wc)) return false;
+        fence_after();
+        return true;
+      };
       for (int it = cid; it < lv.total && ok; it += ncl) {
-        const Tile t = tile_of(g, lv, it);
+        const Tile t = tile_of<S::kCols>(g, lv, it);
         const int nb = t.kb1 - t.kb0;
         const int all = nb + (Ext::kOn ? ext.entries(t.m) : 0);
-        uint32_t d = 0;
-        for (int j = 0, in_seg = 0; j < all; ++j) {
-          if (in_seg == 0) {
-            const uint32_t b = seg & 1u;
-            if (!mbar_try_wait_cluster(acc_empty(b), ((seg >> 1) & 1u) ^ 1u) &&
-                !mbar_wait_cluster(acc_empty(b), ((seg >> 1) & 1u) ^ 1u, wc)) {
-              ok = false;
-              break;
+        if constexpr (kWide) {
+          if (all == 0) continue;
+          const bool two = g.cols - t.col0 > TN;  // the second accumulator holds columns of the output
+          const int head = all < STAGES ? all : STAGES;
+          const int stage0 = stage;
+          ok = wait_acc(0, (seg & 1u) ^ 1u);
+          for (int j = 0; ok && j < head; ++j) {
+            if (!(ok = wait_full(stage, phase))) break;
+            block(stage, tmem_base, 0, j >= nb, j == 0);
+            issued = true;
+            if (++stage == STAGES) { stage = 0; phase ^= 1u; }
+          }
+          // (waited for without a second accumulator too: acc_full(1) must not complete twice unseen)
+          if (!ok || !(ok = wait_acc(1, (seg & 1u) ^ 1u))) break;
+          if (all == head) mma_commit_pair_mc(acc_full(0), 0x3);
+          for (int j = 0, s = stage0; j < head; ++j) {
+            if (two) block(s, tmem_base + uint32_t(TN), 1, j >= nb, j == 0);
+            mma_commit_pair_mc(empty_bar(s), 0x3);
+            if (++s == STAGES) s = 0;
+          }
+          for (int j = head; j < all; ++j) {
+            if (!(ok = wait_full(stage, phase))) break;
+            block(stage, tmem_base, 0, j >= nb, false);
+            if (j == all - 1) mma_commit_pair_mc(acc_full(0), 0x3);
+            if (two) block(stage, tmem_base + uint32_t(TN), 1, j >= nb, false);
+            mma_commit_pair_mc(empty_bar(stage), 0x3);
+            if (++stage == STAGES) { stage = 0; phase ^= 1u; }
+          }
+          if (!ok) break;
+          // (a tile without a second accumulator completes that barrier all the same: one phase a tile)
+          mma_commit_pair_mc(acc_full(1), 0x3);
+          ++seg;
+        } else {
+          uint32_t d = 0;
+          for (int j = 0, in_seg = 0; j < all; ++j) {
+            if (in_seg == 0) {
+              const uint32_t b = seg & 1u;
+              if (!(ok = wait_acc(b, ((seg >> 1) & 1u) ^ 1u))) break;
+              d = tmem_base + b * uint32_t(TN);
             }
-            d = tmem_base + b * uint32_t(TN);
-          }
-          if (!mbar_try_wait_cluster(full_bar(stage), phase) && !mbar_wait_cluster(full_bar(stage), phase, wc)) {
-            ok = false;
-            break;
-          }
-          fence_after();
-          const uint64_t so = uint64_t(stage) * uint64_t(STAGE_BYTES >> 4);
-          if (!Ext::kOn || j < nb) {
-#pragma unroll
-            for (int kk = 0; kk < BK / 16; ++kk)
-              mma_f16_pair(d, a0 + so + kk * kAStep, b0 + so + kk * kBStep, kId, (in_seg | kk) != 0 ? 1u : 0u);
-          } else {
-            for (int kk = 0; kk < ext.ksteps(); ++kk)
-              mma_f16_pair(d, a_kmaj + so + kk * 2, b_kmaj + so + kk * 2, kIdX, (in_seg | kk) != 0 ? 1u : 0u);
-          }
-          issued = true;
-          mma_commit_pair_mc(empty_bar(stage), 0x3);
-          if (++stage == STAGES) { stage = 0; phase ^= 1u; }
-          if (++in_seg == g.seg_kb || j == all - 1) {
-            mma_commit_pair_mc(acc_full(seg & 1u), 0x3);
-            ++seg;
-            in_seg = 0;
+            if (!(ok = wait_full(stage, phase))) break;
+            block(stage, d, 0, j >= nb, in_seg == 0);
+            issued = true;
+            mma_commit_pair_mc(empty_bar(stage), 0x3);
+            if (++stage == STAGES) { stage = 0; phase ^= 1u; }
+            if (++in_seg == g.seg_kb || j == all - 1) {
+              mma_commit_pair_mc(acc_full(seg & 1u), 0x3);
+              ++seg;
+              in_seg = 0;
+            }
           }
         }
       }
@@ -340,44 +402,77 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
     uint32_t seg = 0;
     bool go = true;
     for (int it = cid; it < lv.total && go; it += ncl) {
-      const Tile t = tile_of(g, lv, it);
+      const Tile t = tile_of<S::kCols>(g, lv, it);
       const int all = t.kb1 - t.kb0 + (Ext::kOn ? ext.entries(t.m) : 0);
-      const int nseg = (all + g.seg_kb - 1) / g.seg_kb;
-      float v[128];
-      if (nseg == 0) {
-#pragma unroll
-        for (int i = 0; i < 128; ++i) v[i] = 0.f;
-      }
-      for (int s = 0; s < nseg; ++s, ++seg) {
-        const uint32_t b = seg & 1u;
-        const bool ok = mbar_wait_cluster(acc_full(b), (seg >> 1) & 1u, wc);
-        if (!__all_sync(0xffffffffu, ok)) {
-          go = false;
-          break;
-        }
-        fence_after();
-        const uint32_t ta = tmem_base + (uint32_t(q * 32) << 16) + b * uint32_t(TN) + uint32_t(h * 128);
-        if (s == 0) {
+      const int row = t.m * TM + int(rank) * HALF + q * 32 + lane;
+      if constexpr (kWide) {
+#pragma unroll 1
+        for (uint32_t a = 0; a < 2; ++a) {
+          const int col0 = t.col0 + int(a) * TN + h * HALF;
+          if (all > 0) {
+            const bool ok = mbar_wait_cluster(acc_full(a), seg & 1u, wc);
+            if (!__all_sync(0xffffffffu, ok)) {
+              go = false;
+              break;
+            }
+          }
+          fence_after();
+          const uint32_t ta = tmem_base + (uint32_t(q * 32) << 16) + a * uint32_t(TN) + uint32_t(h * HALF);
+          float v[128];
 #pragma unroll
           for (int c = 0; c < 4; ++c) tmem_ld32(ta + c * 32, v + c * 32);
-        } else {
+          fence_before();
+          __syncwarp();
+          if (lane == 0 && all > 0) {
+            if (leader) mbar_arrive(acc_empty(a));
+            else mbar_arrive_remote(mapa_shared(acc_empty(a), 0));
+          }
+          if (all == 0) {  // no k: the sums are zero
 #pragma unroll
-          for (int c = 0; c < 4; ++c) {
-            float u[32];
-            tmem_ld32(ta + c * 32, u);
+            for (int i = 0; i < 128; ++i) v[i] = 0.f;
+          }
+          if (col0 < g.cols) epi(t, v, row, col0, lane, box, &tmO);
+        }
+        if (!go) break;
+        if (all > 0) ++seg;
+      } else {
+        const int nseg = (all + g.seg_kb - 1) / g.seg_kb;
+        float v[128];
+        if (nseg == 0) {
 #pragma unroll
-            for (int i = 0; i < 32; ++i) v[c * 32 + i] += u[i];
+          for (int i = 0; i < 128; ++i) v[i] = 0.f;
+        }
+        for (int s = 0; s < nseg; ++s, ++seg) {
+          const uint32_t b = seg & 1u;
+          const bool ok = mbar_wait_cluster(acc_full(b), (seg >> 1) & 1u, wc);
+          if (!__all_sync(0xffffffffu, ok)) {
+            go = false;
+            break;
+          }
+          fence_after();
+          const uint32_t ta = tmem_base + (uint32_t(q * 32) << 16) + b * uint32_t(TN) + uint32_t(h * HALF);
+          if (s == 0) {
+#pragma unroll
+            for (int c = 0; c < 4; ++c) tmem_ld32(ta + c * 32, v + c * 32);
+          } else {
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+              float u[32];
+              tmem_ld32(ta + c * 32, u);
+#pragma unroll
+              for (int i = 0; i < 32; ++i) v[c * 32 + i] += u[i];
+            }
+          }
+          fence_before();
+          __syncwarp();
+          if (lane == 0) {
+            if (leader) mbar_arrive(acc_empty(b));
+            else mbar_arrive_remote(mapa_shared(acc_empty(b), 0));
           }
         }
-        fence_before();
-        __syncwarp();
-        if (lane == 0) {
-          if (leader) mbar_arrive(acc_empty(b));
-          else mbar_arrive_remote(mapa_shared(acc_empty(b), 0));
-        }
+        if (!go) break;
+        epi(t, v, row, t.col0 + h * HALF, lane, box, &tmO);
       }
-      if (!go) break;
-      epi(t, v, t.m * TM + int(rank) * HALF + q * 32 + lane, t.n * TN + h * 128, lane, box, &tmO);
     }
     if (lane == 0) bulk_wait_group0();  // every box written before the CTA can leave
     __syncwarp();
@@ -495,10 +590,11 @@ inline cudaError_t launch_early(void (*kernel)(P...), dim3 grid, dim3 block, siz
   return cudaLaunchKernelEx(&cfg, kernel, args...);
 }
 
-template <bool kAmn, bool kBmn, class Epi, class Ext>
+template <bool kWide, bool kAmn, bool kBmn, class Epi, class Ext>
 inline cudaError_t launch(const CUtensorMap& a, const CUtensorMap& b, const CUtensorMap& ax, const CUtensorMap& bx,
-                          const CUtensorMap& o, const Geo& g, const Epi& epi, const Ext& ext, cudaStream_t s) {
-  auto kernel = k_gemm_pair<kAmn, kBmn, Epi, Ext>;
+                          const CUtensorMap& o, Geo g, const Epi& epi, const Ext& ext, cudaStream_t s) {
+  auto kernel = k_gemm_pair<kWide, kAmn, kBmn, Epi, Ext>;
+  g.n_tiles = (g.cols + Shape<kWide>::kCols - 1) / Shape<kWide>::kCols;
   cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM);
   if (e != cudaSuccess) return e;
   static const int pairs = resident_pairs(kernel);

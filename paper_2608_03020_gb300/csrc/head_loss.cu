@@ -463,10 +463,10 @@ BwdWs bwd_ws(int64_t N, int64_t V, int64_t d, bool dh, bool dw) {
   return o;
 }
 
-gp::Geo geo(int64_t m_tiles, int64_t n_tiles, int64_t nkb, int seg_kb, const Rows& r, int32_t* status) {
+gp::Geo geo(int64_t m_tiles, int64_t cols, int64_t nkb, int seg_kb, const Rows& r, int32_t* status) {
   gp::Geo g{};
   g.m_tiles = int(m_tiles);
-  g.n_tiles = int(n_tiles);
+  g.cols = int(cols);
   g.nkb = int(nkb);
   g.splits = 1;
   g.seg_kb = seg_kb;
@@ -513,11 +513,11 @@ cudaError_t launch_head_loss(const void* H, int64_t ldh, int64_t N, int64_t d, c
     const int64_t rows = np - p0 < lay.piece ? np - p0 : lay.piece;
     CUtensorMap ma;
     if (!gp::map_kmajor(&ma, r.H + p0 * d, d, rows, d)) return cudaErrorInvalidValue;
-    gp::Geo g = geo(rows / gp::TM, vt, (d + gp::BK - 1) / gp::BK, kSegKb, r, status);
+    gp::Geo g = geo(rows / gp::TM, V, (d + gp::BK - 1) / gp::BK, kSegKb, r, status);
     g.rows_live = r.count;
     g.m_first = int(p0 / gp::TM);
     EpiStats epi{part, lay.piece, r.y + p0, zy, cols, E ? C : 0, zc, V};
-    e = gp::launch<false, false>(ma, mb, ma, mb, ma, g, epi, gp::NoExt{}, s);
+    e = gp::launch<false, false, false>(ma, mb, ma, mb, ma, g, epi, gp::NoExt{}, s);
     if (e != cudaSuccess) return e;
     e = gp::launch_early(k_head_join, dim3(unsigned(rows / 32)), dim3(32, 2 * vt >= 128 ? 32 : 8), 0, s, part, lay.piece,
                          int(2 * vt), r, p0, zy, zc, cols, C, loss, lse, E);
@@ -536,7 +536,6 @@ cudaError_t launch_head_loss_backward(const void* H, int64_t ldh, int64_t N, int
   cudaError_t e = launch_rows(H, ldh, N, d, V, y, w, dloss, lse, r, nullptr, nullptr, nullptr, 0, dH, lddh, s);
   if (e != cudaSuccess) return e;
   const int64_t np = round_up(N < 1 ? 1 : N, gp::TM);
-  const int64_t dt = (d + gp::TN - 1) / gp::TN;
   const __nv_bfloat16* Wb = static_cast<const __nv_bfloat16*>(W);
   void* dz = ws + lay.dz;
   float* part = reinterpret_cast<float*>(ws + lay.part);
@@ -549,11 +548,12 @@ cudaError_t launch_head_loss_backward(const void* H, int64_t ldh, int64_t N, int
       if (!gp::map_kmajor(&mh, r.H + p0 * d, d, rows, d) || !gp::map_kmajor(&mw, Wb + v0 * d, d, vn, d) ||
           !gp::map_out_bf16(&mz_out, dz, lay.vc, lay.piece, lay.vc))
         return cudaErrorInvalidValue;
-      gp::Geo g = geo(rows / gp::TM, vtiles, (d + gp::BK - 1) / gp::BK, kSegKb, r, status);
+      gp::Geo g = geo(rows / gp::TM, vn, (d + gp::BK - 1) / gp::BK, kSegKb, r, status);
       g.rows_live = r.count;
       g.m_first = int(p0 / gp::TM);
-      e = gp::launch<false, false>(mh, mw, mh, mw, mz_out, g,
-                                   EpiDz{r.lse + p0, r.w + p0, r.y + p0, r.count, p0, v0, V}, gp::NoExt{}, s);
+      const EpiDz dz_epi{r.lse + p0, r.w + p0, r.y + p0, r.count, p0, v0, V};
+      e = d <= gp::kWideK ? gp::launch<true, false, false>(mh, mw, mh, mw, mz_out, g, dz_epi, gp::NoExt{}, s)
+                          : gp::launch<false, false, false>(mh, mw, mh, mw, mz_out, g, dz_epi, gp::NoExt{}, s);
       if (e != cudaSuccess) return e;
       if (dH) {
         CUtensorMap mo;
@@ -561,11 +561,14 @@ cudaError_t launch_head_loss_backward(const void* H, int64_t ldh, int64_t N, int
             !gp::map_3d(&mo, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 4, part, d, lay.piece, lay.splits, d, lay.piece * d, 32,
                         32))
           return cudaErrorInvalidValue;
-        gp::Geo gh = geo(rows / gp::TM, dt, (vn + gp::BK - 1) / gp::BK, kSegKbGrad, r, status);
+        gp::Geo gh = geo(rows / gp::TM, d, (vn + gp::BK - 1) / gp::BK, kSegKbGrad, r, status);
         gh.rows_live = r.count;
         gh.m_first = g.m_first;
         gh.splits = lay.splits;
-        e = gp::launch<false, true>(mz_k, mw_mn, mz_k, mw_mn, mo, gh, EpiAcc{lay.piece, v0 > 0 ? 1 : 0}, gp::NoExt{}, s);
+        const EpiAcc acc{lay.piece, v0 > 0 ? 1 : 0};
+        e = vn <= gp::kWideK * lay.splits
+                ? gp::launch<true, false, true>(mz_k, mw_mn, mz_k, mw_mn, mo, gh, acc, gp::NoExt{}, s)
+                : gp::launch<false, false, true>(mz_k, mw_mn, mz_k, mw_mn, mo, gh, acc, gp::NoExt{}, s);
         if (e != cudaSuccess) return e;
       }
       if (dW) {
@@ -574,9 +577,11 @@ cudaError_t launch_head_loss_backward(const void* H, int64_t ldh, int64_t N, int
         if (!gp::map_mnmajor(&mz_mn, dz, lay.vc, lay.piece, lay.vc) || !gp::map_mnmajor(&mh_mn, r.H, d, np, d) ||
             !gp::map_out_bf16(&mo, o, d, vn, d))
           return cudaErrorInvalidValue;
-        gp::Geo gw = geo(vtiles, dt, np / gp::BK, kSegKbGrad, r, status);
+        gp::Geo gw = geo(vtiles, d, np / gp::BK, kSegKbGrad, r, status);
         gw.k_live = r.count;
-        e = gp::launch<true, true>(mz_mn, mh_mn, mz_mn, mh_mn, mo, gw, EpiScaled{scale}, gp::NoExt{}, s);
+        e = np <= gp::kWideK
+                ? gp::launch<true, true, true>(mz_mn, mh_mn, mz_mn, mh_mn, mo, gw, EpiScaled{scale}, gp::NoExt{}, s)
+                : gp::launch<false, true, true>(mz_mn, mh_mn, mz_mn, mh_mn, mo, gw, EpiScaled{scale}, gp::NoExt{}, s);
         if (e != cudaSuccess) return e;
       }
     }
