@@ -575,7 +575,7 @@ int loca_adapter_backward(const void* X, int64_t ldx, const void* dY, int64_t ld
  * max_norm  > 0; infinity gives the norm alone
  * norm   one float, device memory: the norm before clipping.  A norm that is not finite says so here;
  *        f is then 0 (infinite norm) or 1 (NaN), and the caller should skip the step
- * Pointers need the alignment of their elements; n <= 100000.  Sums in fp32 over at most 64 squares
+ * Pointers need the alignment of their elements; n <= 100000.  Sums in fp32 over at most 34 squares
  * and in fp64 above, no overflow below the square root of fp64's range.  Deterministic.  The host
  * arrays are read before the call returns.
  */

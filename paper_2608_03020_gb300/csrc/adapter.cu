@@ -959,12 +959,10 @@ struct AdapterExt {
 };
 
 struct EpiRows {
-  __device__ __forceinline__ void operator()(const gp::Tile&, float (&v)[128], int row, int col0, int lane, uint8_t* box,
-                                             const CUtensorMap* out) const {
-#pragma unroll
-    for (int b = 0; b < 2; ++b)
-      gp::store_box_bf16(box, out, lane, col0 + 64 * b, row - lane, [&](int i) { return v[64 * b + i]; });
-  }
+  static constexpr bool kPacks = true;
+  struct Row {};
+  __device__ __forceinline__ Row row_of(int) const { return Row{}; }
+  __device__ __forceinline__ float value(const Row&, int, float v) const { return v; }
 };
 
 // ------------------------------------------------------------------ dA and dB: channels x k sums over tokens
@@ -1589,8 +1587,7 @@ cudaError_t project(const Call& c, const void* X, int64_t ldx, int64_t d, const 
   g.mark = c.mark;
   const AdapterExt ext{c.plan, c.p.tile_base, c.p.pair_count, c.p.pair_ad, c.p.pair_s0, c.p.pair_s1,
                        int(slots * kSlotRows), (c.k + 15) / 16};
-  return d <= gp::kWideK ? gp::launch<true, false, kWmn>(mx, mw, mu, mb, mo, g, EpiRows{}, ext, c.s)
-                         : gp::launch<false, false, kWmn>(mx, mw, mu, mb, mo, g, EpiRows{}, ext, c.s);
+  return gp::launch_either<false, kWmn>(mx, mw, mu, mb, mo, g, EpiRows{}, ext, c.s);
 }
 
 // dA from X and T, and / or dB from dY and U.

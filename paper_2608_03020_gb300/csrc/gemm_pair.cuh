@@ -142,22 +142,16 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
   return *reinterpret_cast<const uint32_t*>(&p);
 }
 
-// Hands a warp's 32 rows x 64 bf16 columns (thread `lane` holds its row's values f(i), i < 64) to the
-// TMA unit as one box of a 2-D map at (c0, r0).  The box buffer's previous contents have been read
-// before it is written again.
-template <class F>
-__device__ __forceinline__ void store_box_bf16(uint8_t* box, const CUtensorMap* map, int lane, int c0, int r0, F&& f) {
+// Hands a warp's 32 rows x 64 bf16 columns (thread `lane` holds its row's 32 pairs) to the TMA unit as
+// one box of a 2-D map at (c0, r0).  The box buffer's previous contents have been read before it is
+// written again.
+__device__ __forceinline__ void store_box_bf16(uint8_t* box, const CUtensorMap* map, int lane, int c0, int r0,
+                                               const uint32_t* w) {
   if (lane == 0) bulk_wait_group_read0();
   __syncwarp();
 #pragma unroll
-  for (int u = 0; u < 8; ++u) {
-    uint4 q;
-    q.x = pack_bf16(f(8 * u), f(8 * u + 1));
-    q.y = pack_bf16(f(8 * u + 2), f(8 * u + 3));
-    q.z = pack_bf16(f(8 * u + 4), f(8 * u + 5));
-    q.w = pack_bf16(f(8 * u + 6), f(8 * u + 7));
-    *reinterpret_cast<uint4*>(box + box_off(lane, u)) = q;
-  }
+  for (int u = 0; u < 8; ++u)
+    *reinterpret_cast<uint4*>(box + box_off(lane, u)) = make_uint4(w[4 * u], w[4 * u + 1], w[4 * u + 2], w[4 * u + 3]);
   fence_proxy_async_smem();
   __syncwarp();
   if (lane == 0) {
@@ -176,10 +170,12 @@ struct NoExt {
   __device__ void entry(int, int, uint32_t, int&, int&) const {}
 };
 
-// Epi: struct with  void operator()(const Tile&, float (&v)[128], int row, int col0, int lane,
+// What becomes of a finished tile.  An output in bf16 is given value by value (kPacks): Row row_of(row)
+// reads what a row needs, before its sums are complete; value(Row, column, sum) is the output.  Other
+// uses take the sums themselves:  void operator()(const Tile&, float (&v)[128], int row, int col0, int lane,
 //                                   uint8_t* box, const CUtensorMap* out) const
-// called once per finished tile by every epilogue thread, with the sums of row `row` (of the whole
-// operand A), columns col0 .. col0 + 127.
+// called once per finished accumulator by every epilogue thread, with the sums of row `row`, columns
+// col0 .. col0 + 127.
 template <bool kWide, bool kAmn, bool kBmn, class Epi, class Ext>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
     k_gemm_pair(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB,
@@ -405,32 +401,64 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
       const Tile t = tile_of<S::kCols>(g, lv, it);
       const int all = t.kb1 - t.kb0 + (Ext::kOn ? ext.entries(t.m) : 0);
       const int row = t.m * TM + int(rank) * HALF + q * 32 + lane;
-      if constexpr (kWide) {
+      auto wait_sums = [&](uint32_t b, uint32_t par) {
+        const bool ok = mbar_wait_cluster(acc_full(b), par, wc);
+        const bool every = __all_sync(0xffffffffu, ok);
+        fence_after();
+        return every;
+      };
+      auto release = [&](uint32_t b) {  // this warp has read the accumulator
+        fence_before();
+        __syncwarp();
+        if (lane == 0) {
+          if (leader) mbar_arrive(acc_empty(b));
+          else mbar_arrive_remote(mapa_shared(acc_empty(b), 0));
+        }
+      };
+      const int r0 = row - lane;
+      if constexpr (kWide && Epi::kPacks) {
+        // both accumulators are in registers, rounded and packed, before the stores that the MMAs need
+        // not wait for: 64 words of the first, of which a box (32) leaves before the second is read
+        const auto pre = epi.row_of(row);
+        const int col0 = t.col0 + h * HALF, col1 = col0 + TN;
+        const uint32_t ta = tmem_base + (uint32_t(q * 32) << 16) + uint32_t(h * HALF);
+        auto take = [&](uint32_t a, int col, uint32_t* w) {
+#pragma unroll
+          for (int c = 0; c < 4; ++c) {
+            float v[32];
+            tmem_ld32(ta + a * uint32_t(TN) + c * 32, v);
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+              w[c * 16 + i] = pack_bf16(epi.value(pre, col + c * 32 + 2 * i, all > 0 ? v[2 * i] : 0.f),
+                                        epi.value(pre, col + c * 32 + 2 * i + 1, all > 0 ? v[2 * i + 1] : 0.f));
+          }
+        };
+        uint32_t w0[64], w1[64];
+        if (all > 0 && !(go = wait_sums(0, seg & 1u))) break;
+        take(0, col0, w0);
+        if (all > 0) release(0);
+        if (col0 < g.cols) store_box_bf16(box, &tmO, lane, col0, r0, w0);
+        if (all > 0 && !(go = wait_sums(1, seg & 1u))) break;
+        take(1, col1, w1);
+        if (all > 0) release(1);
+        if (col0 + 64 < g.cols) store_box_bf16(box, &tmO, lane, col0 + 64, r0, w0 + 32);
+        if (col1 < g.cols) store_box_bf16(box, &tmO, lane, col1, r0, w1);
+        if (col1 + 64 < g.cols) store_box_bf16(box, &tmO, lane, col1 + 64, r0, w1 + 32);
+        if (all > 0) ++seg;
+      } else if constexpr (kWide) {
 #pragma unroll 1
         for (uint32_t a = 0; a < 2; ++a) {
-          const int col0 = t.col0 + int(a) * TN + h * HALF;
-          if (all > 0) {
-            const bool ok = mbar_wait_cluster(acc_full(a), seg & 1u, wc);
-            if (!__all_sync(0xffffffffu, ok)) {
-              go = false;
-              break;
-            }
-          }
-          fence_after();
+          if (all > 0 && !(go = wait_sums(a, seg & 1u))) break;
           const uint32_t ta = tmem_base + (uint32_t(q * 32) << 16) + a * uint32_t(TN) + uint32_t(h * HALF);
           float v[128];
 #pragma unroll
           for (int c = 0; c < 4; ++c) tmem_ld32(ta + c * 32, v + c * 32);
-          fence_before();
-          __syncwarp();
-          if (lane == 0 && all > 0) {
-            if (leader) mbar_arrive(acc_empty(a));
-            else mbar_arrive_remote(mapa_shared(acc_empty(a), 0));
-          }
+          if (all > 0) release(a);
           if (all == 0) {  // no k: the sums are zero
 #pragma unroll
             for (int i = 0; i < 128; ++i) v[i] = 0.f;
           }
+          const int col0 = t.col0 + int(a) * TN + h * HALF;
           if (col0 < g.cols) epi(t, v, row, col0, lane, box, &tmO);
         }
         if (!go) break;
@@ -444,12 +472,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
         }
         for (int s = 0; s < nseg; ++s, ++seg) {
           const uint32_t b = seg & 1u;
-          const bool ok = mbar_wait_cluster(acc_full(b), (seg >> 1) & 1u, wc);
-          if (!__all_sync(0xffffffffu, ok)) {
-            go = false;
-            break;
-          }
-          fence_after();
+          if (!(go = wait_sums(b, (seg >> 1) & 1u))) break;
           const uint32_t ta = tmem_base + (uint32_t(q * 32) << 16) + b * uint32_t(TN) + uint32_t(h * HALF);
           if (s == 0) {
 #pragma unroll
@@ -463,15 +486,24 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
               for (int i = 0; i < 32; ++i) v[c * 32 + i] += u[i];
             }
           }
-          fence_before();
-          __syncwarp();
-          if (lane == 0) {
-            if (leader) mbar_arrive(acc_empty(b));
-            else mbar_arrive_remote(mapa_shared(acc_empty(b), 0));
-          }
+          release(b);
         }
         if (!go) break;
-        epi(t, v, row, t.col0 + h * HALF, lane, box, &tmO);
+        const int col0 = t.col0 + h * HALF;
+        if constexpr (Epi::kPacks) {
+          const auto pre = epi.row_of(row);
+#pragma unroll
+          for (int b = 0; b < 2; ++b) {
+            uint32_t w[32];
+#pragma unroll
+            for (int i = 0; i < 32; ++i)
+              w[i] = pack_bf16(epi.value(pre, col0 + 64 * b + 2 * i, v[64 * b + 2 * i]),
+                               epi.value(pre, col0 + 64 * b + 2 * i + 1, v[64 * b + 2 * i + 1]));
+            if (col0 + 64 * b < g.cols) store_box_bf16(box, &tmO, lane, col0 + 64 * b, r0, w);
+          }
+        } else {
+          epi(t, v, row, col0, lane, box, &tmO);
+        }
       }
     }
     if (lane == 0) bulk_wait_group0();  // every box written before the CTA can leave
@@ -590,6 +622,21 @@ inline cudaError_t launch_early(void (*kernel)(P...), dim3 grid, dim3 block, siz
   return cudaLaunchKernelEx(&cfg, kernel, args...);
 }
 
+// Which shape: rounds of the pairs times a tile's cycles.  Measured on 1024 x 19456 outputs (4 narrow, 2
+// wide rounds) at k = 512 .. 8192: narrow 672 cycles a k-block and 3000 a tile, wide 1030 and 9000 (both
+// with a share of the launch and of the last tiles' stores); at k = 8192 204 and 170 us (1.60 and 1.92
+// PFLOP/s), at k = 512 25 us each.
+inline double cycles(bool wide, int64_t m_tiles, int64_t cols, int64_t nkb, int splits) {
+  const int64_t pairs = sm_count() / 2;
+  const int64_t n = wide ? (cols + 2 * TN - 1) / (2 * TN) : (cols + TN - 1) / TN;
+  const double rounds = double((m_tiles * n * splits + pairs - 1) / pairs);
+  const double kb = double((nkb + splits - 1) / splits);
+  return rounds * (wide ? 1030.0 * kb + 9000.0 : 672.0 * kb + 3000.0);
+}
+inline bool prefer_wide(int64_t m_tiles, int64_t cols, int64_t nkb, int splits) {
+  return nkb <= kWideK / BK * splits && cycles(true, m_tiles, cols, nkb, splits) < cycles(false, m_tiles, cols, nkb, splits);
+}
+
 template <bool kWide, bool kAmn, bool kBmn, class Epi, class Ext>
 inline cudaError_t launch(const CUtensorMap& a, const CUtensorMap& b, const CUtensorMap& ax, const CUtensorMap& bx,
                           const CUtensorMap& o, Geo g, const Epi& epi, const Ext& ext, cudaStream_t s) {
@@ -602,6 +649,15 @@ inline cudaError_t launch(const CUtensorMap& a, const CUtensorMap& b, const CUte
   if (total < 1) return cudaSuccess;
   const int n = total < pairs ? int(total) : pairs;
   return launch_early(kernel, dim3(unsigned(2 * n)), dim3(THREADS), SMEM, s, a, b, ax, bx, o, g, epi, ext);
+}
+
+// The shape that prefer_wide() names.
+template <bool kAmn, bool kBmn, class Epi, class Ext>
+inline cudaError_t launch_either(const CUtensorMap& a, const CUtensorMap& b, const CUtensorMap& ax, const CUtensorMap& bx,
+                                 const CUtensorMap& o, const Geo& g, const Epi& epi, const Ext& ext, cudaStream_t s) {
+  return prefer_wide(g.m_tiles, g.cols, g.nkb, g.splits)
+             ? launch<true, kAmn, kBmn, Epi, Ext>(a, b, ax, bx, o, g, epi, ext, s)
+             : launch<false, kAmn, kBmn, Epi, Ext>(a, b, ax, bx, o, g, epi, ext, s);
 }
 
 }  // namespace gp

@@ -2,11 +2,11 @@
 //   norm = sqrt(sum_t sum_i g_t[i]^2),  out_t = f g_t,  f = max_norm / norm if norm > max_norm, else 1
 //
 // Two launches per up to kMany tensors, whatever their number and sizes: the list of tensors travels
-// in the kernel's parameters, cut into chunks of kChunk elements that the blocks take in turn.
-//   k_clip_sumsq   squares summed in fp32 over the (at most kChunk / 256) elements of a thread and chunk,
-//                  everything above in fp64, in a fixed order; a thread whose fp32 sum leaves the range
-//                  in which it is exact enough (overflow, squares near the smallest normal) sums its
-//                  elements again in fp64
+// in the kernel's parameters, cut into chunks of kChunk elements that the blocks take in turn, each
+// thread with its part of a chunk in registers before it uses the first of it.
+//   k_clip_sumsq   squares summed in fp32 over the (at most 34) elements of a thread and chunk, everything
+//                  above in fp64, in a fixed order; a thread whose fp32 sum leaves the range in which it
+//                  is exact enough (overflow, squares near the smallest normal) sums them again in fp64
 //   k_clip_scale   every block adds the partial sums in the same order and scales its chunks, the last
 //                  ones first: they are the ones still in L2.  In place with f = 1 nothing is written
 // Bound: HBM, one read for the norm, and the second read (as far as L2 does not hold it) and one write
@@ -24,6 +24,7 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kChunk = 8192;
+constexpr int kSumBlocks = 4, kScaleBlocks = 6;  // resident blocks per SM
 constexpr int kFew = 64;     // tensors of one launch: a small list keeps the launch short
 constexpr int kMany = 1000;  // 24 KB of parameters
 
@@ -63,32 +64,52 @@ __device__ __forceinline__ Chunk chunk_of(const List<kCap>& l, int c) {
 __device__ __forceinline__ float to_f(float x) { return x; }
 __device__ __forceinline__ float to_f(__nv_bfloat16 x) { return __bfloat162float(x); }
 
-// f(value) over this thread's share of a chunk: 16-byte vectors where the address allows, single
-// elements at the two ends.
-template <class T, class F>
-__device__ __forceinline__ void each(const T* p, int count, F&& f) {
-  constexpr int kVec = 16 / sizeof(T);
-  int head = int((16 - (reinterpret_cast<uintptr_t>(p) & 15)) & 15) / int(sizeof(T));
-  if (head > count) head = count;
-  const int vecs = (count - head) / kVec;
-  for (int i = threadIdx.x; i < head; i += kThreads) f(to_f(p[i]));
-#pragma unroll 4
-  for (int i = threadIdx.x; i < vecs; i += kThreads) {
-    const uint4 q = __ldg(reinterpret_cast<const uint4*>(p + head) + i);
-    const T* v = reinterpret_cast<const T*>(&q);
+// This thread's share of a chunk: 16-byte vectors, all loaded before the first is used, and the single
+// elements before and behind them.
+template <class T>
+struct Share {
+  static constexpr int kVec = 16 / sizeof(T);
+  static constexpr int kIter = kChunk / (kVec * kThreads);
+  const T* p;
+  int count, head, vecs;
+  uint4 q[kIter];
+
+  __device__ __forceinline__ Share(const T* p_, int count_) : p(p_), count(count_) {
+    head = int((16 - (reinterpret_cast<uintptr_t>(p) & 15)) & 15) / int(sizeof(T));
+    if (head > count) head = count;
+    vecs = (count - head) / kVec;
 #pragma unroll
-    for (int j = 0; j < kVec; ++j) f(to_f(v[j]));
+    for (int j = 0; j < kIter; ++j) {
+      const int i = j * kThreads + int(threadIdx.x);
+      q[j] = i < vecs ? __ldg(reinterpret_cast<const uint4*>(p + head) + i) : make_uint4(0, 0, 0, 0);
+    }
   }
-  for (int i = head + vecs * kVec + threadIdx.x; i < count; i += kThreads) f(to_f(p[i]));
-}
+  // f(index) over this thread's single elements
+  template <class F>
+  __device__ __forceinline__ void singles(F&& f) const {
+    for (int i = threadIdx.x; i < head; i += kThreads) f(i);
+    for (int i = head + vecs * kVec + int(threadIdx.x); i < count; i += kThreads) f(i);
+  }
+};
 
 template <class T>
 __device__ __forceinline__ double sum_squares(const T* p, int count) {
+  const Share<T> c(p, count);
   float s = 0.f;
-  each(p, count, [&](float g) { s = fmaf(g, g, s); });
+#pragma unroll
+  for (int j = 0; j < Share<T>::kIter; ++j) {
+    const T* v = reinterpret_cast<const T*>(&c.q[j]);
+#pragma unroll
+    for (int i = 0; i < Share<T>::kVec; ++i) s = fmaf(to_f(v[i]), to_f(v[i]), s);
+  }
+  c.singles([&](int i) { s = fmaf(to_f(p[i]), to_f(p[i]), s); });
   if (s >= 1e-30f && s <= 1e38f) return double(s);
   double d = 0.0;
-  each(p, count, [&](float g) { d = fma(double(g), double(g), d); });
+  for (int j = 0; j < Share<T>::kIter; ++j) {
+    const T* v = reinterpret_cast<const T*>(&c.q[j]);
+    for (int i = 0; i < Share<T>::kVec; ++i) d = fma(double(to_f(v[i])), double(to_f(v[i])), d);
+  }
+  c.singles([&](int i) { d = fma(double(to_f(p[i])), double(to_f(p[i])), d); });
   return d;
 }
 
@@ -105,8 +126,9 @@ __device__ __forceinline__ double block_sum(double v, double* sh) {
 }
 
 template <int kCap>
-__global__ void __launch_bounds__(kThreads) k_clip_sumsq(const __grid_constant__ List<kCap> l, double* part) {
+__global__ void __launch_bounds__(kThreads, kSumBlocks) k_clip_sumsq(const __grid_constant__ List<kCap> l, double* part) {
   __shared__ double sh[kThreads / 32];
+  tc::wait_for_previous();
   tc::launch_dependents();
   double s = 0.0;
   for (int c = blockIdx.x; c < l.chunks; c += gridDim.x) {
@@ -127,32 +149,30 @@ __device__ __forceinline__ __nv_bfloat16 from_f<__nv_bfloat16>(float x) { return
 
 template <class T>
 __device__ __forceinline__ void scale_chunk(const T* p, T* o, int count, float f) {
-  constexpr int kVec = 16 / sizeof(T);
-  const uintptr_t a = reinterpret_cast<uintptr_t>(p) & 15, b = reinterpret_cast<uintptr_t>(o) & 15;
-  if (a != b) {  // the two do not share 16-byte boundaries
+  if (((reinterpret_cast<uintptr_t>(p) ^ reinterpret_cast<uintptr_t>(o)) & 15) != 0) {
+    // the two do not share 16-byte boundaries
+#pragma unroll 8
     for (int i = threadIdx.x; i < count; i += kThreads) o[i] = from_f<T>(f * to_f(p[i]));
     return;
   }
-  int head = int((16 - a) & 15) / int(sizeof(T));
-  if (head > count) head = count;
-  const int vecs = (count - head) / kVec;
-  for (int i = threadIdx.x; i < head; i += kThreads) o[i] = from_f<T>(f * to_f(p[i]));
-#pragma unroll 4
-  for (int i = threadIdx.x; i < vecs; i += kThreads) {
-    uint4 q = *(reinterpret_cast<const uint4*>(p + head) + i);
-    T* v = reinterpret_cast<T*>(&q);
+  Share<T> c(p, count);
 #pragma unroll
-    for (int j = 0; j < kVec; ++j) v[j] = from_f<T>(f * to_f(v[j]));
-    __stcs(reinterpret_cast<uint4*>(o + head) + i, q);
+  for (int j = 0; j < Share<T>::kIter; ++j) {
+    const int i = j * kThreads + int(threadIdx.x);
+    T* v = reinterpret_cast<T*>(&c.q[j]);
+#pragma unroll
+    for (int e = 0; e < Share<T>::kVec; ++e) v[e] = from_f<T>(f * to_f(v[e]));
+    if (i < c.vecs) __stcs(reinterpret_cast<uint4*>(o + c.head) + i, c.q[j]);
   }
-  for (int i = head + vecs * kVec + threadIdx.x; i < count; i += kThreads) o[i] = from_f<T>(f * to_f(p[i]));
+  c.singles([&](int i) { o[i] = from_f<T>(f * to_f(p[i])); });
 }
 
 template <int kCap>
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(kThreads, kScaleBlocks)
     k_clip_scale(const __grid_constant__ List<kCap> l, const double* part, int parts, float max_norm, float* norm) {
   __shared__ double sh[kThreads / 32];
   tc::wait_for_previous();
+  tc::launch_dependents();
   double s = 0.0;
   for (int i = threadIdx.x; i < parts; i += kThreads) s += part[i];
   s = block_sum(s, sh);
@@ -170,7 +190,10 @@ __global__ void __launch_bounds__(kThreads)
   }
 }
 
-int clip_blocks() { return 4 * sm_count(); }
+int blocks_of(int chunks, int per_sm) {
+  const int most = per_sm * sm_count();
+  return chunks < 1 ? 1 : chunks < most ? chunks : most;
+}
 
 template <int kCap>
 void fill(List<kCap>& l, const void* const* grads, void* const* out, const int64_t* numel, const int32_t* dtype, int n) {
@@ -194,21 +217,10 @@ struct Args {
   int n;
 };
 
-template <int kCap>
-cudaError_t sumsq(const Args& a, double* part, cudaStream_t s) {
-  List<kCap> l;
-  fill(l, a.grads, a.out, a.numel, a.dtype, a.n);
-  k_clip_sumsq<kCap><<<unsigned(clip_blocks()), kThreads, 0, s>>>(l, part);
-  return cudaGetLastError();
-}
-
-template <int kCap>
-cudaError_t scale(const Args& a, const double* part, int parts, float max_norm, float* norm, cudaStream_t s) {
-  List<kCap> l;
-  fill(l, a.grads, a.out, a.numel, a.dtype, a.n);
+template <class... P, class... A>
+cudaError_t launch_early(void (*kernel)(P...), int blocks, cudaStream_t s, A... args) {
   cudaLaunchConfig_t cfg = {};
-  const int blocks = clip_blocks();
-  cfg.gridDim = dim3(unsigned(l.chunks < blocks ? (l.chunks < 1 ? 1 : l.chunks) : blocks));
+  cfg.gridDim = dim3(unsigned(blocks));
   cfg.blockDim = dim3(kThreads);
   cfg.stream = s;
   cudaLaunchAttribute at[1];
@@ -216,7 +228,26 @@ cudaError_t scale(const Args& a, const double* part, int parts, float max_norm, 
   at[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = at;
   cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, k_clip_scale<kCap>, l, part, parts, max_norm, norm);
+  return cudaLaunchKernelEx(&cfg, kernel, args...);
+}
+
+// Squares of one list: adds its blocks to `parts`.
+template <int kCap>
+cudaError_t sumsq(const Args& a, double* part, int& parts, cudaStream_t s) {
+  List<kCap> l;
+  fill(l, a.grads, a.out, a.numel, a.dtype, a.n);
+  const int blocks = blocks_of(l.chunks, kSumBlocks);
+  double* to = part + parts;
+  parts += blocks;
+  return launch_early(k_clip_sumsq<kCap>, blocks, s, l, to);
+}
+
+template <int kCap>
+cudaError_t scale(const Args& a, const double* part, int parts, float max_norm, float* norm, cudaStream_t s) {
+  List<kCap> l;
+  fill(l, a.grads, a.out, a.numel, a.dtype, a.n);
+  const int blocks = blocks_of(l.chunks, kScaleBlocks);
+  return launch_early(k_clip_scale<kCap>, blocks, s, l, part, parts, max_norm, norm);
 }
 
 Args part_of(const Args& a, int first) {
@@ -235,7 +266,7 @@ int64_t grad_clip_max_numel() { return int64_t(kChunk) * 2000000; }
 
 size_t grad_clip_workspace_bytes(int n) {
   const size_t launches = n < 1 ? 1 : (size_t(n) + kMany - 1) / kMany;
-  return align256(launches * size_t(clip_blocks()) * sizeof(double));
+  return align256(launches * size_t(kSumBlocks) * size_t(sm_count()) * sizeof(double));
 }
 
 cudaError_t launch_grad_clip(const void* const* grads, void* const* out, const int64_t* numel, const int32_t* dtype,
@@ -245,9 +276,8 @@ cudaError_t launch_grad_clip(const void* const* grads, void* const* out, const i
   int parts = 0;
   for (int i = 0; i < n || i == 0; i += kMany) {
     const Args a = part_of(all, i);
-    const cudaError_t e = a.n <= kFew ? sumsq<kFew>(a, part + parts, s) : sumsq<kMany>(a, part + parts, s);
+    const cudaError_t e = a.n <= kFew ? sumsq<kFew>(a, part, parts, s) : sumsq<kMany>(a, part, parts, s);
     if (e != cudaSuccess) return e;
-    parts += clip_blocks();
   }
   for (int i = 0; i < n || i == 0; i += kMany) {
     const Args a = part_of(all, i);

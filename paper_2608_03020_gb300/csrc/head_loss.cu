@@ -151,6 +151,7 @@ __global__ void __launch_bounds__(256)
 // ------------------------------------------------------------------ epilogues of the logit tiles
 // Forward: maximum and sum of exponentials of 128 logits of a row.
 struct EpiStats {
+  static constexpr bool kPacks = false;
   float2* part;        // (2 column tiles) x pitch
   int64_t pitch;       // rows of a piece
   const int32_t* y;    // this piece's rows
@@ -215,38 +216,39 @@ struct EpiStats {
 // Backward: dZ = g w (p - onehot) of the same tile, bf16, for the gradient products.  Columns past
 // the vocabulary and rows past the live ones are zero.
 struct EpiDz {
+  static constexpr bool kPacks = true;
   const float* lse;
   const float* w;      // w_n dloss_n
   const int32_t* y;
   const int32_t* count;
   int64_t row_first;   // this piece's first row among the live rows
   int64_t v_first;     // this piece's first vocabulary column
-  int64_t v_end;       // end of the vocabulary
+  int v_cols;          // its columns of the vocabulary
 
-  __device__ __forceinline__ void operator()(const gp::Tile&, float (&v)[128], int row, int col0, int lane, uint8_t* box,
-                                             const CUtensorMap* out) const {
+  struct Row {
+    float lse, g;
+    int at, end;  // the target's column and the columns that count (none in rows past the live ones)
+  };
+  __device__ __forceinline__ Row row_of(int row) const {
+    Row r;
     const bool live = row_first + row < *count;
-    const float l = lse[row];
-    const float g = live ? w[row] : 0.f;
-    const int64_t vc = v_first + col0;
-    const int left = int(v_end - vc < 128 ? v_end - vc : 128);
-    const int64_t at64 = int64_t(y[row]) - vc;
-    const int at = at64 >= 0 && at64 < 128 ? int(at64) : -1;
-#pragma unroll
-    for (int i = 0; i < 128; ++i) {
-      const float p = exp_diff(v[i], l) - (i == at ? 1.f : 0.f);
-      v[i] = live && i < left ? g * p : 0.f;
-    }
-    const int r0 = row - lane;
-#pragma unroll
-    for (int b = 0; b < 2; ++b)
-      gp::store_box_bf16(box, out, lane, col0 + 64 * b, r0, [&](int i) { return v[64 * b + i]; });
+    r.lse = lse[row];
+    r.g = w[row];
+    const int64_t at = int64_t(y[row]) - v_first;
+    r.at = at >= 0 && at < v_cols ? int(at) : -1;
+    r.end = live ? v_cols : 0;
+    return r;
+  }
+  __device__ __forceinline__ float value(const Row& r, int col, float z) const {
+    const float p = exp_diff(z, r.lse) - (col == r.at ? 1.f : 0.f);
+    return col < r.end ? r.g * p : 0.f;
   }
 };
 
 // dH: fp32 sums of one k range, stored or added to the sums of the earlier pieces of the vocabulary
 // (one writer per element and launch: a fixed order of additions).
 struct EpiAcc {
+  static constexpr bool kPacks = false;
   int64_t rows;  // rows of one split's sums
   int add;
 
@@ -277,14 +279,12 @@ struct EpiAcc {
 
 // dW: scaled and rounded once.
 struct EpiScaled {
+  static constexpr bool kPacks = true;
   float scale;
 
-  __device__ __forceinline__ void operator()(const gp::Tile&, float (&v)[128], int row, int col0, int lane, uint8_t* box,
-                                             const CUtensorMap* out) const {
-#pragma unroll
-    for (int b = 0; b < 2; ++b)
-      gp::store_box_bf16(box, out, lane, col0 + 64 * b, row - lane, [&](int i) { return scale * v[64 * b + i]; });
-  }
+  struct Row {};
+  __device__ __forceinline__ Row row_of(int) const { return Row{}; }
+  __device__ __forceinline__ float value(const Row&, int, float v) const { return scale * v; }
 };
 
 // ------------------------------------------------------------------ joins
@@ -424,19 +424,16 @@ struct BwdWs {
   int splits;     // k ranges of dH
   size_t dz, part, total;
 };
-// k ranges of the dH product: its tiles (rows / 256 x d / 256) are few, so one range per tile would
-// leave the last wave of CTA pairs mostly idle.  More ranges fill it and cost 8 bytes per element
-// and range (written, then read by k_head_dh).  Both sides of the choice in tensor-core cycles.
+// k ranges of the dH product: its tiles (rows / 256 x d / 512) are few, so one range per tile would
+// leave the last round of CTA pairs mostly idle.  More ranges fill it and cost 8 bytes per element and
+// range (written, then read by k_head_dh).  Both sides of the choice in cycles.
 int dh_splits(int64_t rows, int64_t d, int64_t vc) {
-  const int64_t pairs = sm_count() / 2;
-  const int64_t tiles = (rows / gp::TM) * ((d + gp::TN - 1) / gp::TN);
-  const double nkb = double(vc) / gp::BK;
+  const int64_t m = rows / gp::TM, nkb = vc / gp::BK;
   int best = 1;
   double best_c = 0;
-  for (int s = 1; s <= 8; ++s) {
+  for (int s = 1; s <= 32; ++s) {
     if (s > 1 && nkb / s < 16) break;
-    const double waves = double((tiles * s + pairs - 1) / pairs);
-    const double c = waves * (nkb / s * 512.0 + 2000.0) + double(s) * double(rows) * double(d) * 8.0 / 3000.0;
+    const double c = gp::cycles(gp::prefer_wide(m, d, nkb, s), m, d, nkb, s) + double(s) * double(rows) * double(d) * 8.0 / 3000.0;
     if (s == 1 || c < best_c) {
       best = s;
       best_c = c;
@@ -551,9 +548,8 @@ cudaError_t launch_head_loss_backward(const void* H, int64_t ldh, int64_t N, int
       gp::Geo g = geo(rows / gp::TM, vn, (d + gp::BK - 1) / gp::BK, kSegKb, r, status);
       g.rows_live = r.count;
       g.m_first = int(p0 / gp::TM);
-      const EpiDz dz_epi{r.lse + p0, r.w + p0, r.y + p0, r.count, p0, v0, V};
-      e = d <= gp::kWideK ? gp::launch<true, false, false>(mh, mw, mh, mw, mz_out, g, dz_epi, gp::NoExt{}, s)
-                          : gp::launch<false, false, false>(mh, mw, mh, mw, mz_out, g, dz_epi, gp::NoExt{}, s);
+      e = gp::launch_either<false, false>(mh, mw, mh, mw, mz_out, g,
+                                          EpiDz{r.lse + p0, r.w + p0, r.y + p0, r.count, p0, v0, int(vn)}, gp::NoExt{}, s);
       if (e != cudaSuccess) return e;
       if (dH) {
         CUtensorMap mo;
@@ -565,10 +561,8 @@ cudaError_t launch_head_loss_backward(const void* H, int64_t ldh, int64_t N, int
         gh.rows_live = r.count;
         gh.m_first = g.m_first;
         gh.splits = lay.splits;
-        const EpiAcc acc{lay.piece, v0 > 0 ? 1 : 0};
-        e = vn <= gp::kWideK * lay.splits
-                ? gp::launch<true, false, true>(mz_k, mw_mn, mz_k, mw_mn, mo, gh, acc, gp::NoExt{}, s)
-                : gp::launch<false, false, true>(mz_k, mw_mn, mz_k, mw_mn, mo, gh, acc, gp::NoExt{}, s);
+        e = gp::launch_either<false, true>(mz_k, mw_mn, mz_k, mw_mn, mo, gh, EpiAcc{lay.piece, v0 > 0 ? 1 : 0},
+                                           gp::NoExt{}, s);
         if (e != cudaSuccess) return e;
       }
       if (dW) {
@@ -579,9 +573,7 @@ cudaError_t launch_head_loss_backward(const void* H, int64_t ldh, int64_t N, int
           return cudaErrorInvalidValue;
         gp::Geo gw = geo(vtiles, d, np / gp::BK, kSegKbGrad, r, status);
         gw.k_live = r.count;
-        e = np <= gp::kWideK
-                ? gp::launch<true, true, true>(mz_mn, mh_mn, mz_mn, mh_mn, mo, gw, EpiScaled{scale}, gp::NoExt{}, s)
-                : gp::launch<false, true, true>(mz_mn, mh_mn, mz_mn, mh_mn, mo, gw, EpiScaled{scale}, gp::NoExt{}, s);
+        e = gp::launch_either<true, true>(mz_mn, mh_mn, mz_mn, mh_mn, mo, gw, EpiScaled{scale}, gp::NoExt{}, s);
         if (e != cudaSuccess) return e;
       }
     }
