@@ -5,7 +5,7 @@
 // by the adapter projection.  Each operand is K-major (k contiguous) or MN-major (m or n
 // contiguous); the tensor maps and the MMA descriptors carry the difference.
 //
-// Two shapes (kWide).  Narrow: a pair of CTAs holds a 256 x 256 fp32 tile (128 rows per CTA: half of
+// Three shapes.  Narrow: a pair of CTAs holds a 256 x 256 fp32 tile (128 rows per CTA: half of
 // TMEM); the other half of TMEM takes the next tile while eight warps read this one.  Wide: 256 x 512,
 // two accumulators that share A, all of TMEM.  What bounds the narrow one is shared memory: per 64-wide
 // k-block and CTA the loads write 32 KB and the MMAs read 32 KB in the 512 cycles that the MMAs take,
@@ -13,11 +13,15 @@
 // the MMAs, about 450).  The wide one writes 48 KB for 1024 cycles of MMAs.  Its epilogue is not
 // hidden behind a second buffer, so the MMAs of the next tile's first four k-blocks go to the first
 // accumulator, which is read first, before any goes to the second.
+// Single: up to 128 rows of A in all (a few tokens against a vocabulary).  A pair would leave its odd CTA
+// multiplying zero rows, so each CTA works alone on 128 x 256 tiles, with the narrow shape's segments
+// and two buffers; B's read from HBM is then the bound.  With B K-major its tiles may be narrower than
+// 256 columns (`width`, a multiple of 16), so that the last round of CTAs is as full as the others.
 //   warp 0       TMA producer (both CTAs): its CTA's 128 rows of A and 128 rows of B per accumulator
 //   warp 1       one thread of the even CTA issues the MMAs (M = 256, N = 256, K = 16)
 //   warps 2..9   take the sums out of TMEM: warp w holds rows 32 (w & 3) .. + 31 of its CTA, one row
 //                per lane, and 128 of an accumulator's 256 columns, in registers
-// Segments (narrow only): the tensor cores' fp32 accumulation loses a fraction of an ulp of the running
+// Segments (narrow and single): the tensor cores' fp32 accumulation loses a fraction of an ulp of the running
 // sum at every step, always toward zero.  The sums restart every `seg_kb` k-blocks and the epilogue
 // warps add the segments in registers with round-to-nearest additions, which bounds that bias whatever
 // K is (a logit at K = 5120 comes out ~10x nearer to its 64-bit value than with one accumulator).  A
@@ -50,19 +54,20 @@ constexpr int EPI_WARPS = 8;
 constexpr int BOX = 4096;             // one epilogue warp's staging box: 32 rows x 128 bytes
 constexpr int THREADS = 64 + 32 * EPI_WARPS;
 constexpr int64_t kWideK = 16384;
-template <bool kWide>
+enum : int { kNarrow = 0, kWide = 1, kSingle = 2 };
+template <int kShape>
 struct Shape {
-  static constexpr int kAcc = kWide ? 2 : 1;       // accumulators of a tile
+  static constexpr int kCtas = kShape == kSingle ? 1 : 2;  // CTAs of a tile
+  static constexpr int kAcc = kShape == kWide ? 2 : 1;     // accumulators of a tile
   static constexpr int kCols = TN * kAcc;
-  static constexpr int kStages = kWide ? 4 : 6;
-  static constexpr int kStageBytes = (1 + kAcc) * OPB;
-  static constexpr int kBars = 2 * kStages + 5;    // full[S], empty[S], acc_full[2], acc_empty[2], drain
+  static constexpr int kOpsB = kShape == kNarrow ? 1 : 2;  // 128-row operands of B per CTA and stage
+  static constexpr int kStageBytes = (1 + kOpsB) * OPB;
+  static constexpr int kStages = 12 * OPB / kStageBytes;
+  static constexpr int kBars = 2 * kStages + 5;            // full[S], empty[S], acc_full[2], acc_empty[2], drain
 };
 constexpr int SMEM = 12 * OPB + EPI_WARPS * BOX + 256 + 1024;
 static_assert(SMEM <= 232448, "shared memory per CTA");
-static_assert(Shape<false>::kStages * Shape<false>::kStageBytes == 12 * OPB, "ring");
-static_assert(Shape<true>::kStages * Shape<true>::kStageBytes == 12 * OPB, "ring");
-static_assert(Shape<false>::kBars * 8 + 8 <= 256, "barrier area");
+static_assert(Shape<kNarrow>::kBars * 8 + 8 <= 256, "barrier area");
 
 // One launch's work.  Tiles are taken in groups of `group` row tiles that sweep all column tiles,
 // row tile fastest: the CTA pairs at work share a few column tiles and one group of row tiles,
@@ -70,6 +75,8 @@ static_assert(Shape<false>::kBars * 8 + 8 <= 256, "barrier area");
 struct Geo {
   int m_tiles, n_tiles;  // upper bounds (rows_live may lower m_tiles, k_live the k-blocks); set by launch()
   int cols;              // columns of the output
+  int rows;              // rows of A (host: 128 or fewer take the single shape)
+  int width;             // columns of a tile (launch() sets all but the single shape's)
   int nkb;               // k-blocks of the product
   int splits;            // the k-blocks are cut into this many ranges, each a tile of its own
   int seg_kb;            // k-blocks per accumulation segment
@@ -84,7 +91,8 @@ struct Geo {
 };
 
 struct Tile {
-  int m, col0, split;
+  int m, n, col0, split;
+  int end;  // column behind the tile's last
   int kb0, kb1;
 };
 
@@ -112,7 +120,6 @@ __device__ __forceinline__ Live live_of(const Geo& g) {
   return v;
 }
 
-template <int kCols>
 __device__ __forceinline__ Tile tile_of(const Geo& g, const Live& v, int it) {
   Tile t;
   const int per_split = v.m_tiles * g.n_tiles;
@@ -123,9 +130,10 @@ __device__ __forceinline__ Tile tile_of(const Geo& g, const Live& v, int it) {
   r -= gi * per_group;
   const int m0 = gi * g.group;
   const int gm = v.m_tiles - m0 < g.group ? v.m_tiles - m0 : g.group;
-  const int n = r / gm;
-  t.m = m0 + r - n * gm;
-  t.col0 = n * kCols;
+  t.n = r / gm;
+  t.m = m0 + r - t.n * gm;
+  t.col0 = t.n * g.width;
+  t.end = t.col0 + g.width < g.cols ? t.col0 + g.width : g.cols;
   const int per = (v.nkb + g.splits - 1) / g.splits;
   t.kb0 = t.split * per < v.nkb ? t.split * per : v.nkb;
   t.kb1 = t.kb0 + per < v.nkb ? t.kb0 + per : v.nkb;
@@ -176,13 +184,16 @@ struct NoExt {
 //                                   uint8_t* box, const CUtensorMap* out) const
 // called once per finished accumulator by every epilogue thread, with the sums of row `row`, columns
 // col0 .. col0 + 127.
-template <bool kWide, bool kAmn, bool kBmn, class Epi, class Ext>
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
+template <int kShape, bool kAmn, bool kBmn, class Epi, class Ext>
+__global__ void __cluster_dims__(Shape<kShape>::kCtas, 1, 1) __launch_bounds__(THREADS, 1)
     k_gemm_pair(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB,
                 const __grid_constant__ CUtensorMap tmAx, const __grid_constant__ CUtensorMap tmBx,
                 const __grid_constant__ CUtensorMap tmO, const __grid_constant__ Geo g,
                 const __grid_constant__ Epi epi, const __grid_constant__ Ext ext) {
-  using S = Shape<kWide>;
+  using S = Shape<kShape>;
+  constexpr bool kPair = S::kCtas == 2;
+  constexpr bool kSlim = kShape == kSingle && !kBmn;  // tiles of `width` columns: two boxes of width / 2 rows
+  static_assert(kPair || !Ext::kOn, "an extended k axis takes pairs");
   constexpr int STAGES = S::kStages, STAGE_BYTES = S::kStageBytes, BARS = S::kBars;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
@@ -213,7 +224,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
     }
     for (uint32_t b = 0; b < 2; ++b) {
       mbar_init(acc_full(b), 1);
-      mbar_init(acc_empty(b), 2 * EPI_WARPS);  // lane 0 of the epilogue warps of both CTAs
+      mbar_init(acc_empty(b), S::kCtas * EPI_WARPS);  // lane 0 of the epilogue warps
     }
     mbar_init(drain_bar, 1);
     *odd_issued = 0;
@@ -226,7 +237,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
       prefetch_tensormap(&tmBx);
     }
   }
-  if (warp == 1) tmem_alloc_pair(smem_u32(tmem_slot), 512);
+  if (warp == 1) {
+    if (kPair) tmem_alloc_pair(smem_u32(tmem_slot), 512);
+    else tmem_alloc(smem_u32(tmem_slot), 512);
+  }
   fence_before();
   cluster_sync();
   fence_after();
@@ -244,7 +258,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
       uint32_t iter = 0;
       bool ok = true;
       for (int it = cid; it < lv.total && ok; it += ncl) {
-        const Tile t = tile_of<S::kCols>(g, lv, it);
+        const Tile t = tile_of(g, lv, it);
         const int m0 = t.m * TM + int(rank) * HALF;
         const int n0 = t.col0 + int(rank) * HALF;
         const int nx = Ext::kOn ? ext.entries(t.m) : 0;
@@ -255,33 +269,42 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
             ok = false;
             break;
           }
-          if (leader) mbar_arrive_expect_tx(full_bar(stage), 2u * STAGE_BYTES);
+          if (leader) mbar_arrive_expect_tx(full_bar(stage), kSlim ? uint32_t(OPB + g.width * BK * 2)
+                                                                   : uint32_t(S::kCtas) * STAGE_BYTES);
           const uint32_t fb = mapa_shared(full_bar(stage), 0);
           const uint32_t a = smem_base + uint32_t(stage) * STAGE_BYTES;
           const uint32_t b = a + OPB;
           if (!Ext::kOn || j < nb) {
             const int k0 = (t.kb0 + j) * BK;
+            auto load = [&](uint32_t dst, const CUtensorMap* map, int c0, int c1) {
+              if constexpr (kPair) tma_load_2d_pair(dst, map, fb, c0, c1);
+              else tma_load_2d(dst, map, fb, c0, c1);
+            };
             if (kAmn) {
-              tma_load_2d_pair(a, &tmA, fb, m0, k0);
-              tma_load_2d_pair(a + SUB, &tmA, fb, m0 + 64, k0);
+              load(a, &tmA, m0, k0);
+              load(a + SUB, &tmA, m0 + 64, k0);
             } else {
-              tma_load_2d_pair(a, &tmA, fb, k0, m0);
+              load(a, &tmA, k0, m0);
             }
+            // 128 rows of B per operand: this CTA's half of each accumulator, or (single) both halves
 #pragma unroll
-            for (int c = 0; c < S::kAcc; ++c) {
-              if (kBmn) {
-                tma_load_2d_pair(b + c * OPB, &tmB, fb, n0 + c * TN, k0);
-                tma_load_2d_pair(b + c * OPB + SUB, &tmB, fb, n0 + c * TN + 64, k0);
+            for (int c = 0; c < S::kOpsB; ++c) {
+              const int n = n0 + c * (kPair ? TN : kSlim ? g.width / 2 : HALF);
+              if (kSlim) {
+                load(b + c * uint32_t(g.width * BK), &tmB, k0, n);
+              } else if (kBmn) {
+                load(b + c * OPB, &tmB, n, k0);
+                load(b + c * OPB + SUB, &tmB, n + 64, k0);
               } else {
-                tma_load_2d_pair(b + c * OPB, &tmB, fb, k0, n0 + c * TN);
+                load(b + c * OPB, &tmB, k0, n);
               }
             }
           } else {
-            int a_row, block;
-            ext.entry(t.m, j - nb, rank, a_row, block);
+            int a_row, at;
+            ext.entry(t.m, j - nb, rank, a_row, at);
             tma_load_2d_pair(a, &tmAx, fb, 0, a_row);
 #pragma unroll
-            for (int c = 0; c < S::kAcc; ++c) tma_load_3d_pair(b + c * OPB, &tmBx, fb, 0, n0 + c * TN, block);
+            for (int c = 0; c < S::kAcc; ++c) tma_load_3d_pair(b + c * OPB, &tmBx, fb, 0, n0 + c * TN, at);
           }
           ++iter;
           if (++stage == STAGES) { stage = 0; phase ^= 1u; }
@@ -303,7 +326,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
       const uint64_t b_kmaj = sdesc(smem_base + OPB, kKLbo, 1024u, kSwizzle128B);
       const uint64_t b0 = kBmn ? sdesc(smem_base + OPB, SUB, 1024u, kSwizzle128B) : b_kmaj;
       constexpr uint64_t kAStep = kAmn ? 2048 >> 4 : 32 >> 4, kBStep = kBmn ? 2048 >> 4 : 32 >> 4;
-      constexpr uint32_t kId = tc::idesc(1, 1, kAmn ? 1 : 0, kBmn ? 1 : 0, TM, TN);
+      const uint32_t id = tc::idesc(1, 1, kAmn ? 1 : 0, kBmn ? 1 : 0, S::kCtas * HALF, kSlim ? uint32_t(g.width) : TN);
       constexpr uint32_t kIdX = tc::idesc(1, 1, 0, 0, TM, TN);
       // the MMAs of one k-block into accumulator c
       auto block = [&](int s, uint32_t d, int c, bool from_ext, bool first) {
@@ -311,11 +334,18 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
         if (!Ext::kOn || !from_ext) {
 #pragma unroll
           for (int kk = 0; kk < BK / 16; ++kk)
-            mma_f16_pair(d, a0 + so + kk * kAStep, b0 + bo + kk * kBStep, kId, !first || kk != 0 ? 1u : 0u);
+            if constexpr (kPair)
+              mma_f16_pair(d, a0 + so + kk * kAStep, b0 + bo + kk * kBStep, id, !first || kk != 0 ? 1u : 0u);
+            else
+              mma_f16(d, a0 + so + kk * kAStep, b0 + bo + kk * kBStep, id, !first || kk != 0 ? 1u : 0u);
         } else {
           for (int kk = 0; kk < ext.ksteps(); ++kk)
             mma_f16_pair(d, a_kmaj + so + kk * 2, b_kmaj + bo + kk * 2, kIdX, !first || kk != 0 ? 1u : 0u);
         }
+      };
+      auto commit = [&](uint32_t bar) {
+        if constexpr (kPair) mma_commit_pair_mc(bar, 0x3);
+        else mma_commit(bar);
       };
       auto wait_full = [&](int s, uint32_t ph) {
         if (!mbar_try_wait_cluster(full_bar(s), ph) && !mbar_wait_cluster(full_bar(s), ph, wc)) return false;
@@ -328,10 +358,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
         return true;
       };
       for (int it = cid; it < lv.total && ok; it += ncl) {
-        const Tile t = tile_of<S::kCols>(g, lv, it);
+        const Tile t = tile_of(g, lv, it);
         const int nb = t.kb1 - t.kb0;
         const int all = nb + (Ext::kOn ? ext.entries(t.m) : 0);
-        if constexpr (kWide) {
+        if constexpr (kShape == kWide) {
           if (all == 0) continue;
           const bool two = g.cols - t.col0 > TN;  // the second accumulator holds columns of the output
           const int head = all < STAGES ? all : STAGES;
@@ -345,23 +375,23 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
           }
           // (waited for without a second accumulator too: acc_full(1) must not complete twice unseen)
           if (!ok || !(ok = wait_acc(1, (seg & 1u) ^ 1u))) break;
-          if (all == head) mma_commit_pair_mc(acc_full(0), 0x3);
+          if (all == head) commit(acc_full(0));
           for (int j = 0, s = stage0; j < head; ++j) {
             if (two) block(s, tmem_base + uint32_t(TN), 1, j >= nb, j == 0);
-            mma_commit_pair_mc(empty_bar(s), 0x3);
+            commit(empty_bar(s));
             if (++s == STAGES) s = 0;
           }
           for (int j = head; j < all; ++j) {
             if (!(ok = wait_full(stage, phase))) break;
             block(stage, tmem_base, 0, j >= nb, false);
-            if (j == all - 1) mma_commit_pair_mc(acc_full(0), 0x3);
+            if (j == all - 1) commit(acc_full(0));
             if (two) block(stage, tmem_base + uint32_t(TN), 1, j >= nb, false);
-            mma_commit_pair_mc(empty_bar(stage), 0x3);
+            commit(empty_bar(stage));
             if (++stage == STAGES) { stage = 0; phase ^= 1u; }
           }
           if (!ok) break;
           // (a tile without a second accumulator completes that barrier all the same: one phase a tile)
-          mma_commit_pair_mc(acc_full(1), 0x3);
+          commit(acc_full(1));
           ++seg;
         } else {
           uint32_t d = 0;
@@ -374,10 +404,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
             if (!(ok = wait_full(stage, phase))) break;
             block(stage, d, 0, j >= nb, in_seg == 0);
             issued = true;
-            mma_commit_pair_mc(empty_bar(stage), 0x3);
+            commit(empty_bar(stage));
             if (++stage == STAGES) { stage = 0; phase ^= 1u; }
             if (++in_seg == g.seg_kb || j == all - 1) {
-              mma_commit_pair_mc(acc_full(seg & 1u), 0x3);
+              commit(acc_full(seg & 1u));
               ++seg;
               in_seg = 0;
             }
@@ -385,7 +415,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
         }
       }
       if (issued) {
-        mma_commit_pair(drain_bar);
+        if (kPair) mma_commit_pair(drain_bar);
+        else mma_commit(drain_bar);
         mbar_drain(drain_bar, 0, kDrainLimitNs);
       }
     }
@@ -398,7 +429,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
     uint32_t seg = 0;
     bool go = true;
     for (int it = cid; it < lv.total && go; it += ncl) {
-      const Tile t = tile_of<S::kCols>(g, lv, it);
+      const Tile t = tile_of(g, lv, it);
       const int all = t.kb1 - t.kb0 + (Ext::kOn ? ext.entries(t.m) : 0);
       const int row = t.m * TM + int(rank) * HALF + q * 32 + lane;
       auto wait_sums = [&](uint32_t b, uint32_t par) {
@@ -416,7 +447,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
         }
       };
       const int r0 = row - lane;
-      if constexpr (kWide && Epi::kPacks) {
+      if constexpr (kShape == kWide && Epi::kPacks) {
         // both accumulators are in registers, rounded and packed, before the stores that the MMAs need
         // not wait for: 64 words of the first, of which a box (32) leaves before the second is read
         const auto pre = epi.row_of(row);
@@ -445,7 +476,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
         if (col1 < g.cols) store_box_bf16(box, &tmO, lane, col1, r0, w1);
         if (col1 + 64 < g.cols) store_box_bf16(box, &tmO, lane, col1 + 64, r0, w1 + 32);
         if (all > 0) ++seg;
-      } else if constexpr (kWide) {
+      } else if constexpr (kShape == kWide) {
 #pragma unroll 1
         for (uint32_t a = 0; a < 2; ++a) {
           if (all > 0 && !(go = wait_sums(a, seg & 1u))) break;
@@ -518,7 +549,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
     // odd CTA never issued gets its bytes settled, one only the odd CTA issued gets armed, and each
     // of the last STAGES iterations is waited for (the earlier ones have landed).
     const uint32_t n_even = iters_done;
-    const uint32_t n_odd = *reinterpret_cast<volatile uint32_t*>(odd_issued);
+    const uint32_t n_odd = kPair ? *reinterpret_cast<volatile uint32_t*>(odd_issued) : n_even;
     const uint32_t hi = n_even > n_odd ? n_even : n_odd;
     const uint32_t lo = hi > uint32_t(STAGES) ? hi - uint32_t(STAGES) : 0u;
     for (uint32_t i = lo; i < hi; ++i) {
@@ -531,7 +562,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
   fence_before();
   cluster_sync();
   fence_after();
-  if (warp == 1) tmem_dealloc_pair(tmem_base, 512);
+  if (warp == 1) {
+    if (kPair) tmem_dealloc_pair(tmem_base, 512);
+    else tmem_dealloc(tmem_base, 512);
+  }
 }
 
 // ------------------------------------------------------------------ host side
@@ -573,10 +607,11 @@ inline bool map_out_bf16(CUtensorMap* m, void* base, int64_t cols, int64_t rows,
   return map_2d(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, base, cols, rows, pitch, 64, 32);
 }
 
-// Pairs of CTAs that can be resident at once (76 on 152 SMs).
+// Tiles at work at once: pairs of CTAs (76 on 152 SMs), or CTAs.
 template <class K>
-inline int resident_pairs(K kernel) {
-  int clusters = sm_count() / 2;
+inline int resident_tiles(K kernel, int ctas) {
+  int clusters = sm_count() / ctas;
+  if (ctas == 1) return clusters;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(unsigned(2 * clusters));
   cfg.blockDim = dim3(THREADS);
@@ -626,38 +661,54 @@ inline cudaError_t launch_early(void (*kernel)(P...), dim3 grid, dim3 block, siz
 // wide rounds) at k = 512 .. 8192: narrow 672 cycles a k-block and 3000 a tile, wide 1030 and 9000 (both
 // with a share of the launch and of the last tiles' stores); at k = 8192 204 and 170 us (1.60 and 1.92
 // PFLOP/s), at k = 512 25 us each.
-inline double cycles(bool wide, int64_t m_tiles, int64_t cols, int64_t nkb, int splits) {
-  const int64_t pairs = sm_count() / 2;
-  const int64_t n = wide ? (cols + 2 * TN - 1) / (2 * TN) : (cols + TN - 1) / TN;
-  const double rounds = double((m_tiles * n * splits + pairs - 1) / pairs);
+inline double cycles(int shape, int64_t m_tiles, int64_t cols, int64_t nkb, int splits) {
+  const int64_t n = shape == kWide ? (cols + 2 * TN - 1) / (2 * TN) : (cols + TN - 1) / TN;
+  const int64_t at_once = shape == kSingle ? sm_count() : sm_count() / 2;
+  const double rounds = double((m_tiles * n * splits + at_once - 1) / at_once);
   const double kb = double((nkb + splits - 1) / splits);
-  return rounds * (wide ? 1030.0 * kb + 9000.0 : 672.0 * kb + 3000.0);
+  return rounds * (shape == kWide ? 1030.0 * kb + 9000.0 : 672.0 * kb + 3000.0);
 }
-inline bool prefer_wide(int64_t m_tiles, int64_t cols, int64_t nkb, int splits) {
-  return nkb <= kWideK / BK * splits && cycles(true, m_tiles, cols, nkb, splits) < cycles(false, m_tiles, cols, nkb, splits);
+// rows: those of A, where 128 or fewer may take the single shape (0: they may not)
+inline int pick_shape(int64_t rows, int64_t m_tiles, int64_t cols, int64_t nkb, int splits) {
+  if (rows > 0 && rows <= HALF) return kSingle;
+  const bool wide = nkb <= kWideK / BK * splits &&
+                    cycles(kWide, m_tiles, cols, nkb, splits) < cycles(kNarrow, m_tiles, cols, nkb, splits);
+  return wide ? kWide : kNarrow;
 }
 
-template <bool kWide, bool kAmn, bool kBmn, class Epi, class Ext>
+// Width of the single shape's tiles: as few rounds of the CTAs as 256 columns would take, in equal parts.
+inline int slim_width(int64_t cols) {
+  const int64_t at_once = sm_count();
+  const int64_t rounds = (cols + TN * at_once - 1) / (TN * at_once);
+  const int64_t w = (cols + rounds * at_once - 1) / (rounds * at_once);
+  return int((w + 15) / 16 * 16);
+}
+
+template <int kShape, bool kAmn, bool kBmn, class Epi, class Ext>
 inline cudaError_t launch(const CUtensorMap& a, const CUtensorMap& b, const CUtensorMap& ax, const CUtensorMap& bx,
                           const CUtensorMap& o, Geo g, const Epi& epi, const Ext& ext, cudaStream_t s) {
-  auto kernel = k_gemm_pair<kWide, kAmn, kBmn, Epi, Ext>;
-  g.n_tiles = (g.cols + Shape<kWide>::kCols - 1) / Shape<kWide>::kCols;
+  auto kernel = k_gemm_pair<kShape, kAmn, kBmn, Epi, Ext>;
+  constexpr int kCtas = Shape<kShape>::kCtas;
+  if (kShape != kSingle || kBmn || g.width == 0) g.width = Shape<kShape>::kCols;
+  g.n_tiles = (g.cols + g.width - 1) / g.width;
   cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM);
   if (e != cudaSuccess) return e;
-  static const int pairs = resident_pairs(kernel);
+  static const int at_once = resident_tiles(kernel, kCtas);
   const int64_t total = int64_t(g.m_tiles) * g.n_tiles * g.splits;
   if (total < 1) return cudaSuccess;
-  const int n = total < pairs ? int(total) : pairs;
-  return launch_early(kernel, dim3(unsigned(2 * n)), dim3(THREADS), SMEM, s, a, b, ax, bx, o, g, epi, ext);
+  const int n = total < at_once ? int(total) : at_once;
+  return launch_early(kernel, dim3(unsigned(kCtas * n)), dim3(THREADS), SMEM, s, a, b, ax, bx, o, g, epi, ext);
 }
 
-// The shape that prefer_wide() names.
+// The shape that pick_shape() names.
 template <bool kAmn, bool kBmn, class Epi, class Ext>
 inline cudaError_t launch_either(const CUtensorMap& a, const CUtensorMap& b, const CUtensorMap& ax, const CUtensorMap& bx,
                                  const CUtensorMap& o, const Geo& g, const Epi& epi, const Ext& ext, cudaStream_t s) {
-  return prefer_wide(g.m_tiles, g.cols, g.nkb, g.splits)
-             ? launch<true, kAmn, kBmn, Epi, Ext>(a, b, ax, bx, o, g, epi, ext, s)
-             : launch<false, kAmn, kBmn, Epi, Ext>(a, b, ax, bx, o, g, epi, ext, s);
+  const int shape = pick_shape(g.rows, g.m_tiles, g.cols, g.nkb, g.splits);
+  if constexpr (!Ext::kOn && !kAmn)
+    if (shape == kSingle) return launch<kSingle, kAmn, kBmn, Epi, Ext>(a, b, ax, bx, o, g, epi, ext, s);
+  return shape == kWide ? launch<kWide, kAmn, kBmn, Epi, Ext>(a, b, ax, bx, o, g, epi, ext, s)
+                        : launch<kNarrow, kAmn, kBmn, Epi, Ext>(a, b, ax, bx, o, g, epi, ext, s);
 }
 
 }  // namespace gp

@@ -159,12 +159,11 @@ struct EpiStats {
   const int32_t* cols; // label words
   int C;
   float* zc;           // C x pitch: the label words' logits
-  int64_t V;
 
   __device__ __forceinline__ void operator()(const gp::Tile& t, float (&v)[128], int row, int col0, int lane, uint8_t*,
                                              const CUtensorMap*) const {
     if (!LOCA_CHECK(row, pitch)) return;
-    const int left = int(V - col0 < 128 ? V - col0 : 128);  // columns of the vocabulary among these
+    const int left = t.end - col0 < 128 ? t.end - col0 : 128;  // columns of the vocabulary among these
     if (left < 128) {
 #pragma unroll
       for (int i = 0; i < 128; ++i)
@@ -189,12 +188,13 @@ struct EpiStats {
         s3 += exp_diff(v[i + 3], m);
       }
     }
-    part[int64_t(col0 / 128) * pitch + row] = make_float2(m, (s0 + s1) + (s2 + s3));
+    part[int64_t(2 * t.n + (col0 > t.col0 ? 1 : 0)) * pitch + row] = make_float2(m, (s0 + s1) + (s2 + s3));
     const int at = y[row] - col0;
-    if (__any_sync(0xffffffffu, at >= 0 && at < left)) {
+    const bool here_y = at >= 0 && at < left;  // (a label past this tile's end is the next tile's)
+    if (__any_sync(0xffffffffu, here_y)) {
 #pragma unroll
       for (int i = 0; i < 128; ++i)
-        if (i == at) zy[row] = v[i];
+        if (here_y && i == at) zy[row] = v[i];
     }
     for (int c0 = 0; c0 < C; c0 += 32) {
       const int col = c0 + lane < C ? cols[c0 + lane] - col0 : -1;
@@ -408,7 +408,8 @@ FwdWs fwd_ws(int64_t N, int64_t V, int64_t d, int C) {
   o.rows = rows_ws(N, d);
   const int64_t np = round_up(N < 1 ? 1 : N, gp::TM);
   o.piece = np < kFwdRows ? np : kFwdRows;
-  const size_t nparts = 2 * size_t((V + gp::TN - 1) / gp::TN);
+  const int width = N <= gp::HALF ? gp::slim_width(V) : gp::TN;
+  const size_t nparts = 2 * size_t((V + width - 1) / width);
   size_t at = o.rows.total;
   o.part = at; at += align256(nparts * size_t(o.piece) * sizeof(float2));
   o.zy = at; at += align256(4 * size_t(o.piece));
@@ -427,13 +428,13 @@ struct BwdWs {
 // k ranges of the dH product: its tiles (rows / 256 x d / 512) are few, so one range per tile would
 // leave the last round of CTA pairs mostly idle.  More ranges fill it and cost 8 bytes per element and
 // range (written, then read by k_head_dh).  Both sides of the choice in cycles.
-int dh_splits(int64_t rows, int64_t d, int64_t vc) {
+int dh_splits(int64_t n, int64_t rows, int64_t d, int64_t vc) {
   const int64_t m = rows / gp::TM, nkb = vc / gp::BK;
   int best = 1;
   double best_c = 0;
   for (int s = 1; s <= 32; ++s) {
     if (s > 1 && nkb / s < 16) break;
-    const double c = gp::cycles(gp::prefer_wide(m, d, nkb, s), m, d, nkb, s) + double(s) * double(rows) * double(d) * 8.0 / 3000.0;
+    const double c = gp::cycles(gp::pick_shape(n, m, d, nkb, s), m, d, nkb, s) + double(s) * double(rows) * double(d) * 8.0 / 3000.0;
     if (s == 1 || c < best_c) {
       best = s;
       best_c = c;
@@ -452,7 +453,7 @@ BwdWs bwd_ws(int64_t N, int64_t V, int64_t d, bool dh, bool dw) {
   if (vc > vp) vc = vp;
   const int64_t chunks = (vp + vc - 1) / vc;
   o.vc = round_up((vp + chunks - 1) / chunks, gp::TN);
-  o.splits = dh ? dh_splits(o.piece, d, o.vc) : 0;
+  o.splits = dh ? dh_splits(N, o.piece, d, o.vc) : 0;
   size_t at = o.rows.total;
   o.dz = at; at += align256(2 * size_t(o.piece) * size_t(o.vc));
   o.part = at; at += align256(4 * size_t(o.splits) * size_t(o.piece) * size_t(d));
@@ -500,9 +501,13 @@ cudaError_t launch_head_loss(const void* H, int64_t ldh, int64_t N, int64_t d, c
   cudaError_t e = launch_rows(H, ldh, N, d, V, y, w, nullptr, nullptr, r, loss, lse, E, C, nullptr, 0, s);
   if (e != cudaSuccess) return e;
   const int64_t np = round_up(N, gp::TM);
-  const int64_t vt = (V + gp::TN - 1) / gp::TN;
+  const bool single = N <= gp::HALF;
+  const int width = single ? gp::slim_width(V) : gp::TN;
+  const int nparts = int(2 * ((V + width - 1) / width));
   CUtensorMap mb;
-  if (!gp::map_kmajor(&mb, W, d, V, d)) return cudaErrorInvalidValue;
+  if (single ? !gp::map_2d(&mb, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, W, d, V, d, gp::BK, width / 2)
+             : !gp::map_kmajor(&mb, W, d, V, d))
+    return cudaErrorInvalidValue;
   float2* part = reinterpret_cast<float2*>(ws + lay.part);
   float* zy = reinterpret_cast<float*>(ws + lay.zy);
   float* zc = reinterpret_cast<float*>(ws + lay.zc);
@@ -513,11 +518,13 @@ cudaError_t launch_head_loss(const void* H, int64_t ldh, int64_t N, int64_t d, c
     gp::Geo g = geo(rows / gp::TM, V, (d + gp::BK - 1) / gp::BK, kSegKb, r, status);
     g.rows_live = r.count;
     g.m_first = int(p0 / gp::TM);
-    EpiStats epi{part, lay.piece, r.y + p0, zy, cols, E ? C : 0, zc, V};
-    e = gp::launch<false, false, false>(ma, mb, ma, mb, ma, g, epi, gp::NoExt{}, s);
+    EpiStats epi{part, lay.piece, r.y + p0, zy, cols, E ? C : 0, zc};
+    g.width = width;
+    e = single ? gp::launch<gp::kSingle, false, false>(ma, mb, ma, mb, ma, g, epi, gp::NoExt{}, s)
+                      : gp::launch<gp::kNarrow, false, false>(ma, mb, ma, mb, ma, g, epi, gp::NoExt{}, s);
     if (e != cudaSuccess) return e;
-    e = gp::launch_early(k_head_join, dim3(unsigned(rows / 32)), dim3(32, 2 * vt >= 128 ? 32 : 8), 0, s, part, lay.piece,
-                         int(2 * vt), r, p0, zy, zc, cols, C, loss, lse, E);
+    e = gp::launch_early(k_head_join, dim3(unsigned(rows / 32)), dim3(32, nparts >= 128 ? 32 : 8), 0, s, part, lay.piece,
+                         nparts, r, p0, zy, zc, cols, C, loss, lse, E);
     if (e != cudaSuccess) return e;
   }
   return cudaSuccess;
@@ -548,6 +555,7 @@ cudaError_t launch_head_loss_backward(const void* H, int64_t ldh, int64_t N, int
       gp::Geo g = geo(rows / gp::TM, vn, (d + gp::BK - 1) / gp::BK, kSegKb, r, status);
       g.rows_live = r.count;
       g.m_first = int(p0 / gp::TM);
+      g.rows = int(N);
       e = gp::launch_either<false, false>(mh, mw, mh, mw, mz_out, g,
                                           EpiDz{r.lse + p0, r.w + p0, r.y + p0, r.count, p0, v0, int(vn)}, gp::NoExt{}, s);
       if (e != cudaSuccess) return e;
@@ -561,6 +569,7 @@ cudaError_t launch_head_loss_backward(const void* H, int64_t ldh, int64_t N, int
         gh.rows_live = r.count;
         gh.m_first = g.m_first;
         gh.splits = lay.splits;
+        gh.rows = int(N);
         e = gp::launch_either<false, true>(mz_k, mw_mn, mz_k, mw_mn, mo, gh, EpiAcc{lay.piece, v0 > 0 ? 1 : 0},
                                            gp::NoExt{}, s);
         if (e != cudaSuccess) return e;
