@@ -16,7 +16,9 @@
 // Single: up to 128 rows of A in all (a few tokens against a vocabulary).  A pair would leave its odd CTA
 // multiplying zero rows, so each CTA works alone on 128 x 256 tiles, with the narrow shape's segments
 // and two buffers; B's read from HBM is then the bound.  With B K-major its tiles may be narrower than
-// 256 columns (`width`, a multiple of 16), so that the last round of CTAs is as full as the others.
+// 256 columns (`width`, a multiple of 16), so that the last round of CTAs is as full as the others, and
+// A's loads bring only the rows there are (the MMA's other rows read what lies behind; nobody reads
+// their sums): the ring is as deep as that allows.
 //   warp 0       TMA producer (both CTAs): its CTA's 128 rows of A and 128 rows of B per accumulator
 //   warp 1       one thread of the even CTA issues the MMAs (M = 256, N = 256, K = 16)
 //   warps 2..9   take the sums out of TMEM: warp w holds rows 32 (w & 3) .. + 31 of its CTA, one row
@@ -63,11 +65,12 @@ struct Shape {
   static constexpr int kOpsB = kShape == kNarrow ? 1 : 2;  // 128-row operands of B per CTA and stage
   static constexpr int kStageBytes = (1 + kOpsB) * OPB;
   static constexpr int kStages = 12 * OPB / kStageBytes;
-  static constexpr int kBars = 2 * kStages + 5;            // full[S], empty[S], acc_full[2], acc_empty[2], drain
+  static constexpr int kMostStages = kShape == kSingle ? 8 : kStages;
+  static constexpr int kBars = 2 * kMostStages + 5;        // full[S], empty[S], acc_full[2], acc_empty[2], drain
 };
 constexpr int SMEM = 12 * OPB + EPI_WARPS * BOX + 256 + 1024;
 static_assert(SMEM <= 232448, "shared memory per CTA");
-static_assert(Shape<kNarrow>::kBars * 8 + 8 <= 256, "barrier area");
+static_assert(Shape<kNarrow>::kBars * 8 + 8 <= 256 && Shape<kSingle>::kBars * 8 + 8 <= 256, "barrier area");
 
 // One launch's work.  Tiles are taken in groups of `group` row tiles that sweep all column tiles,
 // row tile fastest: the CTA pairs at work share a few column tiles and one group of row tiles,
@@ -77,6 +80,7 @@ struct Geo {
   int cols;              // columns of the output
   int rows;              // rows of A (host: 128 or fewer take the single shape)
   int width;             // columns of a tile (launch() sets all but the single shape's)
+  int arows, stages;     // single shape, B K-major: rows of A's boxes, stages of the ring (launch())
   int nkb;               // k-blocks of the product
   int splits;            // the k-blocks are cut into this many ranges, each a tile of its own
   int seg_kb;            // k-blocks per accumulation segment
@@ -192,22 +196,25 @@ __global__ void __cluster_dims__(Shape<kShape>::kCtas, 1, 1) __launch_bounds__(T
                 const __grid_constant__ Epi epi, const __grid_constant__ Ext ext) {
   using S = Shape<kShape>;
   constexpr bool kPair = S::kCtas == 2;
-  constexpr bool kSlim = kShape == kSingle && !kBmn;  // tiles of `width` columns: two boxes of width / 2 rows
   static_assert(kPair || !Ext::kOn, "an extended k axis takes pairs");
-  constexpr int STAGES = S::kStages, STAGE_BYTES = S::kStageBytes, BARS = S::kBars;
+  constexpr int MOST = S::kMostStages, BARS = S::kBars;
+  constexpr bool kSlim = kShape == kSingle && !kBmn;  // tiles of `width` columns: two boxes of width / 2 rows
+  const int STAGES = kSlim ? g.stages : S::kStages;
+  const uint32_t a_bytes = kSlim ? uint32_t(g.arows) * 128u : uint32_t(OPB);
+  const uint32_t STAGE_BYTES = kSlim ? a_bytes + uint32_t(g.width) * 128u : uint32_t(S::kStageBytes);
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
-  uint8_t* boxes = smem + STAGES * STAGE_BYTES;
+  uint8_t* boxes = smem + 12 * OPB;
   uint64_t* bars = reinterpret_cast<uint64_t*>(boxes + EPI_WARPS * BOX);
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + BARS);
   uint32_t* odd_issued = tmem_slot + 1;
   const uint32_t smem_base = smem_u32(smem);
   const uint32_t bar_base = smem_u32(bars);
   auto full_bar = [&](int s) { return bar_base + 8u * s; };
-  auto empty_bar = [&](int s) { return bar_base + 8u * (STAGES + s); };
-  auto acc_full = [&](uint32_t b) { return bar_base + 8u * (2 * STAGES + b); };
-  auto acc_empty = [&](uint32_t b) { return bar_base + 8u * (2 * STAGES + 2 + b); };
-  const uint32_t drain_bar = bar_base + 8u * (2 * STAGES + 4);
+  auto empty_bar = [&](int s) { return bar_base + 8u * (MOST + s); };
+  auto acc_full = [&](uint32_t b) { return bar_base + 8u * (2 * MOST + b); };
+  auto acc_empty = [&](uint32_t b) { return bar_base + 8u * (2 * MOST + 2 + b); };
+  const uint32_t drain_bar = bar_base + 8u * (2 * MOST + 4);
 
   const int warp = threadIdx.x >> 5;
   const int lane = threadIdx.x & 31;
@@ -218,7 +225,7 @@ __global__ void __cluster_dims__(Shape<kShape>::kCtas, 1, 1) __launch_bounds__(T
   const WaitCtl wc{g.status, g.abort_flag, g.limit_ns, g.mark};
 
   if (threadIdx.x == 0) {
-    for (int s = 0; s < STAGES; ++s) {
+    for (int s = 0; s < MOST; ++s) {
       mbar_init(full_bar(s), 1);
       mbar_init(empty_bar(s), 1);
     }
@@ -269,11 +276,10 @@ __global__ void __cluster_dims__(Shape<kShape>::kCtas, 1, 1) __launch_bounds__(T
             ok = false;
             break;
           }
-          if (leader) mbar_arrive_expect_tx(full_bar(stage), kSlim ? uint32_t(OPB + g.width * BK * 2)
-                                                                   : uint32_t(S::kCtas) * STAGE_BYTES);
+          if (leader) mbar_arrive_expect_tx(full_bar(stage), uint32_t(S::kCtas) * STAGE_BYTES);
           const uint32_t fb = mapa_shared(full_bar(stage), 0);
           const uint32_t a = smem_base + uint32_t(stage) * STAGE_BYTES;
-          const uint32_t b = a + OPB;
+          const uint32_t b = a + a_bytes;
           if (!Ext::kOn || j < nb) {
             const int k0 = (t.kb0 + j) * BK;
             auto load = [&](uint32_t dst, const CUtensorMap* map, int c0, int c1) {
@@ -323,8 +329,8 @@ __global__ void __cluster_dims__(Shape<kShape>::kCtas, 1, 1) __launch_bounds__(T
       constexpr uint32_t kKLbo = 16u;  // K-major with the 128-byte swizzle: leading offset unused
       const uint64_t a_kmaj = sdesc(smem_base, kKLbo, 1024u, kSwizzle128B);
       const uint64_t a0 = kAmn ? sdesc(smem_base, SUB, 1024u, kSwizzle128B) : a_kmaj;
-      const uint64_t b_kmaj = sdesc(smem_base + OPB, kKLbo, 1024u, kSwizzle128B);
-      const uint64_t b0 = kBmn ? sdesc(smem_base + OPB, SUB, 1024u, kSwizzle128B) : b_kmaj;
+      const uint64_t b_kmaj = sdesc(smem_base + a_bytes, kKLbo, 1024u, kSwizzle128B);
+      const uint64_t b0 = kBmn ? sdesc(smem_base + a_bytes, SUB, 1024u, kSwizzle128B) : b_kmaj;
       constexpr uint64_t kAStep = kAmn ? 2048 >> 4 : 32 >> 4, kBStep = kBmn ? 2048 >> 4 : 32 >> 4;
       const uint32_t id = tc::idesc(1, 1, kAmn ? 1 : 0, kBmn ? 1 : 0, S::kCtas * HALF, kSlim ? uint32_t(g.width) : TN);
       constexpr uint32_t kIdX = tc::idesc(1, 1, 0, 0, TM, TN);
@@ -690,6 +696,11 @@ inline cudaError_t launch(const CUtensorMap& a, const CUtensorMap& b, const CUte
   auto kernel = k_gemm_pair<kShape, kAmn, kBmn, Epi, Ext>;
   constexpr int kCtas = Shape<kShape>::kCtas;
   if (kShape != kSingle || kBmn || g.width == 0) g.width = Shape<kShape>::kCols;
+  if (kShape == kSingle && !kBmn) {
+    if (g.arows == 0) g.arows = HALF;
+    const int s = 12 * OPB / ((g.arows + g.width) * 128);
+    g.stages = s < Shape<kSingle>::kMostStages ? s : Shape<kSingle>::kMostStages;
+  }
   g.n_tiles = (g.cols + g.width - 1) / g.width;
   cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM);
   if (e != cudaSuccess) return e;

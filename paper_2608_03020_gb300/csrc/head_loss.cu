@@ -514,12 +514,15 @@ cudaError_t launch_head_loss(const void* H, int64_t ldh, int64_t N, int64_t d, c
   for (int64_t p0 = 0; p0 < np; p0 += lay.piece) {
     const int64_t rows = np - p0 < lay.piece ? np - p0 : lay.piece;
     CUtensorMap ma;
-    if (!gp::map_kmajor(&ma, r.H + p0 * d, d, rows, d)) return cudaErrorInvalidValue;
+    const int arows = single ? int(round_up(N, 8)) : gp::HALF;
+    if (!gp::map_2d(&ma, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, r.H + p0 * d, d, rows, d, gp::BK, arows))
+      return cudaErrorInvalidValue;
     gp::Geo g = geo(rows / gp::TM, V, (d + gp::BK - 1) / gp::BK, kSegKb, r, status);
     g.rows_live = r.count;
     g.m_first = int(p0 / gp::TM);
     EpiStats epi{part, lay.piece, r.y + p0, zy, cols, E ? C : 0, zc};
     g.width = width;
+    g.arows = arows;
     e = single ? gp::launch<gp::kSingle, false, false>(ma, mb, ma, mb, ma, g, epi, gp::NoExt{}, s)
                       : gp::launch<gp::kNarrow, false, false>(ma, mb, ma, mb, ma, g, epi, gp::NoExt{}, s);
     if (e != cudaSuccess) return e;
