@@ -197,7 +197,7 @@ __global__ void __launch_bounds__(kTile) k_plan_pairs(int32_t* plan, PlanLay p) 
     if (w < warp) at += warp_sum[w];
     total += warp_sum[w];
   }
-  if (alone) {
+  if (alone && LOCA_CHECK(b0 + at, p.smax)) {
     plan[p.pair_ad + b0 + at] = a1;
     plan[p.pair_s0 + b0 + at] = -1;
     plan[p.pair_s1 + b0 + at] = b1 + j;
@@ -299,7 +299,7 @@ __global__ void __launch_bounds__(256)
     for (int q = 0; q < kParts; ++q) {
       const __nv_bfloat16 h = __float2bfloat16_rn(x);
       x -= __bfloat162float(h);
-      if (q == 0) (isb ? pb : pa)[e] = h;
+      if (q == 0 && LOCA_CHECK(e, isb ? nb : na)) (isb ? pb : pa)[e] = h;
       all[q * kp] = h;
     }
   }
@@ -664,7 +664,8 @@ __global__ void __launch_bounds__(kTokThreads) k_adapter_tokens(const TokGeo g) 
     float s = 0.f;
 #pragma unroll
     for (int w = 0; w < kTokThreads / 32; ++w) s += part[w][threadIdx.x];
-    g.out[(int64_t(blockIdx.x) * g.N + n) * g.kp + threadIdx.x] = spoiled ? __int_as_float(0x7fffffff) : s;
+    if (LOCA_CHECK((int64_t(blockIdx.x) * g.N + n) * g.kp + threadIdx.x, int64_t(g.ranges) * g.N * g.kp))
+      g.out[(int64_t(blockIdx.x) * g.N + n) * g.kp + threadIdx.x] = spoiled ? __int_as_float(0x7fffffff) : s;
   }
 }
 
@@ -1345,7 +1346,7 @@ __global__ void __launch_bounds__(256)
       v.w += __shfl_xor_sync(0xffffffffu, v.w, o);
     }
     const int col = c + lane4;
-    if (on && col < k) {
+    if (on && col < k && LOCA_CHECK(row * k + col, j.rows * k)) {
       float x = lane4 == 0 ? v.x : lane4 == 1 ? v.y : lane4 == 2 ? v.z : v.w;
       if (j.scale) x *= j.scale[a];
       if constexpr (sizeof(T) == 4) static_cast<float*>(j.out)[row * k + col] = x;

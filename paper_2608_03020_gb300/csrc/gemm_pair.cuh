@@ -613,28 +613,6 @@ inline bool map_out_bf16(CUtensorMap* m, void* base, int64_t cols, int64_t rows,
   return map_2d(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, base, cols, rows, pitch, 64, 32);
 }
 
-// Tiles at work at once: pairs of CTAs (76 on 152 SMs), or CTAs.
-template <class K>
-inline int resident_tiles(K kernel, int ctas) {
-  int clusters = sm_count() / ctas;
-  if (ctas == 1) return clusters;
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(unsigned(2 * clusters));
-  cfg.blockDim = dim3(THREADS);
-  cfg.dynamicSmemBytes = SMEM;
-  cudaLaunchAttribute at[1];
-  at[0].id = cudaLaunchAttributeClusterDimension;
-  at[0].val.clusterDim.x = 2;
-  at[0].val.clusterDim.y = 1;
-  at[0].val.clusterDim.z = 1;
-  cfg.attrs = at;
-  cfg.numAttrs = 1;
-  int n = 0;
-  if (cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) == cudaSuccess && n > 0 && n < clusters) clusters = n;
-  cudaGetLastError();
-  return clusters;
-}
-
 // Small kernels between those with 200 KB of shared memory ask for the same split of L1: changing it
 // drains the SM (64 single tokens through an adapted projection: 27.1 us with the change, 23.4 without).
 template <class K>
@@ -704,9 +682,9 @@ inline cudaError_t launch(const CUtensorMap& a, const CUtensorMap& b, const CUte
   g.n_tiles = (g.cols + g.width - 1) / g.width;
   cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM);
   if (e != cudaSuccess) return e;
-  static const int at_once = resident_tiles(kernel, kCtas);
   const int64_t total = int64_t(g.m_tiles) * g.n_tiles * g.splits;
   if (total < 1) return cudaSuccess;
+  const int at_once = sm_count() / kCtas;  // pairs (76 on 152 SMs) or CTAs at work at once
   const int n = total < at_once ? int(total) : at_once;
   return launch_early(kernel, dim3(unsigned(kCtas * n)), dim3(THREADS), SMEM, s, a, b, ax, bx, o, g, epi, ext);
 }

@@ -58,6 +58,7 @@ __device__ __forceinline__ Chunk chunk_of(const List<kCap>& l, int c) {
   const int64_t numel = l.numel_type[lo] >> 1;
   k.first = int64_t(c - (lo ? l.chunk_end[lo - 1] : 0)) * kChunk;
   k.count = int(numel - k.first < kChunk ? numel - k.first : kChunk);
+  if (!LOCA_CHECK_SPAN(k.first, k.count, numel)) k.count = 0;
   return k;
 }
 

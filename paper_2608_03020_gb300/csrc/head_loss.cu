@@ -131,6 +131,7 @@ __global__ void __launch_bounds__(256)
     if (n >= N) break;
     const int p = place[i];
     if (p >= 0) {
+      if (!LOCA_CHECK_SPAN(int64_t(p) * d, d, npad * d)) break;
       const uint4* src = reinterpret_cast<const uint4*>(H + n * ldh);
       uint4* dst = reinterpret_cast<uint4*>(out.H + int64_t(p) * d);
 #pragma unroll 8
@@ -299,7 +300,7 @@ __global__ void __launch_bounds__(1024)
   const int64_t row = int64_t(blockIdx.x) * 32 + threadIdx.x;
   const bool live = row_first + row < *in.count;
   float m = -INFINITY, s = 0.f;
-  if (live) {
+  if (live && LOCA_CHECK(row, pitch)) {
     constexpr int kAhead = 8;
     for (int p0 = threadIdx.y; p0 < nparts; p0 += kAhead * int(blockDim.y)) {
       float2 q[kAhead];
