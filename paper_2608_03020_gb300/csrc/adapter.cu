@@ -274,36 +274,55 @@ __device__ __forceinline__ float as_float<float>(float x) { return x; }
 template <>
 __device__ __forceinline__ float as_float<__nv_bfloat16>(__nv_bfloat16 x) { return __bfloat162float(x); }
 
+// One thread per 8 columns of a padded row: one 16-byte store for each copy of a part.
 template <class T>
 __global__ void __launch_bounds__(256)
     k_adapter_pack(const T* __restrict__ A, const T* __restrict__ B, int n, int64_t d_in, int64_t d_out, int k, int kp,
                    const float* __restrict__ scale, __nv_bfloat16* __restrict__ pa, __nv_bfloat16* __restrict__ pb,
                    __nv_bfloat16* __restrict__ all_a, __nv_bfloat16* __restrict__ all_b, float* __restrict__ ps,
                    int32_t* __restrict__ marks) {
-  const int64_t na = int64_t(n) * d_in * kp, nb = int64_t(n) * d_out * kp;
-  const int64_t stride = int64_t(gridDim.x) * blockDim.x;
-  for (int64_t i = int64_t(blockIdx.x) * blockDim.x + threadIdx.x; i < na + nb; i += stride) {
-    const bool isb = i >= na;
-    const int64_t e = isb ? i - na : i;
-    const int64_t row = e / kp;
-    const int c = int(e - row * kp);
-    float x = 0.f;
-    if (c < k) x = as_float<T>(isb ? B[row * k + c] : A[row * k + c]);
-    if (isb && scale) x *= scale[row / d_out];
-    if (!isfinite(__bfloat162float(__float2bfloat16_rn(x)))) {
-      x = 0.f;
-      marks[row / (isb ? d_out : d_in)] = 1;
+  const int per_row = kp / 8;
+  const int64_t rows_a = int64_t(n) * d_in, rows_b = int64_t(n) * d_out;
+  const int64_t stride = int64_t(gridDim.x) * blockDim.x, first = int64_t(blockIdx.x) * blockDim.x + threadIdx.x;
+  for (int64_t i = first; i < (rows_a + rows_b) * per_row; i += stride) {
+    const int64_t flat = i / per_row;
+    const int c = int(i - flat * per_row) * 8;
+    const bool isb = flat >= rows_a;
+    const int64_t row = isb ? flat - rows_a : flat;
+    const T* src = (isb ? B : A) + row * k + c;
+    const int have = k - c < 8 ? (k - c < 0 ? 0 : k - c) : 8;
+    float x[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) x[j] = j < have ? as_float<T>(src[j]) : 0.f;
+    const int64_t a = row / (isb ? d_out : d_in);
+    if (isb && scale) {
+      const float s = scale[a];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) x[j] *= s;
     }
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      if (!isfinite(__bfloat162float(__float2bfloat16_rn(x[j])))) {
+        x[j] = 0.f;
+        marks[a] = 1;
+      }
     __nv_bfloat16* all = (isb ? all_b : all_a) + row * (kParts * kp) + c;
+    __nv_bfloat16* one = (isb ? pb : pa) + row * kp + c;
+    if (!LOCA_CHECK_SPAN(row * kp + c, 8, (isb ? rows_b : rows_a) * kp)) continue;
 #pragma unroll
     for (int q = 0; q < kParts; ++q) {
-      const __nv_bfloat16 h = __float2bfloat16_rn(x);
-      x -= __bfloat162float(h);
-      if (q == 0 && LOCA_CHECK(e, isb ? nb : na)) (isb ? pb : pa)[e] = h;
-      all[q * kp] = h;
+      __align__(16) __nv_bfloat16 h[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        h[j] = __float2bfloat16_rn(x[j]);
+        x[j] -= __bfloat162float(h[j]);
+      }
+      const uint4 v = *reinterpret_cast<const uint4*>(h);
+      if (q == 0) *reinterpret_cast<uint4*>(one) = v;
+      *reinterpret_cast<uint4*>(all + q * kp) = v;
     }
   }
-  for (int64_t i = int64_t(blockIdx.x) * blockDim.x + threadIdx.x; i < n; i += stride) ps[i] = scale ? scale[i] : 1.f;
+  for (int64_t i = first; i < n; i += stride) ps[i] = scale ? scale[i] : 1.f;
 }
 
 // ------------------------------------------------------------------ U and T: tokens x k sums over d
@@ -915,17 +934,27 @@ __global__ void __launch_bounds__(kFewThreads, 1)
     const int i = (warp - 2) * 32 + lane;
     const int64_t o = o0 + i;
     const uint32_t red_s = smem_u32(red);
-    for (int t = 0; t < own; ++t) {
-      const int n = rank + ks * t;
-      if (n >= ntok) break;
-      float x[8];  // all loads first: one round trip
+    constexpr int kAhead = 4;  // tokens whose sums are on the way at once
+    for (int t0 = 0; t0 < own; t0 += kAhead) {
+      float x[kAhead][8];
 #pragma unroll
-      for (int j = 0; j < 8; ++j)
-        x[j] = j < ks ? ld_shared_cluster_f32(mapa_shared(red_s + 4u * uint32_t(n * 128 + i), uint32_t(j))) : 0.f;
-      float y = g.tokens ? low[t * 128 + i] : 0.f;
+      for (int q = 0; q < kAhead; ++q) {
+        const int n = rank + ks * (t0 + q);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) y += x[j];
-      if (o < g.o && LOCA_CHECK(n0 + n, g.N)) g.Y[(n0 + n) * g.ldy + o] = __float2bfloat16_rn(y);
+        for (int j = 0; j < 8; ++j)
+          x[q][j] = j < ks && n < ntok
+                        ? ld_shared_cluster_f32(mapa_shared(red_s + 4u * uint32_t(n * 128 + i), uint32_t(j)))
+                        : 0.f;
+      }
+#pragma unroll
+      for (int q = 0; q < kAhead; ++q) {
+        const int n = rank + ks * (t0 + q);
+        if (n >= ntok) break;
+        float y = g.tokens ? low[(t0 + q) * 128 + i] : 0.f;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) y += x[q][j];
+        if (o < g.o && LOCA_CHECK(n0 + n, g.N)) g.Y[(n0 + n) * g.ldy + o] = __float2bfloat16_rn(y);
+      }
     }
   }
   if (warp == 0 && lane == 0) {
@@ -1528,7 +1557,8 @@ cudaError_t project(const Call& c, const void* X, int64_t ldx, int64_t d, const 
   const bool few = token_sums || c.N <= kTile || 2 * tiles < sm_count() / 2;
   CUtensorMap mw, mx, mb, mu;
   if (kWmn ? !gp::map_mnmajor(&mw, W, o, d, o) : !gp::map_kmajor(&mw, W, d, o, d)) return cudaErrorInvalidValue;
-  if (!gp::map_3d(&mb, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, P, c.kp, o, c.n, c.kp, o * c.kp, 64, 128))
+  if (token_sums) mb = mw;  // (not loaded from)
+  else if (!gp::map_3d(&mb, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, P, c.kp, o, c.n, c.kp, o * c.kp, 64, 128))
     return cudaErrorInvalidValue;
   if (few) {
     FewGeo g{};
@@ -1688,7 +1718,7 @@ cudaError_t launch_adapter_pack(const void* A, const void* B, int dtype, int n, 
   const cudaError_t e = cudaMemsetAsync(marks, 0, 4 * size_t(n), s);
   if (e != cudaSuccess) return e;
   const int kp = k_padded(k);
-  const int64_t values = int64_t(n) * (d_in + d_out) * kp;
+  const int64_t values = int64_t(n) * (d_in + d_out) * (kp / 8);
   const unsigned blocks = unsigned(values / 256 + 1 < 8 * sm_count() ? values / 256 + 1 : 8 * sm_count());
   if (dtype == LOCA_F32)
     k_adapter_pack<float><<<blocks, 256, 0, s>>>(static_cast<const float*>(A), static_cast<const float*>(B), n, d_in,

@@ -341,29 +341,42 @@ __global__ void __launch_bounds__(1024)
   }
 }
 
+// One thread per 8 elements of a row; the k ranges' sums are loaded four at a time and added in order.
 __global__ void __launch_bounds__(256)
     k_head_dh(const float* __restrict__ part, int64_t rows, int splits, int64_t d, Rows in, int64_t row_first,
               float scale, __nv_bfloat16* __restrict__ dH, int64_t lddh) {
-  const int64_t dv = d / 8;
-  const int64_t row = int64_t(blockIdx.x);
   wait_for_previous();
   launch_dependents();
-  if (row_first + row >= *in.count) return;
-  const int64_t n = in.idx[row_first + row];
-  for (int64_t j = threadIdx.x; j < dv; j += blockDim.x) {
+  const int dv = int(d / 8);
+  const int64_t live = *in.count - row_first;
+  const int64_t total = (live < rows ? live : rows) * dv;
+  for (int64_t e = int64_t(blockIdx.x) * blockDim.x + threadIdx.x; e < total; e += int64_t(gridDim.x) * blockDim.x) {
+    const int64_t row = e / dv;
+    const int64_t at = row * d + 8 * (e - row * dv);
+    const int64_t n = in.idx[row_first + row];
     float a[8] = {};
-    for (int s = 0; s < splits; ++s) {
-      const float4* p = reinterpret_cast<const float4*>(part + (int64_t(s) * rows + row) * d + 8 * j);
-      const float4 x = p[0], z = p[1];
-      a[0] += x.x; a[1] += x.y; a[2] += x.z; a[3] += x.w;
-      a[4] += z.x; a[5] += z.y; a[6] += z.z; a[7] += z.w;
+    for (int s0 = 0; s0 < splits; s0 += 4) {
+      float4 x[4][2];
+#pragma unroll
+      for (int s = 0; s < 4; ++s)
+        if (s0 + s < splits) {
+          const float4* p = reinterpret_cast<const float4*>(part + int64_t(s0 + s) * rows * d + at);
+          x[s][0] = p[0];
+          x[s][1] = p[1];
+        }
+#pragma unroll
+      for (int s = 0; s < 4; ++s)
+        if (s0 + s < splits) {
+          a[0] += x[s][0].x; a[1] += x[s][0].y; a[2] += x[s][0].z; a[3] += x[s][0].w;
+          a[4] += x[s][1].x; a[5] += x[s][1].y; a[6] += x[s][1].z; a[7] += x[s][1].w;
+        }
     }
     uint4 q;
     q.x = gp::pack_bf16(scale * a[0], scale * a[1]);
     q.y = gp::pack_bf16(scale * a[2], scale * a[3]);
     q.z = gp::pack_bf16(scale * a[4], scale * a[5]);
     q.w = gp::pack_bf16(scale * a[6], scale * a[7]);
-    *reinterpret_cast<uint4*>(dH + n * lddh + 8 * j) = q;
+    *reinterpret_cast<uint4*>(dH + n * lddh + (at - row * d)) = q;
   }
 }
 
@@ -591,7 +604,9 @@ cudaError_t launch_head_loss_backward(const void* H, int64_t ldh, int64_t N, int
       }
     }
     if (dH) {
-      e = gp::launch_early(k_head_dh, dim3(unsigned(rows)), dim3(256), 0, s, part, lay.piece, lay.splits, d, r, p0, scale,
+      const int64_t blocks = rows * (d / 8) / 256 + 1;
+      const int64_t most = 8 * int64_t(sm_count());
+      e = gp::launch_early(k_head_dh, dim3(unsigned(blocks < most ? blocks : most)), dim3(256), 0, s, part, lay.piece, lay.splits, d, r, p0, scale,
                            static_cast<__nv_bfloat16*>(dH), lddh);
       if (e != cudaSuccess) return e;
     }
