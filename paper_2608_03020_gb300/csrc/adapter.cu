@@ -438,8 +438,11 @@ __global__ void __launch_bounds__(kShrinkThreads, 1)
   fence_after();
   const uint32_t tmem_base = *tmem_slot;
   wait_for_previous();
+  if (blockIdx.x == 0 && threadIdx.x == 0) {
+    *g.abort_flag = 0;  // a captured call that gave up may be replayed
+    __threadfence();    // the product may start, and read the flag, from the next line on
+  }
   launch_dependents();
-  if (blockIdx.x == 0 && threadIdx.x == 0) *g.abort_flag = 0;  // a captured call that gave up may be replayed
   const int total = g.plan[g.p.tile_base + g.p.tiles];
   const int seg_kb = g.parts == 1 ? 64 : kShrinkSeg;
 
@@ -634,8 +637,11 @@ __global__ void __launch_bounds__(kTokThreads) k_adapter_tokens(const TokGeo g) 
   __shared__ float part[kTokThreads / 32][kMaxK];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   wait_for_previous();
+  if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) {
+    *g.abort_flag = 0;
+    __threadfence();
+  }
   launch_dependents();
-  if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) *g.abort_flag = 0;
   const int64_t n = blockIdx.y;
   const int a = g.tok_adapter[n];
   if (a < 0) return;  // k_adapter_few does not read this token's sums
@@ -778,6 +784,7 @@ __global__ void __launch_bounds__(kFewThreads, 1)
   __syncthreads();
   fence_after();
   const uint32_t tmem_base = *tmem_slot;
+  launch_dependents();
   // the launch that makes U lets this one start only once everything before it has completed: X, W,
   // the packed adapters and the plan may be read now, U only after wait_for_previous()
   const int nkb = int((g.d + 63) / 64);

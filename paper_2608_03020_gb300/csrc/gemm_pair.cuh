@@ -252,7 +252,10 @@ __global__ void __cluster_dims__(Shape<kShape>::kCtas, 1, 1) __launch_bounds__(T
   cluster_sync();
   fence_after();
   const uint32_t tmem_base = *tmem_slot;
-  wait_for_previous();  // the launch before has completed (the prologue above ran beside its end)
+  // The launch before has completed (the prologue above ran beside its end).  With an extended k axis
+  // only the extension is that launch's work, which let this one start after all launches before it had
+  // completed: the producer waits when it comes to the extension.
+  if (!Ext::kOn) wait_for_previous();
   launch_dependents();
   const Live lv = live_of(g);
   uint32_t iters_done = 0;
@@ -263,7 +266,7 @@ __global__ void __cluster_dims__(Shape<kShape>::kCtas, 1, 1) __launch_bounds__(T
       int stage = 0;
       uint32_t phase = 0;
       uint32_t iter = 0;
-      bool ok = true;
+      bool ok = true, waited = !Ext::kOn;
       for (int it = cid; it < lv.total && ok; it += ncl) {
         const Tile t = tile_of(g, lv, it);
         const int m0 = t.m * TM + int(rank) * HALF;
@@ -306,6 +309,10 @@ __global__ void __cluster_dims__(Shape<kShape>::kCtas, 1, 1) __launch_bounds__(T
               }
             }
           } else {
+            if (!waited) {
+              wait_for_previous();
+              waited = true;
+            }
             int a_row, at;
             ext.entry(t.m, j - nb, rank, a_row, at);
             tma_load_2d_pair(a, &tmAx, fb, 0, a_row);
@@ -316,6 +323,7 @@ __global__ void __cluster_dims__(Shape<kShape>::kCtas, 1, 1) __launch_bounds__(T
           if (++stage == STAGES) { stage = 0; phase ^= 1u; }
         }
       }
+      if (!waited) wait_for_previous();  // this launch ends after the one before it
       if (!leader) st_shared_cluster_u32(mapa_shared(smem_u32(odd_issued), 0), iter);
       iters_done = iter;
     }
