@@ -714,6 +714,7 @@ struct FewGeo {
   int ksteps;            // MMA steps of 16 per slot
   int tokens;            // 1: the low-rank term token by token
   int kp, ranges;        // tokens: U's columns and partial sums
+  int held;              // tokens: how many tokens' rows of s B come to shared memory beforehand
   const float* U;        // tokens: ranges x N x kp
   const __nv_bfloat16* B;  // tokens: adapter x o x kp
   const int32_t* plan;
@@ -732,9 +733,57 @@ __host__ __device__ inline int few_ring(int nt, int stages) {
 // tokens of a tile that one of ks CTAs finishes
 __host__ __device__ inline int few_own(int nt, int ks) { return (nt + ks - 1) / ks; }
 __host__ __device__ inline int few_low(int nt, int ks, int kp) { return few_own(nt, ks) * (512 + 4 * kp + 4); }
-int few_smem(int nt, int stages, int low) { return few_ring(nt, stages) + low + 512 + 1024; }
+// bytes of a token's 128 rows of s B
+__host__ __device__ inline int few_rows(int kp) { return 256 * kp; }
+int few_smem(int nt, int stages, int low, int held, int kp) {
+  return few_ring(nt, stages) + 512 + held * few_rows(kp) + low + 1024;
+}
 
 __device__ __forceinline__ void epi_bar() { asm volatile("bar.sync 1, 128;" ::: "memory"); }
+
+// The sums of up to kSplits CTAs and the low-rank term, for the tokens rank + ks t of this CTA: an
+// epilogue warp takes a token, a lane four channels.  kAhead tokens are on the way at once: many where
+// a CTA has many and no other's sums to fetch (one channel a lane: 512 tokens by 3584 channels at
+// d = 1024 23.4 us, so 12.3), one at a time in a wide cluster, where more only made the code longer (64
+// tokens at d = 3584 20.5 us with four).
+template <int kSplits, int kAhead>
+__device__ __forceinline__ void few_out(const FewGeo& g, const float* low, float* red, int own, int ks, int rank,
+                                        int64_t n0, int ntok, int o0) {
+  const int warp = int(threadIdx.x >> 5) - 2, c = 4 * int(threadIdx.x & 31);
+  constexpr int kWarps = 4;
+  const uint32_t red_s = smem_u32(red);
+  const bool in = o0 + c < g.o;  // d_out is a multiple of 8
+  for (int t0 = warp; t0 < own; t0 += kAhead * kWarps) {
+    float4 x[kAhead][kSplits];
+#pragma unroll
+    for (int q = 0; q < kAhead; ++q) {
+      const int n = rank + ks * (t0 + q * kWarps);
+#pragma unroll
+      for (int j = 0; j < kSplits; ++j)
+        if (j < ks && n < ntok) {
+          const int at = n * 128 + c;
+          x[q][j] = kSplits == 1 ? *reinterpret_cast<const float4*>(red + at)
+                                 : ld_shared_cluster_f32x4(mapa_shared(red_s + 4u * uint32_t(at), uint32_t(j)));
+        } else {
+          x[q][j] = make_float4(0.f, 0.f, 0.f, 0.f);
+        }
+    }
+#pragma unroll
+    for (int q = 0; q < kAhead; ++q) {
+      const int t = t0 + q * kWarps, n = rank + ks * t;
+      if (n >= ntok) break;
+      float4 y = g.tokens ? *reinterpret_cast<const float4*>(low + t * 128 + c) : make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+      for (int j = 0; j < kSplits; ++j) {
+        y.x += x[q][j].x; y.y += x[q][j].y; y.z += x[q][j].z; y.w += x[q][j].w;
+      }
+      if (in && LOCA_CHECK(n0 + n, g.N)) {
+        __nv_bfloat162 h[2] = {__floats2bfloat162_rn(y.x, y.y), __floats2bfloat162_rn(y.z, y.w)};
+        *reinterpret_cast<uint2*>(g.Y + (n0 + n) * g.ldy + o0 + c) = *reinterpret_cast<const uint2*>(h);
+      }
+    }
+  }
+}
 
 template <bool kWmn>
 __global__ void __launch_bounds__(kFewThreads, 1)
@@ -749,13 +798,15 @@ __global__ void __launch_bounds__(kFewThreads, 1)
   uint64_t* bars = reinterpret_cast<uint64_t*>(smem + few_ring(g.nt, g.stages));
   const uint32_t bar_base = smem_u32(bars);
   constexpr int kBarStages = 12;
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 * kBarStages + 1);
-  float* low = reinterpret_cast<float*>(smem + few_ring(g.nt, g.stages) + 512);  // [own][128] low-rank term
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 * kBarStages + 2);
+  uint8_t* rows = smem + few_ring(g.nt, g.stages) + 512;                        // [held][128][kp] bf16 of s B
+  float* low = reinterpret_cast<float*>(rows + g.held * few_rows(g.kp));        // [own][128] low-rank term
   float* us = low + own * 128;                                                  // [own][kp] U
   int32_t* ad = reinterpret_cast<int32_t*>(us + own * g.kp);                    // [own] adapters
   auto full_bar = [&](int s) { return bar_base + 8u * s; };
   auto empty_bar = [&](int s) { return bar_base + 8u * (kBarStages + s); };
   const uint32_t acc_full = bar_base + 8u * (2 * kBarStages);
+  const uint32_t rows_full = bar_base + 8u * (2 * kBarStages + 1);
   float* red = reinterpret_cast<float*>(smem);  // [token][128 channels], in the ring's place
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -773,6 +824,7 @@ __global__ void __launch_bounds__(kFewThreads, 1)
       mbar_init(empty_bar(s), 1);
     }
     mbar_init(acc_full, 1);
+    mbar_init(rows_full, 1);
     mbar_init_fence();
     prefetch_tensormap(&tmW);
     prefetch_tensormap(&tmX);
@@ -861,29 +913,70 @@ __global__ void __launch_bounds__(kFewThreads, 1)
       // this CTA's tokens n0 + rank + ks t: U's partial sums in order, then a row of s B per thread
       for (int t = i; t < own; t += 128) ad[t] = rank + ks * t < ntok ? g.plan[g.tok_adapter + n0 + rank + ks * t] : -1;
       epi_bar();
-      if (o0 + i < g.o)
-        for (int t = 0; t < own; ++t)
+      const int64_t o = o0 + i;
+      if (warp == 2) {
+        const int64_t left = g.o - o0;
+        const uint32_t bytes = uint32_t(left < 128 ? left : 128) * 2u * uint32_t(g.kp);
+        uint32_t n = 0;
+        for (int t = 0; t < g.held; ++t) n += ad[t] >= 0 ? 1u : 0u;
+        if (lane == 0) mbar_arrive_expect_tx(rows_full, n * bytes);
+        __syncwarp();
+        for (int t = lane; t < g.held; t += 32)
+          if (ad[t] >= 0)
+            bulk_load(smem_u32(rows + t * few_rows(g.kp)), g.B + (int64_t(ad[t]) * g.o + o0) * g.kp, bytes, rows_full);
+      }
+      if (o < g.o)
+        for (int t = g.held; t < own; ++t)
           if (ad[t] >= 0) {
-            const __nv_bfloat16* p = g.B + (int64_t(ad[t]) * g.o + o0 + i) * g.kp;
+            const __nv_bfloat16* p = g.B + (int64_t(ad[t]) * g.o + o) * g.kp;
             for (int c = 0; c < g.kp; c += 16) asm volatile("prefetch.global.L2 [%0];" ::"l"(p + c));
           }
       wait_for_previous();
-      for (int e = i; e < own * g.kp; e += 128) {
-        const int t = e / g.kp, c = e - t * g.kp;
-        float u = 0.f;
+      for (int e = i; e < own * (g.kp / 4); e += 128) {
+        const int t = e / (g.kp / 4), c = 4 * (e - t * (g.kp / 4));
+        float4 u = make_float4(0.f, 0.f, 0.f, 0.f);
         if (ad[t] >= 0) {
           const float* p = g.U + (n0 + rank + ks * t) * g.kp + c;
-          float x[8];
+          float4 x[8];
 #pragma unroll
-          for (int r = 0; r < 8; ++r) x[r] = r < g.ranges ? p[r * g.N * g.kp] : 0.f;
+          for (int r = 0; r < 8; ++r)
+            x[r] = r < g.ranges ? *reinterpret_cast<const float4*>(p + r * g.N * g.kp) : make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-          for (int r = 0; r < 8; ++r) u += x[r];
+          for (int r = 0; r < 8; ++r) {
+            u.x += x[r].x; u.y += x[r].y; u.z += x[r].z; u.w += x[r].w;
+          }
         }
-        us[e] = u;
+        *reinterpret_cast<float4*>(us + 4 * e) = u;
       }
       epi_bar();
-      const int64_t o = o0 + i;
-      for (int t0 = 0; t0 < own; t0 += 4) {  // four tokens' rows in flight
+      if (g.held > 0) {
+        mbar_wait(rows_full, 0, wc);
+        // 16-byte chunks of a row in an order of the thread's own: no bank conflicts
+        const int nc = g.kp / 8, c0 = (i * nc / 8) % nc;
+        for (int t0 = 0; t0 < g.held; t0 += 4) {
+          float y[4] = {};
+          for (int q = 0, c = c0; q < nc; ++q, c = c + 1 < nc ? c + 1 : 0) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              const int t = t0 + j < g.held ? t0 + j : t0;
+              const uint4 v = *reinterpret_cast<const uint4*>(rows + t * few_rows(g.kp) + i * 2 * g.kp + 16 * c);
+              const __nv_bfloat162* h = reinterpret_cast<const __nv_bfloat162*>(&v);
+              const float4* u = reinterpret_cast<const float4*>(us + t * g.kp + 8 * c);
+              const float4 ua = u[0], ub = u[1];
+              const float2 f0 = __bfloat1622float2(h[0]), f1 = __bfloat1622float2(h[1]);
+              const float2 f2 = __bfloat1622float2(h[2]), f3 = __bfloat1622float2(h[3]);
+              y[j] = fmaf(ua.x, f0.x, y[j]); y[j] = fmaf(ua.y, f0.y, y[j]);
+              y[j] = fmaf(ua.z, f1.x, y[j]); y[j] = fmaf(ua.w, f1.y, y[j]);
+              y[j] = fmaf(ub.x, f2.x, y[j]); y[j] = fmaf(ub.y, f2.y, y[j]);
+              y[j] = fmaf(ub.z, f3.x, y[j]); y[j] = fmaf(ub.w, f3.y, y[j]);
+            }
+          }
+#pragma unroll
+          for (int j = 0; j < 4; ++j)  // (without an adapter, or past d_out, nothing has come to the row)
+            if (t0 + j < g.held) low[(t0 + j) * 128 + i] = ad[t0 + j] >= 0 && o < g.o ? y[j] : 0.f;
+        }
+      }
+      for (int t0 = g.held; t0 < own; t0 += 4) {  // four tokens' rows in flight
         float y[4] = {};
         for (int c = 0; c < g.kp; c += 16) {
           uint4 v[4][2];
@@ -938,31 +1031,9 @@ __global__ void __launch_bounds__(kFewThreads, 1)
   cluster_sync();
   fence_after();
   if (warp >= 2) {
-    const int i = (warp - 2) * 32 + lane;
-    const int64_t o = o0 + i;
-    const uint32_t red_s = smem_u32(red);
-    constexpr int kAhead = 4;  // tokens whose sums are on the way at once
-    for (int t0 = 0; t0 < own; t0 += kAhead) {
-      float x[kAhead][8];
-#pragma unroll
-      for (int q = 0; q < kAhead; ++q) {
-        const int n = rank + ks * (t0 + q);
-#pragma unroll
-        for (int j = 0; j < 8; ++j)
-          x[q][j] = j < ks && n < ntok
-                        ? ld_shared_cluster_f32(mapa_shared(red_s + 4u * uint32_t(n * 128 + i), uint32_t(j)))
-                        : 0.f;
-      }
-#pragma unroll
-      for (int q = 0; q < kAhead; ++q) {
-        const int n = rank + ks * (t0 + q);
-        if (n >= ntok) break;
-        float y = g.tokens ? low[(t0 + q) * 128 + i] : 0.f;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) y += x[q][j];
-        if (o < g.o && LOCA_CHECK(n0 + n, g.N)) g.Y[(n0 + n) * g.ldy + o] = __float2bfloat16_rn(y);
-      }
-    }
+    if (ks == 1) few_out<1, 8>(g, low, red, own, 1, 0, n0, ntok, o0);
+    else if (ks <= 4) few_out<4, 2>(g, low, red, own, ks, rank, n0, ntok, o0);
+    else few_out<8, 1>(g, low, red, own, ks, rank, n0, ntok, o0);
   }
   if (warp == 0 && lane == 0) {
     const uint32_t n = uint32_t(g.stages);
@@ -970,6 +1041,7 @@ __global__ void __launch_bounds__(kFewThreads, 1)
       mbar_drain(full_bar(int(i % n)), (i / n) & 1u, kDrainLimitNs);
   }
   if (warp == 1 && lane == 0) mbar_drain(acc_full, 0, kDrainLimitNs);
+  if (warp == 2 && lane == 0 && g.tokens) mbar_drain(rows_full, 0, kDrainLimitNs);
   __syncwarp();
   fence_before();
   cluster_sync();  // no CTA leaves while its peers read its sums
@@ -1392,10 +1464,12 @@ __global__ void __launch_bounds__(256)
 }
 
 // ------------------------------------------------------------------ host side
-// Token by token, or by slots: a batch in which one adapter serves few tokens (there are more than
-// N / 4 adapters) spends one slot per token or two.  64 tokens with an adapter each at d = 3584,
-// k = 16: 30 us by slots; measured both ways below.
-bool by_token(int64_t N, int n) { return N <= 16 || (N <= 512 && 4 * int64_t(n) > N); }
+// Token by token, or by slots.  A token costs the read of its adapter whoever else has it, a slot a
+// tile of X.  At d_in = 3584, d_out = 2048: 9 us + 0.0039 N kp (64 tokens 12 us with k = 16, 25 with 64;
+// 400 tokens 33 and 113) against 12 us + 0.23 a slot whatever k (64 tokens 12 us in one slot, 20 in 32,
+// 27 in 64; 400 tokens 22 us in 4, 65 in 200).  The host does not know the slots: half of what they may
+// come to is the guess.  Measured up to 512 tokens.
+bool by_token(int64_t N, int n, int k) { return N <= 512 && N * k_padded(k) < 768 + 30 * plan_lay(N, n).smax; }
 // Ranges of d for the token kernel: about four blocks per SM.
 int tok_ranges(int64_t N, int64_t d) {
   int64_t r = 4 * int64_t(sm_count()) / (N < 1 ? 1 : N);
@@ -1432,7 +1506,7 @@ AdapterWs adapter_ws(int64_t N, int64_t d_in, int64_t d_out, int k, int n, bool 
   size_t at = 256;  // the launches' abort flag
   // U: the slots' tiles, or the tokens' partial sums
   const size_t tok = align256(4 * 8 * size_t(N) * size_t(k_padded(k)));
-  const size_t need = by_token(N, n) && tok > one ? tok : one;
+  const size_t need = by_token(N, n, k) && tok > one ? tok : one;
   w.u = at; at += need;
   if (backward) {
     w.t = at; at += need;
@@ -1482,11 +1556,52 @@ cudaError_t launch_cluster(void (*kernel)(P...), dim3 grid, int threads, int sme
   return cudaLaunchKernelEx(&cfg, kernel, args...);
 }
 
-// Largest power of two up to 8 that keeps items * ks within the SMs and leaves each CTA two k-blocks.
-int cluster_split(int64_t items, int64_t blocks) {
-  int ks = 1;
-  while (ks < 8 && items * ks * 2 <= sm_count() && blocks >= 4 * ks) ks *= 2;
-  return ks;
+// Clusters of ks CTAs with an SM each that run at once: less than sm_count() / ks where a cluster does
+// not fill what is left of a group of SMs (of 152 SMs: 46 of three, 36 of four, 28 of five, 15 of eight).
+int clusters_at_once(int ks) {
+  constexpr int kDevices = 64;
+  static std::atomic<int> cache[kDevices][9] = {};
+  if (ks == 1) return sm_count();
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kDevices) return sm_count() / ks;
+  int n = cache[dev][ks].load(std::memory_order_relaxed);
+  if (n > 0) return n;
+  const int smem = 200 * 1024;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(unsigned(ks));
+  cfg.blockDim = dim3(kFewThreads);
+  cfg.dynamicSmemBytes = size_t(smem);
+  cudaLaunchAttribute at[1];
+  at[0].id = cudaLaunchAttributeClusterDimension;
+  at[0].val.clusterDim.x = unsigned(ks);
+  at[0].val.clusterDim.y = 1;
+  at[0].val.clusterDim.z = 1;
+  cfg.attrs = at;
+  cfg.numAttrs = 1;
+  if (cudaFuncSetAttribute(k_adapter_few<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess ||
+      cudaOccupancyMaxActiveClusters(&n, k_adapter_few<false>, &cfg) != cudaSuccess || n < 1) {
+    cudaGetLastError();
+    n = sm_count() / ks;
+  }
+  cache[dev][ks].store(n, std::memory_order_relaxed);
+  return n;
+}
+
+// CTAs that share the k axis of an item: whole rounds of the clusters that run at once, each of a CTA's
+// k-blocks and `fixed` more for its beginning and end.
+int cluster_split(int64_t items, int64_t blocks, int64_t fixed, bool powers) {
+  int best = 1;
+  int64_t best_c = 0;
+  for (int ks = 1; ks <= 8 && (ks == 1 || blocks >= 2 * ks); ks = powers ? 2 * ks : ks + 1) {
+    const int at_once = clusters_at_once(ks);
+    const int64_t rounds = (items + at_once - 1) / at_once;
+    const int64_t c = rounds * ((blocks + ks - 1) / ks + fixed);
+    if (ks == 1 || c < best_c) {
+      best = ks;
+      best_c = c;
+    }
+  }
+  return best;
 }
 
 // U and / or T of every slot: rows X (N x d) against the packed operand P, `sets` of them in one launch.
@@ -1528,8 +1643,8 @@ cudaError_t shrink(const Call& c, const Shrink* set, int sets, const int32_t* ma
   // slots are known to the device only: between one per tile and smax
   int64_t guess = c.p.tiles > c.n ? c.p.tiles : c.n;
   if (guess > c.p.smax) guess = c.p.smax;
-  const int ks = cluster_split(guess * sets, (dmin + 63) / 64);
-  int64_t clusters = sm_count() / ks;
+  const int ks = cluster_split(guess * sets, (dmin + 63) / 64, 6, true);
+  int64_t clusters = clusters_at_once(ks);
   if (clusters > c.p.smax * sets) clusters = c.p.smax * sets;
   const int second = sets - 1;
   return launch_cluster(k_adapter_shrink, dim3(unsigned(clusters * ks)), kShrinkThreads, shrink_smem(ctiles, g.stages),
@@ -1595,18 +1710,20 @@ cudaError_t project(const Call& c, const void* X, int64_t ldx, int64_t d, const 
         !gp::map_2d(&mu, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, U, kMaxK, slots * kSlotRows, kMaxK, 64, g.nt))
       return cudaErrorInvalidValue;
     const int64_t ot = (o + 127) / 128, nt = (c.N + g.nt - 1) / g.nt;
-    int ks = int(sm_count() / (ot * nt));
-    const int64_t most = (d + 127) / 128;  // two k-blocks for each CTA
-    if (ks > most) ks = int(most);
-    if (ks > 8) ks = 8;
-    if (ks < 1) ks = 1;
+    const int ks = cluster_split(ot * nt, (d + 63) / 64, 16, false);
     // slots of one tile: a ring that fits beside a CTA of k_adapter_shrink with its small one
+    const int stage = kWBytes + g.nt * 128;
     const int low = token_sums ? few_low(g.nt, ks, c.kp) : 0;
-    const int room = (token_sums || c.N > kTile ? 200 : 110) * 1024 - low;
-    g.stages = room / (kWBytes + g.nt * 128);  // at least 3: low is at most 98 KB
+    // (with 222 KB no block of k_adapter_tokens fits beside it: one token 10.0 us, with 206 KB 9.4)
+    const int room = (token_sums || c.N > kTile ? 206 : 110) * 1024 - low;
+    if (token_sums) {  // rows of s B, beside at least three stages (low is at most 98 KB)
+      const int most = room - 3 * stage < 72 * 1024 ? room - 3 * stage : 72 * 1024;
+      g.held = few_own(g.nt, ks) < most / few_rows(c.kp) ? few_own(g.nt, ks) : most / few_rows(c.kp);
+    }
+    g.stages = (room - g.held * few_rows(c.kp)) / stage;
     if (g.stages > 12) g.stages = 12;
     return launch_cluster(k_adapter_few<kWmn>, dim3(unsigned(ot * ks), unsigned(nt)), kFewThreads,
-                          few_smem(g.nt, g.stages, low), ks, c.s, mw, mx, mb, mu, g);
+                          few_smem(g.nt, g.stages, low, g.held, c.kp), ks, c.s, mw, mx, mb, mu, g);
   }
   CUtensorMap mo;
   if (!gp::map_kmajor(&mx, X, d, c.N, ldx) || !gp::map_out_bf16(&mo, Y, o, c.N, ldy) ||
@@ -1759,7 +1876,7 @@ cudaError_t launch_adapter_apply(const void* X, int64_t ldx, int64_t N, int64_t 
   uint8_t* ws = static_cast<uint8_t*>(workspace);
   const __nv_bfloat16* pa = reinterpret_cast<const __nv_bfloat16*>(pb + pk.a);
   const int32_t* marks = reinterpret_cast<const int32_t*>(pb + pk.marks);
-  const bool tok = by_token(N, n);
+  const bool tok = by_token(N, n, k);
   const Shrink u{X, ldx, d_in, pa, ws + w.u};
   const cudaError_t e = tok ? tokens(c, X, ldx, d_in, pa, marks, ws + w.u) : shrink(c, &u, 1, marks, 1);
   if (e != cudaSuccess) return e;
