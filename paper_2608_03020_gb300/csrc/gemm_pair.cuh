@@ -72,6 +72,48 @@ constexpr int SMEM = 12 * OPB + EPI_WARPS * BOX + 256 + 1024;
 static_assert(SMEM <= 232448, "shared memory per CTA");
 static_assert(Shape<kNarrow>::kBars * 8 + 8 <= 256 && Shape<kSingle>::kBars * 8 + 8 <= 256, "barrier area");
 
+// What the device chooses the number of k ranges by where fewer rows are live than the host planned for:
+// the sums' room in row tiles, and the costs of cycles() with those of writing and adding a range's sums.
+// 819 live rows of 8192 at d = 896, V = 32000: loss and dH 256 us with the host's ranges, 156 so.
+// Integers throughout: the product and the kernel that adds its ranges come to the same number.
+constexpr int kRangeCycles = 250;  // k_head_dh fetches four ranges at a time
+struct Fit {
+  int room = 0;  // row tiles x ranges that the sums' memory holds (0: the host's choice stands)
+  int at_once, n_tiles, nkb;
+  int kb_cycles, tile_cycles, row_tile_cycles;
+};
+__device__ __forceinline__ int fit_splits(const Fit& f, int planned, int m_planned, int m) {
+  if (f.room == 0 || m < 1 || m >= m_planned) return planned;
+  int most = f.room / m < 32 ? f.room / m : 32;
+  if (most > f.nkb / 16) most = f.nkb / 16;
+  const int tiles = m * f.n_tiles;
+  int best = planned;
+  int64_t best_c = 0;
+#pragma unroll
+  for (int r = 0; r <= 4; ++r) {  // as planned, or what fills one to four rounds
+    int s = r == 0 ? planned : r * f.at_once / tiles;
+    if (s > most) s = most;
+    if (s < planned) s = planned;
+    const int rounds = (tiles * s + f.at_once - 1) / f.at_once;
+    const int64_t c = int64_t(rounds) * (f.kb_cycles * ((f.nkb + s - 1) / s) + f.tile_cycles) +
+                      int64_t(s) * (m * f.row_tile_cycles + kRangeCycles);
+    if (r == 0 || c + c / 32 < best_c) {  // (3 % is as near as the costs are known)
+      best = s;
+      best_c = c;
+    }
+  }
+  return best;
+}
+// Row tiles of a piece that hold one of `rows` live rows, m_first row tiles before the piece; at least
+// one in all, so that a call with no live row still writes zeros.
+__device__ __forceinline__ int live_tiles(int rows, int m_first, int m_tiles) {
+  int t = (rows + TM - 1) / TM;
+  if (t < 1) t = 1;
+  t -= m_first;
+  if (t < 0) t = 0;
+  return t < m_tiles ? t : m_tiles;
+}
+
 // One launch's work.  Tiles are taken in groups of `group` row tiles that sweep all column tiles,
 // row tile fastest: the CTA pairs at work share a few column tiles and one group of row tiles,
 // which stay in L2.
@@ -92,35 +134,33 @@ struct Geo {
   int32_t* abort_flag;
   unsigned long long limit_ns;
   int32_t mark = 1;  // value of the abort flag that means this launch's
+  Fit fit;
 };
 
 struct Tile {
   int m, n, col0, split;
+  int split_row;  // row tiles before this range's, times their rows
   int end;  // column behind the tile's last
   int kb0, kb1;
 };
 
 struct Live {
-  int m_tiles, nkb, total;
+  int m_tiles, nkb, splits, total;
 };
 
+template <bool kFits>
 __device__ __forceinline__ Live live_of(const Geo& g) {
   Live v;
   v.m_tiles = g.m_tiles;
   v.nkb = g.nkb;
-  if (g.rows_live) {  // at least one row tile in all, so that a call with no live row still writes zeros
-    int t = (*g.rows_live + TM - 1) / TM;
-    if (t < 1) t = 1;
-    t -= g.m_first;
-    if (t < 0) t = 0;
-    if (t < v.m_tiles) v.m_tiles = t;
-  }
+  if (g.rows_live) v.m_tiles = live_tiles(*g.rows_live, g.m_first, g.m_tiles);
   if (g.k_live) {
     int t = (*g.k_live + BK - 1) / BK;
     if (t < 1) t = 1;
     if (t < v.nkb) v.nkb = t;
   }
-  v.total = v.m_tiles * g.n_tiles * g.splits;
+  v.splits = kFits ? fit_splits(g.fit, g.splits, g.m_tiles, v.m_tiles) : g.splits;
+  v.total = v.m_tiles * g.n_tiles * v.splits;
   return v;
 }
 
@@ -138,7 +178,8 @@ __device__ __forceinline__ Tile tile_of(const Geo& g, const Live& v, int it) {
   t.m = m0 + r - t.n * gm;
   t.col0 = t.n * g.width;
   t.end = t.col0 + g.width < g.cols ? t.col0 + g.width : g.cols;
-  const int per = (v.nkb + g.splits - 1) / g.splits;
+  t.split_row = t.split * v.m_tiles * TM;
+  const int per = (v.nkb + v.splits - 1) / v.splits;
   t.kb0 = t.split * per < v.nkb ? t.split * per : v.nkb;
   t.kb1 = t.kb0 + per < v.nkb ? t.kb0 + per : v.nkb;
   return t;
@@ -187,7 +228,7 @@ struct NoExt {
 // uses take the sums themselves:  void operator()(const Tile&, float (&v)[128], int row, int col0, int lane,
 //                                   uint8_t* box, const CUtensorMap* out) const
 // called once per finished accumulator by every epilogue thread, with the sums of row `row`, columns
-// col0 .. col0 + 127.
+// col0 .. col0 + 127.  kFits: the number of k ranges is the device's choice (Fit).
 template <int kShape, bool kAmn, bool kBmn, class Epi, class Ext>
 __global__ void __cluster_dims__(Shape<kShape>::kCtas, 1, 1) __launch_bounds__(THREADS, 1)
     k_gemm_pair(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB,
@@ -257,7 +298,7 @@ __global__ void __cluster_dims__(Shape<kShape>::kCtas, 1, 1) __launch_bounds__(T
   // completed: the producer waits when it comes to the extension.
   if (!Ext::kOn) wait_for_previous();
   launch_dependents();
-  const Live lv = live_of(g);
+  const Live lv = live_of<Epi::kFits>(g);
   uint32_t iters_done = 0;
 
   if (warp == 0) {
@@ -653,12 +694,14 @@ inline cudaError_t launch_early(void (*kernel)(P...), dim3 grid, dim3 block, siz
 // wide rounds) at k = 512 .. 8192: narrow 672 cycles a k-block and 3000 a tile, wide 1030 and 9000 (both
 // with a share of the launch and of the last tiles' stores); at k = 8192 204 and 170 us (1.60 and 1.92
 // PFLOP/s), at k = 512 25 us each.
+inline double kb_cycles(int shape) { return shape == kWide ? 1030.0 : 672.0; }
+inline double tile_cycles(int shape) { return shape == kWide ? 9000.0 : 3000.0; }
 inline double cycles(int shape, int64_t m_tiles, int64_t cols, int64_t nkb, int splits) {
   const int64_t n = shape == kWide ? (cols + 2 * TN - 1) / (2 * TN) : (cols + TN - 1) / TN;
   const int64_t at_once = shape == kSingle ? sm_count() : sm_count() / 2;
   const double rounds = double((m_tiles * n * splits + at_once - 1) / at_once);
   const double kb = double((nkb + splits - 1) / splits);
-  return rounds * (shape == kWide ? 1030.0 * kb + 9000.0 : 672.0 * kb + 3000.0);
+  return rounds * (kb_cycles(shape) * kb + tile_cycles(shape));
 }
 // rows: those of A, where 128 or fewer may take the single shape (0: they may not)
 inline int pick_shape(int64_t rows, int64_t m_tiles, int64_t cols, int64_t nkb, int splits) {
@@ -693,19 +736,25 @@ inline cudaError_t launch(const CUtensorMap& a, const CUtensorMap& b, const CUte
   const int64_t total = int64_t(g.m_tiles) * g.n_tiles * g.splits;
   if (total < 1) return cudaSuccess;
   const int at_once = sm_count() / kCtas;  // pairs (76 on 152 SMs) or CTAs at work at once
-  const int n = total < at_once ? int(total) : at_once;
+  const int n = total < at_once && g.fit.room == 0 ? int(total) : at_once;
   return launch_early(kernel, dim3(unsigned(kCtas * n)), dim3(THREADS), SMEM, s, a, b, ax, bx, o, g, epi, ext);
 }
 
-// The shape that pick_shape() names.
 template <bool kAmn, bool kBmn, class Epi, class Ext>
-inline cudaError_t launch_either(const CUtensorMap& a, const CUtensorMap& b, const CUtensorMap& ax, const CUtensorMap& bx,
-                                 const CUtensorMap& o, const Geo& g, const Epi& epi, const Ext& ext, cudaStream_t s) {
-  const int shape = pick_shape(g.rows, g.m_tiles, g.cols, g.nkb, g.splits);
+inline cudaError_t launch_shape(int shape, const CUtensorMap& a, const CUtensorMap& b, const CUtensorMap& ax,
+                                const CUtensorMap& bx, const CUtensorMap& o, const Geo& g, const Epi& epi, const Ext& ext,
+                                cudaStream_t s) {
   if constexpr (!Ext::kOn && !kAmn)
     if (shape == kSingle) return launch<kSingle, kAmn, kBmn, Epi, Ext>(a, b, ax, bx, o, g, epi, ext, s);
   return shape == kWide ? launch<kWide, kAmn, kBmn, Epi, Ext>(a, b, ax, bx, o, g, epi, ext, s)
                         : launch<kNarrow, kAmn, kBmn, Epi, Ext>(a, b, ax, bx, o, g, epi, ext, s);
+}
+
+// In the shape that pick_shape() names.
+template <bool kAmn, bool kBmn, class Epi, class Ext>
+inline cudaError_t launch_either(const CUtensorMap& a, const CUtensorMap& b, const CUtensorMap& ax, const CUtensorMap& bx,
+                                 const CUtensorMap& o, const Geo& g, const Epi& epi, const Ext& ext, cudaStream_t s) {
+  return launch_shape<kAmn, kBmn>(pick_shape(g.rows, g.m_tiles, g.cols, g.nkb, g.splits), a, b, ax, bx, o, g, epi, ext, s);
 }
 
 }  // namespace gp

@@ -64,7 +64,14 @@ __device__ __forceinline__ bool live_label(int32_t y, int64_t V) { return y >= 0
 // Live labels among y[0 .. n), counted by the whole block.
 __device__ int count_live(const int32_t* __restrict__ y, int64_t n, int64_t V, int* scratch) {
   int c = 0;
-  for (int64_t i = threadIdx.x; i < n; i += blockDim.x) c += live_label(y[i], V) ? 1 : 0;
+  constexpr int kAhead = 8;
+  for (int64_t i0 = threadIdx.x; i0 < n; i0 += kAhead * blockDim.x) {
+    int32_t v[kAhead];
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) v[j] = i0 + j * int64_t(blockDim.x) < n ? __ldg(y + i0 + j * int64_t(blockDim.x)) : -1;
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) c += live_label(v[j], V) ? 1 : 0;
+  }
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) c += __shfl_xor_sync(0xffffffffu, c, o);
   __syncthreads();
@@ -153,6 +160,7 @@ __global__ void __launch_bounds__(256)
 // Forward: maximum and sum of exponentials of 128 logits of a row.
 struct EpiStats {
   static constexpr bool kPacks = false;
+  static constexpr bool kFits = false;
   float2* part;        // (2 column tiles) x pitch
   int64_t pitch;       // rows of a piece
   const int32_t* y;    // this piece's rows
@@ -218,6 +226,7 @@ struct EpiStats {
 // the vocabulary and rows past the live ones are zero.
 struct EpiDz {
   static constexpr bool kPacks = true;
+  static constexpr bool kFits = false;
   const float* lse;
   const float* w;      // w_n dloss_n
   const int32_t* y;
@@ -250,13 +259,12 @@ struct EpiDz {
 // (one writer per element and launch: a fixed order of additions).
 struct EpiAcc {
   static constexpr bool kPacks = false;
-  int64_t rows;  // rows of one split's sums
+  static constexpr bool kFits = true;
   int add;
 
   __device__ __forceinline__ void operator()(const gp::Tile& t, float (&v)[128], int row, int col0, int lane, uint8_t* box,
                                              const CUtensorMap* out) const {
-    const int r0 = row - lane;
-    if (r0 >= rows) return;
+    const int r0 = t.split_row + row - lane;
 #pragma unroll
     for (int b = 0; b < 4; ++b) {
       if (lane == 0) bulk_wait_group_read0();
@@ -269,8 +277,8 @@ struct EpiAcc {
       __syncwarp();
       if (lane == 0) {
         if (LOCA_REQUIRE(col0 >= 0 && r0 >= 0)) {
-          if (add) tma_reduce_add_3d(out, smem_u32(box), col0 + 32 * b, r0, t.split);
-          else tma_store_3d(out, smem_u32(box), col0 + 32 * b, r0, t.split);
+          if (add) tma_reduce_add_2d(out, smem_u32(box), col0 + 32 * b, r0);
+          else tma_store_2d(out, smem_u32(box), col0 + 32 * b, r0);
         }
         bulk_commit_group();
       }
@@ -281,6 +289,7 @@ struct EpiAcc {
 // dW: scaled and rounded once.
 struct EpiScaled {
   static constexpr bool kPacks = true;
+  static constexpr bool kFits = false;
   float scale;
 
   struct Row {};
@@ -343,13 +352,16 @@ __global__ void __launch_bounds__(1024)
 
 // One thread per 8 elements of a row; the k ranges' sums are loaded four at a time and added in order.
 __global__ void __launch_bounds__(256)
-    k_head_dh(const float* __restrict__ part, int64_t rows, int splits, int64_t d, Rows in, int64_t row_first,
-              float scale, __nv_bfloat16* __restrict__ dH, int64_t lddh) {
+    k_head_dh(const float* __restrict__ part, int64_t rows, int planned, const gp::Fit fit, int64_t d, Rows in,
+              int64_t row_first, float scale, __nv_bfloat16* __restrict__ dH, int64_t lddh) {
   wait_for_previous();
   launch_dependents();
   const int dv = int(d / 8);
   const int64_t live = *in.count - row_first;
   const int64_t total = (live < rows ? live : rows) * dv;
+  const int m_tiles = gp::live_tiles(*in.count, int(row_first / gp::TM), int(rows / gp::TM));
+  const int splits = gp::fit_splits(fit, planned, int(rows / gp::TM), m_tiles);
+  const int64_t pitch = int64_t(m_tiles) * gp::TM * d;  // sums of a k range
   for (int64_t e = int64_t(blockIdx.x) * blockDim.x + threadIdx.x; e < total; e += int64_t(gridDim.x) * blockDim.x) {
     const int64_t row = e / dv;
     const int64_t at = row * d + 8 * (e - row * dv);
@@ -360,7 +372,7 @@ __global__ void __launch_bounds__(256)
 #pragma unroll
       for (int s = 0; s < 4; ++s)
         if (s0 + s < splits) {
-          const float4* p = reinterpret_cast<const float4*>(part + int64_t(s0 + s) * rows * d + at);
+          const float4* p = reinterpret_cast<const float4*>(part + int64_t(s0 + s) * pitch + at);
           x[s][0] = p[0];
           x[s][1] = p[1];
         }
@@ -448,7 +460,8 @@ int dh_splits(int64_t n, int64_t rows, int64_t d, int64_t vc) {
   double best_c = 0;
   for (int s = 1; s <= 32; ++s) {
     if (s > 1 && nkb / s < 16) break;
-    const double c = gp::cycles(gp::pick_shape(n, m, d, nkb, s), m, d, nkb, s) + double(s) * double(rows) * double(d) * 8.0 / 3000.0;
+    const double c = gp::cycles(gp::pick_shape(n, m, d, nkb, s), m, d, nkb, s) + 
+                     double(s) * (double(rows) * double(d) * 8.0 / 3000.0 + gp::kRangeCycles);
     if (s == 1 || c < best_c) {
       best = s;
       best_c = c;
@@ -562,6 +575,19 @@ cudaError_t launch_head_loss_backward(const void* H, int64_t ldh, int64_t N, int
   float* part = reinterpret_cast<float*>(ws + lay.part);
   for (int64_t p0 = 0; p0 < np; p0 += lay.piece) {
     const int64_t rows = np - p0 < lay.piece ? np - p0 : lay.piece;
+    const int64_t kblocks = (lay.vc + gp::BK - 1) / gp::BK;  // of a whole piece of the vocabulary
+    const int shape = gp::pick_shape(N, rows / gp::TM, d, kblocks, lay.splits);
+    gp::Fit fit{};
+    if (dH && shape != gp::kSingle) {
+      const int width = shape == gp::kWide ? 2 * gp::TN : gp::TN;
+      fit.room = int(lay.splits * (lay.piece / gp::TM));
+      fit.at_once = sm_count() / 2;
+      fit.n_tiles = int((d + width - 1) / width);
+      fit.nkb = int(kblocks);
+      fit.kb_cycles = int(gp::kb_cycles(shape));
+      fit.tile_cycles = int(gp::tile_cycles(shape));
+      fit.row_tile_cycles = int(gp::TM * d * 8 / 3000);
+    }
     for (int64_t v0 = 0; v0 < V; v0 += lay.vc) {
       const int64_t vn = V - v0 < lay.vc ? V - v0 : lay.vc;   // columns of the vocabulary
       const int64_t vtiles = (vn + gp::TN - 1) / gp::TN;
@@ -579,16 +605,15 @@ cudaError_t launch_head_loss_backward(const void* H, int64_t ldh, int64_t N, int
       if (dH) {
         CUtensorMap mo;
         if (!gp::map_kmajor(&mz_k, dz, lay.vc, lay.piece, lay.vc) || !gp::map_mnmajor(&mw_mn, Wb + v0 * d, d, vn, d) ||
-            !gp::map_3d(&mo, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 4, part, d, lay.piece, lay.splits, d, lay.piece * d, 32,
-                        32))
+            !gp::map_2d(&mo, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 4, part, d, lay.piece * lay.splits, d, 32, 32))
           return cudaErrorInvalidValue;
         gp::Geo gh = geo(rows / gp::TM, d, (vn + gp::BK - 1) / gp::BK, kSegKbGrad, r, status);
         gh.rows_live = r.count;
         gh.m_first = g.m_first;
         gh.splits = lay.splits;
         gh.rows = int(N);
-        e = gp::launch_either<false, true>(mz_k, mw_mn, mz_k, mw_mn, mo, gh, EpiAcc{lay.piece, v0 > 0 ? 1 : 0},
-                                           gp::NoExt{}, s);
+        gh.fit = fit;
+        e = gp::launch_shape<false, true>(shape, mz_k, mw_mn, mz_k, mw_mn, mo, gh, EpiAcc{v0 > 0 ? 1 : 0}, gp::NoExt{}, s);
         if (e != cudaSuccess) return e;
       }
       if (dW) {
@@ -606,7 +631,7 @@ cudaError_t launch_head_loss_backward(const void* H, int64_t ldh, int64_t N, int
     if (dH) {
       const int64_t blocks = rows * (d / 8) / 256 + 1;
       const int64_t most = 8 * int64_t(sm_count());
-      e = gp::launch_early(k_head_dh, dim3(unsigned(blocks < most ? blocks : most)), dim3(256), 0, s, part, lay.piece, lay.splits, d, r, p0, scale,
+      e = gp::launch_early(k_head_dh, dim3(unsigned(blocks < most ? blocks : most)), dim3(256), 0, s, part, rows, lay.splits, fit, d, r, p0, scale,
                            static_cast<__nv_bfloat16*>(dH), lddh);
       if (e != cudaSuccess) return e;
     }

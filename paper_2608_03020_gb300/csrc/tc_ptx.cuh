@@ -423,6 +423,13 @@ __device__ __forceinline__ void tma_reduce_add_3d(const CUtensorMap* map, uint32
                "r"(src), "r"(c0), "r"(c1), "r"(c2)
                : "memory");
 }
+// The same of one box of a 2-D map.
+__device__ __forceinline__ void tma_reduce_add_2d(const CUtensorMap* map, uint32_t src, int c0, int c1) {
+  asm volatile("cp.reduce.async.bulk.tensor.2d.global.shared::cta.add.tile.bulk_group [%0, {%2, %3}], [%1];" ::"l"(
+                   reinterpret_cast<uint64_t>(map)),
+               "r"(src), "r"(c0), "r"(c1)
+               : "memory");
+}
 // Count `bytes` of expected transfer as complete on a barrier of this CTA without a transfer
 // (settles the bytes of copies that were armed but never issued).
 __device__ __forceinline__ void mbar_complete_tx(uint32_t bar, uint32_t bytes) {
