@@ -114,21 +114,40 @@ __device__ __forceinline__ double sum_squares(const T* p, int count) {
   return d;
 }
 
-__device__ __forceinline__ double block_sum(double v, double* sh) {
+__device__ __forceinline__ double warp_sum(double v) {
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-  __syncthreads();
-  if ((threadIdx.x & 31) == 0) sh[threadIdx.x >> 5] = v;
-  __syncthreads();
-  double s = 0.0;
-#pragma unroll
-  for (int w = 0; w < kThreads / 32; ++w) s += sh[w];
-  return s;
+  return v;
+}
+
+// sqrt(s) and the factor.  The chip adds two doubles a cycle and SM: a double square root and division in
+// every block took 15 us of 25 at 4 million elements.  The root is taken of the leading 24 bits of
+// s 4^-e in [1, 4), and one Newton step with the exact remainder leaves it, and likewise the quotient,
+// within 2^-40 before its one rounding to fp32.
+__device__ __forceinline__ void norm_and_factor(double s, float max_norm, float& norm, float& f) {
+  f = 1.f;
+  if (!(s < INFINITY)) {  // infinite: every finite element becomes 0; NaN: nothing is scaled
+    norm = float(s);
+    if (s > 0.0) f = max_norm < INFINITY ? 0.f : 1.f;
+    return;
+  }
+  norm = 0.f;
+  if (!(s > 0.0)) return;
+  const int e = ((__double2hiint(s) >> 20) - 1023) >> 1;  // s is a normal double: squares of fp32 values
+  const double m = __hiloint2double(__double2hiint(s) - e * (1 << 21), __double2loint(s));
+  const float mh = float(m), ml = float(m - double(mh));
+  const float r = sqrtf(mh);
+  const float lo = (fmaf(-r, r, mh) + ml) / (2.f * r);
+  norm = ldexpf(r + lo, e);
+  if (s > double(max_norm) * double(max_norm)) {
+    const float q = max_norm / r;
+    f = ldexpf(q + (fmaf(-q, r, max_norm) - q * lo) / r, -e);
+  }
 }
 
 template <int kCap>
 __global__ void __launch_bounds__(kThreads, kSumBlocks) k_clip_sumsq(const __grid_constant__ List<kCap> l, double* part) {
-  __shared__ double sh[kThreads / 32];
+  __shared__ double sh[kThreads];
   tc::wait_for_previous();
   tc::launch_dependents();
   double s = 0.0;
@@ -137,7 +156,13 @@ __global__ void __launch_bounds__(kThreads, kSumBlocks) k_clip_sumsq(const __gri
     s += k.bf16 ? sum_squares(static_cast<const __nv_bfloat16*>(l.in[k.t]) + k.first, k.count)
                 : sum_squares(static_cast<const float*>(l.in[k.t]) + k.first, k.count);
   }
-  s = block_sum(s, sh);
+  sh[threadIdx.x] = s;
+  __syncthreads();
+  if (threadIdx.x >= 32) return;
+  s = 0.0;
+#pragma unroll
+  for (int w = 0; w < kThreads / 32; ++w) s += sh[32 * w + threadIdx.x];
+  s = warp_sum(s);
   if (threadIdx.x == 0) part[blockIdx.x] = s;
 }
 
@@ -149,21 +174,65 @@ template <>
 __device__ __forceinline__ __nv_bfloat16 from_f<__nv_bfloat16>(float x) { return __float2bfloat16_rn(x); }
 
 template <class T>
+__device__ __forceinline__ uint4 scaled(uint4 q, float f) {
+  T* v = reinterpret_cast<T*>(&q);
+#pragma unroll
+  for (int e = 0; e < 16 / int(sizeof(T)); ++e) v[e] = from_f<T>(f * to_f(v[e]));
+  return q;
+}
+
+template <class T>
 __device__ __forceinline__ void scale_chunk(const T* p, T* o, int count, float f) {
-  if (((reinterpret_cast<uintptr_t>(p) ^ reinterpret_cast<uintptr_t>(o)) & 15) != 0) {
-    // the two do not share 16-byte boundaries
-#pragma unroll 8
-    for (int i = threadIdx.x; i < count; i += kThreads) o[i] = from_f<T>(f * to_f(p[i]));
+  using S = Share<T>;
+  const int apart = int((reinterpret_cast<uintptr_t>(p) - reinterpret_cast<uintptr_t>(o)) & 15);
+  if (apart != 0) {
+    // The two do not share 16-byte boundaries (tensors of odd sizes behind one another in a buffer):
+    // each vector of the output comes from the two aligned vectors of the input that it lies across.
+    // All of both lies inside the chunk.
+    int head = int((16 - (reinterpret_cast<uintptr_t>(o) & 15)) & 15) / int(sizeof(T));
+    if (head * int(sizeof(T)) < apart) head += S::kVec;
+    if (head > count) head = count;
+    int vecs = ((count - head) * int(sizeof(T)) + apart) / 16 - 1;
+    if (vecs < 0) vecs = 0;
+    // p + head is `apart` bytes behind a boundary
+    const uint4* src = reinterpret_cast<const uint4*>(reinterpret_cast<uintptr_t>(p + head) - apart);
+    constexpr int kAhead = 2;  // vectors on the way at once
+    for (int i0 = threadIdx.x; i0 < vecs; i0 += kAhead * kThreads) {
+      uint4 a[kAhead], b[kAhead];
+#pragma unroll
+      for (int j = 0; j < kAhead; ++j) {
+        const int i = i0 + j * kThreads;
+        a[j] = b[j] = make_uint4(0, 0, 0, 0);
+        if (i < vecs) {
+          a[j] = __ldg(src + i);
+          b[j] = __ldg(src + i + 1);
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < kAhead; ++j) {
+        const int i = i0 + j * kThreads;
+        const uint32_t w[8] = {a[j].x, a[j].y, a[j].z, a[j].w, b[j].x, b[j].y, b[j].z, b[j].w};
+        uint32_t r[4];
+        const unsigned bits = 8u * unsigned(apart & 3);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const uint32_t lo = apart < 4 ? w[e] : apart < 8 ? w[e + 1] : apart < 12 ? w[e + 2] : w[e + 3];
+          const uint32_t hi = apart < 4 ? w[e + 1] : apart < 8 ? w[e + 2] : apart < 12 ? w[e + 3] : w[e + 4];
+          r[e] = __funnelshift_r(lo, hi, bits);
+        }
+        if (i < vecs) __stcs(reinterpret_cast<uint4*>(o + head) + i, scaled<T>(make_uint4(r[0], r[1], r[2], r[3]), f));
+      }
+    }
+    for (int i = threadIdx.x; i < head; i += kThreads) o[i] = from_f<T>(f * to_f(p[i]));
+    for (int i = head + vecs * S::kVec + int(threadIdx.x); i < count; i += kThreads) o[i] = from_f<T>(f * to_f(p[i]));
     return;
   }
-  Share<T> c(p, count);
+  S c(p, count);
 #pragma unroll
-  for (int j = 0; j < Share<T>::kIter; ++j) {
+  for (int j = 0; j < S::kIter; ++j) {
     const int i = j * kThreads + int(threadIdx.x);
-    T* v = reinterpret_cast<T*>(&c.q[j]);
-#pragma unroll
-    for (int e = 0; e < Share<T>::kVec; ++e) v[e] = from_f<T>(f * to_f(v[e]));
-    if (i < c.vecs) __stcs(reinterpret_cast<uint4*>(o + c.head) + i, c.q[j]);
+    const uint4 q = scaled<T>(c.q[j], f);
+    if (i < c.vecs) __stcs(reinterpret_cast<uint4*>(o + c.head) + i, q);
   }
   c.singles([&](int i) { o[i] = from_f<T>(f * to_f(p[i])); });
 }
@@ -171,15 +240,28 @@ __device__ __forceinline__ void scale_chunk(const T* p, T* o, int count, float f
 template <int kCap>
 __global__ void __launch_bounds__(kThreads, kScaleBlocks)
     k_clip_scale(const __grid_constant__ List<kCap> l, const double* part, int parts, float max_norm, float* norm) {
-  __shared__ double sh[kThreads / 32];
+  __shared__ float factor;
   tc::wait_for_previous();
   tc::launch_dependents();
-  double s = 0.0;
-  for (int i = threadIdx.x; i < parts; i += kThreads) s += part[i];
-  s = block_sum(s, sh);
-  const double n = sqrt(s);
-  if (blockIdx.x == 0 && threadIdx.x == 0) *norm = float(n);
-  const float f = n > double(max_norm) ? float(double(max_norm) / n) : 1.f;
+  if (threadIdx.x < 32) {
+    double s = 0.0;
+    constexpr int kAhead = 8;
+    for (int i0 = threadIdx.x; i0 < parts; i0 += 32 * kAhead) {
+      double v[kAhead];
+#pragma unroll
+      for (int j = 0; j < kAhead; ++j) v[j] = i0 + 32 * j < parts ? part[i0 + 32 * j] : 0.0;
+#pragma unroll
+      for (int j = 0; j < kAhead; ++j) s += v[j];
+    }
+    s = warp_sum(s);
+    if (threadIdx.x == 0) {
+      float n;
+      norm_and_factor(s, max_norm, n, factor);
+      if (blockIdx.x == 0) *norm = n;
+    }
+  }
+  __syncthreads();
+  const float f = factor;
   for (int c = l.chunks - 1 - int(blockIdx.x); c >= 0; c -= int(gridDim.x)) {
     const Chunk k = chunk_of(l, c);
     if (f == 1.f && l.in[k.t] == l.out[k.t]) continue;
