@@ -1411,55 +1411,57 @@ struct JoinOne {
   const float* part;
   const float* scale;  // per adapter, or null
   void* out;
-  int64_t rows, d;     // n d rows of k values (0: nothing to do)
+  int64_t d;           // n d rows of k values
   int ranges;
 };
-// Four lanes share the ranges of four neighbouring columns of a row; their sums meet in a fixed order.
-template <class T>
+// One adapter's gradient per (y, z) of the grid.  kLanes lanes share the ranges of four neighbouring
+// columns of a channel; their sums meet in a fixed order.  Four where a product was cut into many ranges
+// (one adapter, 23 ranges, 896 channels), one where it was not: 7 adapters of rank 64 over 5120
+// channels in two ranges took 26 us with four.
+template <class T, int kLanes>
 __global__ void __launch_bounds__(256)
     k_adapter_join(const JoinOne j0, const JoinOne j1, int k, int kp, const int32_t* __restrict__ plan,
                    const __grid_constant__ PlanLay pl) {
   wait_for_previous();
   launch_dependents();
-  const int all_slots = plan[pl.tile_base + pl.tiles];
-  const int lane4 = threadIdx.x & 3;
-  const int64_t groups = (j0.rows + j1.rows) * (kp / 4);
-  for (int64_t b0 = int64_t(blockIdx.x) * 64; b0 < groups; b0 += int64_t(gridDim.x) * 64) {
-    const int64_t gi = b0 + threadIdx.x / 4;
-    const bool on = gi < groups;
-    const int64_t flat = on ? gi / (kp / 4) : 0;
-    const int c = on ? int(gi - flat * (kp / 4)) * 4 : 0;
-    const JoinOne& j = flat < j0.rows ? j0 : j1;
-    const int64_t row = flat < j0.rows ? flat : flat - j0.rows;
-    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-    const int64_t a = row / j.d;
-    if (on) {
-      const int s0 = plan[pl.ad_off + a], s1 = plan[pl.ad_off + a + 1];
-      if (s0 < s1) {  // the ranges that hold slots of this adapter
-        const int per = (all_slots + j.ranges - 1) / j.ranges;
-        const int r1 = (s1 - 1) / per;
-        const float* p = j.part + row * kp + c;  // number r + a: row is a d + channel
-        const int64_t pitch = j.d * kp;
+  const JoinOne& j = blockIdx.z ? j1 : j0;
+  const int a = int(blockIdx.y);
+  const int per_row = kp / 4;
+  const int lane = threadIdx.x % kLanes;
+  const int gi = int(blockIdx.x) * (256 / kLanes) + int(threadIdx.x) / kLanes;
+  const bool on = gi < int(j.d) * per_row;
+  const int channel = on ? gi / per_row : 0;
+  const int c = on ? 4 * (gi - channel * per_row) : 0;
+  const int64_t row = int64_t(a) * j.d + channel;
+  float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+  const int s0 = plan[pl.ad_off + a], s1 = plan[pl.ad_off + a + 1];
+  if (on && s0 < s1) {  // the ranges that hold slots of this adapter
+    const int per = (plan[pl.tile_base + pl.tiles] + j.ranges - 1) / j.ranges;
+    const int r1 = (s1 - 1) / per;
+    const float* p = j.part + row * kp + c;  // number r + a: row is a d + channel
+    const int64_t pitch = j.d * kp;
 #pragma unroll 4
-        for (int r = s0 / per + lane4; r <= r1; r += 4) {
-          const float4 x = *reinterpret_cast<const float4*>(p + r * pitch);
-          v.x += x.x; v.y += x.y; v.z += x.z; v.w += x.w;
-        }
-      }
+    for (int r = s0 / per + lane; r <= r1; r += kLanes) {
+      const float4 x = *reinterpret_cast<const float4*>(p + r * pitch);
+      v.x += x.x; v.y += x.y; v.z += x.z; v.w += x.w;
     }
+  }
 #pragma unroll
-    for (int o = 1; o < 4; o <<= 1) {
-      v.x += __shfl_xor_sync(0xffffffffu, v.x, o);
-      v.y += __shfl_xor_sync(0xffffffffu, v.y, o);
-      v.z += __shfl_xor_sync(0xffffffffu, v.z, o);
-      v.w += __shfl_xor_sync(0xffffffffu, v.w, o);
-    }
-    const int col = c + lane4;
-    if (on && col < k && LOCA_CHECK(row * k + col, j.rows * k)) {
-      float x = lane4 == 0 ? v.x : lane4 == 1 ? v.y : lane4 == 2 ? v.z : v.w;
-      if (j.scale) x *= j.scale[a];
-      if constexpr (sizeof(T) == 4) static_cast<float*>(j.out)[row * k + col] = x;
-      else static_cast<__nv_bfloat16*>(j.out)[row * k + col] = __float2bfloat16_rn(x);
+  for (int o = 1; o < kLanes; o <<= 1) {
+    v.x += __shfl_xor_sync(0xffffffffu, v.x, o);
+    v.y += __shfl_xor_sync(0xffffffffu, v.y, o);
+    v.z += __shfl_xor_sync(0xffffffffu, v.z, o);
+    v.w += __shfl_xor_sync(0xffffffffu, v.w, o);
+  }
+  if (!on || !LOCA_CHECK_SPAN(row * k, k, int64_t(gridDim.y) * j.d * k)) return;
+  T* out = static_cast<T*>(j.out) + row * k;
+  const float scale = j.scale ? j.scale[a] : 1.f;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float x = scale * (i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w);
+    if (i % kLanes == lane && c + i < k) {
+      if constexpr (sizeof(T) == 4) out[c + i] = x;
+      else out[c + i] = __float2bfloat16_rn(x);
     }
   }
 }
@@ -1760,7 +1762,7 @@ cudaError_t grad(const Call& c, const Grad* set, int sets, int parts, int dtype)
   CUtensorMap ms[2], mu[2];
   GradGeo g{};
   JoinOne j[2] = {};
-  int64_t groups = 0;
+  int64_t dmax = 0;
   const int utiles = col_tiles(c.kp, parts);
   for (int i = 0; i < sets; ++i) {
     const Grad& v = set[i];
@@ -1777,10 +1779,9 @@ cudaError_t grad(const Call& c, const Grad* set, int sets, int parts, int dtype)
     j[i].part = v.part;
     j[i].scale = v.scale;
     j[i].out = v.out;
-    j[i].rows = int64_t(c.n) * v.d;
     j[i].d = v.d;
     j[i].ranges = v.ranges;
-    groups += j[i].rows * (c.kp / 4);
+    if (v.d > dmax) dmax = v.d;
   }
   g.N = c.N;
   g.n = c.n;
@@ -1799,9 +1800,12 @@ cudaError_t grad(const Call& c, const Grad* set, int sets, int parts, int dtype)
   const cudaError_t e = launch_cluster(k_adapter_grad, dim3(blocks), kGradThreads, grad_smem(utiles, g.stages), 1, c.s, ms[0], mu[0],
                                        ms[second], mu[second], g);
   if (e != cudaSuccess) return e;
-  const unsigned jb = unsigned(groups / 64 + 1 < 16 * sm_count() ? groups / 64 + 1 : 16 * sm_count());
-  return launch_cluster(dtype == LOCA_F32 ? k_adapter_join<float> : k_adapter_join<__nv_bfloat16>, dim3(jb), 256, 0, 1,
-                        c.s, j[0], j[1], c.k, c.kp, c.plan, c.p);
+  const bool wide = set[0].ranges >= 8;
+  const int64_t groups = dmax * (c.kp / 4), per = wide ? 64 : 256;
+  auto join = dtype == LOCA_F32 ? (wide ? k_adapter_join<float, 4> : k_adapter_join<float, 1>)
+                                : (wide ? k_adapter_join<__nv_bfloat16, 4> : k_adapter_join<__nv_bfloat16, 1>);
+  return launch_cluster(join, dim3(unsigned((groups + per - 1) / per), unsigned(c.n), unsigned(sets)), 256, 0, 1, c.s,
+                        j[0], j[1], c.k, c.kp, c.plan, c.p);
 }
 
 Call call_of(int64_t N, int n, int k, const void* plan, void* workspace, int32_t* status, cudaStream_t s) {
