@@ -148,13 +148,13 @@ struct Live {
   int m_tiles, nkb, splits, total;
 };
 
-template <bool kFits>
+template <bool kFits, bool kSingleTile>
 __device__ __forceinline__ Live live_of(const Geo& g) {
   Live v;
   v.m_tiles = g.m_tiles;
   v.nkb = g.nkb;
-  if (g.rows_live) v.m_tiles = live_tiles(*g.rows_live, g.m_first, g.m_tiles);
-  if (g.k_live) {
+  if (!kSingleTile && g.rows_live) v.m_tiles = live_tiles(*g.rows_live, g.m_first, g.m_tiles);
+  if (!kSingleTile && g.k_live) {
     int t = (*g.k_live + BK - 1) / BK;
     if (t < 1) t = 1;
     if (t < v.nkb) v.nkb = t;
@@ -295,10 +295,13 @@ __global__ void __cluster_dims__(Shape<kShape>::kCtas, 1, 1) __launch_bounds__(T
   const uint32_t tmem_base = *tmem_slot;
   // The launch before has completed (the prologue above ran beside its end).  With an extended k axis
   // only the extension is that launch's work, which let this one start after all launches before it had
-  // completed: the producer waits when it comes to the extension.
-  if (!Ext::kOn) wait_for_previous();
-  launch_dependents();
-  const Live lv = live_of<Epi::kFits>(g);
+  // completed: the producer waits when it comes to the extension.  In the single shape B is the caller's
+  // (the launch before makes A and lets this one start only after all before it): the producer fills the
+  // ring with B first.
+  constexpr bool kEarlyB = kShape == kSingle;
+  if (!Ext::kOn && !(kEarlyB && warp == 0)) wait_for_previous();
+  if (!(kEarlyB && warp == 0)) launch_dependents();
+  const Live lv = live_of<Epi::kFits, kShape == kSingle>(g);
   uint32_t iters_done = 0;
 
   if (warp == 0) {
@@ -308,47 +311,63 @@ __global__ void __cluster_dims__(Shape<kShape>::kCtas, 1, 1) __launch_bounds__(T
       uint32_t phase = 0;
       uint32_t iter = 0;
       bool ok = true, waited = !Ext::kOn;
+      auto load = [&](uint32_t dst, const CUtensorMap* map, uint32_t bar, int c0, int c1) {
+        if constexpr (kPair) tma_load_2d_pair(dst, map, bar, c0, c1);
+        else tma_load_2d(dst, map, bar, c0, c1);
+      };
+      auto load_a = [&](const Tile& t, int s, int k0, uint32_t fb) {
+        const uint32_t a = smem_base + uint32_t(s) * STAGE_BYTES;
+        const int m0 = t.m * TM + int(rank) * HALF;
+        if (kAmn) {
+          load(a, &tmA, fb, m0, k0);
+          load(a + SUB, &tmA, fb, m0 + 64, k0);
+        } else {
+          load(a, &tmA, fb, k0, m0);
+        }
+      };
+      // 128 rows of B per operand: this CTA's half of each accumulator, or (single) both halves
+      auto load_b = [&](const Tile& t, int s, int k0, uint32_t fb) {
+        const uint32_t b = smem_base + uint32_t(s) * STAGE_BYTES + a_bytes;
+#pragma unroll
+        for (int c = 0; c < S::kOpsB; ++c) {
+          const int n = t.col0 + int(rank) * HALF + c * (kPair ? TN : kSlim ? g.width / 2 : HALF);
+          if (kSlim) {
+            load(b + c * uint32_t(g.width * BK), &tmB, fb, k0, n);
+          } else if (kBmn) {
+            load(b + c * OPB, &tmB, fb, n, k0);
+            load(b + c * OPB + SUB, &tmB, fb, n + 64, k0);
+          } else {
+            load(b + c * OPB, &tmB, fb, k0, n);
+          }
+        }
+      };
+      uint32_t early = 0;
+      if constexpr (kEarlyB) {
+        if (cid < lv.total) {
+          const Tile t = tile_of(g, lv, cid);
+          for (; int(early) < STAGES && int(early) < t.kb1 - t.kb0; ++early) {
+            mbar_arrive_expect_tx(full_bar(int(early)), STAGE_BYTES);
+            load_b(t, int(early), (t.kb0 + int(early)) * BK, full_bar(int(early)));
+          }
+        }
+        wait_for_previous();
+      }
       for (int it = cid; it < lv.total && ok; it += ncl) {
         const Tile t = tile_of(g, lv, it);
-        const int m0 = t.m * TM + int(rank) * HALF;
-        const int n0 = t.col0 + int(rank) * HALF;
         const int nx = Ext::kOn ? ext.entries(t.m) : 0;
         const int nb = t.kb1 - t.kb0;
         for (int j = 0; j < nb + nx; ++j) {
-          if (!mbar_try_wait_cluster(empty_bar(stage), phase ^ 1u) &&
+          const bool ahead = kEarlyB && iter < early;
+          if (!ahead && !mbar_try_wait_cluster(empty_bar(stage), phase ^ 1u) &&
               !mbar_wait_cluster(empty_bar(stage), phase ^ 1u, wc)) {
             ok = false;
             break;
           }
-          if (leader) mbar_arrive_expect_tx(full_bar(stage), uint32_t(S::kCtas) * STAGE_BYTES);
-          const uint32_t fb = mapa_shared(full_bar(stage), 0);
-          const uint32_t a = smem_base + uint32_t(stage) * STAGE_BYTES;
-          const uint32_t b = a + a_bytes;
+          if (leader && !ahead) mbar_arrive_expect_tx(full_bar(stage), uint32_t(S::kCtas) * STAGE_BYTES);
+          const uint32_t fb = kPair ? mapa_shared(full_bar(stage), 0) : full_bar(stage);
           if (!Ext::kOn || j < nb) {
-            const int k0 = (t.kb0 + j) * BK;
-            auto load = [&](uint32_t dst, const CUtensorMap* map, int c0, int c1) {
-              if constexpr (kPair) tma_load_2d_pair(dst, map, fb, c0, c1);
-              else tma_load_2d(dst, map, fb, c0, c1);
-            };
-            if (kAmn) {
-              load(a, &tmA, m0, k0);
-              load(a + SUB, &tmA, m0 + 64, k0);
-            } else {
-              load(a, &tmA, k0, m0);
-            }
-            // 128 rows of B per operand: this CTA's half of each accumulator, or (single) both halves
-#pragma unroll
-            for (int c = 0; c < S::kOpsB; ++c) {
-              const int n = n0 + c * (kPair ? TN : kSlim ? g.width / 2 : HALF);
-              if (kSlim) {
-                load(b + c * uint32_t(g.width * BK), &tmB, k0, n);
-              } else if (kBmn) {
-                load(b + c * OPB, &tmB, n, k0);
-                load(b + c * OPB + SUB, &tmB, n + 64, k0);
-              } else {
-                load(b + c * OPB, &tmB, k0, n);
-              }
-            }
+            load_a(t, stage, (t.kb0 + j) * BK, fb);
+            if (!ahead) load_b(t, stage, (t.kb0 + j) * BK, fb);
           } else {
             if (!waited) {
               wait_for_previous();
@@ -356,9 +375,11 @@ __global__ void __cluster_dims__(Shape<kShape>::kCtas, 1, 1) __launch_bounds__(T
             }
             int a_row, at;
             ext.entry(t.m, j - nb, rank, a_row, at);
+            const uint32_t a = smem_base + uint32_t(stage) * STAGE_BYTES, b = a + a_bytes;
             tma_load_2d_pair(a, &tmAx, fb, 0, a_row);
 #pragma unroll
-            for (int c = 0; c < S::kAcc; ++c) tma_load_3d_pair(b + c * OPB, &tmBx, fb, 0, n0 + c * TN, at);
+            for (int c = 0; c < S::kAcc; ++c)
+              tma_load_3d_pair(b + c * OPB, &tmBx, fb, 0, t.col0 + int(rank) * HALF + c * TN, at);
           }
           ++iter;
           if (++stage == STAGES) { stage = 0; phase ^= 1u; }
