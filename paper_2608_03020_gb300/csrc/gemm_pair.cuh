@@ -606,7 +606,7 @@ __global__ void __cluster_dims__(Shape<kShape>::kCtas, 1, 1) __launch_bounds__(T
             for (int i = 0; i < 32; ++i)
               w[i] = pack_bf16(epi.value(pre, col0 + 64 * b + 2 * i, v[64 * b + 2 * i]),
                                epi.value(pre, col0 + 64 * b + 2 * i + 1, v[64 * b + 2 * i + 1]));
-            if (col0 + 64 * b < g.cols) store_box_bf16(box, &tmO, lane, col0 + 64 * b, r0, w);
+            if (col0 + 64 * b < (kSlim ? t.end : g.cols)) store_box_bf16(box, &tmO, lane, col0 + 64 * b, r0, w);
           }
         } else {
           epi(t, v, row, col0, lane, box, &tmO);
@@ -724,20 +724,27 @@ inline double cycles(int shape, int64_t m_tiles, int64_t cols, int64_t nkb, int 
   const double kb = double((nkb + splits - 1) / splits);
   return rounds * (kb_cycles(shape) * kb + tile_cycles(shape));
 }
-// rows: those of A, where 128 or fewer may take the single shape (0: they may not)
-inline int pick_shape(int64_t rows, int64_t m_tiles, int64_t cols, int64_t nkb, int splits) {
+// rows: those of A, where 128 or fewer may take the single shape (0: they may not).  masked: some row
+// tiles may hold no live row, which the host does not know; all, half and an eighth of them then count
+// alike (1307 rows, 131 live, d = 3368, V = 3502, loss and dH: 107 us with dZ in 42 wide tiles, 93 us in 84
+// narrow ones).
+inline int pick_shape(int64_t rows, int64_t m_tiles, int64_t cols, int64_t nkb, int splits, bool masked = false) {
   if (rows > 0 && rows <= HALF) return kSingle;
-  const bool wide = nkb <= kWideK / BK * splits &&
-                    cycles(kWide, m_tiles, cols, nkb, splits) < cycles(kNarrow, m_tiles, cols, nkb, splits);
-  return wide ? kWide : kNarrow;
+  auto cost = [&](int shape) {
+    const double c = cycles(shape, m_tiles, cols, nkb, splits);
+    return masked ? c + cycles(shape, (m_tiles + 1) / 2, cols, nkb, splits) + cycles(shape, (m_tiles + 7) / 8, cols, nkb, splits)
+                  : c;
+  };
+  return nkb <= kWideK / BK * splits && cost(kWide) < cost(kNarrow) ? kWide : kNarrow;
 }
 
-// Width of the single shape's tiles: as few rounds of the CTAs as 256 columns would take, in equal parts.
-inline int slim_width(int64_t cols) {
+// Width of the single shape's tiles: as few rounds of the CTAs as 256 columns would take, in equal parts
+// of whole units of 16 columns (64 where they are stored in boxes).
+inline int slim_width(int64_t cols, int unit = 16) {
   const int64_t at_once = sm_count();
   const int64_t rounds = (cols + TN * at_once - 1) / (TN * at_once);
   const int64_t w = (cols + rounds * at_once - 1) / (rounds * at_once);
-  return int((w + 15) / 16 * 16);
+  return int((w + unit - 1) / unit * unit);
 }
 
 template <int kShape, bool kAmn, bool kBmn, class Epi, class Ext>

@@ -456,12 +456,13 @@ struct BwdWs {
 // range (written, then read by k_head_dh).  Both sides of the choice in cycles.
 int dh_splits(int64_t n, int64_t rows, int64_t d, int64_t vc) {
   const int64_t m = rows / gp::TM, nkb = vc / gp::BK;
+  const bool single = n > 0 && n <= gp::HALF;
+  const double range = double(single ? n : rows) * double(d) * 8.0 / 3000.0 + gp::kRangeCycles;
   int best = 1;
   double best_c = 0;
   for (int s = 1; s <= 32; ++s) {
-    if (s > 1 && nkb / s < 16) break;
-    const double c = gp::cycles(gp::pick_shape(n, m, d, nkb, s), m, d, nkb, s) + 
-                     double(s) * (double(rows) * double(d) * 8.0 / 3000.0 + gp::kRangeCycles);
+    if (s > 1 && nkb / s < (single ? 4 : 16)) break;
+    const double c = gp::cycles(gp::pick_shape(n, m, d, nkb, s), m, d, nkb, s) + double(s) * range;
     if (s == 1 || c < best_c) {
       best = s;
       best_c = c;
@@ -592,15 +593,18 @@ cudaError_t launch_head_loss_backward(const void* H, int64_t ldh, int64_t N, int
       const int64_t vn = V - v0 < lay.vc ? V - v0 : lay.vc;   // columns of the vocabulary
       const int64_t vtiles = (vn + gp::TN - 1) / gp::TN;
       CUtensorMap mh, mw, mz_out, mz_k, mw_mn;
-      if (!gp::map_kmajor(&mh, r.H + p0 * d, d, rows, d) || !gp::map_kmajor(&mw, Wb + v0 * d, d, vn, d) ||
-          !gp::map_out_bf16(&mz_out, dz, lay.vc, lay.piece, lay.vc))
-        return cudaErrorInvalidValue;
+      const bool single = N > 0 && N <= gp::HALF;
       gp::Geo g = geo(rows / gp::TM, vn, (d + gp::BK - 1) / gp::BK, kSegKb, r, status);
       g.rows_live = r.count;
       g.m_first = int(p0 / gp::TM);
-      g.rows = int(N);
-      e = gp::launch_either<false, false>(mh, mw, mh, mw, mz_out, g,
-                                          EpiDz{r.lse + p0, r.w + p0, r.y + p0, r.count, p0, v0, int(vn)}, gp::NoExt{}, s);
+      g.arows = single ? int(round_up(N, 8)) : gp::HALF;
+      g.width = single ? gp::slim_width(vn, 64) : gp::TN;
+      if (!gp::map_2d(&mh, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, r.H + p0 * d, d, rows, d, gp::BK, g.arows) ||
+          !gp::map_2d(&mw, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, Wb + v0 * d, d, vn, d, gp::BK, g.width / 2) ||
+          !gp::map_out_bf16(&mz_out, dz, lay.vc, lay.piece, lay.vc))
+        return cudaErrorInvalidValue;
+      e = gp::launch_shape<false, false>(gp::pick_shape(N, g.m_tiles, vn, g.nkb, 1, true), mh, mw, mh, mw, mz_out, g,
+                                         EpiDz{r.lse + p0, r.w + p0, r.y + p0, r.count, p0, v0, int(vn)}, gp::NoExt{}, s);
       if (e != cudaSuccess) return e;
       if (dH) {
         CUtensorMap mo;
