@@ -78,8 +78,8 @@ int loca_version(void);
  * other waits of its launch give up, lets the copies and MMAs already in flight land, frees its
  * tensor memory and returns, so the context stays usable.  This sets, for the whole process,
  * how long such a wait may take in the tensor-core kernels (loca_targets, loca_kspace_accumulate,
- * the CTA-pair Gram / cross kernel of loca_gram_cross, loca_accumulate and their variants, and the
- * projection of loca_ridge_solve)
+ * the CTA-pair Gram / cross kernel of loca_gram_cross, loca_accumulate and their variants, the
+ * projection of loca_ridge_solve, loca_head_loss, loca_adapter_apply and their backward calls)
  * before it gives up: ns = 0 restores the default of 4 s; a tiny value makes a call time out on
  * purpose, to test that path.
  */
@@ -543,7 +543,7 @@ int loca_head_loss_backward(const void* H, int64_t ldh, int64_t N, int64_t d, co
  *                    fp32; Y is rounded once
  * loca_adapter_backward  dX (like Y; with row pitch), dA (n x d_in x k) and dB (n x d_out x k) of
  *                    type grad_dtype; each may be NULL, not all.  U and T are kept to 2^-26 for dA
- *                    and dB.  An adapter without a token gets zeros.  A token outside an adapter
+ *                    and dB in LOCA_F32 and to 2^-17 in LOCA_BF16.  An adapter without a token gets zeros.  A token outside an adapter
  *                    reaches its gradients in no way, whatever its row holds
  * loca_adapter_workspace_size  scratch of one apply (backward 0) or of apply and backward (1)
  * All are deterministic.  X, dY, Y, dX, W 16-byte aligned, row pitches multiples of 8.

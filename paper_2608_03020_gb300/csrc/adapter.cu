@@ -15,14 +15,20 @@
 //                     projection of a step)
 //   k_adapter_pack    A and s B as three bf16 parts (hi + mid + lo = the fp32 value to 2^-26)
 //   k_adapter_shrink  U (or T) of every slot: tokens x k sums over d.  Bound: the read of X
-//   k_gemm_pair       the extended product in 256 x 256 tiles (many tokens)
+//   k_adapter_tokens  U of single tokens, where most have an adapter of their own.  Bound: the read of
+//                     the adapters
+//   k_gemm_pair       the extended product in 256 x 256 or 256 x 512 tiles (many tokens).  Bound: the
+//                     tensor cores (8192 tokens of 8 requests at d_in = d_out = 2048, k = 32: 61 us for
+//                     the call, 1.15 PFLOP/s)
 //   k_adapter_few     the extended product with the roles of the operands exchanged, W's rows as M,
-//                     the tokens as N, k split over a cluster (few tokens).  Bound: the read of W
+//                     the tokens as N, k split over a cluster (few tokens).  Bound: the read of W, and
+//                     with more than 128 tokens what one SM can fetch from L2
 //   k_adapter_grad    dA and dB: channels x k sums over an adapter's tokens.  Bound: the read of X, dY
 //   k_adapter_join    sums the token ranges of dA, dB in a fixed order, scales, rounds once
 // Rounding.  The low-rank term of a bf16 output uses the first part of U and of s B: its relative
-// error 2^-8 is of a term that is itself rounded to bf16 with the sum.  dA and dB may be fp32, so U and
-// T are then summed from all three parts of the adapters and passed on in three parts.
+// error 2^-8 is of a term that is itself rounded to bf16 with the sum.  fp32 gradients dA and dB take U
+// and T summed from all three parts of the adapters and pass them on in three parts; bf16 gradients
+// two (2^-17, next to their own rounding of 2^-9).
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
@@ -702,8 +708,14 @@ __global__ void __launch_bounds__(kTokThreads) k_adapter_tokens(const TokGeo g) 
 //   slots (batches that share few adapters)  as k blocks behind those of W and X, from U's slots
 //   tokens (an adapter for most tokens)      the epilogue warps, idle until the sums are complete,
 //                                            multiply U by each token's rows of s B meanwhile: a
-//                                            k-block per adapter would cost as much as W itself
-// The loads of W and X do not wait for U; only what follows them does.
+//                                            k-block per adapter would cost as much as W itself.  The
+//                                            rows of the first `held` tokens come to shared memory
+//                                            before U is there (64 adapters of rank 16 at d = 3584: 26
+//                                            us without, 20 with), the others' from L2 when it is
+// The loads of W and X do not wait for U; only what follows them does.  Measured: one token at d_in =
+// d_out = 3584 9.4 us with k_adapter_tokens, 64 tokens without an adapter 10.2 us (W at 2.5 TB/s: the
+// call's two launches and the sums' way through the cluster are two thirds of it), 512 tokens 26 us at
+// d = 4096, 0.31 us a k-block and CTA (105 GB/s per SM, 11.7 TB/s from L2 in all).
 constexpr int kFewThreads = 192;
 constexpr int kWBytes = 128 * 64 * 2;
 
@@ -1080,9 +1092,11 @@ struct EpiRows {
 // range).  M = channels, N = the columns of U or T (kp per part, side by side), K = the slots' 128 tokens
 // in two stages, both operands MN-major as they lie in memory.  A range that crosses from one adapter to
 // the next writes a partial sum for each: range r's of adapter a is number r + a (each step of the list
-// raises r or a, so no two share a number).  The segments (512 tokens) are added in registers.  A slot whose tile also holds other
-// tokens has those rows of X (or dY) zeroed in shared memory first: their U is zero, but a product with
-// whatever else stands there (infinities, NaN) need not be.
+// raises r or a, so no two share a number).  The segments (512 tokens) are added in registers.  A slot
+// whose tile also holds other tokens has those rows of X (or dY) zeroed in shared memory first: their U
+// is zero, but a product with whatever else stands there (infinities, NaN) need not be.  Measured, X and
+// dY from HBM: 16384 tokens x 2 x 896 channels 17.4 us (3.4 TB/s; launch and join of the ranges aside),
+// 8191 tokens x 2 x 3584 channels 31 us (3.8 TB/s): the ring of 18 KB boxes is short of HBM's latency.
 constexpr int kGradThreads = 224;
 constexpr int kGradMaxStages = 8;
 constexpr int kGradSeg = 8;
@@ -1643,7 +1657,8 @@ cudaError_t shrink(const Call& c, const Shrink* set, int sets, const int32_t* ma
   g.abort_flag = c.abort_flag;
   g.limit_ns = wait_limit_ns();
   g.mark = c.mark;
-  // slots are known to the device only: between one per tile and smax
+  // slots are known to the device only: between one per tile and smax.  An item's beginning and end
+  // cost about as much as six k-blocks (2 us)
   int64_t guess = c.p.tiles > c.n ? c.p.tiles : c.n;
   if (guess > c.p.smax) guess = c.p.smax;
   const int ks = cluster_split(guess * sets, (dmin + 63) / 64, 6, true);
@@ -1679,6 +1694,9 @@ cudaError_t project(const Call& c, const void* X, int64_t ldx, int64_t d, const 
                     const __nv_bfloat16* P, const void* U, bool token_sums, void* Y, int64_t ldy) {
   const int64_t slots = c.p.smax;
   const int64_t tiles = ((c.N + gp::TM - 1) / gp::TM) * ((o + gp::TN - 1) / gp::TN);
+  // Tiles of 128 x 128 by single CTAs fetch twice the bytes per product that a pair's 256 x 256 do, but
+  // four times as many fill the SMs.  With 32 pair tiles (1024 tokens x 2048 channels) they take 11.9 us
+  // at d = 1024 and 26 at 4096; one round of pairs takes 15 and 32 whatever it holds up to 76.
   const bool few = token_sums || c.N <= kTile || 2 * tiles < sm_count() / 2;
   CUtensorMap mw, mx, mb, mu;
   if (kWmn ? !gp::map_mnmajor(&mw, W, o, d, o) : !gp::map_kmajor(&mw, W, d, o, d)) return cudaErrorInvalidValue;
@@ -1713,6 +1731,8 @@ cudaError_t project(const Call& c, const void* X, int64_t ldx, int64_t d, const 
         !gp::map_2d(&mu, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, U, kMaxK, slots * kSlotRows, kMaxK, 64, g.nt))
       return cudaErrorInvalidValue;
     const int64_t ot = (o + 127) / 128, nt = (c.N + g.nt - 1) / g.nt;
+    // (5 us of beginning and end are worth 16 k-blocks of 128 tokens; they keep 56 tiles in one round of
+    // two CTAs each where five each would take two: 28 us against 35 at d = 8192)
     const int ks = cluster_split(ot * nt, (d + 63) / 64, 16, false);
     // slots of one tile: a ring that fits beside a CTA of k_adapter_shrink with its small one
     const int stage = kWBytes + g.nt * 128;

@@ -18,7 +18,7 @@
 // and two buffers; B's read from HBM is then the bound.  With B K-major its tiles may be narrower than
 // 256 columns (`width`, a multiple of 16), so that the last round of CTAs is as full as the others, and
 // A's loads bring only the rows there are (the MMA's other rows read what lies behind; nobody reads
-// their sums): the ring is as deep as that allows.
+// their sums): the ring is as deep as that allows.  (16 stages instead of at most 8 gained nothing.)
 //   warp 0       TMA producer (both CTAs): its CTA's 128 rows of A and 128 rows of B per accumulator
 //   warp 1       one thread of the even CTA issues the MMAs (M = 256, N = 256, K = 16)
 //   warps 2..9   take the sums out of TMEM: warp w holds rows 32 (w & 3) .. + 31 of its CTA, one row
@@ -731,9 +731,10 @@ inline double cycles(int shape, int64_t m_tiles, int64_t cols, int64_t nkb, int 
 inline int pick_shape(int64_t rows, int64_t m_tiles, int64_t cols, int64_t nkb, int splits, bool masked = false) {
   if (rows > 0 && rows <= HALF) return kSingle;
   auto cost = [&](int shape) {
-    const double c = cycles(shape, m_tiles, cols, nkb, splits);
-    return masked ? c + cycles(shape, (m_tiles + 1) / 2, cols, nkb, splits) + cycles(shape, (m_tiles + 7) / 8, cols, nkb, splits)
-                  : c;
+    double c = 0;
+    for (int part = 1; part <= (masked ? 8 : 1); part = part == 1 ? 2 : 4 * part)
+      c += cycles(shape, (m_tiles + part - 1) / part, cols, nkb, splits);
+    return c;
   };
   return nkb <= kWideK / BK * splits && cost(kWide) < cost(kNarrow) ? kWide : kNarrow;
 }

@@ -19,6 +19,11 @@
 // k_head_dh      sums the k ranges of dH, scales, rounds once and puts each row back in its place
 // Computing the logits a second time costs 2 N d V operations; keeping them would cost 4 N V bytes
 // (2.5 GB per 4096 tokens at V = 151936).
+// Bound: the tensor cores from a few hundred tokens on, the read of W below.  8192 live of 16384 tokens at
+// d = 2048, V = 49152: 1.06 ms (1.55 PFLOP/s; the rest is the epilogue's exponentials and the clock under
+// load); 37 tokens 48 us (201 MB of W: 4.2 TB/s for the call, 4.8 in k_gemm_pair).  Loss and dH of 1531
+// tokens at d = 5120, V = 151936: 4.4 ms for 7.15 TFLOP (1.62 PFLOP/s).  Up to 128 tokens each gradient
+// reads W again (8 tokens at d = 4648, V = 70557: 353 us for three reads of 656 MB).
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
@@ -635,8 +640,8 @@ cudaError_t launch_head_loss_backward(const void* H, int64_t ldh, int64_t N, int
     if (dH) {
       const int64_t blocks = rows * (d / 8) / 256 + 1;
       const int64_t most = 8 * int64_t(sm_count());
-      e = gp::launch_early(k_head_dh, dim3(unsigned(blocks < most ? blocks : most)), dim3(256), 0, s, part, rows, lay.splits, fit, d, r, p0, scale,
-                           static_cast<__nv_bfloat16*>(dH), lddh);
+      e = gp::launch_early(k_head_dh, dim3(unsigned(blocks < most ? blocks : most)), dim3(256), 0, s, part, rows,
+                           lay.splits, fit, d, r, p0, scale, static_cast<__nv_bfloat16*>(dH), lddh);
       if (e != cudaSuccess) return e;
     }
   }
