@@ -1429,9 +1429,9 @@ struct JoinOne {
   int ranges;
 };
 // One adapter's gradient per (y, z) of the grid.  kLanes lanes share the ranges of four neighbouring
-// columns of a channel; their sums meet in a fixed order.  Four where a product was cut into many ranges
-// (one adapter, 23 ranges, 896 channels), one where it was not: 7 adapters of rank 64 over 5120
-// channels in two ranges took 26 us with four.
+// columns of a channel; their sums meet in a fixed order.  Four where the sums were cut into many ranges
+// (16384 tokens of one adapter over 2 x 896 channels: ten, 5 us), one where they were not: 7 adapters of
+// rank 64 over 5120 channels in two ranges took 26 us with four and takes 10 with one.
 template <class T, int kLanes>
 __global__ void __launch_bounds__(256)
     k_adapter_join(const JoinOne j0, const JoinOne j1, int k, int kp, const int32_t* __restrict__ plan,
