@@ -710,8 +710,8 @@ __global__ void __launch_bounds__(kTokThreads) k_adapter_tokens(const TokGeo g) 
 //                                            multiply U by each token's rows of s B meanwhile: a
 //                                            k-block per adapter would cost as much as W itself.  The
 //                                            rows of the first `held` tokens come to shared memory
-//                                            before U is there (64 adapters of rank 16 at d = 3584: 26
-//                                            us without, 20 with), the others' from L2 when it is
+//                                            before U is there (64 adapters of rank 16 at d = 3584: 4
+//                                            us less), the others' from L2 when it is
 // The loads of W and X do not wait for U; only what follows them does.  Measured: one token at d_in =
 // d_out = 3584 9.4 us with k_adapter_tokens, 64 tokens without an adapter 10.2 us (W at 2.5 TB/s: the
 // call's two launches and the sums' way through the cluster are two thirds of it), 512 tokens 26 us at
@@ -757,7 +757,7 @@ __device__ __forceinline__ void epi_bar() { asm volatile("bar.sync 1, 128;" ::: 
 // epilogue warp takes a token, a lane four channels.  kAhead tokens are on the way at once: many where
 // a CTA has many and no other's sums to fetch (one channel a lane: 512 tokens by 3584 channels at
 // d = 1024 23.4 us, so 12.3), one at a time in a wide cluster, where more only made the code longer (64
-// tokens at d = 3584 20.5 us with four).
+// tokens at d = 3584: 0.5 us more with four).
 template <int kSplits, int kAhead>
 __device__ __forceinline__ void few_out(const FewGeo& g, const float* low, float* red, int own, int ks, int rank,
                                         int64_t n0, int ntok, int o0) {
@@ -1605,12 +1605,16 @@ int clusters_at_once(int ks) {
 }
 
 // CTAs that share the k axis of an item: whole rounds of the clusters that run at once, each of a CTA's
-// k-blocks and `fixed` more for its beginning and end.
-int cluster_split(int64_t items, int64_t blocks, int64_t fixed, bool powers) {
+// k-blocks and `fixed` more for its beginning and end.  crowded: the SMs come free one by one, and
+// clusters of three and more then do not pack as tightly as on an idle chip (64 adapters at d_in = d_out =
+// 3584: of 28 clusters of five the last began when the first had ended, 20.0 us; 28 of four, where 36
+// fit, 14.2; 200 tokens of 8 requests at 2048 x 2048 14.9 and 13.5; in some sizes the smaller split costs
+// up to 6 %).
+int cluster_split(int64_t items, int64_t blocks, int64_t fixed, bool powers, bool crowded) {
   int best = 1;
   int64_t best_c = 0;
   for (int ks = 1; ks <= 8 && (ks == 1 || blocks >= 2 * ks); ks = powers ? 2 * ks : ks + 1) {
-    const int at_once = clusters_at_once(ks);
+    const int at_once = clusters_at_once(ks) * (crowded && ks > 2 ? 7 : 8) / 8;
     const int64_t rounds = (items + at_once - 1) / at_once;
     const int64_t c = rounds * ((blocks + ks - 1) / ks + fixed);
     if (ks == 1 || c < best_c) {
@@ -1661,7 +1665,7 @@ cudaError_t shrink(const Call& c, const Shrink* set, int sets, const int32_t* ma
   // cost about as much as six k-blocks (2 us)
   int64_t guess = c.p.tiles > c.n ? c.p.tiles : c.n;
   if (guess > c.p.smax) guess = c.p.smax;
-  const int ks = cluster_split(guess * sets, (dmin + 63) / 64, 6, true);
+  const int ks = cluster_split(guess * sets, (dmin + 63) / 64, 6, true, false);
   int64_t clusters = clusters_at_once(ks);
   if (clusters > c.p.smax * sets) clusters = c.p.smax * sets;
   const int second = sets - 1;
@@ -1733,7 +1737,9 @@ cudaError_t project(const Call& c, const void* X, int64_t ldx, int64_t d, const 
     const int64_t ot = (o + 127) / 128, nt = (c.N + g.nt - 1) / g.nt;
     // (5 us of beginning and end are worth 16 k-blocks of 128 tokens; they keep 56 tiles in one round of
     // two CTAs each where five each would take two: 28 us against 35 at d = 8192)
-    const int ks = cluster_split(ot * nt, (d + 63) / 64, 16, false);
+    // by k_adapter_shrink's CTAs, or by two and more blocks of k_adapter_tokens on an SM
+    const bool crowded = !token_sums || c.N * g.ranges > 2 * sm_count();
+    const int ks = cluster_split(ot * nt, (d + 63) / 64, 16, false, crowded);
     // slots of one tile: a ring that fits beside a CTA of k_adapter_shrink with its small one
     const int stage = kWBytes + g.nt * 128;
     const int low = token_sums ? few_low(g.nt, ks, c.kp) : 0;
