@@ -492,8 +492,9 @@ int loca_calib_fit_rsvd(const float* E_probe, const float* G_probe, int64_t Np, 
  * label_cols  C int32 vocabulary indices in [0, V), 1 <= C <= 1024; with E only (else NULL, C 0)
  * loss        N float output;  lse  N float output, or NULL;  E  N x C float output, or NULL
  * d a multiple of 8, ldh a multiple of 8, H and W 16-byte aligned (TMA); N, V <= 2^24, d <= 65536.
- * Arithmetic: bf16 products on the tensor cores, fp32 sums restarted every 1024 terms, fp32
- * exponentials and normalisers.  Deterministic.  Masked positions cost no product.
+ * Arithmetic: bf16 products on the tensor cores, fp32 sums restarted every 1024 terms (every 256
+ * for up to 128 positions), fp32 exponentials and normalisers.  Deterministic.  Masked positions
+ * cost no product.
  */
 int loca_head_loss_workspace_size(int64_t N, int64_t V, int64_t d, int32_t C, size_t* bytes);
 int loca_head_loss(const void* H, int64_t ldh, int64_t N, int64_t d, const void* W, int64_t V, const int32_t* y,
