@@ -1604,17 +1604,23 @@ int clusters_at_once(int ks) {
   return n;
 }
 
+// The same on SMs that come free one by one: clusters of three and more then do not pack as tightly as on
+// an idle chip (64 adapters at d_in = d_out = 3584: of 28 clusters of five the last began when the first
+// had ended, 20.0 us; 28 of four, where 36 fit, 14.2; 200 tokens of 8 requests at 2048 x 2048 14.9 and
+// 13.5 us; forward and gradients of 780 tokens, 1792 x 4088, with U's clusters planned so 92 and 86 us; in
+// some sizes the smaller split costs up to 6 %).
+int clusters_at_once(int ks, bool crowded) {
+  const int n = clusters_at_once(ks);
+  return crowded && ks > 2 && n > 1 ? n * 7 / 8 : n;
+}
+
 // CTAs that share the k axis of an item: whole rounds of the clusters that run at once, each of a CTA's
-// k-blocks and `fixed` more for its beginning and end.  crowded: the SMs come free one by one, and
-// clusters of three and more then do not pack as tightly as on an idle chip (64 adapters at d_in = d_out =
-// 3584: of 28 clusters of five the last began when the first had ended, 20.0 us; 28 of four, where 36
-// fit, 14.2; 200 tokens of 8 requests at 2048 x 2048 14.9 and 13.5; in some sizes the smaller split costs
-// up to 6 %).
+// k-blocks and `fixed` more for its beginning and end.
 int cluster_split(int64_t items, int64_t blocks, int64_t fixed, bool powers, bool crowded) {
   int best = 1;
   int64_t best_c = 0;
   for (int ks = 1; ks <= 8 && (ks == 1 || blocks >= 2 * ks); ks = powers ? 2 * ks : ks + 1) {
-    const int at_once = clusters_at_once(ks) * (crowded && ks > 2 ? 7 : 8) / 8;
+    const int at_once = clusters_at_once(ks, crowded);
     const int64_t rounds = (items + at_once - 1) / at_once;
     const int64_t c = rounds * ((blocks + ks - 1) / ks + fixed);
     if (ks == 1 || c < best_c) {
@@ -1665,8 +1671,8 @@ cudaError_t shrink(const Call& c, const Shrink* set, int sets, const int32_t* ma
   // cost about as much as six k-blocks (2 us)
   int64_t guess = c.p.tiles > c.n ? c.p.tiles : c.n;
   if (guess > c.p.smax) guess = c.p.smax;
-  const int ks = cluster_split(guess * sets, (dmin + 63) / 64, 6, true, false);
-  int64_t clusters = clusters_at_once(ks);
+  const int ks = cluster_split(guess * sets, (dmin + 63) / 64, 6, true, true);
+  int64_t clusters = clusters_at_once(ks, true);
   if (clusters > c.p.smax * sets) clusters = c.p.smax * sets;
   const int second = sets - 1;
   return launch_cluster(k_adapter_shrink, dim3(unsigned(clusters * ks)), kShrinkThreads, shrink_smem(ctiles, g.stages),
