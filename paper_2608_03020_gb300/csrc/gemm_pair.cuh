@@ -27,8 +27,10 @@
 // sum at every step, always toward zero.  The sums restart every `seg_kb` k-blocks and the epilogue
 // warps add the segments in registers with round-to-nearest additions, which bounds that bias whatever
 // K is (a logit at K = 5120 comes out ~10x nearer to its 64-bit value than with one accumulator).  A
-// segment is also the unit of the TMEM double buffer.  The wide shape serves outputs in bf16 with K up
-// to kWideK, where the bias (below 2^-13 of a sum) disappears in the rounding.
+// segment is also the unit of the TMEM double buffer.  The wide shape never restarts: it serves outputs
+// that are the sum itself, rounded to bf16, with K up to kWideK.  A step loses up to 2^-22 of the
+// running sum, so 1024 steps lose up to 2^-12 of it, within the rounding's 2^-9.  It does not serve logits,
+// whose exponentials turn a bias of the sum into one of the result.
 // Every wait is bounded; the failure path is that of the Gram kernel: the first waiter that gives up
 // records LOCA_ERR_TIMEOUT and raises the launch's abort flag, every role stops at its own point,
 // the even CTA settles the copies that only one CTA issued, MMAs and copies in flight land, TMEM is
@@ -724,19 +726,11 @@ inline double cycles(int shape, int64_t m_tiles, int64_t cols, int64_t nkb, int 
   const double kb = double((nkb + splits - 1) / splits);
   return rounds * (kb_cycles(shape) * kb + tile_cycles(shape));
 }
-// rows: those of A, where 128 or fewer may take the single shape (0: they may not).  masked: some row
-// tiles may hold no live row, which the host does not know; all, half and an eighth of them then count
-// alike (1307 rows, 131 live, d = 3368, V = 3502, loss and dH: 107 us with dZ in 42 wide tiles, 93 us in 84
-// narrow ones).
-inline int pick_shape(int64_t rows, int64_t m_tiles, int64_t cols, int64_t nkb, int splits, bool masked = false) {
+// rows: those of A, where 128 or fewer may take the single shape (0: they may not).
+inline int pick_shape(int64_t rows, int64_t m_tiles, int64_t cols, int64_t nkb, int splits) {
   if (rows > 0 && rows <= HALF) return kSingle;
-  auto cost = [&](int shape) {
-    double c = 0;
-    for (int part = 1; part <= (masked ? 8 : 1); part = part == 1 ? 2 : 4 * part)
-      c += cycles(shape, (m_tiles + part - 1) / part, cols, nkb, splits);
-    return c;
-  };
-  return nkb <= kWideK / BK * splits && cost(kWide) < cost(kNarrow) ? kWide : kNarrow;
+  const bool wide = cycles(kWide, m_tiles, cols, nkb, splits) < cycles(kNarrow, m_tiles, cols, nkb, splits);
+  return wide && nkb <= kWideK / BK * splits ? kWide : kNarrow;
 }
 
 // Width of the single shape's tiles: as few rounds of the CTAs as 256 columns would take, in equal parts

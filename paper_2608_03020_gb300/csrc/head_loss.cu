@@ -10,7 +10,10 @@
 // k_gemm_pair    logit tiles (256 x 256) on the tensor cores.  Forward: each epilogue thread has 128
 //                logits of one row in registers and writes their maximum and sum of exponentials,
 //                plus the target's and the label words' logits where its columns hold them.
-//                Backward: the same tiles again, turned into dZ = g w (p - onehot), rounded to bf16
+//                Backward: the same tiles again, summed in the same segments (p = exp(z - lse) is only
+//                as good as z and lse agree: with one accumulator over d = 5120 the gradient of a
+//                position with 1 - p = 1e-5 came out 50 times too large), turned into
+//                dZ = g w (p - onehot), rounded to bf16
 //                as the operand of the two gradient products, for one piece of the vocabulary at a
 //                time (a bf16 operand moves a sum of many such products by less than the gradients'
 //                own rounding to bf16; the factor `scale` is applied to the fp32 sums, so it
@@ -604,7 +607,8 @@ cudaError_t launch_head_loss_backward(const void* H, int64_t ldh, int64_t N, int
       const int64_t vtiles = (vn + gp::TN - 1) / gp::TN;
       CUtensorMap mh, mw, mz_out, mz_k, mw_mn;
       const bool single = N > 0 && N <= gp::HALF;
-      gp::Geo g = geo(rows / gp::TM, vn, (d + gp::BK - 1) / gp::BK, kSegKb, r, status);
+      // the forward pass's shape and segments, so that z comes out as it went into lse
+      gp::Geo g = geo(rows / gp::TM, vn, (d + gp::BK - 1) / gp::BK, single ? kSegKbFew : kSegKb, r, status);
       g.rows_live = r.count;
       g.m_first = int(p0 / gp::TM);
       g.arows = single ? int(round_up(N, 8)) : gp::HALF;
@@ -613,8 +617,9 @@ cudaError_t launch_head_loss_backward(const void* H, int64_t ldh, int64_t N, int
           !gp::map_2d(&mw, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, Wb + v0 * d, d, vn, d, gp::BK, g.width / 2) ||
           !gp::map_out_bf16(&mz_out, dz, lay.vc, lay.piece, lay.vc))
         return cudaErrorInvalidValue;
-      e = gp::launch_shape<false, false>(gp::pick_shape(N, g.m_tiles, vn, g.nkb, 1, true), mh, mw, mh, mw, mz_out, g,
-                                         EpiDz{r.lse + p0, r.w + p0, r.y + p0, r.count, p0, v0, int(vn)}, gp::NoExt{}, s);
+      const EpiDz dzed{r.lse + p0, r.w + p0, r.y + p0, r.count, p0, v0, int(vn)};
+      e = single ? gp::launch<gp::kSingle, false, false>(mh, mw, mh, mw, mz_out, g, dzed, gp::NoExt{}, s)
+                 : gp::launch<gp::kNarrow, false, false>(mh, mw, mh, mw, mz_out, g, dzed, gp::NoExt{}, s);
       if (e != cudaSuccess) return e;
       if (dH) {
         CUtensorMap mo;
