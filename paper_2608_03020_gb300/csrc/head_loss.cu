@@ -200,15 +200,15 @@ struct EpiStats {
       m3 = fmaxf(m3, v[i + 3]);
     }
     const float m = fmaxf(fmaxf(m0, m1), fmaxf(m2, m3));
+    // (a maximum passes over NaN, also where it finds nothing else: the sum of exponentials keeps it)
+    const float base = m == -INFINITY ? 0.f : m;
     float s0 = 0.f, s1 = 0.f, s2 = 0.f, s3 = 0.f;
-    if (left > 0 && m != -INFINITY) {
 #pragma unroll
-      for (int i = 0; i < 128; i += 4) {
-        s0 += exp_diff(v[i], m);
-        s1 += exp_diff(v[i + 1], m);
-        s2 += exp_diff(v[i + 2], m);
-        s3 += exp_diff(v[i + 3], m);
-      }
+    for (int i = 0; i < 128; i += 4) {
+      s0 += exp_diff(v[i], base);
+      s1 += exp_diff(v[i + 1], base);
+      s2 += exp_diff(v[i + 2], base);
+      s3 += exp_diff(v[i + 3], base);
     }
     part[int64_t(2 * t.n + (col0 > t.col0 ? 1 : 0)) * pitch + row] = make_float2(m, (s0 + s1) + (s2 + s3));
     const int at = y[row] - col0;
