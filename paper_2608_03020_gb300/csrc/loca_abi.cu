@@ -36,17 +36,29 @@ constexpr int kMaxDevices = 64;
 
 }  // namespace
 
+// The encoder is a driver call: unlike a runtime call it needs a context that is current in the calling
+// thread, which a host thread without a CUDA call so far does not have.
 TensorMapEncodeFn tensor_map_encoder() {
   static TensorMapEncodeFn fn = nullptr;
+  static CUresult (*current)(CUcontext*) = nullptr;
   static std::once_flag once;
   std::call_once(once, [] {
     void* p = nullptr;
     cudaDriverEntryPointQueryResult q;
+    if (cudaGetDriverEntryPointByVersion("cuCtxGetCurrent", &p, 12000, cudaEnableDefault, &q) != cudaSuccess ||
+        q != cudaDriverEntryPointSuccess)
+      return;
+    current = reinterpret_cast<CUresult (*)(CUcontext*)>(p);
     if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &q) ==
             cudaSuccess &&
         q == cudaDriverEntryPointSuccess)
       fn = reinterpret_cast<TensorMapEncodeFn>(p);
   });
+  CUcontext ctx = nullptr;
+  int dev = 0;
+  if (fn && (current(&ctx) != CUDA_SUCCESS || !ctx) &&
+      (cudaGetDevice(&dev) != cudaSuccess || cudaSetDevice(dev) != cudaSuccess))
+    return nullptr;
   return fn;
 }
 

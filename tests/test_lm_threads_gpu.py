@@ -31,49 +31,36 @@ CALLS = {
 }
 
 
-def _program(lc, N, d, o, k, n, seed):
+def _arguments(lc, N, d, o, k, n, seed):
     g = torch.Generator(device="cuda")
     g.manual_seed(seed)
     rn = lambda *s: torch.randn(s, generator=g, device="cuda")  # noqa: E731
-    X, W, dY = rn(N, d).to(torch.bfloat16), (rn(o, d) / d ** 0.5).to(torch.bfloat16), rn(N, o).to(torch.bfloat16)
-    A, B = rn(n, d, k) / d ** 0.5, rn(n, o, k)
+    m = dict(X=rn(N, d).to(torch.bfloat16), W=(rn(o, d) / d ** 0.5).to(torch.bfloat16))
     ids = torch.randint(0, n, (N,), generator=g, device="cuda", dtype=torch.int32)
-    ad, plan = lc.AdapterSet(n, d, o, k).pack(A, B), lc.AdapterPlan(ids, n)
-    ws = torch.empty(lc.adapter_workspace_size(N, d, o, k, n, backward=True), dtype=torch.uint8, device="cuda")
-    Y, dX, dA = torch.empty_like(dY), torch.empty_like(X), torch.empty_like(A)
-
-    def call():
-        lc.loca_adapter_apply(X, W, ad, plan, Y, workspace=ws)
-        lc.loca_adapter_backward(X, dY, W, ad, plan, dX=dX, dA=dA, workspace=ws)
-        return Y, dX, dA
-
-    return call
-
-
-def test_threads_with_calls_of_different_sizes(lc):
-    programs = [_program(lc, *sizes, seed=i) for i, sizes in enumerate(CALLS.values())]
-    want = [[t.clone() for t in p()] for p in programs]
+    m["set"] = lc.AdapterSet(n, d, o, k).pack(rn(n, d, k) / d ** 0.5, rn(n, o, k))
+    m["plan"] = lc.AdapterPlan(ids, n)
+    m["ws"] = torch.empty(lc.adapter_workspace_size(N, d, o, k, n), dtype=torch.uint8, device="cuda")
+    m["Y"] = torch.empty((N, o), dtype=torch.bfloat16, device="cuda")
+    p = lc._ptr
+    m["args"] = (p(m["X"]), d, N, d, p(m["W"]), o, p(m["set"].packed), n, k, p(m["plan"].buf), p(m["Y"]), o, p(m["ws"]),
+                 m["ws"].numel())
     torch.cuda.synchronize()
-    failed, start = [], threading.Barrier(len(programs))
+    return m
 
-    def work(i):
-        try:
-            s = torch.cuda.Stream()
-            with torch.cuda.stream(s):
-                start.wait(timeout=60)
-                for _ in range(1500):
-                    got = programs[i]()
-                s.synchronize()
-                for a, b in zip(want[i], got):
-                    assert torch.equal(a, b), list(CALLS)[i]
-        except Exception as e:  # noqa: BLE001 (reported below)
-            failed.append((list(CALLS)[i], repr(e)))
 
-    threads = [threading.Thread(target=work, args=(i,)) for i in range(len(programs))]
-    for t in threads:
-        t.start()
-    for t in threads:
-        t.join()
+@pytest.mark.parametrize("name", sorted(CALLS))
+def test_first_cuda_call_of_a_thread(lc, name):
+    """A host thread that has made no CUDA call has no current context yet."""
+    m = _arguments(lc, *CALLS[name], seed=1)
+    args = (*m["args"], lc._stream(None))
+    assert lc.lib().loca_adapter_apply(*args) == 0
     torch.cuda.synchronize()
-    assert not failed, failed
-    assert lc.loca_device_status() == 0
+    want, codes = m["Y"].clone(), []
+    m["Y"].zero_()
+    torch.cuda.synchronize()
+    t = threading.Thread(target=lambda: codes.append(lc.lib().loca_adapter_apply(*args)))
+    t.start()
+    t.join()
+    torch.cuda.synchronize()
+    assert codes == [0]
+    assert torch.equal(want, m["Y"]) and lc.loca_device_status() == 0
