@@ -1547,13 +1547,17 @@ struct Call {
   cudaStream_t s;
 };
 
+// The limit on dynamic shared memory that every launch of a kernel sets: the limit belongs to the kernel, not
+// to the launch, so a size of the call's own could be replaced by another thread's before the launch.
+constexpr int kMostSmem = 232448;
+
 // Every launch may start while the one before it ends (its prologue runs early; wait_for_previous()
 // holds back what depends on it).
 template <class... P, class... A>
 cudaError_t launch_cluster(void (*kernel)(P...), dim3 grid, int threads, int smem, int cluster, cudaStream_t s,
                            A... args) {
   cudaError_t e = cudaSuccess;
-  if (smem > 48 * 1024) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  if (smem > 48 * 1024) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostSmem);
   else e = gp::keep_carveout(kernel);
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
@@ -1595,7 +1599,7 @@ int clusters_at_once(int ks) {
   at[0].val.clusterDim.z = 1;
   cfg.attrs = at;
   cfg.numAttrs = 1;
-  if (cudaFuncSetAttribute(k_adapter_few<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess ||
+  if (cudaFuncSetAttribute(k_adapter_few<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostSmem) != cudaSuccess ||
       cudaOccupancyMaxActiveClusters(&n, k_adapter_few<false>, &cfg) != cudaSuccess || n < 1) {
     cudaGetLastError();
     n = sm_count() / ks;

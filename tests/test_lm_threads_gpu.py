@@ -48,6 +48,39 @@ def _arguments(lc, N, d, o, k, n, seed):
     return m
 
 
+def test_threads_with_calls_of_different_sizes(lc):
+    """The C calls in a tight loop (the interpreter's lock is free while they run): the same kernel with
+    206 KB of shared memory from one thread and with 110 KB from another."""
+    names = ["tokens", "one tile", "tokens", "one tile"]
+    made = [_arguments(lc, *CALLS[name], seed=i) for i, name in enumerate(names)]
+    fn = lc.lib().loca_adapter_apply
+    for m in made:
+        assert fn(*m["args"], lc._stream(None)) == 0
+    torch.cuda.synchronize()
+    want = [m["Y"].clone() for m in made]
+    codes, start = [{} for _ in names], threading.Barrier(len(names))
+
+    def work(i):
+        s = torch.cuda.Stream()
+        args = (*made[i]["args"], lc._stream(s))
+        start.wait(timeout=60)
+        for _ in range(100):
+            for _ in range(100):
+                rc = fn(*args)
+                codes[i][rc] = codes[i].get(rc, 0) + 1
+            s.synchronize()
+
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(len(names))]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    torch.cuda.synchronize()
+    assert codes == [{0: 10000}] * len(names), codes
+    assert all(torch.equal(w, m["Y"]) for w, m in zip(want, made))
+    assert lc.loca_device_status() == 0
+
+
 @pytest.mark.parametrize("name", sorted(CALLS))
 def test_first_cuda_call_of_a_thread(lc, name):
     """A host thread that has made no CUDA call has no current context yet."""
