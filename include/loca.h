@@ -513,9 +513,12 @@ int loca_head_loss(const void* H, int64_t ldh, int64_t N, int64_t d, const void*
  * dH     N x d bf16 output, row pitch lddh (a multiple of 8), or NULL; rows of masked positions are
  *        0.  With unit weights it is the d-wide top error that loca_calib_fit_rsvd takes (in fp32)
  * dW     V x d bf16 output, or NULL; at least one of dH and dW
- * The logits are computed again; dZ is rounded to bf16 as an operand, sums are fp32, each gradient
- * is rounded once.  Deterministic.  The workspace holds dZ of one piece of the vocabulary (up to
- * 1 GiB, more for a dW over more than 2^19 positions) and the fp32 sums of dH.
+ * The logits are computed again, summed as those of loca_head_loss, and the target's entry of dZ is
+ * minus the sum of the others: positions of a probability near 1 keep their small gradient.  dZ is
+ * rounded to bf16 as an operand, sums are fp32, each gradient is rounded once.  Deterministic.  The
+ * workspace holds dZ of a piece of the rows (dH alone: up to 1 GiB) or, with dW, of the vocabulary (up to
+ * 4 GiB, more over more than 2^21 positions) and the fp32 sums of dH.  Where the vocabulary comes in
+ * pieces (dW and N V > 2^31, or dH alone and V > 2^21) the logits are computed a third time.
  */
 int loca_head_loss_backward_workspace_size(int64_t N, int64_t V, int64_t d, int want_dH, int want_dW, size_t* bytes);
 int loca_head_loss_backward(const void* H, int64_t ldh, int64_t N, int64_t d, const void* W, int64_t V,

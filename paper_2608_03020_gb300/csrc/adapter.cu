@@ -1082,6 +1082,7 @@ struct AdapterExt {
 struct EpiRows {
   static constexpr bool kPacks = true;
   static constexpr bool kFits = false;
+  static constexpr bool kSums = false;
   struct Row {};
   __device__ __forceinline__ Row row_of(int) const { return Row{}; }
   __device__ __forceinline__ float value(const Row&, int, float v) const { return v; }

@@ -226,7 +226,8 @@ struct NoExt {
 };
 
 // What becomes of a finished tile.  An output in bf16 is given value by value (kPacks): Row row_of(row)
-// reads what a row needs, before its sums are complete; value(Row, column, sum) is the output.  Other
+// reads what a row needs, before its sums are complete; value(Row, column, sum) is the output.  kSums (not
+// in the wide shape): Row adds something up over the values, which finish(Row, half tile, row) gets.  Other
 // uses take the sums themselves:  void operator()(const Tile&, float (&v)[128], int row, int col0, int lane,
 //                                   uint8_t* box, const CUtensorMap* out) const
 // called once per finished accumulator by every epilogue thread, with the sums of row `row`, columns
@@ -600,16 +601,20 @@ __global__ void __cluster_dims__(Shape<kShape>::kCtas, 1, 1) __launch_bounds__(T
         if (!go) break;
         const int col0 = t.col0 + h * HALF;
         if constexpr (Epi::kPacks) {
-          const auto pre = epi.row_of(row);
+          auto pre = epi.row_of(row);
 #pragma unroll
           for (int b = 0; b < 2; ++b) {
+            if (col0 + 64 * b >= (kSlim ? t.end : g.cols)) continue;
             uint32_t w[32];
 #pragma unroll
-            for (int i = 0; i < 32; ++i)
-              w[i] = pack_bf16(epi.value(pre, col0 + 64 * b + 2 * i, v[64 * b + 2 * i]),
-                               epi.value(pre, col0 + 64 * b + 2 * i + 1, v[64 * b + 2 * i + 1]));
-            if (col0 + 64 * b < (kSlim ? t.end : g.cols)) store_box_bf16(box, &tmO, lane, col0 + 64 * b, r0, w);
+            for (int i = 0; i < 32; ++i) {
+              const float lo = epi.value(pre, col0 + 64 * b + 2 * i, v[64 * b + 2 * i]);
+              const float hi = epi.value(pre, col0 + 64 * b + 2 * i + 1, v[64 * b + 2 * i + 1]);
+              w[i] = pack_bf16(lo, hi);
+            }
+            store_box_bf16(box, &tmO, lane, col0 + 64 * b, r0, w);
           }
+          if constexpr (Epi::kSums) epi.finish(pre, 2 * t.n + h, row);
         } else {
           epi(t, v, row, col0, lane, box, &tmO);
         }

@@ -18,6 +18,9 @@
 //                time (a bf16 operand moves a sum of many such products by less than the gradients'
 //                own rounding to bf16; the factor `scale` is applied to the fp32 sums, so it
 //                rounds nothing)
+// k_head_target  the target's p - 1 as minus the sum of the others' p.  Where a dW over many rows cuts the
+//                vocabulary into pieces (N V > 2^31) the sum over all of them comes first, from a pass
+//                over the logits of its own
 // k_head_join    combines a row's maxima and sums in a fixed order: lse, loss, E
 // k_head_dh      sums the k ranges of dH, scales, rounds once and puts each row back in its place
 // Computing the logits a second time costs 2 N d V operations; keeping them would cost 4 N V bytes
@@ -44,8 +47,11 @@ constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kRowsPerBlock = 8;          // one per warp
 constexpr int kPadBlocks = 16;         // blocks of k_head_rows that write the zero rows
 constexpr int64_t kFwdRows = 16384;    // rows per forward piece (bounds the partial maxima and sums)
-constexpr int64_t kBwdRows = 8192;     // rows per backward piece when dW is not wanted
-constexpr int64_t kDzBytes = int64_t(1) << 30;  // dZ of one piece of the vocabulary
+constexpr int64_t kBwdRows = 8192;     // rows per backward piece at most when dW is not wanted
+constexpr int64_t kDzBytes = int64_t(1) << 30;  // dZ of a piece of the rows (dH alone)
+// dZ of a piece of the vocabulary where dW sums over all rows: two pieces cost the logits once more (16384
+// tokens at d = 1024, V = 65536 with dH and dW: 5.9 ms in two pieces of 1 GiB, 4.2 in one of 2)
+constexpr int64_t kDzBytesAll = int64_t(4) << 30;
 constexpr int kSegKb = 16;             // logits: 1024 k per accumulation segment
 // Up to 128 tokens wait for W, and shorter segments cost them 1 % where they cost the pairs 12 %: the
 // error of lse comes down from 3e-7 to 8e-8 of it.  That counts for few tokens: E of a token whose target
@@ -235,11 +241,13 @@ struct EpiStats {
   }
 };
 
-// Backward: dZ = g w (p - onehot) of the same tile, bf16, for the gradient products.  Columns past
-// the vocabulary and rows past the live ones are zero.
+// Backward: dZ = g w p of the same tile, bf16, for the gradient products.  Columns past the vocabulary
+// and rows past the live ones are zero; the target's entry waits for k_head_target, which gets the sum of
+// the other columns' p.
 struct EpiDz {
   static constexpr bool kPacks = true;
   static constexpr bool kFits = false;
+  static constexpr bool kSums = true;
   const float* lse;
   const float* w;      // w_n dloss_n
   const int32_t* y;
@@ -247,9 +255,11 @@ struct EpiDz {
   int64_t row_first;   // this piece's first row among the live rows
   int64_t v_first;     // this piece's first vocabulary column
   int v_cols;          // its columns of the vocabulary
+  float* others;       // (2 column tiles) x pitch
+  int64_t pitch;       // rows of a piece
 
   struct Row {
-    float lse, g;
+    float lse, g, others;
     int at, end;  // the target's column and the columns that count (none in rows past the live ones)
   };
   __device__ __forceinline__ Row row_of(int row) const {
@@ -257,14 +267,19 @@ struct EpiDz {
     const bool live = row_first + row < *count;
     r.lse = lse[row];
     r.g = w[row];
+    r.others = 0.f;
     const int64_t at = int64_t(y[row]) - v_first;
     r.at = at >= 0 && at < v_cols ? int(at) : -1;
     r.end = live ? v_cols : 0;
     return r;
   }
-  __device__ __forceinline__ float value(const Row& r, int col, float z) const {
-    const float p = exp_diff(z, r.lse) - (col == r.at ? 1.f : 0.f);
+  __device__ __forceinline__ float value(Row& r, int col, float z) const {
+    const float p = col < r.end && col != r.at ? exp_diff(z, r.lse) : 0.f;
+    r.others += p;
     return col < r.end ? r.g * p : 0.f;
+  }
+  __device__ __forceinline__ void finish(const Row& r, int part, int row) const {
+    if (LOCA_CHECK(row, pitch)) others[int64_t(part) * pitch + row] = r.others;
   }
 };
 
@@ -303,6 +318,7 @@ struct EpiAcc {
 struct EpiScaled {
   static constexpr bool kPacks = true;
   static constexpr bool kFits = false;
+  static constexpr bool kSums = false;
   float scale;
 
   struct Row {};
@@ -361,6 +377,34 @@ __global__ void __launch_bounds__(1024)
     for (int c = 0; c < C; ++c)
       E[int64_t(n) * C + c] = w * (exp_diff(zc[int64_t(c) * pitch + row], l) - (cols[c] == y ? 1.f : 0.f));
   }
+}
+
+// The target's entry of dZ: p - 1 = -(sum of the others' p).  As a difference it would be no better than
+// lse's rounding to fp32: at lse = 40 and 1 - p = 1e-5 a fifth of it.  32 rows per block, `blockDim.y` groups of
+// partial sums.  add: the sum goes on from `sum`; keep: it goes there; put: it is complete.
+__global__ void __launch_bounds__(1024)
+    k_head_target(const float* __restrict__ part, int64_t pitch, int nparts, Rows in, int64_t row_first, float* sum,
+                  int add, int keep, int put, int64_t v_first, int64_t v_cols, __nv_bfloat16* dz, int64_t ldz) {
+  __shared__ float sh[32][33];
+  wait_for_previous();
+  launch_dependents();
+  const int64_t row = int64_t(blockIdx.x) * 32 + threadIdx.x;
+  const bool live = row_first + row < *in.count;
+  float s = 0.f;
+  if (live && LOCA_CHECK(row, pitch)) {
+#pragma unroll 8
+    for (int p = threadIdx.y; p < nparts; p += int(blockDim.y)) s += part[int64_t(p) * pitch + row];
+  }
+  sh[threadIdx.y][threadIdx.x] = s;
+  __syncthreads();
+  if (threadIdx.y != 0 || !live) return;
+  for (int j = 1; j < int(blockDim.y); ++j) s += sh[j][threadIdx.x];
+  if (add) s += sum[row];
+  if (keep) sum[row] = s;
+  if (!isfinite(in.lse[row_first + row])) s = NAN;  // (also where there is no other column to say so)
+  const int64_t at = int64_t(in.y[row_first + row]) - v_first;
+  if (put && at >= 0 && at < v_cols && LOCA_CHECK(at, ldz))
+    dz[row * ldz + at] = __float2bfloat16_rn(-in.w[row_first + row] * s);
 }
 
 // One thread per 8 elements of a row; the k ranges' sums are loaded four at a time and added in order.
@@ -462,14 +506,21 @@ struct BwdWs {
   int64_t piece;  // rows of dZ
   int64_t vc;     // vocabulary columns of dZ (a multiple of 256)
   int splits;     // k ranges of dH
-  size_t dz, part, total;
+  size_t dz, part, others, sum, total;
 };
+bool few_rows(int64_t N) { return N > 0 && N <= gp::HALF; }
+// Column tiles that cols vocabulary columns take at most (few rows: whole rounds of the CTAs, whatever the
+// tiles' width).
+int64_t dz_tiles(int64_t N, int64_t cols) {
+  const int64_t tiles = (cols + gp::TN - 1) / gp::TN;
+  return few_rows(N) ? round_up(tiles, sm_count()) : tiles;
+}
 // k ranges of the dH product: its tiles (rows / 256 x d / 512) are few, so one range per tile would
 // leave the last round of CTA pairs mostly idle.  More ranges fill it and cost 8 bytes per element and
 // range (written, then read by k_head_dh).  Both sides of the choice in cycles.
 int dh_splits(int64_t n, int64_t rows, int64_t d, int64_t vc) {
   const int64_t m = rows / gp::TM, nkb = vc / gp::BK;
-  const bool single = n > 0 && n <= gp::HALF;
+  const bool single = few_rows(n);
   const double range = double(single ? n : rows) * double(d) * 8.0 / 3000.0 + gp::kRangeCycles;
   int best = 1;
   double best_c = 0;
@@ -487,9 +538,14 @@ BwdWs bwd_ws(int64_t N, int64_t V, int64_t d, bool dh, bool dw) {
   BwdWs o{};
   o.rows = rows_ws(N, d);
   const int64_t np = round_up(N < 1 ? 1 : N, gp::TM);
-  o.piece = dw || np < kBwdRows ? np : kBwdRows;
   const int64_t vp = round_up(V, gp::TN);
-  int64_t vc = kDzBytes / (2 * o.piece) / gp::TN * gp::TN;
+  // dH alone: as many rows at a time as fit with the whole vocabulary.  dW sums over all rows, so there it
+  // is the vocabulary that is cut, if anything is
+  int64_t most = kDzBytes / (2 * vp) / gp::TM * gp::TM;
+  most = most < gp::TM ? gp::TM : most < kBwdRows ? most : kBwdRows;
+  const int64_t cuts = dw ? 1 : (np + most - 1) / most;
+  o.piece = round_up((np + cuts - 1) / cuts, gp::TM);
+  int64_t vc = (dw ? kDzBytesAll : kDzBytes) / (2 * o.piece) / gp::TN * gp::TN;
   if (vc < 4 * gp::TN) vc = 4 * gp::TN;
   if (vc > vp) vc = vp;
   const int64_t chunks = (vp + vc - 1) / vc;
@@ -498,6 +554,8 @@ BwdWs bwd_ws(int64_t N, int64_t V, int64_t d, bool dh, bool dw) {
   size_t at = o.rows.total;
   o.dz = at; at += align256(2 * size_t(o.piece) * size_t(o.vc));
   o.part = at; at += align256(4 * size_t(o.splits) * size_t(o.piece) * size_t(d));
+  o.others = at; at += align256(4 * 2 * size_t(dz_tiles(N, o.vc)) * size_t(o.piece));
+  o.sum = at; at += align256(4 * size_t(o.piece));
   o.total = at;
   return o;
 }
@@ -585,8 +643,10 @@ cudaError_t launch_head_loss_backward(const void* H, int64_t ldh, int64_t N, int
   if (e != cudaSuccess) return e;
   const int64_t np = round_up(N < 1 ? 1 : N, gp::TM);
   const __nv_bfloat16* Wb = static_cast<const __nv_bfloat16*>(W);
-  void* dz = ws + lay.dz;
+  __nv_bfloat16* dz = reinterpret_cast<__nv_bfloat16*>(ws + lay.dz);
   float* part = reinterpret_cast<float*>(ws + lay.part);
+  float* others = reinterpret_cast<float*>(ws + lay.others);
+  float* sum = reinterpret_cast<float*>(ws + lay.sum);
   for (int64_t p0 = 0; p0 < np; p0 += lay.piece) {
     const int64_t rows = np - p0 < lay.piece ? np - p0 : lay.piece;
     const int64_t kblocks = (lay.vc + gp::BK - 1) / gp::BK;  // of a whole piece of the vocabulary
@@ -602,11 +662,11 @@ cudaError_t launch_head_loss_backward(const void* H, int64_t ldh, int64_t N, int
       fit.tile_cycles = int(gp::tile_cycles(shape));
       fit.row_tile_cycles = int(gp::TM * d * 8 / 3000);
     }
-    for (int64_t v0 = 0; v0 < V; v0 += lay.vc) {
-      const int64_t vn = V - v0 < lay.vc ? V - v0 : lay.vc;   // columns of the vocabulary
-      const int64_t vtiles = (vn + gp::TN - 1) / gp::TN;
-      CUtensorMap mh, mw, mz_out, mz_k, mw_mn;
-      const bool single = N > 0 && N <= gp::HALF;
+    // dZ of the vocabulary columns v0 .. v0 + vn.  all: they are all there are, so the sum of the others' p that
+    // the target's entry takes is whole; done: earlier calls have made it; neither: this call adds to it
+    const bool single = few_rows(N);
+    auto make_dz = [&](int64_t v0, int64_t vn, bool all, bool done) {
+      CUtensorMap mh, mw, mz_out;
       // the forward pass's shape and segments, so that z comes out as it went into lse
       gp::Geo g = geo(rows / gp::TM, vn, (d + gp::BK - 1) / gp::BK, single ? kSegKbFew : kSegKb, r, status);
       g.rows_live = r.count;
@@ -617,10 +677,23 @@ cudaError_t launch_head_loss_backward(const void* H, int64_t ldh, int64_t N, int
           !gp::map_2d(&mw, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, Wb + v0 * d, d, vn, d, gp::BK, g.width / 2) ||
           !gp::map_out_bf16(&mz_out, dz, lay.vc, lay.piece, lay.vc))
         return cudaErrorInvalidValue;
-      const EpiDz dzed{r.lse + p0, r.w + p0, r.y + p0, r.count, p0, v0, int(vn)};
-      e = single ? gp::launch<gp::kSingle, false, false>(mh, mw, mh, mw, mz_out, g, dzed, gp::NoExt{}, s)
-                 : gp::launch<gp::kNarrow, false, false>(mh, mw, mh, mw, mz_out, g, dzed, gp::NoExt{}, s);
+      const EpiDz dzed{r.lse + p0, r.w + p0, r.y + p0, r.count, p0, v0, int(vn), others, lay.piece};
+      const cudaError_t e = single ? gp::launch<gp::kSingle, false, false>(mh, mw, mh, mw, mz_out, g, dzed, gp::NoExt{}, s)
+                                   : gp::launch<gp::kNarrow, false, false>(mh, mw, mh, mw, mz_out, g, dzed, gp::NoExt{}, s);
       if (e != cudaSuccess) return e;
+      const int nparts = done ? 0 : int(2 * ((vn + g.width - 1) / g.width));
+      return gp::launch_early(k_head_target, dim3(unsigned(rows / 32)), dim3(32, nparts >= 128 ? 32 : 8), 0, s, others,
+                              lay.piece, nparts, r, p0, sum, int(done || v0 > 0), int(!all && !done), int(all || done), v0,
+                              vn, dz, lay.vc);
+    };
+    const bool whole = V <= lay.vc;
+    for (int64_t v0 = 0; v0 < V && !whole; v0 += lay.vc)
+      if ((e = make_dz(v0, V - v0 < lay.vc ? V - v0 : lay.vc, false, false)) != cudaSuccess) return e;
+    for (int64_t v0 = 0; v0 < V; v0 += lay.vc) {
+      const int64_t vn = V - v0 < lay.vc ? V - v0 : lay.vc;   // columns of the vocabulary
+      const int64_t vtiles = (vn + gp::TN - 1) / gp::TN;
+      if ((e = make_dz(v0, vn, whole, !whole)) != cudaSuccess) return e;
+      CUtensorMap mz_k, mw_mn;
       if (dH) {
         CUtensorMap mo;
         if (!gp::map_kmajor(&mz_k, dz, lay.vc, lay.piece, lay.vc) || !gp::map_mnmajor(&mw_mn, Wb + v0 * d, d, vn, d) ||
@@ -628,7 +701,7 @@ cudaError_t launch_head_loss_backward(const void* H, int64_t ldh, int64_t N, int
           return cudaErrorInvalidValue;
         gp::Geo gh = geo(rows / gp::TM, d, (vn + gp::BK - 1) / gp::BK, kSegKbGrad, r, status);
         gh.rows_live = r.count;
-        gh.m_first = g.m_first;
+        gh.m_first = int(p0 / gp::TM);
         gh.splits = lay.splits;
         gh.rows = int(N);
         gh.fit = fit;
