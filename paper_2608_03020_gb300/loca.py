@@ -5,6 +5,10 @@ the tensors it is given (device, dtype, shape, contiguity), passes their device 
 the current torch stream, and raises :class:`LocaError` on a non-OK status.  All arithmetic
 of the hot path runs in the library's CUDA kernels; PyTorch only provides device memory and
 streams.  There is no CPU fallback: importing works without a GPU, calling needs one.
+
+Without ``stream`` a call goes to the current torch stream, else to that one; scratch memory that a call
+allocates itself belongs to the stream it goes to.  What the caller hands over follows torch's rules:
+work on another stream has to come after the work that made it, and its memory has to live until then.
 """
 
 from __future__ import annotations
@@ -192,14 +196,28 @@ def _code(dtype) -> int:
     raise TypeError(f"unsupported dtype {dtype}")
 
 
-def _workspace(nbytes: int, device, given=None):
+def _torch_stream(stream):
+    """``stream`` (any object with a ``cuda_stream`` handle) as torch's own type."""
+    return stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(stream.cuda_stream)
+
+
+def _empty(nbytes: int, device, stream=None):
+    """Device memory that belongs to the stream of the call that uses it (``None``: the current one):
+    what is allocated on the current stream after the call cannot get it while that call runs."""
+    if stream is None:
+        return torch.empty(nbytes, dtype=torch.uint8, device=device)
+    with torch.cuda.stream(_torch_stream(stream)):
+        return torch.empty(nbytes, dtype=torch.uint8, device=device)
+
+
+def _workspace(nbytes: int, device, given=None, stream=None):
     if nbytes == 0:
         return None
     if given is not None:
         if given.numel() * given.element_size() < nbytes:
             raise ValueError(f"workspace has {given.numel() * given.element_size()} bytes, need {nbytes}")
         return given
-    return torch.empty(nbytes, dtype=torch.uint8, device=device)
+    return _empty(nbytes, device, stream)
 
 
 def loca_version() -> int:
@@ -268,7 +286,7 @@ def loca_targets(E, P, Q, T, tsq=None, workspace=None, stream=None):
     if C2 != C or L2 != L or r2 != r or tuple(T.shape) != (L, N, d):
         raise ValueError("shape mismatch among E (N x C), P (L x C x r), Q (L x r x d), T (L x N x d)")
     nbytes = targets_workspace_size(N, L, d)
-    ws = _workspace(nbytes, E.device, workspace)
+    ws = _workspace(nbytes, E.device, workspace, stream)
     rc = lib().loca_targets(_ptr(E), N, C, _ptr(P), _ptr(Q), L, r, d, _ptr(T), _code(T.dtype), _ptr(tsq),
                             _ptr(ws), nbytes, _stream(stream))
     _check(rc, "loca_targets")
@@ -293,7 +311,7 @@ def loca_accumulate(X, T, tsq, eta, gram, cross, xsq_total, zero_first, workspac
     if tuple(T.shape) != (L, N, d) or tuple(gram.shape) != (L, d, d) or tuple(cross.shape) != (L, d, d):
         raise ValueError("shape mismatch among X, T (L x N x d) and gram, cross (L x d x d)")
     nbytes = accumulate_workspace_size(L, N, d, X.dtype)
-    ws = _workspace(nbytes, X.device, workspace)
+    ws = _workspace(nbytes, X.device, workspace, stream)
     rc = lib().loca_accumulate(_ptr(X), _ptr(T), _code(X.dtype), L, N, d, _ptr(tsq), float(eta), int(bool(zero_first)),
                                _ptr(gram), _ptr(cross), _ptr(xsq_total), _ptr(ws), nbytes, _stream(stream))
     _check(rc, "loca_accumulate")
@@ -369,7 +387,7 @@ def loca_accumulate_streamed(X_host, staging, T, tsq, eta, gram, cross, xsq_tota
     if staging.numel() < 2 * group * N * d:
         raise ValueError(f"staging has {staging.numel()} elements, need 2 x group x N x d = {2 * group * N * d}")
     nbytes = accumulate_workspace_size(L, N, d, X_host.dtype)
-    ws = _workspace(nbytes, T.device, workspace)
+    ws = _workspace(nbytes, T.device, workspace, stream)
     rc = lib().loca_accumulate_streamed(ctypes.c_void_p(X_host.data_ptr()), _ptr(staging), _ptr(T),
                                         _code(X_host.dtype), L, N, d, group, _ptr(tsq), float(eta),
                                         int(bool(zero_first)), _ptr(gram), _ptr(cross), _ptr(xsq_total),
@@ -392,7 +410,7 @@ def loca_alignment(E_probe, G_probe, P, Q, alpha, workspace=None, stream=None):
         raise ValueError("shape mismatch among E_probe, G_probe, P, Q, alpha")
     out = ctypes.c_size_t(0)
     _check(lib().loca_alignment_workspace_size(Np, m, d, L, r, ctypes.byref(out)), "loca_alignment_workspace_size")
-    ws = _workspace(out.value, G_probe.device, workspace)
+    ws = _workspace(out.value, G_probe.device, workspace, stream)
     rc = lib().loca_alignment(_ptr(E_probe), _ptr(G_probe), Np, m, d, L, _ptr(P), _ptr(Q), r, _ptr(alpha), _ptr(ws),
                               out.value, _stream(stream))
     _check(rc, "loca_alignment")
@@ -425,7 +443,7 @@ def loca_kspace_accumulate(X, A, E, P, Q, eta, G, SC, xsq_total, zero_first, alp
             or tuple(G.shape) != (L, k, k) or tuple(SC.shape) != (L, C, k) or P.shape[0] != L):
         raise ValueError("shape mismatch among X, A, E, P, Q, G, SC")
     nbytes = kspace_workspace_size(L, N, d, k, C, r)
-    ws = _workspace(nbytes, X.device, workspace)
+    ws = _workspace(nbytes, X.device, workspace, stream)
     rc = lib().loca_kspace_accumulate(_ptr(X), LOCA_BF16, L, N, d, _ptr(A), k, _ptr(E), C, _ptr(P), _ptr(Q), r,
                                       float(eta), int(bool(zero_first)), _ptr(G), _ptr(SC), _ptr(xsq_total),
                                       _ptr(alpha), _ptr(ws), nbytes, _stream(stream))
@@ -472,7 +490,7 @@ def loca_batch_step(X, tsq, eta, xsq_total, alpha, zero_first, workspace=None, s
     _dev(alpha, "alpha", torch.float32, 1)
     L, N, d = X.shape
     nbytes = batch_step_workspace_size(L)
-    ws = _workspace(nbytes, X.device, workspace)
+    ws = _workspace(nbytes, X.device, workspace, stream)
     rc = lib().loca_batch_step(_ptr(X), _code(X.dtype), L, N, d, _ptr(tsq), float(eta), int(bool(zero_first)),
                                _ptr(xsq_total), _ptr(alpha), _ptr(ws), nbytes, _stream(stream))
     _check(rc, "loca_batch_step")
@@ -495,7 +513,7 @@ def loca_gram_cross(X, T, alpha, gram, cross, zero_first, workspace=None, stream
     if tuple(T.shape) != (L, N, d) or tuple(gram.shape) != (L, d, d) or tuple(cross.shape) != (L, d, d):
         raise ValueError("shape mismatch among X, T (L x N x d) and gram, cross (L x d x d)")
     nbytes = gram_cross_workspace_size()
-    ws = _workspace(nbytes, X.device, workspace)
+    ws = _workspace(nbytes, X.device, workspace, stream)
     rc = lib().loca_gram_cross(_ptr(X), _ptr(T), _code(X.dtype), L, N, d, _ptr(alpha), int(bool(zero_first)),
                                _ptr(gram), _ptr(cross), _ptr(ws), nbytes, _stream(stream))
     _check(rc, "loca_gram_cross")
@@ -519,7 +537,7 @@ def loca_targets_sq(E, P, Q, tsq, workspace=None, stream=None):
     if C2 != C or L2 != L or r2 != r or tuple(tsq.shape) != (L,):
         raise ValueError("shape mismatch among E (N x C), P (L x C x r), Q (L x r x d), tsq (L)")
     nbytes = targets_sq_workspace_size(N, C)
-    ws = _workspace(nbytes, E.device, workspace)
+    ws = _workspace(nbytes, E.device, workspace, stream)
     rc = lib().loca_targets_sq(_ptr(E), N, C, _ptr(P), _ptr(Q), L, r, d, _ptr(tsq), _ptr(ws), nbytes, _stream(stream))
     _check(rc, "loca_targets_sq")
 
@@ -546,7 +564,7 @@ def loca_gram_cross_fused(X, E, P, Q, alpha, gram, cross, zero_first, workspace=
             or tuple(gram.shape) != (L, d, d) or tuple(cross.shape) != (L, d, d)):
         raise ValueError("shape mismatch among X, E, P, Q, gram, cross")
     nbytes = gram_cross_fused_workspace_size(L, N, r)
-    ws = _workspace(nbytes, X.device, workspace)
+    ws = _workspace(nbytes, X.device, workspace, stream)
     rc = lib().loca_gram_cross_fused(_ptr(X), LOCA_BF16, L, N, d, _ptr(E), C, _ptr(P), _ptr(Q), r, _ptr(alpha),
                                      int(bool(zero_first)), _ptr(gram), _ptr(cross), _ptr(ws), nbytes, _stream(stream))
     _check(rc, "loca_gram_cross_fused")
@@ -579,7 +597,7 @@ def loca_ridge_solve(gram, cross, A, lambda_rel, B, info, xsq_total=None, B_prev
         raise ValueError("B must be nl x L x d x k and info nl x L")
     lam_arr = (ctypes.c_float * max(nl, 1))(*lam)
     nbytes = ridge_solve_workspace_size(L, d, k)
-    ws = _workspace(nbytes, A.device, workspace)
+    ws = _workspace(nbytes, A.device, workspace, stream)
     if cross_scale is not None and tuple(cross_scale.shape) != (L,):
         raise ValueError("cross_scale must have L entries")
     rc = lib().loca_ridge_solve(_ptr(gram), _ptr(cross), _ptr(cross_scale), _ptr(xsq_total), _ptr(A), _ptr(B_prev),
@@ -621,7 +639,7 @@ def loca_calib_fit(E_probe, G_probe, beta, r, P, Q, sigma=None, workspace=None, 
     if Np2 != Np or tuple(P.shape) != (L, m, r) or tuple(Q.shape) != (L, r, d):
         raise ValueError("shape mismatch among E_probe, G_probe, P, Q")
     nbytes = calib_fit_workspace_size(Np, m, d, L, r)
-    ws = _workspace(nbytes, E_probe.device, workspace)
+    ws = _workspace(nbytes, E_probe.device, workspace, stream)
     rc = lib().loca_calib_fit(_ptr(E_probe), _ptr(G_probe), Np, m, d, L, float(beta), r, _ptr(P), _ptr(Q),
                               _ptr(sigma), _ptr(ws), nbytes, _stream(stream))
     _check(rc, "loca_calib_fit")
@@ -650,7 +668,7 @@ def loca_calib_fit_rsvd(E_probe, G_probe, beta, r, Omega, q, P, Q, sigma=None, w
             or (sigma is not None and tuple(sigma.shape) != (L, r))):
         raise ValueError("shape mismatch among E_probe, G_probe, Omega, P, Q, sigma")
     nbytes = calib_fit_rsvd_workspace_size(Np, m, d, L, r, ell)
-    ws = _workspace(nbytes, E_probe.device, workspace)
+    ws = _workspace(nbytes, E_probe.device, workspace, stream)
     rc = lib().loca_calib_fit_rsvd(_ptr(E_probe), _ptr(G_probe), Np, m, d, L, float(beta), r, ell, int(q),
                                    _ptr(Omega), _ptr(P), _ptr(Q), _ptr(sigma), _ptr(ws), nbytes, _stream(stream))
     _check(rc, "loca_calib_fit_rsvd")
@@ -703,7 +721,7 @@ def loca_head_loss(H, W, y, loss, lse=None, w=None, label_cols=None, E=None, wor
     if E is not None and tuple(E.shape) != (N, C):
         raise ValueError("E must be N x C for the C entries of label_cols")
     nbytes = head_loss_workspace_size(N, V, d, C)
-    ws = _workspace(nbytes, H.device, workspace)
+    ws = _workspace(nbytes, H.device, workspace, stream)
     rc = lib().loca_head_loss(_ptr(H), ldh, N, d, _ptr(W), V, _ptr(y), _ptr(w), _ptr(label_cols), C, _ptr(loss),
                               _ptr(lse), _ptr(E), _ptr(ws), nbytes, _stream(stream))
     _check(rc, "loca_head_loss")
@@ -736,7 +754,7 @@ def loca_head_loss_backward(H, W, y, lse, dH=None, dW=None, w=None, dloss=None, 
             or (dloss is not None and dloss.numel() != N) or (dW is not None and tuple(dW.shape) != (V, d))):
         raise ValueError("W and dW must be V x d; y, lse, w and dloss must have N entries")
     nbytes = head_loss_backward_workspace_size(N, V, d, dH is not None, dW is not None)
-    ws = _workspace(nbytes, H.device, workspace)
+    ws = _workspace(nbytes, H.device, workspace, stream)
     rc = lib().loca_head_loss_backward(_ptr(H), ldh, N, d, _ptr(W), V, _ptr(y), _ptr(w), _ptr(lse), _ptr(dloss),
                                        float(grad_scale), _ptr(dH), lddh, _ptr(dW), _ptr(ws), nbytes, _stream(stream))
     _check(rc, "loca_head_loss_backward")
@@ -752,6 +770,8 @@ class AdapterSet:
         _check(lib().loca_adapter_packed_size(n, d_in, d_out, k, ctypes.byref(out)), "loca_adapter_packed_size")
         self.n, self.d_in, self.d_out, self.k = int(n), int(d_in), int(d_out), int(k)
         self.packed = torch.zeros(out.value, dtype=torch.uint8, device=device)
+        if not torch.cuda.is_current_stream_capturing():
+            torch.cuda.current_stream().synchronize()  # the zeros come before a pack on any stream
 
     def pack(self, A, B, scale=None, stream=None):
         _dev(A, "A", (torch.float32, torch.bfloat16), 3)
@@ -776,7 +796,7 @@ class AdapterPlan:
         self.N, self.n = ids.numel(), int(n)
         out = ctypes.c_size_t(0)
         _check(lib().loca_adapter_plan_size(self.N, self.n, ctypes.byref(out)), "loca_adapter_plan_size")
-        self.buf = torch.empty(max(out.value, 256), dtype=torch.uint8, device=ids.device)
+        self.buf = _empty(max(out.value, 256), ids.device, stream)
         self.update(ids, stream=stream)
 
     def update(self, ids, stream=None):
@@ -796,7 +816,7 @@ def adapter_workspace_size(N, d_in, d_out, k, n, backward=False) -> int:
     return out.value
 
 
-def _adapter_args(X, W, adapters, plan):
+def _adapter_args(X, W, adapters, plan, stream):
     ldx = _rows2d(X, "X", torch.bfloat16)
     _dev(W, "W", torch.bfloat16, 2)
     N, d_in = X.shape
@@ -805,6 +825,9 @@ def _adapter_args(X, W, adapters, plan):
                          f"W {tuple(W.shape)}")
     if plan.N != N or plan.n != adapters.n:
         raise ValueError(f"the plan is for {plan.N} tokens and {plan.n} adapters, got {N} and {adapters.n}")
+    if stream is not None:  # their memory outlives them until this call is done
+        for t in (adapters.packed, plan.buf):
+            t.record_stream(_torch_stream(stream))
     return ldx, N, d_in
 
 
@@ -812,10 +835,10 @@ def loca_adapter_apply(X, W, adapters, plan, Y, workspace=None, stream=None):
     """``Y = X W^T + s_a (X A_a) B_a^T`` for tokens with an adapter each (or none): ``X`` N x d_in and
     ``Y`` N x d_out bf16 (rows may be spaced), ``W`` d_out x d_in bf16, ``adapters`` an
     :class:`AdapterSet`, ``plan`` an :class:`AdapterPlan` of the tokens' adapters."""
-    ldx, N, d_in = _adapter_args(X, W, adapters, plan)
+    ldx, N, d_in = _adapter_args(X, W, adapters, plan, stream)
     ldy = _rows2d(Y, "Y", torch.bfloat16, (N, adapters.d_out))
     nbytes = adapter_workspace_size(N, d_in, adapters.d_out, adapters.k, adapters.n)
-    ws = _workspace(nbytes, X.device, workspace)
+    ws = _workspace(nbytes, X.device, workspace, stream)
     rc = lib().loca_adapter_apply(_ptr(X), ldx, N, d_in, _ptr(W), adapters.d_out, _ptr(adapters.packed), adapters.n,
                                   adapters.k, _ptr(plan.buf), _ptr(Y), ldy, _ptr(ws), nbytes, _stream(stream))
     _check(rc, "loca_adapter_apply")
@@ -825,7 +848,7 @@ def loca_adapter_backward(X, dY, W, adapters, plan, dX=None, dA=None, dB=None, w
     """Gradients of :func:`loca_adapter_apply` for the frozen projection's input (``dX``, N x d_in
     bf16) and the adapters (``dA`` n x d_in x k, ``dB`` n x d_out x k, float32 or bfloat16); the
     adapters as last packed."""
-    ldx, N, d_in = _adapter_args(X, W, adapters, plan)
+    ldx, N, d_in = _adapter_args(X, W, adapters, plan, stream)
     lddy = _rows2d(dY, "dY", torch.bfloat16, (N, adapters.d_out))
     lddx = 0 if dX is None else _rows2d(dX, "dX", torch.bfloat16, (N, d_in))
     both = (torch.float32, torch.bfloat16)
@@ -836,7 +859,7 @@ def loca_adapter_backward(X, dY, W, adapters, plan, dX=None, dA=None, dB=None, w
         raise ValueError("dA must be n x d_in x k and dB n x d_out x k")
     kind = torch.float32 if dA is None and dB is None else (dB if dA is None else dA).dtype
     nbytes = adapter_workspace_size(N, d_in, adapters.d_out, adapters.k, adapters.n, backward=True)
-    ws = _workspace(nbytes, X.device, workspace)
+    ws = _workspace(nbytes, X.device, workspace, stream)
     rc = lib().loca_adapter_backward(_ptr(X), ldx, _ptr(dY), lddy, N, d_in, _ptr(W), adapters.d_out,
                                      _ptr(adapters.packed), adapters.n, adapters.k, _ptr(plan.buf), _ptr(dX), lddx,
                                      _ptr(dA), _ptr(dB), _code(kind), _ptr(ws), nbytes, _stream(stream))
@@ -871,7 +894,8 @@ class GradClip:
         size = ctypes.c_size_t(0)
         _check(lib().loca_grad_clip_workspace_size(n, ctypes.byref(size)), "loca_grad_clip_workspace_size")
         self._bytes = size.value
-        self._ws = torch.empty(size.value, dtype=torch.uint8, device=self.grads[0].device if n else "cuda")
+        # scratch memory for each stream, so that steps on two streams do not share their sums
+        self._ws = {_stream(None).value: _empty(self._bytes, self.grads[0].device if n else "cuda")}
 
     def run(self, max_norm, norm, stream=None):
         """Writes the global norm before clipping to ``norm`` (one float, device) and the gradients
@@ -879,8 +903,12 @@ class GradClip:
         _dev(norm, "norm", torch.float32)
         if norm is None or norm.numel() != 1:
             raise ValueError("norm must be a CUDA tensor of one element")
+        on = _stream(stream)
+        ws = self._ws.get(on.value)
+        if ws is None:
+            ws = self._ws[on.value] = _empty(self._bytes, norm.device, stream)
         rc = lib().loca_grad_clip(self._in, self._out, self._numel, self._dtype, len(self.grads), float(max_norm),
-                                  _ptr(norm), _ptr(self._ws), self._bytes, _stream(stream))
+                                  _ptr(norm), _ptr(ws), self._bytes, on)
         _check(rc, "loca_grad_clip")
 
 
