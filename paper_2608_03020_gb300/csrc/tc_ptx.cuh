@@ -50,6 +50,13 @@ struct WaitCtl {
   volatile int32_t* abort_flag;  // launch-local: set to `mark` by the first waiter that gives up
   uint64_t limit_ns;
   int32_t mark = 1;              // a launch with a mark of its own needs no cleared flag
+
+  // The flag alone may be left from an earlier replay of the same captured launch, whose mark is fixed; the
+  // status word says whether that has been reported.  So no wait ends early in a launch whose caller finds
+  // no error.
+  __device__ __forceinline__ bool others_gave_up() const {
+    return *abort_flag == mark && *reinterpret_cast<volatile int32_t*>(status) == int32_t(LOCA_ERR_TIMEOUT);
+  }
 };
 
 // Bounded wait for the phase of parity `parity` of barrier `bar`.  Returns false when the wait
@@ -69,7 +76,7 @@ static __device__ __noinline__ bool mbar_wait(uint32_t bar, uint32_t parity, con
         __threadfence();
         return false;
       }
-      if ((it & 127u) == 0 && *w.abort_flag == w.mark) return false;
+      if ((it & 127u) == 0 && w.others_gave_up()) return false;
     }
   }
 }
@@ -141,7 +148,7 @@ static __device__ __noinline__ bool mbar_wait_cluster(uint32_t bar, uint32_t par
         __threadfence();
         return false;
       }
-      if ((it & 127u) == 0 && *w.abort_flag == w.mark) return false;
+      if ((it & 127u) == 0 && w.others_gave_up()) return false;
     }
   }
 }
