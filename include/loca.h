@@ -510,8 +510,9 @@ int loca_head_loss(const void* H, int64_t ldh, int64_t N, int64_t d, const void*
  *
  * lse    N float, from loca_head_loss on the same H, W, y
  * dloss  N float gradient of each position's loss, or NULL for ones
- * dH     N x d bf16 output, row pitch lddh (a multiple of 8), or NULL; rows of masked positions are
- *        0.  With unit weights it is the d-wide top error that loca_calib_fit_rsvd takes (in fp32)
+ * dH     N x d bf16 output, row pitch lddh (a multiple of 8), or NULL; it may be H itself, but not
+ *        overlap it otherwise.  Rows of masked positions are 0.  With unit weights it is the d-wide
+ *        top error that loca_calib_fit_rsvd takes (in fp32)
  * dW     V x d bf16 output, or NULL; at least one of dH and dW
  * The logits are computed again, summed as those of loca_head_loss, and the target's entry of dZ is
  * minus the sum of the others: positions of a probability near 1 keep their small gradient.  dZ is
@@ -550,7 +551,8 @@ int loca_head_loss_backward(const void* H, int64_t ldh, int64_t N, int64_t d, co
  *                    and dB in LOCA_F32 and to 2^-17 in LOCA_BF16.  An adapter without a token gets zeros.  A token outside an adapter
  *                    reaches its gradients in no way, whatever its row holds
  * loca_adapter_workspace_size  scratch of one apply (backward 0) or of apply and backward (1)
- * All are deterministic.  X, dY, Y, dX, W 16-byte aligned, row pitches multiples of 8.
+ * All are deterministic.  X, dY, Y, dX, W 16-byte aligned, row pitches multiples of 8.  Y may not
+ * overlap X, nor dX dY, nor dX X where dA or dB is wanted (rows side by side in one buffer do not overlap).
  */
 int loca_adapter_packed_size(int32_t n, int64_t d_in, int64_t d_out, int32_t k, size_t* bytes);
 int loca_adapter_pack(const void* A, const void* B, int dtype, int32_t n, int64_t d_in, int64_t d_out, int32_t k,

@@ -52,6 +52,31 @@ int check_rows(const void* p, int64_t pitch, int64_t cols, const char* name) {
   return LOCA_OK;
 }
 
+// Whether rows of `wide` bytes, `pitch` bytes apart, share a byte with the rows of another such matrix
+// (columns of one buffer side by side do not).
+struct Block {
+  const void* p;
+  int64_t pitch, wide;
+};
+bool overlap(const Block& x, const Block& y, int64_t rows) {
+  const int64_t a = reinterpret_cast<int64_t>(x.p), b = reinterpret_cast<int64_t>(y.p);
+  if (!x.p || !y.p || a + (rows - 1) * x.pitch + x.wide <= b || b + (rows - 1) * y.pitch + y.wide <= a) return false;
+  if (x.pitch == y.pitch) {  // row i of y begins `at` bytes behind the begin of row i + q of x
+    int64_t q = (b - a) / x.pitch, at = (b - a) % x.pitch;
+    if (at < 0) {
+      --q;
+      at += x.pitch;
+    }
+    return (at < x.wide && q > -rows && q < rows) || (at + y.wide > x.pitch && q + 1 > -rows && q + 1 < rows);
+  }
+  for (int64_t i = 0; i < rows; ++i) {
+    const int64_t begin = a + i * x.pitch, end = begin + x.wide;
+    int64_t j = begin - y.wide - b < 0 ? 0 : (begin - y.wide - b) / y.pitch + 1;  // first row that ends behind begin
+    if (j < rows && b + j * y.pitch < end) return true;
+  }
+  return false;
+}
+
 }  // namespace
 
 extern "C" {
@@ -121,6 +146,8 @@ int loca_head_loss_backward(const void* H, int64_t ldh, int64_t N, int64_t d, co
   if (!std::isfinite(grad_scale)) return fail(LOCA_ERR_INVALID_ARG, "grad_scale must be finite");
   rc = check_ws(workspace, workspace_bytes, head_loss_backward_workspace_bytes(N, V, d, dH != nullptr, dW != nullptr));
   if (rc != LOCA_OK) return rc;
+  if (N > 0 && (dH != H || lddh != ldh) && overlap({H, 2 * ldh, 2 * d}, {dH, 2 * lddh, 2 * d}, N))
+    return fail(LOCA_ERR_INVALID_ARG, "dH must be H itself or not overlap it");
   int32_t* status = device_status_word();
   if (!status) return fail(LOCA_ERR_CUDA, "cannot resolve the device status word");
   const cudaError_t e = launch_head_loss_backward(H, ldh, N, d, W, V, y, w, lse, dloss, grad_scale, N > 0 ? dH : nullptr,
@@ -201,6 +228,8 @@ int loca_adapter_apply(const void* X, int64_t ldx, int64_t N, int64_t d_in, cons
     return fail(LOCA_ERR_ALIGNMENT, "packed and plan need 256-byte alignment");
   rc = check_ws(workspace, workspace_bytes, adapter_workspace_bytes(N, d_in, d_out, k, n, false));
   if (rc != LOCA_OK) return rc;
+  if (overlap({X, 2 * ldx, 2 * d_in}, {Y, 2 * ldy, 2 * d_out}, N))
+    return fail(LOCA_ERR_INVALID_ARG, "Y must not overlap X");
   int32_t* status = device_status_word();
   if (!status) return fail(LOCA_ERR_CUDA, "cannot resolve the device status word");
   const cudaError_t e = launch_adapter_apply(X, ldx, N, d_in, W, d_out, packed, n, k, plan, Y, ldy, workspace, status,
@@ -236,6 +265,9 @@ int loca_adapter_backward(const void* X, int64_t ldx, const void* dY, int64_t ld
     return fail(LOCA_ERR_ALIGNMENT, "packed and plan need 256-byte alignment");
   rc = check_ws(workspace, workspace_bytes, adapter_workspace_bytes(N, d_in, d_out, k, n, true));
   if (rc != LOCA_OK) return rc;
+  if (dX && (overlap({dY, 2 * lddy, 2 * d_out}, {dX, 2 * lddx, 2 * d_in}, N) ||
+             ((dA || dB) && overlap({X, 2 * ldx, 2 * d_in}, {dX, 2 * lddx, 2 * d_in}, N))))
+    return fail(LOCA_ERR_INVALID_ARG, "dX must not overlap dY, nor X where dA or dB is wanted");
   int32_t* status = device_status_word();
   if (!status) return fail(LOCA_ERR_CUDA, "cannot resolve the device status word");
   const cudaError_t e = launch_adapter_backward(X, ldx, dY, lddy, N, d_in, W, d_out, packed, n, k, plan, dX, lddx, dA, dB,
