@@ -692,11 +692,20 @@ def _rows2d(t, name, dtype, shape=None):
     return pitch
 
 
-@functools.lru_cache(maxsize=1024)  # a size depends on the arguments alone
-def head_loss_workspace_size(N, V, d, C=0) -> int:
+@functools.lru_cache(maxsize=1024)
+def _size_on(device, name, *args) -> int:
     out = ctypes.c_size_t(0)
-    _check(lib().loca_head_loss_workspace_size(N, V, d, C, ctypes.byref(out)), "loca_head_loss_workspace_size")
+    _check(getattr(lib(), name)(*args, ctypes.byref(out)), name)
     return out.value
+
+
+def _size(name, *args) -> int:
+    """A workspace size, asked for once: it depends on the arguments and on the current device."""
+    return _size_on(torch.cuda.current_device() if torch.cuda.is_initialized() else None, name, *args)
+
+
+def head_loss_workspace_size(N, V, d, C=0) -> int:
+    return _size("loca_head_loss_workspace_size", N, V, d, C)
 
 
 def loca_head_loss(H, W, y, loss, lse=None, w=None, label_cols=None, E=None, workspace=None, stream=None):
@@ -727,12 +736,8 @@ def loca_head_loss(H, W, y, loss, lse=None, w=None, label_cols=None, E=None, wor
     _check(rc, "loca_head_loss")
 
 
-@functools.lru_cache(maxsize=1024)  # a size depends on the arguments alone
 def head_loss_backward_workspace_size(N, V, d, want_dH=True, want_dW=True) -> int:
-    out = ctypes.c_size_t(0)
-    _check(lib().loca_head_loss_backward_workspace_size(N, V, d, int(bool(want_dH)), int(bool(want_dW)),
-                                                        ctypes.byref(out)), "loca_head_loss_backward_workspace_size")
-    return out.value
+    return _size("loca_head_loss_backward_workspace_size", N, V, d, int(bool(want_dH)), int(bool(want_dW)))
 
 
 def loca_head_loss_backward(H, W, y, lse, dH=None, dW=None, w=None, dloss=None, grad_scale=1.0, workspace=None,
@@ -808,12 +813,8 @@ class AdapterPlan:
         return self
 
 
-@functools.lru_cache(maxsize=1024)  # a size depends on the arguments alone
 def adapter_workspace_size(N, d_in, d_out, k, n, backward=False) -> int:
-    out = ctypes.c_size_t(0)
-    _check(lib().loca_adapter_workspace_size(N, d_in, d_out, k, n, int(bool(backward)), ctypes.byref(out)),
-           "loca_adapter_workspace_size")
-    return out.value
+    return _size("loca_adapter_workspace_size", N, d_in, d_out, k, n, int(bool(backward)))
 
 
 def _adapter_args(X, W, adapters, plan, stream):
