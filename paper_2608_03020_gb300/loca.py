@@ -214,6 +214,8 @@ def _workspace(nbytes: int, device, given=None, stream=None):
     if nbytes == 0:
         return None
     if given is not None:
+        if not isinstance(given, torch.Tensor) or not given.is_cuda or not given.is_contiguous():
+            raise TypeError("workspace must be a contiguous CUDA tensor")
         if given.numel() * given.element_size() < nbytes:
             raise ValueError(f"workspace has {given.numel() * given.element_size()} bytes, need {nbytes}")
         return given

@@ -1,5 +1,7 @@
-"""Workspace sizes that the binding keeps hold for the device they were asked for."""
+"""Workspaces: sizes that the binding keeps hold for the device they were asked for, and what is handed
+over as one is device memory in one piece."""
 
+import pytest
 import torch
 
 
@@ -29,3 +31,12 @@ def test_sizes_are_kept_for_each_device(monkeypatch):
             assert call() == 1000 * (device[0] + 1) + 123457
         assert len(asked) == 2 and asked[0][1] == asked[1][1]
     loca._size_on.cache_clear()  # (what this stand-in said)
+
+
+def test_a_workspace_in_host_memory_is_refused():
+    from paper_2608_03020_gb300 import loca
+
+    with pytest.raises(TypeError):
+        loca._workspace(64, "cuda", torch.empty(64, dtype=torch.uint8))
+    with pytest.raises(TypeError):
+        loca._workspace(64, "cuda", bytearray(64))
