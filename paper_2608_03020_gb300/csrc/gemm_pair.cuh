@@ -98,7 +98,7 @@ __device__ __forceinline__ int fit_splits(const Fit& f, int planned, int m_plann
     if (s < planned) s = planned;
     const int rounds = (tiles * s + f.at_once - 1) / f.at_once;
     const int64_t c = int64_t(rounds) * (f.kb_cycles * ((f.nkb + s - 1) / s) + f.tile_cycles) +
-                      int64_t(s) * (m * f.row_tile_cycles + kRangeCycles);
+                      int64_t(s) * (int64_t(m) * f.row_tile_cycles + kRangeCycles);
     if (r == 0 || c + c / 32 < best_c) {  // (3 % is as near as the costs are known)
       best = s;
       best_c = c;
@@ -122,7 +122,6 @@ __device__ __forceinline__ int live_tiles(int rows, int m_first, int m_tiles) {
 struct Geo {
   int m_tiles, n_tiles;  // upper bounds (rows_live may lower m_tiles, k_live the k-blocks); set by launch()
   int cols;              // columns of the output
-  int rows;              // rows of A (host: 128 or fewer take the single shape)
   int width;             // columns of a tile (launch() sets all but the single shape's)
   int arows, stages;     // single shape, B K-major: rows of A's boxes, stages of the ring (launch())
   int nkb;               // k-blocks of the product
@@ -778,11 +777,11 @@ inline cudaError_t launch_shape(int shape, const CUtensorMap& a, const CUtensorM
                         : launch<kNarrow, kAmn, kBmn, Epi, Ext>(a, b, ax, bx, o, g, epi, ext, s);
 }
 
-// In the shape that pick_shape() names.
+// In the pair shape that pick_shape() names.
 template <bool kAmn, bool kBmn, class Epi, class Ext>
 inline cudaError_t launch_either(const CUtensorMap& a, const CUtensorMap& b, const CUtensorMap& ax, const CUtensorMap& bx,
                                  const CUtensorMap& o, const Geo& g, const Epi& epi, const Ext& ext, cudaStream_t s) {
-  return launch_shape<kAmn, kBmn>(pick_shape(g.rows, g.m_tiles, g.cols, g.nkb, g.splits), a, b, ax, bx, o, g, epi, ext, s);
+  return launch_shape<kAmn, kBmn>(pick_shape(0, g.m_tiles, g.cols, g.nkb, g.splits), a, b, ax, bx, o, g, epi, ext, s);
 }
 
 }  // namespace gp

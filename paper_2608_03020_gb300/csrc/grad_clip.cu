@@ -28,7 +28,7 @@ constexpr int kThreads = 256;
 constexpr int kChunk = 8192;
 constexpr int kSumBlocks = 4, kScaleBlocks = 6;  // resident blocks per SM
 constexpr int kFew = 64;     // tensors of one launch: a small list keeps the launch short
-constexpr int kMany = 1000;  // 24 KB of parameters
+constexpr int kMany = 1000;  // 28 KB of parameters
 
 template <int kCap>
 struct List {
@@ -39,6 +39,8 @@ struct List {
   int32_t n;
   int32_t chunks;
 };
+
+static_assert(sizeof(List<kMany>) + 64 <= 32764, "a launch's parameters");
 
 struct Chunk {
   int t;

@@ -703,7 +703,6 @@ cudaError_t launch_head_loss_backward(const void* H, int64_t ldh, int64_t N, int
         gh.rows_live = r.count;
         gh.m_first = int(p0 / gp::TM);
         gh.splits = lay.splits;
-        gh.rows = int(N);
         gh.fit = fit;
         e = gp::launch_shape<false, true>(shape, mz_k, mw_mn, mz_k, mw_mn, mo, gh, EpiAcc{v0 > 0 ? 1 : 0}, gp::NoExt{}, s);
         if (e != cudaSuccess) return e;
