@@ -52,6 +52,8 @@ constexpr size_t kSlotElems = size_t(kSlotRows) * kMaxK;
 __host__ __device__ inline int k_padded(int k) { return (k + 15) / 16 * 16; }
 
 // ------------------------------------------------------------------ plan
+// Five launches of some 5 us that wait for one another: 21 us a step, on the GPU, from one token to 16384 and
+// up to 500 adapters.  k_plan_adapters reads every slot for each adapter (2 n slots x 4 bytes from L2).
 // Offsets in int32 from the start of the plan.
 struct PlanLay {
   int64_t tiles, pairs, smax;
@@ -1096,8 +1098,8 @@ struct EpiRows {
 // raises r or a, so no two share a number).  The segments (512 tokens) are added in registers.  A slot
 // whose tile also holds other tokens has those rows of X (or dY) zeroed in shared memory first: their U
 // is zero, but a product with whatever else stands there (infinities, NaN) need not be.  Measured, X and
-// dY from HBM: 16384 tokens x 2 x 896 channels 17.4 us (3.4 TB/s; launch and join of the ranges aside),
-// 8191 tokens x 2 x 3584 channels 31 us (3.8 TB/s): the ring of 18 KB boxes is short of HBM's latency.
+// dY from HBM: 16384 tokens x 2 x 896 channels 18 us, 8192 x 2 x 3584 31 us; twice the tokens take 11 and 17
+// us more (5.8 and 7.0 TB/s), so 8 to 13 us of a launch are its beginning and end.
 constexpr int kGradThreads = 224;
 constexpr int kGradMaxStages = 8;
 constexpr int kGradSeg = 8;

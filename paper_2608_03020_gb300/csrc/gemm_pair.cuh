@@ -76,7 +76,7 @@ static_assert(Shape<kNarrow>::kBars * 8 + 8 <= 256 && Shape<kSingle>::kBars * 8 
 
 // What the device chooses the number of k ranges by where fewer rows are live than the host planned for:
 // the sums' room in row tiles, and the costs of cycles() with those of writing and adding a range's sums.
-// 819 live rows of 8192 at d = 896, V = 32000: loss and dH 256 us with the host's ranges, 156 so.
+// 819 live rows of 8192 at d = 896, V = 32000: loss and dH 256 us with the host's ranges, 154 so.
 // Integers throughout: the product and the kernel that adds its ranges come to the same number.
 constexpr int kRangeCycles = 250;  // k_head_dh fetches four ranges at a time
 struct Fit {
@@ -720,7 +720,8 @@ inline cudaError_t launch_early(void (*kernel)(P...), dim3 grid, dim3 block, siz
 // Which shape: rounds of the pairs times a tile's cycles.  Measured on 1024 x 19456 outputs (4 narrow, 2
 // wide rounds) at k = 512 .. 8192: narrow 672 cycles a k-block and 3000 a tile, wide 1030 and 9000 (both
 // with a share of the launch and of the last tiles' stores); at k = 8192 204 and 170 us (1.60 and 1.92
-// PFLOP/s), at k = 512 25 us each.
+// PFLOP/s), at k = 512 25 us each.  (The k-blocks of an extended k axis are not counted: the device alone
+// knows them.)
 inline double kb_cycles(int shape) { return shape == kWide ? 1030.0 : 672.0; }
 inline double tile_cycles(int shape) { return shape == kWide ? 9000.0 : 3000.0; }
 inline double cycles(int shape, int64_t m_tiles, int64_t cols, int64_t nkb, int splits) {

@@ -13,11 +13,11 @@
 //                Backward: the same tiles again, summed in the same segments (p = exp(z - lse) is only
 //                as good as z and lse agree: with one accumulator over d = 5120 the gradient of a
 //                position with 1 - p = 1e-5 came out 50 times too large), turned into
-//                dZ = g w (p - onehot), rounded to bf16
-//                as the operand of the two gradient products, for one piece of the vocabulary at a
-//                time (a bf16 operand moves a sum of many such products by less than the gradients'
-//                own rounding to bf16; the factor `scale` is applied to the fp32 sums, so it
-//                rounds nothing)
+//                dZ = g w (p - onehot), rounded to bf16 as the operand of the two gradient products, for
+//                one piece of the rows or of the vocabulary at a time.  That rounding moves the gradients
+//                about as much as their own (0.0024 from the 64-bit value in norm, 0.0017 without it); a
+//                second part would cost both products again.  `scale` is applied to the fp32 sums, so it
+//                rounds nothing
 // k_head_target  the target's p - 1 as minus the sum of the others' p.  Where a dW over many rows cuts the
 //                vocabulary into pieces (N V > 2^31) the sum over all of them comes first, from a pass
 //                over the logits of its own
@@ -28,8 +28,8 @@
 // Bound: the tensor cores from a few hundred tokens on, the read of W below.  8192 live of 16384 tokens at
 // d = 2048, V = 49152: 1.06 ms (1.55 PFLOP/s; the rest is the epilogue's exponentials and the clock under
 // load); 37 tokens 48 us (201 MB of W: 4.2 TB/s for the call, 4.8 in k_gemm_pair).  Loss and dH of 1531
-// tokens at d = 5120, V = 151936: 4.4 ms for 7.15 TFLOP (1.62 PFLOP/s).  Up to 128 tokens each gradient
-// reads W again (8 tokens at d = 4648, V = 70557: 353 us for three reads of 656 MB).
+// tokens at d = 5120, V = 151936: 4.5 ms for 7.15 TFLOP (1.59 PFLOP/s).  Up to 128 tokens each gradient
+// reads W again (8 tokens at d = 4648, V = 70557: 370 us for three reads of 656 MB).
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
