@@ -508,7 +508,7 @@ int loca_head_loss(const void* H, int64_t ldh, int64_t N, int64_t d, const void*
  *   dZ[n, v] = dloss_n w_n (exp(z[n, v] - lse_n) - [v == y_n])
  *   dH = grad_scale dZ W  (N x d),   dW = grad_scale dZ^T H  (V x d)
  *
- * lse    N float, from loca_head_loss on the same H, W, y
+ * lse    N float, from loca_head_loss on the same H, W, y: the normaliser over all V columns
  * dloss  N float gradient of each position's loss, or NULL for ones
  * dH     N x d bf16 output, row pitch lddh (a multiple of 8), or NULL; it may be H itself, but not
  *        overlap it otherwise.  Rows of masked positions are 0.  With unit weights it is the d-wide
