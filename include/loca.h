@@ -570,6 +570,32 @@ int loca_adapter_backward(const void* X, int64_t ldx, const void* dY, int64_t ld
                           size_t workspace_bytes, void* stream);
 
 /*
+ * loca_gated — gated feed-forward of a block, both projections, the activation and the product in one launch;
+ * loca_gated_backward — its gradients:
+ *
+ *   G = X Wg^T,  U = X Wu^T,  H = act(G) U
+ *   dG = dH U act'(G),  dU = dH act(G),  dX = dG Wg + dU Wu,  dWg = dG^T X,  dWu = dU^T X
+ *
+ * X, dX   N x d bf16, H, dH N x f bf16, all with row pitches
+ * Wg, Wu  f x d bf16, contiguous;  dWg, dWu the same
+ * act     LOCA_ACT_SILU: g / (1 + e^-g);  LOCA_ACT_GELU: the tanh form, 0.5 g (1 + tanh(sqrt(2/pi) (g + 0.044715 g^3)))
+ * dX, dWg, dWu may each be NULL, not all.  N <= 2^24; d and f multiples of 8, 8 .. 65536.
+ * The backward call keeps nothing of the forward call: it computes G and U again (fp32; one rounding of dG and dU
+ * to bf16 as operands), in pieces of the rows (dX alone: up to 1 GiB of scratch) or of f (up to 4 GiB,
+ * more over more than 2^22 rows).  Sums are fp32, each output is rounded once.  Deterministic.  Pointers 16-byte
+ * aligned, row pitches multiples of 8.  No output may overlap an input or another output (rows side by side in
+ * one buffer do not).
+ */
+enum { LOCA_ACT_SILU = 0, LOCA_ACT_GELU = 1 };
+int loca_gated_workspace_size(int64_t N, int64_t d, int64_t f, size_t* bytes);
+int loca_gated(const void* X, int64_t ldx, int64_t N, int64_t d, const void* Wg, const void* Wu, int64_t f, int act,
+               void* H, int64_t ldh, void* workspace, size_t workspace_bytes, void* stream);
+int loca_gated_backward_workspace_size(int64_t N, int64_t d, int64_t f, int want_dX, int want_dW, size_t* bytes);
+int loca_gated_backward(const void* X, int64_t ldx, int64_t N, int64_t d, const void* Wg, const void* Wu, int64_t f,
+                        int act, const void* dH, int64_t lddh, void* dX, int64_t lddx, void* dWg, void* dWu,
+                        void* workspace, size_t workspace_bytes, void* stream);
+
+/*
  * loca_grad_clip — global norm of a list of gradient tensors, and their clipping:
  *
  *   norm = sqrt(sum_t sum_i g_t[i]^2),   out_t = f g_t,   f = max_norm / norm if norm > max_norm, else 1

@@ -1,8 +1,8 @@
 // Persistent CTA-pair matrix product on the sm_103a tensor cores, with the work on a finished
 // 256 x 256 tile left to the caller:  D[m, n] = sum_k A[m, k] B[n, k]   (bf16 in, fp32 sums).
 //
-// Used by the head loss (logit tiles that never leave the chip, and the two gradient products) and
-// by the adapter projection.  Each operand is K-major (k contiguous) or MN-major (m or n
+// Used by the head loss (logit tiles that never leave the chip, and the two gradient products), by the
+// adapter projection and by the gated feed-forward (two products that share A, side by side).  Each operand is K-major (k contiguous) or MN-major (m or n
 // contiguous); the tensor maps and the MMA descriptors carry the difference.
 //
 // Three shapes.  Narrow: a pair of CTAs holds a 256 x 256 fp32 tile (128 rows per CTA: half of
@@ -39,6 +39,8 @@
 
 #include <cuda.h>
 #include <cuda_bf16.h>
+
+#include <atomic>
 
 #include "loca_internal.h"
 #include "tc_ptx.cuh"
@@ -186,6 +188,13 @@ __device__ __forceinline__ Tile tile_of(const Geo& g, const Live& v, int it) {
   return t;
 }
 
+// A call's value of its launches' abort flag, so that the workspace needs no clearing: no earlier call's (nor,
+// but for one chance in 2^31, what else lay in the workspace).
+inline int32_t call_mark() {
+  static std::atomic<uint32_t> calls{0x1b873593u};
+  return int32_t(calls.fetch_add(0x9e3779b1u, std::memory_order_relaxed) | 1u);
+}
+
 // Byte offset of 16-byte chunk `u` of row `row` in a 128-byte swizzled box.
 __device__ __forceinline__ uint32_t box_off(int row, int u) {
   return uint32_t(row) * 128u + (uint32_t(u ^ (row & 7)) << 4);
@@ -219,9 +228,69 @@ __device__ __forceinline__ void store_box_bf16(uint8_t* box, const CUtensorMap* 
 // column, block b_block), ksteps() MMA steps of 16 each.  None here; the adapter projection has one.
 struct NoExt {
   static constexpr bool kOn = false;
+  static constexpr bool kSecond = false;
+  static constexpr bool kTwin = false;
   __device__ int ksteps() const { return 4; }
   __device__ int entries(int) const { return 0; }
   __device__ void entry(int, int, uint32_t, int&, int&) const {}
+};
+
+// The k axis goes on from k-block `first` with a second pair of operands (maps tmAx and tmBx, laid out as the
+// first pair): D = A B^T + A2 B2^T as one product.
+struct SecondPair : NoExt {
+  static constexpr bool kSecond = true;
+  int first;
+};
+
+// Two products that share A: an accumulator holds the same columns of A B^T and of A B2^T (B2 from tmBx), side
+// by side, so that the epilogue has both sums of an element in one thread.  A pair's even CTA loads the rows
+// of B and its odd one those of B2, 128 columns of each; the single shape loads `width` of each.  Geo's
+// columns and width are those of one product.
+struct Twin : NoExt {
+  static constexpr bool kTwin = true;
+};
+
+// fp32 sums of one k range, stored or added to the sums of earlier launches
+// (one writer per element and launch: a fixed order of additions).
+struct EpiAcc {
+  static constexpr bool kPacks = false;
+  static constexpr bool kFits = true;
+  int add;
+
+  __device__ __forceinline__ void operator()(const Tile& t, float (&v)[128], int row, int col0, int lane, uint8_t* box,
+                                             const CUtensorMap* out) const {
+    const int r0 = t.split_row + row - lane;
+#pragma unroll
+    for (int b = 0; b < 4; ++b) {
+      if (lane == 0) bulk_wait_group_read0();
+      __syncwarp();
+#pragma unroll
+      for (int u = 0; u < 8; ++u)
+        *reinterpret_cast<float4*>(box + box_off(lane, u)) =
+            make_float4(v[32 * b + 4 * u], v[32 * b + 4 * u + 1], v[32 * b + 4 * u + 2], v[32 * b + 4 * u + 3]);
+      fence_proxy_async_smem();
+      __syncwarp();
+      if (lane == 0) {
+        if (LOCA_REQUIRE(col0 >= 0 && r0 >= 0)) {
+          if (add) tma_reduce_add_2d(out, smem_u32(box), col0 + 32 * b, r0);
+          else tma_store_2d(out, smem_u32(box), col0 + 32 * b, r0);
+        }
+        bulk_commit_group();
+      }
+    }
+  }
+};
+
+// Scaled and rounded once.
+struct EpiScaled {
+  static constexpr bool kPacks = true;
+  static constexpr bool kFits = false;
+  static constexpr bool kSums = false;
+  float scale;
+
+  struct Row {};
+  __device__ __forceinline__ Row row_of(int) const { return Row{}; }
+  __device__ __forceinline__ float value(const Row&, int, float v) const { return scale * v; }
 };
 
 // What becomes of a finished tile.  An output in bf16 is given value by value (kPacks): Row row_of(row)
@@ -230,7 +299,10 @@ struct NoExt {
 // uses take the sums themselves:  void operator()(const Tile&, float (&v)[128], int row, int col0, int lane,
 //                                   uint8_t* box, const CUtensorMap* out) const
 // called once per finished accumulator by every epilogue thread, with the sums of row `row`, columns
-// col0 .. col0 + 127.  kFits: the number of k ranges is the device's choice (Fit).
+// col0 .. col0 + 127.  With twin products:  Row before(int row, int col0), called before the sums are complete,
+// and operator()(const Tile&, float (&v)[128], Row&, int row, int col0, int lane, uint8_t* box, out, out2) with 64
+// columns of the first product in v[0 .. 63] and the same of the second behind them; out2 is tmAx.
+// kFits: the number of k ranges is the device's choice (Fit).
 template <int kShape, bool kAmn, bool kBmn, class Epi, class Ext>
 __global__ void __cluster_dims__(Shape<kShape>::kCtas, 1, 1) __launch_bounds__(THREADS, 1)
     k_gemm_pair(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB,
@@ -240,11 +312,13 @@ __global__ void __cluster_dims__(Shape<kShape>::kCtas, 1, 1) __launch_bounds__(T
   using S = Shape<kShape>;
   constexpr bool kPair = S::kCtas == 2;
   static_assert(kPair || !Ext::kOn, "an extended k axis takes pairs");
+  static_assert(!Ext::kTwin || (!kAmn && !kBmn), "twin products are of K-major operands");
   constexpr int MOST = S::kMostStages, BARS = S::kBars;
   constexpr bool kSlim = kShape == kSingle && !kBmn;  // tiles of `width` columns: two boxes of width / 2 rows
   const int STAGES = kSlim ? g.stages : S::kStages;
   const uint32_t a_bytes = kSlim ? uint32_t(g.arows) * 128u : uint32_t(OPB);
-  const uint32_t STAGE_BYTES = kSlim ? a_bytes + uint32_t(g.width) * 128u : uint32_t(S::kStageBytes);
+  const uint32_t b_cols = kSlim ? uint32_t(g.width) * (Ext::kTwin ? 2u : 1u) : uint32_t(TN);  // of an accumulator
+  const uint32_t STAGE_BYTES = kSlim ? a_bytes + b_cols * 128u : uint32_t(S::kStageBytes);
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   uint8_t* boxes = smem + 12 * OPB;
@@ -282,7 +356,7 @@ __global__ void __cluster_dims__(Shape<kShape>::kCtas, 1, 1) __launch_bounds__(T
     prefetch_tensormap(&tmA);
     prefetch_tensormap(&tmB);
     prefetch_tensormap(&tmO);
-    if (Ext::kOn) {
+    if (Ext::kOn || Ext::kSecond || Ext::kTwin) {
       prefetch_tensormap(&tmAx);
       prefetch_tensormap(&tmBx);
     }
@@ -299,8 +373,8 @@ __global__ void __cluster_dims__(Shape<kShape>::kCtas, 1, 1) __launch_bounds__(T
   // only the extension is that launch's work, which let this one start after all launches before it had
   // completed: the producer waits when it comes to the extension.  In the single shape B is the caller's
   // (the launch before makes A and lets this one start only after all before it): the producer fills the
-  // ring with B first.
-  constexpr bool kEarlyB = kShape == kSingle;
+  // ring with B first.  (Twin products come first in their call: B may be the work of the launch before.)
+  constexpr bool kEarlyB = kShape == kSingle && !Ext::kTwin;
   if (!Ext::kOn && !(kEarlyB && warp == 0)) wait_for_previous();
   if (!(kEarlyB && warp == 0)) launch_dependents();
   const Live lv = live_of<Epi::kFits, kShape == kSingle>(g);
@@ -317,29 +391,48 @@ __global__ void __cluster_dims__(Shape<kShape>::kCtas, 1, 1) __launch_bounds__(T
         if constexpr (kPair) tma_load_2d_pair(dst, map, bar, c0, c1);
         else tma_load_2d(dst, map, bar, c0, c1);
       };
-      auto load_a = [&](const Tile& t, int s, int k0, uint32_t fb) {
+      // k-block kb: of the second pair from `first` on
+      auto second = [&](int& kb) {
+        if constexpr (Ext::kSecond) {
+          if (kb >= ext.first) {
+            kb -= ext.first;
+            return true;
+          }
+        }
+        return false;
+      };
+      auto load_a = [&](const Tile& t, int s, int kb, uint32_t fb) {
         const uint32_t a = smem_base + uint32_t(s) * STAGE_BYTES;
         const int m0 = t.m * TM + int(rank) * HALF;
+        const CUtensorMap* map = second(kb) ? &tmAx : &tmA;
+        const int k0 = kb * BK;
         if (kAmn) {
-          load(a, &tmA, fb, m0, k0);
-          load(a + SUB, &tmA, fb, m0 + 64, k0);
+          load(a, map, fb, m0, k0);
+          load(a + SUB, map, fb, m0 + 64, k0);
         } else {
-          load(a, &tmA, fb, k0, m0);
+          load(a, map, fb, k0, m0);
         }
       };
       // 128 rows of B per operand: this CTA's half of each accumulator, or (single) both halves
-      auto load_b = [&](const Tile& t, int s, int k0, uint32_t fb) {
+      auto load_b = [&](const Tile& t, int s, int kb, uint32_t fb) {
         const uint32_t b = smem_base + uint32_t(s) * STAGE_BYTES + a_bytes;
+        const CUtensorMap* map = second(kb) ? &tmBx : &tmB;
+        const int k0 = kb * BK;
 #pragma unroll
         for (int c = 0; c < S::kOpsB; ++c) {
+          if constexpr (Ext::kTwin) {
+            if (kSlim) load(b + c * uint32_t(g.width) * 128u, c ? &tmBx : &tmB, fb, k0, t.col0);
+            else load(b + c * OPB, rank ? &tmBx : &tmB, fb, k0, t.col0 + c * HALF);
+            continue;
+          }
           const int n = t.col0 + int(rank) * HALF + c * (kPair ? TN : kSlim ? g.width / 2 : HALF);
           if (kSlim) {
-            load(b + c * uint32_t(g.width * BK), &tmB, fb, k0, n);
+            load(b + c * uint32_t(g.width * BK), map, fb, k0, n);
           } else if (kBmn) {
-            load(b + c * OPB, &tmB, fb, n, k0);
-            load(b + c * OPB + SUB, &tmB, fb, n + 64, k0);
+            load(b + c * OPB, map, fb, n, k0);
+            load(b + c * OPB + SUB, map, fb, n + 64, k0);
           } else {
-            load(b + c * OPB, &tmB, fb, k0, n);
+            load(b + c * OPB, map, fb, k0, n);
           }
         }
       };
@@ -349,7 +442,7 @@ __global__ void __cluster_dims__(Shape<kShape>::kCtas, 1, 1) __launch_bounds__(T
           const Tile t = tile_of(g, lv, cid);
           for (; int(early) < STAGES && int(early) < t.kb1 - t.kb0; ++early) {
             mbar_arrive_expect_tx(full_bar(int(early)), STAGE_BYTES);
-            load_b(t, int(early), (t.kb0 + int(early)) * BK, full_bar(int(early)));
+            load_b(t, int(early), t.kb0 + int(early), full_bar(int(early)));
           }
         }
         wait_for_previous();
@@ -368,8 +461,8 @@ __global__ void __cluster_dims__(Shape<kShape>::kCtas, 1, 1) __launch_bounds__(T
           if (leader && !ahead) mbar_arrive_expect_tx(full_bar(stage), uint32_t(S::kCtas) * STAGE_BYTES);
           const uint32_t fb = kPair ? mapa_shared(full_bar(stage), 0) : full_bar(stage);
           if (!Ext::kOn || j < nb) {
-            load_a(t, stage, (t.kb0 + j) * BK, fb);
-            if (!ahead) load_b(t, stage, (t.kb0 + j) * BK, fb);
+            load_a(t, stage, t.kb0 + j, fb);
+            if (!ahead) load_b(t, stage, t.kb0 + j, fb);
           } else {
             if (!waited) {
               wait_for_previous();
@@ -404,7 +497,7 @@ __global__ void __cluster_dims__(Shape<kShape>::kCtas, 1, 1) __launch_bounds__(T
       const uint64_t b_kmaj = sdesc(smem_base + a_bytes, kKLbo, 1024u, kSwizzle128B);
       const uint64_t b0 = kBmn ? sdesc(smem_base + a_bytes, SUB, 1024u, kSwizzle128B) : b_kmaj;
       constexpr uint64_t kAStep = kAmn ? 2048 >> 4 : 32 >> 4, kBStep = kBmn ? 2048 >> 4 : 32 >> 4;
-      const uint32_t id = tc::idesc(1, 1, kAmn ? 1 : 0, kBmn ? 1 : 0, S::kCtas * HALF, kSlim ? uint32_t(g.width) : TN);
+      const uint32_t id = tc::idesc(1, 1, kAmn ? 1 : 0, kBmn ? 1 : 0, S::kCtas * HALF, b_cols);
       constexpr uint32_t kIdX = tc::idesc(1, 1, 0, 0, TM, TN);
       // the MMAs of one k-block into accumulator c
       auto block = [&](int s, uint32_t d, int c, bool from_ext, bool first) {
@@ -441,7 +534,7 @@ __global__ void __cluster_dims__(Shape<kShape>::kCtas, 1, 1) __launch_bounds__(T
         const int all = nb + (Ext::kOn ? ext.entries(t.m) : 0);
         if constexpr (kShape == kWide) {
           if (all == 0) continue;
-          const bool two = g.cols - t.col0 > TN;  // the second accumulator holds columns of the output
+          const bool two = g.cols - t.col0 > (Ext::kTwin ? HALF : TN);  // the second accumulator holds columns of the output
           const int head = all < STAGES ? all : STAGES;
           const int stage0 = stage;
           ok = wait_acc(0, (seg & 1u) ^ 1u);
@@ -525,7 +618,40 @@ __global__ void __cluster_dims__(Shape<kShape>::kCtas, 1, 1) __launch_bounds__(T
         }
       };
       const int r0 = row - lane;
-      if constexpr (kShape == kWide && Epi::kPacks) {
+      if constexpr (Ext::kTwin) {
+        // 64 columns of the first product and the same of the second, for every accumulator
+        const uint32_t second = kSlim ? uint32_t(g.width) : uint32_t(HALF);
+        const int nseg = kShape == kWide ? 1 : (all + g.seg_kb - 1) / g.seg_kb;
+#pragma unroll 1
+        for (uint32_t a = 0; a < uint32_t(S::kAcc); ++a) {
+          const int col0 = t.col0 + int(a) * HALF + h * 64;
+          auto pre = epi.before(row, col0);
+          float v[128];
+          for (int s = 0; s < nseg; ++s) {
+            const uint32_t n = kShape == kWide ? seg : (seg + uint32_t(s)) >> 1;
+            const uint32_t b = kShape == kWide ? a : (seg + uint32_t(s)) & 1u;
+            if (!(go = wait_sums(b, n & 1u))) break;
+            const uint32_t ta = tmem_base + (uint32_t(q * 32) << 16) + b * uint32_t(TN) + uint32_t(h * 64);
+            if (s == 0) {
+#pragma unroll
+              for (int c = 0; c < 4; ++c) tmem_ld32(ta + (c & 1) * 32 + (c >> 1) * second, v + c * 32);
+            } else {
+#pragma unroll
+              for (int c = 0; c < 4; ++c) {
+                float u[32];
+                tmem_ld32(ta + (c & 1) * 32 + (c >> 1) * second, u);
+#pragma unroll
+                for (int i = 0; i < 32; ++i) v[c * 32 + i] += u[i];
+              }
+            }
+            release(b);
+          }
+          if (!go) break;
+          if (col0 < t.end) epi(t, v, pre, row, col0, lane, box, &tmO, &tmAx);
+        }
+        if (!go) break;
+        seg += uint32_t(nseg);
+      } else if constexpr (kShape == kWide && Epi::kPacks) {
         // both accumulators are in registers, rounded and packed, before the stores that the MMAs need
         // not wait for: 64 words of the first, of which a box (32) leaves before the second is read
         const auto pre = epi.row_of(row);
@@ -752,10 +878,10 @@ inline cudaError_t launch(const CUtensorMap& a, const CUtensorMap& b, const CUte
                           const CUtensorMap& o, Geo g, const Epi& epi, const Ext& ext, cudaStream_t s) {
   auto kernel = k_gemm_pair<kShape, kAmn, kBmn, Epi, Ext>;
   constexpr int kCtas = Shape<kShape>::kCtas;
-  if (kShape != kSingle || kBmn || g.width == 0) g.width = Shape<kShape>::kCols;
+  if (kShape != kSingle || kBmn || g.width == 0) g.width = Shape<kShape>::kCols / (Ext::kTwin ? 2 : 1);
   if (kShape == kSingle && !kBmn) {
     if (g.arows == 0) g.arows = HALF;
-    const int s = 12 * OPB / ((g.arows + g.width) * 128);
+    const int s = 12 * OPB / ((g.arows + g.width * (Ext::kTwin ? 2 : 1)) * 128);
     g.stages = s < Shape<kSingle>::kMostStages ? s : Shape<kSingle>::kMostStages;
   }
   g.n_tiles = (g.cols + g.width - 1) / g.width;
@@ -772,7 +898,7 @@ template <bool kAmn, bool kBmn, class Epi, class Ext>
 inline cudaError_t launch_shape(int shape, const CUtensorMap& a, const CUtensorMap& b, const CUtensorMap& ax,
                                 const CUtensorMap& bx, const CUtensorMap& o, const Geo& g, const Epi& epi, const Ext& ext,
                                 cudaStream_t s) {
-  if constexpr (!Ext::kOn && !kAmn)
+  if constexpr (!Ext::kOn && !Ext::kTwin && !kAmn)
     if (shape == kSingle) return launch<kSingle, kAmn, kBmn, Epi, Ext>(a, b, ax, bx, o, g, epi, ext, s);
   return shape == kWide ? launch<kWide, kAmn, kBmn, Epi, Ext>(a, b, ax, bx, o, g, epi, ext, s)
                         : launch<kNarrow, kAmn, kBmn, Epi, Ext>(a, b, ax, bx, o, g, epi, ext, s);

@@ -283,49 +283,6 @@ struct EpiDz {
   }
 };
 
-// dH: fp32 sums of one k range, stored or added to the sums of the earlier pieces of the vocabulary
-// (one writer per element and launch: a fixed order of additions).
-struct EpiAcc {
-  static constexpr bool kPacks = false;
-  static constexpr bool kFits = true;
-  int add;
-
-  __device__ __forceinline__ void operator()(const gp::Tile& t, float (&v)[128], int row, int col0, int lane, uint8_t* box,
-                                             const CUtensorMap* out) const {
-    const int r0 = t.split_row + row - lane;
-#pragma unroll
-    for (int b = 0; b < 4; ++b) {
-      if (lane == 0) bulk_wait_group_read0();
-      __syncwarp();
-#pragma unroll
-      for (int u = 0; u < 8; ++u)
-        *reinterpret_cast<float4*>(box + gp::box_off(lane, u)) =
-            make_float4(v[32 * b + 4 * u], v[32 * b + 4 * u + 1], v[32 * b + 4 * u + 2], v[32 * b + 4 * u + 3]);
-      fence_proxy_async_smem();
-      __syncwarp();
-      if (lane == 0) {
-        if (LOCA_REQUIRE(col0 >= 0 && r0 >= 0)) {
-          if (add) tma_reduce_add_2d(out, smem_u32(box), col0 + 32 * b, r0);
-          else tma_store_2d(out, smem_u32(box), col0 + 32 * b, r0);
-        }
-        bulk_commit_group();
-      }
-    }
-  }
-};
-
-// dW: scaled and rounded once.
-struct EpiScaled {
-  static constexpr bool kPacks = true;
-  static constexpr bool kFits = false;
-  static constexpr bool kSums = false;
-  float scale;
-
-  struct Row {};
-  __device__ __forceinline__ Row row_of(int) const { return Row{}; }
-  __device__ __forceinline__ float value(const Row&, int, float v) const { return scale * v; }
-};
-
 // ------------------------------------------------------------------ joins
 // 32 rows per block, `blockDim.y` groups of partial maxima and sums.
 __global__ void __launch_bounds__(1024)
@@ -704,7 +661,7 @@ cudaError_t launch_head_loss_backward(const void* H, int64_t ldh, int64_t N, int
         gh.m_first = int(p0 / gp::TM);
         gh.splits = lay.splits;
         gh.fit = fit;
-        e = gp::launch_shape<false, true>(shape, mz_k, mw_mn, mz_k, mw_mn, mo, gh, EpiAcc{v0 > 0 ? 1 : 0}, gp::NoExt{}, s);
+        e = gp::launch_shape<false, true>(shape, mz_k, mw_mn, mz_k, mw_mn, mo, gh, gp::EpiAcc{v0 > 0 ? 1 : 0}, gp::NoExt{}, s);
         if (e != cudaSuccess) return e;
       }
       if (dW) {
@@ -715,7 +672,7 @@ cudaError_t launch_head_loss_backward(const void* H, int64_t ldh, int64_t N, int
           return cudaErrorInvalidValue;
         gp::Geo gw = geo(vtiles, d, np / gp::BK, kSegKbGrad, r, status);
         gw.k_live = r.count;
-        e = gp::launch_either<true, true>(mz_mn, mh_mn, mz_mn, mh_mn, mo, gw, EpiScaled{scale}, gp::NoExt{}, s);
+        e = gp::launch_either<true, true>(mz_mn, mh_mn, mz_mn, mh_mn, mo, gw, gp::EpiScaled{scale}, gp::NoExt{}, s);
         if (e != cudaSuccess) return e;
       }
     }

@@ -77,6 +77,30 @@ bool overlap(const Block& x, const Block& y, int64_t rows) {
   return false;
 }
 
+// Whether two matrices, each with rows of its own number, share a byte: exact where they have the same number of
+// rows, else by their whole extents.
+struct Matrix {
+  const void* p;
+  int64_t rows, pitch, cols;  // pitch and cols in elements of 2 bytes
+};
+bool overlap(const Matrix& x, const Matrix& y) {
+  if (!x.p || !y.p || x.rows < 1 || y.rows < 1) return false;
+  if (x.rows == y.rows) return overlap({x.p, 2 * x.pitch, 2 * x.cols}, {y.p, 2 * y.pitch, 2 * y.cols}, x.rows);
+  const int64_t a = reinterpret_cast<int64_t>(x.p), b = reinterpret_cast<int64_t>(y.p);
+  return a < b + 2 * ((y.rows - 1) * y.pitch + y.cols) && b < a + 2 * ((x.rows - 1) * x.pitch + x.cols);
+}
+
+int check_gated(int64_t N, int64_t d, int64_t f) {
+  if (N < 0 || N > (int64_t(1) << 24)) return fail(LOCA_ERR_SHAPE, "need 0 <= N <= 2^24, got %lld", (long long)N);
+  if (d < 8 || d > 65536 || d % 8 != 0 || f < 8 || f > 65536 || f % 8 != 0)
+    return fail(LOCA_ERR_SHAPE, "need 8 <= d, f <= 65536, multiples of 8, got %lld, %lld", (long long)d, (long long)f);
+  return LOCA_OK;
+}
+int check_act(int act) {
+  if (act != LOCA_ACT_SILU && act != LOCA_ACT_GELU) return fail(LOCA_ERR_INVALID_ARG, "unknown activation code %d", act);
+  return LOCA_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -273,6 +297,85 @@ int loca_adapter_backward(const void* X, int64_t ldx, const void* dY, int64_t ld
   const cudaError_t e = launch_adapter_backward(X, ldx, dY, lddy, N, d_in, W, d_out, packed, n, k, plan, dX, lddx, dA, dB,
                                                 grad_dtype, workspace, status, s);
   if (e != cudaSuccess) return cuda_fail(e, "loca_adapter_backward launch");
+  return LOCA_OK;
+}
+
+int loca_gated_workspace_size(int64_t N, int64_t d, int64_t f, size_t* bytes) {
+  clear();
+  if (!bytes) return fail(LOCA_ERR_INVALID_ARG, "bytes is NULL");
+  const int rc = check_gated(N, d, f);
+  if (rc != LOCA_OK) return rc;
+  *bytes = gated_workspace_bytes();
+  return LOCA_OK;
+}
+
+int loca_gated(const void* X, int64_t ldx, int64_t N, int64_t d, const void* Wg, const void* Wu, int64_t f, int act,
+               void* H, int64_t ldh, void* workspace, size_t workspace_bytes, void* stream) {
+  clear();
+  int rc = check_gated(N, d, f);
+  if (rc != LOCA_OK || (rc = check_act(act)) != LOCA_OK) return rc;
+  if (N == 0) return LOCA_OK;
+  if (!X || !Wg || !Wu || !H) return fail(LOCA_ERR_INVALID_ARG, "X, Wg, Wu and H are required");
+  if ((rc = check_rows(X, ldx, d, "X")) != LOCA_OK || (rc = check_rows(H, ldh, f, "H")) != LOCA_OK ||
+      (rc = check_rows(Wg, d, d, "Wg")) != LOCA_OK || (rc = check_rows(Wu, d, d, "Wu")) != LOCA_OK)
+    return rc;
+  rc = check_ws(workspace, workspace_bytes, gated_workspace_bytes());
+  if (rc != LOCA_OK) return rc;
+  const Matrix h{H, N, ldh, f};
+  if (overlap(h, {X, N, ldx, d}) || overlap(h, {Wg, f, d, d}) || overlap(h, {Wu, f, d, d}))
+    return fail(LOCA_ERR_INVALID_ARG, "H must not overlap X, Wg or Wu");
+  int32_t* status = device_status_word();
+  if (!status) return fail(LOCA_ERR_CUDA, "cannot resolve the device status word");
+  const cudaError_t e =
+      launch_gated(X, ldx, N, d, Wg, Wu, f, act, H, ldh, workspace, status, static_cast<cudaStream_t>(stream));
+  if (e != cudaSuccess) return cuda_fail(e, "loca_gated launch");
+  return LOCA_OK;
+}
+
+int loca_gated_backward_workspace_size(int64_t N, int64_t d, int64_t f, int want_dX, int want_dW, size_t* bytes) {
+  clear();
+  if (!bytes) return fail(LOCA_ERR_INVALID_ARG, "bytes is NULL");
+  const int rc = check_gated(N, d, f);
+  if (rc != LOCA_OK) return rc;
+  *bytes = gated_backward_workspace_bytes(N, d, f, want_dX != 0, want_dW != 0);
+  return LOCA_OK;
+}
+
+int loca_gated_backward(const void* X, int64_t ldx, int64_t N, int64_t d, const void* Wg, const void* Wu, int64_t f,
+                        int act, const void* dH, int64_t lddh, void* dX, int64_t lddx, void* dWg, void* dWu,
+                        void* workspace, size_t workspace_bytes, void* stream) {
+  clear();
+  int rc = check_gated(N, d, f);
+  if (rc != LOCA_OK || (rc = check_act(act)) != LOCA_OK) return rc;
+  if (!dX && !dWg && !dWu) return fail(LOCA_ERR_INVALID_ARG, "one of dX, dWg and dWu is required");
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  if ((dWg && (rc = check_rows(dWg, d, d, "dWg")) != LOCA_OK) || (dWu && (rc = check_rows(dWu, d, d, "dWu")) != LOCA_OK))
+    return rc;
+  const Matrix mg{dWg, f, d, d}, mu{dWu, f, d, d}, mx{dX, N, lddx, d};
+  if (overlap(mg, mu)) return fail(LOCA_ERR_INVALID_ARG, "dWg must not overlap dWu");
+  if (N == 0) {  // sums over no row
+    cudaError_t e = dWg ? cudaMemsetAsync(dWg, 0, 2 * size_t(f) * size_t(d), s) : cudaSuccess;
+    if (e == cudaSuccess && dWu) e = cudaMemsetAsync(dWu, 0, 2 * size_t(f) * size_t(d), s);
+    return e == cudaSuccess ? int(LOCA_OK) : cuda_fail(e, "loca_gated_backward memset");
+  }
+  if (!X || !Wg || !Wu || !dH) return fail(LOCA_ERR_INVALID_ARG, "X, Wg, Wu and dH are required");
+  if ((rc = check_rows(X, ldx, d, "X")) != LOCA_OK || (rc = check_rows(dH, lddh, f, "dH")) != LOCA_OK ||
+      (rc = check_rows(Wg, d, d, "Wg")) != LOCA_OK || (rc = check_rows(Wu, d, d, "Wu")) != LOCA_OK ||
+      (dX && (rc = check_rows(dX, lddx, d, "dX")) != LOCA_OK))
+    return rc;
+  rc = check_ws(workspace, workspace_bytes,
+                gated_backward_workspace_bytes(N, d, f, dX != nullptr, dWg != nullptr || dWu != nullptr));
+  if (rc != LOCA_OK) return rc;
+  const Matrix in[4] = {{X, N, ldx, d}, {dH, N, lddh, f}, {Wg, f, d, d}, {Wu, f, d, d}};
+  for (const Matrix& m : in)
+    if (overlap(mx, m) || overlap(mg, m) || overlap(mu, m))
+      return fail(LOCA_ERR_INVALID_ARG, "dX, dWg and dWu must not overlap X, dH, Wg or Wu");
+  if (overlap(mx, mg) || overlap(mx, mu)) return fail(LOCA_ERR_INVALID_ARG, "dX must not overlap dWg or dWu");
+  int32_t* status = device_status_word();
+  if (!status) return fail(LOCA_ERR_CUDA, "cannot resolve the device status word");
+  const cudaError_t e = launch_gated_backward(X, ldx, N, d, Wg, Wu, f, act, dH, lddh, dX, lddx, dWg, dWu, workspace,
+                                              status, s);
+  if (e != cudaSuccess) return cuda_fail(e, "loca_gated_backward launch");
   return LOCA_OK;
 }
 

@@ -185,6 +185,15 @@ cudaError_t launch_adapter_backward(const void* X, int64_t ldx, const void* dY, 
                                     void* dX, int64_t lddx, void* dA, void* dB, int grad_dtype, void* workspace,
                                     int32_t* status, cudaStream_t s);
 
+// ---- gated feed-forward (gated.cu)
+size_t gated_workspace_bytes();
+size_t gated_backward_workspace_bytes(int64_t N, int64_t d, int64_t f, bool dx, bool dw);
+cudaError_t launch_gated(const void* X, int64_t ldx, int64_t N, int64_t d, const void* Wg, const void* Wu, int64_t f,
+                         int act, void* H, int64_t ldh, void* workspace, int32_t* status, cudaStream_t s);
+cudaError_t launch_gated_backward(const void* X, int64_t ldx, int64_t N, int64_t d, const void* Wg, const void* Wu,
+                                  int64_t f, int act, const void* dH, int64_t lddh, void* dX, int64_t lddx, void* dWg,
+                                  void* dWu, void* workspace, int32_t* status, cudaStream_t s);
+
 // ---- gradient norm and clipping (grad_clip.cu); grads, out, numel, dtype: host arrays
 int64_t grad_clip_max_numel();
 size_t grad_clip_workspace_bytes(int n);

@@ -25,6 +25,7 @@ LIB_DEBUG_PATH = os.path.join(_PKG, "libloca_debug.so")  # built with -DLOCA_DEB
 
 LOCA_F32 = 0
 LOCA_BF16 = 1
+ACTIVATIONS = {"silu": 0, "gelu": 1}  # LOCA_ACT_SILU, LOCA_ACT_GELU (the tanh form)
 
 STATUS_NAMES = {
     0: "LOCA_OK", 1: "LOCA_ERR_INVALID_ARG", 2: "LOCA_ERR_SHAPE", 3: "LOCA_ERR_ALIGNMENT",
@@ -101,6 +102,13 @@ SIGNATURES = [
      [_P, _I64, _I64, _I64, _P, _I64, _P, _I32, _I32, _P, _P, _I64, _P, _SZ, _P]),
     ("loca_adapter_backward", ctypes.c_int,
      [_P, _I64, _P, _I64, _I64, _I64, _P, _I64, _P, _I32, _I32, _P, _P, _I64, _P, _P, ctypes.c_int, _P, _SZ, _P]),
+    ("loca_gated_workspace_size", ctypes.c_int, [_I64, _I64, _I64, ctypes.POINTER(_SZ)]),
+    ("loca_gated", ctypes.c_int,
+     [_P, _I64, _I64, _I64, _P, _P, _I64, ctypes.c_int, _P, _I64, _P, _SZ, _P]),
+    ("loca_gated_backward_workspace_size", ctypes.c_int,
+     [_I64, _I64, _I64, ctypes.c_int, ctypes.c_int, ctypes.POINTER(_SZ)]),
+    ("loca_gated_backward", ctypes.c_int,
+     [_P, _I64, _I64, _I64, _P, _P, _I64, ctypes.c_int, _P, _I64, _P, _I64, _P, _P, _P, _SZ, _P]),
     ("loca_grad_clip_workspace_size", ctypes.c_int, [_I32, ctypes.POINTER(_SZ)]),
     ("loca_grad_clip", ctypes.c_int, [_P, _P, _P, _P, _I32, _F, _P, _P, _SZ, _P]),
 ]
@@ -867,6 +875,66 @@ def loca_adapter_backward(X, dY, W, adapters, plan, dX=None, dA=None, dB=None, w
                                      _ptr(adapters.packed), adapters.n, adapters.k, _ptr(plan.buf), _ptr(dX), lddx,
                                      _ptr(dA), _ptr(dB), _code(kind), _ptr(ws), nbytes, _stream(stream))
     _check(rc, "loca_adapter_backward")
+
+
+def _same_device(*tensors):
+    """The call runs on the current device: refuses tensors of another one."""
+    here = torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and t.device.index != here:
+            raise ValueError(f"a tensor is on {t.device}, the current device is cuda:{here}")
+
+
+def gated_workspace_size(N, d, f) -> int:
+    return _size("loca_gated_workspace_size", N, d, f)
+
+
+def _gated_args(X, Wg, Wu, act):
+    ldx = _rows2d(X, "X", torch.bfloat16)
+    _dev(Wg, "Wg", torch.bfloat16, 2)
+    _dev(Wu, "Wu", torch.bfloat16, 2)
+    N, d = X.shape
+    if Wg.shape[1] != d or Wu.shape != Wg.shape:
+        raise ValueError(f"Wg and Wu must be f x {d}, got {tuple(Wg.shape)} and {tuple(Wu.shape)}")
+    if act not in ACTIVATIONS:
+        raise ValueError(f"act must be one of {sorted(ACTIVATIONS)}, got {act!r}")
+    return ldx, N, d, Wg.shape[0], ACTIVATIONS[act]
+
+
+def loca_gated(X, Wg, Wu, H, act="silu", workspace=None, stream=None):
+    """Gated feed-forward ``H = act(X Wg^T) * (X Wu^T)`` in one launch: ``X`` N x d and ``H`` N x f bf16 (rows
+    may be spaced), ``Wg`` and ``Wu`` f x d bf16; ``act`` "silu" or "gelu" (the tanh form)."""
+    ldx, N, d, f, code = _gated_args(X, Wg, Wu, act)
+    ldh = _rows2d(H, "H", torch.bfloat16, (N, f))
+    _same_device(X, Wg, Wu, H)
+    nbytes = gated_workspace_size(N, d, f)
+    ws = _workspace(nbytes, X.device, workspace, stream)
+    rc = lib().loca_gated(_ptr(X), ldx, N, d, _ptr(Wg), _ptr(Wu), f, code, _ptr(H), ldh, _ptr(ws), nbytes,
+                          _stream(stream))
+    _check(rc, "loca_gated")
+
+
+def gated_backward_workspace_size(N, d, f, want_dX=True, want_dW=True) -> int:
+    return _size("loca_gated_backward_workspace_size", N, d, f, int(bool(want_dX)), int(bool(want_dW)))
+
+
+def loca_gated_backward(X, Wg, Wu, dH, dX=None, dWg=None, dWu=None, act="silu", workspace=None, stream=None):
+    """Gradients of :func:`loca_gated` from ``dH`` (N x f bf16, rows may be spaced): ``dX`` (N x d bf16, rows
+    may be spaced), ``dWg`` and ``dWu`` (f x d bf16), each optional.  Keeps nothing of the forward call: the
+    pre-activations are computed again."""
+    ldx, N, d, f, code = _gated_args(X, Wg, Wu, act)
+    lddh = _rows2d(dH, "dH", torch.bfloat16, (N, f))
+    lddx = 0 if dX is None else _rows2d(dX, "dX", torch.bfloat16, (N, d))
+    _dev(dWg, "dWg", torch.bfloat16, 2)
+    _dev(dWu, "dWu", torch.bfloat16, 2)
+    if any(g is not None and tuple(g.shape) != (f, d) for g in (dWg, dWu)):
+        raise ValueError("dWg and dWu must be f x d")
+    _same_device(X, Wg, Wu, dH, dX, dWg, dWu)
+    nbytes = gated_backward_workspace_size(N, d, f, dX is not None, dWg is not None or dWu is not None)
+    ws = _workspace(nbytes, X.device, workspace, stream)
+    rc = lib().loca_gated_backward(_ptr(X), ldx, N, d, _ptr(Wg), _ptr(Wu), f, code, _ptr(dH), lddh, _ptr(dX), lddx,
+                                   _ptr(dWg), _ptr(dWu), _ptr(ws), nbytes, _stream(stream))
+    _check(rc, "loca_gated_backward")
 
 
 class GradClip:

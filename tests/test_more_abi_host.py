@@ -1,0 +1,74 @@
+"""Host-side checks of the gated feed-forward, distillation and 4-bit entry points (no GPU needed): sizes, and
+argument validation that rejects bad calls with the documented codes before any CUDA call."""
+
+import ctypes
+
+import pytest
+
+P = ctypes.c_void_p
+BIG = 1 << 40
+
+
+def at(i):
+    """An address that is never dereferenced: validation fails first.  Buffers lie 16 MB apart."""
+    return P((i + 1) << 24)
+
+
+@pytest.fixture(scope="module")
+def L():
+    from paper_2608_03020_gb300 import _build
+    from paper_2608_03020_gb300 import loca
+
+    _build.build()
+    return loca.lib()
+
+
+def _size(fn, *args):
+    out = ctypes.c_size_t(0)
+    rc = fn(*args, ctypes.byref(out))
+    return rc, out.value
+
+
+def test_gated_sizes(L):
+    assert _size(L.loca_gated_workspace_size, 4096, 2048, 8192) == (0, 256)
+    rc, n = _size(L.loca_gated_backward_workspace_size, 4096, 2048, 8192, 1, 1)
+    # dG and dU in bf16, and the k ranges of dX in fp32
+    assert rc == 0 and 4 * 4096 * 8192 <= n <= 4 * 4096 * 8192 + 32 * 4 * 4096 * 2048 + 4096
+    rc, rows = _size(L.loca_gated_backward_workspace_size, 1 << 20, 2048, 8192, 1, 0)
+    assert rc == 0 and rows < (1 << 30) + 32 * 4 * 32768 * 2048 + 4096
+    rc, cols = _size(L.loca_gated_backward_workspace_size, 1 << 20, 2048, 8192, 0, 1)
+    assert rc == 0 and cols <= (4 << 30) + 4096
+    for bad in ((-1, 64, 64), (4, 60, 64), (4, 64, 60), (4, 0, 64), (4, 64, 65544), ((1 << 24) + 1, 64, 64)):
+        assert _size(L.loca_gated_workspace_size, *bad)[0] == 2, bad
+        assert _size(L.loca_gated_backward_workspace_size, *bad, 1, 1)[0] == 2, bad
+    assert L.loca_gated_workspace_size(4, 64, 64, None) == 1
+
+
+def test_gated_codes(L):
+    def fwd(X=at(0), ldx=64, N=4, d=64, Wg=at(1), Wu=at(2), f=72, act=0, H=at(3), ldh=72, ws=at(4), n=BIG):
+        return L.loca_gated(X, ldx, N, d, Wg, Wu, f, act, H, ldh, ws, n, None)
+
+    assert fwd(N=0, X=None, Wg=None, Wu=None, H=None, ws=None, n=0) == 0  # nothing to do
+    assert fwd(N=-1) == 2 and fwd(d=12) == 2 and fwd(f=12) == 2 and fwd(act=2) == 1 and fwd(act=-1) == 1
+    assert fwd(X=None) == 1 and fwd(Wg=None) == 1 and fwd(Wu=None) == 1 and fwd(H=None) == 1
+    assert fwd(ldx=56) == 2 and fwd(ldh=64) == 2 and fwd(ldx=68) == 3 and fwd(ldh=76) == 3
+    assert fwd(X=P(8)) == 3 and fwd(Wg=P(8)) == 3 and fwd(Wu=P(8)) == 3 and fwd(H=P(8)) == 3
+    assert fwd(ws=None) == 7 and fwd(n=16) == 7 and fwd(ws=P(16)) == 3
+    assert fwd(H=at(0)) == 1 and fwd(H=at(1)) == 1 and fwd(H=at(2)) == 1
+    # rows side by side share no byte, rows that reach into each other do
+    assert fwd(H=P(at(0).value + 128), ldx=136, ldh=136, ws=None) == 7
+    assert fwd(H=P(at(0).value + 112), ldx=136, ldh=136) == 1
+
+    def back(X=at(0), ldx=64, N=4, d=64, Wg=at(1), Wu=at(2), f=72, act=0, dH=at(3), lddh=72, dX=at(4), lddx=64, dWg=at(5),
+             dWu=at(6), ws=at(7), n=BIG):
+        return L.loca_gated_backward(X, ldx, N, d, Wg, Wu, f, act, dH, lddh, dX, lddx, dWg, dWu, ws, n, None)
+
+    assert back(N=0, X=None, Wg=None, Wu=None, dH=None, dWg=None, dWu=None, ws=None, n=0) == 0
+    assert back(dX=None, dWg=None, dWu=None) == 1 and back(act=7) == 1
+    assert back(X=None) == 1 and back(dH=None) == 1 and back(Wg=None) == 1 and back(Wu=None) == 1
+    assert back(lddh=64) == 2 and back(lddx=56) == 2 and back(lddx=68) == 3 and back(dWg=P(8)) == 3 and back(dWu=P(8)) == 3
+    assert back(n=256) == 7 and back(ws=None) == 7
+    for out in ("dX", "dWg", "dWu"):
+        for inp in (0, 1, 2, 3):
+            assert back(**{out: at(inp)}) == 1, (out, inp)
+    assert back(dWu=at(5)) == 1 and back(dX=at(5)) == 1 and back(dX=at(6)) == 1
