@@ -527,6 +527,36 @@ int loca_head_loss_backward(const void* H, int64_t ldh, int64_t N, int64_t d, co
                             void* dH, int64_t lddh, void* dW, void* workspace, size_t workspace_bytes, void* stream);
 
 /*
+ * loca_head_distill / loca_head_distill_backward — distillation from a teacher's top logits, from hidden states and
+ * the vocabulary head, without the student's logits in memory.  For position n with the teacher's logits t[n, k] at the
+ * words idx[n, k], k < K:
+ *
+ *   z = H W^T,   q_n = softmax(t[n, :] / tau),   lse_n = log sum_v exp(z[n, v] / tau)
+ *   loss_n = w_n tau^2 sum_k q_nk (log q_nk - z[n, idx_nk] / tau + lse_n)
+ *   dZ = dloss_n w_n tau (exp(z / tau - lse) - q),   dH = grad_scale dZ W,   dW = grad_scale dZ^T H
+ *
+ * idx     N x K int32, 1 <= K <= 256, in any order; an entry outside [0, V) (-1) is none, a word that comes twice
+ *         counts with both its logits.  A position without an entry, or with logits of -inf alone, is
+ *         masked: its loss, lse and gradients are 0, whatever H holds there
+ * t       N x K float; -inf gives a word no share, NaN or +inf make the position's loss and gradients NaN
+ * tau     > 0, the temperature
+ * H, W, w, loss, lse, dloss, grad_scale, dH, dW, limits, arithmetic and scratch memory as for loca_head_loss and its
+ * backward call; lse is that of z / tau.  q is taken off in fp32 before dZ is rounded: an entry has an error of some
+ * 2^-19 of p, so that for positions where one word has all of q and p nearly all loca_head_loss keeps more of the
+ * gradient.  Deterministic.
+ */
+int loca_head_distill_workspace_size(int64_t N, int64_t V, int64_t d, int32_t K, size_t* bytes);
+int loca_head_distill(const void* H, int64_t ldh, int64_t N, int64_t d, const void* W, int64_t V, const int32_t* idx,
+                      const float* t, int32_t K, float tau, const float* w, float* loss, float* lse, void* workspace,
+                      size_t workspace_bytes, void* stream);
+int loca_head_distill_backward_workspace_size(int64_t N, int64_t V, int64_t d, int32_t K, int want_dH, int want_dW,
+                                              size_t* bytes);
+int loca_head_distill_backward(const void* H, int64_t ldh, int64_t N, int64_t d, const void* W, int64_t V,
+                               const int32_t* idx, const float* t, int32_t K, float tau, const float* w,
+                               const float* lse, const float* dloss, float grad_scale, void* dH, int64_t lddh, void* dW,
+                               void* workspace, size_t workspace_bytes, void* stream);
+
+/*
  * Adapters of many requests beside a shared frozen projection (Eq. 1), forward and backward:
  *
  *   U = X A_a,   Y = X W^T + s_a U B_a^T                       a = ids[n]; outside [0, n): Y = X W^T

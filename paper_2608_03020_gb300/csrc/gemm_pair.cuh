@@ -284,6 +284,7 @@ struct EpiAcc {
 // Scaled and rounded once.
 struct EpiScaled {
   static constexpr bool kPacks = true;
+  static constexpr bool kSeeks = false;
   static constexpr bool kFits = false;
   static constexpr bool kSums = false;
   float scale;
@@ -295,7 +296,8 @@ struct EpiScaled {
 
 // What becomes of a finished tile.  An output in bf16 is given value by value (kPacks): Row row_of(row)
 // reads what a row needs, before its sums are complete; value(Row, column, sum) is the output.  kSums (not
-// in the wide shape): Row adds something up over the values, which finish(Row, half tile, row) gets.  Other
+// in the wide shape): Row adds something up over the values, which finish(Row, half tile, row) gets.  kSeeks (not in
+// the wide shape): seek(Row, column) is called ahead of the first of a thread's columns, which come in order.  Other
 // uses take the sums themselves:  void operator()(const Tile&, float (&v)[128], int row, int col0, int lane,
 //                                   uint8_t* box, const CUtensorMap* out) const
 // called once per finished accumulator by every epilogue thread, with the sums of row `row`, columns
@@ -727,6 +729,7 @@ __global__ void __cluster_dims__(Shape<kShape>::kCtas, 1, 1) __launch_bounds__(T
         const int col0 = t.col0 + h * HALF;
         if constexpr (Epi::kPacks) {
           auto pre = epi.row_of(row);
+          if constexpr (Epi::kSeeks) epi.seek(pre, col0);
 #pragma unroll
           for (int b = 0; b < 2; ++b) {
             if (col0 + 64 * b >= (kSlim ? t.end : g.cols)) continue;

@@ -23,6 +23,15 @@
 //                over the logits of its own
 // k_head_join    combines a row's maxima and sums in a fixed order: lse, loss, E
 // k_head_dh      sums the k ranges of dH, scales, rounds once and puts each row back in its place
+// Distillation from K teacher logits t of a position, at words i_k:
+//   q = softmax(t / tau) over the K,  p = softmax(z / tau) over the vocabulary
+//   loss_n = w_n tau^2 sum_k q_k (log q_k - log p_{i_k}),  dZ = g_n w_n tau (p - q)
+// k_teacher      each position's words in order, a word that comes twice once with both shares, q and
+//                sum q log q; positions without a word are masked
+// The epilogue of a logit tile finds the row's first word at or behind its columns by bisection and goes on
+// from word to word as the columns pass: forward it stores their logits (K of V), backward it takes q off
+// p in fp32, before dZ is rounded.
+// k_teacher_join as k_head_join, with the sum over the words
 // Computing the logits a second time costs 2 N d V operations; keeping them would cost 4 N V bytes
 // (2.5 GB per 4096 tokens at V = 151936).
 // Bound: the tensor cores from a few hundred tokens on, the read of W below.  8192 live of 16384 tokens at
@@ -65,6 +74,13 @@ constexpr int kSegKbGrad = 64;         // gradients (rounded to bf16): 4096 k pe
 __device__ __forceinline__ float exp_diff(float a, float b) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"((a - b) * kLog2e));
+  return y;
+}
+
+// e^((a - b) / tau) with scale = log2(e) / tau
+__device__ __forceinline__ float exp_scaled(float a, float b, float scale) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"((a - b) * scale));
   return y;
 }
 
@@ -246,6 +262,7 @@ struct EpiStats {
 // the other columns' p.
 struct EpiDz {
   static constexpr bool kPacks = true;
+  static constexpr bool kSeeks = false;
   static constexpr bool kFits = false;
   static constexpr bool kSums = true;
   const float* lse;
@@ -283,17 +300,237 @@ struct EpiDz {
   }
 };
 
-// ------------------------------------------------------------------ joins
-// 32 rows per block, `blockDim.y` groups of partial maxima and sums.
-__global__ void __launch_bounds__(1024)
-    k_head_join(const float2* __restrict__ part, int64_t pitch, int nparts, Rows in, int64_t row_first,
-                const float* __restrict__ zy, const float* __restrict__ zc, const int32_t* __restrict__ cols, int C,
-                float* __restrict__ loss, float* __restrict__ lse, float* __restrict__ E) {
-  __shared__ float2 sh[32][33];
+// ------------------------------------------------------------------ a teacher's words
+constexpr int kMostWords = 256;
+constexpr int kTeacherWarps = 4;  // rows of a block of k_teacher
+constexpr int32_t kNoWord = 0x7fffffff;
+
+// Each position's words, ascending and without repetition (kNoWord behind the last), with their shares q.
+struct Words {
+  int32_t* at;   // N x K
+  float* q;      // N x K
+  float* ent;    // N: sum q log q over the given entries
+  int32_t* live; // N: 0, or -1 where a position has no word (or no share: all its logits -inf)
+  int K;
+};
+
+// One warp a row: the words sorted in shared memory by exchanges whose order the sizes alone fix (bitonic), then
+// runs of one word joined from left to right.  Entries outside [0, V) are none.  A NaN among the logits, or +inf,
+// makes the row's q NaN.  Bound: latency; 16384 rows of 128 words take 3 waves of the SMs' warps.
+__global__ void __launch_bounds__(32 * kTeacherWarps)
+    k_teacher(const int32_t* __restrict__ idx, const float* __restrict__ t, int64_t N, int64_t V, float inv_tau, int padded,
+              Words out) {
+  extern __shared__ uint8_t smem_raw[];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  int32_t* key = reinterpret_cast<int32_t*>(smem_raw) + warp * 2 * padded;
+  float* val = reinterpret_cast<float*>(key + padded);
   wait_for_previous();
   launch_dependents();
-  const int64_t row = int64_t(blockIdx.x) * 32 + threadIdx.x;
-  const bool live = row_first + row < *in.count;
+  const int64_t n = int64_t(blockIdx.x) * kTeacherWarps + warp;
+  if (n >= N) return;
+  const int K = out.K;
+  for (int i = lane; i < padded; i += 32) {
+    const int32_t v = i < K ? __ldg(idx + n * K + i) : -1;
+    const bool word = v >= 0 && v < V;
+    key[i] = word ? v : kNoWord;
+    val[i] = word ? __ldg(t + n * K + i) * inv_tau : -INFINITY;
+  }
+  __syncwarp();
+  for (int span = 2; span <= padded; span <<= 1)
+    for (int step = span >> 1; step > 0; step >>= 1) {
+      for (int c = lane; c < padded / 2; c += 32) {
+        const int i = 2 * c - (c & (step - 1)), j = i + step;
+        const int32_t a = key[i], b = key[j];
+        if ((a > b) == ((i & span) == 0) && a != b) {
+          key[i] = b;
+          key[j] = a;
+          const float x = val[i];
+          val[i] = val[j];
+          val[j] = x;
+        }
+      }
+      __syncwarp();
+    }
+  float m = -INFINITY;
+  for (int i = lane; i < padded; i += 32) m = fmaxf(m, val[i]);
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+  const float base = m == -INFINITY ? 0.f : m;  // (a maximum passes over NaN: the mass keeps it)
+  float mass = 0.f;
+  for (int i = lane; i < padded; i += 32) mass += expf(val[i] - base);
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) mass += __shfl_xor_sync(0xffffffffu, mass, o);
+  const float log_mass = logf(mass);
+  float ent = 0.f;
+  int count = 0;
+  for (int i0 = 0; i0 < padded; i0 += 32) {
+    const int i = i0 + lane;
+    const int32_t w = i < padded ? key[i] : kNoWord;
+    const bool word = w != kNoWord;
+    const bool first = word && (i == 0 || key[i - 1] != w);
+    float q = 0.f;
+    if (word) {
+      const float l = val[i] - base - log_mass;
+      const float share = expf(l);
+      if (!(share == 0.f)) ent += share * l;
+      if (first)
+        for (int j = i; j < padded && key[j] == w; ++j) q += expf(val[j] - base - log_mass);
+    }
+    const unsigned all = __ballot_sync(0xffffffffu, first);
+    const int at = count + __popc(all & ((1u << lane) - 1u));
+    if (first && LOCA_CHECK(n * K + at, N * K)) {
+      out.at[n * K + at] = w;
+      out.q[n * K + at] = q;
+    }
+    count += __popc(all);
+  }
+  for (int i = count + lane; i < K; i += 32) {
+    out.at[n * K + i] = kNoWord;
+    out.q[n * K + i] = 0.f;
+  }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) ent += __shfl_xor_sync(0xffffffffu, ent, o);
+  if (lane == 0) {
+    out.ent[n] = ent;
+    out.live[n] = mass == 0.f ? -1 : 0;  // (NaN lives)
+  }
+}
+
+// A row's words from a column on.
+struct Cursor {
+  const int32_t* at;  // the row's words (null: none)
+  int j;              // the next one
+  int next;           // its column, or kNoWord
+};
+__device__ __forceinline__ Cursor word_cursor(const Words& t, int32_t n) {
+  return Cursor{n >= 0 ? t.at + int64_t(n) * t.K : nullptr, 0, kNoWord};
+}
+__device__ __forceinline__ int word_column(const Words& t, const Cursor& c, int64_t v_first) {
+  const int32_t w = c.j < t.K ? __ldg(c.at + c.j) : kNoWord;
+  return w == kNoWord ? kNoWord : int(w - v_first);
+}
+// To the first word at or behind column col0 (v_first + col0 of the vocabulary).
+__device__ __forceinline__ void word_seek(const Words& t, Cursor& c, int64_t v_first, int col0) {
+  if (!c.at) return;
+  const int64_t v = v_first + col0;
+  int lo = 0, hi = t.K;
+  while (lo < hi) {
+    const int mid = (lo + hi) >> 1;
+    if (int64_t(__ldg(c.at + mid)) < v) lo = mid + 1;
+    else hi = mid;
+  }
+  c.j = lo;
+  c.next = word_column(t, c, v_first);
+}
+
+// Forward: maximum and sum of exponentials of 128 logits of a row, and the logits of its words.
+struct EpiTeacher {
+  static constexpr bool kPacks = false;
+  static constexpr bool kFits = false;
+  float2* part;        // (2 column tiles) x pitch
+  int64_t pitch;       // rows of a piece
+  const int32_t* idx;  // this piece's rows: their places in the call's order
+  Words words;
+  float* zk;           // pitch x K
+  float scale;         // log2(e) / tau
+
+  __device__ __forceinline__ void operator()(const gp::Tile& t, float (&v)[128], int row, int col0, int lane, uint8_t*,
+                                             const CUtensorMap*) const {
+    if (!LOCA_CHECK(row, pitch)) return;
+    Cursor c = word_cursor(words, idx[row]);
+    word_seek(words, c, 0, col0);
+    const int left = t.end - col0 < 128 ? t.end - col0 : 128;  // columns of the vocabulary among these
+    if (left < 128) {
+#pragma unroll
+      for (int i = 0; i < 128; ++i)
+        if (i >= left) v[i] = -INFINITY;
+    }
+    float m0 = v[0], m1 = v[1], m2 = v[2], m3 = v[3];
+#pragma unroll
+    for (int i = 4; i < 128; i += 4) {
+      m0 = fmaxf(m0, v[i]);
+      m1 = fmaxf(m1, v[i + 1]);
+      m2 = fmaxf(m2, v[i + 2]);
+      m3 = fmaxf(m3, v[i + 3]);
+    }
+    const float m = fmaxf(fmaxf(m0, m1), fmaxf(m2, m3));
+    const float base = m == -INFINITY ? 0.f : m;  // (as EpiStats)
+    float s0 = 0.f, s1 = 0.f, s2 = 0.f, s3 = 0.f;
+#pragma unroll
+    for (int i = 0; i < 128; i += 4) {
+      s0 += exp_scaled(v[i], base, scale);
+      s1 += exp_scaled(v[i + 1], base, scale);
+      s2 += exp_scaled(v[i + 2], base, scale);
+      s3 += exp_scaled(v[i + 3], base, scale);
+    }
+    part[int64_t(2 * t.n + (col0 > t.col0 ? 1 : 0)) * pitch + row] = make_float2(m, (s0 + s1) + (s2 + s3));
+    const int end = col0 + left;
+    if (__any_sync(0xffffffffu, c.next < end)) {
+      float* z = zk + int64_t(row) * words.K;
+#pragma unroll
+      for (int i = 0; i < 128; ++i)
+        if (c.next == col0 + i && i < left) {
+          if (LOCA_CHECK(c.j, words.K)) z[c.j] = v[i];
+          ++c.j;
+          c.next = word_column(words, c, 0);
+        }
+    }
+  }
+};
+
+// Backward: dZ = g tau (p - q) of the same tile, bf16, for the gradient products.  Columns past the vocabulary and
+// rows past the live ones are zero.
+struct EpiDzTeacher {
+  static constexpr bool kPacks = true;
+  static constexpr bool kSeeks = true;
+  static constexpr bool kFits = false;
+  static constexpr bool kSums = false;
+  const float* lse;    // this piece's rows
+  const float* w;      // w_n dloss_n
+  const int32_t* idx;
+  Words words;
+  float tau, inv_tau;
+  const int32_t* count;
+  int64_t row_first;   // this piece's first row among the live rows
+  int64_t v_first;     // this piece's first vocabulary column
+  int v_cols;          // its columns of the vocabulary
+
+  struct Row {
+    float lse, g;
+    int end;  // the columns that count (none in rows past the live ones)
+    Cursor c;
+    const float* q;
+  };
+  __device__ __forceinline__ Row row_of(int row) const {
+    Row r;
+    const bool live = row_first + row < *count;
+    r.lse = lse[row];
+    r.g = w[row] * tau;
+    r.end = live ? v_cols : 0;
+    const int32_t n = live ? idx[row] : -1;
+    r.c = word_cursor(words, n);
+    r.q = words.q + int64_t(n < 0 ? 0 : n) * words.K;
+    return r;
+  }
+  __device__ __forceinline__ void seek(Row& r, int col0) const { word_seek(words, r.c, v_first, col0); }
+  __device__ __forceinline__ float value(Row& r, int col, float z) const {
+    if (col >= r.end) return 0.f;
+    float p = exp_diff(fmaf(z, inv_tau, -r.lse), 0.f);
+    if (col == r.c.next) {
+      if (LOCA_CHECK(r.c.j, words.K)) p -= __ldg(r.q + r.c.j);
+      ++r.c.j;
+      r.c.next = word_column(words, r.c, v_first);
+    }
+    return r.g * p;
+  }
+};
+
+// ------------------------------------------------------------------ joins
+// A row's maximum and sum of exponentials from `blockDim.y` groups of partial ones, 32 rows per block; complete in
+// the threads of group 0.  exp: e^(difference).
+template <class Exp>
+__device__ __forceinline__ float2 join_parts(const float2* __restrict__ part, int64_t pitch, int nparts, int64_t row,
+                                             bool live, float2 (&sh)[32][33], const Exp& exp) {
   float m = -INFINITY, s = 0.f;
   if (live && LOCA_CHECK(row, pitch)) {
     constexpr int kAhead = 8;
@@ -307,7 +544,7 @@ __global__ void __launch_bounds__(1024)
 #pragma unroll
       for (int i = 0; i < kAhead; ++i) {
         const float mm = fmaxf(m, q[i].x);
-        if (mm != -INFINITY) s = s * exp_diff(m, mm) + q[i].y * exp_diff(q[i].x, mm);
+        if (mm != -INFINITY) s = s * exp(m, mm) + q[i].y * exp(q[i].x, mm);
         else s += q[i].y;  // keeps a NaN
         m = mm;
       }
@@ -315,14 +552,29 @@ __global__ void __launch_bounds__(1024)
   }
   sh[threadIdx.y][threadIdx.x] = make_float2(m, s);
   __syncthreads();
+  if (threadIdx.y == 0 && live)
+    for (int j = 1; j < int(blockDim.y); ++j) {
+      const float2 q = sh[j][threadIdx.x];
+      const float mm = fmaxf(m, q.x);
+      if (mm != -INFINITY) s = s * exp(m, mm) + q.y * exp(q.x, mm);
+      else s += q.y;
+      m = mm;
+    }
+  return make_float2(m, s);
+}
+
+__global__ void __launch_bounds__(1024)
+    k_head_join(const float2* __restrict__ part, int64_t pitch, int nparts, Rows in, int64_t row_first,
+                const float* __restrict__ zy, const float* __restrict__ zc, const int32_t* __restrict__ cols, int C,
+                float* __restrict__ loss, float* __restrict__ lse, float* __restrict__ E) {
+  __shared__ float2 sh[32][33];
+  wait_for_previous();
+  launch_dependents();
+  const int64_t row = int64_t(blockIdx.x) * 32 + threadIdx.x;
+  const bool live = row_first + row < *in.count;
+  const float2 ms = join_parts(part, pitch, nparts, row, live, sh, [](float a, float b) { return exp_diff(a, b); });
   if (threadIdx.y != 0 || !live) return;
-  for (int j = 1; j < int(blockDim.y); ++j) {
-    const float2 q = sh[j][threadIdx.x];
-    const float mm = fmaxf(m, q.x);
-    if (mm != -INFINITY) s = s * exp_diff(m, mm) + q.y * exp_diff(q.x, mm);
-    else s += q.y;
-    m = mm;
-  }
+  const float m = ms.x, s = ms.y;
   const float l = m + logf(s);
   const int64_t k = row_first + row;
   const int32_t n = in.idx[k];
@@ -333,6 +585,42 @@ __global__ void __launch_bounds__(1024)
     const int32_t y = in.y[k];
     for (int c = 0; c < C; ++c)
       E[int64_t(n) * C + c] = w * (exp_diff(zc[int64_t(c) * pitch + row], l) - (cols[c] == y ? 1.f : 0.f));
+  }
+}
+
+// lse, and the loss from the words' logits: a warp per row, in the order of the words within a lane.
+__global__ void __launch_bounds__(1024)
+    k_teacher_join(const float2* __restrict__ part, int64_t pitch, int nparts, Rows in, int64_t row_first,
+                   const float* __restrict__ zk, Words words, float tau, float inv_tau, float* __restrict__ loss,
+                   float* __restrict__ lse) {
+  __shared__ float2 sh[32][33];
+  wait_for_previous();
+  launch_dependents();
+  const int64_t row = int64_t(blockIdx.x) * 32 + threadIdx.x;
+  const bool live = row_first + row < *in.count;
+  const float scale = kLog2e * inv_tau;
+  const float2 ms =
+      join_parts(part, pitch, nparts, row, live, sh, [scale](float a, float b) { return exp_scaled(a, b, scale); });
+  __syncthreads();
+  if (threadIdx.y == 0) sh[0][threadIdx.x] = make_float2(ms.x, logf(ms.y));
+  __syncthreads();
+  for (int r = threadIdx.y; r < 32; r += int(blockDim.y)) {
+    const int64_t k = row_first + int64_t(blockIdx.x) * 32 + r;
+    if (k >= *in.count) break;
+    const float m = sh[0][r].x, log_s = sh[0][r].y;
+    const int32_t n = in.idx[k];
+    const int64_t at = int64_t(n) * words.K, from = (k - row_first) * words.K;
+    float sum = 0.f;
+    for (int j = threadIdx.x; j < words.K; j += 32) {
+      const float q = words.q[at + j];
+      if (words.at[at + j] != kNoWord && !(q == 0.f)) sum += q * ((zk[from + j] - m) * inv_tau - log_s);
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    if (threadIdx.x == 0) {
+      loss[n] = in.w[k] * tau * tau * (words.ent[n] - sum);
+      if (lse) lse[n] = m * inv_tau + log_s;
+    }
   }
 }
 
@@ -491,7 +779,7 @@ int dh_splits(int64_t n, int64_t rows, int64_t d, int64_t vc) {
   }
   return best;
 }
-BwdWs bwd_ws(int64_t N, int64_t V, int64_t d, bool dh, bool dw) {
+BwdWs bwd_ws(int64_t N, int64_t V, int64_t d, bool dh, bool dw, bool target) {
   BwdWs o{};
   o.rows = rows_ws(N, d);
   const int64_t np = round_up(N < 1 ? 1 : N, gp::TM);
@@ -511,8 +799,8 @@ BwdWs bwd_ws(int64_t N, int64_t V, int64_t d, bool dh, bool dw) {
   size_t at = o.rows.total;
   o.dz = at; at += align256(2 * size_t(o.piece) * size_t(o.vc));
   o.part = at; at += align256(4 * size_t(o.splits) * size_t(o.piece) * size_t(d));
-  o.others = at; at += align256(4 * 2 * size_t(dz_tiles(N, o.vc)) * size_t(o.piece));
-  o.sum = at; at += align256(4 * size_t(o.piece));
+  o.others = at; at += target ? align256(4 * 2 * size_t(dz_tiles(N, o.vc)) * size_t(o.piece)) : 0;
+  o.sum = at; at += target ? align256(4 * size_t(o.piece)) : 0;
   o.total = at;
   return o;
 }
@@ -541,69 +829,73 @@ cudaError_t launch_rows(const void* H, int64_t ldh, int64_t N, int64_t d, int64_
                           static_cast<__nv_bfloat16*>(dH0), lddh);
 }
 
-}  // namespace
-
-size_t head_loss_workspace_bytes(int64_t N, int64_t V, int64_t d, int C) { return fwd_ws(N, V, d, C).total; }
-size_t head_loss_backward_workspace_bytes(int64_t N, int64_t V, int64_t d, bool dh, bool dw) {
-  return bwd_ws(N, V, d, dh, dw).total;
-}
-
-cudaError_t launch_head_loss(const void* H, int64_t ldh, int64_t N, int64_t d, const void* W, int64_t V,
-                             const int32_t* y, const float* w, const int32_t* cols, int C, float* loss, float* lse,
-                             float* E, void* workspace, int32_t* status, cudaStream_t s) {
-  const FwdWs lay = fwd_ws(N, V, d, C);
-  uint8_t* ws = static_cast<uint8_t*>(workspace);
-  const Rows r = rows_at(workspace, lay.rows);
-  cudaError_t e = launch_rows(H, ldh, N, d, V, y, w, nullptr, nullptr, r, loss, lse, E, C, nullptr, 0, s);
-  if (e != cudaSuccess) return e;
-  const int64_t np = round_up(N, gp::TM);
+// The logit tiles of a forward piece; *width: columns of a tile.
+template <class Epi>
+cudaError_t forward_tiles(const Rows& r, int64_t N, int64_t p0, int64_t rows, int64_t d, const void* W, int64_t V,
+                          const Epi& epi, int32_t* status, int* width, cudaStream_t s) {
   const bool single = N <= gp::HALF;
-  const int width = single ? gp::slim_width(V) : gp::TN;
-  const int nparts = int(2 * ((V + width - 1) / width));
-  CUtensorMap mb;
-  if (single ? !gp::map_2d(&mb, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, W, d, V, d, gp::BK, width / 2)
-             : !gp::map_kmajor(&mb, W, d, V, d))
+  *width = single ? gp::slim_width(V) : gp::TN;
+  const int arows = single ? int(round_up(N, 8)) : gp::HALF;
+  CUtensorMap ma, mb;
+  if ((single ? !gp::map_2d(&mb, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, W, d, V, d, gp::BK, *width / 2)
+              : !gp::map_kmajor(&mb, W, d, V, d)) ||
+      !gp::map_2d(&ma, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, r.H + p0 * d, d, rows, d, gp::BK, arows))
     return cudaErrorInvalidValue;
-  float2* part = reinterpret_cast<float2*>(ws + lay.part);
-  float* zy = reinterpret_cast<float*>(ws + lay.zy);
-  float* zc = reinterpret_cast<float*>(ws + lay.zc);
-  for (int64_t p0 = 0; p0 < np; p0 += lay.piece) {
-    const int64_t rows = np - p0 < lay.piece ? np - p0 : lay.piece;
-    CUtensorMap ma;
-    const int arows = single ? int(round_up(N, 8)) : gp::HALF;
-    if (!gp::map_2d(&ma, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, r.H + p0 * d, d, rows, d, gp::BK, arows))
-      return cudaErrorInvalidValue;
-    gp::Geo g = geo(rows / gp::TM, V, (d + gp::BK - 1) / gp::BK, single ? kSegKbFew : kSegKb, r, status);
-    g.rows_live = r.count;
-    g.m_first = int(p0 / gp::TM);
-    EpiStats epi{part, lay.piece, r.y + p0, zy, cols, E ? C : 0, zc};
-    g.width = width;
-    g.arows = arows;
-    e = single ? gp::launch<gp::kSingle, false, false>(ma, mb, ma, mb, ma, g, epi, gp::NoExt{}, s)
-                      : gp::launch<gp::kNarrow, false, false>(ma, mb, ma, mb, ma, g, epi, gp::NoExt{}, s);
-    if (e != cudaSuccess) return e;
-    e = gp::launch_early(k_head_join, dim3(unsigned(rows / 32)), dim3(32, nparts >= 128 ? 32 : 8), 0, s, part, lay.piece,
-                         nparts, r, p0, zy, zc, cols, C, loss, lse, E);
-    if (e != cudaSuccess) return e;
-  }
-  return cudaSuccess;
+  gp::Geo g = geo(rows / gp::TM, V, (d + gp::BK - 1) / gp::BK, single ? kSegKbFew : kSegKb, r, status);
+  g.rows_live = r.count;
+  g.m_first = int(p0 / gp::TM);
+  g.width = *width;
+  g.arows = arows;
+  return single ? gp::launch<gp::kSingle, false, false>(ma, mb, ma, mb, ma, g, epi, gp::NoExt{}, s)
+                : gp::launch<gp::kNarrow, false, false>(ma, mb, ma, mb, ma, g, epi, gp::NoExt{}, s);
 }
 
-cudaError_t launch_head_loss_backward(const void* H, int64_t ldh, int64_t N, int64_t d, const void* W, int64_t V,
-                                      const int32_t* y, const float* w, const float* lse, const float* dloss,
-                                      float scale, void* dH, int64_t lddh, void* dW, void* workspace, int32_t* status,
-                                      cudaStream_t s) {
-  const BwdWs lay = bwd_ws(N, V, d, dH != nullptr, dW != nullptr);
-  uint8_t* ws = static_cast<uint8_t*>(workspace);
-  const Rows r = rows_at(workspace, lay.rows);
-  cudaError_t e = launch_rows(H, ldh, N, d, V, y, w, dloss, lse, r, nullptr, nullptr, nullptr, 0, dH, lddh, s);
-  if (e != cudaSuccess) return e;
+struct Backward {
+  BwdWs lay;
+  Rows r;
+  uint8_t* ws;
+  int64_t N, d;
+  const __nv_bfloat16* W;
+  int64_t V;
+  float scale;
+  __nv_bfloat16* dH;
+  int64_t lddh;
+  __nv_bfloat16* dW;
+  int32_t* status;
+  cudaStream_t s;
+};
+
+// The logits of a piece once more, into dZ, in the forward pass's shape and segments, so that z comes out as it went
+// into lse; *width: columns of a tile.
+template <class Epi>
+cudaError_t logit_tiles(const Backward& b, int64_t p0, int64_t rows, int64_t v0, int64_t vn, const Epi& epi, int* width) {
+  const bool single = few_rows(b.N);
+  CUtensorMap mh, mw, mz_out;
+  gp::Geo g = geo(rows / gp::TM, vn, (b.d + gp::BK - 1) / gp::BK, single ? kSegKbFew : kSegKb, b.r, b.status);
+  g.rows_live = b.r.count;
+  g.m_first = int(p0 / gp::TM);
+  g.arows = single ? int(round_up(b.N, 8)) : gp::HALF;
+  g.width = *width = single ? gp::slim_width(vn, 64) : gp::TN;
+  if (!gp::map_2d(&mh, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, b.r.H + p0 * b.d, b.d, rows, b.d, gp::BK, g.arows) ||
+      !gp::map_2d(&mw, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, b.W + v0 * b.d, b.d, vn, b.d, gp::BK, g.width / 2) ||
+      !gp::map_out_bf16(&mz_out, b.ws + b.lay.dz, b.lay.vc, b.lay.piece, b.lay.vc))
+    return cudaErrorInvalidValue;
+  return single ? gp::launch<gp::kSingle, false, false>(mh, mw, mh, mw, mz_out, g, epi, gp::NoExt{}, b.s)
+                : gp::launch<gp::kNarrow, false, false>(mh, mw, mh, mw, mz_out, g, epi, gp::NoExt{}, b.s);
+}
+
+// dH and dW in pieces of the rows and of the vocabulary.  before(p0, rows) comes ahead of a piece of rows;
+// make_dz(p0, rows, v0, vn) leaves its dZ of vn vocabulary columns in the workspace.
+template <class Before, class MakeDz>
+cudaError_t backward_pieces(const Backward& b, const Before& before, const MakeDz& make_dz) {
+  const BwdWs& lay = b.lay;
+  const Rows& r = b.r;
+  const int64_t N = b.N, d = b.d, V = b.V, lddh = b.lddh;
+  __nv_bfloat16 *dH = b.dH, *dW = b.dW;
   const int64_t np = round_up(N < 1 ? 1 : N, gp::TM);
-  const __nv_bfloat16* Wb = static_cast<const __nv_bfloat16*>(W);
-  __nv_bfloat16* dz = reinterpret_cast<__nv_bfloat16*>(ws + lay.dz);
-  float* part = reinterpret_cast<float*>(ws + lay.part);
-  float* others = reinterpret_cast<float*>(ws + lay.others);
-  float* sum = reinterpret_cast<float*>(ws + lay.sum);
+  __nv_bfloat16* dz = reinterpret_cast<__nv_bfloat16*>(b.ws + lay.dz);
+  float* part = reinterpret_cast<float*>(b.ws + lay.part);
+  cudaError_t e = cudaSuccess;
   for (int64_t p0 = 0; p0 < np; p0 += lay.piece) {
     const int64_t rows = np - p0 < lay.piece ? np - p0 : lay.piece;
     const int64_t kblocks = (lay.vc + gp::BK - 1) / gp::BK;  // of a whole piece of the vocabulary
@@ -619,72 +911,219 @@ cudaError_t launch_head_loss_backward(const void* H, int64_t ldh, int64_t N, int
       fit.tile_cycles = int(gp::tile_cycles(shape));
       fit.row_tile_cycles = int(gp::TM * d * 8 / 3000);
     }
-    // dZ of the vocabulary columns v0 .. v0 + vn.  all: they are all there are, so the sum of the others' p that
-    // the target's entry takes is whole; done: earlier calls have made it; neither: this call adds to it
-    const bool single = few_rows(N);
-    auto make_dz = [&](int64_t v0, int64_t vn, bool all, bool done) {
-      CUtensorMap mh, mw, mz_out;
-      // the forward pass's shape and segments, so that z comes out as it went into lse
-      gp::Geo g = geo(rows / gp::TM, vn, (d + gp::BK - 1) / gp::BK, single ? kSegKbFew : kSegKb, r, status);
-      g.rows_live = r.count;
-      g.m_first = int(p0 / gp::TM);
-      g.arows = single ? int(round_up(N, 8)) : gp::HALF;
-      g.width = single ? gp::slim_width(vn, 64) : gp::TN;
-      if (!gp::map_2d(&mh, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, r.H + p0 * d, d, rows, d, gp::BK, g.arows) ||
-          !gp::map_2d(&mw, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, Wb + v0 * d, d, vn, d, gp::BK, g.width / 2) ||
-          !gp::map_out_bf16(&mz_out, dz, lay.vc, lay.piece, lay.vc))
-        return cudaErrorInvalidValue;
-      const EpiDz dzed{r.lse + p0, r.w + p0, r.y + p0, r.count, p0, v0, int(vn), others, lay.piece};
-      const cudaError_t e = single ? gp::launch<gp::kSingle, false, false>(mh, mw, mh, mw, mz_out, g, dzed, gp::NoExt{}, s)
-                                   : gp::launch<gp::kNarrow, false, false>(mh, mw, mh, mw, mz_out, g, dzed, gp::NoExt{}, s);
-      if (e != cudaSuccess) return e;
-      const int nparts = done ? 0 : int(2 * ((vn + g.width - 1) / g.width));
-      return gp::launch_early(k_head_target, dim3(unsigned(rows / 32)), dim3(32, nparts >= 128 ? 32 : 8), 0, s, others,
-                              lay.piece, nparts, r, p0, sum, int(done || v0 > 0), int(!all && !done), int(all || done), v0,
-                              vn, dz, lay.vc);
-    };
-    const bool whole = V <= lay.vc;
-    for (int64_t v0 = 0; v0 < V && !whole; v0 += lay.vc)
-      if ((e = make_dz(v0, V - v0 < lay.vc ? V - v0 : lay.vc, false, false)) != cudaSuccess) return e;
+    if ((e = before(p0, rows)) != cudaSuccess) return e;
     for (int64_t v0 = 0; v0 < V; v0 += lay.vc) {
       const int64_t vn = V - v0 < lay.vc ? V - v0 : lay.vc;   // columns of the vocabulary
       const int64_t vtiles = (vn + gp::TN - 1) / gp::TN;
-      if ((e = make_dz(v0, vn, whole, !whole)) != cudaSuccess) return e;
+      if ((e = make_dz(p0, rows, v0, vn)) != cudaSuccess) return e;
       CUtensorMap mz_k, mw_mn;
       if (dH) {
         CUtensorMap mo;
-        if (!gp::map_kmajor(&mz_k, dz, lay.vc, lay.piece, lay.vc) || !gp::map_mnmajor(&mw_mn, Wb + v0 * d, d, vn, d) ||
+        if (!gp::map_kmajor(&mz_k, dz, lay.vc, lay.piece, lay.vc) || !gp::map_mnmajor(&mw_mn, b.W + v0 * d, d, vn, d) ||
             !gp::map_2d(&mo, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 4, part, d, lay.piece * lay.splits, d, 32, 32))
           return cudaErrorInvalidValue;
-        gp::Geo gh = geo(rows / gp::TM, d, (vn + gp::BK - 1) / gp::BK, kSegKbGrad, r, status);
+        gp::Geo gh = geo(rows / gp::TM, d, (vn + gp::BK - 1) / gp::BK, kSegKbGrad, r, b.status);
         gh.rows_live = r.count;
         gh.m_first = int(p0 / gp::TM);
         gh.splits = lay.splits;
         gh.fit = fit;
-        e = gp::launch_shape<false, true>(shape, mz_k, mw_mn, mz_k, mw_mn, mo, gh, gp::EpiAcc{v0 > 0 ? 1 : 0}, gp::NoExt{}, s);
+        e = gp::launch_shape<false, true>(shape, mz_k, mw_mn, mz_k, mw_mn, mo, gh, gp::EpiAcc{v0 > 0 ? 1 : 0}, gp::NoExt{},
+                                          b.s);
         if (e != cudaSuccess) return e;
       }
       if (dW) {
         CUtensorMap mz_mn, mh_mn, mo;
-        __nv_bfloat16* o = static_cast<__nv_bfloat16*>(dW) + v0 * d;
         if (!gp::map_mnmajor(&mz_mn, dz, lay.vc, lay.piece, lay.vc) || !gp::map_mnmajor(&mh_mn, r.H, d, np, d) ||
-            !gp::map_out_bf16(&mo, o, d, vn, d))
+            !gp::map_out_bf16(&mo, dW + v0 * d, d, vn, d))
           return cudaErrorInvalidValue;
-        gp::Geo gw = geo(vtiles, d, np / gp::BK, kSegKbGrad, r, status);
+        gp::Geo gw = geo(vtiles, d, np / gp::BK, kSegKbGrad, r, b.status);
         gw.k_live = r.count;
-        e = gp::launch_either<true, true>(mz_mn, mh_mn, mz_mn, mh_mn, mo, gw, gp::EpiScaled{scale}, gp::NoExt{}, s);
+        e = gp::launch_either<true, true>(mz_mn, mh_mn, mz_mn, mh_mn, mo, gw, gp::EpiScaled{b.scale}, gp::NoExt{}, b.s);
         if (e != cudaSuccess) return e;
       }
     }
     if (dH) {
       const int64_t blocks = rows * (d / 8) / 256 + 1;
       const int64_t most = 8 * int64_t(sm_count());
-      e = gp::launch_early(k_head_dh, dim3(unsigned(blocks < most ? blocks : most)), dim3(256), 0, s, part, rows,
-                           lay.splits, fit, d, r, p0, scale, static_cast<__nv_bfloat16*>(dH), lddh);
+      e = gp::launch_early(k_head_dh, dim3(unsigned(blocks < most ? blocks : most)), dim3(256), 0, b.s,
+                           static_cast<const float*>(part), rows, lay.splits, fit, d, r, p0, b.scale, dH, lddh);
       if (e != cudaSuccess) return e;
     }
   }
   return cudaSuccess;
+}
+
+}  // namespace
+
+size_t head_loss_workspace_bytes(int64_t N, int64_t V, int64_t d, int C) { return fwd_ws(N, V, d, C).total; }
+size_t head_loss_backward_workspace_bytes(int64_t N, int64_t V, int64_t d, bool dh, bool dw) {
+  return bwd_ws(N, V, d, dh, dw, true).total;
+}
+
+cudaError_t launch_head_loss(const void* H, int64_t ldh, int64_t N, int64_t d, const void* W, int64_t V,
+                             const int32_t* y, const float* w, const int32_t* cols, int C, float* loss, float* lse,
+                             float* E, void* workspace, int32_t* status, cudaStream_t s) {
+  const FwdWs lay = fwd_ws(N, V, d, C);
+  uint8_t* ws = static_cast<uint8_t*>(workspace);
+  const Rows r = rows_at(workspace, lay.rows);
+  cudaError_t e = launch_rows(H, ldh, N, d, V, y, w, nullptr, nullptr, r, loss, lse, E, C, nullptr, 0, s);
+  if (e != cudaSuccess) return e;
+  const int64_t np = round_up(N, gp::TM);
+  float2* part = reinterpret_cast<float2*>(ws + lay.part);
+  float* zy = reinterpret_cast<float*>(ws + lay.zy);
+  float* zc = reinterpret_cast<float*>(ws + lay.zc);
+  for (int64_t p0 = 0; p0 < np; p0 += lay.piece) {
+    const int64_t rows = np - p0 < lay.piece ? np - p0 : lay.piece;
+    int width = 0;
+    e = forward_tiles(r, N, p0, rows, d, W, V, EpiStats{part, lay.piece, r.y + p0, zy, cols, E ? C : 0, zc}, status, &width,
+                      s);
+    if (e != cudaSuccess) return e;
+    const int nparts = int(2 * ((V + width - 1) / width));
+    e = gp::launch_early(k_head_join, dim3(unsigned(rows / 32)), dim3(32, nparts >= 128 ? 32 : 8), 0, s, part, lay.piece,
+                         nparts, r, p0, zy, zc, cols, C, loss, lse, E);
+    if (e != cudaSuccess) return e;
+  }
+  return cudaSuccess;
+}
+
+cudaError_t launch_head_loss_backward(const void* H, int64_t ldh, int64_t N, int64_t d, const void* W, int64_t V,
+                                      const int32_t* y, const float* w, const float* lse, const float* dloss,
+                                      float scale, void* dH, int64_t lddh, void* dW, void* workspace, int32_t* status,
+                                      cudaStream_t s) {
+  const BwdWs lay = bwd_ws(N, V, d, dH != nullptr, dW != nullptr, true);
+  uint8_t* ws = static_cast<uint8_t*>(workspace);
+  const Rows r = rows_at(workspace, lay.rows);
+  cudaError_t e = launch_rows(H, ldh, N, d, V, y, w, dloss, lse, r, nullptr, nullptr, nullptr, 0, dH, lddh, s);
+  if (e != cudaSuccess) return e;
+  float* others = reinterpret_cast<float*>(ws + lay.others);
+  float* sum = reinterpret_cast<float*>(ws + lay.sum);
+  const Backward b{lay, r, ws, N, d, static_cast<const __nv_bfloat16*>(W), V, scale, static_cast<__nv_bfloat16*>(dH), lddh,
+                   static_cast<__nv_bfloat16*>(dW), status, s};
+  // dZ of the vocabulary columns v0 .. v0 + vn.  all: they are all there are, so the sum of the others' p that
+  // the target's entry takes is whole; done: earlier calls have made it; neither: this call adds to it
+  auto make_dz = [&](int64_t p0, int64_t rows, int64_t v0, int64_t vn, bool all, bool done) {
+    int width = 0;
+    const cudaError_t e =
+        logit_tiles(b, p0, rows, v0, vn, EpiDz{r.lse + p0, r.w + p0, r.y + p0, r.count, p0, v0, int(vn), others, lay.piece},
+                    &width);
+    if (e != cudaSuccess) return e;
+    const int nparts = done ? 0 : int(2 * ((vn + width - 1) / width));
+    return gp::launch_early(k_head_target, dim3(unsigned(rows / 32)), dim3(32, nparts >= 128 ? 32 : 8), 0, s, others,
+                            lay.piece, nparts, r, p0, sum, int(done || v0 > 0), int(!all && !done), int(all || done), v0,
+                            vn, reinterpret_cast<__nv_bfloat16*>(ws + lay.dz), lay.vc);
+  };
+  const bool whole = V <= lay.vc;
+  return backward_pieces(
+      b,
+      [&](int64_t p0, int64_t rows) {
+        for (int64_t v0 = 0; v0 < V && !whole; v0 += lay.vc) {
+          const cudaError_t e = make_dz(p0, rows, v0, V - v0 < lay.vc ? V - v0 : lay.vc, false, false);
+          if (e != cudaSuccess) return e;
+        }
+        return cudaSuccess;
+      },
+      [&](int64_t p0, int64_t rows, int64_t v0, int64_t vn) { return make_dz(p0, rows, v0, vn, whole, !whole); });
+}
+
+// ------------------------------------------------------------------ distillation
+namespace {
+
+struct WordsWs {
+  size_t at, q, ent, live, total;
+};
+WordsWs words_ws(int64_t N, int K, size_t from) {
+  WordsWs o{};
+  o.at = from; from += align256(4 * size_t(N) * size_t(K));
+  o.q = from; from += align256(4 * size_t(N) * size_t(K));
+  o.ent = from; from += align256(4 * size_t(N));
+  o.live = from; from += align256(4 * size_t(N));
+  o.total = from;
+  return o;
+}
+struct DistillWs {
+  FwdWs fwd;
+  WordsWs words;
+  size_t zk, total;
+};
+DistillWs distill_ws(int64_t N, int64_t V, int64_t d, int K) {
+  DistillWs o{};
+  o.fwd = fwd_ws(N, V, d, 0);
+  o.words = words_ws(N, K, o.fwd.total);
+  o.zk = o.words.total;
+  o.total = o.zk + align256(4 * size_t(o.fwd.piece) * size_t(K));
+  return o;
+}
+
+cudaError_t launch_teacher(const int32_t* idx, const float* t, int64_t N, int64_t V, int K, float tau, uint8_t* ws,
+                           const WordsWs& lay, Words* out, cudaStream_t s) {
+  *out = Words{reinterpret_cast<int32_t*>(ws + lay.at), reinterpret_cast<float*>(ws + lay.q),
+               reinterpret_cast<float*>(ws + lay.ent), reinterpret_cast<int32_t*>(ws + lay.live), K};
+  int padded = 32;
+  while (padded < K) padded *= 2;
+  const cudaError_t e = gp::keep_carveout(k_teacher);
+  if (e != cudaSuccess) return e;
+  return gp::launch_early(k_teacher, dim3(unsigned((N + kTeacherWarps - 1) / kTeacherWarps)), dim3(32 * kTeacherWarps),
+                          size_t(kTeacherWarps) * 8 * size_t(padded), s, idx, t, N, V, 1.f / tau, padded, *out);
+}
+
+}  // namespace
+
+int head_distill_max_words() { return kMostWords; }
+size_t head_distill_workspace_bytes(int64_t N, int64_t V, int64_t d, int K) { return distill_ws(N, V, d, K).total; }
+size_t head_distill_backward_workspace_bytes(int64_t N, int64_t V, int64_t d, int K, bool dh, bool dw) {
+  return words_ws(N, K, bwd_ws(N, V, d, dh, dw, false).total).total;
+}
+
+cudaError_t launch_head_distill(const void* H, int64_t ldh, int64_t N, int64_t d, const void* W, int64_t V,
+                                const int32_t* idx, const float* t, int K, float tau, const float* w, float* loss,
+                                float* lse, void* workspace, int32_t* status, cudaStream_t s) {
+  const DistillWs lay = distill_ws(N, V, d, K);
+  uint8_t* ws = static_cast<uint8_t*>(workspace);
+  Words words;
+  cudaError_t e = launch_teacher(idx, t, N, V, K, tau, ws, lay.words, &words, s);
+  if (e != cudaSuccess) return e;
+  const Rows r = rows_at(workspace, lay.fwd.rows);
+  e = launch_rows(H, ldh, N, d, 1, words.live, w, nullptr, nullptr, r, loss, lse, nullptr, 0, nullptr, 0, s);
+  if (e != cudaSuccess) return e;
+  float2* part = reinterpret_cast<float2*>(ws + lay.fwd.part);
+  float* zk = reinterpret_cast<float*>(ws + lay.zk);
+  const int64_t np = round_up(N, gp::TM);
+  for (int64_t p0 = 0; p0 < np; p0 += lay.fwd.piece) {
+    const int64_t rows = np - p0 < lay.fwd.piece ? np - p0 : lay.fwd.piece;
+    int width = 0;
+    e = forward_tiles(r, N, p0, rows, d, W, V, EpiTeacher{part, lay.fwd.piece, r.idx + p0, words, zk, kLog2e / tau}, status,
+                      &width, s);
+    if (e != cudaSuccess) return e;
+    const int nparts = int(2 * ((V + width - 1) / width));
+    e = gp::launch_early(k_teacher_join, dim3(unsigned(rows / 32)), dim3(32, nparts >= 128 ? 32 : 8), 0, s, part,
+                         lay.fwd.piece, nparts, r, p0, zk, words, tau, 1.f / tau, loss, lse);
+    if (e != cudaSuccess) return e;
+  }
+  return cudaSuccess;
+}
+
+cudaError_t launch_head_distill_backward(const void* H, int64_t ldh, int64_t N, int64_t d, const void* W, int64_t V,
+                                         const int32_t* idx, const float* t, int K, float tau, const float* w,
+                                         const float* lse, const float* dloss, float scale, void* dH, int64_t lddh,
+                                         void* dW, void* workspace, int32_t* status, cudaStream_t s) {
+  const BwdWs lay = bwd_ws(N, V, d, dH != nullptr, dW != nullptr, false);
+  uint8_t* ws = static_cast<uint8_t*>(workspace);
+  Words words;
+  cudaError_t e = launch_teacher(idx, t, N, V, K, tau, ws, words_ws(N, K, lay.total), &words, s);
+  if (e != cudaSuccess) return e;
+  const Rows r = rows_at(workspace, lay.rows);
+  e = launch_rows(H, ldh, N, d, 1, words.live, w, dloss, lse, r, nullptr, nullptr, nullptr, 0, dH, lddh, s);
+  if (e != cudaSuccess) return e;
+  const Backward b{lay, r, ws, N, d, static_cast<const __nv_bfloat16*>(W), V, scale, static_cast<__nv_bfloat16*>(dH), lddh,
+                   static_cast<__nv_bfloat16*>(dW), status, s};
+  return backward_pieces(
+      b, [](int64_t, int64_t) { return cudaSuccess; },
+      [&](int64_t p0, int64_t rows, int64_t v0, int64_t vn) {
+        int width = 0;
+        return logit_tiles(b, p0, rows, v0, vn,
+                           EpiDzTeacher{r.lse + p0, r.w + p0, r.idx + p0, words, tau, 1.f / tau, r.count, p0, v0, int(vn)},
+                           &width);
+      });
 }
 
 }  // namespace loca

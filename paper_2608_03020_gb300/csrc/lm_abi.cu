@@ -96,6 +96,14 @@ int check_gated(int64_t N, int64_t d, int64_t f) {
     return fail(LOCA_ERR_SHAPE, "need 8 <= d, f <= 65536, multiples of 8, got %lld, %lld", (long long)d, (long long)f);
   return LOCA_OK;
 }
+int check_distill(int64_t N, int64_t V, int64_t d, int32_t K, float tau) {
+  const int rc = check_head(N, V, d);
+  if (rc != LOCA_OK) return rc;
+  if (K < 1 || K > head_distill_max_words())
+    return fail(LOCA_ERR_SHAPE, "need 1 <= K <= %d words, got %d", head_distill_max_words(), K);
+  if (!(tau > 0.f) || !std::isfinite(tau)) return fail(LOCA_ERR_INVALID_ARG, "tau must be positive and finite");
+  return LOCA_OK;
+}
 int check_act(int act) {
   if (act != LOCA_ACT_SILU && act != LOCA_ACT_GELU) return fail(LOCA_ERR_INVALID_ARG, "unknown activation code %d", act);
   return LOCA_OK;
@@ -177,6 +185,82 @@ int loca_head_loss_backward(const void* H, int64_t ldh, int64_t N, int64_t d, co
   const cudaError_t e = launch_head_loss_backward(H, ldh, N, d, W, V, y, w, lse, dloss, grad_scale, N > 0 ? dH : nullptr,
                                                   lddh, dW, workspace, status, static_cast<cudaStream_t>(stream));
   if (e != cudaSuccess) return cuda_fail(e, "loca_head_loss_backward launch");
+  return LOCA_OK;
+}
+
+int loca_head_distill_workspace_size(int64_t N, int64_t V, int64_t d, int32_t K, size_t* bytes) {
+  clear();
+  if (!bytes) return fail(LOCA_ERR_INVALID_ARG, "bytes is NULL");
+  const int rc = check_distill(N, V, d, K, 1.f);
+  if (rc != LOCA_OK) return rc;
+  *bytes = head_distill_workspace_bytes(N, V, d, K);
+  return LOCA_OK;
+}
+
+int loca_head_distill(const void* H, int64_t ldh, int64_t N, int64_t d, const void* W, int64_t V, const int32_t* idx,
+                      const float* t, int32_t K, float tau, const float* w, float* loss, float* lse, void* workspace,
+                      size_t workspace_bytes, void* stream) {
+  clear();
+  int rc = check_distill(N, V, d, K, tau);
+  if (rc != LOCA_OK) return rc;
+  if (N == 0) return LOCA_OK;
+  if (!H || !W || !idx || !t || !loss) return fail(LOCA_ERR_INVALID_ARG, "H, W, idx, t and loss are required");
+  if ((rc = check_rows(H, ldh, d, "H")) != LOCA_OK || (rc = check_rows(W, d, d, "W")) != LOCA_OK) return rc;
+  if (!aligned(idx, 4) || !aligned(t, 4) || !aligned(w, 4) || !aligned(loss, 4) || !aligned(lse, 4))
+    return fail(LOCA_ERR_ALIGNMENT, "idx, t, w, loss and lse need 4-byte alignment");
+  rc = check_ws(workspace, workspace_bytes, head_distill_workspace_bytes(N, V, d, K));
+  if (rc != LOCA_OK) return rc;
+  int32_t* status = device_status_word();
+  if (!status) return fail(LOCA_ERR_CUDA, "cannot resolve the device status word");
+  const cudaError_t e = launch_head_distill(H, ldh, N, d, W, V, idx, t, K, tau, w, loss, lse, workspace, status,
+                                            static_cast<cudaStream_t>(stream));
+  if (e != cudaSuccess) return cuda_fail(e, "loca_head_distill launch");
+  return LOCA_OK;
+}
+
+int loca_head_distill_backward_workspace_size(int64_t N, int64_t V, int64_t d, int32_t K, int want_dH, int want_dW,
+                                              size_t* bytes) {
+  clear();
+  if (!bytes) return fail(LOCA_ERR_INVALID_ARG, "bytes is NULL");
+  const int rc = check_distill(N, V, d, K, 1.f);
+  if (rc != LOCA_OK) return rc;
+  *bytes = head_distill_backward_workspace_bytes(N, V, d, K, want_dH != 0, want_dW != 0);
+  return LOCA_OK;
+}
+
+int loca_head_distill_backward(const void* H, int64_t ldh, int64_t N, int64_t d, const void* W, int64_t V,
+                               const int32_t* idx, const float* t, int32_t K, float tau, const float* w,
+                               const float* lse, const float* dloss, float grad_scale, void* dH, int64_t lddh, void* dW,
+                               void* workspace, size_t workspace_bytes, void* stream) {
+  clear();
+  int rc = check_distill(N, V, d, K, tau);
+  if (rc != LOCA_OK) return rc;
+  if (!dH && !dW) return fail(LOCA_ERR_INVALID_ARG, "dH or dW is required");
+  if (!std::isfinite(grad_scale)) return fail(LOCA_ERR_INVALID_ARG, "grad_scale must be finite");
+  if (dW && (rc = check_rows(dW, d, d, "dW")) != LOCA_OK) return rc;
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  if (N == 0) {  // sums over no position
+    const cudaError_t e = dW ? cudaMemsetAsync(dW, 0, 2 * size_t(V) * size_t(d), s) : cudaSuccess;
+    return e == cudaSuccess ? int(LOCA_OK) : cuda_fail(e, "loca_head_distill_backward memset");
+  }
+  if (!H || !W || !idx || !t || !lse) return fail(LOCA_ERR_INVALID_ARG, "H, W, idx, t and lse are required");
+  if ((rc = check_rows(H, ldh, d, "H")) != LOCA_OK || (rc = check_rows(W, d, d, "W")) != LOCA_OK ||
+      (dH && (rc = check_rows(dH, lddh, d, "dH")) != LOCA_OK))
+    return rc;
+  if (!aligned(idx, 4) || !aligned(t, 4) || !aligned(w, 4) || !aligned(lse, 4) || !aligned(dloss, 4))
+    return fail(LOCA_ERR_ALIGNMENT, "idx, t, w, lse and dloss need 4-byte alignment");
+  rc = check_ws(workspace, workspace_bytes, head_distill_backward_workspace_bytes(N, V, d, K, dH != nullptr, dW != nullptr));
+  if (rc != LOCA_OK) return rc;
+  if ((dH != H || lddh != ldh) && overlap(Matrix{H, N, ldh, d}, Matrix{dH, N, lddh, d}))
+    return fail(LOCA_ERR_INVALID_ARG, "dH must be H itself or not overlap it");
+  const Matrix mw{W, V, d, d}, mdw{dW, V, d, d}, mdh{dH, N, lddh, d};
+  if (overlap(mw, mdw) || overlap(mw, mdh) || overlap(mdw, mdh) || overlap(mdw, Matrix{H, N, ldh, d}))
+    return fail(LOCA_ERR_INVALID_ARG, "dH and dW must not overlap W or one another, nor dW H");
+  int32_t* status = device_status_word();
+  if (!status) return fail(LOCA_ERR_CUDA, "cannot resolve the device status word");
+  const cudaError_t e = launch_head_distill_backward(H, ldh, N, d, W, V, idx, t, K, tau, w, lse, dloss, grad_scale, dH,
+                                                     lddh, dW, workspace, status, s);
+  if (e != cudaSuccess) return cuda_fail(e, "loca_head_distill_backward launch");
   return LOCA_OK;
 }
 

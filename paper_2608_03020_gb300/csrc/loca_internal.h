@@ -169,6 +169,18 @@ cudaError_t launch_head_loss_backward(const void* H, int64_t ldh, int64_t N, int
                                       float scale, void* dH, int64_t lddh, void* dW, void* workspace, int32_t* status,
                                       cudaStream_t s);
 
+// ---- distillation at the head (head_loss.cu)
+int head_distill_max_words();
+size_t head_distill_workspace_bytes(int64_t N, int64_t V, int64_t d, int K);
+size_t head_distill_backward_workspace_bytes(int64_t N, int64_t V, int64_t d, int K, bool dh, bool dw);
+cudaError_t launch_head_distill(const void* H, int64_t ldh, int64_t N, int64_t d, const void* W, int64_t V,
+                                const int32_t* idx, const float* t, int K, float tau, const float* w, float* loss,
+                                float* lse, void* workspace, int32_t* status, cudaStream_t s);
+cudaError_t launch_head_distill_backward(const void* H, int64_t ldh, int64_t N, int64_t d, const void* W, int64_t V,
+                                         const int32_t* idx, const float* t, int K, float tau, const float* w,
+                                         const float* lse, const float* dloss, float scale, void* dH, int64_t lddh,
+                                         void* dW, void* workspace, int32_t* status, cudaStream_t s);
+
 // ---- adapters beside a shared projection (adapter.cu)
 int adapter_max_k();
 size_t adapter_packed_bytes(int n, int64_t d_in, int64_t d_out, int k);

@@ -92,6 +92,13 @@ SIGNATURES = [
      [_I64, _I64, _I64, ctypes.c_int, ctypes.c_int, ctypes.POINTER(_SZ)]),
     ("loca_head_loss_backward", ctypes.c_int,
      [_P, _I64, _I64, _I64, _P, _I64, _P, _P, _P, _P, _F, _P, _I64, _P, _P, _SZ, _P]),
+    ("loca_head_distill_workspace_size", ctypes.c_int, [_I64, _I64, _I64, _I32, ctypes.POINTER(_SZ)]),
+    ("loca_head_distill", ctypes.c_int,
+     [_P, _I64, _I64, _I64, _P, _I64, _P, _P, _I32, _F, _P, _P, _P, _P, _SZ, _P]),
+    ("loca_head_distill_backward_workspace_size", ctypes.c_int,
+     [_I64, _I64, _I64, _I32, ctypes.c_int, ctypes.c_int, ctypes.POINTER(_SZ)]),
+    ("loca_head_distill_backward", ctypes.c_int,
+     [_P, _I64, _I64, _I64, _P, _I64, _P, _P, _I32, _F, _P, _P, _P, _F, _P, _I64, _P, _P, _SZ, _P]),
     ("loca_adapter_packed_size", ctypes.c_int, [_I32, _I64, _I64, _I32, ctypes.POINTER(_SZ)]),
     ("loca_adapter_pack", ctypes.c_int, [_P, _P, ctypes.c_int, _I32, _I64, _I64, _I32, _P, _P, _P]),
     ("loca_adapter_plan_size", ctypes.c_int, [_I64, _I32, ctypes.POINTER(_SZ)]),
@@ -775,6 +782,72 @@ def loca_head_loss_backward(H, W, y, lse, dH=None, dW=None, w=None, dloss=None, 
     _check(rc, "loca_head_loss_backward")
 
 
+def _same_device(*tensors):
+    """The call runs on the current device: refuses tensors of another one."""
+    here = torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and t.device.index != here:
+            raise ValueError(f"a tensor is on {t.device}, the current device is cuda:{here}")
+
+
+def head_distill_workspace_size(N, V, d, K) -> int:
+    return _size("loca_head_distill_workspace_size", N, V, d, K)
+
+
+def _distill_args(H, W, idx, t, w, lse):
+    ldh = _rows2d(H, "H", torch.bfloat16)
+    N, d = H.shape
+    _dev(W, "W", torch.bfloat16, 2)
+    _dev(idx, "idx", torch.int32, 2)
+    _dev(t, "t", torch.float32, 2)
+    _dev(w, "w", torch.float32, 1)
+    _dev(lse, "lse", torch.float32, 1)
+    if (W.shape[1] != d or idx.shape[0] != N or t.shape != idx.shape or (w is not None and w.numel() != N)
+            or (lse is not None and lse.numel() != N)):
+        raise ValueError("W must be V x d, idx and t N x K; w and lse must have N entries")
+    return ldh, N, d, W.shape[0], idx.shape[1]
+
+
+def loca_head_distill(H, W, idx, t, loss, lse=None, w=None, tau=1.0, workspace=None, stream=None):
+    """Distillation from a teacher's top logits ``t`` (N x K float) at the words ``idx`` (N x K int32; outside
+    [0, V) = none) for hidden states ``H`` (N x d bf16, rows may be spaced) and the head ``W`` (V x d bf16), without
+    the student's logits in memory: ``loss = w tau^2 KL(softmax(t / tau) || softmax(H W^T / tau))`` and ``lse`` of
+    the scaled logits (N float each).  A position without a word is masked."""
+    ldh, N, d, V, K = _distill_args(H, W, idx, t, w, lse)
+    _dev(loss, "loss", torch.float32, 1)
+    if loss.numel() != N:
+        raise ValueError("loss must have N entries")
+    _same_device(H, W, idx, t, w, loss, lse)
+    nbytes = head_distill_workspace_size(N, V, d, K)
+    ws = _workspace(nbytes, H.device, workspace, stream)
+    rc = lib().loca_head_distill(_ptr(H), ldh, N, d, _ptr(W), V, _ptr(idx), _ptr(t), K, float(tau), _ptr(w), _ptr(loss),
+                                 _ptr(lse), _ptr(ws), nbytes, _stream(stream))
+    _check(rc, "loca_head_distill")
+
+
+def head_distill_backward_workspace_size(N, V, d, K, want_dH=True, want_dW=True) -> int:
+    return _size("loca_head_distill_backward_workspace_size", N, V, d, K, int(bool(want_dH)), int(bool(want_dW)))
+
+
+def loca_head_distill_backward(H, W, idx, t, lse, dH=None, dW=None, w=None, dloss=None, tau=1.0, grad_scale=1.0,
+                               workspace=None, stream=None):
+    """Gradients of ``grad_scale * sum_n dloss[n] * loss[n]`` of :func:`loca_head_distill` for the hidden states
+    (``dH``, N x d bf16, rows may be spaced) and the head (``dW``, V x d bf16); ``lse`` is the forward call's."""
+    ldh, N, d, V, K = _distill_args(H, W, idx, t, w, lse)
+    _dev(dloss, "dloss", torch.float32, 1)
+    lddh = 0 if dH is None else _rows2d(dH, "dH", torch.bfloat16, (N, d))
+    _dev(dW, "dW", torch.bfloat16, 2)
+    if (dloss is not None and dloss.numel() != N) or (dW is not None and tuple(dW.shape) != (V, d)):
+        raise ValueError("dW must be V x d and dloss must have N entries")
+    _same_device(H, W, idx, t, lse, dH, dW, w, dloss)
+    nbytes = head_distill_backward_workspace_size(N, V, d, K, dH is not None, dW is not None)
+    ws = _workspace(nbytes, H.device, workspace, stream)
+    rc = lib().loca_head_distill_backward(_ptr(H), ldh, N, d, _ptr(W), V, _ptr(idx), _ptr(t), K, float(tau), _ptr(w),
+                                          _ptr(lse), _ptr(dloss), float(grad_scale), _ptr(dH), lddh, _ptr(dW), _ptr(ws),
+                                          nbytes, _stream(stream))
+    _check(rc, "loca_head_distill_backward")
+
+
 class AdapterSet:
     """The device layout of ``n`` adapters of one projection: ``A`` (n x d_in x k) and ``B``
     (n x d_out x k), float32 or bfloat16, each with an optional ``scale`` (n float).  Call
@@ -875,14 +948,6 @@ def loca_adapter_backward(X, dY, W, adapters, plan, dX=None, dA=None, dB=None, w
                                      _ptr(adapters.packed), adapters.n, adapters.k, _ptr(plan.buf), _ptr(dX), lddx,
                                      _ptr(dA), _ptr(dB), _code(kind), _ptr(ws), nbytes, _stream(stream))
     _check(rc, "loca_adapter_backward")
-
-
-def _same_device(*tensors):
-    """The call runs on the current device: refuses tensors of another one."""
-    here = torch.cuda.current_device()
-    for t in tensors:
-        if t is not None and t.device.index != here:
-            raise ValueError(f"a tensor is on {t.device}, the current device is cuda:{here}")
 
 
 def gated_workspace_size(N, d, f) -> int:

@@ -72,3 +72,44 @@ def test_gated_codes(L):
         for inp in (0, 1, 2, 3):
             assert back(**{out: at(inp)}) == 1, (out, inp)
     assert back(dWu=at(5)) == 1 and back(dX=at(5)) == 1 and back(dX=at(6)) == 1
+
+
+def test_distill_sizes(L):
+    rc, n = _size(L.loca_head_distill_workspace_size, 4096, 151936, 5120, 64)
+    # the hidden states once, two pairs of floats per row and 256 columns, three words' worth per entry
+    assert rc == 0 and 4096 * 5120 * 2 < n < 4096 * 5120 * 2 + 16 * 4096 * 594 + 12 * 4096 * 64 + (1 << 20)
+    rc, b = _size(L.loca_head_distill_backward_workspace_size, 1 << 17, 151936, 5120, 64, 1, 0)
+    assert rc == 0 and b < (1 << 30) + (1 << 17) * (5120 * 2 + 64 * 8) + 32 * 8192 * 5120 * 4 + (1 << 22)
+    for bad in ((-1, 10, 64, 4), (4, 0, 64, 4), (4, 10, 60, 4), (4, 10, 64, 0), (4, 10, 64, 257), (1 << 25, 10, 64, 4)):
+        assert _size(L.loca_head_distill_workspace_size, *bad)[0] == 2, bad
+        assert _size(L.loca_head_distill_backward_workspace_size, *bad, 1, 1)[0] == 2, bad
+    assert L.loca_head_distill_workspace_size(4, 10, 64, 2, None) == 1
+
+
+def test_distill_codes(L):
+    f = ctypes.c_float
+
+    def fwd(H=at(0), ldh=64, N=4, d=64, W=at(1), V=10, idx=at(2), t=at(3), K=3, tau=1.0, w=None, loss=at(4), lse=at(5),
+            ws=at(6), n=BIG):
+        return L.loca_head_distill(H, ldh, N, d, W, V, idx, t, K, f(tau), w, loss, lse, ws, n, None)
+
+    assert fwd(N=0, H=None, W=None, idx=None, t=None, loss=None, ws=None, n=0) == 0  # nothing to do
+    assert fwd(N=-1) == 2 and fwd(V=0) == 2 and fwd(d=12) == 2 and fwd(K=0) == 2 and fwd(K=257) == 2
+    assert fwd(tau=0.0) == 1 and fwd(tau=float("nan")) == 1 and fwd(tau=float("inf")) == 1 and fwd(tau=-1.0) == 1
+    assert fwd(H=None) == 1 and fwd(W=None) == 1 and fwd(idx=None) == 1 and fwd(t=None) == 1 and fwd(loss=None) == 1
+    assert fwd(ldh=56) == 2 and fwd(ldh=68) == 3 and fwd(H=P(8)) == 3 and fwd(W=P(8)) == 3
+    assert fwd(idx=P(2)) == 3 and fwd(t=P(2)) == 3 and fwd(loss=P(2)) == 3 and fwd(lse=P(2)) == 3 and fwd(w=P(2)) == 3
+    assert fwd(ws=None) == 7 and fwd(n=16) == 7 and fwd(ws=P(16)) == 3
+
+    def back(H=at(0), ldh=64, N=4, d=64, W=at(1), V=10, idx=at(2), t=at(3), K=3, tau=1.0, w=None, lse=at(4), g=None, s=1.0,
+             dH=at(5), lddh=64, dW=at(6), ws=at(7), n=BIG):
+        return L.loca_head_distill_backward(H, ldh, N, d, W, V, idx, t, K, f(tau), w, lse, g, f(s), dH, lddh, dW, ws, n, None)
+
+    assert back(dH=None, dW=None) == 1 and back(lse=None) == 1 and back(H=None) == 1 and back(idx=None) == 1
+    assert back(N=0, H=None, W=None, idx=None, t=None, lse=None, dW=None, ws=None, n=0) == 0
+    assert back(s=float("nan")) == 1 and back(tau=0.0) == 1
+    assert back(lddh=56) == 2 and back(lddh=68) == 3 and back(dW=P(8)) == 3 and back(g=P(2)) == 3 and back(lse=P(2)) == 3
+    assert back(n=256) == 7
+    assert back(dH=at(0), ws=None) == 7  # over H itself: allowed
+    assert back(dH=P(at(0).value + 16)) == 1 and back(dW=at(0)) == 1 and back(dW=at(1)) == 1 and back(dH=at(1)) == 1
+    assert back(dH=at(6)) == 1
