@@ -600,6 +600,34 @@ int loca_adapter_backward(const void* X, int64_t ldx, const void* dY, int64_t ld
                           size_t workspace_bytes, void* stream);
 
 /*
+ * A frozen projection in 4 bits with group scales, for a few tokens, with each token's adapter beside it:
+ *
+ *   W[o, i] = s[o, i / group] (q[o, i] - z[o, i / group]),   Y = X W^T + s_a (X A_a) B_a^T
+ *
+ * codes   d_out x d_in / 2 bytes, row-major: q of an even i in the low four bits, of i + 1 in the high ones
+ * scales  d_out x d_in / group, LOCA_F32 or LOCA_BF16;  zeros  d_out x d_in / group bytes 0 .. 15 (the low four bits
+ *         count), or NULL for 8
+ * group   32, 64 or 128;  d_in a multiple of it, up to 65536;  1 <= d_out <= 2^24;  N <= 65535
+ * loca_q4_pack   lays codes, scales and zeros out for the kernel in `packed` (256-byte aligned,
+ *                loca_q4_packed_size bytes): once, the source arrays are not needed any more
+ * loca_q4_apply  Y (N x d_out bf16, row pitch ldy, 2-byte aligned) of X (N x d_in bf16, 16-byte aligned, row pitch a
+ *                multiple of 8).  group, scale_dtype and with_zeros as packed.  adapters: what loca_adapter_pack
+ *                packed of n adapters of rank k for d_out x d_in, with the tokens' plan (loca_adapter_plan),
+ *                and then d_out as loca_adapter_apply takes it; or NULL (plan NULL, n and k 0).  It reads the
+ *                weights once for up to 64 tokens, and again for every 64 more
+ * Arithmetic: q - z and X are exact in bf16, their products are summed in fp32 over up to 64 terms of a group and
+ * scaled in fp32: W is never rounded.  The low-rank term as in loca_adapter_apply, U in fp32.  Y is rounded
+ * once.  Deterministic.  Y may not overlap X (rows side by side in one buffer do not).
+ */
+int loca_q4_packed_size(int64_t d_out, int64_t d_in, int32_t group, int scale_dtype, int with_zeros, size_t* bytes);
+int loca_q4_pack(const void* codes, const void* scales, int scale_dtype, const void* zeros, int64_t d_out, int64_t d_in,
+                 int32_t group, void* packed, void* stream);
+int loca_q4_workspace_size(int64_t N, int64_t d_in, int64_t d_out, int32_t k, int32_t n, size_t* bytes);
+int loca_q4_apply(const void* X, int64_t ldx, int64_t N, int64_t d_in, const void* packed, int64_t d_out, int32_t group,
+                  int scale_dtype, int with_zeros, const void* adapters, int32_t n, int32_t k, const void* plan, void* Y,
+                  int64_t ldy, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
  * loca_gated — gated feed-forward of a block, both projections, the activation and the product in one launch;
  * loca_gated_backward — its gradients:
  *

@@ -1931,6 +1931,21 @@ cudaError_t launch_adapter_apply(const void* X, int64_t ldx, int64_t N, int64_t 
                         ldy);
 }
 
+size_t adapter_tokens_workspace_bytes(int64_t N, int64_t d_in, int k) {
+  return 256 + align256(4 * size_t(tok_ranges(N, d_in)) * size_t(N) * size_t(k_padded(k)));
+}
+cudaError_t launch_adapter_tokens(const void* X, int64_t ldx, int64_t N, int64_t d_in, int64_t d_out, const void* packed,
+                                  int n, int k, const void* plan, void* workspace, AdapterTokens* out, cudaStream_t s) {
+  const Call c = call_of(N, n, k, plan, workspace, nullptr, s);
+  const PackLay pk = pack_lay(n, d_in, d_out, k);
+  const uint8_t* pb = static_cast<const uint8_t*>(packed);
+  uint8_t* u = static_cast<uint8_t*>(workspace) + 256;
+  *out = AdapterTokens{reinterpret_cast<const float*>(u), reinterpret_cast<const __nv_bfloat16*>(pb + pk.b),
+                       c.plan + c.p.tok_adapter, c.kp, tok_ranges(N, d_in)};
+  return tokens(c, X, ldx, d_in, reinterpret_cast<const __nv_bfloat16*>(pb + pk.a),
+                reinterpret_cast<const int32_t*>(pb + pk.marks), u);
+}
+
 cudaError_t launch_adapter_backward(const void* X, int64_t ldx, const void* dY, int64_t lddy, int64_t N, int64_t d_in,
                                     const void* W, int64_t d_out, const void* packed, int n, int k, const void* plan,
                                     void* dX, int64_t lddx, void* dA, void* dB, int grad_dtype, void* workspace,

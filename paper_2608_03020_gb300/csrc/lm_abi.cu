@@ -104,6 +104,16 @@ int check_distill(int64_t N, int64_t V, int64_t d, int32_t K, float tau) {
   if (!(tau > 0.f) || !std::isfinite(tau)) return fail(LOCA_ERR_INVALID_ARG, "tau must be positive and finite");
   return LOCA_OK;
 }
+int check_q4(int64_t d_out, int64_t d_in, int32_t group, int scale_dtype) {
+  if (group != 32 && group != 64 && group != 128) return fail(LOCA_ERR_SHAPE, "group must be 32, 64 or 128, got %d", group);
+  if (d_in < group || d_in > 65536 || d_in % group != 0)
+    return fail(LOCA_ERR_SHAPE, "need d_in <= 65536, a multiple of group = %d, got %lld", group, (long long)d_in);
+  if (d_out < 1 || d_out > (int64_t(1) << 24))
+    return fail(LOCA_ERR_SHAPE, "need 1 <= d_out <= 2^24, got %lld", (long long)d_out);
+  if (scale_dtype != LOCA_F32 && scale_dtype != LOCA_BF16)
+    return fail(LOCA_ERR_UNSUPPORTED_DTYPE, "unknown dtype code %d", scale_dtype);
+  return LOCA_OK;
+}
 int check_act(int act) {
   if (act != LOCA_ACT_SILU && act != LOCA_ACT_GELU) return fail(LOCA_ERR_INVALID_ARG, "unknown activation code %d", act);
   return LOCA_OK;
@@ -381,6 +391,67 @@ int loca_adapter_backward(const void* X, int64_t ldx, const void* dY, int64_t ld
   const cudaError_t e = launch_adapter_backward(X, ldx, dY, lddy, N, d_in, W, d_out, packed, n, k, plan, dX, lddx, dA, dB,
                                                 grad_dtype, workspace, status, s);
   if (e != cudaSuccess) return cuda_fail(e, "loca_adapter_backward launch");
+  return LOCA_OK;
+}
+
+int loca_q4_packed_size(int64_t d_out, int64_t d_in, int32_t group, int scale_dtype, int with_zeros, size_t* bytes) {
+  clear();
+  if (!bytes) return fail(LOCA_ERR_INVALID_ARG, "bytes is NULL");
+  const int rc = check_q4(d_out, d_in, group, scale_dtype);
+  if (rc != LOCA_OK) return rc;
+  *bytes = q4_packed_bytes(d_out, d_in, group, scale_dtype, with_zeros != 0);
+  return LOCA_OK;
+}
+
+int loca_q4_pack(const void* codes, const void* scales, int scale_dtype, const void* zeros, int64_t d_out, int64_t d_in,
+                 int32_t group, void* packed, void* stream) {
+  clear();
+  const int rc = check_q4(d_out, d_in, group, scale_dtype);
+  if (rc != LOCA_OK) return rc;
+  if (!codes || !scales || !packed) return fail(LOCA_ERR_INVALID_ARG, "codes, scales and packed are required");
+  if (!aligned(scales, scale_dtype == LOCA_F32 ? 4 : 2) || !aligned(packed, 256))
+    return fail(LOCA_ERR_ALIGNMENT, "scales need the alignment of their elements, packed 256 bytes");
+  const cudaError_t e =
+      launch_q4_pack(codes, scales, scale_dtype, zeros, d_out, d_in, group, packed, static_cast<cudaStream_t>(stream));
+  if (e != cudaSuccess) return cuda_fail(e, "loca_q4_pack launch");
+  return LOCA_OK;
+}
+
+int loca_q4_workspace_size(int64_t N, int64_t d_in, int64_t d_out, int32_t k, int32_t n, size_t* bytes) {
+  clear();
+  if (!bytes) return fail(LOCA_ERR_INVALID_ARG, "bytes is NULL");
+  int rc = check_q4(d_out, d_in, 32, LOCA_F32);
+  if (rc != LOCA_OK) return rc;
+  if (N < 0 || N > 65535) return fail(LOCA_ERR_SHAPE, "need 0 <= N <= 65535, got %lld", (long long)N);
+  *bytes = 0;
+  if (n == 0 && k == 0) return LOCA_OK;
+  rc = check_adapter(N, d_in, d_out, k, n);
+  if (rc != LOCA_OK) return rc;
+  *bytes = N > 0 ? adapter_tokens_workspace_bytes(N, d_in, k) : 0;
+  return LOCA_OK;
+}
+
+int loca_q4_apply(const void* X, int64_t ldx, int64_t N, int64_t d_in, const void* packed, int64_t d_out, int32_t group,
+                  int scale_dtype, int with_zeros, const void* adapters, int32_t n, int32_t k, const void* plan, void* Y,
+                  int64_t ldy, void* workspace, size_t workspace_bytes, void* stream) {
+  clear();
+  int rc = check_q4(d_out, d_in, group, scale_dtype);
+  if (rc != LOCA_OK) return rc;
+  if (N < 0 || N > 65535) return fail(LOCA_ERR_SHAPE, "need 0 <= N <= 65535, got %lld", (long long)N);
+  if (!adapters != !plan || (!adapters && (n != 0 || k != 0)))
+    return fail(LOCA_ERR_INVALID_ARG, "adapters and plan come together, or neither, with n and k 0");
+  if (adapters && (rc = check_adapter(N, d_in, d_out, k, n)) != LOCA_OK) return rc;
+  if (N == 0) return LOCA_OK;
+  if (!X || !packed || !Y) return fail(LOCA_ERR_INVALID_ARG, "X, packed and Y are required");
+  if ((rc = check_rows(X, ldx, d_in, "X")) != LOCA_OK) return rc;
+  if (ldy < d_out) return fail(LOCA_ERR_SHAPE, "row pitch of Y %lld is below its %lld columns", (long long)ldy, (long long)d_out);
+  if (!aligned(Y, 2) || !aligned(packed, 256) || !aligned(adapters, 256) || !aligned(plan, 256))
+    return fail(LOCA_ERR_ALIGNMENT, "Y needs 2-byte, packed, adapters and plan 256-byte alignment");
+  if (adapters && (rc = check_ws(workspace, workspace_bytes, adapter_tokens_workspace_bytes(N, d_in, k))) != LOCA_OK) return rc;
+  if (overlap(Matrix{X, N, ldx, d_in}, Matrix{Y, N, ldy, d_out})) return fail(LOCA_ERR_INVALID_ARG, "Y must not overlap X");
+  const cudaError_t e = launch_q4_apply(X, ldx, N, d_in, packed, d_out, group, scale_dtype, with_zeros != 0, adapters, n, k,
+                                        plan, Y, ldy, workspace, static_cast<cudaStream_t>(stream));
+  if (e != cudaSuccess) return cuda_fail(e, "loca_q4_apply launch");
   return LOCA_OK;
 }
 

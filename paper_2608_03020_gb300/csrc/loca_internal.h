@@ -2,6 +2,7 @@
 #pragma once
 
 #include <cuda.h>
+#include <cuda_bf16.h>
 #include <cuda_runtime.h>
 #include <stddef.h>
 #include <stdint.h>
@@ -196,6 +197,26 @@ cudaError_t launch_adapter_backward(const void* X, int64_t ldx, const void* dY, 
                                     const void* W, int64_t d_out, const void* packed, int n, int k, const void* plan,
                                     void* dX, int64_t lddx, void* dA, void* dB, int grad_dtype, void* workspace,
                                     int32_t* status, cudaStream_t s);
+
+// U of single tokens: partial sums, ranges x N x kp fp32 (not written for a token without an adapter), what
+// multiplies them (adapter x d_out x kp bf16) and each token's adapter (-1: none).
+struct AdapterTokens {
+  const float* U;
+  const __nv_bfloat16* B;
+  const int32_t* tok_adapter;
+  int kp, ranges;
+};
+size_t adapter_tokens_workspace_bytes(int64_t N, int64_t d_in, int k);
+cudaError_t launch_adapter_tokens(const void* X, int64_t ldx, int64_t N, int64_t d_in, int64_t d_out, const void* packed,
+                                  int n, int k, const void* plan, void* workspace, AdapterTokens* out, cudaStream_t s);
+
+// ---- 4-bit projection (q4.cu)
+size_t q4_packed_bytes(int64_t o, int64_t d, int group, int scale_dtype, bool zeros);
+cudaError_t launch_q4_pack(const void* codes, const void* scales, int scale_dtype, const void* zeros, int64_t o, int64_t d,
+                           int group, void* packed, cudaStream_t s);
+cudaError_t launch_q4_apply(const void* X, int64_t ldx, int64_t N, int64_t d, const void* packed, int64_t o, int group,
+                            int scale_dtype, bool zeros, const void* adapters, int n, int k, const void* plan, void* Y,
+                            int64_t ldy, void* workspace, cudaStream_t s);
 
 // ---- gated feed-forward (gated.cu)
 size_t gated_workspace_bytes();

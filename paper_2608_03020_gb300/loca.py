@@ -109,6 +109,11 @@ SIGNATURES = [
      [_P, _I64, _I64, _I64, _P, _I64, _P, _I32, _I32, _P, _P, _I64, _P, _SZ, _P]),
     ("loca_adapter_backward", ctypes.c_int,
      [_P, _I64, _P, _I64, _I64, _I64, _P, _I64, _P, _I32, _I32, _P, _P, _I64, _P, _P, ctypes.c_int, _P, _SZ, _P]),
+    ("loca_q4_packed_size", ctypes.c_int, [_I64, _I64, _I32, ctypes.c_int, ctypes.c_int, ctypes.POINTER(_SZ)]),
+    ("loca_q4_pack", ctypes.c_int, [_P, _P, ctypes.c_int, _P, _I64, _I64, _I32, _P, _P]),
+    ("loca_q4_workspace_size", ctypes.c_int, [_I64, _I64, _I64, _I32, _I32, ctypes.POINTER(_SZ)]),
+    ("loca_q4_apply", ctypes.c_int,
+     [_P, _I64, _I64, _I64, _P, _I64, _I32, ctypes.c_int, ctypes.c_int, _P, _I32, _I32, _P, _P, _I64, _P, _SZ, _P]),
     ("loca_gated_workspace_size", ctypes.c_int, [_I64, _I64, _I64, ctypes.POINTER(_SZ)]),
     ("loca_gated", ctypes.c_int,
      [_P, _I64, _I64, _I64, _P, _P, _I64, ctypes.c_int, _P, _I64, _P, _SZ, _P]),
@@ -948,6 +953,71 @@ def loca_adapter_backward(X, dY, W, adapters, plan, dX=None, dA=None, dB=None, w
                                      _ptr(adapters.packed), adapters.n, adapters.k, _ptr(plan.buf), _ptr(dX), lddx,
                                      _ptr(dA), _ptr(dB), _code(kind), _ptr(ws), nbytes, _stream(stream))
     _check(rc, "loca_adapter_backward")
+
+
+class Q4Weight:
+    """The device layout of a frozen projection in 4 bits: ``codes`` (d_out x d_in / 2 uint8, the even column in
+    the low four bits), ``scales`` (d_out x d_in / group, float32 or bfloat16; group 32, 64 or 128) and optional
+    ``zeros`` (like scales, uint8 0 .. 15; default 8), ``W = scale (code - zero)``.  Packs at once; the arguments are
+    not needed afterwards."""
+
+    def __init__(self, codes, scales, zeros=None, stream=None):
+        _dev(codes, "codes", torch.uint8, 2)
+        _dev(scales, "scales", (torch.float32, torch.bfloat16), 2)
+        _dev(zeros, "zeros", torch.uint8, 2)
+        if codes is None or scales is None:
+            raise TypeError("codes and scales must be CUDA tensors")
+        d_out, d_in = codes.shape[0], 2 * codes.shape[1]
+        groups = scales.shape[1]
+        if scales.shape[0] != d_out or groups < 1 or d_in % groups != 0:
+            raise ValueError(f"scales must be {d_out} x (columns / group), got {tuple(scales.shape)} for {d_in} columns")
+        if zeros is not None and zeros.shape != scales.shape:
+            raise ValueError("zeros must have the shape of scales")
+        _same_device(codes, scales, zeros)
+        self.d_out, self.d_in, self.group = d_out, d_in, d_in // groups
+        self.scale_code, self.with_zeros = _code(scales.dtype), zeros is not None
+        out = ctypes.c_size_t(0)
+        _check(lib().loca_q4_packed_size(d_out, d_in, self.group, self.scale_code, int(self.with_zeros), ctypes.byref(out)),
+               "loca_q4_packed_size")
+        self.packed = _empty(out.value, codes.device, stream)
+        rc = lib().loca_q4_pack(_ptr(codes), _ptr(scales), self.scale_code, _ptr(zeros), d_out, d_in, self.group,
+                                _ptr(self.packed), _stream(stream))
+        _check(rc, "loca_q4_pack")
+
+
+def q4_workspace_size(N, d_in, d_out, k=0, n=0) -> int:
+    return _size("loca_q4_workspace_size", N, d_in, d_out, k, n)
+
+
+def loca_q4_apply(X, weight, Y, adapters=None, plan=None, workspace=None, stream=None):
+    """``Y = X W^T + s_a (X A_a) B_a^T`` for a few tokens with a 4-bit ``weight`` (a :class:`Q4Weight`): ``X`` N x d_in
+    and ``Y`` N x d_out bf16 (rows may be spaced); ``adapters`` (an :class:`AdapterSet`) and ``plan`` (an
+    :class:`AdapterPlan` of the tokens' adapters), or neither."""
+    ldx = _rows2d(X, "X", torch.bfloat16)
+    N, d_in = X.shape
+    if d_in != weight.d_in:
+        raise ValueError(f"the weight has {weight.d_in} columns, X {d_in}")
+    ldy = _rows2d(Y, "Y", torch.bfloat16, (N, weight.d_out))
+    if (adapters is None) != (plan is None):
+        raise ValueError("adapters and plan come together")
+    n = k = 0
+    if adapters is not None:
+        n, k = adapters.n, adapters.k
+        if (adapters.d_in, adapters.d_out) != (d_in, weight.d_out):
+            raise ValueError(f"the adapters are for a {adapters.d_out} x {adapters.d_in} projection")
+        if plan.N != N or plan.n != n:
+            raise ValueError(f"the plan is for {plan.N} tokens and {plan.n} adapters, got {N} and {n}")
+    kept = [weight.packed] + ([] if adapters is None else [adapters.packed, plan.buf])
+    _same_device(X, Y, *kept)
+    if stream is not None:  # their memory outlives them until this call is done
+        for t in kept:
+            t.record_stream(_torch_stream(stream))
+    nbytes = q4_workspace_size(N, d_in, weight.d_out, k, n)
+    ws = _workspace(nbytes, X.device, workspace, stream)
+    rc = lib().loca_q4_apply(_ptr(X), ldx, N, d_in, _ptr(weight.packed), weight.d_out, weight.group, weight.scale_code,
+                             int(weight.with_zeros), None if adapters is None else _ptr(adapters.packed), n, k,
+                             None if plan is None else _ptr(plan.buf), _ptr(Y), ldy, _ptr(ws), nbytes, _stream(stream))
+    _check(rc, "loca_q4_apply")
 
 
 def gated_workspace_size(N, d, f) -> int:

@@ -113,3 +113,44 @@ def test_distill_codes(L):
     assert back(dH=at(0), ws=None) == 7  # over H itself: allowed
     assert back(dH=P(at(0).value + 16)) == 1 and back(dW=at(0)) == 1 and back(dW=at(1)) == 1 and back(dH=at(1)) == 1
     assert back(dH=at(6)) == 1
+
+
+def test_q4_sizes(L):
+    rc, n = _size(L.loca_q4_packed_size, 20480, 5120, 64, 1, 1)
+    # four bits a code, a scale and half a byte of zero for each group
+    want = 20480 * 5120 // 2 + 20480 * 80 * 2 + 20480 * 80 // 2
+    assert rc == 0 and want <= n <= want + 1024
+    assert _size(L.loca_q4_packed_size, 20480, 5120, 64, 0, 0)[1] > n
+    for bad in ((0, 64, 32), (64, 0, 32), (64, 48, 32), (64, 64, 16), (64, 64, 128), (64, 65568, 32), ((1 << 24) + 1, 64, 32)):
+        assert _size(L.loca_q4_packed_size, *bad, 0, 0)[0] == 2, bad
+    assert _size(L.loca_q4_packed_size, 64, 64, 32, 3, 0)[0] == 4
+    assert _size(L.loca_q4_workspace_size, 64, 5120, 20480, 0, 0) == (0, 0)
+    rc, n = _size(L.loca_q4_workspace_size, 64, 5120, 20480, 16, 4)
+    assert rc == 0 and n >= 64 * 16 * 4
+    assert _size(L.loca_q4_workspace_size, 64, 5120, 20481, 16, 4)[0] == 2  # adapters want multiples of 8
+    assert _size(L.loca_q4_workspace_size, 65536, 5120, 20480, 0, 0)[0] == 2
+    assert _size(L.loca_q4_workspace_size, 64, 5120, 20480, 65, 4)[0] == 2
+    assert L.loca_q4_packed_size(64, 64, 32, 0, 0, None) == 1 and L.loca_q4_workspace_size(4, 64, 64, 0, 0, None) == 1
+
+
+def test_q4_codes(L):
+    def pack(codes=at(0), scales=at(1), t=0, zeros=None, o=72, d=64, group=32, to=at(2)):
+        return L.loca_q4_pack(codes, scales, t, zeros, o, d, group, to, None)
+
+    assert pack(codes=None) == 1 and pack(scales=None) == 1 and pack(to=None) == 1
+    assert pack(t=2) == 4 and pack(group=48) == 2 and pack(d=96, group=64) == 2 and pack(o=0) == 2
+    assert pack(scales=P(2)) == 3 and pack(scales=P(1), t=1) == 3 and pack(to=P(16)) == 3
+
+    def run(X=at(0), ldx=64, N=4, d=64, w=at(1), o=72, group=32, t=0, z=0, ad=at(2), n=2, k=4, plan=at(3), Y=at(4), ldy=72,
+            ws=at(5), nb=BIG):
+        return L.loca_q4_apply(X, ldx, N, d, w, o, group, t, z, ad, n, k, plan, Y, ldy, ws, nb, None)
+
+    assert run(N=0, X=None, w=None, Y=None, ws=None, nb=0) == 0  # nothing to do
+    assert run(N=-1) == 2 and run(N=65536) == 2 and run(group=16) == 2 and run(t=5) == 4 and run(d=80, ldx=80) == 2
+    assert run(ad=None) == 1 and run(plan=None) == 1 and run(ad=None, plan=None) == 1 and run(ad=None, plan=None, n=0) == 1
+    assert run(o=73, ldy=80) == 2 and run(k=65) == 2 and run(n=0) == 2  # adapters' own limits
+    assert run(X=None) == 1 and run(w=None) == 1 and run(Y=None) == 1
+    assert run(ldx=56) == 2 and run(ldx=68) == 3 and run(ldy=71) == 2 and run(X=P(8)) == 3 and run(Y=P(1)) == 3
+    assert run(w=P(16)) == 3 and run(ad=P(16)) == 3 and run(plan=P(16)) == 3
+    assert run(ws=None) == 7 and run(nb=16) == 7
+    assert run(Y=at(0)) == 1
