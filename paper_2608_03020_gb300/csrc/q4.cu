@@ -8,12 +8,18 @@
 // shift and mask and one subtraction for two of them; tcgen05 would want the 16-bit operand written to
 // shared memory first, four bytes for each byte read, and its 128 rows of tokens filled to an eighth).
 //
-//   k_q4_pack   codes in the order of the MMAs' fragments: a warp's load of 512 bytes is 16 rows x 64 k, of
-//               which each lane gets what it multiplies; the order of k within 64 is chosen so that a lane's
-//               part of X is two runs of 16 bytes and that 32 k of one group stay together
-//   k_q4        a warp takes 16 or 32 rows and every ks-th 64 k; ks warps' sums meet in shared memory, in order,
-//               with the low-rank term of each token's adapter (U in fp32 from k_adapter_tokens); one rounding
-// Bound: the read of the codes and scales.
+//   k_q4_pack   codes in the order of the MMAs' fragments: 512 bytes are 16 rows x 64 k, of which each lane's 16
+//               are what it multiplies; the order of k within 64 is chosen so that a lane's part of X is two runs
+//               of 16 bytes and that 32 k of one group stay together.  Rows and k are padded to 32 and 128
+//   k_q4        a warp takes 16 rows and a range of k in spans of 128, three of which are on the way to its part of
+//               shared memory (each lane copies and reads its own 16 bytes, so that it waits for nothing else);
+//               ks warps' sums meet in shared memory, in order, with the low-rank term of each token's adapter
+//               (U in fp32 from k_adapter_tokens); one rounding
+// Bound: up to 16 tokens the instructions that make operands of codes (a span takes 44 of some 75 for 64 of its k;
+// 58 to 70 % of the issue slots and of the integer pipe), next to the read of the codes and scales; above, X's way
+// from L2 for every 16 rows, and the legacy MMAs' rate (1024 products a cycle and SM).  One token at
+// 28672 x 8192 30.9 us (3.9 TB/s), 3 tokens at 151931 x 2048 with groups of 32 51 us (3.9 TB/s), 8 tokens at
+// 20480 x 5120 20 us (2.9 TB/s), 16, 32 and 64 tokens at 14336 x 3584 14.8, 23 and 43 us.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
@@ -26,7 +32,6 @@ using namespace tc;
 
 constexpr int kThreads = 256;
 constexpr int kWarps = kThreads / 32;
-constexpr int kAhead = 4;    // chunks of 64 k that a warp has on the way
 constexpr int kMaxSmem = 98304;
 
 __host__ __device__ inline int64_t div_up(int64_t a, int64_t b) { return (a + b - 1) / b; }
@@ -40,8 +45,8 @@ __host__ __device__ inline size_t up256(size_t n) { return (n + 255) & ~size_t(2
 PackLay pack_lay(int64_t o, int64_t d, int group, int dtype, bool zeros) {
   PackLay p{};
   p.tiles = div_up(o, 32) * 2;
-  p.chunks = div_up(d, 64);
-  p.groups = d / group;
+  p.chunks = div_up(d, 128) * 2;
+  p.groups = p.chunks * 64 / group;  // (those behind the last have scales of 0)
   p.scales = up256(size_t(p.tiles) * size_t(p.chunks) * 512);
   p.zeros = p.scales + up256(size_t(p.tiles) * size_t(p.groups) * 16 * (dtype == LOCA_F32 ? 4 : 2));
   p.total = p.zeros + (zeros ? up256(size_t(p.tiles) * size_t(p.groups) * 8) : 0);
@@ -84,8 +89,8 @@ __global__ void __launch_bounds__(256)
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       const int64_t row = tile * 16 + g + 8 * h;
-      const int64_t at = row * p.groups + q;
-      const bool in = row < o;
+      const int64_t at = row * (d / group) + q;
+      const bool in = row < o && q < d / group;
       if (f32)
         reinterpret_cast<float*>(packed + p.scales)[2 * i + h] = in ? static_cast<const float*>(scales)[at] : 0.f;
       else
@@ -104,8 +109,8 @@ struct Q4Geo {
   int shift;             // log2(group)
   int64_t o, d;
   int64_t tiles;
-  int chunks, groups;
-  int ks;                // warps that share rows
+  int spans, groups;
+  int ks, per_warp;      // warps that share rows, their spans
   int row_blocks;        // blocks of rows
   const __nv_bfloat16* X;
   int64_t ldx, N;
@@ -130,121 +135,205 @@ __device__ __forceinline__ uint32_t two_codes(uint32_t w, __nv_bfloat162 zero) {
   return *reinterpret_cast<const uint32_t*>(&v);
 }
 
-template <int NT, int MT>
-__global__ void __launch_bounds__(kThreads) k_q4(const __grid_constant__ Q4Geo g) {
+// Blocks of a SM (registers decide).
+constexpr int resident(int nt) { return nt == 1 ? 3 : nt <= 4 ? 2 : 1; }
+constexpr int kMetaBytes = 32 * 8 + 32;  // of four groups: 32 pairs of scales, 32 bytes of zeros
+// A warp's shared memory: four spans of 128 k on the way, the scales and zeros of two rounds of four spans.
+__host__ __device__ constexpr int warp_bytes(int groups) { return 4 * 1024 + 2 * groups * kMetaBytes; }
+
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ void copy8(uint32_t dst, const void* src) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ void copy4(uint32_t dst, const void* src) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int kLeft>
+__device__ __forceinline__ void copy_wait() {
+  asm volatile("cp.async.wait_group %0;" ::"n"(kLeft) : "memory");
+}
+
+// kGroups: of 128 k (1, 2 or 4).
+template <int NT, int kGroups>
+__global__ void __launch_bounds__(kThreads, resident(NT)) k_q4(const __grid_constant__ Q4Geo g) {
   extern __shared__ float smem[];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int gr = lane >> 2, t = lane & 3;
   const int rb = int(blockIdx.x) % g.row_blocks;
-  const int64_t n0 = int64_t(int(blockIdx.x) / g.row_blocks) * (8 * NT);
-  const int per_block = kWarps / g.ks;  // row groups of a block
+  const int n0 = int(blockIdx.x) / g.row_blocks * (8 * NT);
+  const int per_block = kWarps / g.ks;  // tiles of a block
   const int kw = warp % g.ks;
-  const int64_t tile0 = (int64_t(rb) * per_block + warp / g.ks) * MT;
-  constexpr int R = 16 * MT, T = 8 * NT;
+  const int64_t tile = int64_t(rb) * per_block + warp / g.ks;
+  constexpr int R = 16, T = 8 * NT;
   // With adapters the launch before is k_adapter_tokens, which let this one start only after all launches before
   // it had completed: what it writes is needed at the end.
   if (!g.low.U) wait_for_previous();
   launch_dependents();
-  float acc[MT][NT][4];
+  float acc[NT][4];
 #pragma unroll
-  for (int m = 0; m < MT; ++m)
+  for (int n = 0; n < NT; ++n)
 #pragma unroll
-    for (int n = 0; n < NT; ++n)
+    for (int e = 0; e < 4; ++e) acc[n][e] = 0.f;
+  const int tokens = int(g.N) - n0 < T ? int(g.N) - n0 : T;
+  const int rows = per_block * R;
+  const int64_t row0 = int64_t(rb) * rows;
+  // the adapters' rows that this thread multiplies at the end, to L2 meanwhile
+  auto prefetch_rows = [&]() {
+    for (int i = threadIdx.x; i < rows * tokens; i += kThreads) {
+      const int n = i / rows, r = i - n * rows;
+      const int a = g.low.tok_adapter[n0 + n];
+      if (a >= 0 && row0 + r < g.o)
+        asm volatile("prefetch.global.L2 [%0];" ::"l"(g.low.B + (int64_t(a) * g.o + row0 + r) * g.low.kp));
+    }
+  };
+  const int c0 = kw * g.per_warp, c1 = c0 + g.per_warp < g.spans ? c0 + g.per_warp : g.spans;
+  if (tile < g.tiles && c0 < c1) {
+    uint8_t* mine = reinterpret_cast<uint8_t*>(smem) + warp * warp_bytes(kGroups);
+    const uint8_t* slots = mine + lane * 16;  // span i of a round: at 1024 i, in two halves
+    const uint32_t slots_s = smem_u32(slots), metas_s = smem_u32(mine) + 4096;
+    const uint8_t* metas = mine + 4096;
+    const uint4* codes = g.codes + (tile * g.spans + c0) * 64 + lane;
+    // scales and zeros of the four spans from c on, into half `to` of theirs
+    const int meta_end = g.groups * 8;  // pairs of rows and groups of a tile
+    auto fetch_meta = [&](int c, uint32_t to) {
+      if (c >= c1) return;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) acc[m][n][i] = 0.f;
-  if (tile0 < g.tiles) {
-    const uint4* codes = g.codes + tile0 * g.chunks * 32 + lane;
-    const __nv_bfloat16* x = g.X + (n0 + gr) * g.ldx + 8 * t;
-    for (int c0 = kw; c0 < g.chunks; c0 += kAhead * g.ks) {
-      uint4 w[kAhead][MT];
-#pragma unroll
-      for (int j = 0; j < kAhead; ++j) {
-        const int c = c0 + j * g.ks;
-#pragma unroll
-        for (int m = 0; m < MT; ++m)
-          w[j][m] = c < g.chunks && LOCA_CHECK((tile0 + m) * g.chunks + c, g.tiles * g.chunks)
-                        ? __ldg(codes + (int64_t(m) * g.chunks + c) * 32)
-                        : make_uint4(0, 0, 0, 0);
-      }
-#pragma unroll
-      for (int j = 0; j < kAhead; ++j) {
-        const int c = c0 + j * g.ks;
-        if (c >= g.chunks) break;
-        const bool second = 64 * c + 32 < g.d;  // (a last half chunk, with groups of 32)
-        uint4 xv[NT][2];
-#pragma unroll
-        for (int n = 0; n < NT; ++n) {
-          const bool in = n0 + 8 * n + gr < g.N && LOCA_CHECK_SPAN(64 * c + 8 * t + (second ? 32 : 0), 8, g.d);
-          const uint4* p = reinterpret_cast<const uint4*>(x + 8 * n * g.ldx + 64 * c);
-          xv[n][0] = in ? __ldg(p) : make_uint4(0, 0, 0, 0);
-          xv[n][1] = in && second ? __ldg(p + 4) : make_uint4(0, 0, 0, 0);
+      for (int i = 0; i < kGroups; ++i) {
+        const int e = (c * kGroups + 4 * i) * 8;
+        const int64_t at = tile * meta_end + e;
+        const uint32_t dst = metas_s + to + uint32_t(i * kMetaBytes);
+        if (e + lane < meta_end && LOCA_CHECK(at + lane, g.tiles * meta_end)) {
+          if (g.f32) copy8(dst + lane * 8, g.scales + (at + lane) * 8);
+          else copy4(dst + lane * 8, g.scales + (at + lane) * 4);
         }
-        const int q0 = (64 * c) >> g.shift, q1 = second ? (64 * c + 32) >> g.shift : q0;
+        if (g.zeros && lane < 8 && e + 4 * lane < meta_end) copy4(dst + 256 + lane * 4, g.zeros + at + 4 * lane);
+      }
+    };
+    // span i of this round (i >= 4: of the next) where it is there
+    auto fetch = [&](int i, int left) {
+      if (i < left && LOCA_CHECK(codes + i * 64 - g.codes, g.tiles * g.spans * 64)) {
+        copy16(slots_s + uint32_t((i & 3) * 1024), codes + i * 64);
+        copy16(slots_s + uint32_t((i & 3) * 1024 + 512), codes + i * 64 + 32);
+      }
+      copy_commit();
+    };
+    fetch_meta(c0, 0);
 #pragma unroll
-        for (int m = 0; m < MT; ++m) {
-          float part[NT][4];
+    for (int i = 0; i < 3; ++i) fetch(i, c1 - c0);
+    if (g.low.U) prefetch_rows();
+    // (columns of tokens that are not there hold the last token's and are not stored)
+    const __nv_bfloat16* x[NT];
 #pragma unroll
-          for (int half = 0; half < 2; ++half) {
-            const int64_t at = ((tile0 + m) * g.groups + (half ? q1 : q0)) * 8 + gr;
-            uint32_t z = 0x88u;
-            if (!LOCA_CHECK(at, g.tiles * g.groups * 8)) continue;
-            if (g.zeros) z = __ldg(g.zeros + at);
-            const uint32_t z0 = (z & 15u) | 0x4300u, z1 = (z >> 4) | 0x4300u;
-            const uint32_t zz0 = z0 | z0 << 16, zz1 = z1 | z1 << 16;
-            const __nv_bfloat162 zero0 = *reinterpret_cast<const __nv_bfloat162*>(&zz0);
-            const __nv_bfloat162 zero1 = *reinterpret_cast<const __nv_bfloat162*>(&zz1);
-            if (half == 0 || q1 != q0) {
+    for (int n = 0; n < NT; ++n) {
+      const int tok = n0 + 8 * n + gr < int(g.N) ? n0 + 8 * n + gr : int(g.N) - 1;
+      x[n] = g.X + int64_t(tok) * g.ldx + 128 * c0 + 8 * t;
+    }
+    uint32_t half = 0;
+    for (int left = c1 - c0, k_left = int(g.d) - 128 * c0; left > 0; left -= 4, k_left -= 512) {
 #pragma unroll
-              for (int n = 0; n < NT; ++n)
+      for (int i = 0; i < 4; ++i) {
+        if (i >= left) break;
+        copy_wait<2>();
+        if (i == 0) {
+          __syncwarp();  // the round's scales and zeros are everyone's, and those of the last round have been read
+          fetch_meta(c1 - left + 4, half ^ uint32_t(kGroups * kMetaBytes));
+        }
+        const uint4 w[2] = {*reinterpret_cast<const uint4*>(slots + i * 1024),
+                            *reinterpret_cast<const uint4*>(slots + i * 1024 + 512)};
+        fetch(i + 3, left);
+        // X: the whole span where it fits in registers, else 32 k at a time, 32 ahead
+        constexpr int kQ = NT <= 2 ? 4 : 2;
+        uint4 xv[kQ][NT];
+        auto load_x = [&](int q, bool full) {
 #pragma unroll
-                for (int i = 0; i < 4; ++i) part[n][i] = 0.f;
+          for (int n = 0; n < NT; ++n)
+            xv[q & (kQ - 1)][n] = full || 128 * i + 32 * q < k_left ? __ldg(reinterpret_cast<const uint4*>(x[n] + 128 * i) + 4 * q)
+                                                                    : make_uint4(0, 0, 0, 0);
+        };
+        const bool full = 128 * (i + 1) <= k_left;  // (else the last span of rows that are no multiple of 128)
+        if (kQ == 4) {
+          if (full) {
+#pragma unroll
+            for (int q = 0; q < 4; ++q) load_x(q, true);
+          } else {
+#pragma unroll
+            for (int q = 0; q < 4; ++q) load_x(q, false);
+          }
+        } else {
+          load_x(0, false);
+        }
+        float part[NT][4];
+        float s0 = 0.f, s1 = 0.f;
+        __nv_bfloat162 zero0, zero1;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {  // 32 k
+          if (kQ == 2 && q < 3) load_x(q + 1, false);
+          if (q % (4 / kGroups) == 0) {
+            const int group = i * kGroups + q * kGroups / 4;  // of the round
+            const uint8_t* meta = metas + half + (group >> 2) * kMetaBytes;
+            const int e = (group & 3) * 8 + gr;
+            if (g.f32) {
+              const float2 s = *reinterpret_cast<const float2*>(meta + e * 8);
+              s0 = s.x;
+              s1 = s.y;
+            } else {
+              const uint32_t s = *reinterpret_cast<const uint32_t*>(meta + e * 8);
+              s0 = __uint_as_float(s << 16);
+              s1 = __uint_as_float(s & 0xffff0000u);
             }
-#pragma unroll
-            for (int s = 0; s < 2; ++s) {
-              const uint32_t word = reinterpret_cast<const uint32_t*>(&w[j][m])[2 * half + s];
-              const uint32_t a[4] = {two_codes<0>(word, zero0), two_codes<4>(word, zero1), two_codes<8>(word, zero0),
-                                     two_codes<12>(word, zero1)};
-#pragma unroll
-              for (int n = 0; n < NT; ++n) {
-                const uint32_t* b = reinterpret_cast<const uint32_t*>(&xv[n][half]) + 2 * s;
-                mma_16816(part[n], a, b[0], b[1]);
-              }
+            uint32_t z0 = 0x43084308u, z1 = 0x43084308u;
+            if (g.zeros) {
+              const uint32_t z = meta[256 + e];
+              z0 = (z & 15u) * 0x10001u + 0x43004300u;
+              z1 = (z >> 4) * 0x10001u + 0x43004300u;
             }
-            if (half == 1 || q1 != q0) {
-              float s0, s1;
-              if (g.f32) {
-                const float2 s = __ldg(reinterpret_cast<const float2*>(g.scales) + at);
-                s0 = s.x;
-                s1 = s.y;
-              } else {
-                const uint32_t s = __ldg(reinterpret_cast<const uint32_t*>(g.scales) + at);
-                s0 = __uint_as_float(s << 16);
-                s1 = __uint_as_float(s & 0xffff0000u);
-              }
+            zero0 = *reinterpret_cast<const __nv_bfloat162*>(&z0);
+            zero1 = *reinterpret_cast<const __nv_bfloat162*>(&z1);
 #pragma unroll
-              for (int n = 0; n < NT; ++n) {
-                acc[m][n][0] = fmaf(s0, part[n][0], acc[m][n][0]);
-                acc[m][n][1] = fmaf(s0, part[n][1], acc[m][n][1]);
-                acc[m][n][2] = fmaf(s1, part[n][2], acc[m][n][2]);
-                acc[m][n][3] = fmaf(s1, part[n][3], acc[m][n][3]);
-              }
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+              for (int f = 0; f < 4; ++f) part[n][f] = 0.f;
+          }
+#pragma unroll
+          for (int s = 0; s < 2; ++s) {  // 16 k
+            const uint32_t word = reinterpret_cast<const uint32_t*>(&w[q >> 1])[2 * (q & 1) + s];
+            const uint32_t a[4] = {two_codes<0>(word, zero0), two_codes<4>(word, zero1), two_codes<8>(word, zero0),
+                                   two_codes<12>(word, zero1)};
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+              const uint32_t* b = reinterpret_cast<const uint32_t*>(&xv[q & (kQ - 1)][n]) + 2 * s;
+              mma_16816(part[n], a, b[0], b[1]);
+            }
+          }
+          if ((q + 1) % (4 / kGroups) == 0) {
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+              acc[n][0] = fmaf(s0, part[n][0], acc[n][0]);
+              acc[n][1] = fmaf(s0, part[n][1], acc[n][1]);
+              acc[n][2] = fmaf(s1, part[n][2], acc[n][2]);
+              acc[n][3] = fmaf(s1, part[n][3], acc[n][3]);
             }
           }
         }
       }
+      codes += 256;
+      half ^= uint32_t(kGroups * kMetaBytes);
+#pragma unroll
+      for (int n = 0; n < NT; ++n) x[n] += 512;
     }
+    copy_wait<0>();
   }
+  __syncthreads();  // the sums take the rings' place
   if (g.low.U) wait_for_previous();
   // sums of the warps: [warp][token][row]
 #pragma unroll
-  for (int m = 0; m < MT; ++m)
+  for (int n = 0; n < NT; ++n)
 #pragma unroll
-    for (int n = 0; n < NT; ++n)
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-        smem[(warp * T + 8 * n + 2 * t + (i & 1)) * R + 16 * m + gr + 8 * (i >> 1)] = acc[m][n][i];
+    for (int i = 0; i < 4; ++i) smem[(warp * T + 8 * n + 2 * t + (i & 1)) * R + gr + 8 * (i >> 1)] = acc[n][i];
   float* u = smem + kWarps * T * R;
-  const int tokens = g.N - n0 < T ? int(g.N - n0) : T;
   if (g.low.U)
     for (int i = threadIdx.x; i < tokens * g.low.kp; i += kThreads) {
       const int n = i / g.low.kp, r = i - n * g.low.kp;
@@ -254,8 +343,6 @@ __global__ void __launch_bounds__(kThreads) k_q4(const __grid_constant__ Q4Geo g
       u[i] = s;
     }
   __syncthreads();
-  const int rows = per_block * R;
-  const int64_t row0 = int64_t(rb) * rows;
   for (int i = threadIdx.x; i < rows * tokens; i += kThreads) {
     const int n = i / rows, r = i - n * rows;
     const int64_t row = row0 + r;
@@ -285,19 +372,47 @@ __global__ void __launch_bounds__(kThreads) k_q4(const __grid_constant__ Q4Geo g
   }
 }
 
-template <int NT, int MT>
+// Warps on the same rows: more of them shorten a warp's way through k, and add a block's start and end (about
+// 2 us, and 0.4 for each that shares the SM) for each of its fewer spans.  A span takes a lone block's warps 0.62 us; eight warps' worth of a span
+// keeps an SM busy for `busy` of it, whatever shares the SM.  20480 x 5120, 8 tokens: 28.6 us with one warp, 22.3 with
+// two, 20.0 with four, 20.6 with eight; 3584 x 3584, one token: 15.3, 9.5, 6.5 and 5.6.
+template <int NT>
+void share_rows(Q4Geo& g, int64_t sets) {
+  constexpr double busy = NT <= 2 ? 0.44 : NT == 4 ? 0.8 : 1.2;
+  auto round = [](int64_t blocks, int64_t spans) {
+    const double each = blocks * busy;
+    return blocks > 0 ? double(spans) * (each > 0.62 ? each : 0.62) + 2.0 + 0.4 * blocks : 0.0;
+  };
+  double best = 0;
+  for (int ks = 1; ks <= kWarps; ks *= 2) {
+    const int64_t per = div_up(g.spans, ks), blocks = div_up(div_up(g.tiles, kWarps / ks) * sets, sm_count());
+    const double c = double(blocks / resident(NT)) * round(resident(NT), per) + round(blocks % resident(NT), per);
+    if (ks == 1 || c < best) {
+      best = c;
+      g.ks = ks;
+      g.per_warp = int(per);
+    }
+  }
+}
+
+template <int NT, int kGroups>
 cudaError_t launch_one(Q4Geo g, cudaStream_t s) {
-  // as many warps on the same rows as it takes to give every SM two blocks
-  const int64_t groups = g.tiles / MT;
-  g.ks = 1;
-  while (g.ks < kWarps && div_up(groups, kWarps / g.ks) < 2 * sm_count() && g.chunks >= 2 * kAhead * g.ks) g.ks *= 2;
-  const int per_block = kWarps / g.ks;
-  g.row_blocks = int(div_up(groups, per_block));
-  const int64_t blocks = int64_t(g.row_blocks) * div_up(g.N, 8 * NT);
-  const int smem = 4 * (kWarps * 8 * NT * 16 * MT + (g.low.U ? 8 * NT * g.low.kp : 0));
-  cudaError_t e = cudaFuncSetAttribute(k_q4<NT, MT>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxSmem);
+  const int64_t sets = div_up(g.N, 8 * NT);
+  share_rows<NT>(g, sets);
+  g.row_blocks = int(div_up(g.tiles, kWarps / g.ks));
+  const int sums = 4 * (kWarps * 8 * NT * 16 + (g.low.U ? 8 * NT * g.low.kp : 0)), rings = kWarps * warp_bytes(kGroups);
+  const cudaError_t e = cudaFuncSetAttribute(k_q4<NT, kGroups>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxSmem);
   if (e != cudaSuccess) return e;
-  return gp::launch_early(k_q4<NT, MT>, dim3(unsigned(blocks)), dim3(kThreads), size_t(smem), s, g);
+  return gp::launch_early(k_q4<NT, kGroups>, dim3(unsigned(g.row_blocks * sets)), dim3(kThreads),
+                          size_t(sums > rings ? sums : rings), s, g);
+}
+
+template <int kGroups>
+cudaError_t launch_tokens(const Q4Geo& g, cudaStream_t s) {
+  if (g.N <= 8) return launch_one<1, kGroups>(g, s);
+  if (g.N <= 16) return launch_one<2, kGroups>(g, s);
+  if (g.N <= 32) return launch_one<4, kGroups>(g, s);
+  return launch_one<8, kGroups>(g, s);
 }
 
 }  // namespace
@@ -330,7 +445,7 @@ cudaError_t launch_q4_apply(const void* X, int64_t ldx, int64_t N, int64_t d, co
   g.o = o;
   g.d = d;
   g.tiles = p.tiles;
-  g.chunks = int(p.chunks);
+  g.spans = int(p.chunks / 2);
   g.groups = int(p.groups);
   g.X = static_cast<const __nv_bfloat16*>(X);
   g.ldx = ldx;
@@ -341,10 +456,11 @@ cudaError_t launch_q4_apply(const void* X, int64_t ldx, int64_t N, int64_t d, co
     const cudaError_t e = launch_adapter_tokens(X, ldx, N, d, o, adapters, n, k, plan, workspace, &g.low, s);
     if (e != cudaSuccess) return e;
   }
-  if (N <= 8) return launch_one<1, 2>(g, s);
-  if (N <= 16) return launch_one<2, 2>(g, s);
-  if (N <= 32) return launch_one<4, 2>(g, s);
-  return launch_one<8, 2>(g, s);
+  switch (128 / group) {
+    case 1: return launch_tokens<1>(g, s);
+    case 2: return launch_tokens<2>(g, s);
+    default: return launch_tokens<4>(g, s);
+  }
 }
 
 }  // namespace loca
