@@ -1085,7 +1085,7 @@ struct AdapterExt {
 
 struct EpiRows {
   static constexpr bool kPacks = true;
-  static constexpr bool kSeeks = false;
+  static constexpr bool kAhead = false;
   static constexpr bool kFits = false;
   static constexpr bool kSums = false;
   struct Row {};

@@ -64,6 +64,7 @@ __device__ __forceinline__ float gate_of(const Act& p, float x) {
 
 struct EpiGate {
   static constexpr bool kFits = false;
+  static constexpr bool kAhead = false;
   Act p;
 
   struct Row {};
@@ -83,6 +84,7 @@ struct EpiGate {
 
 struct EpiGateBack {
   static constexpr bool kFits = false;
+  static constexpr bool kAhead = false;
   Act p;
   const __nv_bfloat16* dH;  // this piece's rows and columns
   int64_t pitch;

@@ -254,6 +254,7 @@ struct Twin : NoExt {
 // (one writer per element and launch: a fixed order of additions).
 struct EpiAcc {
   static constexpr bool kPacks = false;
+  static constexpr bool kAhead = false;
   static constexpr bool kFits = true;
   int add;
 
@@ -281,10 +282,20 @@ struct EpiAcc {
   }
 };
 
+struct NoState {};
+template <class Epi, bool kOn>
+struct StateOf {
+  using type = NoState;
+};
+template <class Epi>
+struct StateOf<Epi, true> {
+  using type = typename Epi::State;
+};
+
 // Scaled and rounded once.
 struct EpiScaled {
   static constexpr bool kPacks = true;
-  static constexpr bool kSeeks = false;
+  static constexpr bool kAhead = false;
   static constexpr bool kFits = false;
   static constexpr bool kSums = false;
   float scale;
@@ -296,14 +307,17 @@ struct EpiScaled {
 
 // What becomes of a finished tile.  An output in bf16 is given value by value (kPacks): Row row_of(row)
 // reads what a row needs, before its sums are complete; value(Row, column, sum) is the output.  kSums (not
-// in the wide shape): Row adds something up over the values, which finish(Row, half tile, row) gets.  kSeeks (not in
-// the wide shape): seek(Row, column) is called ahead of the first of a thread's columns, which come in order.  Other
+// in the wide shape): Row adds something up over the values, which finish(Row, half tile, row) gets.  Other
 // uses take the sums themselves:  void operator()(const Tile&, float (&v)[128], int row, int col0, int lane,
 //                                   uint8_t* box, const CUtensorMap* out) const
 // called once per finished accumulator by every epilogue thread, with the sums of row `row`, columns
 // col0 .. col0 + 127.  With twin products:  Row before(int row, int col0), called before the sums are complete,
 // and operator()(const Tile&, float (&v)[128], Row&, int row, int col0, int lane, uint8_t* box, out, out2) with 64
 // columns of the first product in v[0 .. 63] and the same of the second behind them; out2 is tmAx.
+// kAhead (narrow and single): what an epilogue has to look up for a tile is on its way while the sums are not
+// complete: a State for each thread; start(State, row of the first tile), ahead(State, row, half tile, row of the next
+// tile) before the sums; the state goes to row_of(), which also gets the first column, or to operator().  With
+// kPacks  bool simple(Row)  chooses for a warp between value1() and value().
 // kFits: the number of k ranges is the device's choice (Fit).
 template <int kShape, bool kAmn, bool kBmn, class Epi, class Ext>
 __global__ void __cluster_dims__(Shape<kShape>::kCtas, 1, 1) __launch_bounds__(THREADS, 1)
@@ -601,6 +615,9 @@ __global__ void __cluster_dims__(Shape<kShape>::kCtas, 1, 1) __launch_bounds__(T
     uint8_t* box = boxes + (warp - 2) * BOX;
     uint32_t seg = 0;
     bool go = true;
+    typename StateOf<Epi, Epi::kAhead>::type state;
+    if constexpr (Epi::kAhead)
+      if (cid < lv.total) epi.start(state, tile_of(g, lv, cid).m * TM + int(rank) * HALF + q * 32 + lane);
     for (int it = cid; it < lv.total && go; it += ncl) {
       const Tile t = tile_of(g, lv, it);
       const int all = t.kb1 - t.kb0 + (Ext::kOn ? ext.entries(t.m) : 0);
@@ -701,6 +718,10 @@ __global__ void __cluster_dims__(Shape<kShape>::kCtas, 1, 1) __launch_bounds__(T
         if (!go) break;
         if (all > 0) ++seg;
       } else {
+        if constexpr (Epi::kAhead) {
+          const int after = it + ncl < lv.total ? tile_of(g, lv, it + ncl).m - t.m : 0;
+          epi.ahead(state, row, 2 * t.n + h, row + after * TM);
+        }
         const int nseg = (all + g.seg_kb - 1) / g.seg_kb;
         float v[128];
         if (nseg == 0) {
@@ -728,21 +749,38 @@ __global__ void __cluster_dims__(Shape<kShape>::kCtas, 1, 1) __launch_bounds__(T
         if (!go) break;
         const int col0 = t.col0 + h * HALF;
         if constexpr (Epi::kPacks) {
-          auto pre = epi.row_of(row);
-          if constexpr (Epi::kSeeks) epi.seek(pre, col0);
+          auto pre = [&] {
+            if constexpr (Epi::kAhead) return epi.row_of(row, state, col0);
+            else return epi.row_of(row);
+          }();
+          bool simple = false;
+          if constexpr (Epi::kAhead) simple = epi.simple(pre);
 #pragma unroll
           for (int b = 0; b < 2; ++b) {
             if (col0 + 64 * b >= (kSlim ? t.end : g.cols)) continue;
             uint32_t w[32];
+            if (Epi::kAhead && simple) {
+              if constexpr (Epi::kAhead) {
 #pragma unroll
-            for (int i = 0; i < 32; ++i) {
-              const float lo = epi.value(pre, col0 + 64 * b + 2 * i, v[64 * b + 2 * i]);
-              const float hi = epi.value(pre, col0 + 64 * b + 2 * i + 1, v[64 * b + 2 * i + 1]);
-              w[i] = pack_bf16(lo, hi);
+                for (int i = 0; i < 32; ++i) {
+                  const float lo = epi.value1(pre, col0 + 64 * b + 2 * i, v[64 * b + 2 * i]);
+                  const float hi = epi.value1(pre, col0 + 64 * b + 2 * i + 1, v[64 * b + 2 * i + 1]);
+                  w[i] = pack_bf16(lo, hi);
+                }
+              }
+            } else {
+#pragma unroll
+              for (int i = 0; i < 32; ++i) {
+                const float lo = epi.value(pre, col0 + 64 * b + 2 * i, v[64 * b + 2 * i]);
+                const float hi = epi.value(pre, col0 + 64 * b + 2 * i + 1, v[64 * b + 2 * i + 1]);
+                w[i] = pack_bf16(lo, hi);
+              }
             }
             store_box_bf16(box, &tmO, lane, col0 + 64 * b, r0, w);
           }
           if constexpr (Epi::kSums) epi.finish(pre, 2 * t.n + h, row);
+        } else if constexpr (Epi::kAhead) {
+          epi(t, v, state, row, col0, lane, box, &tmO);
         } else {
           epi(t, v, row, col0, lane, box, &tmO);
         }

@@ -28,9 +28,11 @@
 //   loss_n = w_n tau^2 sum_k q_k (log q_k - log p_{i_k}),  dZ = g_n w_n tau (p - q)
 // k_teacher      each position's words in order, a word that comes twice once with both shares, q and
 //                sum q log q; positions without a word are masked
-// The epilogue of a logit tile finds the row's first word at or behind its columns by bisection and goes on
-// from word to word as the columns pass: forward it stores their logits (K of V), backward it takes q off
-// p in fp32, before dZ is rounded.
+//                Beside them goes a table of the first word in each row and 128 columns (2 bytes)
+// The epilogue of a logit tile reads that table while the sums are not complete and goes on from word to word:
+// forward it stores their logits (K of V), backward it takes q off p in fp32, before dZ is rounded.  (Bisection in
+// the row's words and a test for each column took 777 tokens at d = 896, V = 32003 66 and 75 us where the
+// loss without a teacher takes 37 and 47.)
 // k_teacher_join as k_head_join, with the sum over the words
 // Computing the logits a second time costs 2 N d V operations; keeping them would cost 4 N V bytes
 // (2.5 GB per 4096 tokens at V = 151936).
@@ -195,6 +197,7 @@ __global__ void __launch_bounds__(256)
 // Forward: maximum and sum of exponentials of 128 logits of a row.
 struct EpiStats {
   static constexpr bool kPacks = false;
+  static constexpr bool kAhead = false;
   static constexpr bool kFits = false;
   float2* part;        // (2 column tiles) x pitch
   int64_t pitch;       // rows of a piece
@@ -262,7 +265,7 @@ struct EpiStats {
 // the other columns' p.
 struct EpiDz {
   static constexpr bool kPacks = true;
-  static constexpr bool kSeeks = false;
+  static constexpr bool kAhead = false;
   static constexpr bool kFits = false;
   static constexpr bool kSums = true;
   const float* lse;
@@ -311,8 +314,22 @@ struct Words {
   float* q;      // N x K
   float* ent;    // N: sum q log q over the given entries
   int32_t* live; // N: 0, or -1 where a position has no word (or no share: all its logits -inf)
+  uint16_t* table;  // N x pitch: the first word in a half tile (kNoEntry: none)
   int K;
+  int pitch;     // half tiles of a row, to a multiple of 8
+  // the half tiles: of tiles of `width` columns, in pieces of the vocabulary of `piece` columns and `of_piece` half tiles
+  int width, piece, of_piece;
 };
+// Column within the half tile | place among the row's words << 7 | whether the next word may be here too << 15.
+constexpr uint32_t kNoEntry = 0xffffu;  // (word 255 is the last: none comes after it)
+__device__ __forceinline__ int half_of(const Words& t, int32_t v, int& at) {
+  const int p = v / t.piece;
+  v -= p * t.piece;
+  const int n = v / t.width;
+  v -= n * t.width;
+  at = v & 127;
+  return p * t.of_piece + 2 * n + (v >> 7);
+}
 
 // One warp a row: the words sorted in shared memory by exchanges whose order the sizes alone fix (bitonic), then
 // runs of one word joined from left to right.  Entries outside [0, V) are none.  A NaN among the logits, or +inf,
@@ -329,6 +346,8 @@ __global__ void __launch_bounds__(32 * kTeacherWarps)
   const int64_t n = int64_t(blockIdx.x) * kTeacherWarps + warp;
   if (n >= N) return;
   const int K = out.K;
+  uint16_t* table = out.table + n * out.pitch;
+  for (int i = lane; i < out.pitch / 8; i += 32) reinterpret_cast<uint4*>(table)[i] = make_uint4(~0u, ~0u, ~0u, ~0u);
   for (int i = lane; i < padded; i += 32) {
     const int32_t v = i < K ? __ldg(idx + n * K + i) : -1;
     const bool word = v >= 0 && v < V;
@@ -373,14 +392,20 @@ __global__ void __launch_bounds__(32 * kTeacherWarps)
       const float l = val[i] - base - log_mass;
       const float share = expf(l);
       if (!(share == 0.f)) ent += share * l;
-      if (first)
-        for (int j = i; j < padded && key[j] == w; ++j) q += expf(val[j] - base - log_mass);
     }
+    int end = i;  // of the word's run
+    if (first)
+      for (; end < padded && key[end] == w; ++end) q += expf(val[end] - base - log_mass);
     const unsigned all = __ballot_sync(0xffffffffu, first);
     const int at = count + __popc(all & ((1u << lane) - 1u));
     if (first && LOCA_CHECK(n * K + at, N * K)) {
       out.at[n * K + at] = w;
       out.q[n * K + at] = q;
+      int col, other;
+      const int half = half_of(out, w, col);
+      const bool more = end < padded && key[end] != kNoWord && half_of(out, key[end], other) == half;
+      if ((i == 0 || half_of(out, key[i - 1], other) != half) && LOCA_CHECK(half, out.pitch))
+        table[half] = uint16_t(col | at << 7 | (more ? 1 << 15 : 0));
     }
     count += __popc(all);
   }
@@ -396,37 +421,36 @@ __global__ void __launch_bounds__(32 * kTeacherWarps)
   }
 }
 
-// A row's words from a column on.
-struct Cursor {
-  const int32_t* at;  // the row's words (null: none)
-  int j;              // the next one
-  int next;           // its column, or kNoWord
+// A thread's look-ups: its row's place in the call's order, a tile ahead, and what the table has for this tile.
+struct WordState {
+  int32_t n, next_n;
+  uint32_t entry;
 };
-__device__ __forceinline__ Cursor word_cursor(const Words& t, int32_t n) {
-  return Cursor{n >= 0 ? t.at + int64_t(n) * t.K : nullptr, 0, kNoWord};
+__device__ __forceinline__ void words_ahead(const Words& t, const int32_t* idx, WordState& s, int half, int next_row) {
+  s.n = s.next_n;
+  s.entry = kNoEntry;
+  if (s.n >= 0 && LOCA_CHECK(half, t.pitch)) s.entry = __ldg(t.table + int64_t(s.n) * t.pitch + half);
+  s.next_n = idx[next_row];
 }
-__device__ __forceinline__ int word_column(const Words& t, const Cursor& c, int64_t v_first) {
-  const int32_t w = c.j < t.K ? __ldg(c.at + c.j) : kNoWord;
-  return w == kNoWord ? kNoWord : int(w - v_first);
-}
-// To the first word at or behind column col0 (v_first + col0 of the vocabulary).
-__device__ __forceinline__ void word_seek(const Words& t, Cursor& c, int64_t v_first, int col0) {
-  if (!c.at) return;
-  const int64_t v = v_first + col0;
-  int lo = 0, hi = t.K;
-  while (lo < hi) {
-    const int mid = (lo + hi) >> 1;
-    if (int64_t(__ldg(c.at + mid)) < v) lo = mid + 1;
-    else hi = mid;
-  }
-  c.j = lo;
-  c.next = word_column(t, c, v_first);
+
+// v[i] for an i that differs from thread to thread: halves chosen bit by bit.
+__device__ __forceinline__ float pick(const float (&v)[128], int i) {
+  float a[64];
+#pragma unroll
+  for (int k = 0; k < 64; ++k) a[k] = i & 64 ? v[64 + k] : v[k];
+#pragma unroll
+  for (int w = 32; w > 0; w >>= 1)
+#pragma unroll
+    for (int k = 0; k < w; ++k) a[k] = i & w ? a[w + k] : a[k];
+  return a[0];
 }
 
 // Forward: maximum and sum of exponentials of 128 logits of a row, and the logits of its words.
 struct EpiTeacher {
   static constexpr bool kPacks = false;
   static constexpr bool kFits = false;
+  static constexpr bool kAhead = true;
+  using State = WordState;
   float2* part;        // (2 column tiles) x pitch
   int64_t pitch;       // rows of a piece
   const int32_t* idx;  // this piece's rows: their places in the call's order
@@ -434,11 +458,13 @@ struct EpiTeacher {
   float* zk;           // pitch x K
   float scale;         // log2(e) / tau
 
-  __device__ __forceinline__ void operator()(const gp::Tile& t, float (&v)[128], int row, int col0, int lane, uint8_t*,
-                                             const CUtensorMap*) const {
+  __device__ __forceinline__ void start(State& s, int row) const { s.next_n = idx[row]; }
+  __device__ __forceinline__ void ahead(State& s, int row, int half, int next_row) const {
+    words_ahead(words, idx, s, half, next_row);
+  }
+  __device__ __forceinline__ void operator()(const gp::Tile& t, float (&v)[128], const State& st, int row, int col0, int lane,
+                                             uint8_t*, const CUtensorMap*) const {
     if (!LOCA_CHECK(row, pitch)) return;
-    Cursor c = word_cursor(words, idx[row]);
-    word_seek(words, c, 0, col0);
     const int left = t.end - col0 < 128 ? t.end - col0 : 128;  // columns of the vocabulary among these
     if (left < 128) {
 #pragma unroll
@@ -464,16 +490,17 @@ struct EpiTeacher {
       s3 += exp_scaled(v[i + 3], base, scale);
     }
     part[int64_t(2 * t.n + (col0 > t.col0 ? 1 : 0)) * pitch + row] = make_float2(m, (s0 + s1) + (s2 + s3));
-    const int end = col0 + left;
-    if (__any_sync(0xffffffffu, c.next < end)) {
-      float* z = zk + int64_t(row) * words.K;
-#pragma unroll
-      for (int i = 0; i < 128; ++i)
-        if (c.next == col0 + i && i < left) {
-          if (LOCA_CHECK(c.j, words.K)) z[c.j] = v[i];
-          ++c.j;
-          c.next = word_column(words, c, 0);
-        }
+    bool here = st.entry != kNoEntry;
+    int at = st.entry & 127, k = st.entry >> 7 & 255;
+    bool more = st.entry >> 15 & 1;
+    while (__any_sync(0xffffffffu, here)) {
+      const float z = pick(v, at);
+      if (here && LOCA_CHECK(k, words.K)) zk[int64_t(row) * words.K + k] = z;
+      here = here && more && ++k < words.K;
+      if (here) {
+        at = __ldg(words.at + int64_t(st.n) * words.K + k) - col0;
+        here = at < left;
+      }
     }
   }
 };
@@ -482,9 +509,10 @@ struct EpiTeacher {
 // rows past the live ones are zero.
 struct EpiDzTeacher {
   static constexpr bool kPacks = true;
-  static constexpr bool kSeeks = true;
   static constexpr bool kFits = false;
   static constexpr bool kSums = false;
+  static constexpr bool kAhead = true;
+  using State = WordState;
   const float* lse;    // this piece's rows
   const float* w;      // w_n dloss_n
   const int32_t* idx;
@@ -494,32 +522,52 @@ struct EpiDzTeacher {
   int64_t row_first;   // this piece's first row among the live rows
   int64_t v_first;     // this piece's first vocabulary column
   int v_cols;          // its columns of the vocabulary
+  int half_first;      // its first half tile
 
   struct Row {
-    float lse, g;
-    int end;  // the columns that count (none in rows past the live ones)
-    Cursor c;
-    const float* q;
+    float lse, g, q;
+    int end;   // the columns that count (none in rows past the live ones)
+    int next;  // the next word's column, its place and whether another may follow
+    int k;
+    bool more;
+    int64_t from;  // of the row's words
   };
-  __device__ __forceinline__ Row row_of(int row) const {
+  __device__ __forceinline__ void start(State& s, int row) const { s.next_n = idx[row]; }
+  __device__ __forceinline__ void ahead(State& s, int row, int half, int next_row) const {
+    words_ahead(words, idx, s, half_first + half, next_row);
+  }
+  __device__ __forceinline__ Row row_of(int row, const State& st, int col0) const {
     Row r;
-    const bool live = row_first + row < *count;
+    const bool here = st.entry != kNoEntry;  // (the table has nothing for rows past the live ones)
+    r.end = row_first + row < *count ? v_cols : 0;
+    r.k = st.entry >> 7 & 255;
+    r.from = int64_t(st.n) * words.K;
+    r.next = here ? col0 + int(st.entry & 127) : kNoWord;
+    r.q = here ? __ldg(words.q + r.from + r.k) : 0.f;
+    r.more = here && (st.entry >> 15 & 1);
     r.lse = lse[row];
     r.g = w[row] * tau;
-    r.end = live ? v_cols : 0;
-    const int32_t n = live ? idx[row] : -1;
-    r.c = word_cursor(words, n);
-    r.q = words.q + int64_t(n < 0 ? 0 : n) * words.K;
     return r;
   }
-  __device__ __forceinline__ void seek(Row& r, int col0) const { word_seek(words, r.c, v_first, col0); }
+  __device__ __forceinline__ bool simple(const Row& r) const { return !__any_sync(0xffffffffu, r.more); }
+  __device__ __forceinline__ float value1(Row& r, int col, float z) const {
+    float p = exp_diff(fmaf(z, inv_tau, -r.lse), 0.f);
+    if (col == r.next) p -= r.q;
+    return col < r.end ? r.g * p : 0.f;
+  }
   __device__ __forceinline__ float value(Row& r, int col, float z) const {
     if (col >= r.end) return 0.f;
     float p = exp_diff(fmaf(z, inv_tau, -r.lse), 0.f);
-    if (col == r.c.next) {
-      if (LOCA_CHECK(r.c.j, words.K)) p -= __ldg(r.q + r.c.j);
-      ++r.c.j;
-      r.c.next = word_column(words, r.c, v_first);
+    if (col == r.next) {
+      p -= r.q;
+      r.next = kNoWord;
+      if (++r.k < words.K) {
+        const int32_t v = __ldg(words.at + r.from + r.k);
+        if (v != kNoWord) {
+          r.next = int(v - v_first);
+          r.q = __ldg(words.q + r.from + r.k);
+        }
+      }
     }
     return r.g * p;
   }
@@ -726,6 +774,8 @@ Rows rows_at(void* ws, const RowsWs& o) {
   return r;
 }
 
+int fwd_width(int64_t N, int64_t V) { return N <= gp::HALF ? gp::slim_width(V) : gp::TN; }
+
 struct FwdWs {
   RowsWs rows;
   int64_t piece;
@@ -736,7 +786,7 @@ FwdWs fwd_ws(int64_t N, int64_t V, int64_t d, int C) {
   o.rows = rows_ws(N, d);
   const int64_t np = round_up(N < 1 ? 1 : N, gp::TM);
   o.piece = np < kFwdRows ? np : kFwdRows;
-  const int width = N <= gp::HALF ? gp::slim_width(V) : gp::TN;
+  const int width = fwd_width(N, V);
   const size_t nparts = 2 * size_t((V + width - 1) / width);
   size_t at = o.rows.total;
   o.part = at; at += align256(nparts * size_t(o.piece) * sizeof(float2));
@@ -829,26 +879,28 @@ cudaError_t launch_rows(const void* H, int64_t ldh, int64_t N, int64_t d, int64_
                           static_cast<__nv_bfloat16*>(dH0), lddh);
 }
 
-// The logit tiles of a forward piece; *width: columns of a tile.
+// The logit tiles of a forward piece; width: columns of a tile.
 template <class Epi>
 cudaError_t forward_tiles(const Rows& r, int64_t N, int64_t p0, int64_t rows, int64_t d, const void* W, int64_t V,
-                          const Epi& epi, int32_t* status, int* width, cudaStream_t s) {
+                          const Epi& epi, int32_t* status, int width, cudaStream_t s) {
   const bool single = N <= gp::HALF;
-  *width = single ? gp::slim_width(V) : gp::TN;
   const int arows = single ? int(round_up(N, 8)) : gp::HALF;
   CUtensorMap ma, mb;
-  if ((single ? !gp::map_2d(&mb, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, W, d, V, d, gp::BK, *width / 2)
+  if ((single ? !gp::map_2d(&mb, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, W, d, V, d, gp::BK, width / 2)
               : !gp::map_kmajor(&mb, W, d, V, d)) ||
       !gp::map_2d(&ma, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, r.H + p0 * d, d, rows, d, gp::BK, arows))
     return cudaErrorInvalidValue;
   gp::Geo g = geo(rows / gp::TM, V, (d + gp::BK - 1) / gp::BK, single ? kSegKbFew : kSegKb, r, status);
   g.rows_live = r.count;
   g.m_first = int(p0 / gp::TM);
-  g.width = *width;
+  g.width = width;
   g.arows = arows;
   return single ? gp::launch<gp::kSingle, false, false>(ma, mb, ma, mb, ma, g, epi, gp::NoExt{}, s)
                 : gp::launch<gp::kNarrow, false, false>(ma, mb, ma, mb, ma, g, epi, gp::NoExt{}, s);
 }
+
+// Columns of the backward pass's logit tiles.
+int back_width(int64_t N, int64_t cols) { return few_rows(N) ? gp::slim_width(cols, 64) : gp::TN; }
 
 struct Backward {
   BwdWs lay;
@@ -866,16 +918,16 @@ struct Backward {
 };
 
 // The logits of a piece once more, into dZ, in the forward pass's shape and segments, so that z comes out as it went
-// into lse; *width: columns of a tile.
+// into lse; width: columns of a tile.
 template <class Epi>
-cudaError_t logit_tiles(const Backward& b, int64_t p0, int64_t rows, int64_t v0, int64_t vn, const Epi& epi, int* width) {
+cudaError_t logit_tiles(const Backward& b, int64_t p0, int64_t rows, int64_t v0, int64_t vn, const Epi& epi, int width) {
   const bool single = few_rows(b.N);
   CUtensorMap mh, mw, mz_out;
   gp::Geo g = geo(rows / gp::TM, vn, (b.d + gp::BK - 1) / gp::BK, single ? kSegKbFew : kSegKb, b.r, b.status);
   g.rows_live = b.r.count;
   g.m_first = int(p0 / gp::TM);
   g.arows = single ? int(round_up(b.N, 8)) : gp::HALF;
-  g.width = *width = single ? gp::slim_width(vn, 64) : gp::TN;
+  g.width = width;
   if (!gp::map_2d(&mh, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, b.r.H + p0 * b.d, b.d, rows, b.d, gp::BK, g.arows) ||
       !gp::map_2d(&mw, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, b.W + v0 * b.d, b.d, vn, b.d, gp::BK, g.width / 2) ||
       !gp::map_out_bf16(&mz_out, b.ws + b.lay.dz, b.lay.vc, b.lay.piece, b.lay.vc))
@@ -974,8 +1026,8 @@ cudaError_t launch_head_loss(const void* H, int64_t ldh, int64_t N, int64_t d, c
   float* zc = reinterpret_cast<float*>(ws + lay.zc);
   for (int64_t p0 = 0; p0 < np; p0 += lay.piece) {
     const int64_t rows = np - p0 < lay.piece ? np - p0 : lay.piece;
-    int width = 0;
-    e = forward_tiles(r, N, p0, rows, d, W, V, EpiStats{part, lay.piece, r.y + p0, zy, cols, E ? C : 0, zc}, status, &width,
+    const int width = fwd_width(N, V);
+    e = forward_tiles(r, N, p0, rows, d, W, V, EpiStats{part, lay.piece, r.y + p0, zy, cols, E ? C : 0, zc}, status, width,
                       s);
     if (e != cudaSuccess) return e;
     const int nparts = int(2 * ((V + width - 1) / width));
@@ -1002,10 +1054,10 @@ cudaError_t launch_head_loss_backward(const void* H, int64_t ldh, int64_t N, int
   // dZ of the vocabulary columns v0 .. v0 + vn.  all: they are all there are, so the sum of the others' p that
   // the target's entry takes is whole; done: earlier calls have made it; neither: this call adds to it
   auto make_dz = [&](int64_t p0, int64_t rows, int64_t v0, int64_t vn, bool all, bool done) {
-    int width = 0;
+    const int width = back_width(N, vn);
     const cudaError_t e =
         logit_tiles(b, p0, rows, v0, vn, EpiDz{r.lse + p0, r.w + p0, r.y + p0, r.count, p0, v0, int(vn), others, lay.piece},
-                    &width);
+                    width);
     if (e != cudaSuccess) return e;
     const int nparts = done ? 0 : int(2 * ((vn + width - 1) / width));
     return gp::launch_early(k_head_target, dim3(unsigned(rows / 32)), dim3(32, nparts >= 128 ? 32 : 8), 0, s, others,
@@ -1029,14 +1081,20 @@ cudaError_t launch_head_loss_backward(const void* H, int64_t ldh, int64_t N, int
 namespace {
 
 struct WordsWs {
-  size_t at, q, ent, live, total;
+  int width, piece, of_piece, pitch;
+  size_t at, q, ent, live, table, total;
 };
-WordsWs words_ws(int64_t N, int K, size_t from) {
+WordsWs words_ws(int64_t N, int64_t V, int K, int width, int64_t piece, size_t from) {
   WordsWs o{};
+  o.width = width;
+  o.piece = int(piece);
+  o.of_piece = int(2 * ((piece + width - 1) / width));
+  o.pitch = int(round_up((V + piece - 1) / piece * o.of_piece, 8));
   o.at = from; from += align256(4 * size_t(N) * size_t(K));
   o.q = from; from += align256(4 * size_t(N) * size_t(K));
   o.ent = from; from += align256(4 * size_t(N));
   o.live = from; from += align256(4 * size_t(N));
+  o.table = from; from += align256(2 * size_t(N) * size_t(o.pitch));
   o.total = from;
   return o;
 }
@@ -1048,7 +1106,7 @@ struct DistillWs {
 DistillWs distill_ws(int64_t N, int64_t V, int64_t d, int K) {
   DistillWs o{};
   o.fwd = fwd_ws(N, V, d, 0);
-  o.words = words_ws(N, K, o.fwd.total);
+  o.words = words_ws(N, V, K, fwd_width(N, V), V, o.fwd.total);
   o.zk = o.words.total;
   o.total = o.zk + align256(4 * size_t(o.fwd.piece) * size_t(K));
   return o;
@@ -1057,7 +1115,8 @@ DistillWs distill_ws(int64_t N, int64_t V, int64_t d, int K) {
 cudaError_t launch_teacher(const int32_t* idx, const float* t, int64_t N, int64_t V, int K, float tau, uint8_t* ws,
                            const WordsWs& lay, Words* out, cudaStream_t s) {
   *out = Words{reinterpret_cast<int32_t*>(ws + lay.at), reinterpret_cast<float*>(ws + lay.q),
-               reinterpret_cast<float*>(ws + lay.ent), reinterpret_cast<int32_t*>(ws + lay.live), K};
+               reinterpret_cast<float*>(ws + lay.ent), reinterpret_cast<int32_t*>(ws + lay.live),
+               reinterpret_cast<uint16_t*>(ws + lay.table), K, lay.pitch, lay.width, lay.piece, lay.of_piece};
   int padded = 32;
   while (padded < K) padded *= 2;
   const cudaError_t e = gp::keep_carveout(k_teacher);
@@ -1066,12 +1125,17 @@ cudaError_t launch_teacher(const int32_t* idx, const float* t, int64_t N, int64_
                           size_t(kTeacherWarps) * 8 * size_t(padded), s, idx, t, N, V, 1.f / tau, padded, *out);
 }
 
+WordsWs back_words(int64_t N, int64_t V, int K, const BwdWs& lay) {
+  const int64_t piece = V < lay.vc ? V : lay.vc;
+  return words_ws(N, V, K, back_width(N, piece), piece, lay.total);
+}
+
 }  // namespace
 
 int head_distill_max_words() { return kMostWords; }
 size_t head_distill_workspace_bytes(int64_t N, int64_t V, int64_t d, int K) { return distill_ws(N, V, d, K).total; }
 size_t head_distill_backward_workspace_bytes(int64_t N, int64_t V, int64_t d, int K, bool dh, bool dw) {
-  return words_ws(N, K, bwd_ws(N, V, d, dh, dw, false).total).total;
+  return back_words(N, V, K, bwd_ws(N, V, d, dh, dw, false)).total;
 }
 
 cudaError_t launch_head_distill(const void* H, int64_t ldh, int64_t N, int64_t d, const void* W, int64_t V,
@@ -1090,11 +1154,10 @@ cudaError_t launch_head_distill(const void* H, int64_t ldh, int64_t N, int64_t d
   const int64_t np = round_up(N, gp::TM);
   for (int64_t p0 = 0; p0 < np; p0 += lay.fwd.piece) {
     const int64_t rows = np - p0 < lay.fwd.piece ? np - p0 : lay.fwd.piece;
-    int width = 0;
     e = forward_tiles(r, N, p0, rows, d, W, V, EpiTeacher{part, lay.fwd.piece, r.idx + p0, words, zk, kLog2e / tau}, status,
-                      &width, s);
+                      lay.words.width, s);
     if (e != cudaSuccess) return e;
-    const int nparts = int(2 * ((V + width - 1) / width));
+    const int nparts = lay.words.of_piece;
     e = gp::launch_early(k_teacher_join, dim3(unsigned(rows / 32)), dim3(32, nparts >= 128 ? 32 : 8), 0, s, part,
                          lay.fwd.piece, nparts, r, p0, zk, words, tau, 1.f / tau, loss, lse);
     if (e != cudaSuccess) return e;
@@ -1107,9 +1170,10 @@ cudaError_t launch_head_distill_backward(const void* H, int64_t ldh, int64_t N, 
                                          const float* lse, const float* dloss, float scale, void* dH, int64_t lddh,
                                          void* dW, void* workspace, int32_t* status, cudaStream_t s) {
   const BwdWs lay = bwd_ws(N, V, d, dH != nullptr, dW != nullptr, false);
+  const WordsWs wlay = back_words(N, V, K, lay);
   uint8_t* ws = static_cast<uint8_t*>(workspace);
   Words words;
-  cudaError_t e = launch_teacher(idx, t, N, V, K, tau, ws, words_ws(N, K, lay.total), &words, s);
+  cudaError_t e = launch_teacher(idx, t, N, V, K, tau, ws, wlay, &words, s);
   if (e != cudaSuccess) return e;
   const Rows r = rows_at(workspace, lay.rows);
   e = launch_rows(H, ldh, N, d, 1, words.live, w, dloss, lse, r, nullptr, nullptr, nullptr, 0, dH, lddh, s);
@@ -1119,10 +1183,10 @@ cudaError_t launch_head_distill_backward(const void* H, int64_t ldh, int64_t N, 
   return backward_pieces(
       b, [](int64_t, int64_t) { return cudaSuccess; },
       [&](int64_t p0, int64_t rows, int64_t v0, int64_t vn) {
-        int width = 0;
         return logit_tiles(b, p0, rows, v0, vn,
-                           EpiDzTeacher{r.lse + p0, r.w + p0, r.idx + p0, words, tau, 1.f / tau, r.count, p0, v0, int(vn)},
-                           &width);
+                           EpiDzTeacher{r.lse + p0, r.w + p0, r.idx + p0, words, tau, 1.f / tau, r.count, p0, v0, int(vn),
+                                        int(v0 / wlay.piece) * wlay.of_piece},
+                           wlay.width);
       });
 }
 
