@@ -20,8 +20,9 @@
 // k_gemm_pair         dWg and dWu
 // k_gated_join        sums the k ranges of dX where its tiles alone would not fill the SMs
 // Bound: the tensor cores from a few hundred tokens on, the read of Wg and Wu below.  8192 tokens at d = 3584,
-// f = 14336: 938 us (1.79 PFLOP/s); one token there 46 us (206 MB: 4.5 TB/s); forward and backward of 4096 tokens
-// at d = 2048, f = 8192 708 us (1.55 PFLOP/s with the products computed again).
+// f = 14336: 856 us (1.97 PFLOP/s); one token there 39 us (206 MB: 5.3 TB/s); 64 tokens at d = 2048, f = 8192
+// 18.9 us (3.6 TB/s); forward and backward of 4096 tokens there 700 us (1.57 PFLOP/s with the products computed
+// again).
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
@@ -33,6 +34,10 @@ namespace {
 using namespace tc;
 
 constexpr int kSegKb = 64;             // 4096 k per accumulation segment: outputs are rounded to bf16
+// dX sums 2 f terms, and a wide tile has one running sum: up to 2048 steps of at most 2^-22 of it, within 2^-11
+// where its rounding is 2^-9.  1531 x 5120 over k = 27312: one round of 60 wide tiles without ranges, against five
+// ranges and their join (dX after dG and dU 250 us, 265 with ranges).
+constexpr int64_t kLongK = 32768;
 constexpr int64_t kRowBytes = int64_t(1) << 30;  // dG and dU of a piece of the rows (dX alone)
 constexpr int64_t kAllBytes = int64_t(4) << 30;  // of a piece of the columns (dWg and dWu sum over all rows)
 
@@ -62,23 +67,35 @@ __device__ __forceinline__ float gate_of(const Act& p, float x) {
   return rcp_approx(1.f + e);
 }
 
+// 8 columns of a row at `at`.
+__device__ __forceinline__ void put8(__nv_bfloat16* at, const uint32_t* w) {
+  *reinterpret_cast<uint4*>(at) = make_uint4(w[0], w[1], w[2], w[3]);
+}
+
 struct EpiGate {
   static constexpr bool kFits = false;
   static constexpr bool kAhead = false;
   Act p;
+  __nv_bfloat16* H;
+  int64_t pitch;
+  int rows;
 
   struct Row {};
   __device__ __forceinline__ Row before(int, int) const { return Row{}; }
+  __device__ __forceinline__ float value(float g, float u) const { return g * gate_of(p, clamped(p, g)) * u; }
   __device__ __forceinline__ void operator()(const gp::Tile&, float (&v)[128], Row&, int row, int col0, int lane,
                                              uint8_t* box, const CUtensorMap* out, const CUtensorMap*) const {
     uint32_t w[32];
 #pragma unroll
-    for (int i = 0; i < 32; ++i) {
-      const float g0 = v[2 * i], g1 = v[2 * i + 1];
-      w[i] = gp::pack_bf16(g0 * gate_of(p, clamped(p, g0)) * v[64 + 2 * i],
-                           g1 * gate_of(p, clamped(p, g1)) * v[64 + 2 * i + 1]);
-    }
+    for (int i = 0; i < 32; ++i)
+      w[i] = gp::pack_bf16(value(v[2 * i], v[64 + 2 * i]), value(v[2 * i + 1], v[64 + 2 * i + 1]));
     gp::store_box_bf16(box, out, lane, col0, row - lane, w);
+  }
+  __device__ __forceinline__ void store8(float (&v)[16], int row, int col) const {
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = gp::pack_bf16(value(v[2 * i], v[8 + 2 * i]), value(v[2 * i + 1], v[8 + 2 * i + 1]));
+    if (row < rows && LOCA_CHECK_SPAN(col, 8, pitch)) put8(H + int64_t(row) * pitch + col, w);
   }
 };
 
@@ -89,17 +106,18 @@ struct EpiGateBack {
   const __nv_bfloat16* dH;  // this piece's rows and columns
   int64_t pitch;
   int rows, cols;           // of the piece
+  __nv_bfloat16* D;         // its dG; dU is fc columns behind
+  int64_t fc;
 
-  struct Row {
-    uint4 dh[8];
-  };
+  struct Row {};
+  // dH is on its way to L2 while the sums are not complete (its place in registers is the sums').
   __device__ __forceinline__ Row before(int row, int col0) const {
-    Row r;
-    const __nv_bfloat16* src = dH + int64_t(row) * pitch + col0;
-#pragma unroll
-    for (int j = 0; j < 8; ++j)
-      r.dh[j] = row < rows && col0 + 8 * j < cols ? __ldg(reinterpret_cast<const uint4*>(src) + j) : make_uint4(0, 0, 0, 0);
-    return r;
+    if (row < rows && col0 < cols) {
+      const __nv_bfloat16* at = dH + int64_t(row) * pitch + col0;
+      asm volatile("prefetch.global.L2 [%0];" ::"l"(at));
+      if (col0 + 56 < cols) asm volatile("prefetch.global.L2 [%0];" ::"l"(at + 56));
+    }
+    return Row{};
   }
   __device__ __forceinline__ void one(float g, float u, float dh, float& dg, float& du) const {
     const float x = clamped(p, g);
@@ -109,21 +127,55 @@ struct EpiGateBack {
     dg = dh * u * d;
     du = dh * (g * s);
   }
-  __device__ __forceinline__ void operator()(const gp::Tile&, float (&v)[128], Row& r, int row, int col0, int lane,
-                                             uint8_t* box, const CUtensorMap* out, const CUtensorMap* out2) const {
-    uint32_t wg[32], wu[32];
+  // 8 columns: dG in wg, dU in wu
+  __device__ __forceinline__ void eight(const float* g, const float* u, const uint4& dh, uint32_t* wg, uint32_t* wu) const {
 #pragma unroll
-    for (int i = 0; i < 32; ++i) {
-      const uint32_t two = reinterpret_cast<const uint32_t*>(&r.dh[i / 4])[i & 3];
-      const float2 dh = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&two));
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t two = reinterpret_cast<const uint32_t*>(&dh)[i];
+      const float2 h = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&two));
       float g0, g1, u0, u1;
-      one(v[2 * i], v[64 + 2 * i], dh.x, g0, u0);
-      one(v[2 * i + 1], v[64 + 2 * i + 1], dh.y, g1, u1);
+      one(g[2 * i], u[2 * i], h.x, g0, u0);
+      one(g[2 * i + 1], u[2 * i + 1], h.y, g1, u1);
       wg[i] = gp::pack_bf16(g0, g1);
       wu[i] = gp::pack_bf16(u0, u1);
     }
-    gp::store_box_bf16(box, out, lane, col0, row - lane, wg);
+  }
+  __device__ __forceinline__ uint4 dh8(int row, int col) const {
+    return row < rows && col < cols ? __ldg(reinterpret_cast<const uint4*>(dH + int64_t(row) * pitch + col))
+                                    : make_uint4(0, 0, 0, 0);
+  }
+  __device__ __forceinline__ void operator()(const gp::Tile&, float (&v)[128], Row&, int row, int col0, int lane,
+                                             uint8_t* box, const CUtensorMap* out, const CUtensorMap* out2) const {
+    uint32_t wu[32];
+    if (lane == 0) bulk_wait_group_read0();
+    __syncwarp();
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+      uint4 dh[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) dh[j] = dh8(row, col0 + 32 * b + 8 * j);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int at = 32 * b + 8 * j;
+        uint32_t wg[4];
+        eight(v + at, v + 64 + at, dh[j], wg, wu + at / 2);
+        *reinterpret_cast<uint4*>(box + gp::box_off(lane, at / 8)) = make_uint4(wg[0], wg[1], wg[2], wg[3]);
+      }
+    }
+    fence_proxy_async_smem();
+    __syncwarp();
+    if (lane == 0) {
+      if (LOCA_REQUIRE(col0 >= 0 && row >= 0 && col0 % 8 == 0)) tma_store_2d(out, smem_u32(box), col0, row);
+      bulk_commit_group();
+    }
     gp::store_box_bf16(box, out2, lane, col0, row - lane, wu);
+  }
+  __device__ __forceinline__ void store8(float (&v)[16], int row, int col) const {
+    uint32_t wg[4], wu[4];
+    eight(v, v + 8, dh8(row, col), wg, wu);
+    if (row >= rows || !LOCA_CHECK_SPAN(col, 8, fc)) return;
+    put8(D + int64_t(row) * 2 * fc + col, wg);
+    put8(D + int64_t(row) * 2 * fc + fc + col, wu);
   }
 };
 
@@ -180,13 +232,20 @@ gp::Geo geo(int64_t rows, int64_t cols, int64_t nkb, int32_t* status, void* work
   return g;
 }
 
-// Columns of the single shape's tiles.  A CTA reads its weights at a rate of its own, so what counts is how many
-// rows of both operands a CTA fetches in all.
+// Columns of the single shape's tiles, a multiple of 16 up to 128: what counts is how many rows of both operands
+// a CTA fetches in all.  3584 x 14336 takes 150 tiles of 96.
 int twin_width(int64_t rows, int64_t cols) {
   const int64_t a = ceil_div(rows, 8) * 8;
-  const int64_t c64 = ceil_div(ceil_div(cols, 64), sm_count()) * (a + 128);
-  const int64_t c128 = ceil_div(ceil_div(cols, 128), sm_count()) * (a + 256);
-  return c64 < c128 ? 64 : 128;
+  int64_t best = 0;
+  int width = 0;
+  for (int w = 32; w <= 128; w += 16) {
+    const int64_t c = ceil_div(ceil_div(cols, w), sm_count()) * (a + 2 * w);
+    if (width == 0 || c < best) {
+      best = c;
+      width = w;
+    }
+  }
+  return width;
 }
 
 // Both products of a piece: rows of X against cols rows of Wg and of Wu.
@@ -196,7 +255,7 @@ cudaError_t launch_twin(const void* X, int64_t ldx, int64_t rows, int64_t d, con
                         const Epi& epi, cudaStream_t s) {
   CUtensorMap mx, mg, mu;
   const int64_t nkb = ceil_div(d, gp::BK);
-  const bool single = rows <= gp::HALF;
+  const bool single = rows <= gp::HALF && d <= gp::kWideK;  // (one sum per tile there)
   g.arows = single ? int(ceil_div(rows, 8) * 8) : gp::HALF;
   g.width = single ? twin_width(rows, cols) : 0;
   const int brows = single ? g.width : gp::HALF;
@@ -227,7 +286,7 @@ int dx_splits(int64_t rows, int64_t d, int64_t nkb) {
   for (int s = 1; s <= 32; ++s) {
     if (s > 1 && nkb / s < (single ? 4 : 16)) break;
     const double join = s > 1 ? double(s) * (double(single ? rows : m * gp::TM) * double(d) * 8.0 / 3000.0 + gp::kRangeCycles) + 3000.0 : 0.0;
-    const double c = gp::cycles(gp::pick_shape(rows, m, d, nkb, s), m, d, nkb, s) + join;
+    const double c = gp::cycles(gp::pick_shape(rows, m, d, nkb, s, kLongK), m, d, nkb, s) + join;
     if (s == 1 || c < best_c) {
       best = s;
       best_c = c;
@@ -272,7 +331,7 @@ cudaError_t launch_gated(const void* X, int64_t ldx, int64_t N, int64_t d, const
   if (!gp::map_out_bf16(&mo, H, f, N, ldh)) return cudaErrorInvalidValue;
   const gp::Geo g = geo(N, f, ceil_div(d, gp::BK), status, workspace, gp::call_mark());
   return launch_twin(X, ldx, N, d, static_cast<const __nv_bfloat16*>(Wg), static_cast<const __nv_bfloat16*>(Wu), f, mo, mo,
-                     g, EpiGate{act_of(act)}, s);
+                     g, EpiGate{act_of(act), static_cast<__nv_bfloat16*>(H), ldh, int(N)}, s);
 }
 
 cudaError_t launch_gated_backward(const void* X, int64_t ldx, int64_t N, int64_t d, const void* Wg, const void* Wu,
@@ -293,14 +352,14 @@ cudaError_t launch_gated_backward(const void* X, int64_t ldx, int64_t N, int64_t
     const int64_t rows = N - p0 < lay.piece ? N - p0 : lay.piece;
     const __nv_bfloat16* Xp = Xb + p0 * ldx;
     const int64_t range = ceil_div(rows, gp::TM) * gp::TM * d;  // sums of a k range
-    const int shape = gp::pick_shape(rows, ceil_div(rows, gp::TM), d, 2 * ceil_div(lay.fc, gp::BK), lay.splits);
+    const int shape = gp::pick_shape(rows, ceil_div(rows, gp::TM), d, 2 * ceil_div(lay.fc, gp::BK), lay.splits, kLongK);
     for (int64_t v0 = 0; v0 < f; v0 += lay.fc) {
       const int64_t vn = f - v0 < lay.fc ? f - v0 : lay.fc;
       const int64_t pitch = 2 * lay.fc;  // a row's dG, then its dU
       CUtensorMap og, ou;
       if (!gp::map_out_bf16(&og, D, vn, rows, pitch) || !gp::map_out_bf16(&ou, D + lay.fc, vn, rows, pitch))
         return cudaErrorInvalidValue;
-      const EpiGateBack epi{act_of(act), dHb + p0 * lddh + v0, lddh, int(rows), int(vn)};
+      const EpiGateBack epi{act_of(act), dHb + p0 * lddh + v0, lddh, int(rows), int(vn), D, lay.fc};
       e = launch_twin(Xp, ldx, rows, d, Wgb + v0 * d, Wub + v0 * d, vn, og, ou,
                       geo(rows, vn, ceil_div(d, gp::BK), status, workspace, mark), epi, s);
       if (e != cudaSuccess) return e;

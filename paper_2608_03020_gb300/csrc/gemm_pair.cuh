@@ -313,7 +313,9 @@ struct EpiScaled {
 // called once per finished accumulator by every epilogue thread, with the sums of row `row`, columns
 // col0 .. col0 + 127.  With twin products:  Row before(int row, int col0), called before the sums are complete,
 // and operator()(const Tile&, float (&v)[128], Row&, int row, int col0, int lane, uint8_t* box, out, out2) with 64
-// columns of the first product in v[0 .. 63] and the same of the second behind them; out2 is tmAx.
+// columns of the first product in v[0 .. 63] and the same of the second behind them; out2 is tmAx.  The single shape,
+// whose tiles are no whole boxes, calls store8(float (&v)[16], int row, int col) for 8 columns of both, in warps that
+// hold one of the epilogue's `rows`.
 // kAhead (narrow and single): what an epilogue has to look up for a tile is on its way while the sums are not
 // complete: a State for each thread; start(State, row of the first tile), ahead(State, row, half tile, row of the next
 // tile) before the sums; the state goes to row_of(), which also gets the first column, or to operator().  With
@@ -637,9 +639,26 @@ __global__ void __cluster_dims__(Shape<kShape>::kCtas, 1, 1) __launch_bounds__(T
         }
       };
       const int r0 = row - lane;
-      if constexpr (Ext::kTwin) {
+      if constexpr (Ext::kTwin && kSlim) {
+        // Half of the tile's columns (a multiple of 8) of the first product, and the same of the second `width` columns
+        // behind.  One sum per tile (launch()), and code that runs once: a loop over 8 columns straight from
+        // tensor memory, whose instructions need not all be fetched for one tile (64 columns from registers at a
+        // time: one token at 3584 x 14336 46.7 us, so 39.1).  Warps without a row do nothing.
+        const int half = g.width / 2, col0 = t.col0 + h * half, end = col0 + half < t.end ? col0 + half : t.end;
+        const uint32_t b = seg & 1u;
+        if (!(go = wait_sums(b, (seg >> 1) & 1u))) break;
+        const uint32_t ta = tmem_base + (uint32_t(q * 32) << 16) + b * uint32_t(TN) + uint32_t(h * half);
+        if (r0 < epi.rows)
+#pragma unroll 1
+          for (int c = 0; col0 + c < end; c += 8) {
+            float v[16];
+            tmem_ld8x2(ta + uint32_t(c), uint32_t(g.width), v);
+            epi.store8(v, row, col0 + c);
+          }
+        release(b);
+        ++seg;
+      } else if constexpr (Ext::kTwin) {
         // 64 columns of the first product and the same of the second, for every accumulator
-        const uint32_t second = kSlim ? uint32_t(g.width) : uint32_t(HALF);
         const int nseg = kShape == kWide ? 1 : (all + g.seg_kb - 1) / g.seg_kb;
 #pragma unroll 1
         for (uint32_t a = 0; a < uint32_t(S::kAcc); ++a) {
@@ -653,12 +672,12 @@ __global__ void __cluster_dims__(Shape<kShape>::kCtas, 1, 1) __launch_bounds__(T
             const uint32_t ta = tmem_base + (uint32_t(q * 32) << 16) + b * uint32_t(TN) + uint32_t(h * 64);
             if (s == 0) {
 #pragma unroll
-              for (int c = 0; c < 4; ++c) tmem_ld32(ta + (c & 1) * 32 + (c >> 1) * second, v + c * 32);
+              for (int c = 0; c < 4; ++c) tmem_ld32(ta + (c & 1) * 32 + (c >> 1) * HALF, v + c * 32);
             } else {
 #pragma unroll
               for (int c = 0; c < 4; ++c) {
                 float u[32];
-                tmem_ld32(ta + (c & 1) * 32 + (c >> 1) * second, u);
+                tmem_ld32(ta + (c & 1) * 32 + (c >> 1) * HALF, u);
 #pragma unroll
                 for (int i = 0; i < 32; ++i) v[c * 32 + i] += u[i];
               }
@@ -898,11 +917,12 @@ inline double cycles(int shape, int64_t m_tiles, int64_t cols, int64_t nkb, int 
   const double kb = double((nkb + splits - 1) / splits);
   return rounds * (kb_cycles(shape) * kb + tile_cycles(shape));
 }
-// rows: those of A, where 128 or fewer may take the single shape (0: they may not).
-inline int pick_shape(int64_t rows, int64_t m_tiles, int64_t cols, int64_t nkb, int splits) {
+// rows: those of A, where 128 or fewer may take the single shape (0: they may not).  wide_k: the longest k range
+// that the wide shape may sum.
+inline int pick_shape(int64_t rows, int64_t m_tiles, int64_t cols, int64_t nkb, int splits, int64_t wide_k = kWideK) {
   if (rows > 0 && rows <= HALF) return kSingle;
   const bool wide = cycles(kWide, m_tiles, cols, nkb, splits) < cycles(kNarrow, m_tiles, cols, nkb, splits);
-  return wide && nkb <= kWideK / BK * splits ? kWide : kNarrow;
+  return wide && nkb <= wide_k / BK * splits ? kWide : kNarrow;
 }
 
 // Width of the single shape's tiles: as few rounds of the CTAs as 256 columns would take, in equal parts
@@ -924,6 +944,7 @@ inline cudaError_t launch(const CUtensorMap& a, const CUtensorMap& b, const CUte
     if (g.arows == 0) g.arows = HALF;
     const int s = 12 * OPB / ((g.arows + g.width * (Ext::kTwin ? 2 : 1)) * 128);
     g.stages = s < Shape<kSingle>::kMostStages ? s : Shape<kSingle>::kMostStages;
+    if (Ext::kTwin) g.seg_kb = g.nkb;
   }
   g.n_tiles = (g.cols + g.width - 1) / g.width;
   cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM);
