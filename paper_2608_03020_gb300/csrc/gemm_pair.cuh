@@ -319,7 +319,8 @@ struct EpiScaled {
 // kAhead (narrow and single): what an epilogue has to look up for a tile is on its way while the sums are not
 // complete: a State for each thread; start(State, row of the first tile), ahead(State, row, half tile, row of the next
 // tile) before the sums; the state goes to row_of(), which also gets the first column, or to operator().  With
-// kPacks  bool simple(Row)  chooses for a warp between value1() and value().
+// kPacks  bool simple(Row)  chooses for a warp between value1() and value(), and in the single shape, where low_row is
+// not 0, store_parts(float (&)[32], row, column) takes the values of the rows before it.
 // kFits: the number of k ranges is the device's choice (Fit).
 template <int kShape, bool kAmn, bool kBmn, class Epi, class Ext>
 __global__ void __cluster_dims__(Shape<kShape>::kCtas, 1, 1) __launch_bounds__(THREADS, 1)
@@ -774,6 +775,25 @@ __global__ void __cluster_dims__(Shape<kShape>::kCtas, 1, 1) __launch_bounds__(T
           }();
           bool simple = false;
           if constexpr (Epi::kAhead) simple = epi.simple(pre);
+          if constexpr (Epi::kAhead && kShape == kSingle) {
+            if (epi.low_row > 0) {  // rows below low_row are given in two parts, the second low_row rows behind
+              if (q * 32 >= epi.low_row) continue;
+#pragma unroll 1
+              for (int b = 0; b < 4; ++b) {
+                if (col0 + 64 * (b >> 1) >= t.end) break;  // (whole k-blocks of what reads them)
+                float f[32];
+#pragma unroll
+                for (int i = 0; i < 32; ++i) {
+                  float z = 0.f;
+#pragma unroll
+                  for (int c = 0; c < 4; ++c) z = c == b ? v[32 * c + i] : z;
+                  f[i] = epi.value(pre, col0 + 32 * b + i, z);
+                }
+                epi.store_parts(f, row, col0 + 32 * b);
+              }
+              continue;
+            }
+          }
 #pragma unroll
           for (int b = 0; b < 2; ++b) {
             if (col0 + 64 * b >= (kSlim ? t.end : g.cols)) continue;

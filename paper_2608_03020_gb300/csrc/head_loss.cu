@@ -121,13 +121,14 @@ __device__ int count_live(const int32_t* __restrict__ y, int64_t n, int64_t V, i
 
 // Blocks 0 .. nb - 1 take kRowsPerBlock source rows each: the live ones move to their place among the
 // live rows, the others' outputs are zeroed.  The last kPadBlocks blocks write the zero rows behind.
+// dup > 0: the live rows (at most dup of them) come a second time, dup rows behind.
 // Bound: reads and writes 2 N d bytes each way; every block counts the labels before its own rows
 // (4 N bytes from L2), which keeps the pass one launch without a scan.
 __global__ void __launch_bounds__(256)
     k_head_rows(const __nv_bfloat16* __restrict__ H, int64_t ldh, int64_t N, int64_t d, int64_t V,
                 const int32_t* __restrict__ y, const float* __restrict__ w, const float* __restrict__ dloss,
                 const float* __restrict__ lse, Rows out, int64_t npad, int nb, float* loss0, float* lse0, float* E0,
-                int C, __nv_bfloat16* dH0, int64_t lddh) {
+                int C, __nv_bfloat16* dH0, int64_t lddh, int dup) {
   __shared__ int scratch[8];
   __shared__ int place[32];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -143,7 +144,8 @@ __global__ void __launch_bounds__(256)
     for (int64_t r = total + (blockIdx.x - nb) * 8 + warp; r < end; r += kPadBlocks * 8) {
       if (!LOCA_CHECK(r, npad)) break;
       uint4* dst = reinterpret_cast<uint4*>(out.H + r * d);
-      for (int64_t i = lane; i < dv; i += 32) dst[i] = make_uint4(0, 0, 0, 0);
+      if (dup == 0 || r < dup || r >= dup + total)
+        for (int64_t i = lane; i < dv; i += 32) dst[i] = make_uint4(0, 0, 0, 0);
       if (lane == 0) {
         out.idx[r] = -1;
         out.y[r] = -1;
@@ -180,6 +182,8 @@ __global__ void __launch_bounds__(256)
       uint4* dst = reinterpret_cast<uint4*>(out.H + int64_t(p) * d);
 #pragma unroll 8
       for (int64_t j = lane; j < dv; j += 32) dst[j] = __ldg(src + j);
+      if (dup > 0)
+        for (int64_t j = lane; j < dv; j += 32) dst[dup * dv + j] = __ldg(src + j);
     } else {
       if (lane == 0 && loss0) loss0[n] = 0.f;
       if (lane == 0 && lse0) lse0[n] = 0.f;
@@ -523,6 +527,29 @@ struct EpiDzTeacher {
   int64_t v_first;     // this piece's first vocabulary column
   int v_cols;          // its columns of the vocabulary
   int half_first;      // its first half tile
+  // Few rows: dZ in two bf16 parts (2^-17), the second low_row rows behind the first, where the tile of 128 rows has
+  // room for it, so that it costs no product.  The gradient of a row of few words is as good as its largest entries.
+  int low_row;
+  __nv_bfloat16* dz;
+  int64_t ldz;
+
+  __device__ __forceinline__ void store_parts(const float (&f)[32], int row, int col) const {
+    if (row >= low_row) return;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      uint32_t hi[4], lo[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float a = f[8 * j + 2 * i], b = f[8 * j + 2 * i + 1];
+        hi[i] = gp::pack_bf16(a, b);
+        const float2 r = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&hi[i]));
+        lo[i] = gp::pack_bf16(a - r.x, b - r.y);
+      }
+      if (col + 8 * j >= int(ldz) || !LOCA_CHECK_SPAN(col + 8 * j, 8, ldz)) continue;
+      *reinterpret_cast<uint4*>(dz + row * ldz + col + 8 * j) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+      *reinterpret_cast<uint4*>(dz + (row + low_row) * ldz + col + 8 * j) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+    }
+  }
 
   struct Row {
     float lse, g, q;
@@ -703,7 +730,7 @@ __global__ void __launch_bounds__(1024)
 // One thread per 8 elements of a row; the k ranges' sums are loaded four at a time and added in order.
 __global__ void __launch_bounds__(256)
     k_head_dh(const float* __restrict__ part, int64_t rows, int planned, const gp::Fit fit, int64_t d, Rows in,
-              int64_t row_first, float scale, __nv_bfloat16* __restrict__ dH, int64_t lddh) {
+              int64_t row_first, float scale, int low_row, __nv_bfloat16* __restrict__ dH, int64_t lddh) {
   wait_for_previous();
   launch_dependents();
   const int dv = int(d / 8);
@@ -733,6 +760,13 @@ __global__ void __launch_bounds__(256)
           a[4] += x[s][1].x; a[5] += x[s][1].y; a[6] += x[s][1].z; a[7] += x[s][1].w;
         }
     }
+    if (low_row > 0)  // the sums of dZ's second part
+      for (int s = 0; s < splits; ++s) {
+        const float4* p = reinterpret_cast<const float4*>(part + int64_t(s) * pitch + at + low_row * d);
+        const float4 x = p[0], y = p[1];
+        a[0] += x.x; a[1] += x.y; a[2] += x.z; a[3] += x.w;
+        a[4] += y.x; a[5] += y.y; a[6] += y.z; a[7] += y.w;
+      }
     uint4 q;
     q.x = gp::pack_bf16(scale * a[0], scale * a[1]);
     q.y = gp::pack_bf16(scale * a[2], scale * a[3]);
@@ -871,12 +905,12 @@ gp::Geo geo(int64_t m_tiles, int64_t cols, int64_t nkb, int seg_kb, const Rows& 
 
 cudaError_t launch_rows(const void* H, int64_t ldh, int64_t N, int64_t d, int64_t V, const int32_t* y, const float* w,
                         const float* dloss, const float* lse, const Rows& r, float* loss0, float* lse0, float* E0, int C,
-                        void* dH0, int64_t lddh, cudaStream_t s) {
+                        void* dH0, int64_t lddh, cudaStream_t s, int dup = 0) {
   const int64_t nb = (N + kRowsPerBlock - 1) / kRowsPerBlock;
   return gp::launch_early(k_head_rows, dim3(unsigned(nb + kPadBlocks)), dim3(256), 0, s,
                           static_cast<const __nv_bfloat16*>(H), ldh, N, d, V, y, w, dloss, lse, r,
                           round_up(N < 1 ? 1 : N, gp::TM), int(nb), loss0, lse0, E0, C,
-                          static_cast<__nv_bfloat16*>(dH0), lddh);
+                          static_cast<__nv_bfloat16*>(dH0), lddh, dup);
 }
 
 // The logit tiles of a forward piece; width: columns of a tile.
@@ -915,6 +949,7 @@ struct Backward {
   __nv_bfloat16* dW;
   int32_t* status;
   cudaStream_t s;
+  int low_row = 0;  // dZ has a second part so many rows behind the first (0: none)
 };
 
 // The logits of a piece once more, into dZ, in the forward pass's shape and segments, so that z comes out as it went
@@ -989,7 +1024,8 @@ cudaError_t backward_pieces(const Backward& b, const Before& before, const MakeD
             !gp::map_out_bf16(&mo, dW + v0 * d, d, vn, d))
           return cudaErrorInvalidValue;
         gp::Geo gw = geo(vtiles, d, np / gp::BK, kSegKbGrad, r, b.status);
-        gw.k_live = r.count;
+        if (b.low_row > 0) gw.nkb = 2 * b.low_row / gp::BK;  // both parts of dZ, against H twice
+        else gw.k_live = r.count;
         e = gp::launch_either<true, true>(mz_mn, mh_mn, mz_mn, mh_mn, mo, gw, gp::EpiScaled{b.scale}, gp::NoExt{}, b.s);
         if (e != cudaSuccess) return e;
       }
@@ -998,7 +1034,7 @@ cudaError_t backward_pieces(const Backward& b, const Before& before, const MakeD
       const int64_t blocks = rows * (d / 8) / 256 + 1;
       const int64_t most = 8 * int64_t(sm_count());
       e = gp::launch_early(k_head_dh, dim3(unsigned(blocks < most ? blocks : most)), dim3(256), 0, b.s,
-                           static_cast<const float*>(part), rows, lay.splits, fit, d, r, p0, b.scale, dH, lddh);
+                           static_cast<const float*>(part), rows, lay.splits, fit, d, r, p0, b.scale, b.low_row, dH, lddh);
       if (e != cudaSuccess) return e;
     }
   }
@@ -1176,16 +1212,18 @@ cudaError_t launch_head_distill_backward(const void* H, int64_t ldh, int64_t N, 
   cudaError_t e = launch_teacher(idx, t, N, V, K, tau, ws, wlay, &words, s);
   if (e != cudaSuccess) return e;
   const Rows r = rows_at(workspace, lay.rows);
-  e = launch_rows(H, ldh, N, d, 1, words.live, w, dloss, lse, r, nullptr, nullptr, nullptr, 0, dH, lddh, s);
+  const int low_row = N <= gp::HALF / 2 ? gp::HALF / 2 : 0;
+  e = launch_rows(H, ldh, N, d, 1, words.live, w, dloss, lse, r, nullptr, nullptr, nullptr, 0, dH, lddh, s, low_row);
   if (e != cudaSuccess) return e;
   const Backward b{lay, r, ws, N, d, static_cast<const __nv_bfloat16*>(W), V, scale, static_cast<__nv_bfloat16*>(dH), lddh,
-                   static_cast<__nv_bfloat16*>(dW), status, s};
+                   static_cast<__nv_bfloat16*>(dW), status, s, low_row};
   return backward_pieces(
       b, [](int64_t, int64_t) { return cudaSuccess; },
       [&](int64_t p0, int64_t rows, int64_t v0, int64_t vn) {
         return logit_tiles(b, p0, rows, v0, vn,
                            EpiDzTeacher{r.lse + p0, r.w + p0, r.idx + p0, words, tau, 1.f / tau, r.count, p0, v0, int(vn),
-                                        int(v0 / wlay.piece) * wlay.of_piece},
+                                        int(v0 / wlay.piece) * wlay.of_piece, b.low_row,
+                                        reinterpret_cast<__nv_bfloat16*>(ws + lay.dz), lay.vc},
                            wlay.width);
       });
 }

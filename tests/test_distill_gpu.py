@@ -290,3 +290,23 @@ def test_python_refusals(lc):
     for bad in (dict(dH=dH, dW=W), dict(dW=W), dict(dH=W[:10])):
         with pytest.raises(lc.LocaError, match="overlap"):
             lc.loca_head_distill_backward(H, W, idx, t, lse, **bad)
+
+
+@pytest.mark.parametrize("N,K", [(1, 1), (1, 3), (5, 1), (63, 2), (64, 1)])
+def test_few_positions_round_their_gradients_once(lc, N, K):
+    """Up to 64 positions dZ has two parts (2^-17): what is left is the gradients' own rounding, half a step (2^-8)
+    of each value, plus the products' 2^-15 (two parts and sums) of the sums of magnitudes, and where the student's
+    logits are off (2 ez of p) as in _check."""
+    H, W, idx, t, w, gl = _inputs(N, 264, 1999, K, mask="none")
+    out = _run(lc, H, W, idx, t, w, gl, 1.0, 1.0)
+    ref = _reference(H, W, idx, t, w, gl, 1.0, 1.0)
+    z = H.double() @ W.double().T
+    p = torch.softmax(z, 1)
+    dz = p.clone()
+    dz.scatter_add_(1, idx.long(), -torch.softmax(t.double(), 1))
+    dz = dz.abs() * (w * gl.abs()).double()[:, None]
+    ez = 2e-5 * (1 + ref["zmax"])
+    off = 2.0 ** -15 * dz + 3 * ez * p * (w * gl.abs()).double()[:, None]
+    for k, e in (("dH", off @ W.double().abs()), ("dW", off.T @ H.double().abs())):
+        tol = 2.0 ** -8 * ref[k].abs() + 1.01 * e + 1e-37
+        assert bool(((out[k].double() - ref[k]).abs() <= tol).all()), k
