@@ -251,8 +251,10 @@ __global__ void __launch_bounds__(kThreads, resident(NT)) k_q4(const __grid_cons
         auto load_x = [&](int q, bool full) {
 #pragma unroll
           for (int n = 0; n < NT; ++n)
-            xv[q & (kQ - 1)][n] = full || 128 * i + 32 * q < k_left ? __ldg(reinterpret_cast<const uint4*>(x[n] + 128 * i) + 4 * q)
-                                                                    : make_uint4(0, 0, 0, 0);
+            xv[q & (kQ - 1)][n] = (full || 128 * i + 32 * q < k_left) &&
+                                          LOCA_CHECK_SPAN(x[n] + 128 * i + 32 * q - g.X, 8, (g.N - 1) * g.ldx + g.d)
+                                      ? __ldg(reinterpret_cast<const uint4*>(x[n] + 128 * i) + 4 * q)
+                                      : make_uint4(0, 0, 0, 0);
         };
         const bool full = 128 * (i + 1) <= k_left;  // (else the last span of rows that are no multiple of 128)
         if (kQ == 4) {
@@ -339,7 +341,7 @@ __global__ void __launch_bounds__(kThreads, resident(NT)) k_q4(const __grid_cons
     for (int i = threadIdx.x; i < tokens * g.low.kp; i += kThreads) {
       const int n = i / g.low.kp, r = i - n * g.low.kp;
       float s = 0.f;
-      if (g.low.tok_adapter[n0 + n] >= 0)
+      if (g.low.tok_adapter[n0 + n] >= 0 && LOCA_CHECK(n0 + n, g.N))
         for (int q = 0; q < g.low.ranges; ++q) s += g.low.U[(int64_t(q) * g.N + n0 + n) * g.low.kp + r];
       u[i] = s;
     }
