@@ -1068,6 +1068,7 @@ struct AdapterExt {
   static constexpr bool kOn = true;
   static constexpr bool kSecond = false;
   static constexpr bool kTwin = false;
+  static constexpr bool kEarlyA = false;
   const int32_t* plan;
   int64_t tile_base, pair_count, pair_ad, pair_s0, pair_s1;
   int none_row;  // past the last slot: the loads fill zeros

@@ -232,13 +232,13 @@ gp::Geo geo(int64_t rows, int64_t cols, int64_t nkb, int32_t* status, void* work
   return g;
 }
 
-// Columns of the single shape's tiles, a multiple of 16 up to 128: what counts is how many rows of both operands
+// Columns of the single shape's tiles, a multiple of 8 up to 128: what counts is how many rows of both operands
 // a CTA fetches in all.  3584 x 14336 takes 150 tiles of 96.
 int twin_width(int64_t rows, int64_t cols) {
   const int64_t a = ceil_div(rows, 8) * 8;
   int64_t best = 0;
   int width = 0;
-  for (int w = 32; w <= 128; w += 16) {
+  for (int w = 32; w <= 128; w += 8) {
     const int64_t c = ceil_div(ceil_div(cols, w), sm_count()) * (a + 2 * w);
     if (width == 0 || c < best) {
       best = c;

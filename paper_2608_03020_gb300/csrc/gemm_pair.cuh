@@ -230,6 +230,7 @@ struct NoExt {
   static constexpr bool kOn = false;
   static constexpr bool kSecond = false;
   static constexpr bool kTwin = false;
+  static constexpr bool kEarlyA = false;
   __device__ int ksteps() const { return 4; }
   __device__ int entries(int) const { return 0; }
   __device__ void entry(int, int, uint32_t, int&, int&) const {}
@@ -303,6 +304,12 @@ struct EpiScaled {
   struct Row {};
   __device__ __forceinline__ Row row_of(int) const { return Row{}; }
   __device__ __forceinline__ float value(const Row&, int, float v) const { return scale * v; }
+};
+
+// Single shape: A is the caller's too, and only the epilogue needs the launch before (which lets this one start
+// after all launches before it have completed): the producer waits for it at its own end.
+struct CallersA : NoExt {
+  static constexpr bool kEarlyA = true;
 };
 
 // What becomes of a finished tile.  An output in bf16 is given value by value (kPacks): Row row_of(row)
@@ -405,7 +412,7 @@ __global__ void __cluster_dims__(Shape<kShape>::kCtas, 1, 1) __launch_bounds__(T
       int stage = 0;
       uint32_t phase = 0;
       uint32_t iter = 0;
-      bool ok = true, waited = !Ext::kOn;
+      bool ok = true, waited = !Ext::kOn && !(kEarlyB && Ext::kEarlyA);
       auto load = [&](uint32_t dst, const CUtensorMap* map, uint32_t bar, int c0, int c1) {
         if constexpr (kPair) tma_load_2d_pair(dst, map, bar, c0, c1);
         else tma_load_2d(dst, map, bar, c0, c1);
@@ -464,7 +471,7 @@ __global__ void __cluster_dims__(Shape<kShape>::kCtas, 1, 1) __launch_bounds__(T
             load_b(t, int(early), t.kb0 + int(early), full_bar(int(early)));
           }
         }
-        wait_for_previous();
+        if constexpr (!Ext::kEarlyA) wait_for_previous();
       }
       for (int it = cid; it < lv.total && ok; it += ncl) {
         const Tile t = tile_of(g, lv, it);
@@ -641,11 +648,11 @@ __global__ void __cluster_dims__(Shape<kShape>::kCtas, 1, 1) __launch_bounds__(T
       };
       const int r0 = row - lane;
       if constexpr (Ext::kTwin && kSlim) {
-        // Half of the tile's columns (a multiple of 8) of the first product, and the same of the second `width` columns
+        // Half of the tile's columns (in units of 8) of the first product, and the same of the second `width` columns
         // behind.  One sum per tile (launch()), and code that runs once: a loop over 8 columns straight from
         // tensor memory, whose instructions need not all be fetched for one tile (64 columns from registers at a
         // time: one token at 3584 x 14336 46.7 us, so 39.1).  Warps without a row do nothing.
-        const int half = g.width / 2, col0 = t.col0 + h * half, end = col0 + half < t.end ? col0 + half : t.end;
+        const int half = (g.width / 2 + 7) / 8 * 8, col0 = t.col0 + h * half, end = col0 + half < t.end ? col0 + half : t.end;
         const uint32_t b = seg & 1u;
         if (!(go = wait_sums(b, (seg >> 1) & 1u))) break;
         const uint32_t ta = tmem_base + (uint32_t(q * 32) << 16) + b * uint32_t(TN) + uint32_t(h * half);

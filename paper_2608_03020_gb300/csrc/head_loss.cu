@@ -430,11 +430,16 @@ struct WordState {
   int32_t n, next_n;
   uint32_t entry;
 };
-__device__ __forceinline__ void words_ahead(const Words& t, const int32_t* idx, WordState& s, int half, int next_row) {
+// idx: the rows' places in the call's order, or null where they stand in it (`rows` of them).
+__device__ __forceinline__ int32_t place_of(const int32_t* idx, int rows, int row) {
+  return idx ? idx[row] : row < rows ? row : -1;
+}
+__device__ __forceinline__ void words_ahead(const Words& t, const int32_t* idx, int rows, WordState& s, int half,
+                                            int next_row) {
   s.n = s.next_n;
   s.entry = kNoEntry;
   if (s.n >= 0 && LOCA_CHECK(half, t.pitch)) s.entry = __ldg(t.table + int64_t(s.n) * t.pitch + half);
-  s.next_n = idx[next_row];
+  s.next_n = place_of(idx, rows, next_row);
 }
 
 // v[i] for an i that differs from thread to thread: halves chosen bit by bit.
@@ -457,14 +462,15 @@ struct EpiTeacher {
   using State = WordState;
   float2* part;        // (2 column tiles) x pitch
   int64_t pitch;       // rows of a piece
-  const int32_t* idx;  // this piece's rows: their places in the call's order
+  const int32_t* idx;  // this piece's rows: their places in the call's order (null: `rows` of them in it)
+  int rows;
   Words words;
   float* zk;           // pitch x K
   float scale;         // log2(e) / tau
 
-  __device__ __forceinline__ void start(State& s, int row) const { s.next_n = idx[row]; }
+  __device__ __forceinline__ void start(State& s, int row) const { s.next_n = place_of(idx, rows, row); }
   __device__ __forceinline__ void ahead(State& s, int row, int half, int next_row) const {
-    words_ahead(words, idx, s, half, next_row);
+    words_ahead(words, idx, rows, s, half, next_row);
   }
   __device__ __forceinline__ void operator()(const gp::Tile& t, float (&v)[128], const State& st, int row, int col0, int lane,
                                              uint8_t*, const CUtensorMap*) const {
@@ -561,7 +567,7 @@ struct EpiDzTeacher {
   };
   __device__ __forceinline__ void start(State& s, int row) const { s.next_n = idx[row]; }
   __device__ __forceinline__ void ahead(State& s, int row, int half, int next_row) const {
-    words_ahead(words, idx, s, half_first + half, next_row);
+    words_ahead(words, idx, 0, s, half_first + half, next_row);
   }
   __device__ __forceinline__ Row row_of(int row, const State& st, int col0) const {
     Row r;
@@ -696,6 +702,71 @@ __global__ void __launch_bounds__(1024)
       loss[n] = in.w[k] * tau * tau * (words.ent[n] - sum);
       if (lse) lse[n] = m * inv_tau + log_s;
     }
+  }
+}
+
+// The same for few rows that stand in the call's order: a block per row.
+constexpr int kJoinThreads = 256;
+__global__ void __launch_bounds__(kJoinThreads)
+    k_teacher_join_few(const float2* __restrict__ part, int64_t pitch, int nparts, const float* __restrict__ zk, Words words,
+                       const float* __restrict__ w, float tau, float inv_tau, float* __restrict__ loss,
+                       float* __restrict__ lse) {
+  __shared__ float2 sh[kJoinThreads / 32];
+  __shared__ float sums[kJoinThreads / 32];
+  wait_for_previous();
+  launch_dependents();
+  const int n = blockIdx.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  if (words.live[n] < 0) {
+    if (threadIdx.x == 0) {
+      loss[n] = 0.f;
+      if (lse) lse[n] = 0.f;
+    }
+    return;
+  }
+  const float scale = kLog2e * inv_tau;
+  float m = -INFINITY, s = 0.f;
+  auto add = [&](float m2, float s2) {
+    const float mm = fmaxf(m, m2);
+    if (mm != -INFINITY) s = s * exp_scaled(m, mm, scale) + s2 * exp_scaled(m2, mm, scale);
+    else s += s2;  // keeps a NaN
+    m = mm;
+  };
+  constexpr int kMore = 4;
+  for (int p0 = threadIdx.x; p0 < nparts; p0 += kMore * kJoinThreads) {
+    float2 q[kMore];
+#pragma unroll
+    for (int i = 0; i < kMore; ++i)
+      q[i] = p0 + i * kJoinThreads < nparts ? part[int64_t(p0 + i * kJoinThreads) * pitch + n] : make_float2(-INFINITY, 0.f);
+#pragma unroll
+    for (int i = 0; i < kMore; ++i) add(q[i].x, q[i].y);
+  }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) {
+    const float m2 = __shfl_down_sync(0xffffffffu, m, o), s2 = __shfl_down_sync(0xffffffffu, s, o);
+    add(m2, s2);
+  }
+  if (lane == 0) sh[warp] = make_float2(m, s);
+  __syncthreads();
+  m = sh[0].x;
+  s = sh[0].y;
+  for (int i = 1; i < kJoinThreads / 32; ++i) add(sh[i].x, sh[i].y);
+  const float log_s = logf(s);
+  float sum = 0.f;
+  static_assert(kMostWords <= kJoinThreads, "a word a thread");
+  if (int(threadIdx.x) < words.K) {
+    const int64_t at = int64_t(n) * words.K + threadIdx.x;
+    const float q = words.q[at];
+    if (words.at[at] != kNoWord && !(q == 0.f)) sum = q * ((zk[at] - m) * inv_tau - log_s);
+  }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+  if (lane == 0) sums[warp] = sum;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    sum = sums[0];
+    for (int i = 1; i < kJoinThreads / 32; ++i) sum += sums[i];
+    loss[n] = (w ? w[n] : 1.f) * tau * tau * (words.ent[n] - sum);
+    if (lse) lse[n] = m * inv_tau + log_s;
   }
 }
 
@@ -1183,14 +1254,34 @@ cudaError_t launch_head_distill(const void* H, int64_t ldh, int64_t N, int64_t d
   cudaError_t e = launch_teacher(idx, t, N, V, K, tau, ws, lay.words, &words, s);
   if (e != cudaSuccess) return e;
   const Rows r = rows_at(workspace, lay.fwd.rows);
-  e = launch_rows(H, ldh, N, d, 1, words.live, w, nullptr, nullptr, r, loss, lse, nullptr, 0, nullptr, 0, s);
-  if (e != cudaSuccess) return e;
   float2* part = reinterpret_cast<float2*>(ws + lay.fwd.part);
   float* zk = reinterpret_cast<float*>(ws + lay.zk);
+  if (N <= gp::HALF) {
+    // Few rows cost the same with the masked ones among them (a row's sums are its own): nothing is gathered, and
+    // the product reads hidden states and head while k_teacher runs.  37 tokens at 2048 x 49152: 56.5 us with
+    // the gathering, 51 without.
+    const int width = lay.words.width, arows = int(round_up(N, 8));
+    CUtensorMap ma, mb;
+    if (!gp::map_2d(&mb, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, W, d, V, d, gp::BK, width / 2) ||
+        !gp::map_2d(&ma, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, H, d, N, ldh, gp::BK, arows))
+      return cudaErrorInvalidValue;
+    gp::Geo g = geo(1, V, (d + gp::BK - 1) / gp::BK, kSegKbFew, r, status);
+    g.width = width;
+    g.arows = arows;
+    g.mark = gp::call_mark();
+    e = gp::launch<gp::kSingle, false, false>(
+        ma, mb, ma, mb, ma, g, EpiTeacher{part, lay.fwd.piece, nullptr, int(N), words, zk, kLog2e / tau}, gp::CallersA{}, s);
+    if (e != cudaSuccess) return e;
+    return gp::launch_early(k_teacher_join_few, dim3(unsigned(N)), dim3(kJoinThreads), 0, s,
+                            static_cast<const float2*>(part), lay.fwd.piece, lay.words.of_piece, static_cast<const float*>(zk),
+                            words, w, tau, 1.f / tau, loss, lse);
+  }
+  e = launch_rows(H, ldh, N, d, 1, words.live, w, nullptr, nullptr, r, loss, lse, nullptr, 0, nullptr, 0, s);
+  if (e != cudaSuccess) return e;
   const int64_t np = round_up(N, gp::TM);
   for (int64_t p0 = 0; p0 < np; p0 += lay.fwd.piece) {
     const int64_t rows = np - p0 < lay.fwd.piece ? np - p0 : lay.fwd.piece;
-    e = forward_tiles(r, N, p0, rows, d, W, V, EpiTeacher{part, lay.fwd.piece, r.idx + p0, words, zk, kLog2e / tau}, status,
+    e = forward_tiles(r, N, p0, rows, d, W, V, EpiTeacher{part, lay.fwd.piece, r.idx + p0, 0, words, zk, kLog2e / tau}, status,
                       lay.words.width, s);
     if (e != cudaSuccess) return e;
     const int nparts = lay.words.of_piece;

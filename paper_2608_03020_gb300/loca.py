@@ -791,7 +791,7 @@ def _same_device(*tensors):
     """The call runs on the current device: refuses tensors of another one."""
     here = torch.cuda.current_device()
     for t in tensors:
-        if t is not None and t.device.index != here:
+        if t is not None and t.get_device() != here:
             raise ValueError(f"a tensor is on {t.device}, the current device is cuda:{here}")
 
 
