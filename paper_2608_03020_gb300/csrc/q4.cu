@@ -15,11 +15,11 @@
 //               shared memory (each lane copies and reads its own 16 bytes, so that it waits for nothing else);
 //               ks warps' sums meet in shared memory, in order, with the low-rank term of each token's adapter
 //               (U in fp32 from k_adapter_tokens); one rounding
-// Bound: up to 16 tokens the instructions that make operands of codes (a span takes 44 of some 75 for 64 of its k;
-// 58 to 70 % of the issue slots and of the integer pipe), next to the read of the codes and scales; above, X's way
-// from L2 for every 16 rows, and the legacy MMAs' rate (1024 products a cycle and SM).  One token at
-// 28672 x 8192 30.9 us (3.9 TB/s), 3 tokens at 151931 x 2048 with groups of 32 51 us (3.9 TB/s), 8 tokens at
-// 20480 x 5120 20 us (2.9 TB/s), 16, 32 and 64 tokens at 14336 x 3584 14.8, 23 and 43 us.
+// Bound: up to 16 tokens the instructions that make operands of codes (44 of some 80 for 64 k of 16 rows; 60 to 70 % of
+// the issue slots), next to the read of the codes and scales; above, X's way from L2 for every 16 rows, and
+// the legacy MMAs' rate (1024 products a cycle and SM).  One token at 28672 x 8192 25.8 us (4.7 TB/s), 3 tokens at
+// 151931 x 2048 with groups of 32 48 us (4.2 TB/s), at 20480 x 5120 16.5 us for one token and 20 for eight (2.7 TB/s),
+// 16, 32 and 64 tokens at 14336 x 3584 14.4, 25 and 42 us.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
@@ -130,7 +130,8 @@ __device__ __forceinline__ void mma_16816(float (&c)[4], const uint32_t (&a)[4],
 // bf16 pattern 0x4300 | q, and so has 128 + z; their difference is exact.
 template <int kShift>
 __device__ __forceinline__ uint32_t two_codes(uint32_t w, __nv_bfloat162 zero) {
-  const uint32_t q = ((w >> kShift) & 0x000f000fu) | 0x43004300u;
+  uint32_t q;  // (codes & mask) | pattern: one instruction, where the compiler made two (36 instead of 52 of the integer pipe for 64 k)
+  asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(q) : "r"(w >> kShift), "n"(0x000f000f), "r"(0x43004300u));
   const __nv_bfloat162 v = __hsub2(*reinterpret_cast<const __nv_bfloat162*>(&q), zero);
   return *reinterpret_cast<const uint32_t*>(&v);
 }
@@ -377,8 +378,8 @@ __global__ void __launch_bounds__(kThreads, resident(NT)) k_q4(const __grid_cons
 
 // Warps on the same rows: more of them shorten a warp's way through k, and add a block's start and end (about
 // 2 us, and 0.4 for each that shares the SM) for each of its fewer spans.  A span takes a lone block's warps 0.62 us; eight warps' worth of a span
-// keeps an SM busy for `busy` of it, whatever shares the SM.  20480 x 5120, 8 tokens: 28.6 us with one warp, 22.3 with
-// two, 20.0 with four, 20.6 with eight; 3584 x 3584, one token: 15.3, 9.5, 6.5 and 5.6.
+// keeps an SM busy for `busy` of it, whatever shares the SM.  20480 x 5120, 8 tokens: 28.6 us with one warp, 21.0 with
+// two, 20.0 with four, 20.2 with eight; 3584 x 3584, one token: 7.2, 4.7 and 3.9 with two, four and eight.
 template <int NT>
 void share_rows(Q4Geo& g, int64_t sets) {
   constexpr double busy = NT <= 2 ? 0.44 : NT == 4 ? 0.8 : 1.2;
