@@ -79,7 +79,8 @@ int loca_version(void);
  * tensor memory and returns, so the context stays usable.  This sets, for the whole process,
  * how long such a wait may take in the tensor-core kernels (loca_targets, loca_kspace_accumulate,
  * the CTA-pair Gram / cross kernel of loca_gram_cross, loca_accumulate and their variants, the
- * projection of loca_ridge_solve, loca_head_loss, loca_adapter_apply and their backward calls)
+ * projection of loca_ridge_solve, loca_head_loss, loca_head_distill, loca_adapter_apply, loca_gated
+ * and their backward calls, loca_q4_apply)
  * before it gives up: ns = 0 restores the default of 4 s; a tiny value makes a call time out on
  * purpose, to test that path.
  */
@@ -613,11 +614,12 @@ int loca_adapter_backward(const void* X, int64_t ldx, const void* dY, int64_t ld
  * loca_q4_apply  Y (N x d_out bf16, row pitch ldy, 2-byte aligned) of X (N x d_in bf16, 16-byte aligned, row pitch a
  *                multiple of 8).  group, scale_dtype and with_zeros as packed.  adapters: what loca_adapter_pack
  *                packed of n adapters of rank k for d_out x d_in, with the tokens' plan (loca_adapter_plan),
- *                and then d_out as loca_adapter_apply takes it; or NULL (plan NULL, n and k 0).  It reads the
- *                weights once for up to 64 tokens, and again for every 64 more
- * Arithmetic: q - z and X are exact in bf16, their products are summed in fp32 over up to 64 terms of a group and
- * scaled in fp32: W is never rounded.  The low-rank term as in loca_adapter_apply, U in fp32.  Y is rounded
- * once.  Deterministic.  Y may not overlap X (rows side by side in one buffer do not).
+ *                and then d_out as loca_adapter_apply takes it; or NULL (plan NULL, n and k 0).  workspace of
+ *                loca_q4_workspace_size bytes, 256-byte aligned, with or without adapters.  It reads the weights
+ *                once for up to 128 tokens (64 with groups of 32 or 64) and again for as many more
+ * Arithmetic: q - z and X are exact in bf16, their products are summed in fp32 over a group and scaled in fp32: W is
+ * never rounded.  The low-rank term as in loca_adapter_apply, U in fp32.  Y is rounded once.  Deterministic.
+ * With more than 16 tokens the kernel's waits are bounded (loca_set_wait_limit).  Y may not overlap X (rows side by side in one buffer do not).
  */
 int loca_q4_packed_size(int64_t d_out, int64_t d_in, int32_t group, int scale_dtype, int with_zeros, size_t* bytes);
 int loca_q4_pack(const void* codes, const void* scales, int scale_dtype, const void* zeros, int64_t d_out, int64_t d_in,

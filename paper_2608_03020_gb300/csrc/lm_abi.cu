@@ -423,11 +423,8 @@ int loca_q4_workspace_size(int64_t N, int64_t d_in, int64_t d_out, int32_t k, in
   int rc = check_q4(d_out, d_in, 32, LOCA_F32);
   if (rc != LOCA_OK) return rc;
   if (N < 0 || N > 65535) return fail(LOCA_ERR_SHAPE, "need 0 <= N <= 65535, got %lld", (long long)N);
-  *bytes = 0;
-  if (n == 0 && k == 0) return LOCA_OK;
-  rc = check_adapter(N, d_in, d_out, k, n);
-  if (rc != LOCA_OK) return rc;
-  *bytes = N > 0 ? adapter_tokens_workspace_bytes(N, d_in, k) : 0;
+  if ((n != 0 || k != 0) && (rc = check_adapter(N, d_in, d_out, k, n)) != LOCA_OK) return rc;
+  *bytes = q4_workspace_bytes(N, d_in, k);
   return LOCA_OK;
 }
 
@@ -447,10 +444,12 @@ int loca_q4_apply(const void* X, int64_t ldx, int64_t N, int64_t d_in, const voi
   if (ldy < d_out) return fail(LOCA_ERR_SHAPE, "row pitch of Y %lld is below its %lld columns", (long long)ldy, (long long)d_out);
   if (!aligned(Y, 2) || !aligned(packed, 256) || !aligned(adapters, 256) || !aligned(plan, 256))
     return fail(LOCA_ERR_ALIGNMENT, "Y needs 2-byte, packed, adapters and plan 256-byte alignment");
-  if (adapters && (rc = check_ws(workspace, workspace_bytes, adapter_tokens_workspace_bytes(N, d_in, k))) != LOCA_OK) return rc;
+  if ((rc = check_ws(workspace, workspace_bytes, q4_workspace_bytes(N, d_in, k))) != LOCA_OK) return rc;
   if (overlap(Matrix{X, N, ldx, d_in}, Matrix{Y, N, ldy, d_out})) return fail(LOCA_ERR_INVALID_ARG, "Y must not overlap X");
+  int32_t* status = device_status_word();
+  if (!status) return fail(LOCA_ERR_CUDA, "cannot resolve the device status word");
   const cudaError_t e = launch_q4_apply(X, ldx, N, d_in, packed, d_out, group, scale_dtype, with_zeros != 0, adapters, n, k,
-                                        plan, Y, ldy, workspace, static_cast<cudaStream_t>(stream));
+                                        plan, Y, ldy, workspace, status, static_cast<cudaStream_t>(stream));
   if (e != cudaSuccess) return cuda_fail(e, "loca_q4_apply launch");
   return LOCA_OK;
 }

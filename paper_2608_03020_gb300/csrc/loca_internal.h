@@ -216,7 +216,8 @@ cudaError_t launch_q4_pack(const void* codes, const void* scales, int scale_dtyp
                            int group, void* packed, cudaStream_t s);
 cudaError_t launch_q4_apply(const void* X, int64_t ldx, int64_t N, int64_t d, const void* packed, int64_t o, int group,
                             int scale_dtype, bool zeros, const void* adapters, int n, int k, const void* plan, void* Y,
-                            int64_t ldy, void* workspace, cudaStream_t s);
+                            int64_t ldy, void* workspace, int32_t* status, cudaStream_t s);
+size_t q4_workspace_bytes(int64_t N, int64_t d, int k);
 
 // ---- gated feed-forward (gated.cu)
 size_t gated_workspace_bytes();

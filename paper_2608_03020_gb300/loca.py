@@ -992,7 +992,8 @@ def q4_workspace_size(N, d_in, d_out, k=0, n=0) -> int:
 def loca_q4_apply(X, weight, Y, adapters=None, plan=None, workspace=None, stream=None):
     """``Y = X W^T + s_a (X A_a) B_a^T`` for a few tokens with a 4-bit ``weight`` (a :class:`Q4Weight`): ``X`` N x d_in
     and ``Y`` N x d_out bf16 (rows may be spaced); ``adapters`` (an :class:`AdapterSet`) and ``plan`` (an
-    :class:`AdapterPlan` of the tokens' adapters), or neither."""
+    :class:`AdapterPlan` of the tokens' adapters), or neither.  More than a few tokens too: it reads the weight again
+    for every 128 of them (64 with groups below 128)."""
     ldx = _rows2d(X, "X", torch.bfloat16)
     N, d_in = X.shape
     if d_in != weight.d_in:

@@ -126,7 +126,7 @@ def test_q4_sizes(L):
     for bad in ((0, 64, 32), (64, 0, 32), (64, 48, 32), (64, 64, 16), (64, 64, 128), (64, 65568, 32), ((1 << 24) + 1, 64, 32)):
         assert _size(L.loca_q4_packed_size, *bad, 0, 0)[0] == 2, bad
     assert _size(L.loca_q4_packed_size, 64, 64, 32, 3, 0)[0] == 4
-    assert _size(L.loca_q4_workspace_size, 64, 5120, 20480, 0, 0) == (0, 0)
+    assert _size(L.loca_q4_workspace_size, 64, 5120, 20480, 0, 0) == (0, 256)
     rc, n = _size(L.loca_q4_workspace_size, 64, 5120, 20480, 16, 4)
     assert rc == 0 and n >= 64 * 16 * 4
     assert _size(L.loca_q4_workspace_size, 64, 5120, 20481, 16, 4)[0] == 2  # adapters want multiples of 8

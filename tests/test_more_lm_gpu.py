@@ -260,6 +260,7 @@ LONG = {
     "gated": (lambda lc: _gated(lc, _plain, 1000, 16384, 2048), True),
     "gated, narrow tiles": (lambda lc: _gated(lc, _plain, 700, 20000, 1024), True),
     "gated, few tokens": (lambda lc: _gated(lc, _plain, 64, 8192, 4096), False),
+    "q4, many tokens": (lambda lc: _q4(lc, _plain, 200, 65536, 1024, 64, 8, 2), True),
 }
 
 

@@ -119,6 +119,18 @@ def test_adapters(lc, N, o, d, k, n, dtype):
     _check(lc, _tokens(N, d), lc.Q4Weight(codes, scales, zeros=z), W, _adapters(lc, N, d, o, k, n, dtype))
 
 
+@pytest.mark.parametrize("zeros", [False, True])
+@pytest.mark.parametrize("N,o,d,group,k,n", [
+    (17, 136, 256, 128, 4, 2), (32, 64, 65536, 64, 0, 0), (33, 128, 128, 32, 8, 1), (100, 264, 2048, 128, 8, 3),
+    (128, 2000, 1152, 128, 0, 0), (129, 8, 512, 128, 33, 5), (300, 392, 640, 128, 16, 4), (257, 1000, 256, 64, 0, 0),
+])
+def test_many_tokens(lc, N, o, d, group, k, n, zeros):
+    """Every width of the tokens' tiles and of the clusters on the same rows, several tiles of tokens, ragged ones."""
+    codes, scales, z, W = _weight(o, d, group, torch.bfloat16 if zeros else torch.float32, zeros)
+    ad = _adapters(lc, N, d, o, k, n, torch.bfloat16) if n else None
+    _check(lc, _tokens(N, d), lc.Q4Weight(codes, scales, zeros=z), W, ad)
+
+
 @pytest.mark.parametrize("ids", [-1, 0])
 def test_all_tokens_without_or_with_one_adapter(lc, ids):
     codes, scales, z, W = _weight(264, 512, 128, torch.float32, False)
