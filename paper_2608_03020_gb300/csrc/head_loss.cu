@@ -504,13 +504,13 @@ struct EpiTeacher {
     int at = st.entry & 127, k = st.entry >> 7 & 255;
     bool more = st.entry >> 15 & 1;
     while (__any_sync(0xffffffffu, here)) {
+      const bool on = here && more && k + 1 < words.K;
+      const int32_t next = on ? __ldg(words.at + int64_t(st.n) * words.K + k + 1) : kNoWord;  // (back before pick() is)
       const float z = pick(v, at);
       if (here && LOCA_CHECK(k, words.K)) zk[int64_t(row) * words.K + k] = z;
-      here = here && more && ++k < words.K;
-      if (here) {
-        at = __ldg(words.at + int64_t(st.n) * words.K + k) - col0;
-        here = at < left;
-      }
+      here = on && next < col0 + left;
+      at = next - col0;
+      ++k;
     }
   }
 };
@@ -596,10 +596,8 @@ struct EpiDzTeacher {
       r.next = kNoWord;
       if (++r.k < words.K) {
         const int32_t v = __ldg(words.at + r.from + r.k);
-        if (v != kNoWord) {
-          r.next = int(v - v_first);
-          r.q = __ldg(words.q + r.from + r.k);
-        }
+        r.q = __ldg(words.q + r.from + r.k);  // (with it, not behind it: behind the last word nobody takes it)
+        if (v != kNoWord) r.next = int(v - v_first);
       }
     }
     return r.g * p;
