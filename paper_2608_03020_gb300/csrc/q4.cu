@@ -158,6 +158,21 @@ __device__ __forceinline__ void copy_wait() {
   asm volatile("cp.async.wait_group %0;" ::"n"(kLeft) : "memory");
 }
 
+// U[n, r], the sum over the ranges of k in order, eight of them on the way at a time.
+__device__ __forceinline__ float low_sum(const Q4Geo& g, int64_t n, int r) {
+  const float* u = g.low.U + n * g.low.kp + r;
+  const int64_t pitch = g.N * g.low.kp;
+  float sum = 0.f;
+  for (int c = 0; c < g.low.ranges; c += 8) {
+    float x[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = c + i < g.low.ranges ? u[(c + i) * pitch] : 0.f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) sum += x[i];
+  }
+  return sum;
+}
+
 // kGroups: of 128 k (1, 2 or 4).
 template <int NT, int kGroups>
 __global__ void __launch_bounds__(kThreads, resident(NT)) k_q4(const __grid_constant__ Q4Geo g) {
@@ -331,10 +346,7 @@ __global__ void __launch_bounds__(kThreads, resident(NT)) k_q4(const __grid_cons
   if (g.low.U)
     for (int i = threadIdx.x; i < tokens * g.low.kp; i += kThreads) {
       const int n = i / g.low.kp, r = i - n * g.low.kp;
-      float s = 0.f;
-      if (g.low.tok_adapter[n] >= 0 && LOCA_CHECK(n, g.N))
-        for (int q = 0; q < g.low.ranges; ++q) s += g.low.U[(int64_t(q) * g.N + n) * g.low.kp + r];
-      u[i] = s;
+      u[i] = g.low.tok_adapter[n] >= 0 && LOCA_CHECK(n, g.N) ? low_sum(g, n, r) : 0.f;
     }
   __syncthreads();
   for (int i = threadIdx.x; i < rows * tokens; i += kThreads) {
@@ -418,6 +430,8 @@ cudaError_t launch_tokens(const Q4Geo& g, cudaStream_t s) {
 // 3584: 31.7 us so, 23.5 with whole spans, 21.8 with 32 rows).  Times at 14336 x 3584: 32 tokens 20.7 us (k_q4, built for
 // as many: 25.3), 64 21.8 (42.2), 128 26.9, 512 with groups of 64 139; 64 at 151931 x 2048 118 (246); 24 at 20480 x 5120
 // with groups of 64 50.0 (48.7: 160 tiles are two rounds of the SMs).
+// A token's adapter is multiplied at the end, a row a lane: 25 tokens of rank 24 at 55544 x 6016 125 us, 99 without
+// (their rows brought to L2 meanwhile, as k_q4 does, took 2 us more; all of a row's loads at once 8).
 // Every wait is bounded; the failure path is that of the adapters' kernels.
 constexpr int kTileThreads = 576;
 constexpr int kDequantWarps = 8, kSumWarps = 8;
@@ -682,30 +696,29 @@ __global__ void __launch_bounds__(kTileThreads, 1)
     if (a >= 0) {
       float* u = us + warp * p.low.kp;
       __syncwarp();
-      for (int r = lane; r < p.low.kp; r += 32) {
-        float sum = 0.f;
-        for (int c = 0; c < p.low.ranges; ++c) sum += p.low.U[(int64_t(c) * p.N + n0 + n) * p.low.kp + r];
-        u[r] = sum;
-      }
+      for (int r = lane; r < p.low.kp; r += 32) u[r] = low_sum(p, n0 + n, r);
       __syncwarp();
+      float low[4] = {};
+      const __nv_bfloat16* b = p.low.B + (int64_t(a) * p.o + o0 + lane) * p.low.kp;
+#pragma unroll 1
+      for (int c = 0; c < p.low.kp; c += 8) {
+        uint4 v[4];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const int64_t row = o0 + 32 * j + lane;
-        if (row >= p.o) continue;
-        const uint4* b = reinterpret_cast<const uint4*>(p.low.B + (int64_t(a) * p.o + row) * p.low.kp);
-        float s = 0.f;
-        for (int c = 0; c < p.low.kp / 8; ++c) {
-          const uint4 v = __ldg(b + c);
-          const __nv_bfloat162* hh = reinterpret_cast<const __nv_bfloat162*>(&v);
+        for (int j = 0; j < 4; ++j)
+          v[j] = o0 + 32 * j + lane < p.o ? __ldg(reinterpret_cast<const uint4*>(b + 32 * j * p.low.kp + c)) : make_uint4(0, 0, 0, 0);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const __nv_bfloat162* hh = reinterpret_cast<const __nv_bfloat162*>(&v[j]);
 #pragma unroll
           for (int k = 0; k < 4; ++k) {
             const float2 f = __bfloat1622float2(hh[k]);
-            s = fmaf(u[8 * c + 2 * k], f.x, s);
-            s = fmaf(u[8 * c + 2 * k + 1], f.y, s);
+            low[j] = fmaf(u[c + 2 * k], f.x, low[j]);
+            low[j] = fmaf(u[c + 2 * k + 1], f.y, low[j]);
           }
         }
-        y[j] += s;
       }
+#pragma unroll
+      for (int j = 0; j < 4; ++j) y[j] += low[j];
     }
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
