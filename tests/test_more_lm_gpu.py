@@ -117,6 +117,8 @@ PROGRAMS = {
     "q4, one token": lambda lc, mk: _q4(lc, mk, 1, 640, 264, 128, 16, 3),
     "q4, decode": lambda lc, mk: _q4(lc, mk, 40, 1056, 1000, 32, 24, 40),
     "q4, two blocks of tokens": lambda lc, mk: _q4(lc, mk, 100, 512, 136, 64, 8, 3),
+    "q4, sixteen tokens": lambda lc, mk: _q4(lc, mk, 16, 1056, 264, 32, 8, 5),
+    "q4, tiles of 128 tokens": lambda lc, mk: _q4(lc, mk, 150, 1152, 264, 128, 16, 3),
 }
 
 
