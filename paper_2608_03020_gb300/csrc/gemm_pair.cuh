@@ -902,6 +902,19 @@ inline bool map_out_bf16(CUtensorMap* m, void* base, int64_t cols, int64_t rows,
   return map_2d(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, base, cols, rows, pitch, 64, 32);
 }
 
+// Lets a kernel have `bytes` of dynamic shared memory, asked for once on each device (`done`: a bit for each, of that
+// kernel alone), which saves 0.45 us of the host's time for a launch.
+inline cudaError_t allow_smem(std::atomic<uint64_t>& done, const void* kernel, int bytes) {
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  const uint64_t bit = dev < 64 ? uint64_t(1) << dev : 0;
+  if (done.load(std::memory_order_acquire) & bit) return cudaSuccess;
+  e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  if (e == cudaSuccess) done.fetch_or(bit, std::memory_order_release);
+  return e;
+}
+
 // Small kernels between those with 200 KB of shared memory ask for the same split of L1: changing it
 // drains the SM (64 single tokens through an adapted projection: 27.1 us with the change, 23.4 without).
 template <class K>
@@ -961,8 +974,9 @@ inline int slim_width(int64_t cols, int unit = 16) {
   return int((w + unit - 1) / unit * unit);
 }
 
+// (static: a kernel of the same name is another one in each source file, with an `allowed` of its own.)
 template <int kShape, bool kAmn, bool kBmn, class Epi, class Ext>
-inline cudaError_t launch(const CUtensorMap& a, const CUtensorMap& b, const CUtensorMap& ax, const CUtensorMap& bx,
+static cudaError_t launch(const CUtensorMap& a, const CUtensorMap& b, const CUtensorMap& ax, const CUtensorMap& bx,
                           const CUtensorMap& o, Geo g, const Epi& epi, const Ext& ext, cudaStream_t s) {
   auto kernel = k_gemm_pair<kShape, kAmn, kBmn, Epi, Ext>;
   constexpr int kCtas = Shape<kShape>::kCtas;
@@ -974,7 +988,8 @@ inline cudaError_t launch(const CUtensorMap& a, const CUtensorMap& b, const CUte
     if (Ext::kTwin) g.seg_kb = g.nkb;
   }
   g.n_tiles = (g.cols + g.width - 1) / g.width;
-  cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM);
+  static std::atomic<uint64_t> allowed{0};
+  cudaError_t e = allow_smem(allowed, reinterpret_cast<const void*>(kernel), SMEM);
   if (e != cudaSuccess) return e;
   const int64_t total = int64_t(g.m_tiles) * g.n_tiles * g.splits;
   if (total < 1) return cudaSuccess;

@@ -404,7 +404,8 @@ template <int NT, int kGroups>
 cudaError_t launch_one(Q4Geo g, cudaStream_t s) {
   share_rows<NT>(g);
   const int sums = 4 * (kWarps * 8 * NT * 16 + (g.low.U ? 8 * NT * g.low.kp : 0)), rings = kWarps * warp_bytes(kGroups);
-  const cudaError_t e = cudaFuncSetAttribute(k_q4<NT, kGroups>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxSmem);
+  static std::atomic<uint64_t> allowed{0};
+  const cudaError_t e = gp::allow_smem(allowed, reinterpret_cast<const void*>(k_q4<NT, kGroups>), kMaxSmem);
   if (e != cudaSuccess) return e;
   return gp::launch_early(k_q4<NT, kGroups>, dim3(unsigned(div_up(g.tiles, kWarps / g.ks))), dim3(kThreads),
                           size_t(sums > rings ? sums : rings), s, g);
@@ -765,7 +766,8 @@ cudaError_t launch_tiles(const Q4Geo& q, void* flag, int32_t* status, cudaStream
   }
   g.per_cta = int(div_up(q.spans, ks));
   auto kernel = k_q4_tiles<kHalf, kGroups>;
-  cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kTileSmem);
+  static std::atomic<uint64_t> allowed{0};
+  cudaError_t e = gp::allow_smem(allowed, reinterpret_cast<const void*>(kernel), kTileSmem);
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(unsigned(rows * ks), unsigned(sets));

@@ -180,11 +180,15 @@ def _check(rc: int, where: str):
 
 
 def _ptr(t):
-    return None if t is None else ctypes.c_void_p(t.data_ptr())
+    return None if t is None else t.data_ptr()
 
 
 # handle of the current stream without building a Stream object (3 us of a call that takes 6)
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
+# the current device of a process that has CUDA tensors (a third of torch.cuda.current_device()'s 0.26 us)
+_get_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 
 
 def _stream(stream):
@@ -789,7 +793,7 @@ def loca_head_loss_backward(H, W, y, lse, dH=None, dW=None, w=None, dloss=None, 
 
 def _same_device(*tensors):
     """The call runs on the current device: refuses tensors of another one."""
-    here = torch.cuda.current_device()
+    here = _get_device()
     for t in tensors:
         if t is not None and t.get_device() != here:
             raise ValueError(f"a tensor is on {t.device}, the current device is cuda:{here}")
