@@ -904,6 +904,7 @@ struct BwdWs {
   int64_t piece;  // rows of dZ
   int64_t vc;     // vocabulary columns of dZ (a multiple of 256)
   int splits;     // k ranges of dH
+  int room;       // row tiles x ranges that the sums' memory holds
   size_t dz, part, others, sum, total;
 };
 bool few_rows(int64_t N) { return N > 0 && N <= gp::HALF; }
@@ -932,7 +933,9 @@ int dh_splits(int64_t n, int64_t rows, int64_t d, int64_t vc) {
   }
   return best;
 }
-BwdWs bwd_ws(int64_t N, int64_t V, int64_t d, bool dh, bool dw, bool target) {
+// fill: room for as many ranges of the live rows as fill four rounds of the pairs (fit_splits(); without it 3081 live of 4096
+// tokens at d = 2048, V = 49152 are three rounds of 256 k-blocks, with it three of 192: dH of distillation 952 and 855 us).
+BwdWs bwd_ws(int64_t N, int64_t V, int64_t d, bool dh, bool dw, bool target, bool fill) {
   BwdWs o{};
   o.rows = rows_ws(N, d);
   const int64_t np = round_up(N < 1 ? 1 : N, gp::TM);
@@ -949,9 +952,17 @@ BwdWs bwd_ws(int64_t N, int64_t V, int64_t d, bool dh, bool dw, bool target) {
   const int64_t chunks = (vp + vc - 1) / vc;
   o.vc = round_up((vp + chunks - 1) / chunks, gp::TN);
   o.splits = dh ? dh_splits(N, o.piece, d, o.vc) : 0;
+  const int64_t m = o.piece / gp::TM;
+  o.room = int(o.splits * m);
+  if (fill && dh && !few_rows(N)) {
+    const int64_t ranges = o.vc / gp::BK / 16 < 32 ? o.vc / gp::BK / 16 : 32;  // (at most: as fit_splits())
+    int64_t room = 4 * (sm_count() / 2) / ((d + 2 * gp::TN - 1) / (2 * gp::TN));
+    if (room > m * ranges) room = m * ranges;
+    if (room > o.room) o.room = int(room);
+  }
   size_t at = o.rows.total;
   o.dz = at; at += align256(2 * size_t(o.piece) * size_t(o.vc));
-  o.part = at; at += align256(4 * size_t(o.splits) * size_t(o.piece) * size_t(d));
+  o.part = at; at += align256(4 * size_t(o.room) * gp::TM * size_t(d));
   o.others = at; at += target ? align256(4 * 2 * size_t(dz_tiles(N, o.vc)) * size_t(o.piece)) : 0;
   o.sum = at; at += target ? align256(4 * size_t(o.piece)) : 0;
   o.total = at;
@@ -1059,7 +1070,7 @@ cudaError_t backward_pieces(const Backward& b, const Before& before, const MakeD
     gp::Fit fit{};
     if (dH && shape != gp::kSingle) {
       const int width = shape == gp::kWide ? 2 * gp::TN : gp::TN;
-      fit.room = int(lay.splits * (lay.piece / gp::TM));
+      fit.room = lay.room;
       fit.at_once = sm_count() / 2;
       fit.n_tiles = int((d + width - 1) / width);
       fit.nkb = int(kblocks);
@@ -1076,7 +1087,7 @@ cudaError_t backward_pieces(const Backward& b, const Before& before, const MakeD
       if (dH) {
         CUtensorMap mo;
         if (!gp::map_kmajor(&mz_k, dz, lay.vc, lay.piece, lay.vc) || !gp::map_mnmajor(&mw_mn, b.W + v0 * d, d, vn, d) ||
-            !gp::map_2d(&mo, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 4, part, d, lay.piece * lay.splits, d, 32, 32))
+            !gp::map_2d(&mo, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 4, part, d, int64_t(lay.room) * gp::TM, d, 32, 32))
           return cudaErrorInvalidValue;
         gp::Geo gh = geo(rows / gp::TM, d, (vn + gp::BK - 1) / gp::BK, kSegKbGrad, r, b.status);
         gh.rows_live = r.count;
@@ -1114,7 +1125,7 @@ cudaError_t backward_pieces(const Backward& b, const Before& before, const MakeD
 
 size_t head_loss_workspace_bytes(int64_t N, int64_t V, int64_t d, int C) { return fwd_ws(N, V, d, C).total; }
 size_t head_loss_backward_workspace_bytes(int64_t N, int64_t V, int64_t d, bool dh, bool dw) {
-  return bwd_ws(N, V, d, dh, dw, true).total;
+  return bwd_ws(N, V, d, dh, dw, true, false).total;
 }
 
 cudaError_t launch_head_loss(const void* H, int64_t ldh, int64_t N, int64_t d, const void* W, int64_t V,
@@ -1147,7 +1158,7 @@ cudaError_t launch_head_loss_backward(const void* H, int64_t ldh, int64_t N, int
                                       const int32_t* y, const float* w, const float* lse, const float* dloss,
                                       float scale, void* dH, int64_t lddh, void* dW, void* workspace, int32_t* status,
                                       cudaStream_t s) {
-  const BwdWs lay = bwd_ws(N, V, d, dH != nullptr, dW != nullptr, true);
+  const BwdWs lay = bwd_ws(N, V, d, dH != nullptr, dW != nullptr, true, false);
   uint8_t* ws = static_cast<uint8_t*>(workspace);
   const Rows r = rows_at(workspace, lay.rows);
   cudaError_t e = launch_rows(H, ldh, N, d, V, y, w, dloss, lse, r, nullptr, nullptr, nullptr, 0, dH, lddh, s);
@@ -1240,7 +1251,7 @@ WordsWs back_words(int64_t N, int64_t V, int K, const BwdWs& lay) {
 int head_distill_max_words() { return kMostWords; }
 size_t head_distill_workspace_bytes(int64_t N, int64_t V, int64_t d, int K) { return distill_ws(N, V, d, K).total; }
 size_t head_distill_backward_workspace_bytes(int64_t N, int64_t V, int64_t d, int K, bool dh, bool dw) {
-  return back_words(N, V, K, bwd_ws(N, V, d, dh, dw, false)).total;
+  return back_words(N, V, K, bwd_ws(N, V, d, dh, dw, false, true)).total;
 }
 
 cudaError_t launch_head_distill(const void* H, int64_t ldh, int64_t N, int64_t d, const void* W, int64_t V,
@@ -1294,7 +1305,7 @@ cudaError_t launch_head_distill_backward(const void* H, int64_t ldh, int64_t N, 
                                          const int32_t* idx, const float* t, int K, float tau, const float* w,
                                          const float* lse, const float* dloss, float scale, void* dH, int64_t lddh,
                                          void* dW, void* workspace, int32_t* status, cudaStream_t s) {
-  const BwdWs lay = bwd_ws(N, V, d, dH != nullptr, dW != nullptr, false);
+  const BwdWs lay = bwd_ws(N, V, d, dH != nullptr, dW != nullptr, false, true);
   const WordsWs wlay = back_words(N, V, K, lay);
   uint8_t* ws = static_cast<uint8_t*>(workspace);
   Words words;
