@@ -791,10 +791,16 @@ __global__ void __cluster_dims__(Shape<kShape>::kCtas, 1, 1) __launch_bounds__(T
                 float f[32];
 #pragma unroll
                 for (int i = 0; i < 32; ++i) {
-                  float z = 0.f;
+                  f[i] = v[i];
 #pragma unroll
-                  for (int c = 0; c < 4; ++c) z = c == b ? v[32 * c + i] : z;
-                  f[i] = epi.value(pre, col0 + 32 * b + i, z);
+                  for (int c = 1; c < 4; ++c) f[i] = c == b ? v[32 * c + i] : f[i];
+                }
+                if (simple) {
+#pragma unroll
+                  for (int i = 0; i < 32; ++i) f[i] = epi.value1(pre, col0 + 32 * b + i, f[i]);
+                } else {
+#pragma unroll
+                  for (int i = 0; i < 32; ++i) f[i] = epi.value(pre, col0 + 32 * b + i, f[i]);
                 }
                 epi.store_parts(f, row, col0 + 32 * b);
               }

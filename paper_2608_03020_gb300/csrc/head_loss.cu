@@ -799,7 +799,7 @@ __global__ void __launch_bounds__(1024)
 // One thread per 8 elements of a row; the k ranges' sums are loaded four at a time and added in order.
 __global__ void __launch_bounds__(256)
     k_head_dh(const float* __restrict__ part, int64_t rows, int planned, const gp::Fit fit, int64_t d, Rows in,
-              int64_t row_first, float scale, int low_row, __nv_bfloat16* __restrict__ dH, int64_t lddh) {
+              int64_t row_first, float scale, __nv_bfloat16* __restrict__ dH, int64_t lddh) {
   wait_for_previous();
   launch_dependents();
   const int dv = int(d / 8);
@@ -829,13 +829,6 @@ __global__ void __launch_bounds__(256)
           a[4] += x[s][1].x; a[5] += x[s][1].y; a[6] += x[s][1].z; a[7] += x[s][1].w;
         }
     }
-    if (low_row > 0)  // the sums of dZ's second part
-      for (int s = 0; s < splits; ++s) {
-        const float4* p = reinterpret_cast<const float4*>(part + int64_t(s) * pitch + at + low_row * d);
-        const float4 x = p[0], y = p[1];
-        a[0] += x.x; a[1] += x.y; a[2] += x.z; a[3] += x.w;
-        a[4] += y.x; a[5] += y.y; a[6] += y.z; a[7] += y.w;
-      }
     uint4 q;
     q.x = gp::pack_bf16(scale * a[0], scale * a[1]);
     q.y = gp::pack_bf16(scale * a[2], scale * a[3]);
@@ -843,6 +836,42 @@ __global__ void __launch_bounds__(256)
     q.w = gp::pack_bf16(scale * a[6], scale * a[7]);
     *reinterpret_cast<uint4*>(dH + n * lddh + (at - row * d)) = q;
   }
+}
+
+// Few rows, dZ in two parts: eight warps share an output's ranges (both parts' sums of each), and meet in order.  In one
+// thread they took 10 us more (one row, d = 2048, 19 ranges).
+__global__ void __launch_bounds__(256) k_head_dh_few(const float* __restrict__ part, int splits, int64_t d, Rows in, float scale,
+                                                     int low_row, __nv_bfloat16* __restrict__ dH, int64_t lddh) {
+  __shared__ float sums[8][32][9];
+  wait_for_previous();
+  launch_dependents();
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, dv = int(d / 8);
+  const int total = *in.count * dv, e = int(blockIdx.x) * 32 + lane;
+  const int row = e / dv, col = 8 * (e - row * dv);
+  float a[8] = {};
+  if (e < total)
+#pragma unroll 2
+    for (int s = warp; s < splits; s += 8)
+#pragma unroll
+      for (int lo = 0; lo < 2; ++lo) {
+        const float4* p = reinterpret_cast<const float4*>(part + (int64_t(s) * gp::TM + row + lo * low_row) * d + col);
+        const float4 x = p[0], y = p[1];
+        a[0] += x.x; a[1] += x.y; a[2] += x.z; a[3] += x.w;
+        a[4] += y.x; a[5] += y.y; a[6] += y.z; a[7] += y.w;
+      }
+#pragma unroll
+  for (int i = 0; i < 8; ++i) sums[warp][lane][i] = a[i];
+  __syncthreads();
+  if (warp > 0 || e >= total) return;
+  for (int w = 1; w < 8; ++w)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) a[i] += sums[w][lane][i];
+  uint4 q;
+  q.x = gp::pack_bf16(scale * a[0], scale * a[1]);
+  q.y = gp::pack_bf16(scale * a[2], scale * a[3]);
+  q.z = gp::pack_bf16(scale * a[4], scale * a[5]);
+  q.w = gp::pack_bf16(scale * a[6], scale * a[7]);
+  *reinterpret_cast<uint4*>(dH + int64_t(in.idx[row]) * lddh + col) = q;
 }
 
 // ------------------------------------------------------------------ host side
@@ -1113,8 +1142,11 @@ cudaError_t backward_pieces(const Backward& b, const Before& before, const MakeD
     if (dH) {
       const int64_t blocks = rows * (d / 8) / 256 + 1;
       const int64_t most = 8 * int64_t(sm_count());
-      e = gp::launch_early(k_head_dh, dim3(unsigned(blocks < most ? blocks : most)), dim3(256), 0, b.s,
-                           static_cast<const float*>(part), rows, lay.splits, fit, d, r, p0, b.scale, b.low_row, dH, lddh);
+      e = b.low_row > 0
+              ? gp::launch_early(k_head_dh_few, dim3(unsigned((N * (d / 8) + 31) / 32)), dim3(256), 0, b.s,
+                                 static_cast<const float*>(part), lay.splits, d, r, b.scale, b.low_row, dH, lddh)
+              : gp::launch_early(k_head_dh, dim3(unsigned(blocks < most ? blocks : most)), dim3(256), 0, b.s,
+                                 static_cast<const float*>(part), rows, lay.splits, fit, d, r, p0, b.scale, dH, lddh);
       if (e != cudaSuccess) return e;
     }
   }
