@@ -325,9 +325,11 @@ struct CallersA : NoExt {
 // hold one of the epilogue's `rows`.
 // kAhead (narrow and single): what an epilogue has to look up for a tile is on its way while the sums are not
 // complete: a State for each thread; start(State, row of the first tile), ahead(State, row, half tile, row of the next
-// tile) before the sums; the state goes to row_of(), which also gets the first column, or to operator().  With
-// kPacks  bool simple(Row)  chooses for a warp between value1() and value(), and in the single shape, where low_row is
-// not 0, store_parts(float (&)[32], row, column) takes the values of the rows before it.
+// tile) before the sums; the state goes to operator().  With kPacks  void all(float (&v)[128], State, int row, int col0)
+// puts the values in the sums' place in the narrow shape; in the single shape, whose one tile waits for each instruction's
+// first fetch, the state goes to row_of(), which also gets the first column, bool simple(Row) chooses for a warp between
+// value1() and value(), and where low_row is not 0, store_parts(float (&)[32], row, column) takes the values of the rows
+// before it.
 // kFits: the number of k ranges is the device's choice (Fit).
 template <int kShape, bool kAmn, bool kBmn, class Epi, class Ext>
 __global__ void __cluster_dims__(Shape<kShape>::kCtas, 1, 1) __launch_bounds__(THREADS, 1)
@@ -776,13 +778,22 @@ __global__ void __cluster_dims__(Shape<kShape>::kCtas, 1, 1) __launch_bounds__(T
         if (!go) break;
         const int col0 = t.col0 + h * HALF;
         if constexpr (Epi::kPacks) {
-          auto pre = [&] {
-            if constexpr (Epi::kAhead) return epi.row_of(row, state, col0);
-            else return epi.row_of(row);
-          }();
-          bool simple = false;
-          if constexpr (Epi::kAhead) simple = epi.simple(pre);
+          const auto store = [&](auto value) {
+#pragma unroll
+            for (int b = 0; b < 2; ++b) {
+              if (col0 + 64 * b >= (kSlim ? t.end : g.cols)) continue;
+              uint32_t w[32];
+#pragma unroll
+              for (int i = 0; i < 32; ++i) {
+                const float lo = value(64 * b + 2 * i), hi = value(64 * b + 2 * i + 1);
+                w[i] = pack_bf16(lo, hi);
+              }
+              store_box_bf16(box, &tmO, lane, col0 + 64 * b, r0, w);
+            }
+          };
           if constexpr (Epi::kAhead && kShape == kSingle) {
+            auto pre = epi.row_of(row, state, col0);
+            const bool simple = epi.simple(pre);
             if (epi.low_row > 0) {  // rows below low_row are given in two parts, the second low_row rows behind
               if (q * 32 >= epi.low_row) continue;
 #pragma unroll 1
@@ -806,31 +817,35 @@ __global__ void __cluster_dims__(Shape<kShape>::kCtas, 1, 1) __launch_bounds__(T
               }
               continue;
             }
-          }
 #pragma unroll
-          for (int b = 0; b < 2; ++b) {
-            if (col0 + 64 * b >= (kSlim ? t.end : g.cols)) continue;
-            uint32_t w[32];
-            if (Epi::kAhead && simple) {
-              if constexpr (Epi::kAhead) {
+            for (int b = 0; b < 2; ++b) {
+              if (col0 + 64 * b >= (kSlim ? t.end : g.cols)) continue;
+              uint32_t w[32];
+              if (simple) {
 #pragma unroll
                 for (int i = 0; i < 32; ++i) {
                   const float lo = epi.value1(pre, col0 + 64 * b + 2 * i, v[64 * b + 2 * i]);
                   const float hi = epi.value1(pre, col0 + 64 * b + 2 * i + 1, v[64 * b + 2 * i + 1]);
                   w[i] = pack_bf16(lo, hi);
                 }
-              }
-            } else {
+              } else {
 #pragma unroll
-              for (int i = 0; i < 32; ++i) {
-                const float lo = epi.value(pre, col0 + 64 * b + 2 * i, v[64 * b + 2 * i]);
-                const float hi = epi.value(pre, col0 + 64 * b + 2 * i + 1, v[64 * b + 2 * i + 1]);
-                w[i] = pack_bf16(lo, hi);
+                for (int i = 0; i < 32; ++i) {
+                  const float lo = epi.value(pre, col0 + 64 * b + 2 * i, v[64 * b + 2 * i]);
+                  const float hi = epi.value(pre, col0 + 64 * b + 2 * i + 1, v[64 * b + 2 * i + 1]);
+                  w[i] = pack_bf16(lo, hi);
+                }
               }
+              store_box_bf16(box, &tmO, lane, col0 + 64 * b, r0, w);
             }
-            store_box_bf16(box, &tmO, lane, col0 + 64 * b, r0, w);
+          } else if constexpr (Epi::kAhead) {
+            epi.all(v, state, row, col0);
+            store([&](int i) { return v[i]; });
+          } else {
+            auto pre = epi.row_of(row);
+            store([&](int i) { return epi.value(pre, col0 + i, v[i]); });
+            if constexpr (Epi::kSums) epi.finish(pre, 2 * t.n + h, row);
           }
-          if constexpr (Epi::kSums) epi.finish(pre, 2 * t.n + h, row);
         } else if constexpr (Epi::kAhead) {
           epi(t, v, state, row, col0, lane, box, &tmO);
         } else {

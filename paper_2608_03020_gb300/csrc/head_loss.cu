@@ -520,7 +520,6 @@ struct EpiTeacher {
 struct EpiDzTeacher {
   static constexpr bool kPacks = true;
   static constexpr bool kFits = false;
-  static constexpr bool kSums = false;
   static constexpr bool kAhead = true;
   using State = WordState;
   const float* lse;    // this piece's rows
@@ -601,6 +600,56 @@ struct EpiDzTeacher {
       }
     }
     return r.g * p;
+  }
+  // p of every column, then q off it, then the factor.  The first words of the warp's rows go one by one, each against
+  // all columns (260 instructions); where a row has more than kOneByOne, the rest column by column, where a lane that
+  // meets its word waits for the next.  (Loss and dH, one by one alone, column by column alone, and both: 4217 positions with
+  // 96 words at d = 744, V = 48060 1102, 1700 and 1034 us; 192 with 87 words at V = 4839 163, 125 and 125.)
+  static constexpr int kOneByOne = 8;
+  __device__ __forceinline__ void all(float (&v)[128], const State& st, int row, int col0) const {
+    const float row_lse = lse[row], g = w[row] * tau;
+    const int end = row_first + row < *count ? v_cols - col0 : 0;  // the columns that count (none in rows past the live ones)
+    const bool here = st.entry != kNoEntry;  // (the table has nothing for rows past the live ones)
+    const int32_t first = int32_t(v_first) + col0;
+    const int64_t from = int64_t(st.n) * words.K;
+    int k = st.entry >> 7 & 255;
+    int last = here ? st.entry >> 15 & 1 ? words.K - 1 : k : -1;  // no word here behind it
+    int at = here ? int(st.entry & 127) : -1;
+    float q = here ? __ldg(words.q + from + k) : 0.f;
+    int32_t next = kNoWord;  // the word behind, and its share
+    float next_q = 0.f;
+    auto fetch = [&] {
+      next = kNoWord;
+      if (++k <= last) {
+        next = __ldg(words.at + from + k);
+        next_q = __ldg(words.q + from + k);
+      }
+    };
+    auto advance = [&] {  // (a column below 0 or from 128 on is none of these)
+      at = next < first + 128 ? next - first : -1;
+      q = next_q;
+      fetch();
+    };
+    fetch();
+#pragma unroll
+    for (int i = 0; i < 128; ++i) v[i] = exp_diff(fmaf(v[i], inv_tau, -row_lse), 0.f);
+    int n = 0;
+    for (; n < kOneByOne && __any_sync(0xffffffffu, at >= 0); ++n) {
+#pragma unroll
+      for (int i = 0; i < 128; ++i)
+        if (i == at) v[i] -= q;
+      advance();
+    }
+    if (n == kOneByOne && __any_sync(0xffffffffu, at >= 0)) {
+#pragma unroll
+      for (int i = 0; i < 128; ++i)
+        if (i == at) {
+          v[i] -= q;
+          advance();
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < 128; ++i) v[i] = i < end ? g * v[i] : 0.f;
   }
 };
 
