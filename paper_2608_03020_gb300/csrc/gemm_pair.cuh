@@ -60,6 +60,7 @@ constexpr int EPI_WARPS = 8;
 constexpr int BOX = 4096;             // one epilogue warp's staging box: 32 rows x 128 bytes
 constexpr int THREADS = 64 + 32 * EPI_WARPS;
 constexpr int64_t kWideK = 16384;
+constexpr int kMostPer = 4;           // k-blocks of a stage at most
 enum : int { kNarrow = 0, kWide = 1, kSingle = 2 };
 template <int kShape>
 struct Shape {
@@ -126,6 +127,7 @@ struct Geo {
   int cols;              // columns of the output
   int width;             // columns of a tile (launch() sets all but the single shape's)
   int arows, stages;     // single shape, B K-major: rows of A's boxes, stages of the ring (launch())
+  int per = 1;           // and k-blocks of a stage (launch())
   int nkb;               // k-blocks of the product
   int splits;            // the k-blocks are cut into this many ranges, each a tile of its own
   int seg_kb;            // k-blocks per accumulation segment
@@ -162,6 +164,7 @@ __device__ __forceinline__ Live live_of(const Geo& g) {
     if (t < 1) t = 1;
     if (t < v.nkb) v.nkb = t;
   }
+  if (kSingleTile) v.nkb = (v.nkb + g.per - 1) / g.per;  // (from here on a k-block is all that a stage holds)
   v.splits = kFits ? fit_splits(g.fit, g.splits, g.m_tiles, v.m_tiles) : g.splits;
   v.total = v.m_tiles * g.n_tiles * v.splits;
   return v;
@@ -346,7 +349,8 @@ __global__ void __cluster_dims__(Shape<kShape>::kCtas, 1, 1) __launch_bounds__(T
   const int STAGES = kSlim ? g.stages : S::kStages;
   const uint32_t a_bytes = kSlim ? uint32_t(g.arows) * 128u : uint32_t(OPB);
   const uint32_t b_cols = kSlim ? uint32_t(g.width) * (Ext::kTwin ? 2u : 1u) : uint32_t(TN);  // of an accumulator
-  const uint32_t STAGE_BYTES = kSlim ? a_bytes + b_cols * 128u : uint32_t(S::kStageBytes);
+  const int per = kSlim ? g.per : 1, seg_kb = kSlim ? g.seg_kb / g.per : g.seg_kb;
+  const uint32_t STAGE_BYTES = kSlim ? uint32_t(per) * (a_bytes + b_cols * 128u) : uint32_t(S::kStageBytes);
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   uint8_t* boxes = smem + 12 * OPB;
@@ -438,24 +442,34 @@ __global__ void __cluster_dims__(Shape<kShape>::kCtas, 1, 1) __launch_bounds__(T
           load(a, map, fb, m0, k0);
           load(a + SUB, map, fb, m0 + 64, k0);
         } else {
-          load(a, map, fb, k0, m0);
+#pragma unroll
+          for (int i = 0; i < (kSlim ? kMostPer : 1); ++i)
+            if (i < per) load(a + i * a_bytes, map, fb, per * k0 + i * BK, m0);
         }
       };
       // 128 rows of B per operand: this CTA's half of each accumulator, or (single) both halves
       auto load_b = [&](const Tile& t, int s, int kb, uint32_t fb) {
-        const uint32_t b = smem_base + uint32_t(s) * STAGE_BYTES + a_bytes;
+        const uint32_t b = smem_base + uint32_t(s) * STAGE_BYTES + uint32_t(per) * a_bytes;
         const CUtensorMap* map = second(kb) ? &tmBx : &tmB;
-        const int k0 = kb * BK;
+        const int k0 = kb * per * BK;
 #pragma unroll
         for (int c = 0; c < S::kOpsB; ++c) {
           if constexpr (Ext::kTwin) {
-            if (kSlim) load(b + c * uint32_t(g.width) * 128u, c ? &tmBx : &tmB, fb, k0, t.col0);
-            else load(b + c * OPB, rank ? &tmBx : &tmB, fb, k0, t.col0 + c * HALF);
+            if constexpr (kSlim) {
+#pragma unroll
+              for (int i = 0; i < kMostPer; ++i)
+                if (i < per)
+                  load(b + i * b_cols * 128u + c * uint32_t(g.width) * 128u, c ? &tmBx : &tmB, fb, k0 + i * BK, t.col0);
+            } else {
+              load(b + c * OPB, rank ? &tmBx : &tmB, fb, k0, t.col0 + c * HALF);
+            }
             continue;
           }
           const int n = t.col0 + int(rank) * HALF + c * (kPair ? TN : kSlim ? g.width / 2 : HALF);
           if (kSlim) {
-            load(b + c * uint32_t(g.width * BK), map, fb, k0, n);
+#pragma unroll
+            for (int i = 0; i < kMostPer; ++i)
+              if (i < per) load(b + i * b_cols * 128u + c * uint32_t(g.width * BK), map, fb, k0 + i * BK, n);
           } else if (kBmn) {
             load(b + c * OPB, map, fb, n, k0);
             load(b + c * OPB + SUB, map, fb, n + 64, k0);
@@ -522,7 +536,7 @@ __global__ void __cluster_dims__(Shape<kShape>::kCtas, 1, 1) __launch_bounds__(T
       constexpr uint32_t kKLbo = 16u;  // K-major with the 128-byte swizzle: leading offset unused
       const uint64_t a_kmaj = sdesc(smem_base, kKLbo, 1024u, kSwizzle128B);
       const uint64_t a0 = kAmn ? sdesc(smem_base, SUB, 1024u, kSwizzle128B) : a_kmaj;
-      const uint64_t b_kmaj = sdesc(smem_base + a_bytes, kKLbo, 1024u, kSwizzle128B);
+      const uint64_t b_kmaj = sdesc(smem_base + uint32_t(per) * a_bytes, kKLbo, 1024u, kSwizzle128B);
       const uint64_t b0 = kBmn ? sdesc(smem_base + a_bytes, SUB, 1024u, kSwizzle128B) : b_kmaj;
       constexpr uint64_t kAStep = kAmn ? 2048 >> 4 : 32 >> 4, kBStep = kBmn ? 2048 >> 4 : 32 >> 4;
       const uint32_t id = tc::idesc(1, 1, kAmn ? 1 : 0, kBmn ? 1 : 0, S::kCtas * HALF, b_cols);
@@ -537,6 +551,15 @@ __global__ void __cluster_dims__(Shape<kShape>::kCtas, 1, 1) __launch_bounds__(T
               mma_f16_pair(d, a0 + so + kk * kAStep, b0 + bo + kk * kBStep, id, !first || kk != 0 ? 1u : 0u);
             else
               mma_f16(d, a0 + so + kk * kAStep, b0 + bo + kk * kBStep, id, !first || kk != 0 ? 1u : 0u);
+          if constexpr (kSlim) {
+#pragma unroll
+            for (int i = 1; i < kMostPer; ++i)
+              if (i < per) {
+#pragma unroll
+                for (int kk = 0; kk < BK / 16; ++kk)
+                  mma_f16(d, a0 + so + i * (a_bytes >> 4) + kk * kAStep, b0 + bo + i * (b_cols * 128u >> 4) + kk * kBStep, id, 1u);
+              }
+          }
         } else {
           for (int kk = 0; kk < ext.ksteps(); ++kk)
             mma_f16_pair(d, a_kmaj + so + kk * 2, b_kmaj + bo + kk * 2, kIdX, !first || kk != 0 ? 1u : 0u);
@@ -605,7 +628,7 @@ __global__ void __cluster_dims__(Shape<kShape>::kCtas, 1, 1) __launch_bounds__(T
             issued = true;
             commit(empty_bar(stage));
             if (++stage == STAGES) { stage = 0; phase ^= 1u; }
-            if (++in_seg == g.seg_kb || j == all - 1) {
+            if (++in_seg == seg_kb || j == all - 1) {
               commit(acc_full(seg & 1u));
               ++seg;
               in_seg = 0;
@@ -669,7 +692,7 @@ __global__ void __cluster_dims__(Shape<kShape>::kCtas, 1, 1) __launch_bounds__(T
         ++seg;
       } else if constexpr (Ext::kTwin) {
         // 64 columns of the first product and the same of the second, for every accumulator
-        const int nseg = kShape == kWide ? 1 : (all + g.seg_kb - 1) / g.seg_kb;
+        const int nseg = kShape == kWide ? 1 : (all + seg_kb - 1) / seg_kb;
 #pragma unroll 1
         for (uint32_t a = 0; a < uint32_t(S::kAcc); ++a) {
           const int col0 = t.col0 + int(a) * HALF + h * 64;
@@ -751,7 +774,7 @@ __global__ void __cluster_dims__(Shape<kShape>::kCtas, 1, 1) __launch_bounds__(T
           const int after = it + ncl < lv.total ? tile_of(g, lv, it + ncl).m - t.m : 0;
           epi.ahead(state, row, 2 * t.n + h, row + after * TM);
         }
-        const int nseg = (all + g.seg_kb - 1) / g.seg_kb;
+        const int nseg = (all + seg_kb - 1) / seg_kb;
         float v[128];
         if (nseg == 0) {
 #pragma unroll
@@ -1005,8 +1028,12 @@ static cudaError_t launch(const CUtensorMap& a, const CUtensorMap& b, const CUte
   if (kShape == kSingle && !kBmn) {
     if (g.arows == 0) g.arows = HALF;
     const int s = 12 * OPB / ((g.arows + g.width * (Ext::kTwin ? 2 : 1)) * 128);
-    g.stages = s < Shape<kSingle>::kMostStages ? s : Shape<kSingle>::kMostStages;
-    if (Ext::kTwin) g.seg_kb = g.nkb;
+    // Waiting and signalling cost a stage 0.28 us whatever its size, so two or four k-blocks share one where four such
+    // stages fit (gated products: 64 tokens 2048 to 8192 19.0 us with one, 17.2 with two; 7 tokens 4376 to 752 28.1, 22.1
+    // and 19.2 with one, two and four).
+    g.per = g.splits > 1 ? 1 : s >= 16 && g.seg_kb % 4 == 0 ? 4 : s >= 8 && g.seg_kb % 2 == 0 ? 2 : 1;
+    g.stages = s / g.per < Shape<kSingle>::kMostStages ? s / g.per : Shape<kSingle>::kMostStages;
+    if (Ext::kTwin) g.seg_kb = g.nkb + g.per - 1;
   }
   g.n_tiles = (g.cols + g.width - 1) / g.width;
   static std::atomic<uint64_t> allowed{0};
