@@ -1065,6 +1065,7 @@ __global__ void __launch_bounds__(kFewThreads, 1)
 
 // ------------------------------------------------------------------ many tokens
 struct AdapterExt {
+  static constexpr bool kDeep = false;
   static constexpr bool kOn = true;
   static constexpr bool kSecond = false;
   static constexpr bool kTwin = false;

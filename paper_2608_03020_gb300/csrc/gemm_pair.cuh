@@ -153,7 +153,7 @@ struct Live {
   int m_tiles, nkb, splits, total;
 };
 
-template <bool kFits, bool kSingleTile>
+template <bool kFits, bool kSingleTile, bool kDeep>
 __device__ __forceinline__ Live live_of(const Geo& g) {
   Live v;
   v.m_tiles = g.m_tiles;
@@ -164,7 +164,7 @@ __device__ __forceinline__ Live live_of(const Geo& g) {
     if (t < 1) t = 1;
     if (t < v.nkb) v.nkb = t;
   }
-  if (kSingleTile) v.nkb = (v.nkb + g.per - 1) / g.per;  // (from here on a k-block is all that a stage holds)
+  if (kDeep) v.nkb = (v.nkb + g.per - 1) / g.per;  // (from here on a k-block is all that a stage holds)
   v.splits = kFits ? fit_splits(g.fit, g.splits, g.m_tiles, v.m_tiles) : g.splits;
   v.total = v.m_tiles * g.n_tiles * v.splits;
   return v;
@@ -230,6 +230,7 @@ __device__ __forceinline__ void store_box_bf16(uint8_t* box, const CUtensorMap* 
 // tmAx (row coordinate a_row of the CTA's 128 rows) and whose B rows from tmBx (b_row0 + the tile's
 // column, block b_block), ksteps() MMA steps of 16 each.  None here; the adapter projection has one.
 struct NoExt {
+  static constexpr bool kDeep = false;
   static constexpr bool kOn = false;
   static constexpr bool kSecond = false;
   static constexpr bool kTwin = false;
@@ -315,6 +316,13 @@ struct CallersA : NoExt {
   static constexpr bool kEarlyA = true;
 };
 
+// Single shape, B K-major: two or four k-blocks to a stage (Geo::per).  A kernel of its own: the choice at run time took one
+// token 2 us more of 51 at 2048 x 49152, where a stage holds one.
+template <class Ext>
+struct Deep : Ext {
+  static constexpr bool kDeep = true;
+};
+
 // What becomes of a finished tile.  An output in bf16 is given value by value (kPacks): Row row_of(row)
 // reads what a row needs, before its sums are complete; value(Row, column, sum) is the output.  kSums (not
 // in the wide shape): Row adds something up over the values, which finish(Row, half tile, row) gets.  Other
@@ -349,7 +357,8 @@ __global__ void __cluster_dims__(Shape<kShape>::kCtas, 1, 1) __launch_bounds__(T
   const int STAGES = kSlim ? g.stages : S::kStages;
   const uint32_t a_bytes = kSlim ? uint32_t(g.arows) * 128u : uint32_t(OPB);
   const uint32_t b_cols = kSlim ? uint32_t(g.width) * (Ext::kTwin ? 2u : 1u) : uint32_t(TN);  // of an accumulator
-  const int per = kSlim ? g.per : 1, seg_kb = kSlim ? g.seg_kb / g.per : g.seg_kb;
+  constexpr bool kDeep = Ext::kDeep;
+  const int per = kDeep ? g.per : 1, seg_kb = kDeep ? g.seg_kb / g.per : g.seg_kb;
   const uint32_t STAGE_BYTES = kSlim ? uint32_t(per) * (a_bytes + b_cols * 128u) : uint32_t(S::kStageBytes);
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
@@ -409,7 +418,7 @@ __global__ void __cluster_dims__(Shape<kShape>::kCtas, 1, 1) __launch_bounds__(T
   constexpr bool kEarlyB = kShape == kSingle && !Ext::kTwin;
   if (!Ext::kOn && !(kEarlyB && warp == 0)) wait_for_previous();
   if (!(kEarlyB && warp == 0)) launch_dependents();
-  const Live lv = live_of<Epi::kFits, kShape == kSingle>(g);
+  const Live lv = live_of<Epi::kFits, kShape == kSingle, Ext::kDeep>(g);
   uint32_t iters_done = 0;
 
   if (warp == 0) {
@@ -442,9 +451,12 @@ __global__ void __cluster_dims__(Shape<kShape>::kCtas, 1, 1) __launch_bounds__(T
           load(a, map, fb, m0, k0);
           load(a + SUB, map, fb, m0 + 64, k0);
         } else {
+          load(a, map, fb, per * k0, m0);
+          if constexpr (kDeep) {
 #pragma unroll
-          for (int i = 0; i < (kSlim ? kMostPer : 1); ++i)
-            if (i < per) load(a + i * a_bytes, map, fb, per * k0 + i * BK, m0);
+            for (int i = 1; i < kMostPer; ++i)
+              if (i < per) load(a + i * a_bytes, map, fb, per * k0 + i * BK, m0);
+          }
         }
       };
       // 128 rows of B per operand: this CTA's half of each accumulator, or (single) both halves
@@ -456,10 +468,13 @@ __global__ void __cluster_dims__(Shape<kShape>::kCtas, 1, 1) __launch_bounds__(T
         for (int c = 0; c < S::kOpsB; ++c) {
           if constexpr (Ext::kTwin) {
             if constexpr (kSlim) {
+              const uint32_t at = b + c * uint32_t(g.width) * 128u;
+              load(at, c ? &tmBx : &tmB, fb, k0, t.col0);
+              if constexpr (kDeep) {
 #pragma unroll
-              for (int i = 0; i < kMostPer; ++i)
-                if (i < per)
-                  load(b + i * b_cols * 128u + c * uint32_t(g.width) * 128u, c ? &tmBx : &tmB, fb, k0 + i * BK, t.col0);
+                for (int i = 1; i < kMostPer; ++i)
+                  if (i < per) load(at + i * b_cols * 128u, c ? &tmBx : &tmB, fb, k0 + i * BK, t.col0);
+              }
             } else {
               load(b + c * OPB, rank ? &tmBx : &tmB, fb, k0, t.col0 + c * HALF);
             }
@@ -467,9 +482,13 @@ __global__ void __cluster_dims__(Shape<kShape>::kCtas, 1, 1) __launch_bounds__(T
           }
           const int n = t.col0 + int(rank) * HALF + c * (kPair ? TN : kSlim ? g.width / 2 : HALF);
           if (kSlim) {
+            const uint32_t at = b + c * uint32_t(g.width * BK);
+            load(at, map, fb, k0, n);
+            if constexpr (kDeep) {
 #pragma unroll
-            for (int i = 0; i < kMostPer; ++i)
-              if (i < per) load(b + i * b_cols * 128u + c * uint32_t(g.width * BK), map, fb, k0 + i * BK, n);
+              for (int i = 1; i < kMostPer; ++i)
+                if (i < per) load(at + i * b_cols * 128u, map, fb, k0 + i * BK, n);
+            }
           } else if (kBmn) {
             load(b + c * OPB, map, fb, n, k0);
             load(b + c * OPB + SUB, map, fb, n + 64, k0);
@@ -551,7 +570,7 @@ __global__ void __cluster_dims__(Shape<kShape>::kCtas, 1, 1) __launch_bounds__(T
               mma_f16_pair(d, a0 + so + kk * kAStep, b0 + bo + kk * kBStep, id, !first || kk != 0 ? 1u : 0u);
             else
               mma_f16(d, a0 + so + kk * kAStep, b0 + bo + kk * kBStep, id, !first || kk != 0 ? 1u : 0u);
-          if constexpr (kSlim) {
+          if constexpr (kDeep) {
 #pragma unroll
             for (int i = 1; i < kMostPer; ++i)
               if (i < per) {
@@ -1021,7 +1040,7 @@ inline int slim_width(int64_t cols, int unit = 16) {
 // (static: a kernel of the same name is another one in each source file, with an `allowed` of its own.)
 template <int kShape, bool kAmn, bool kBmn, class Epi, class Ext>
 static cudaError_t launch(const CUtensorMap& a, const CUtensorMap& b, const CUtensorMap& ax, const CUtensorMap& bx,
-                          const CUtensorMap& o, Geo g, const Epi& epi, const Ext& ext, cudaStream_t s) {
+                          const CUtensorMap& o, Geo g, const Epi& epi, const Ext& ext, cudaStream_t stream) {
   auto kernel = k_gemm_pair<kShape, kAmn, kBmn, Epi, Ext>;
   constexpr int kCtas = Shape<kShape>::kCtas;
   if (kShape != kSingle || kBmn || g.width == 0) g.width = Shape<kShape>::kCols / (Ext::kTwin ? 2 : 1);
@@ -1032,6 +1051,8 @@ static cudaError_t launch(const CUtensorMap& a, const CUtensorMap& b, const CUte
     // stages fit (gated products: 64 tokens 2048 to 8192 19.0 us with one, 17.2 with two; 7 tokens 4376 to 752 28.1, 22.1
     // and 19.2 with one, two and four).
     g.per = g.splits > 1 ? 1 : s >= 16 && g.seg_kb % 4 == 0 ? 4 : s >= 8 && g.seg_kb % 2 == 0 ? 2 : 1;
+    if constexpr (!Ext::kDeep && kShape == kSingle && !kBmn)
+      if (g.per > 1) return launch<kShape, kAmn, kBmn, Epi, Deep<Ext>>(a, b, ax, bx, o, g, epi, Deep<Ext>{ext}, stream);
     g.stages = s / g.per < Shape<kSingle>::kMostStages ? s / g.per : Shape<kSingle>::kMostStages;
     if (Ext::kTwin) g.seg_kb = g.nkb + g.per - 1;
   }
@@ -1043,7 +1064,7 @@ static cudaError_t launch(const CUtensorMap& a, const CUtensorMap& b, const CUte
   if (total < 1) return cudaSuccess;
   const int at_once = sm_count() / kCtas;  // pairs (76 on 152 SMs) or CTAs at work at once
   const int n = total < at_once && g.fit.room == 0 ? int(total) : at_once;
-  return launch_early(kernel, dim3(unsigned(kCtas * n)), dim3(THREADS), SMEM, s, a, b, ax, bx, o, g, epi, ext);
+  return launch_early(kernel, dim3(unsigned(kCtas * n)), dim3(THREADS), SMEM, stream, a, b, ax, bx, o, g, epi, ext);
 }
 
 template <bool kAmn, bool kBmn, class Epi, class Ext>
