@@ -20,9 +20,9 @@
 // k_gemm_pair         dWg and dWu
 // k_gated_join        sums the k ranges of dX where its tiles alone would not fill the SMs
 // Bound: the tensor cores from a few hundred tokens on, the read of Wg and Wu below.  8192 tokens at d = 3584,
-// f = 14336: 856 us (1.97 PFLOP/s); one token there 39 us (206 MB: 5.3 TB/s); 64 tokens at d = 2048, f = 8192
-// 18.9 us (3.6 TB/s); forward and backward of 4096 tokens there 700 us (1.57 PFLOP/s with the products computed
-// again).
+// f = 14336: 856 us cold, 935 to 948 under load (1.97 and 1.79 PFLOP/s); one token there 37.5 us (206 MB: 5.5 TB/s); 64
+// tokens at d = 2048, f = 8192 17.0 us (3.9 TB/s); forward and backward of 4096 tokens there 700 us (1.57 PFLOP/s with
+// the products computed again).
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 

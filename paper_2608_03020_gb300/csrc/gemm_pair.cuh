@@ -18,7 +18,8 @@
 // and two buffers; B's read from HBM is then the bound.  With B K-major its tiles may be narrower than
 // 256 columns (`width`, a multiple of 16), so that the last round of CTAs is as full as the others, and
 // A's loads bring only the rows there are (the MMA's other rows read what lies behind; nobody reads
-// their sums): the ring is as deep as that allows.  (16 stages instead of at most 8 gained nothing.)
+// their sums): the ring is as deep as that allows, in at most 8 stages (16 or 24 gained nothing) of one, two or four
+// k-blocks.
 //   warp 0       TMA producer (both CTAs): its CTA's 128 rows of A and 128 rows of B per accumulator
 //   warp 1       one thread of the even CTA issues the MMAs (M = 256, N = 256, K = 16)
 //   warps 2..9   take the sums out of TMEM: warp w holds rows 32 (w & 3) .. + 31 of its CTA, one row
@@ -695,7 +696,7 @@ __global__ void __cluster_dims__(Shape<kShape>::kCtas, 1, 1) __launch_bounds__(T
         // Half of the tile's columns (in units of 8) of the first product, and the same of the second `width` columns
         // behind.  One sum per tile (launch()), and code that runs once: a loop over 8 columns straight from
         // tensor memory, whose instructions need not all be fetched for one tile (64 columns from registers at a
-        // time: one token at 3584 x 14336 46.7 us, so 39.1).  Warps without a row do nothing.
+        // time: one token at 3584 x 14336 46.7 us, so 37.5).  Warps without a row do nothing.
         const int half = (g.width / 2 + 7) / 8 * 8, col0 = t.col0 + h * half, end = col0 + half < t.end ? col0 + half : t.end;
         const uint32_t b = seg & 1u;
         if (!(go = wait_sums(b, (seg >> 1) & 1u))) break;
