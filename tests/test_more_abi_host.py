@@ -117,6 +117,14 @@ def test_distill_codes(L):
     assert back(dH=at(6)) == 1
 
 
+@pytest.mark.parametrize("tau", [1e-39, 1e-45, 2e19, 3e38])
+def test_temperatures_whose_square_or_reciprocal_is_not_finite(L, tau):
+    one, f = at(0), ctypes.c_float
+    assert L.loca_head_distill(one, 64, 4, 64, at(1), 10, at(2), at(3), 3, f(tau), None, at(4), at(5), at(6), BIG, None) == 1
+    assert L.loca_head_distill_backward(one, 64, 4, 64, at(1), 10, at(2), at(3), 3, f(tau), None, at(4), None, f(1.0), at(5), 64,
+                                        at(6), at(7), BIG, None) == 1
+
+
 def test_q4_sizes(L):
     rc, n = _size(L.loca_q4_packed_size, 20480, 5120, 64, 1, 1)
     # four bits a code, a scale and half a byte of zero for each group
