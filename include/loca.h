@@ -543,9 +543,9 @@ int loca_head_loss_backward(const void* H, int64_t ldh, int64_t N, int64_t d, co
  * tau     > 0, the temperature; tau^2 and 1 / tau finite
  * H, W, w, loss, lse, dloss, grad_scale, dH, dW, limits, arithmetic and scratch memory (and 8 bytes for each entry
  * and 2 for each position and 128 words; for dH up to 160 MB more) as for loca_head_loss and its backward call; lse is that of z / tau.  q is taken
- * off in fp32 before dZ is rounded: an entry has an error of some
- * 2^-19 of p, so that for positions where one word has all of q and p nearly all loca_head_loss keeps more of the
- * gradient.  Deterministic.
+ * off in fp32 before dZ is rounded: an entry has an error of some 2^-19 of p (lse's rounding).  The entry of a word with
+ * more than half of q is minus the sum of the others, with some 2^-19 of 1 - p: a position where student and teacher
+ * agree on a word almost surely keeps its gradient.  Deterministic.
  */
 int loca_head_distill_workspace_size(int64_t N, int64_t V, int64_t d, int32_t K, size_t* bytes);
 int loca_head_distill(const void* H, int64_t ldh, int64_t N, int64_t d, const void* W, int64_t V, const int32_t* idx,

@@ -337,11 +337,11 @@ struct Deep : Ext {
 // hold one of the epilogue's `rows`.
 // kAhead (narrow and single): what an epilogue has to look up for a tile is on its way while the sums are not
 // complete: a State for each thread; start(State, row of the first tile), ahead(State, row, half tile, row of the next
-// tile) before the sums; the state goes to operator().  With kPacks  void all(float (&v)[128], State, int row, int col0)
-// puts the values in the sums' place in the narrow shape; in the single shape, whose one tile waits for each instruction's
-// first fetch, the state goes to row_of(), which also gets the first column, bool simple(Row) chooses for a warp between
-// value1() and value(), and where low_row is not 0, store_parts(float (&)[32], row, column) takes the values of the rows
-// before it.
+// tile) before the sums; the state goes to operator().  With kPacks  void all(float (&v)[128], State, int row, int col0,
+// int half tile) puts the values in the sums' place in the narrow shape; in the single shape, whose one tile waits for
+// each instruction's first fetch, the state goes to row_of(), which also gets the first column, bool simple(Row) chooses
+// for a warp between value1() and value(), where low_row is not 0, store_parts(float (&)[32], row, column) takes the values
+// of the rows before it, and finish(Row::others, half tile, row) what the values add up to.
 // kFits: the number of k ranges is the device's choice (Fit).
 template <int kShape, bool kAmn, bool kBmn, class Epi, class Ext>
 __global__ void __cluster_dims__(Shape<kShape>::kCtas, 1, 1) __launch_bounds__(THREADS, 1)
@@ -858,6 +858,7 @@ __global__ void __cluster_dims__(Shape<kShape>::kCtas, 1, 1) __launch_bounds__(T
                 }
                 epi.store_parts(f, row, col0 + 32 * b);
               }
+              epi.finish(pre.others, 2 * t.n + h, row);
               continue;
             }
 #pragma unroll
@@ -881,8 +882,9 @@ __global__ void __cluster_dims__(Shape<kShape>::kCtas, 1, 1) __launch_bounds__(T
               }
               store_box_bf16(box, &tmO, lane, col0 + 64 * b, r0, w);
             }
+            epi.finish(pre.others, 2 * t.n + h, row);
           } else if constexpr (Epi::kAhead) {
-            epi.all(v, state, row, col0);
+            epi.all(v, state, row, col0, 2 * t.n + h);
             store([&](int i) { return v[i]; });
           } else {
             auto pre = epi.row_of(row);

@@ -18,7 +18,8 @@
 //                about as much as their own (0.0024 from the 64-bit value in norm, 0.0017 without it); a
 //                second part would cost both products again.  `scale` is applied to the fp32 sums, so it
 //                rounds nothing
-// k_head_target  the target's p - 1 as minus the sum of the others' p.  Where a dW over many rows cuts the
+// k_head_target  the target's p - 1 as minus the sum of the others' p (with a teacher: p - q of a word with more than
+//                half of q as minus the sum of the others' p - q).  Where a dW over many rows cuts the
 //                vocabulary into pieces (N V > 2^31) the sum over all of them comes first, from a pass
 //                over the logits of its own
 // k_head_join    combines a row's maxima and sums in a fixed order: lse, loss, E
@@ -28,12 +29,14 @@
 //   q = softmax(t / tau) over the K,  p = softmax(z / tau) over the vocabulary
 //   loss_n = w_n tau^2 sum_k q_k (log q_k - log p_{i_k}),  dZ = g_n w_n tau (p - q)
 // k_teacher      each position's words in order, a word that comes twice once with both shares, q and
-//                sum q log q; positions without a word are masked
+//                sum q log q, and which word has more than half of q; positions without a word are masked
 //                Beside them goes a table of the first word in each row and 128 columns (2 bytes)
 // The epilogue of a logit tile reads that table while the sums are not complete and goes on from word to word:
-// forward it stores their logits (K of V), backward it takes q off p in fp32, before dZ is rounded.  (Bisection in
-// the row's words and a test for each column took 777 tokens at d = 896, V = 32003 66 and 75 us where the
-// loss without a teacher takes 37 and 47.)
+// forward it stores their logits (K of V), backward it takes q off p in fp32, before dZ is rounded, but for a word with
+// more than half of q: where p and q are both nearly one their difference is no better than lse's rounding (1 - p = 1e-5
+// at lse = 30: 10 % of it), the others' sum is.  (The sum and k_head_target cost 4096 x 2048 x 49152 with both gradients
+// 1 %, one position with dH 16 us of 183.)  Bisection in the row's words and a test for each column took 777 tokens at
+// d = 896, V = 32003 66 and 75 us where the loss without a teacher takes 37 and 47.
 // k_teacher_join as k_head_join, with the sum over the words
 // Computing the logits a second time costs 2 N d V operations; keeping them would cost 4 N V bytes
 // (2.5 GB per 4096 tokens at V = 151936).
@@ -319,7 +322,9 @@ struct Words {
   int32_t* at;   // N x K
   float* q;      // N x K
   float* ent;    // N: sum q log q over the given entries
-  int32_t* live; // N: 0, or -1 where a position has no word (or no share: all its logits -inf)
+  // N: the word with more than half of q, V where there is none, -1 where a position has no word (or no share: all
+  // its logits -inf)
+  int32_t* main;
   uint16_t* table;  // N x pitch: the first word in a half tile (kNoEntry: none)
   int K;
   int pitch;     // half tiles of a row, to a multiple of 8
@@ -387,7 +392,7 @@ __global__ void __launch_bounds__(32 * kTeacherWarps)
   for (int o = 16; o > 0; o >>= 1) mass += __shfl_xor_sync(0xffffffffu, mass, o);
   const float log_mass = logf(mass);
   float ent = 0.f;
-  int count = 0;
+  int count = 0, main = -1;
   for (int i0 = 0; i0 < padded; i0 += 32) {
     const int i = i0 + lane;
     const int32_t w = i < padded ? key[i] : kNoWord;
@@ -407,6 +412,7 @@ __global__ void __launch_bounds__(32 * kTeacherWarps)
     if (first && LOCA_CHECK(n * K + at, N * K)) {
       out.at[n * K + at] = w;
       out.q[n * K + at] = q;
+      if (q > 0.5f) main = w;
       int col, other;
       const int half = half_of(out, w, col);
       const bool more = end < padded && key[end] != kNoWord && half_of(out, key[end], other) == half;
@@ -421,9 +427,10 @@ __global__ void __launch_bounds__(32 * kTeacherWarps)
   }
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) ent += __shfl_xor_sync(0xffffffffu, ent, o);
+  main = __reduce_max_sync(0xffffffffu, main);  // (one lane's at most)
   if (lane == 0) {
     out.ent[n] = ent;
-    out.live[n] = mass == 0.f ? -1 : 0;  // (NaN lives)
+    out.main[n] = mass == 0.f ? -1 : main >= 0 ? main : int32_t(V);  // (NaN lives, without such a word)
   }
 }
 
@@ -518,7 +525,8 @@ struct EpiTeacher {
 };
 
 // Backward: dZ = g tau (p - q) of the same tile, bf16, for the gradient products.  Columns past the vocabulary and
-// rows past the live ones are zero.
+// rows past the live ones are zero.  The entry of a word with more than half of q waits for k_head_target, which gets the
+// sum of the other columns' p - q.
 struct EpiDzTeacher {
   static constexpr bool kPacks = true;
   static constexpr bool kFits = false;
@@ -526,6 +534,7 @@ struct EpiDzTeacher {
   using State = WordState;
   const float* lse;    // this piece's rows
   const float* w;      // w_n dloss_n
+  const int32_t* y;    // the word with more than half of q, or none of [0, V)
   const int32_t* idx;
   Words words;
   float tau, inv_tau;
@@ -534,6 +543,8 @@ struct EpiDzTeacher {
   int64_t v_first;     // this piece's first vocabulary column
   int v_cols;          // its columns of the vocabulary
   int half_first;      // its first half tile
+  float* others;       // (2 column tiles) x pitch
+  int64_t pitch;       // rows of a piece
   // Few rows: dZ in two bf16 parts (2^-17), the second low_row rows behind the first, where the tile of 128 rows has
   // room for it, so that it costs no product.  The gradient of a row of few words is as good as its largest entries.
   int low_row;
@@ -559,8 +570,10 @@ struct EpiDzTeacher {
   }
 
   struct Row {
-    float lse, g, q;
+    float lse, g, others;
+    float keep, q;  // what becomes of the next word's p: p - q, or 0
     int end;   // the columns that count (none in rows past the live ones)
+    int main;  // the column of the word with more than half of q
     int next;  // the next word's column, its place and whether another may follow
     int k;
     bool more;
@@ -574,10 +587,13 @@ struct EpiDzTeacher {
     Row r;
     const bool here = st.entry != kNoEntry;  // (the table has nothing for rows past the live ones)
     r.end = row_first + row < *count ? v_cols : 0;
+    r.main = int(y[row] - v_first);
+    r.others = 0.f;
     r.k = st.entry >> 7 & 255;
     r.from = int64_t(st.n) * words.K;
     r.next = here ? col0 + int(st.entry & 127) : kNoWord;
-    r.q = here ? __ldg(words.q + r.from + r.k) : 0.f;
+    r.keep = r.next != r.main ? 1.f : 0.f;
+    r.q = here && r.next != r.main ? __ldg(words.q + r.from + r.k) : 0.f;
     r.more = here && (st.entry >> 15 & 1);
     r.lse = lse[row];
     r.g = w[row] * tau;
@@ -586,29 +602,37 @@ struct EpiDzTeacher {
   __device__ __forceinline__ bool simple(const Row& r) const { return !__any_sync(0xffffffffu, r.more); }
   __device__ __forceinline__ float value1(Row& r, int col, float z) const {
     float p = exp_diff(fmaf(z, inv_tau, -r.lse), 0.f);
-    if (col == r.next) p -= r.q;
-    return col < r.end ? r.g * p : 0.f;
+    if (col == r.next) p = fmaf(p, r.keep, -r.q);
+    p = col < r.end ? p : 0.f;
+    r.others += p;
+    return r.g * p;
   }
   __device__ __forceinline__ float value(Row& r, int col, float z) const {
     if (col >= r.end) return 0.f;
     float p = exp_diff(fmaf(z, inv_tau, -r.lse), 0.f);
     if (col == r.next) {
-      p -= r.q;
+      p = fmaf(p, r.keep, -r.q);
       r.next = kNoWord;
       if (++r.k < words.K) {
         const int32_t v = __ldg(words.at + r.from + r.k);
         r.q = __ldg(words.q + r.from + r.k);  // (with it, not behind it: behind the last word nobody takes it)
         if (v != kNoWord) r.next = int(v - v_first);
+        r.keep = r.next != r.main ? 1.f : 0.f;
+        if (r.next == r.main) r.q = 0.f;
       }
     }
+    r.others += p;
     return r.g * p;
+  }
+  __device__ __forceinline__ void finish(float sum, int part, int row) const {
+    if (LOCA_CHECK(row, pitch)) others[int64_t(part) * pitch + row] = sum;
   }
   // p of every column, then q off it, then the factor.  The first words of the warp's rows go one by one, each against
   // all columns (260 instructions); where a row has more than kOneByOne, the rest column by column, where a lane that
   // meets its word waits for the next.  (Loss and dH, one by one alone, column by column alone, and both: 4217 positions with
   // 96 words at d = 744, V = 48060 1102, 1700 and 1034 us; 192 with 87 words at V = 4839 163, 125 and 125.)
   static constexpr int kOneByOne = 8;
-  __device__ __forceinline__ void all(float (&v)[128], const State& st, int row, int col0) const {
+  __device__ __forceinline__ void all(float (&v)[128], const State& st, int row, int col0, int part) const {
     const float row_lse = lse[row], g = w[row] * tau;
     const int end = row_first + row < *count ? v_cols - col0 : 0;  // the columns that count (none in rows past the live ones)
     const bool here = st.entry != kNoEntry;  // (the table has nothing for rows past the live ones)
@@ -617,7 +641,9 @@ struct EpiDzTeacher {
     int k = st.entry >> 7 & 255;
     int last = here ? st.entry >> 15 & 1 ? words.K - 1 : k : -1;  // no word here behind it
     int at = here ? int(st.entry & 127) : -1;
-    float q = here ? __ldg(words.q + from + k) : 0.f;
+    const int main = int(y[row] - first);
+    // what becomes of the word's p: p - q, or 0
+    float q = here && at != main ? __ldg(words.q + from + k) : 0.f, keep = at != main ? 1.f : 0.f;
     int32_t next = kNoWord;  // the word behind, and its share
     float next_q = 0.f;
     auto fetch = [&] {
@@ -629,7 +655,8 @@ struct EpiDzTeacher {
     };
     auto advance = [&] {  // (a column below 0 or from 128 on is none of these)
       at = next < first + 128 ? next - first : -1;
-      q = next_q;
+      keep = at != main ? 1.f : 0.f;
+      q = at != main ? next_q : 0.f;
       fetch();
     };
     fetch();
@@ -639,19 +666,25 @@ struct EpiDzTeacher {
     for (; n < kOneByOne && __any_sync(0xffffffffu, at >= 0); ++n) {
 #pragma unroll
       for (int i = 0; i < 128; ++i)
-        if (i == at) v[i] -= q;
+        if (i == at) v[i] = fmaf(v[i], keep, -q);
       advance();
     }
     if (n == kOneByOne && __any_sync(0xffffffffu, at >= 0)) {
 #pragma unroll
       for (int i = 0; i < 128; ++i)
         if (i == at) {
-          v[i] -= q;
+          v[i] = fmaf(v[i], keep, -q);
           advance();
         }
     }
+    float s[4] = {};
 #pragma unroll
-    for (int i = 0; i < 128; ++i) v[i] = i < end ? g * v[i] : 0.f;
+    for (int i = 0; i < 128; ++i) {
+      v[i] = i < end ? v[i] : 0.f;
+      s[i & 3] += v[i];
+      v[i] *= g;
+    }
+    finish((s[0] + s[1]) + (s[2] + s[3]), part, row);
   }
 };
 
@@ -765,7 +798,7 @@ __global__ void __launch_bounds__(kJoinThreads)
   wait_for_previous();
   launch_dependents();
   const int n = blockIdx.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  if (words.live[n] < 0) {
+  if (words.main[n] < 0) {
     if (threadIdx.x == 0) {
       loss[n] = 0.f;
       if (lse) lse[n] = 0.f;
@@ -820,11 +853,14 @@ __global__ void __launch_bounds__(kJoinThreads)
 }
 
 // The target's entry of dZ: p - 1 = -(sum of the others' p).  As a difference it would be no better than
-// lse's rounding to fp32: at lse = 40 and 1 - p = 1e-5 a fifth of it.  32 rows per block, `blockDim.y` groups of
-// partial sums.  add: the sum goes on from `sum`; keep: it goes there; put: it is complete.
+// lse's rounding to fp32: at lse = 40 and 1 - p = 1e-5 a fifth of it.  With a teacher p - q = -(sum of the others' p - q)
+// where one word has more than half of q: the others' p, which carry lse's rounding too, then have less of the error than
+// the word's own.  32 rows per block, `blockDim.y` groups of partial sums.  add: the sum goes on from `sum`; keep: it goes
+// there; put: it is complete.  low_row > 0: the second part of the entry comes so many rows behind.
 __global__ void __launch_bounds__(1024)
     k_head_target(const float* __restrict__ part, int64_t pitch, int nparts, Rows in, int64_t row_first, float* sum,
-                  int add, int keep, int put, int64_t v_first, int64_t v_cols, __nv_bfloat16* dz, int64_t ldz) {
+                  int add, int keep, int put, int64_t v_first, int64_t v_cols, float factor, int low_row,
+                  __nv_bfloat16* dz, int64_t ldz) {
   __shared__ float sh[32][33];
   wait_for_previous();
   launch_dependents();
@@ -843,8 +879,12 @@ __global__ void __launch_bounds__(1024)
   if (keep) sum[row] = s;
   if (!isfinite(in.lse[row_first + row])) s = NAN;  // (also where there is no other column to say so)
   const int64_t at = int64_t(in.y[row_first + row]) - v_first;
-  if (put && at >= 0 && at < v_cols && LOCA_CHECK(at, ldz))
-    dz[row * ldz + at] = __float2bfloat16_rn(-in.w[row_first + row] * s);
+  if (put && at >= 0 && at < v_cols && LOCA_CHECK(at, ldz)) {
+    const float v = -(in.w[row_first + row] * factor) * s;
+    const __nv_bfloat16 hi = __float2bfloat16_rn(v);
+    dz[row * ldz + at] = hi;
+    if (low_row > 0 && LOCA_CHECK(row, low_row)) dz[(row + low_row) * ldz + at] = __float2bfloat16_rn(v - __bfloat162float(hi));
+  }
 }
 
 // One thread per 8 elements of a row; the k ranges' sums are loaded four at a time and added in order.
@@ -1015,7 +1055,7 @@ int dh_splits(int64_t n, int64_t rows, int64_t d, int64_t vc) {
 }
 // fill: room for as many ranges of the live rows as fill four rounds of the pairs (fit_splits(); without it 3081 live of 4096
 // tokens at d = 2048, V = 49152 are three rounds of 256 k-blocks, with it three of 192: dH of distillation 952 and 855 us).
-BwdWs bwd_ws(int64_t N, int64_t V, int64_t d, bool dh, bool dw, bool target, bool fill) {
+BwdWs bwd_ws(int64_t N, int64_t V, int64_t d, bool dh, bool dw, bool fill) {
   BwdWs o{};
   o.rows = rows_ws(N, d);
   const int64_t np = round_up(N < 1 ? 1 : N, gp::TM);
@@ -1043,8 +1083,8 @@ BwdWs bwd_ws(int64_t N, int64_t V, int64_t d, bool dh, bool dw, bool target, boo
   size_t at = o.rows.total;
   o.dz = at; at += align256(2 * size_t(o.piece) * size_t(o.vc));
   o.part = at; at += align256(4 * size_t(o.room) * gp::TM * size_t(d));
-  o.others = at; at += target ? align256(4 * 2 * size_t(dz_tiles(N, o.vc)) * size_t(o.piece)) : 0;
-  o.sum = at; at += target ? align256(4 * size_t(o.piece)) : 0;
+  o.others = at; at += align256(4 * 2 * size_t(dz_tiles(N, o.vc)) * size_t(o.piece));
+  o.sum = at; at += align256(4 * size_t(o.piece));
   o.total = at;
   return o;
 }
@@ -1204,11 +1244,44 @@ cudaError_t backward_pieces(const Backward& b, const Before& before, const MakeD
   return cudaSuccess;
 }
 
+// backward_pieces() of a dZ whose entries at the rows' words `y` are minus the sum of the others (k_head_target), times
+// `factor`.  tiles(p0, rows, v0, vn, width, others) leaves the other entries in the workspace and the sums of tiles of
+// width(vn) columns in `others`.
+template <class Width, class Tiles>
+cudaError_t backward_with_target(const Backward& b, float factor, const Width& width_of, const Tiles& tiles) {
+  const BwdWs& lay = b.lay;
+  float* others = reinterpret_cast<float*>(b.ws + lay.others);
+  float* sum = reinterpret_cast<float*>(b.ws + lay.sum);
+  const int64_t V = b.V;
+  // dZ of the vocabulary columns v0 .. v0 + vn.  all: they are all there are, so the sum of the others that
+  // the target's entry takes is whole; done: earlier calls have made it; neither: this call adds to it
+  auto make_dz = [&](int64_t p0, int64_t rows, int64_t v0, int64_t vn, bool all, bool done) {
+    const int width = width_of(vn);
+    const cudaError_t e = tiles(p0, rows, v0, vn, width, others);
+    if (e != cudaSuccess) return e;
+    const int nparts = done ? 0 : int(2 * ((vn + width - 1) / width));
+    return gp::launch_early(k_head_target, dim3(unsigned(rows / 32)), dim3(32, nparts >= 128 ? 32 : 8), 0, b.s, others,
+                            lay.piece, nparts, b.r, p0, sum, int(done || v0 > 0), int(!all && !done), int(all || done), v0,
+                            vn, factor, b.low_row, reinterpret_cast<__nv_bfloat16*>(b.ws + lay.dz), lay.vc);
+  };
+  const bool whole = V <= lay.vc;
+  return backward_pieces(
+      b,
+      [&](int64_t p0, int64_t rows) {
+        for (int64_t v0 = 0; v0 < V && !whole; v0 += lay.vc) {
+          const cudaError_t e = make_dz(p0, rows, v0, V - v0 < lay.vc ? V - v0 : lay.vc, false, false);
+          if (e != cudaSuccess) return e;
+        }
+        return cudaSuccess;
+      },
+      [&](int64_t p0, int64_t rows, int64_t v0, int64_t vn) { return make_dz(p0, rows, v0, vn, whole, !whole); });
+}
+
 }  // namespace
 
 size_t head_loss_workspace_bytes(int64_t N, int64_t V, int64_t d, int C) { return fwd_ws(N, V, d, C).total; }
 size_t head_loss_backward_workspace_bytes(int64_t N, int64_t V, int64_t d, bool dh, bool dw) {
-  return bwd_ws(N, V, d, dh, dw, true, false).total;
+  return bwd_ws(N, V, d, dh, dw, false).total;
 }
 
 cudaError_t launch_head_loss(const void* H, int64_t ldh, int64_t N, int64_t d, const void* W, int64_t V,
@@ -1241,39 +1314,19 @@ cudaError_t launch_head_loss_backward(const void* H, int64_t ldh, int64_t N, int
                                       const int32_t* y, const float* w, const float* lse, const float* dloss,
                                       float scale, void* dH, int64_t lddh, void* dW, void* workspace, int32_t* status,
                                       cudaStream_t s) {
-  const BwdWs lay = bwd_ws(N, V, d, dH != nullptr, dW != nullptr, true, false);
+  const BwdWs lay = bwd_ws(N, V, d, dH != nullptr, dW != nullptr, false);
   uint8_t* ws = static_cast<uint8_t*>(workspace);
   const Rows r = rows_at(workspace, lay.rows);
   cudaError_t e = launch_rows(H, ldh, N, d, V, y, w, dloss, lse, r, nullptr, nullptr, nullptr, 0, dH, lddh, s);
   if (e != cudaSuccess) return e;
-  float* others = reinterpret_cast<float*>(ws + lay.others);
-  float* sum = reinterpret_cast<float*>(ws + lay.sum);
   const Backward b{lay, r, ws, N, d, static_cast<const __nv_bfloat16*>(W), V, scale, static_cast<__nv_bfloat16*>(dH), lddh,
                    static_cast<__nv_bfloat16*>(dW), status, s};
-  // dZ of the vocabulary columns v0 .. v0 + vn.  all: they are all there are, so the sum of the others' p that
-  // the target's entry takes is whole; done: earlier calls have made it; neither: this call adds to it
-  auto make_dz = [&](int64_t p0, int64_t rows, int64_t v0, int64_t vn, bool all, bool done) {
-    const int width = back_width(N, vn);
-    const cudaError_t e =
-        logit_tiles(b, p0, rows, v0, vn, EpiDz{r.lse + p0, r.w + p0, r.y + p0, r.count, p0, v0, int(vn), others, lay.piece},
-                    width);
-    if (e != cudaSuccess) return e;
-    const int nparts = done ? 0 : int(2 * ((vn + width - 1) / width));
-    return gp::launch_early(k_head_target, dim3(unsigned(rows / 32)), dim3(32, nparts >= 128 ? 32 : 8), 0, s, others,
-                            lay.piece, nparts, r, p0, sum, int(done || v0 > 0), int(!all && !done), int(all || done), v0,
-                            vn, reinterpret_cast<__nv_bfloat16*>(ws + lay.dz), lay.vc);
-  };
-  const bool whole = V <= lay.vc;
-  return backward_pieces(
-      b,
-      [&](int64_t p0, int64_t rows) {
-        for (int64_t v0 = 0; v0 < V && !whole; v0 += lay.vc) {
-          const cudaError_t e = make_dz(p0, rows, v0, V - v0 < lay.vc ? V - v0 : lay.vc, false, false);
-          if (e != cudaSuccess) return e;
-        }
-        return cudaSuccess;
-      },
-      [&](int64_t p0, int64_t rows, int64_t v0, int64_t vn) { return make_dz(p0, rows, v0, vn, whole, !whole); });
+  return backward_with_target(
+      b, 1.f, [&](int64_t cols) { return back_width(N, cols); },
+      [&](int64_t p0, int64_t rows, int64_t v0, int64_t vn, int width, float* others) {
+        return logit_tiles(b, p0, rows, v0, vn,
+                           EpiDz{r.lse + p0, r.w + p0, r.y + p0, r.count, p0, v0, int(vn), others, lay.piece}, width);
+      });
 }
 
 // ------------------------------------------------------------------ distillation
@@ -1281,7 +1334,7 @@ namespace {
 
 struct WordsWs {
   int width, piece, of_piece, pitch;
-  size_t at, q, ent, live, table, total;
+  size_t at, q, ent, main, table, total;
 };
 WordsWs words_ws(int64_t N, int64_t V, int K, int width, int64_t piece, size_t from) {
   WordsWs o{};
@@ -1292,7 +1345,7 @@ WordsWs words_ws(int64_t N, int64_t V, int K, int width, int64_t piece, size_t f
   o.at = from; from += align256(4 * size_t(N) * size_t(K));
   o.q = from; from += align256(4 * size_t(N) * size_t(K));
   o.ent = from; from += align256(4 * size_t(N));
-  o.live = from; from += align256(4 * size_t(N));
+  o.main = from; from += align256(4 * size_t(N));
   o.table = from; from += align256(2 * size_t(N) * size_t(o.pitch));
   o.total = from;
   return o;
@@ -1314,7 +1367,7 @@ DistillWs distill_ws(int64_t N, int64_t V, int64_t d, int K) {
 cudaError_t launch_teacher(const int32_t* idx, const float* t, int64_t N, int64_t V, int K, float tau, uint8_t* ws,
                            const WordsWs& lay, Words* out, cudaStream_t s) {
   *out = Words{reinterpret_cast<int32_t*>(ws + lay.at), reinterpret_cast<float*>(ws + lay.q),
-               reinterpret_cast<float*>(ws + lay.ent), reinterpret_cast<int32_t*>(ws + lay.live),
+               reinterpret_cast<float*>(ws + lay.ent), reinterpret_cast<int32_t*>(ws + lay.main),
                reinterpret_cast<uint16_t*>(ws + lay.table), K, lay.pitch, lay.width, lay.piece, lay.of_piece};
   int padded = 32;
   while (padded < K) padded *= 2;
@@ -1334,7 +1387,7 @@ WordsWs back_words(int64_t N, int64_t V, int K, const BwdWs& lay) {
 int head_distill_max_words() { return kMostWords; }
 size_t head_distill_workspace_bytes(int64_t N, int64_t V, int64_t d, int K) { return distill_ws(N, V, d, K).total; }
 size_t head_distill_backward_workspace_bytes(int64_t N, int64_t V, int64_t d, int K, bool dh, bool dw) {
-  return back_words(N, V, K, bwd_ws(N, V, d, dh, dw, false, true)).total;
+  return back_words(N, V, K, bwd_ws(N, V, d, dh, dw, true)).total;
 }
 
 cudaError_t launch_head_distill(const void* H, int64_t ldh, int64_t N, int64_t d, const void* W, int64_t V,
@@ -1368,7 +1421,7 @@ cudaError_t launch_head_distill(const void* H, int64_t ldh, int64_t N, int64_t d
                             static_cast<const float2*>(part), lay.fwd.piece, lay.words.of_piece, static_cast<const float*>(zk),
                             words, w, tau, 1.f / tau, loss, lse);
   }
-  e = launch_rows(H, ldh, N, d, 1, words.live, w, nullptr, nullptr, r, loss, lse, nullptr, 0, nullptr, 0, s);
+  e = launch_rows(H, ldh, N, d, V + 1, words.main, w, nullptr, nullptr, r, loss, lse, nullptr, 0, nullptr, 0, s);
   if (e != cudaSuccess) return e;
   const int64_t np = round_up(N, gp::TM);
   for (int64_t p0 = 0; p0 < np; p0 += lay.fwd.piece) {
@@ -1388,7 +1441,7 @@ cudaError_t launch_head_distill_backward(const void* H, int64_t ldh, int64_t N, 
                                          const int32_t* idx, const float* t, int K, float tau, const float* w,
                                          const float* lse, const float* dloss, float scale, void* dH, int64_t lddh,
                                          void* dW, void* workspace, int32_t* status, cudaStream_t s) {
-  const BwdWs lay = bwd_ws(N, V, d, dH != nullptr, dW != nullptr, false, true);
+  const BwdWs lay = bwd_ws(N, V, d, dH != nullptr, dW != nullptr, true);
   const WordsWs wlay = back_words(N, V, K, lay);
   uint8_t* ws = static_cast<uint8_t*>(workspace);
   Words words;
@@ -1396,18 +1449,18 @@ cudaError_t launch_head_distill_backward(const void* H, int64_t ldh, int64_t N, 
   if (e != cudaSuccess) return e;
   const Rows r = rows_at(workspace, lay.rows);
   const int low_row = N <= gp::HALF / 2 ? gp::HALF / 2 : 0;
-  e = launch_rows(H, ldh, N, d, 1, words.live, w, dloss, lse, r, nullptr, nullptr, nullptr, 0, dH, lddh, s, low_row);
+  e = launch_rows(H, ldh, N, d, V + 1, words.main, w, dloss, lse, r, nullptr, nullptr, nullptr, 0, dH, lddh, s, low_row);
   if (e != cudaSuccess) return e;
   const Backward b{lay, r, ws, N, d, static_cast<const __nv_bfloat16*>(W), V, scale, static_cast<__nv_bfloat16*>(dH), lddh,
                    static_cast<__nv_bfloat16*>(dW), status, s, low_row};
-  return backward_pieces(
-      b, [](int64_t, int64_t) { return cudaSuccess; },
-      [&](int64_t p0, int64_t rows, int64_t v0, int64_t vn) {
+  return backward_with_target(
+      b, tau, [&](int64_t) { return wlay.width; },
+      [&](int64_t p0, int64_t rows, int64_t v0, int64_t vn, int width, float* others) {
         return logit_tiles(b, p0, rows, v0, vn,
-                           EpiDzTeacher{r.lse + p0, r.w + p0, r.idx + p0, words, tau, 1.f / tau, r.count, p0, v0, int(vn),
-                                        int(v0 / wlay.piece) * wlay.of_piece, b.low_row,
+                           EpiDzTeacher{r.lse + p0, r.w + p0, r.y + p0, r.idx + p0, words, tau, 1.f / tau, r.count, p0, v0,
+                                        int(vn), int(v0 / wlay.piece) * wlay.of_piece, others, lay.piece, b.low_row,
                                         reinterpret_cast<__nv_bfloat16*>(ws + lay.dz), lay.vc},
-                           wlay.width);
+                           width);
       });
 }
 
