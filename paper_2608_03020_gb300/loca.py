@@ -234,6 +234,24 @@ def _empty(nbytes: int, device, stream=None):
         return torch.empty(nbytes, dtype=torch.uint8, device=device)
 
 
+class _Owned:
+    """Device memory of an object of this module (:func:`_empty`), which may go out of scope while calls that use it
+    wait: the allocator is told of every stream of theirs but the one that the memory belongs to, once of each."""
+
+    def __init__(self, buf, stream=None):
+        self.buf, self.streams = buf, {_stream(stream).value}
+
+
+def _use(stream, *kept):
+    """Handle of the call's stream, on which it uses the memory of the objects ``kept`` (``None``: none)."""
+    on = _stream(stream)
+    for k in kept:
+        if k is not None and on.value not in k._memory.streams:
+            k._memory.buf.record_stream(torch.cuda.current_stream() if stream is None else _torch_stream(stream))
+            k._memory.streams.add(on.value)
+    return on
+
+
 def _workspace(nbytes: int, device, given=None, stream=None):
     if nbytes == 0:
         return None
@@ -867,6 +885,7 @@ class AdapterSet:
         _check(lib().loca_adapter_packed_size(n, d_in, d_out, k, ctypes.byref(out)), "loca_adapter_packed_size")
         self.n, self.d_in, self.d_out, self.k = int(n), int(d_in), int(d_out), int(k)
         self.packed = torch.zeros(out.value, dtype=torch.uint8, device=device)
+        self._memory = _Owned(self.packed)
         if not torch.cuda.is_current_stream_capturing():
             torch.cuda.current_stream().synchronize()  # the zeros come before a pack on any stream
 
@@ -877,8 +896,9 @@ class AdapterSet:
         if (tuple(A.shape) != (self.n, self.d_in, self.k) or tuple(B.shape) != (self.n, self.d_out, self.k)
                 or (scale is not None and scale.numel() != self.n)):
             raise ValueError("A must be n x d_in x k, B n x d_out x k and scale have n entries")
+        on = _use(stream, self)
         rc = lib().loca_adapter_pack(_ptr(A), _ptr(B), _code(A.dtype), self.n, self.d_in, self.d_out, self.k, _ptr(scale),
-                                     _ptr(self.packed), _stream(stream))
+                                     _ptr(self.packed), on)
         _check(rc, "loca_adapter_pack")
         return self
 
@@ -894,13 +914,15 @@ class AdapterPlan:
         out = ctypes.c_size_t(0)
         _check(lib().loca_adapter_plan_size(self.N, self.n, ctypes.byref(out)), "loca_adapter_plan_size")
         self.buf = _empty(max(out.value, 256), ids.device, stream)
+        self._memory = _Owned(self.buf, stream)
         self.update(ids, stream=stream)
 
     def update(self, ids, stream=None):
         _dev(ids, "ids", torch.int32, 1)
         if ids.numel() != self.N:
             raise ValueError(f"the plan is for {self.N} tokens, got {ids.numel()}")
-        rc = lib().loca_adapter_plan(_ptr(ids), self.N, self.n, _ptr(self.buf), _stream(stream))
+        on = _use(stream, self)
+        rc = lib().loca_adapter_plan(_ptr(ids), self.N, self.n, _ptr(self.buf), on)
         _check(rc, "loca_adapter_plan")
         return self
 
@@ -918,22 +940,19 @@ def _adapter_args(X, W, adapters, plan, stream):
                          f"W {tuple(W.shape)}")
     if plan.N != N or plan.n != adapters.n:
         raise ValueError(f"the plan is for {plan.N} tokens and {plan.n} adapters, got {N} and {adapters.n}")
-    if stream is not None:  # their memory outlives them until this call is done
-        for t in (adapters.packed, plan.buf):
-            t.record_stream(_torch_stream(stream))
-    return ldx, N, d_in
+    return ldx, N, d_in, _use(stream, adapters, plan)
 
 
 def loca_adapter_apply(X, W, adapters, plan, Y, workspace=None, stream=None):
     """``Y = X W^T + s_a (X A_a) B_a^T`` for tokens with an adapter each (or none): ``X`` N x d_in and
     ``Y`` N x d_out bf16 (rows may be spaced), ``W`` d_out x d_in bf16, ``adapters`` an
     :class:`AdapterSet`, ``plan`` an :class:`AdapterPlan` of the tokens' adapters."""
-    ldx, N, d_in = _adapter_args(X, W, adapters, plan, stream)
+    ldx, N, d_in, on = _adapter_args(X, W, adapters, plan, stream)
     ldy = _rows2d(Y, "Y", torch.bfloat16, (N, adapters.d_out))
     nbytes = adapter_workspace_size(N, d_in, adapters.d_out, adapters.k, adapters.n)
     ws = _workspace(nbytes, X.device, workspace, stream)
     rc = lib().loca_adapter_apply(_ptr(X), ldx, N, d_in, _ptr(W), adapters.d_out, _ptr(adapters.packed), adapters.n,
-                                  adapters.k, _ptr(plan.buf), _ptr(Y), ldy, _ptr(ws), nbytes, _stream(stream))
+                                  adapters.k, _ptr(plan.buf), _ptr(Y), ldy, _ptr(ws), nbytes, on)
     _check(rc, "loca_adapter_apply")
 
 
@@ -941,7 +960,7 @@ def loca_adapter_backward(X, dY, W, adapters, plan, dX=None, dA=None, dB=None, w
     """Gradients of :func:`loca_adapter_apply` for the frozen projection's input (``dX``, N x d_in
     bf16) and the adapters (``dA`` n x d_in x k, ``dB`` n x d_out x k, float32 or bfloat16); the
     adapters as last packed."""
-    ldx, N, d_in = _adapter_args(X, W, adapters, plan, stream)
+    ldx, N, d_in, on = _adapter_args(X, W, adapters, plan, stream)
     lddy = _rows2d(dY, "dY", torch.bfloat16, (N, adapters.d_out))
     lddx = 0 if dX is None else _rows2d(dX, "dX", torch.bfloat16, (N, d_in))
     both = (torch.float32, torch.bfloat16)
@@ -955,7 +974,7 @@ def loca_adapter_backward(X, dY, W, adapters, plan, dX=None, dA=None, dB=None, w
     ws = _workspace(nbytes, X.device, workspace, stream)
     rc = lib().loca_adapter_backward(_ptr(X), ldx, _ptr(dY), lddy, N, d_in, _ptr(W), adapters.d_out,
                                      _ptr(adapters.packed), adapters.n, adapters.k, _ptr(plan.buf), _ptr(dX), lddx,
-                                     _ptr(dA), _ptr(dB), _code(kind), _ptr(ws), nbytes, _stream(stream))
+                                     _ptr(dA), _ptr(dB), _code(kind), _ptr(ws), nbytes, on)
     _check(rc, "loca_adapter_backward")
 
 
@@ -963,7 +982,7 @@ class Q4Weight:
     """The device layout of a frozen projection in 4 bits: ``codes`` (d_out x d_in / 2 uint8, the even column in
     the low four bits), ``scales`` (d_out x d_in / group, float32 or bfloat16; group 32, 64 or 128) and optional
     ``zeros`` (like scales, uint8 0 .. 15; default 8), ``W = scale (code - zero)``.  Packs at once; the arguments are
-    not needed afterwards."""
+    not needed afterwards, also where the stream has not come to the packing yet."""
 
     def __init__(self, codes, scales, zeros=None, stream=None):
         _dev(codes, "codes", torch.uint8, 2)
@@ -984,6 +1003,11 @@ class Q4Weight:
         _check(lib().loca_q4_packed_size(d_out, d_in, self.group, self.scale_code, int(self.with_zeros), ctypes.byref(out)),
                "loca_q4_packed_size")
         self.packed = _empty(out.value, codes.device, stream)
+        self._memory = _Owned(self.packed, stream)
+        on = torch.cuda.current_stream() if stream is None else _torch_stream(stream)
+        for t in (codes, scales, zeros):
+            if t is not None:
+                t.record_stream(on)
         rc = lib().loca_q4_pack(_ptr(codes), _ptr(scales), self.scale_code, _ptr(zeros), d_out, d_in, self.group,
                                 _ptr(self.packed), _stream(stream))
         _check(rc, "loca_q4_pack")
@@ -1012,16 +1036,13 @@ def loca_q4_apply(X, weight, Y, adapters=None, plan=None, workspace=None, stream
             raise ValueError(f"the adapters are for a {adapters.d_out} x {adapters.d_in} projection")
         if plan.N != N or plan.n != n:
             raise ValueError(f"the plan is for {plan.N} tokens and {plan.n} adapters, got {N} and {n}")
-    kept = [weight.packed] + ([] if adapters is None else [adapters.packed, plan.buf])
-    _same_device(X, Y, *kept)
-    if stream is not None:  # their memory outlives them until this call is done
-        for t in kept:
-            t.record_stream(_torch_stream(stream))
+    _same_device(X, Y, weight.packed, None if adapters is None else adapters.packed, None if plan is None else plan.buf)
+    on = _use(stream, weight, adapters, plan)
     nbytes = q4_workspace_size(N, d_in, weight.d_out, k, n)
     ws = _workspace(nbytes, X.device, workspace, stream)
     rc = lib().loca_q4_apply(_ptr(X), ldx, N, d_in, _ptr(weight.packed), weight.d_out, weight.group, weight.scale_code,
                              int(weight.with_zeros), None if adapters is None else _ptr(adapters.packed), n, k,
-                             None if plan is None else _ptr(plan.buf), _ptr(Y), ldy, _ptr(ws), nbytes, _stream(stream))
+                             None if plan is None else _ptr(plan.buf), _ptr(Y), ldy, _ptr(ws), nbytes, on)
     _check(rc, "loca_q4_apply")
 
 
