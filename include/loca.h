@@ -540,7 +540,8 @@ int loca_head_loss_backward(const void* H, int64_t ldh, int64_t N, int64_t d, co
  *         counts with both its logits.  A position without an entry, or with logits of -inf alone, is
  *         masked: its loss, lse and gradients are 0, whatever H holds there
  * t       N x K float; -inf gives a word no share, NaN or +inf make the position's loss and gradients NaN
- * tau     > 0, the temperature; tau^2 and 1 / tau finite
+ * tau     > 0, the temperature; tau^2 and log2(e) / tau finite.  z / tau and t / tau are formed in fp32: a position
+ *         where they pass its range has outputs that are not finite
  * H, W, w, loss, lse, dloss, grad_scale, dH, dW, limits, arithmetic and scratch memory (and 8 bytes for each entry
  * and 2 for each position and 128 words; for dH up to 160 MB more) as for loca_head_loss and its backward call; lse is that of z / tau.  q is taken
  * off in fp32 before dZ is rounded: an entry has an error of some 2^-19 of p (lse's rounding).  The entry of a word with

@@ -101,8 +101,9 @@ int check_distill(int64_t N, int64_t V, int64_t d, int32_t K, float tau) {
   if (rc != LOCA_OK) return rc;
   if (K < 1 || K > head_distill_max_words())
     return fail(LOCA_ERR_SHAPE, "need 1 <= K <= %d words, got %d", head_distill_max_words(), K);
-  if (!(tau > 0.f) || !std::isfinite(tau * tau) || !std::isfinite(1.f / tau))
-    return fail(LOCA_ERR_INVALID_ARG, "tau must be positive, tau^2 and 1 / tau finite");
+  constexpr float kLog2e = 1.4426950408889634f;  // (the kernels' exponentials are to the base 2)
+  if (!(tau > 0.f) || !std::isfinite(tau * tau) || !std::isfinite(kLog2e / tau))
+    return fail(LOCA_ERR_INVALID_ARG, "tau must be positive, tau^2 and log2(e) / tau finite");
   return LOCA_OK;
 }
 int check_q4(int64_t d_out, int64_t d_in, int32_t group, int scale_dtype) {
