@@ -34,8 +34,8 @@ namespace {
 using namespace tc;
 
 constexpr int kSegKb = 64;             // 4096 k per accumulation segment: outputs are rounded to bf16
-// dX sums 2 f terms, and a wide tile has one running sum: up to 2048 steps of at most 2^-22 of it, within 2^-11
-// where its rounding is 2^-9.  1531 x 5120 over k = 27312: one round of 60 wide tiles without ranges, against five
+// dX sums 2 f terms, and a wide tile has one running sum: up to 2048 steps that lose at most 2^-22 of it each, 2^-11 in
+// all, where a rounding to bf16 moves the value by up to 2^-8 of it.  1531 x 5120 over k = 27312: one round of 60 wide tiles without ranges, against five
 // ranges and their join (dX after dG and dU 250 us, 265 with ranges).
 constexpr int64_t kLongK = 32768;
 constexpr int64_t kRowBytes = int64_t(1) << 30;  // dG and dU of a piece of the rows (dX alone)

@@ -2,8 +2,9 @@
 // 256 x 256 tile left to the caller:  D[m, n] = sum_k A[m, k] B[n, k]   (bf16 in, fp32 sums).
 //
 // Used by the head loss (logit tiles that never leave the chip, and the two gradient products), by the
-// adapter projection and by the gated feed-forward (two products that share A, side by side).  Each operand is K-major (k contiguous) or MN-major (m or n
-// contiguous); the tensor maps and the MMA descriptors carry the difference.
+// adapter projection and by the gated feed-forward (two products that share A, side by side).  Each operand
+// is K-major (k contiguous) or MN-major (m or n contiguous); the tensor maps and the MMA descriptors carry the
+// difference.
 //
 // Three shapes.  Narrow: a pair of CTAs holds a 256 x 256 fp32 tile (128 rows per CTA: half of
 // TMEM); the other half of TMEM takes the next tile while eight warps read this one.  Wide: 256 x 512,
@@ -16,7 +17,7 @@
 // Single: up to 128 rows of A in all (a few tokens against a vocabulary).  A pair would leave its odd CTA
 // multiplying zero rows, so each CTA works alone on 128 x 256 tiles, with the narrow shape's segments
 // and two buffers; B's read from HBM is then the bound.  With B K-major its tiles may be narrower than
-// 256 columns (`width`, a multiple of 16), so that the last round of CTAs is as full as the others, and
+// 256 columns (`width`, a multiple of 16; of twin products each `width` columns, a multiple of 8), so that the last round of CTAs is as full as the others, and
 // A's loads bring only the rows there are (the MMA's other rows read what lies behind; nobody reads
 // their sums): the ring is as deep as that allows, in at most 8 stages (16 or 24 gained nothing) of one, two or four
 // k-blocks.
@@ -28,9 +29,11 @@
 // sum at every step, always toward zero.  The sums restart every `seg_kb` k-blocks and the epilogue
 // warps add the segments in registers with round-to-nearest additions, which bounds that bias whatever
 // K is (a logit at K = 5120 comes out ~10x nearer to its 64-bit value than with one accumulator).  A
-// segment is also the unit of the TMEM double buffer.  The wide shape never restarts: it serves outputs
-// that are the sum itself, rounded to bf16, with K up to kWideK.  A step loses up to 2^-22 of the
-// running sum, so 1024 steps lose up to 2^-12 of it, within the rounding's 2^-9.  It does not serve logits,
+// segment is also the unit of the TMEM double buffer.  The wide shape never restarts, nor do twin products in
+// the single one: they serve outputs that are the sum itself, rounded to bf16, with K up to kWideK (up to
+// the caller's own limit where it gives pick_shape() one: 32768 for dX of the gated feed-forward).  A step loses up to 2^-22
+// of the running sum, so 1024 steps lose up to 2^-12 of it and 2048 2^-11, next to the rounding's half step of 2^-8 of
+// the value; where terms cancel, the loss is one of the running sum and not of the value.  They do not serve logits,
 // whose exponentials turn a bias of the sum into one of the result.
 // Every wait is bounded; the failure path is that of the Gram kernel: the first waiter that gives up
 // records LOCA_ERR_TIMEOUT and raises the launch's abort flag, every role stops at its own point,
