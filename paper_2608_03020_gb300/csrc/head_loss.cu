@@ -44,8 +44,8 @@
 // d = 2048, V = 49152: 1.06 ms (1.55 PFLOP/s; the rest is the epilogue's exponentials and the clock under
 // load); 37 tokens 48 us (201 MB of W: 4.2 TB/s for the call, 4.8 in k_gemm_pair).  Loss and dH of 1531
 // tokens at d = 5120, V = 151936: 4.5 ms for 7.15 TFLOP (1.59 PFLOP/s).  Up to 128 tokens each gradient
-// reads W again (8 tokens at d = 4648, V = 70557: 370 us for three reads of 656 MB).  Distillation: 37 positions there 51 us,
-// 4096 of which a quarter is masked, with both gradients, 1.66 to 1.70 ms.
+// reads W again (8 tokens at d = 4648, V = 70557: 370 us for three reads of 656 MB).  Distillation at d = 2048, V = 49152:
+// 37 positions 51 us, 4096 of which a quarter is masked, with both gradients, 1.67 to 1.72 ms.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 

@@ -17,10 +17,12 @@
 //               ks warps' sums meet in shared memory, in order, with the low-rank term of each token's adapter
 //               (U in fp32 from k_adapter_tokens); one rounding
 //   k_q4_tiles  more than 16 tokens: see there
-// Bound of k_q4: the instructions that make operands of codes (44 of some 80 for 64 k of 16 rows; 60 to 70 % of the issue
-// slots), next to the read of the codes and scales.  One token at 28672 x 8192 25.8 us (4.7 TB/s), 3 tokens at
-// 151931 x 2048 with groups of 32 48 us (4.2 TB/s), at 20480 x 5120 16.5 us for one token and 20 for eight (2.7 TB/s),
-// 16 tokens at 14336 x 3584 14.4 us.
+// Bound of k_q4, next to the read of the codes and scales: with one token, or groups of 32, the instructions that make
+// operands of codes (44 of some 80 for 64 k of 16 rows; 65 and 73 % of the issue slots); with more tokens nothing alone (8 at
+// 20480 x 5120: 52 % of the issue slots, 58 % of L1's data path, which a warp's X takes 2 KB a span for 1 KB of codes; two
+// fifths of the warps wait for loads).  One token at 28672 x 8192 25.6 us (4.7 TB/s), 3 tokens at 151931 x 2048 with groups
+// of 32 45.5 us (4.4 TB/s), 8 at 20480 x 5120 with groups of 64 18.7 us (3.0 TB/s), with adapters of rank 32 23.7; 16
+// tokens at 14336 x 3584 14.4 us.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
@@ -34,7 +36,7 @@ using namespace tc;
 constexpr int kThreads = 256;
 constexpr int kWarps = kThreads / 32;
 constexpr int kMaxSmem = 98304;
-constexpr int kTokensByWarps = 16;  // (above: 20 tokens with 16 adapters at 3584 x 3584 14.4 us by warps, 11.6 in tiles)
+constexpr int kTokensByWarps = 16;  // (above: 20 tokens with adapters of rank 16 at 3584 x 3584 14.4 us by warps, 10.8 in tiles)
 
 __host__ __device__ inline int64_t div_up(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
@@ -108,7 +110,6 @@ struct Q4Geo {
   const uint8_t* scales;
   const uint8_t* zeros;  // or null: 8
   int f32;
-  int shift;             // log2(group)
   int64_t o, d;
   int64_t tiles;
   int spans, groups;
@@ -127,11 +128,12 @@ __device__ __forceinline__ void mma_16816(float (&c)[4], const uint32_t (&a)[4],
       : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
-// Two codes (bits s .. s + 3 of both halves of w) less their row's zero: 128 + q has q in the last bits of its
-// bf16 pattern 0x4300 | q, and so has 128 + z; their difference is exact.
+// Two codes (bits s .. s + 3 of both halves of w) less their row's zero, by the published way of turning small integers into
+// floating point through the bit pattern: 128 + q has q in the last bits of its bf16 pattern 0x4300 | q, and so has
+// 128 + z; their difference is exact.
 template <int kShift>
 __device__ __forceinline__ uint32_t two_codes(uint32_t w, __nv_bfloat162 zero) {
-  uint32_t q;  // (codes & mask) | pattern: one instruction, where the compiler made two (36 instead of 52 of the integer pipe for 64 k)
+  uint32_t q;  // (codes & mask) | pattern in one instruction (one token at 28672 x 8192 31 us in two, 25.8 in one)
   asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(q) : "r"(w >> kShift), "n"(0x000f000f), "r"(0x43004300u));
   const __nv_bfloat162 v = __hsub2(*reinterpret_cast<const __nv_bfloat162*>(&q), zero);
   return *reinterpret_cast<const uint32_t*>(&v);
@@ -268,6 +270,8 @@ __global__ void __launch_bounds__(kThreads, resident(NT)) k_q4(const __grid_cons
                            ? __ldg(reinterpret_cast<const uint4*>(x[n] + 128 * i) + 4 * q)
                            : make_uint4(0, 0, 0, 0);
         };
+        // (twice the same: without a condition at each load 18.7 us where one loop for both took 19.1, 8 tokens at 20480 x
+        // 5120, and 41.6 us for 43.1, one at 151931 x 2048)
         if (full) {
 #pragma unroll
           for (int q = 0; q < 4; ++q) load_x(q);
@@ -825,7 +829,6 @@ cudaError_t launch_q4_apply(const void* X, int64_t ldx, int64_t N, int64_t d, co
   g.scales = b + p.scales;
   g.zeros = zeros ? b + p.zeros : nullptr;
   g.f32 = scale_dtype == LOCA_F32;
-  g.shift = group == 32 ? 5 : group == 64 ? 6 : 7;
   g.o = o;
   g.d = d;
   g.tiles = p.tiles;
