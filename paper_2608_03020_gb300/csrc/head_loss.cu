@@ -45,7 +45,7 @@
 // load); 37 tokens 48 us (201 MB of W: 4.2 TB/s for the call, 4.8 in k_gemm_pair).  Loss and dH of 1531
 // tokens at d = 5120, V = 151936: 4.5 ms for 7.15 TFLOP (1.59 PFLOP/s).  Up to 128 tokens each gradient
 // reads W again (8 tokens at d = 4648, V = 70557: 370 us for three reads of 656 MB).  Distillation at d = 2048, V = 49152:
-// 37 positions 51 us, 4096 of which a quarter is masked, with both gradients, 1.67 to 1.72 ms.
+// 37 positions 51 us, 4096 of which a quarter is masked, with both gradients, 1.65 to 1.71 ms.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
